@@ -349,6 +349,102 @@ kl_status kl_debug_set_jitter(kl_handle* h, uint32_t seed, uint32_t max_ns);
  * step = 0xffffffff only queries.  wrap_at may be NULL. */
 kl_status kl_debug_set_step(kl_handle* h, uint32_t step, uint32_t* wrap_at);
 
+/* ---- Paged key-value cache: operators without a handle.
+ *
+ * A cache of pages serves sequences of very different lengths from one pool (and lets several share the pages of a
+ * common prefix); e4m3 rows halve the bytes of the part of a decode step that grows with the context.  The paper's
+ * decoder reads one contiguous bf16 cache (its Table 1); these operators are what a serving program needs next to it,
+ * and kl_decode_step_paged runs a whole batched step on such a cache.
+ *
+ * All of them work on the current device, launch on `stream`, allocate nothing and synchronise nothing.  positions_d
+ * follows kl_decode_step: positions_d[s] is the index of the newest token of sequence s, attention covers positions
+ * 0 .. positions_d[s]; a negative entry is an empty slot of the batch.  Position p of a sequence lies in row
+ * p % page_size of page page_table[s][p / page_size].
+ *
+ * status_d: a device word of the caller (zero it first), or NULL.  A page number outside [0, n_pages), a position behind
+ * the page table or a broken row_starts array is never followed: the row or page is left out and the word becomes
+ * KL_ERR_OUT_OF_RANGE, after which the call's results are undefined.  Like the handle's status word it is sticky: while
+ * it is not zero further calls with it do nothing. */
+enum { KL_KV_BF16 = 0, KL_KV_E4M3 = 1 };   /* kl_paged_cache.kv_type */
+enum { KL_F32 = 0, KL_BF16 = 1 };          /* element types of rows, queries and outputs */
+
+typedef struct {
+    uint32_t n_kv_heads;
+    uint32_t head_dim;     /* 64, 128 or 256 */
+    uint32_t page_size;    /* rows of a page: a multiple of 4, 4 .. 1024 */
+    uint32_t n_pages;      /* pages of the pool */
+    uint32_t kv_type;      /* KL_KV_BF16; KL_KV_E4M3: e4m3 codes, every row of every head with a power-of-two scale */
+    /* Strides of k_d and v_d in elements; the head_dim elements of a row are contiguous.  Each a multiple of 16 bytes,
+     * not negative; [page][head][row] and [page][row][head] orders are both just strides. */
+    int64_t page_stride, head_stride, row_stride;
+    void *k_d, *v_d;       /* 16-byte aligned; NULL where a call does not read rows (kl_paged_select) */
+    /* KL_KV_E4M3: [n_pages][n_kv_heads][page_size] bytes, 16-byte aligned: byte e stands for the scale 2^(e - 127) */
+    uint8_t *k_exp_d, *v_exp_d;
+    /* Optional: bf16 [n_pages][n_kv_heads][2][head_dim], 16-byte aligned: per page, head and column the smallest and the
+     * largest key the page holds (the values the cache stands for; NaN does not count).  kl_paged_append keeps them,
+     * kl_paged_select reads them. */
+    void* bounds_d;
+} kl_paged_cache;
+
+typedef struct {
+    const int32_t* positions_d;    /* [n_seqs] */
+    const int32_t* page_table_d;   /* [n_seqs][table_stride]; entries behind a sequence's last page are not read */
+    int64_t table_stride;
+    uint32_t table_pages;          /* entries of a row that may be used (<= table_stride); table_pages * page_size < 2^31 */
+    uint32_t n_seqs;               /* 0: the call does nothing */
+} kl_paged_seqs;
+
+/* Writes new rows into the cache.  Rows row_starts_d[s] .. row_starts_d[s + 1] - 1 of k_rows_d / v_rows_d go to positions
+ * positions_d[s], positions_d[s] + 1, ... of sequence s (row_starts_d: [n_seqs + 1], ascending, at most n_rows; rows
+ * behind row_starts_d[n_seqs] are ignored); row_starts_d == NULL: one row per sequence (n_rows == n_seqs), at
+ * positions_d[s] -- a decode step's append.  A row is [n_kv_heads][head_dim] of row_type (KL_F32 or KL_BF16), rows
+ * k_row_stride / v_row_stride elements apart (16-byte alignment as above), keys already rotated.
+ * KL_KV_BF16: rounded to nearest even.  KL_KV_E4M3: per row and head, e = the smallest integer >= -127 with
+ * (largest finite magnitude) <= 448 * 2^e, scale byte e + 127, codes x / 2^e rounded to nearest even (infinities
+ * saturate, NaN stays NaN).  The scale is a power of two: e4m3 is itself a floating-point format, a finer scale would
+ * gain no precision, and this one makes quantising, reading back and the page bounds exact.
+ * bounds_d (if any): a row 0 of a page starts the page's bounds anew, other rows widen them; overwriting a row in the
+ * middle of a page leaves bounds that still hold, perhaps wider than need be.
+ * Two sequences of a call must not write the same page. */
+kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                          const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                          int32_t* status_d, void* stream);
+
+/* The way back: the rows that kl_paged_append with the same arguments would write are copied out of the cache, as bf16
+ * (exact for both cache types) or fp32.  Output rows that belong to no sequence or to an empty slot are left as they were. */
+kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                        void* k_out_d, void* v_out_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                        int32_t* status_d, void* stream);
+
+/* Bytes of workspace kl_paged_select and kl_paged_attention need for batches of up to n_seqs sequences with page tables
+ * of up to table_pages entries (256-byte aligned, need not be cleared; calls that may run at the same time -- graphs
+ * captured from them included -- need workspaces of their own). */
+kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes);
+
+/* Chooses, for the newest token of every sequence and every kv head, the pages worth attending to.  q_d: [n_seqs]
+ * [n_q_heads][head_dim] of q_type, rows q_row_stride elements apart; query heads h * G .. h * G + G - 1 share kv head h.
+ * The score of a page is the largest, over these G heads, of sum_d max(q_d * lo_d, q_d * hi_d) -- no key of the page has a
+ * larger product with q -- summed in 64 bits and rounded to 32.  The first keep_first and the last keep_last pages of a
+ * sequence are always chosen, then the best scores until n_select (>= keep_first + keep_last, >= 1) are (the lower page
+ * first among equals, NaN last).  selected_d: [n_seqs][n_kv_heads][n_select] logical page numbers in ascending order,
+ * filled up with -1. */
+kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
+                          uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
+                          void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream);
+
+/* Attention of one new token per sequence: out[s][h] = sum_p softmax_p(scale * q[s][h] . k_p) v_p over the positions p of
+ * sequence s -- all of them (window == 0), the last `window`, or, when selected_d is given, those of the listed pages
+ * (kl_paged_select's output, or any [n_seqs][n_kv_heads][n_select] list of distinct logical pages; of a sequence with
+ * fewer than n_select pages only the first entries, one per page, are looked at; a negative entry is no page).  A window
+ * and a selection combine.  q and out: [n_seqs][n_q_heads][head_dim] of q_type; scale <= 0: 1 / sqrt(head_dim).  lse_d
+ * (optional): fp32 [n_seqs][n_q_heads], the natural logarithm of the softmax's denominator sum_p exp(scale * q . k_p), which is
+ * what joining the results of several caches needs.  A sequence without positions to attend to gets zeros, and -inf.
+ * n_q_heads is a multiple of n_kv_heads, any group size. */
+kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,
+                             int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
+                             const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
+                             int32_t* status_d, void* stream);
+
 const char* kl_status_string(kl_status s);
 
 /* Releases host-side state only (the arenas belong to the caller). */

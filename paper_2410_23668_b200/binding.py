@@ -28,6 +28,10 @@ TENSOR_IDS = {"embed": 0, "wq": 1, "wk": 2, "wv": 3, "wo": 4, "wgate": 5, "wup":
               "norm1": 8, "norm2": 9, "norm_f": 10, "lm_head": 11, "bq": 12, "bk": 13, "bv": 14, "router": 15}
 KL_FLAG_QKV_BIAS = 1
 KL_FLAG_NO_STASH = 2
+KL_KV_BF16 = 0
+KL_KV_E4M3 = 1
+KL_F32 = 0
+KL_BF16 = 1
 
 # every symbol include/kl.h declares
 EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_bytes", "kl_set_mode", "kl_decode_step",
@@ -35,7 +39,8 @@ EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_by
            "kl_set_wait_limit_ns", "kl_debug_skip_signal_once", "kl_status_string", "kl_destroy", "kl_profile_enable",
            "kl_profile_read", "kl_set_trace", "kl_set_tensor_core_attention", "kl_stash_mode", "kl_argmax_advance_static", "kl_set_batched_path",
            "kl_set_dependent_launch", "kl_decode_greedy_host", "kl_decode_greedy", "kl_decode_greedy_tokens",
-           "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights")
+           "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights",
+           "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention")
 
 
 class ModelDesc(C.Structure):
@@ -43,6 +48,17 @@ class ModelDesc(C.Structure):
                 ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("ffn", C.c_uint32), ("vocab", C.c_uint32),
                 ("rms_eps", C.c_float), ("rope_theta", C.c_float), ("max_batch", C.c_uint32),
                 ("max_ctx", C.c_uint32), ("flags", C.c_uint32), ("n_experts", C.c_uint32), ("top_k", C.c_uint32)]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_size", C.c_uint32), ("n_pages", C.c_uint32),
+                ("kv_type", C.c_uint32), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("k_d", C.c_void_p), ("v_d", C.c_void_p), ("k_exp_d", C.c_void_p), ("v_exp_d", C.c_void_p), ("bounds_d", C.c_void_p)]
+
+
+class PagedSeqs(C.Structure):
+    _fields_ = [("positions_d", C.c_void_p), ("page_table_d", C.c_void_p), ("table_stride", C.c_int64), ("table_pages", C.c_uint32),
+                ("n_seqs", C.c_uint32)]
 
 
 _lib = None
@@ -114,6 +130,17 @@ def lib():
     l.kl_set_batched_path.restype = i32
     l.kl_set_dependent_launch.argtypes = [vp, C.c_int]
     l.kl_set_dependent_launch.restype = i32
+    pc, ps, i64 = C.POINTER(PagedCacheDesc), C.POINTER(PagedSeqs), C.c_int64
+    l.kl_paged_append.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp]
+    l.kl_paged_append.restype = i32
+    l.kl_paged_read.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp]
+    l.kl_paged_read.restype = i32
+    l.kl_paged_workspace_bytes.argtypes = [pc, u32, u32, u32, C.POINTER(C.c_size_t)]
+    l.kl_paged_workspace_bytes.restype = i32
+    l.kl_paged_select.argtypes = [pc, ps, vp, C.c_int, i64, u32, u32, u32, u32, vp, vp, C.c_size_t, vp, vp]
+    l.kl_paged_select.restype = i32
+    l.kl_paged_attention.argtypes = [pc, ps, vp, vp, C.c_int, i64, i64, u32, C.c_float, u32, vp, u32, vp, vp, C.c_size_t, vp, vp]
+    l.kl_paged_attention.restype = i32
     l.kl_status_string.argtypes = [i32]
     l.kl_status_string.restype = C.c_char_p
     l.kl_destroy.argtypes = [vp]
@@ -162,6 +189,158 @@ def kl_argmax_advance_static(logits_d, tokens_d, positions_d, batch: int, stream
     """Sampling block without a handle: scratch in a fixed array inside the library, nothing is allocated."""
     _check(lib().kl_argmax_advance_static(_ptr(logits_d), int(logits_d.shape[-1]), _ptr(tokens_d), _ptr(positions_d), batch,
                                           _stream_ptr(stream)), "kl_argmax_advance_static")
+
+
+class PagedCache:
+    """A paged key-value cache over tensors of the caller: k and v [n_pages, n_kv_heads, page_size, head_dim], bf16, or
+    e4m3 codes (torch.float8_e4m3fn or uint8) with k_exp and v_exp uint8 [n_pages, n_kv_heads, page_size]; bounds
+    (optional) bf16 [n_pages, n_kv_heads, 2, head_dim].  k and v may be permuted views, e.g. of a [n_pages, page_size,
+    n_kv_heads, head_dim] tensor, as long as a row is contiguous and both have the same strides.  For page selection alone
+    k and v may be None (then page_size and kv_type say what bounds does not).  The tensors must stay alive and in place."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None, bounds=None, page_size=None, kv_type=None):
+        import torch
+        self.tensors = (k, v, k_exp, v_exp, bounds)
+        where = "PagedCache"
+        d = PagedCacheDesc()
+        if k is None:
+            _need(v is None and bounds is not None and page_size is not None and kv_type is not None, where)
+            d.n_pages, d.n_kv_heads, _, d.head_dim = bounds.shape
+            d.page_size, d.kv_type = page_size, kv_type
+        else:
+            _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, where)
+            d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
+            d.page_stride, d.head_stride, d.row_stride = k.stride(0), k.stride(1), k.stride(2)
+            d.kv_type = KL_KV_BF16 if k.dtype == torch.bfloat16 else KL_KV_E4M3
+            _need(k.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn), where)
+            if d.kv_type == KL_KV_E4M3:
+                for e in (k_exp, v_exp):
+                    _need(e is not None and e.dtype == torch.uint8 and e.shape == k.shape[:3] and e.is_contiguous(), where)
+        if bounds is not None:
+            _need(bounds.dtype == torch.bfloat16 and bounds.is_contiguous() and
+                  tuple(bounds.shape) == (d.n_pages, d.n_kv_heads, 2, d.head_dim), where)
+        d.k_d, d.v_d, d.k_exp_d, d.v_exp_d, d.bounds_d = (_ptr(t) or None for t in self.tensors)
+        self.device = (bounds if k is None else k).device
+        _need(all(t is None or t.device == self.device for t in self.tensors), where)
+        self.desc = d
+
+    @classmethod
+    def allocate(cls, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, kv_type: int = KL_KV_BF16, bounds: bool = False,
+                 device="cuda"):
+        """A zeroed pool of its own."""
+        import torch
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        dt = torch.bfloat16 if kv_type == KL_KV_BF16 else torch.float8_e4m3fn
+        k, v = torch.zeros(shape, dtype=dt, device=device), torch.zeros(shape, dtype=dt, device=device)
+        ke = ve = b = None
+        if kv_type == KL_KV_E4M3:
+            ke, ve = (torch.zeros(shape[:3], dtype=torch.uint8, device=device) for _ in range(2))
+        if bounds:
+            b = torch.zeros(n_pages, n_kv_heads, 2, head_dim, dtype=torch.bfloat16, device=device)
+        return cls(k, v, ke, ve, b)
+
+
+def _need(ok: bool, where: str) -> None:
+    if not ok:
+        raise KlError(KL_ERR_INVALID_ARG, where)
+
+
+def _paged_seqs(cache: PagedCache, positions, page_table, where: str) -> PagedSeqs:
+    import torch
+    _need(positions.dtype == page_table.dtype == torch.int32 and page_table.dim() == 2 and positions.is_contiguous() and
+          page_table.stride(1) == 1 and positions.shape == page_table.shape[:1], where)
+    n, pages = page_table.shape
+    return PagedSeqs(positions.data_ptr(), page_table.data_ptr(), max(page_table.stride(0), pages) if n <= 1 else page_table.stride(0), pages, n)
+
+
+def _row_type(t, where: str) -> int:
+    import torch
+    _need(t.dtype in (torch.float32, torch.bfloat16), where)
+    return KL_F32 if t.dtype == torch.float32 else KL_BF16
+
+
+def _on_device(cache: PagedCache, where: str, *tensors) -> None:
+    """The library launches on the current device: everything has to live there."""
+    import torch
+    dev = cache.device
+    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device() and all(t is None or t.device == dev for t in tensors), where)
+
+
+def _paged_rows(fn: str, cache: PagedCache, k, v, positions, page_table, row_starts, status, stream) -> None:
+    import torch
+    _on_device(cache, fn, k, v, positions, page_table, row_starts, status)
+    d = cache.desc
+    _need(k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and tuple(k.shape[1:]) == (d.n_kv_heads, d.head_dim), fn)
+    for t in (k, v):
+        _need(t.stride(2) == 1 and (t.stride(1) == d.head_dim or d.n_kv_heads == 1), fn)
+    n = k.shape[0]
+    if row_starts is not None:
+        _need(row_starts.dtype == torch.int32 and row_starts.is_contiguous() and row_starts.numel() == positions.numel() + 1, fn)
+    seqs = _paged_seqs(cache, positions, page_table, fn)
+    _check(getattr(lib(), fn)(C.byref(d), C.byref(seqs), _ptr(row_starts), n, _ptr(k), _ptr(v), _row_type(k, fn), k.stride(0), v.stride(0),
+                              _ptr(status), _stream_ptr(stream)), fn)
+
+
+def kl_paged_append(cache: PagedCache, k_rows, v_rows, positions, page_table, row_starts=None, status=None, stream=None) -> None:
+    """New rows [n_rows, n_kv_heads, head_dim] (bf16 or fp32; rows may be strided) into the pages; positions int32 [n_seqs],
+    page_table int32 [n_seqs, pages], row_starts int32 [n_seqs + 1] or None (one row per sequence)."""
+    _paged_rows("kl_paged_append", cache, k_rows, v_rows, positions, page_table, row_starts, status, stream)
+
+
+def kl_paged_read(cache: PagedCache, k_out, v_out, positions, page_table, row_starts=None, status=None, stream=None) -> None:
+    """The rows that kl_paged_append with the same arguments would write, copied out."""
+    _paged_rows("kl_paged_read", cache, k_out, v_out, positions, page_table, row_starts, status, stream)
+
+
+def kl_paged_workspace_bytes(cache: PagedCache, n_q_heads: int, n_seqs: int, table_pages: int) -> int:
+    b = C.c_size_t()
+    _check(lib().kl_paged_workspace_bytes(C.byref(cache.desc), n_q_heads, n_seqs, table_pages, C.byref(b)), "kl_paged_workspace_bytes")
+    return b.value
+
+
+def _paged_queries(cache: PagedCache, q, positions, where: str) -> int:
+    d = cache.desc
+    _need(q.dim() == 3 and q.shape[0] == positions.numel() and q.shape[2] == d.head_dim and q.stride(2) == 1 and
+          (q.stride(1) == d.head_dim or q.shape[1] == 1), where)
+    return _row_type(q, where)
+
+
+def kl_paged_select(cache: PagedCache, q, positions, page_table, selected, workspace, keep_first: int = 1, keep_last: int = 1, status=None,
+                    stream=None) -> None:
+    """q [n_seqs, n_q_heads, head_dim] -> selected int32 [n_seqs, n_kv_heads, n_select]."""
+    import torch
+    fn = "kl_paged_select"
+    _on_device(cache, fn, q, positions, page_table, selected, workspace, status)
+    t = _paged_queries(cache, q, positions, fn)
+    n = positions.numel()
+    _need(selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 3 and
+          tuple(selected.shape[:2]) == (n, cache.desc.n_kv_heads) and workspace.dtype == torch.uint8 and workspace.is_contiguous() and
+          keep_first >= 0 and keep_last >= 0, fn)
+    seqs = _paged_seqs(cache, positions, page_table, fn)
+    _check(lib().kl_paged_select(C.byref(cache.desc), C.byref(seqs), _ptr(q), t, q.stride(0), q.shape[1], keep_first, keep_last,
+                                 selected.shape[2], _ptr(selected), _ptr(workspace), workspace.numel(), _ptr(status), _stream_ptr(stream)), fn)
+
+
+def kl_paged_attention(cache: PagedCache, q, out, positions, page_table, workspace, scale: float = 0.0, window: int = 0, selected=None, lse=None,
+                       status=None, stream=None) -> None:
+    """q, out [n_seqs, n_q_heads, head_dim] of one type; selected int32 [n_seqs, n_kv_heads, n_select]; lse fp32 [n_seqs, n_q_heads]."""
+    import torch
+    fn = "kl_paged_attention"
+    _on_device(cache, fn, q, out, positions, page_table, workspace, selected, lse, status)
+    t = _paged_queries(cache, q, positions, fn)
+    n = positions.numel()
+    _need(_paged_queries(cache, out, positions, fn) == t and out.shape == q.shape and workspace.dtype == torch.uint8 and
+          workspace.is_contiguous() and window >= 0, fn)
+    k = 0
+    if selected is not None:
+        _need(selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 3 and
+              tuple(selected.shape[:2]) == (n, cache.desc.n_kv_heads) and selected.shape[2] > 0, fn)
+        k = selected.shape[2]
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2]), fn)
+    seqs = _paged_seqs(cache, positions, page_table, fn)
+    _check(lib().kl_paged_attention(C.byref(cache.desc), C.byref(seqs), _ptr(q), _ptr(out), t, q.stride(0), out.stride(0), q.shape[1], scale, window,
+                                    _ptr(selected), k, _ptr(lse), _ptr(workspace), workspace.numel(), _ptr(status), _stream_ptr(stream)), fn)
 
 
 class Decoder:

@@ -9,10 +9,11 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libkl.so"
-SOURCES = [CSRC / "kl.cu"]
-HEADERS = [CSRC / "kl_device.cuh", CSRC / "kl_attention_tc.cuh", CSRC / "kl_batched.cuh", CSRC / "kl_bloop.cuh", PKG.parent / "include" / "kl.h"]
+SOURCES = [CSRC / "kl.cu", CSRC / "kl_paged.cu"]
+HEADERS = [CSRC / "kl_device.cuh", CSRC / "kl_attention_tc.cuh", CSRC / "kl_batched.cuh", CSRC / "kl_bloop.cuh", CSRC / "kl_paged.cuh",
+           PKG.parent / "include" / "kl.h"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "--shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
 
 def needs_build() -> bool:
@@ -28,11 +29,21 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB.with_suffix(f".so.tmp{os.getpid()}")
     extra = os.environ.get("KL_NVCC_FLAGS", "").split()   # e.g. -DKL_MAX_KP=4096 for tuning experiments
-    cmd = [nvcc, *NVCC_FLAGS, *extra, "-o", str(tmp), *map(str, SOURCES)]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
+    # the sources are compiled side by side and linked; no device code crosses from one to the other
+    objs = [tmp.with_name(f"{f.stem}.{os.getpid()}.o") for f in SOURCES]
+    jobs = [subprocess.Popen([nvcc, *NVCC_FLAGS, *extra, "-c", "-o", str(o), str(f)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+                             text=True) for f, o in zip(SOURCES, objs)]
+    said = [j.communicate()[0] for j in jobs]
+    ok = all(j.returncode == 0 for j in jobs)
+    if ok:
+        res = subprocess.run([nvcc, "--shared", "-o", str(tmp), *map(str, objs)], capture_output=True, text=True)
+        said.append(res.stdout + res.stderr)
+        ok = res.returncode == 0
+    for o in objs:
+        o.unlink(missing_ok=True)
+    if verbose or not ok:
+        sys.stderr.write("".join(said))
+    if not ok:
         raise RuntimeError("nvcc failed building libkl.so")
     os.replace(tmp, LIB)
     return LIB

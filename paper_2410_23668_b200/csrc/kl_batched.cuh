@@ -136,14 +136,6 @@ __device__ __forceinline__ void tma_tensor_5d_g2s(uint32_t dst, const void* tmap
         : "memory");
 }
 
-// Programmatic dependent launch: the kernels of a step are launched with programmatic stream serialisation, so a
-// kernel may start while its predecessor still runs.  griddep_wait() returns when the predecessor has completed and
-// its writes are visible -- everything a kernel reads from or writes to buffers shared with other kernels comes after
-// it; before it a kernel only sets itself up and prefetches data no kernel of the step writes (weights, cache rows of
-// earlier steps).  griddep_launch() lets the successor start its own set-up.
-__device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // Shared-memory matrix descriptor of a K-major bf16 tile stored as rows of 128 bytes with the 128-byte swizzle
 // (what TMA writes with CU_TENSOR_MAP_SWIZZLE_128B; the tile starts on a 1024-byte boundary): start address / 16 in
 // bits 0..13, leading byte offset (unused for this layout) 1 in bits 16..29, stride between groups of eight rows

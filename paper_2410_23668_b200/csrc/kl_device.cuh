@@ -138,6 +138,14 @@ struct StepCtx {
 
 // ------------------------------------------------------------------------------------------------ PTX
 
+// Programmatic dependent launch: the kernels of a step are launched with programmatic stream serialisation, so a
+// kernel may start while its predecessor still runs.  griddep_wait() returns when the predecessor has completed and
+// its writes are visible -- everything a kernel reads from or writes to buffers shared with other kernels comes after
+// it; before it a kernel only sets itself up and prefetches data no kernel of the step writes (weights, cache rows of
+// earlier steps).  griddep_launch() lets the successor start its own set-up.
+__device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ uint64_t globaltimer_ns() {

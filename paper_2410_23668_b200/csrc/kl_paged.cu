@@ -1,0 +1,208 @@
+// Host side of the paged key-value cache operators (contracts in include/kl.h, kernels in kl_paged.cuh).
+#include "kl_paged.cuh"
+
+#include <math.h>
+#include <string.h>
+
+#include <utility>
+
+#include "../../include/kl.h"
+
+using namespace kl;
+
+namespace {
+
+// Launch with programmatic stream serialisation (see griddep_wait): set-up overlaps the end of the stream's previous kernel.
+template <typename... KArgs, typename... Args>
+kl_status launch(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, void* stream, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(std::forward<Args>(args))...) == cudaSuccess ? KL_OK : KL_ERR_CUDA;
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline uint32_t elem(int type) { return type == KL_F32 ? 4u : 2u; }
+
+// The descriptor's own consistency (rows: whether the call touches k_d, v_d and the scales).
+kl_status check_cache(const kl_paged_cache* c, bool rows) {
+    if (!c) return KL_ERR_INVALID_ARG;
+    if (!c->n_kv_heads || (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (c->page_size < 4 || c->page_size > 1024 || c->page_size % 4) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (c->n_kv_heads > 65535u || c->n_pages > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (c->kv_type != KL_KV_BF16 && c->kv_type != KL_KV_E4M3) return KL_ERR_INVALID_ARG;
+    if (!aligned16(c->bounds_d)) return KL_ERR_INVALID_ARG;
+    if (!rows) return KL_OK;
+    const int64_t bytes = c->kv_type == KL_KV_BF16 ? 2 : 1;
+    const int64_t st[3] = {c->page_stride, c->head_stride, c->row_stride};
+    for (int64_t x : st)
+        if (x < 0 || x > (INT64_MAX >> 34) || (x * bytes) % 16) return KL_ERR_INVALID_ARG;
+    if (!c->k_d || !c->v_d || !aligned16(c->k_d) || !aligned16(c->v_d)) return KL_ERR_INVALID_ARG;
+    if (c->kv_type == KL_KV_E4M3 && (!c->k_exp_d || !c->v_exp_d || !aligned16(c->k_exp_d) || !aligned16(c->v_exp_d))) return KL_ERR_INVALID_ARG;
+    return KL_OK;
+}
+kl_status check_seqs(const kl_paged_cache* c, const kl_paged_seqs* s) {
+    if (!s) return KL_ERR_INVALID_ARG;
+    if (s->n_seqs == 0) return KL_OK;
+    if (!s->positions_d || !s->page_table_d) return KL_ERR_INVALID_ARG;
+    if (!s->table_pages || s->table_stride < (int64_t)s->table_pages || s->table_stride > (INT64_MAX >> 34)) return KL_ERR_INVALID_ARG;
+    if ((uint64_t)s->table_pages * c->page_size > 0x7fffffffull || s->n_seqs > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
+    return KL_OK;
+}
+
+PagedView view(const kl_paged_cache* c, const kl_paged_seqs* s, int32_t* status_d) {
+    PagedView v;
+    const int64_t bytes = c->kv_type == KL_KV_BF16 ? 2 : 1;
+    v.k = (uint8_t*)c->k_d; v.v = (uint8_t*)c->v_d;
+    v.ke = c->k_exp_d; v.ve = c->v_exp_d;
+    v.bounds = (__nv_bfloat16*)c->bounds_d;
+    v.page_b = c->page_stride * bytes; v.head_b = c->head_stride * bytes; v.row_b = c->row_stride * bytes;
+    v.nkv = c->n_kv_heads; v.hd = c->head_dim; v.page = c->page_size; v.n_pages = c->n_pages; v.fp8 = c->kv_type == KL_KV_E4M3;
+    v.positions = s->positions_d; v.table = s->page_table_d; v.table_stride = s->table_stride;
+    v.table_pages = s->table_pages; v.n_seqs = s->n_seqs;
+    v.status = status_d;
+    return v;
+}
+
+kl_status check_rows(const kl_paged_cache* c, const kl_paged_seqs* s, const int32_t* row_starts_d, uint32_t n_rows, const void* k,
+                     const void* v, int type, int64_t ks, int64_t vs) {
+    if (type != KL_F32 && type != KL_BF16) return KL_ERR_INVALID_ARG;
+    if (!row_starts_d && n_rows != s->n_seqs) return KL_ERR_INVALID_ARG;
+    if (n_rows > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return KL_ERR_INVALID_ARG;
+    const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
+    if ((n_rows > 1 && (ks < width || vs < width)) || ks < 0 || vs < 0 || ks > (INT64_MAX >> 34) || vs > (INT64_MAX >> 34)) return KL_ERR_INVALID_ARG;
+    if ((ks * elem(type)) % 16 || (vs * elem(type)) % 16) return KL_ERR_INVALID_ARG;
+    return KL_OK;
+}
+
+PagedRows rows_of(const int32_t* row_starts_d, uint32_t n_rows, const void* k, const void* v, int type, int64_t ks, int64_t vs) {
+    PagedRows r;
+    r.row_starts = row_starts_d;
+    r.n_rows = n_rows;
+    r.k = (uint8_t*)const_cast<void*>(k);
+    r.v = (uint8_t*)const_cast<void*>(v);
+    r.k_stride = ks * elem(type);
+    r.v_stride = vs * elem(type);
+    return r;
+}
+
+size_t score_bytes(const kl_paged_cache* c, uint64_t n_seqs, uint64_t table_pages) {
+    return (size_t)((n_seqs * c->n_kv_heads * table_pages * 4 + 255) / 256 * 256);
+}
+
+kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_seqs) {
+    if (!q || (type != KL_F32 && type != KL_BF16)) return KL_ERR_INVALID_ARG;
+    if (!n_q_heads || n_q_heads % c->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
+    if ((uint64_t)n_q_heads * c->head_dim > 0x7fffffffull || n_q_heads > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (stride < 0 || (n_seqs > 1 && stride < (int64_t)n_q_heads * c->head_dim) || stride > (INT64_MAX >> 34)) return KL_ERR_INVALID_ARG;
+    if (!aligned16(q) || (stride * elem(type)) % 16) return KL_ERR_INVALID_ARG;
+    return KL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                          const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                          int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
+    if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
+    const uint64_t units = row_starts_d ? (uint64_t)n_rows / cache->page_size + 2ull * seqs->n_seqs : seqs->n_seqs;
+    if (units > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;
+    const PagedView v = view(cache, seqs, status_d);
+    const PagedRows r = rows_of(row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride);
+    const size_t smem = cache->bounds_d ? (size_t)(PG_THREADS / (cache->head_dim / 8) / 2) * 2 * cache->head_dim * 4 : 0;
+    const dim3 grid((unsigned)units, cache->n_kv_heads);
+    return row_type == KL_F32 ? launch(kl_paged_append_kernel<float>, grid, PG_THREADS, smem, stream, v, r)
+                              : launch(kl_paged_append_kernel<__nv_bfloat16>, grid, PG_THREADS, smem, stream, v, r);
+}
+
+kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                        void* k_out_d, void* v_out_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                        int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
+    if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
+    const PagedView v = view(cache, seqs, status_d);
+    const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
+    return row_type == KL_F32 ? launch(kl_paged_read_kernel<float>, dim3(n_rows), PG_THREADS, 0, stream, v, r)
+                              : launch(kl_paged_read_kernel<__nv_bfloat16>, dim3(n_rows), PG_THREADS, 0, stream, v, r);
+}
+
+kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes) {
+    if (!bytes) return KL_ERR_INVALID_ARG;
+    const kl_status rc = check_cache(cache, false);
+    if (rc != KL_OK) return rc;
+    if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
+    *bytes = score_bytes(cache, n_seqs, table_pages);
+    return KL_OK;
+}
+
+kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
+                          uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
+                          void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, false)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0) return KL_OK;
+    if ((rc = check_queries(cache, q_d, q_type, q_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
+    if (!cache->bounds_d || !selected_d) return KL_ERR_INVALID_ARG;
+    if (!n_select || (uint64_t)keep_first + keep_last > n_select || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
+    if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < score_bytes(cache, seqs->n_seqs, seqs->table_pages)) return KL_ERR_INVALID_ARG;
+    if (seqs->n_seqs > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
+    const PagedView v = view(cache, seqs, status_d);
+    PagedSelect a;
+    a.q = (const uint8_t*)q_d;
+    a.q_stride = q_row_stride * elem(q_type);
+    a.q_f32 = q_type == KL_F32;
+    a.nq = n_q_heads;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.keep_first = keep_first; a.keep_last = keep_last; a.n_select = n_select;
+    a.selected = selected_d;
+    a.scores = (float*)workspace_d;
+    const unsigned blocks = (seqs->table_pages + PG_THREADS / 32 - 1) / (PG_THREADS / 32);
+    if ((rc = launch(kl_paged_score_kernel, dim3(blocks, cache->n_kv_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a)) != KL_OK) return rc;
+    return launch(kl_paged_topk_kernel, dim3(cache->n_kv_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a);
+}
+
+kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,
+                             int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
+                             const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
+                             int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0) return KL_OK;
+    if ((rc = check_queries(cache, q_d, q_type, q_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
+    if ((rc = check_queries(cache, out_d, q_type, out_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
+    if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu || !(scale < INFINITY)) return KL_ERR_INVALID_ARG;
+    if (!workspace_d || ((uintptr_t)workspace_d & 255u)) return KL_ERR_INVALID_ARG;
+    if (seqs->n_seqs > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
+    const PagedView v = view(cache, seqs, status_d);
+    PagedAttn a;
+    a.q = (const uint8_t*)q_d;
+    a.out = (uint8_t*)out_d;
+    a.q_stride = q_row_stride * elem(q_type);
+    a.out_stride = out_row_stride * elem(q_type);
+    a.f32 = q_type == KL_F32;
+    a.nq = n_q_heads;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
+    a.window = window;
+    a.selected = selected_d;
+    a.n_select = n_select;
+    a.lse = lse_d;
+    return launch(kl_paged_attn_kernel, dim3(n_q_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a);
+}
+
+}  // extern "C"
