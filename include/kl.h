@@ -378,7 +378,8 @@ typedef struct {
      * not negative; [page][head][row] and [page][row][head] orders are both just strides. */
     int64_t page_stride, head_stride, row_stride;
     void *k_d, *v_d;       /* 16-byte aligned; NULL where a call does not read rows (kl_paged_select) */
-    /* KL_KV_E4M3: [n_pages][n_kv_heads][page_size] bytes, 16-byte aligned: byte e stands for the scale 2^(e - 127) */
+    /* KL_KV_E4M3: [n_pages][n_kv_heads][page_size] bytes, 16-byte aligned: byte e (0 .. 254) stands for the scale
+     * 2^(e - 127) */
     uint8_t *k_exp_d, *v_exp_d;
     /* Optional: bf16 [n_pages][n_kv_heads][2][head_dim], 16-byte aligned: per page, head and column the smallest and the
      * largest key the page holds (the values the cache stands for; NaN does not count).  kl_paged_append keeps them,

@@ -107,6 +107,48 @@ kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_
     return KL_OK;
 }
 
+// Workspace of kl_paged_attention (byte offsets): room for PA_MAX_BLOCKS blocks of at most eight warps.
+struct AttnSpace { size_t part, part_ml, head, head_ml, meta, bytes; };
+AttnSpace attn_space(uint32_t head_dim) {
+    AttnSpace s;
+    const size_t rec = (size_t)8 * head_dim * 4, ml = 8 * 8;
+    s.part = 0;
+    s.head = s.part + 2 * PA_MAX_BLOCKS * rec;
+    s.part_ml = s.head + 8 * PA_MAX_BLOCKS * rec;
+    s.head_ml = s.part_ml + 2 * PA_MAX_BLOCKS * ml;
+    s.meta = s.head_ml + 8 * PA_MAX_BLOCKS * ml;
+    s.bytes = s.meta + PA_MAX_BLOCKS * sizeof(int4);
+    return s;
+}
+
+// Blocks of the attention grid: one per SM.
+int attn_blocks() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms < PA_MAX_BLOCKS ? sms : PA_MAX_BLOCKS;
+}
+
+template <int HD, bool FP8, int UPT>
+kl_status launch_attn_as(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
+    using Cfg = PaCfg<HD, FP8>;
+    auto* f = kl_paged_attn_kernel<HD, FP8, UPT>;
+    // an attribute of the kernel on the current device; cheap enough to set for every call
+    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess) return KL_ERR_CUDA;
+    return launch(f, dim3((unsigned)blocks), Cfg::NW * 32, Cfg::SMEM, stream, v, a);
+}
+template <int HD>
+kl_status launch_attn_hd(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
+    // pages of whole tiles need one look-up per tile, others (multiples of four rows) four
+    const bool whole = v.page % PA_TILE == 0;
+    if (v.fp8) return whole ? launch_attn_as<HD, true, 1>(v, a, blocks, stream) : launch_attn_as<HD, true, 4>(v, a, blocks, stream);
+    return whole ? launch_attn_as<HD, false, 1>(v, a, blocks, stream) : launch_attn_as<HD, false, 4>(v, a, blocks, stream);
+}
+kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
+    if (v.hd == 64) return launch_attn_hd<64>(v, a, blocks, stream);
+    if (v.hd == 128) return launch_attn_hd<128>(v, a, blocks, stream);
+    return launch_attn_hd<256>(v, a, blocks, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -146,7 +188,8 @@ kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_hea
     const kl_status rc = check_cache(cache, false);
     if (rc != KL_OK) return rc;
     if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
-    *bytes = score_bytes(cache, n_seqs, table_pages);
+    const size_t sel = score_bytes(cache, n_seqs, table_pages), att = attn_space(cache->head_dim).bytes;
+    *bytes = sel > att ? sel : att;
     return KL_OK;
 }
 
@@ -187,22 +230,34 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     if ((rc = check_queries(cache, out_d, q_type, out_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
     if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu || !(scale < INFINITY)) return KL_ERR_INVALID_ARG;
     if (!workspace_d || ((uintptr_t)workspace_d & 255u)) return KL_ERR_INVALID_ARG;
-    if (seqs->n_seqs > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
+    uint8_t* ws = (uint8_t*)workspace_d;
+    const AttnSpace sp = attn_space(cache->head_dim);
+    if (workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
+    const int blocks = attn_blocks();
+    if (blocks <= 0) return KL_ERR_CUDA;
     const PagedView v = view(cache, seqs, status_d);
     PagedAttn a;
     a.q = (const uint8_t*)q_d;
     a.out = (uint8_t*)out_d;
     a.q_stride = q_row_stride * elem(q_type);
     a.out_stride = out_row_stride * elem(q_type);
-    a.f32 = q_type == KL_F32;
+    a.q_f32 = q_type == KL_F32;
+    a.out_mode = q_type == KL_F32 ? PA_F32 : PA_BF16;
     a.nq = n_q_heads;
     a.G = n_q_heads / cache->n_kv_heads;
+    a.HT = (a.G + 7) / 8;
     a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
     a.window = window;
     a.selected = selected_d;
     a.n_select = n_select;
     a.lse = lse_d;
-    return launch(kl_paged_attn_kernel, dim3(n_q_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a);
+    a.part = (float*)(ws + sp.part);
+    a.part_ml = (float*)(ws + sp.part_ml);
+    a.head = (float*)(ws + sp.head);
+    a.head_ml = (float*)(ws + sp.head_ml);
+    a.meta = (int4*)(ws + sp.meta);
+    if ((rc = launch_attn(v, a, blocks, stream)) != KL_OK) return rc;
+    return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
 }
 
 }  // extern "C"
