@@ -36,7 +36,7 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     said = [j.communicate()[0] for j in jobs]
     ok = all(j.returncode == 0 for j in jobs)
     if ok:
-        res = subprocess.run([nvcc, "--shared", "-o", str(tmp), *map(str, objs)], capture_output=True, text=True)
+        res = subprocess.run([nvcc, *NVCC_FLAGS[:2], "--shared", "-o", str(tmp), *map(str, objs)], capture_output=True, text=True)
         said.append(res.stdout + res.stderr)
         ok = res.returncode == 0
     for o in objs:

@@ -4,6 +4,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
 #include <utility>
 
 #include "../../include/kl.h"
@@ -107,16 +108,16 @@ kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_
     return KL_OK;
 }
 
-// Workspace of kl_paged_attention (byte offsets): room for PA_MAX_BLOCKS blocks of at most eight warps.
+// Workspace of kl_paged_attention (byte offsets): room for PA_MAX_BLOCKS blocks of PA_MAX_WARPS warps.
 struct AttnSpace { size_t part, part_ml, head, head_ml, meta, bytes; };
 AttnSpace attn_space(uint32_t head_dim) {
     AttnSpace s;
     const size_t rec = (size_t)8 * head_dim * 4, ml = 8 * 8;
     s.part = 0;
     s.head = s.part + 2 * PA_MAX_BLOCKS * rec;
-    s.part_ml = s.head + 8 * PA_MAX_BLOCKS * rec;
+    s.part_ml = s.head + PA_MAX_WARPS * PA_MAX_BLOCKS * rec;
     s.head_ml = s.part_ml + 2 * PA_MAX_BLOCKS * ml;
-    s.meta = s.head_ml + 8 * PA_MAX_BLOCKS * ml;
+    s.meta = s.head_ml + PA_MAX_WARPS * PA_MAX_BLOCKS * ml;
     s.bytes = s.meta + PA_MAX_BLOCKS * sizeof(int4);
     return s;
 }
@@ -128,25 +129,41 @@ int attn_blocks() {
     return sms < PA_MAX_BLOCKS ? sms : PA_MAX_BLOCKS;
 }
 
-template <int HD, bool FP8, int UPT>
+// Function attributes hold per device: set them on a kernel's first launch there (`done`: one bit per device; devices
+// beyond 63 set them every time).  All kernels of the attention ask for the largest shared-memory carve-out, so that an SM
+// can hold blocks of both at once and is not reconfigured between them.
+kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KL_ERR_CUDA;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return KL_OK;
+    if (cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
+        (smem && cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess))
+        return KL_ERR_CUDA;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return KL_OK;
+}
+
+template <int HD, bool FP8, int UR, bool EX>
 kl_status launch_attn_as(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
-    using Cfg = PaCfg<HD, FP8>;
-    auto* f = kl_paged_attn_kernel<HD, FP8, UPT>;
-    // an attribute of the kernel on the current device; cheap enough to set for every call
-    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM) != cudaSuccess) return KL_ERR_CUDA;
+    using Cfg = PaCfg<HD, FP8, EX>;
+    auto* f = kl_paged_attn_kernel<HD, FP8, UR, EX>;
+    static std::atomic<uint64_t> done{0};
+    const kl_status rc = prepare((const void*)f, (int)Cfg::SMEM, done);
+    if (rc != KL_OK) return rc;
     return launch(f, dim3((unsigned)blocks), Cfg::NW * 32, Cfg::SMEM, stream, v, a);
 }
-template <int HD>
+template <int HD, bool FP8>
 kl_status launch_attn_hd(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
-    // pages of whole tiles need one look-up per tile, others (multiples of four rows) four
-    const bool whole = v.page % PA_TILE == 0;
-    if (v.fp8) return whole ? launch_attn_as<HD, true, 1>(v, a, blocks, stream) : launch_attn_as<HD, true, 4>(v, a, blocks, stream);
-    return whole ? launch_attn_as<HD, false, 1>(v, a, blocks, stream) : launch_attn_as<HD, false, 4>(v, a, blocks, stream);
+    // pages are looked up in units of 16 rows where they consist of such units, else of four
+    const bool whole = v.page % 16 == 0, ex = a.out_mode != PA_BF16;
+    if (ex) return whole ? launch_attn_as<HD, FP8, 16, true>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, true>(v, a, blocks, stream);
+    return whole ? launch_attn_as<HD, FP8, 16, false>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, false>(v, a, blocks, stream);
 }
 kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
-    if (v.hd == 64) return launch_attn_hd<64>(v, a, blocks, stream);
-    if (v.hd == 128) return launch_attn_hd<128>(v, a, blocks, stream);
-    return launch_attn_hd<256>(v, a, blocks, stream);
+    if (v.hd == 64) return v.fp8 ? launch_attn_hd<64, true>(v, a, blocks, stream) : launch_attn_hd<64, false>(v, a, blocks, stream);
+    if (v.hd == 128) return v.fp8 ? launch_attn_hd<128, true>(v, a, blocks, stream) : launch_attn_hd<128, false>(v, a, blocks, stream);
+    return v.fp8 ? launch_attn_hd<256, true>(v, a, blocks, stream) : launch_attn_hd<256, false>(v, a, blocks, stream);
 }
 
 }  // namespace
@@ -241,7 +258,6 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     a.out = (uint8_t*)out_d;
     a.q_stride = q_row_stride * elem(q_type);
     a.out_stride = out_row_stride * elem(q_type);
-    a.q_f32 = q_type == KL_F32;
     a.out_mode = q_type == KL_F32 ? PA_F32 : PA_BF16;
     a.nq = n_q_heads;
     a.G = n_q_heads / cache->n_kv_heads;
@@ -257,6 +273,8 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     a.head_ml = (float*)(ws + sp.head_ml);
     a.meta = (int4*)(ws + sp.meta);
     if ((rc = launch_attn(v, a, blocks, stream)) != KL_OK) return rc;
+    static std::atomic<uint64_t> done{0};
+    if ((rc = prepare((const void*)kl_paged_merge_kernel, 0, done)) != KL_OK) return rc;
     return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
 }
 

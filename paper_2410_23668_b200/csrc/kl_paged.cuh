@@ -429,7 +429,6 @@ struct PagedAttn {
     const uint8_t* q;
     uint8_t* out;
     int64_t q_stride, out_stride;   // bytes
-    uint32_t q_f32;                 // element type of q
     uint32_t out_mode;              // PA_BF16, PA_F32, PA_OPERAND
     uint32_t nq, G, HT;             // G query heads per kv head, in HT tiles of at most eight
     float scale_log2;               // scale * log2(e)
@@ -440,10 +439,10 @@ struct PagedAttn {
     // workspace: partial results, one record = [8 heads][hd] sums and [8 heads] (maximum, sum)
     float *part, *part_ml;          // [blocks][2]: the pair that began in an earlier block, the pair that goes on in the next one
     float *head, *head_ml;          // [blocks][warps]: a warp's first pair when it began in an earlier warp
-    int4* meta;                     // [blocks]: (PA_* flags, sequence and pair-in-sequence of the second record)
+    int4* meta;                     // [blocks]: the pair of the second record (sequence, pair in the sequence) and the last
+                                    // block that shares it; .x = 0: no such pair
 };
 enum { PA_BF16 = 0, PA_F32 = 1, PA_OPERAND = 2 };
-enum { PA_FIRST = 1, PA_FIRST_GOES_ON = 2, PA_SECOND = 4 };
 
 __device__ __forceinline__ float pa_ex2(float x) {
     float y;
@@ -454,28 +453,28 @@ __device__ __forceinline__ uint32_t pa_pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ void pa_mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// D += A * B, one m16n8k16 tile of f16 (e4m3 caches) or bf16 operands.  Not volatile: the compiler may interleave chains.
+template <bool FP8>
+__device__ __forceinline__ void pa_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (FP8)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two numbers rounded to 16 bits (f16 with an e4m3 cache, bf16 else), and what that leaves of them.
+template <bool FP8>
+__device__ __forceinline__ uint32_t pa_round(float x0, float x1) {
+    return FP8 ? pa_pack_f16(x0, x1) : pack_bf16(x0, x1);
 }
 template <bool FP8>
-__device__ __forceinline__ void pa_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if (FP8) pa_mma_f16(d, a, b0, b1);
-    else mma_16816(d, a, b0, b1);
-}
-// Two numbers as their halves: hi rounded to 16 bits, lo what is left (an f16 pair with an e4m3 cache, a bf16 pair else).
-template <bool FP8>
-__device__ __forceinline__ void pa_split(float x0, float x1, uint32_t& hi, uint32_t& lo) {
-    if (FP8) {
-        hi = pa_pack_f16(x0, x1);
-        const float2 f = pg_f16x2_to_float2(hi);
-        lo = pa_pack_f16(x0 - f.x, x1 - f.y);
-    } else {
-        hi = pack_bf16(x0, x1);
-        lo = pack_bf16(x0 - bf_lo(hi), x1 - bf_hi(hi));
-    }
+__device__ __forceinline__ uint32_t pa_rest(float x0, float x1, uint32_t hi) {
+    if (!FP8) return pack_bf16(x0 - bf_lo(hi), x1 - bf_hi(hi));
+    const float2 f = pg_f16x2_to_float2(hi);
+    return pa_pack_f16(x0 - f.x, x1 - f.y);
 }
 // 16 (or 4) bytes to shared memory, asynchronously; nothing is read and zeros are written when `ok` is false.
 __device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src, bool ok) {
@@ -509,23 +508,54 @@ __device__ __forceinline__ void pa_store2(const PagedView& c, const PagedAttn& a
         *reinterpret_cast<uint32_t*>(x + (32 + s) * width + at) = pack_bf16(v0 - bf_lo(hi), v1 - bf_hi(hi));
     }
 }
+__device__ __forceinline__ void pa_store1(const PagedView& c, const PagedAttn& a, uint32_t s, uint32_t hq, uint32_t d, float v) {
+    if (a.out_mode == PA_F32) {
+        *reinterpret_cast<float*>(a.out + (int64_t)s * a.out_stride + ((size_t)hq * c.hd + d) * 4) = v;
+    } else if (a.out_mode == PA_BF16) {
+        *reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)s * a.out_stride + ((size_t)hq * c.hd + d) * 2) = __float2bfloat16_rn(v);
+    } else {
+        __nv_bfloat16* x = reinterpret_cast<__nv_bfloat16*>(a.out);
+        const size_t width = (size_t)a.nq * c.hd, at = (size_t)hq * c.hd + d;
+        const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+        x[s * width + at] = hi;
+        x[(32 + s) * width + at] = __float2bfloat16_rn(v - __bfloat162float(hi));
+    }
+}
 __device__ __forceinline__ void pa_store_lse(const PagedAttn& a, uint32_t s, uint32_t hq, float m, float l) {
     if (a.lse) a.lse[(size_t)s * a.nq + hq] = (m + log2f(l)) * 0.6931471805599453f;   // l == 0: -inf
 }
 
+// 64-bit division that is usually a 32-bit one (a 64-bit division is a few hundred cycles of a kernel that may last 5 us).
+__device__ __forceinline__ uint64_t pa_div(uint64_t x, uint32_t y) { return (x >> 32) == 0u ? (uint64_t)((uint32_t)x / y) : x / y; }
+
 constexpr uint32_t PA_NONE = 0x7fffffffu;   // position of a row group that holds nothing to attend to
-constexpr int PA_TILE = 16;                 // positions per tile
+constexpr int PA_MAX_WARPS = 16;
 constexpr int PA_LENS = 1024;               // sequences whose lengths are kept in shared memory
 constexpr uint32_t PA_MIN_TILES = 8;        // fewest tiles worth a block
 
-template <int HD, bool FP8>
+#ifndef KL_PA_REST
+#define KL_PA_REST 1
+#endif
+#ifndef KL_PA_F8_NW
+#define KL_PA_F8_NW 12
+#endif
+#ifndef KL_PA_F8_TP
+#define KL_PA_F8_TP 32
+#endif
+#ifndef KL_PA_BF_NW
+#define KL_PA_BF_NW 12
+#endif
+// EX: fp32 queries and outputs -- what 16-bit rounding leaves of q and p enters the products too.
+template <int HD, bool FP8, bool EX>
 struct PaCfg {
     static constexpr int ROW = FP8 ? HD : 2 * HD;            // bytes of a cached row
-    static constexpr int TILE = PA_TILE * ROW;               // bytes of a K (or V) tile
-    static constexpr int NW = HD == 256 && !FP8 ? 6 : 8;     // warps
-    static constexpr int RING = 196608 / (NW * 2 * TILE);
+    static constexpr int NW = HD == 256 ? (FP8 ? 8 : 6) : EX && HD == 128 ? 8 : HD == 64 ? 12 : FP8 ? KL_PA_F8_NW : KL_PA_BF_NW;     // warps
+    static constexpr int TP = HD == 64 ? 32 : HD == 128 && FP8 ? KL_PA_F8_TP : 16;     // positions per tile
+    static constexpr int TILE = TP * ROW;                    // bytes of a K (or V) tile
+    static constexpr int RING = 204800 / (NW * 2 * TILE);
     static constexpr int ST = RING > 8 ? 8 : RING;           // tiles of a warp's ring
-    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 32 + 16) + NW * 8 * 8 + 256 * 8 + PA_LENS * 4 + 256;
+    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 64 + 48) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256;
+    static_assert(ST >= 2 && SMEM <= 232448, "ring");
 };
 
 // Positions of sequence s that take part, as tiles.
@@ -534,6 +564,7 @@ struct PaSeq {
     uint32_t t0, nt;    // tiles [t0, t0 + nt) of its (virtual) positions
     uint32_t listed;    // entries of the page list that are looked at
 };
+template <uint32_t TP>
 __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, uint32_t len) {
     PaSeq q;
     q.len = len;
@@ -541,46 +572,50 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
     if (a.selected) {
         q.listed = min(a.n_select, (len + c.page - 1u) / c.page);
         q.t0 = 0;
-        q.nt = (uint32_t)(((uint64_t)q.listed * c.page + PA_TILE - 1u) / PA_TILE);
+        q.nt = (uint32_t)(((uint64_t)q.listed * c.page + TP - 1u) / TP);
     } else {
         q.listed = 0;
-        q.t0 = q.lo / PA_TILE;
-        q.nt = len ? (len + PA_TILE - 1u) / PA_TILE - q.t0 : 0u;
+        q.t0 = q.lo / TP;
+        q.nt = len ? (len + TP - 1u) / TP - q.t0 : 0u;
     }
     return q;
 }
 
 // Attention of one new token per sequence as ONE balanced stream over the whole batch.
 //
-//   * Work: 16 positions of one kv head of one sequence, for up to eight of the query heads that share it, are a tile.  The
+//   * Work: TP positions of one kv head of one sequence, for up to eight of the query heads that share it, are a tile.  The
 //     tiles of all (sequence, kv head, head tile) pairs form one list; every block takes an equal, contiguous range of it and
 //     every warp an equal part of that, whatever the sequences' lengths.  A warp walks its range alone: a ring of its own in
 //     shared memory, filled with 16-byte asynchronous copies ST - 1 tiles ahead (across pair boundaries), no barrier.
 //     Where the range leaves a pair the pair's result is finished, or left as a partial one if other warps share the pair;
 //     those of one block meet in shared memory at the end, those of several blocks in kl_paged_merge_kernel.
-//   * Mathematics: running maximum m and sum l of 2^(s - m) per head, s = q . k * scale * log2(e).  Both products run on
-//     mma.m16n8k16 with the eight heads as rows 0..7 of the A operand and what 16-bit rounding leaves of them as rows
-//     8..15: q = hi + lo and p = hi + lo cost no extra instruction, the sums of the two halves are added in 32 bits.
-//     A score fragment holds head lane / 4 in every register, so p goes straight into the A operand of the value product.
+//   * Mathematics: sums of 2^(s - m) per head, s = q . k * scale * log2(e), m a reference that follows the maximum: it is
+//     raised (and the sums rescaled) only when a score exceeds it by more than 2^8, so that most tiles pass without an
+//     exchange between lanes.  Positions are the 16 rows of mma.m16n8k16, the heads its eight columns:
+//     S[pos, head] = K . Q^T, O^T[d, head] += V^T . P; P leaves the score accumulators in 16-bit pairs and reaches the
+//     layout of a B operand with one movmatrix per 8 x 8 block.  Where 16 bits are not enough (bf16 probabilities;
+//     everything when q and out are fp32: EX) the rounding's rest enters as a second product.
 //   * e4m3 rows become f16 (exact) on the way to the tensor cores.  Their scales are powers of two: 2^(e_k - 127) multiplies
-//     the score, 2^(e_v - 127) the probability.  The weighted probabilities w = p * 2^(e_v - 127) have a running maximum
-//     of their own, so that f16 holds them whatever the scales (w * 2^14 at most 2^14).
-//   * UPT = page_size % 16 == 0 ? 1 : 4 page look-ups per tile (a lane looks up one, 32 / UPT tiles in a go).
-template <int HD, bool FP8, int UPT>
-__global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kernel(const PagedView c, const PagedAttn a) {
-    using Cfg = PaCfg<HD, FP8>;
+//     the score, 2^(e_v - 127) the probability.  The weighted probabilities w = p * 2^(e_v - 127) have a reference of
+//     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
+//   * Pages are looked up in units of UR rows (16 where the page size is a multiple of 16, else 4), one per lane, a batch of
+//     32 ahead of the copies.
+template <int HD, bool FP8, int UR, bool EX>
+__global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_kernel(const PagedView c, const PagedAttn a) {
+    using Cfg = PaCfg<HD, FP8, EX>;
     constexpr int NW = Cfg::NW, ST = Cfg::ST, ROW = Cfg::ROW, TILE = Cfg::TILE, NT = NW * 32;
-    constexpr uint32_t UR = PA_TILE / UPT;                       // rows per page look-up
+    constexpr uint32_t TP = Cfg::TP, UPT = TP / UR;              // positions and page look-ups per tile
+    constexpr int NS = TP / 16;                                  // MMA steps of 16 positions per tile
     constexpr uint32_t TPB = 32 / UPT;                           // tiles per batch of look-ups
     constexpr int CPR = ROW / 16, RPP = 32 / CPR;                // 16-byte pieces per row, rows per pass of a warp
-    constexpr int NMMA = HD / 16, NOUT = HD / 8;
+    constexpr int NMMA = HD / 16;                                // k steps of a score, m tiles of the result
     extern __shared__ __align__(128) uint8_t pa_smem[];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, j = lane & 3u;
     uint8_t* exps_all = pa_smem + (size_t)NW * ST * 2 * TILE;
-    uint32_t* lps_all = reinterpret_cast<uint32_t*>(exps_all + (size_t)NW * ST * 32);
-    float2* ml_all = reinterpret_cast<float2*>(lps_all + NW * ST * 4);          // [NW][8]
+    uint32_t* lps_all = reinterpret_cast<uint32_t*>(exps_all + (size_t)NW * ST * 64);
+    float2* ml_all = reinterpret_cast<float2*>(lps_all + NW * ST * 12);          // [NW][8]
     uint64_t* pre = reinterpret_cast<uint64_t*>(ml_all + NW * 8);               // [NT]
-    uint32_t* lens = reinterpret_cast<uint32_t*>(pre + 256);                    // [PA_LENS]
+    uint32_t* lens = reinterpret_cast<uint32_t*>(pre + 512);                    // [PA_LENS]
     uint32_t* misc = lens + PA_LENS;
     uint64_t* wsum = reinterpret_cast<uint64_t*>(misc);                         // [NW], then the entries below
     griddep_launch();
@@ -593,7 +628,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
     for (uint32_t s = tid * per; s < min(n, (tid + 1u) * per); ++s) {
         const uint32_t len = pg_length(c, s);
         if (s < (uint32_t)PA_LENS) lens[s] = len;
-        mine += (uint64_t)pa_seq(c, a, len).nt * PH;
+        mine += (uint64_t)pa_seq<TP>(c, a, len).nt * PH;
     }
     uint64_t incl = mine;
 #pragma unroll
@@ -619,19 +654,23 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
             for (uint32_t i = tid; i < a.nq; i += NT) pa_store_lse(a, s, i, 0.f, 0.f);
         }
 
-    const uint64_t blocks = min((uint64_t)gridDim.x, (W + PA_MIN_TILES - 1u) / PA_MIN_TILES);   // blocks at work
+    const uint32_t blocks = (uint32_t)min((uint64_t)gridDim.x, (W + PA_MIN_TILES - 1u) / PA_MIN_TILES);   // blocks at work
     if (blockIdx.x >= blocks) {
         if (tid == 0u) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
-    const uint64_t b_lo = W * blockIdx.x / blocks, b_hi = W * (blockIdx.x + 1u) / blocks;
-    const uint64_t lo = b_lo + (b_hi - b_lo) * warp / NW, hi = b_lo + (b_hi - b_lo) * (warp + 1u) / NW;
+    // block b takes tiles [share * b + min(b, over), ...): the first `over` blocks one more than the others
+    const uint64_t share = pa_div(W, blocks), over = W - share * blocks;
+    const uint64_t b_lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), b_n = share + (blockIdx.x < over ? 1u : 0u);
+    const uint64_t w_n = pa_div(b_n, NW), w_over = b_n - w_n * NW;
+    const uint64_t lo = b_lo + w_n * warp + min((uint64_t)warp, w_over), hi = lo + w_n + (warp < w_over ? 1u : 0u);
 
     // ---- this warp's range
     struct Entry { uint32_t valid, s, ph, begins, ends; } first = {0, 0, 0, 0, 0}, last = {0, 0, 0, 0, 0};
+    uint32_t last_tiles = 0;
     const uint32_t ring = smem_u32(pa_smem) + warp * (ST * 2 * TILE);
-    const uint32_t exps = smem_u32(exps_all) + warp * (ST * 32);
-    volatile uint32_t* lps = lps_all + warp * (ST * 4);
+    const uint32_t exps = smem_u32(exps_all) + warp * (ST * 64);
+    volatile uint32_t* lps = lps_all + warp * (ST * 12);
     if (lo < hi) {
         uint32_t i0 = 0, i1 = NT;
         while (i1 - i0 > 1u) {
@@ -641,12 +680,12 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
         }
         uint64_t rem = lo - pre[i0];
         uint32_t cs = i0 * per;                    // cursor of the tiles that are consumed
-        PaSeq cq = pa_seq(c, a, length(cs));
+        PaSeq cq = pa_seq<TP>(c, a, length(cs));
         while (rem >= (uint64_t)cq.nt * PH) {
             rem -= (uint64_t)cq.nt * PH;
-            cq = pa_seq(c, a, length(++cs));
+            cq = pa_seq<TP>(c, a, length(++cs));
         }
-        uint32_t cph = (uint32_t)(rem / cq.nt), ct = (uint32_t)(rem % cq.nt);
+        uint32_t cph = (uint32_t)pa_div(rem, cq.nt), ct = (uint32_t)(rem - (uint64_t)cph * cq.nt);
 
         // cursor of the tiles that are requested, and the look-ups of its batch (this one and the next)
         uint32_t is = cs, iph = cph, it = ct;
@@ -678,86 +717,86 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
         uint64_t left = hi - lo;   // tiles still to request
         auto issue = [&](uint32_t st) {
             const uint32_t b = it / TPB, at = it - b * TPB;
-            if (b != batch) {
-                if (batch != 0xffffffffu && b == batch + 1u) {
-                    b_phys = n_phys; b_lp = n_lp; b_row = n_row;
-                } else {
-                    look_up(b, b_phys, b_lp, b_row);
+            if (b != batch) {   // this batch, unless it has been looked up already, and the next one
+                const bool known = batch != 0xffffffffu;
+                b_phys = n_phys; b_lp = n_lp; b_row = n_row;
+#pragma unroll 1
+                for (uint32_t x = known ? b + 1u : b; x <= b + 1u && x * TPB < iq.nt; ++x) {
+                    look_up(x, n_phys, n_lp, n_row);
+                    if (x == b) { b_phys = n_phys; b_lp = n_lp; b_row = n_row; }
                 }
                 batch = b;
-                if ((b + 1u) * TPB < iq.nt) look_up(b + 1u, n_phys, n_lp, n_row);
             }
             const uint32_t h = iph / a.HT;
             const uint32_t kd = ring + st * (2 * TILE), vd = kd + TILE;
             const int64_t hoff = (int64_t)h * c.head_b;
             const uint32_t ch = lane % CPR, r0 = lane / CPR;
-            if (UPT == 1) {
-                const int32_t phys = __shfl_sync(0xffffffffu, b_phys, at);
-                const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, at), row = __shfl_sync(0xffffffffu, b_row, at);
-                const int32_t r_lo = (int32_t)iq.lo - (int32_t)lp, r_hi = (int32_t)iq.len - (int32_t)lp;   // rows of the tile that count
-                int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + r0) * c.row_b + ch * 16u;
-                const int64_t step = (int64_t)RPP * c.row_b;
+            bool full = true;   // every position of the tile counts
 #pragma unroll
-                for (int i = 0; i < PA_TILE / RPP; ++i) {
-                    const int32_t r = i * RPP + (int32_t)r0;
-                    const bool ok = r >= r_lo && r < r_hi;
-                    const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
-                    const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
-                    pa_copy16(kd + r * ROW + ((ch ^ fk) << 4), c.k + off, ok);
-                    pa_copy16(vd + r * ROW + ((ch ^ fv) << 4), c.v + off, ok);
-                    off += step;
-                }
-                if (FP8 && lane < 2u) {
-                    const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
-                    pa_copy16(exps + st * 32 + lane * 16, (lane ? c.ve : c.ke) + eoff, phys >= 0);
-                }
-                if (lane == 0u) lps[st * 4] = lp;
-            } else {
+            for (uint32_t v = 0; v < UPT; v += UR == 16 ? 1 : UPT) {   // UR == 16: unit after unit; UR == 4: the lanes' units at once
+                if (UR == 16) {
+                    const int32_t phys = __shfl_sync(0xffffffffu, b_phys, at * UPT + v);
+                    const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, at * UPT + v), row = __shfl_sync(0xffffffffu, b_row, at * UPT + v);
+                    const int32_t r_lo = (int32_t)iq.lo - (int32_t)lp, r_hi = (int32_t)iq.len - (int32_t)lp;   // rows of the unit that count
+                    full = full && r_lo <= 0 && r_hi >= 16;
+                    int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + r0) * c.row_b + ch * 16u;
+                    const int64_t step = (int64_t)RPP * c.row_b;
 #pragma unroll
-                for (int i = 0; i < PA_TILE / RPP; ++i) {
-                    const int32_t r = i * RPP + (int32_t)r0;
-                    const uint32_t src = at * UPT + (r >> 2);
-                    const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
-                    const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
-                    const int32_t p = (int32_t)lp + (r & 3);
-                    const bool ok = lp != PA_NONE && p >= (int32_t)iq.lo && p < (int32_t)iq.len;
-                    const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + (r & 3)) * c.row_b + ch * 16u;
-                    const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
-                    const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
-                    pa_copy16(kd + r * ROW + ((ch ^ fk) << 4), c.k + off, ok);
-                    pa_copy16(vd + r * ROW + ((ch ^ fv) << 4), c.v + off, ok);
-                }
-                {
-                    const uint32_t src = at * UPT + (lane & 3u);
-                    const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
-                    const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
-                    if (FP8 && lane < 8u) {
-                        const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
-                        pa_copy4(exps + st * 32 + lane * 4, (lane < 4u ? c.ke : c.ve) + eoff, phys >= 0);
+                    for (int i = 0; i < 16 / RPP; ++i) {
+                        const int32_t r = i * RPP + (int32_t)r0;
+                        const bool ok = r >= r_lo && r < r_hi;
+                        const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
+                        const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
+                        pa_copy16(kd + (v * 16 + r) * ROW + ((ch ^ fk) << 4), c.k + off, ok);
+                        pa_copy16(vd + (v * 16 + r) * ROW + ((ch ^ fv) << 4), c.v + off, ok);
+                        off += step;
                     }
-                    if (lane < 4u) lps[st * 4 + lane] = lp;
+                    if (FP8 && lane < 2u) {
+                        const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
+                        pa_copy16(exps + st * 64 + lane * 32 + v * 16, (lane ? c.ve : c.ke) + eoff, phys >= 0);
+                    }
+                    if (lane == 0u) lps[st * 12 + v] = lp;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < (int)TP / RPP; ++i) {
+                        const int32_t r = i * RPP + (int32_t)r0;
+                        const uint32_t src = at * UPT + (r >> 2);
+                        const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
+                        const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
+                        const int32_t p = (int32_t)lp + (r & 3);
+                        const bool ok = lp != PA_NONE && p >= (int32_t)iq.lo && p < (int32_t)iq.len;
+                        const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + (r & 3)) * c.row_b + ch * 16u;
+                        const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
+                        const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
+                        pa_copy16(kd + r * ROW + ((ch ^ fk) << 4), c.k + off, ok);
+                        pa_copy16(vd + r * ROW + ((ch ^ fv) << 4), c.v + off, ok);
+                    }
+                    const uint32_t u = lane % UPT, src = at * UPT + u;
+                    const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
+                    const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
+                    if (FP8 && lane < 2u * UPT) {
+                        const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
+                        pa_copy4(exps + st * 64 + lane / UPT * 32 + u * 4, (lane < UPT ? c.ke : c.ve) + eoff, phys >= 0);
+                    }
+                    if (lane < UPT) lps[st * 12 + lane] = lp;
+                    full = __all_sync(0xffffffffu, lp != PA_NONE && lp >= iq.lo && lp + UR <= iq.len);
                 }
             }
+            if (lane == 0u) lps[st * 12 + 8] = full;
             --left;
             if (++it == iq.nt && left) {   // on to the next pair, perhaps of the next sequence that has any
                 it = 0;
                 batch = 0xffffffffu;
                 if (++iph == PH) {
                     iph = 0;
-                    do iq = pa_seq(c, a, length(++is));
+                    do iq = pa_seq<TP>(c, a, length(++is));
                     while (iq.nt == 0u);
                 }
             }
         };
-#pragma unroll
-        for (int st = 0; st < ST - 1; ++st) {
-            if (left) issue(st);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-
-        // ---- state of the pair under way: head g of the tile in every lane of its quad
-        uint32_t qa[NMMA][4];
-        float o[NOUT][4], m = -INFINITY, l = 0.f, mw = -INFINITY, qs = 0.f;
+        // ---- state of the pair under way.  Queries: head g; scores and results: heads 2j and 2j + 1
+        uint32_t qh[NMMA][2], ql[EX ? NMMA : 1][2];
+        float o[NMMA][4], m[2], l[2], mw[2], qs[2];
         auto begin_pair = [&]() {
             const uint32_t h = cph / a.HT, hg = (cph - h * a.HT) * 8u + g;
             const bool live = hg < a.G;
@@ -772,7 +811,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i][e] = 0.f;
                 if (live) {
-                    if (a.q_f32) {
+                    if (EX) {
                         const float4 f = *reinterpret_cast<const float4*>(q + (size_t)(base + d) * 4);
                         x[i][0] = f.x; x[i][1] = f.y; x[i][2] = f.z; x[i][3] = f.w;
                     } else {
@@ -784,191 +823,232 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
 #pragma unroll
                     for (int e = 0; e < 4; ++e) big = fmaxf(big, fabsf(x[i][e]));
             }
-            qs = a.scale_log2;
-            float f = 1.f;
+            float mul = a.scale_log2, f = 1.f;
             if (FP8) {   // f16 operands: the head's largest query element comes to lie in [2^14, 2^15)
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const int32_t k = max((int32_t)(__float_as_uint(big) >> 23) - 127, -112);
                 f = __uint_as_float((uint32_t)(127 + 14 - k) << 23);
-                qs *= __uint_as_float((uint32_t)(127 - 14 + k) << 23);
+                mul *= __uint_as_float((uint32_t)(127 - 14 + k) << 23);
             }
+            qs[0] = __shfl_sync(0xffffffffu, mul, j * 8u);
+            qs[1] = __shfl_sync(0xffffffffu, mul, j * 8u + 4u);
 #pragma unroll
-            for (int i = 0; i < NMMA; ++i) {
-                pa_split<FP8>(x[i][0] * f, x[i][1] * f, qa[i][0], qa[i][1]);
-                pa_split<FP8>(x[i][2] * f, x[i][3] * f, qa[i][2], qa[i][3]);
-            }
+            for (int i = 0; i < NMMA; ++i)
 #pragma unroll
-            for (int i = 0; i < NOUT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-            m = mw = -INFINITY;
-            l = 0.f;
-        };
-        // The pair's result over the tiles seen: sums relative to 2^m, columns as emit(head, d, v0, v1) gets them.
-        auto end_pair = [&](auto&& emit) {
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            const float f = !FP8 ? 1.f : mw == -INFINITY ? 0.f : pa_ex2(mw - m - 14.f);
-            if (FP8) {
-                constexpr int W16 = HD >= 128 ? 16 : 8;   // columns of a lane's V piece
-#pragma unroll
-                for (int i = 0; i < NOUT; i += 2) {
-                    const uint32_t d = (i / W16) * (8 * W16) + i % W16;
-                    emit(d + 2u * j * W16, (o[i][0] + o[i][2]) * f, (o[i + 1][0] + o[i + 1][2]) * f);
-                    emit(d + (2u * j + 1u) * W16, (o[i][1] + o[i][3]) * f, (o[i + 1][1] + o[i + 1][3]) * f);
+                for (int e = 0; e < 2; ++e) {
+                    const float x0 = x[i][2 * e] * f, x1 = x[i][2 * e + 1] * f;
+                    qh[i][e] = pa_round<FP8>(x0, x1);
+                    if (EX) ql[i % (EX ? NMMA : 1)][e] = pa_rest<FP8>(x0, x1, qh[i][e]);
                 }
-            } else {
 #pragma unroll
-                for (int i = 0; i < NOUT; ++i) emit(i * 8u + 2u * j, o[i][0] + o[i][2], o[i][1] + o[i][3]);
+            for (int i = 0; i < NMMA; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            m[0] = m[1] = mw[0] = mw[1] = -INFINITY;
+            l[0] = l[1] = 0.f;
+        };
+        // The pair's result over the tiles seen, relative to 2^m: emit(x, d, v0, v1) gets columns d and d + 1 of head 2j + x
+        // (e4m3), or d and d + 8 (bf16).
+        auto end_pair = [&](auto&& emit) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int k = 4; k < 32; k <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], k);
+                const float f = !FP8 ? 1.f : mw[x] == -INFINITY ? 0.f : pa_ex2(mw[x] - m[x] - 7.f);
+                constexpr int W16 = HD >= 128 ? 16 : 8;   // columns of a lane's V piece (e4m3)
+#pragma unroll
+                for (int i = 0; i < NMMA; ++i) {
+                    const uint32_t d = FP8 ? (2 * i / W16) * (8 * W16) + g * W16 + 2 * i % W16 : i * 16 + g;
+                    emit(x, d, o[i][x] * f, o[i][x + 2] * f);
+                }
             }
         };
 
         const uint32_t total = (uint32_t)(hi - lo);   // a warp's share (2^32 tiles would be hours of work)
         uint32_t seg0 = ct;                           // first tile of the pair that this warp has seen
-        begin_pair();
-        for (uint32_t k = 0, st = 0; k < total; ++k) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
-            __syncwarp();
-            if (left) issue(st == 0 ? ST - 1 : st - 1);
+        bool fresh = true;                            // the next tile starts a pair
+        uint32_t to = 0;                              // ring slot of the next request
+        uint32_t k = 0, st = 0;                       // tile of the range, and its slot
+        for (uint32_t ahead = 0; k < total;) {
+            if (ahead >= (uint32_t)ST - 1u) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+                __syncwarp();   // the tile is there for every lane, and every lane is done with the previous one
+            }
+            if (left) issue(to);
+            if (++to == (uint32_t)ST) to = 0;
             asm volatile("cp.async.commit_group;" ::: "memory");
+            if (ahead < (uint32_t)ST - 1u) {   // the first ST - 1 tiles are only requested
+                ++ahead;
+                continue;
+            }
+            if (fresh) begin_pair();
+            fresh = false;
 
             const uint32_t kd = ring + st * (2 * TILE), vd = kd + TILE;
-            // scores of positions 2j, 2j + 1 (s[0], s[1]) and 2j + 8, 2j + 9 (s[2], s[3]) of the tile for head g
-            float sc[2][4];
+            // scores: s[2x + e] is that of position 8x + g and head 2j + e
+            float sc[NS][4], s[4 * NS], sv[4 * NS];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
-                const uint32_t r = t * 8 + g, row = kd + r * ROW;
-                const uint32_t fk = CPR >= 8 ? ((r & 1u) << 2 | ((r >> 1) & 3u)) : 0u;
+            for (int t = 0; t < NS; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+            const uint32_t fk = CPR >= 8 ? ((g & 1u) << 2 | ((g >> 1) & 3u)) : 0u;
 #pragma unroll
-                for (int q = 0; q < CPR / 4; ++q) {
-                    const uint4 w = pa_lds16(row + (((q * 4 + j) ^ fk) << 4));
+            for (int q = 0; q < CPR / 4; ++q)
+#pragma unroll
+                for (int t = 0; t < NS; ++t) {
+                    const uint32_t at = kd + (t * 16 + g) * ROW + (((q * 4 + j) ^ fk) << 4);
+                    const uint4 w = pa_lds16(at), y = pa_lds16(at + 8 * ROW);   // rows g and g + 8: the same swizzle
+                    const uint32_t wa[4] = {w.x, w.y, w.z, w.w}, ya[4] = {y.x, y.y, y.z, y.w};
                     if (FP8) {
-                        pa_mma<true>(sc[t], qa[q * 4 % NMMA], pg_e4m3x2_to_f16x2(w.x & 0xffffu), pg_e4m3x2_to_f16x2(w.x >> 16));
-                        pa_mma<true>(sc[t], qa[(q * 4 + 1) % NMMA], pg_e4m3x2_to_f16x2(w.y & 0xffffu), pg_e4m3x2_to_f16x2(w.y >> 16));
-                        pa_mma<true>(sc[t], qa[(q * 4 + 2) % NMMA], pg_e4m3x2_to_f16x2(w.z & 0xffffu), pg_e4m3x2_to_f16x2(w.z >> 16));
-                        pa_mma<true>(sc[t], qa[(q * 4 + 3) % NMMA], pg_e4m3x2_to_f16x2(w.w & 0xffffu), pg_e4m3x2_to_f16x2(w.w >> 16));
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const uint32_t a0 = pg_e4m3x2_to_f16x2(wa[x] & 0xffffu), a1 = pg_e4m3x2_to_f16x2(ya[x] & 0xffffu);
+                            const uint32_t a2 = pg_e4m3x2_to_f16x2(wa[x] >> 16), a3 = pg_e4m3x2_to_f16x2(ya[x] >> 16);
+                            const int i = (q * 4 + x) % NMMA;
+                            pa_mma<FP8>(sc[t], a0, a1, a2, a3, qh[i][0], qh[i][1]);
+                            if (EX) pa_mma<FP8>(sc[t], a0, a1, a2, a3, ql[i % (EX ? NMMA : 1)][0], ql[i % (EX ? NMMA : 1)][1]);
+                        }
                     } else {
-                        pa_mma<false>(sc[t], qa[q * 2 % NMMA], w.x, w.y);
-                        pa_mma<false>(sc[t], qa[(q * 2 + 1) % NMMA], w.z, w.w);
-                    }
-                }
-            }
-            float s[4] = {(sc[0][0] + sc[0][2]) * qs, (sc[0][1] + sc[0][3]) * qs, (sc[1][0] + sc[1][2]) * qs, (sc[1][1] + sc[1][3]) * qs};
-            float sv[4];
-            if (FP8) {
-                const uint32_t e = exps + st * 32 + 2 * j;
-                uint16_t k0, k1, v0, v1;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(k0) : "r"(e));
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(k1) : "r"(e + 8));
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v0) : "r"(e + 16));
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v1) : "r"(e + 24));
-                s[0] *= pg_scale(k0 & 0xffu);
-                s[1] *= pg_scale(k0 >> 8);
-                s[2] *= pg_scale(k1 & 0xffu);
-                s[3] *= pg_scale(k1 >> 8);
-                sv[0] = (float)(int)(v0 & 0xffu) - 127.f;
-                sv[1] = (float)(int)(v0 >> 8) - 127.f;
-                sv[2] = (float)(int)(v1 & 0xffu) - 127.f;
-                sv[3] = (float)(int)(v1 >> 8) - 127.f;
-            }
-            // positions that do not count
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t r = t * 8 + 2 * j;
-                const uint32_t lp = UPT == 1 ? lps[st * 4] : lps[st * 4 + (r >> 2)];
-                const uint32_t p = lp + (UPT == 1 ? r : (r & 3u));
-                const bool none = lp == PA_NONE;
-                if (none || p < cq.lo || p >= cq.len) s[2 * t] = -INFINITY;
-                if (none || p + 1u < cq.lo || p + 1u >= cq.len) s[2 * t + 1] = -INFINITY;
-            }
-            float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
-            float p[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = pa_ex2(s[i] - mu);
-            l = l * pa_ex2(m - mu) + ((p[0] + p[1]) + (p[2] + p[3]));
-            float old = m, ref = mn;
-            if (FP8) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sv[i] += s[i];
-                mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                old = mw;
-                ref = mw = fmaxf(mw, mx);
-                const float wu = ref == -INFINITY ? 0.f : ref - 14.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = pa_ex2(sv[i] - wu);
-            }
-            m = mn;
-            if (__any_sync(0xffffffffu, ref > old)) {
-                const float f = ref == -INFINITY ? 1.f : pa_ex2(old - ref);
-#pragma unroll
-                for (int i = 0; i < NOUT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] *= f;
-            }
-            uint32_t pa[4];
-            pa_split<FP8>(p[0], p[1], pa[0], pa[1]);
-            pa_split<FP8>(p[2], p[3], pa[2], pa[3]);
-            if (FP8) {
-                constexpr int VW = HD >= 128 ? 4 : 2;            // words of a lane's piece of a row
-#pragma unroll
-                for (int hh = 0; hh < HD / (32 * VW); ++hh) {
-                    uint32_t r[4][4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {                // rows 2j, 2j + 1, 2j + 8, 2j + 9
-                        const uint32_t row = 2 * j + (x & 1) + (x >> 1) * 8;
-                        if (VW == 4) {
-                            const uint4 w = pa_lds16(vd + row * ROW + (((hh * 8 + g) ^ (row & 7u)) << 4));
-                            r[x][0] = w.x; r[x][1] = w.y; r[x][2] = w.z; r[x][3] = w.w;
-                        } else {
-                            const uint2 w = pa_lds8(vd + row * ROW + (((g >> 1) ^ ((row >> 1) & 3u)) << 4) + (g & 1u) * 8u);
-                            r[x][0] = w.x; r[x][1] = w.y;
+                        for (int x = 0; x < 2; ++x) {
+                            const int i = (q * 2 + x) % NMMA;
+                            pa_mma<FP8>(sc[t], wa[2 * x], ya[2 * x], wa[2 * x + 1], ya[2 * x + 1], qh[i][0], qh[i][1]);
+                            if (EX) pa_mma<FP8>(sc[t], wa[2 * x], ya[2 * x], wa[2 * x + 1], ya[2 * x + 1], ql[i % (EX ? NMMA : 1)][0], ql[i % (EX ? NMMA : 1)][1]);
                         }
                     }
+                }
 #pragma unroll
-                    for (int w = 0; w < VW; ++w) {
-                        const uint32_t a01 = __byte_perm(r[0][w], r[1][w], 0x5140), a23 = __byte_perm(r[0][w], r[1][w], 0x7362);
-                        const uint32_t b01 = __byte_perm(r[2][w], r[3][w], 0x5140), b23 = __byte_perm(r[2][w], r[3][w], 0x7362);
-                        float (*oo)[4] = o + hh * 16 + w * 4;
-                        pa_mma<true>(oo[0], pa, pg_e4m3x2_to_f16x2(a01 & 0xffffu), pg_e4m3x2_to_f16x2(b01 & 0xffffu));
-                        pa_mma<true>(oo[1], pa, pg_e4m3x2_to_f16x2(a01 >> 16), pg_e4m3x2_to_f16x2(b01 >> 16));
-                        pa_mma<true>(oo[2], pa, pg_e4m3x2_to_f16x2(a23 & 0xffffu), pg_e4m3x2_to_f16x2(b23 & 0xffffu));
-                        pa_mma<true>(oo[3], pa, pg_e4m3x2_to_f16x2(a23 >> 16), pg_e4m3x2_to_f16x2(b23 >> 16));
+            for (int x = 0; x < 2 * NS; ++x) {
+                float f0 = qs[0], f1 = qs[1], ev = 0.f;
+                if (FP8) {
+                    uint32_t ke, ve;
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ke) : "r"(exps + st * 64 + x * 8 + g));
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ve) : "r"(exps + st * 64 + 32 + x * 8 + g));
+                    f0 *= pg_scale(ke);
+                    f1 *= pg_scale(ke);
+                    ev = (float)(int)ve - 127.f;
+                }
+                s[2 * x] = sc[x / 2][x % 2 * 2] * f0;
+                s[2 * x + 1] = sc[x / 2][x % 2 * 2 + 1] * f1;
+                if (FP8) sv[2 * x] = sv[2 * x + 1] = ev;
+            }
+            if (!lps[st * 12 + 8]) {   // positions that do not count
+#pragma unroll
+                for (int x = 0; x < 2 * NS; ++x) {
+                    const uint32_t r = x * 8 + g, lp = lps[st * 12 + r / UR], p = lp + r % UR;
+                    if (lp == PA_NONE || p < cq.lo || p >= cq.len) s[2 * x] = s[2 * x + 1] = -INFINITY;
+                }
+            }
+            float mx[2] = {s[0], s[1]}, mv[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 2; i < 4 * NS; ++i) mx[i & 1] = fmaxf(mx[i & 1], s[i]);
+            if (FP8)
+#pragma unroll
+                for (int i = 0; i < 4 * NS; ++i) {
+                    sv[i] += s[i];
+                    mv[i & 1] = fmaxf(mv[i & 1], sv[i]);
+                }
+            bool high = mx[0] > m[0] + 8.f || mx[1] > m[1] + 8.f;
+            if (FP8) high = high || mv[0] > mw[0] + 8.f || mv[1] > mw[1] + 8.f;
+            if (__any_sync(0xffffffffu, high)) {   // raise the references to the maxima seen
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                    for (int k = 4; k < 32; k <<= 1) {
+                        mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], k));
+                        if (FP8) mv[x] = fmaxf(mv[x], __shfl_xor_sync(0xffffffffu, mv[x], k));
+                    }
+                    const float mn = fmaxf(m[x], mx[x]), f = mn == m[x] ? 1.f : pa_ex2(m[x] - mn);
+                    m[x] = mn;
+                    l[x] *= f;
+                    float fo = f;
+                    if (FP8) {
+                        const float wn = fmaxf(mw[x], mv[x]);
+                        fo = wn == mw[x] ? 1.f : pa_ex2(mw[x] - wn);
+                        mw[x] = wn;
+                    }
+#pragma unroll
+                    for (int i = 0; i < NMMA; ++i) {
+                        o[i][x] *= fo;
+                        o[i][x + 2] *= fo;
                     }
                 }
-            } else {
-                const uint32_t row = (lane >> 3 & 1u) * 8u + (lane & 7u), base = vd + row * ROW, fv = (row & 1u) << 2 | ((row >> 1) & 3u);
+            }
+            float p[4 * NS];
+            {
+                const float mu[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+                const float wu[2] = {mw[0] == -INFINITY ? 0.f : mw[0] - 7.f, mw[1] == -INFINITY ? 0.f : mw[1] - 7.f};
 #pragma unroll
-                for (int i = 0; i < HD / 16; ++i) {
-                    uint32_t r[4];
-                    ldmatrix_x4_trans(r, base + (((i * 2 + (lane >> 4)) ^ fv) << 4));
-                    pa_mma<false>(o[2 * i], pa, r[0], r[1]);
-                    pa_mma<false>(o[2 * i + 1], pa, r[2], r[3]);
+                for (int i = 0; i < 4 * NS; ++i) {
+                    p[i] = pa_ex2(s[i] - mu[i & 1]);
+                    l[i & 1] += p[i];
+                    if (FP8) p[i] = pa_ex2(sv[i] - wu[i & 1]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                const uint32_t h0 = pa_round<FP8>(p[4 * t], p[4 * t + 1]), h1 = pa_round<FP8>(p[4 * t + 2], p[4 * t + 3]);
+                const uint32_t b0 = movmatrix_trans(h0), b1 = movmatrix_trans(h1);
+                uint32_t c0 = 0u, c1 = 0u;
+                constexpr bool REST = KL_PA_REST || EX || !FP8;
+                if (REST) {
+                    c0 = movmatrix_trans(pa_rest<FP8>(p[4 * t], p[4 * t + 1], h0));
+                    c1 = movmatrix_trans(pa_rest<FP8>(p[4 * t + 2], p[4 * t + 3], h1));
+                }
+                const uint32_t vs = vd + t * 16 * ROW;
+                if (FP8) {
+                    constexpr int VW = HD >= 128 ? 4 : 2;            // words of a lane's piece of a row
+#pragma unroll
+                    for (int hh = 0; hh < HD / (32 * VW); ++hh) {
+                        uint32_t r[4][4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {                // rows 2j, 2j + 1, 2j + 8, 2j + 9
+                            const uint32_t row = 2 * j + (x & 1) + (x >> 1) * 8;
+                            if (VW == 4) {
+                                const uint4 w = pa_lds16(vs + row * ROW + (((hh * 8 + g) ^ (row & 7u)) << 4));
+                                r[x][0] = w.x; r[x][1] = w.y; r[x][2] = w.z; r[x][3] = w.w;
+                            } else {
+                                const uint2 w = pa_lds8(vs + row * ROW + (((g >> 1) ^ ((row >> 1) & 3u)) << 4) + (g & 1u) * 8u);
+                                r[x][0] = w.x; r[x][1] = w.y;
+                            }
+                        }
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) {
+                            const uint32_t a01 = __byte_perm(r[0][w], r[1][w], 0x5140), a23 = __byte_perm(r[0][w], r[1][w], 0x7362);
+                            const uint32_t b01 = __byte_perm(r[2][w], r[3][w], 0x5140), b23 = __byte_perm(r[2][w], r[3][w], 0x7362);
+                            float (*oo)[4] = o + hh * 8 + w * 2;
+                            const uint32_t x0 = pg_e4m3x2_to_f16x2(a01 & 0xffffu), x1 = pg_e4m3x2_to_f16x2(a01 >> 16);
+                            const uint32_t x2 = pg_e4m3x2_to_f16x2(b01 & 0xffffu), x3 = pg_e4m3x2_to_f16x2(b01 >> 16);
+                            const uint32_t y0 = pg_e4m3x2_to_f16x2(a23 & 0xffffu), y1 = pg_e4m3x2_to_f16x2(a23 >> 16);
+                            const uint32_t y2 = pg_e4m3x2_to_f16x2(b23 & 0xffffu), y3 = pg_e4m3x2_to_f16x2(b23 >> 16);
+                            pa_mma<FP8>(oo[0], x0, x1, x2, x3, b0, b1);
+                            pa_mma<FP8>(oo[1], y0, y1, y2, y3, b0, b1);
+                            if (REST) {
+                                pa_mma<FP8>(oo[0], x0, x1, x2, x3, c0, c1);
+                                pa_mma<FP8>(oo[1], y0, y1, y2, y3, c0, c1);
+                            }
+                        }
+                    }
+                } else {
+                    // matrices of a load: positions 0..7 and 8..15 of two neighbouring pieces of eight columns
+                    const uint32_t row = (lane >> 4) * 8u + (lane & 7u), base = vs + row * ROW, fv = (row & 1u) << 2 | ((row >> 1) & 3u);
+#pragma unroll
+                    for (int i = 0; i < NMMA; ++i) {
+                        uint32_t r[4];
+                        ldmatrix_x4_trans(r, base + (((i * 2 + (lane >> 3 & 1u)) ^ fv) << 4));
+                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], b0, b1);
+                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], c0, c1);
+                    }
                 }
             }
             if (++st == ST) st = 0;
 
             ++ct;
             if (ct == cq.nt || k + 1u == total) {   // the pair ends here, for this warp at least
-                const uint32_t h = cph / a.HT, hg = (cph - h * a.HT) * 8u + g, hq = h * a.G + hg;
-                const bool live = hg < a.G, whole = seg0 == 0u && ct == cq.nt;
-                if (whole) {
-                    float inv = 0.f;
-                    end_pair([&](uint32_t d, float v0, float v1) {
-                        inv = l == 0.f ? 0.f : 1.f / l;
-                        if (live) pa_store2(c, a, cs, hq, d, v0 * inv, v1 * inv);
-                    });
-                    if (live && j == 0u) pa_store_lse(a, cs, hq, m, l);
-                } else {
-                    const bool tail = k + 1u == total;
+                const uint32_t h = cph / a.HT, hg = (cph - h * a.HT) * 8u + 2u * j, hq = h * a.G + hg;
+                const bool whole = seg0 == 0u && ct == cq.nt, tail = k + 1u == total;
+                float* dst = nullptr;
+                float2* ml = nullptr;
+                if (!whole) {
                     Entry& e = tail ? last : first;
                     e = {1u, cs, cph, seg0 == 0u, ct == cq.nt};
-                    float* dst;
-                    float2* ml;
                     if (tail) {   // the ring has been read to the end
                         asm volatile("cp.async.wait_group 0;" ::: "memory");
                         __syncwarp();
@@ -979,93 +1059,97 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8>::NW * 32, 1) kl_paged_attn_kern
                         dst = a.head + slot * 8 * HD;
                         ml = reinterpret_cast<float2*>(a.head_ml) + slot * 8;
                     }
-                    end_pair([&](uint32_t d, float v0, float v1) { *reinterpret_cast<float2*>(dst + g * HD + d) = make_float2(v0, v1); });
-                    if (j == 0u) ml[g] = make_float2(m, l);
                 }
-                if (k + 1u < total) {
+                end_pair([&](int x, uint32_t d, float v0, float v1) {
+                    if (!whole) {
+                        dst[(2 * j + x) * HD + d] = v0;
+                        dst[(2 * j + x) * HD + d + (FP8 ? 1 : 8)] = v1;
+                    } else if (hg + x < a.G) {
+                        const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
+                        if (FP8) {
+                            pa_store2(c, a, cs, hq + x, d, v0 * inv, v1 * inv);
+                        } else {
+                            pa_store1(c, a, cs, hq + x, d, v0 * inv);
+                            pa_store1(c, a, cs, hq + x, d + 8u, v1 * inv);
+                        }
+                    }
+                });
+                if (g == 0u)
+                    for (int x = 0; x < 2; ++x) {
+                        if (!whole) ml[2 * j + x] = make_float2(m[x], l[x]);
+                        else if (hg + x < a.G) pa_store_lse(a, cs, hq + x, m[x], l[x]);
+                    }
+                if (!tail) {
                     ct = seg0 = 0;
+                    fresh = true;
                     if (++cph == PH) {
                         cph = 0;
-                        do cq = pa_seq(c, a, length(++cs));
+                        do cq = pa_seq<TP>(c, a, length(++cs));
                         while (cq.nt == 0u);
                     }
-                    begin_pair();
                 }
             }
+            ++k;
         }
+        if (last.valid) last_tiles = cq.nt - ct;   // tiles of its last pair that lie in later ranges
     }
 
     // ---- the partial results of this block's warps, in the order of the list: first[0], last[0], first[1], ...
-    __syncthreads();   // everyone is done with `wsum`, and with the lengths
-    uint32_t* ent = lens;   // [2 NW][4]: valid | begins << 1 | ends << 2, s, ph
-    if (lane == 0u) {
-        for (int x = 0; x < 2; ++x) {
-            const Entry& e = x ? last : first;
-            uint32_t* t = ent + (2 * warp + x) * 4;
-            t[0] = e.valid | e.begins << 1 | e.ends << 2;
-            t[1] = e.s;
-            t[2] = e.ph;
-        }
+    __syncthreads();   // everyone is done with the lengths
+    uint4* ent = reinterpret_cast<uint4*>(lens);   // [2 NW]: (valid | begins << 1 | ends << 2, s, ph, tiles in later ranges)
+    if (lane < 2u) {
+        const Entry e = lane ? last : first;
+        ent[2 * warp + lane] = make_uint4(e.valid | e.begins << 1 | e.ends << 2, e.s, e.ph, lane ? last_tiles : 0u);
     }
-    __threadfence_block();
+    __threadfence_block();   // the first results lie in global memory
     __syncthreads();
     int4 meta = make_int4(0, 0, 0, 0);
     for (uint32_t e0 = 0; e0 < 2u * NW;) {
-        if (!(ent[e0 * 4] & 1u)) {
+        const uint4 head = ent[e0];
+        if (!(head.x & 1u)) {
             ++e0;
             continue;
         }
-        uint32_t e1 = e0 + 1u, end = e0;   // entries [e0, e1) of one pair, `end` the last of them
-        while (e1 < 2u * NW && (!(ent[e1 * 4] & 1u) || (ent[e1 * 4 + 1] == ent[e0 * 4 + 1] && ent[e1 * 4 + 2] == ent[e0 * 4 + 2]))) {
-            if (ent[e1 * 4] & 1u) end = e1;
-            ++e1;
+        uint32_t mask = 1u << e0, e1 = e0 + 1u;   // entries of one pair
+        uint4 end = head;                         // the last of them
+        for (; e1 < 2u * NW; ++e1) {
+            const uint4 x = ent[e1];
+            if (!(x.x & 1u)) continue;
+            if (x.y != head.y || x.z != head.z) break;
+            mask |= 1u << e1;
+            end = x;
         }
-        const uint32_t s = ent[e0 * 4 + 1], ph = ent[e0 * 4 + 2], h = ph / a.HT, h0 = (ph - h * a.HT) * 8u;
-        const bool begins = ent[e0 * 4] & 2u, ends = ent[end * 4] & 4u, whole = begins && ends;
+        const uint32_t s = head.y, ph = head.z, h = ph / a.HT, h0 = (ph - h * a.HT) * 8u;
+        const bool begins = head.x & 2u, whole = begins && (end.x & 4u);
         const size_t slot = (size_t)blockIdx.x * 2 + (begins ? 1 : 0);
-        if (!whole) {
-            if (begins) {
-                meta.x |= PA_SECOND;
-                meta.y = (int)s;
-                meta.z = (int)ph;
-            } else {
-                meta.x |= PA_FIRST | (ends ? 0 : PA_FIRST_GOES_ON);
-            }
+        if (begins && !whole) {   // the last block that shares the pair: the one that holds its last tile
+            const uint64_t last_tile = b_lo + b_n - 1u + end.w;
+            const uint64_t wide = (share + 1u) * over;
+            const uint64_t lb = last_tile < wide ? pa_div(last_tile, (uint32_t)share + 1u) : over + pa_div(last_tile - wide, (uint32_t)share);
+            meta = make_int4(1, (int)s, (int)ph, (int)lb);
         }
         const uint32_t heads = min(8u, a.G - h0);
         for (uint32_t i = tid; i < heads * (HD / 2); i += NT) {
             const uint32_t hh = i / (HD / 2), d = i % (HD / 2) * 2u;
-            auto rec = [&](uint32_t e, const float*& o, float2& ml) {
-                const size_t gs = (size_t)blockIdx.x * NW + e / 2u;
+            auto record = [&](uint32_t e, float2& ml) -> const float* {
                 if (e & 1u) {
-                    o = reinterpret_cast<const float*>(pa_smem + (e / 2u) * (ST * 2 * TILE));
                     ml = ml_all[(e / 2u) * 8 + hh];
-                } else {
-                    o = a.head + gs * 8 * HD;
-                    ml = reinterpret_cast<const float2*>(a.head_ml)[gs * 8 + hh];
+                    return reinterpret_cast<const float*>(pa_smem + (e / 2u) * (ST * 2 * TILE)) + hh * HD + d;
                 }
-                o += hh * HD + d;
+                const size_t gs = ((size_t)blockIdx.x * NW + e / 2u) * 8 + hh;
+                ml = reinterpret_cast<const float2*>(a.head_ml)[gs];
+                return a.head + gs * HD + d;
             };
             float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
-            for (uint32_t e = e0; e < e1; ++e)
-                if (ent[e * 4] & 1u) {
-                    const float* o;
-                    float2 ml;
-                    rec(e, o, ml);
-                    M = fmaxf(M, ml.x);
-                }
-            const float mu = M == -INFINITY ? 0.f : M;
-            for (uint32_t e = e0; e < e1; ++e)
-                if (ent[e * 4] & 1u) {
-                    const float* o;
-                    float2 ml;
-                    rec(e, o, ml);
-                    const float f = pa_ex2(ml.x - mu);
-                    const float2 x = *reinterpret_cast<const float2*>(o);
-                    L += ml.y * f;
-                    v0 += x.x * f;
-                    v1 += x.y * f;
-                }
+            for (uint32_t x = mask; x; x &= x - 1u) {   // in the order of the list
+                float2 ml;
+                const float2 o = *reinterpret_cast<const float2*>(record(__ffs(x) - 1, ml));
+                const float mn = fmaxf(M, ml.x), mu = mn == -INFINITY ? 0.f : mn, f = pa_ex2(M - mu), w = pa_ex2(ml.x - mu);
+                M = mn;
+                L = L * f + ml.y * w;
+                v0 = v0 * f + o.x * w;
+                v1 = v1 * f + o.y * w;
+            }
             if (whole) {
                 const float inv = L == 0.f ? 0.f : 1.f / L;
                 pa_store2(c, a, s, h * a.G + h0 + hh, d, v0 * inv, v1 * inv);
@@ -1086,37 +1170,39 @@ constexpr int PA_MERGE_THREADS = 128;
 constexpr int PA_MAX_BLOCKS = 256;
 __global__ void __launch_bounds__(PA_MERGE_THREADS) kl_paged_merge_kernel(const PagedView c, const PagedAttn a) {
     __shared__ float2 ml[PA_MAX_BLOCKS];
-    __shared__ int end_s;
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const int b = (int)blockIdx.x, nb = (int)gridDim.x, tid = (int)threadIdx.x;
+    const int b = (int)blockIdx.x, tid = (int)threadIdx.x;
     const int4 meta = a.meta[b];
     const uint32_t s = (uint32_t)meta.y, ph = (uint32_t)meta.z, h = ph / a.HT, h0 = (ph - h * a.HT) * 8u, hh = blockIdx.y;
-    if (!(meta.x & PA_SECOND) || h0 + hh >= a.G) return;
-    if (tid == 0) end_s = nb - 1;
-    __syncthreads();
-    for (int i = b + 1 + tid; i < nb; i += PA_MERGE_THREADS)   // the last block that shares the pair
-        if (!(a.meta[i].x & PA_FIRST_GOES_ON)) atomicMin(&end_s, i);
-    __syncthreads();
-    const int cnt = end_s - b + 1;
+    if (!meta.x || h0 + hh >= a.G) return;
+    const int cnt = meta.w - b + 1;   // blocks b .. meta.w
     auto slot = [&](int i) { return i == 0 ? (size_t)b * 2 + 1 : (size_t)(b + i) * 2; };
     for (int i = tid; i < cnt; i += PA_MERGE_THREADS) ml[i] = reinterpret_cast<const float2*>(a.part_ml)[slot(i) * 8 + hh];
+    const uint32_t d = 2u * tid, dd = d < c.hd ? d : 0u;
+    constexpr int AHEAD = 16;   // records loaded before the maximum is known
+    float2 x[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < cnt) x[i] = *reinterpret_cast<const float2*>(a.part + (slot(i) * 8 + hh) * c.hd + dd);
     __syncthreads();
     float M = -INFINITY;
     for (int i = 0; i < cnt; ++i) M = fmaxf(M, ml[i].x);
     const float mu = M == -INFINITY ? 0.f : M;
-    const uint32_t d = 2u * tid;
-    if (d >= c.hd) return;
     float L = 0.f, v0 = 0.f, v1 = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < cnt; ++i) {
+    auto add = [&](int i, float2 y) {
         const float f = pa_ex2(ml[i].x - mu);
-        const float2 x = *reinterpret_cast<const float2*>(a.part + (slot(i) * 8 + hh) * c.hd + d);
         L += ml[i].y * f;
-        v0 += x.x * f;
-        v1 += x.y * f;
-    }
+        v0 += y.x * f;
+        v1 += y.y * f;
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < cnt) add(i, x[i]);
+#pragma unroll 8
+    for (int i = AHEAD; i < cnt; ++i) add(i, *reinterpret_cast<const float2*>(a.part + (slot(i) * 8 + hh) * c.hd + dd));
+    if (d >= c.hd) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;
     pa_store2(c, a, s, h * a.G + h0 + hh, d, v0 * inv, v1 * inv);
     if (d == 0u) pa_store_lse(a, s, h * a.G + h0 + hh, M, L);
