@@ -130,16 +130,13 @@ int attn_blocks() {
 }
 
 // Function attributes hold per device: set them on a kernel's first launch there (`done`: one bit per device; devices
-// beyond 63 set them every time).  All kernels of the attention ask for the largest shared-memory carve-out, so that an SM
-// can hold blocks of both at once and is not reconfigured between them.
+// beyond 63 set them every time).
 kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return KL_ERR_CUDA;
     const uint64_t bit = dev < 64 ? 1ull << dev : 0;
     if (bit && (done.load(std::memory_order_relaxed) & bit)) return KL_OK;
-    if (cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
-        (smem && cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess))
-        return KL_ERR_CUDA;
+    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return KL_ERR_CUDA;
     done.fetch_or(bit, std::memory_order_relaxed);
     return KL_OK;
 }
@@ -273,8 +270,6 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     a.head_ml = (float*)(ws + sp.head_ml);
     a.meta = (int4*)(ws + sp.meta);
     if ((rc = launch_attn(v, a, blocks, stream)) != KL_OK) return rc;
-    static std::atomic<uint64_t> done{0};
-    if ((rc = prepare((const void*)kl_paged_merge_kernel, 0, done)) != KL_OK) return rc;
     return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
 }
 

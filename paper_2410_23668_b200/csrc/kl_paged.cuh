@@ -672,12 +672,9 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     const uint32_t exps = smem_u32(exps_all) + warp * (ST * 64);
     volatile uint32_t* lps = lps_all + warp * (ST * 12);
     if (lo < hi) {
-        uint32_t i0 = 0, i1 = NT;
-        while (i1 - i0 > 1u) {
-            const uint32_t mid = (i0 + i1) / 2u;
-            if (pre[mid] <= lo) i0 = mid;
-            else i1 = mid;
-        }
+        // the largest i0 with pre[i0] <= lo: which of 32 groups of NW entries, then which entry
+        uint32_t i0 = (__popc(__ballot_sync(0xffffffffu, pre[lane * NW] <= lo)) - 1) * NW;
+        i0 += __popc(__ballot_sync(0xffffffffu, lane < (uint32_t)NW && pre[i0 + lane % NW] <= lo)) - 1;
         uint64_t rem = lo - pre[i0];
         uint32_t cs = i0 * per;                    // cursor of the tiles that are consumed
         PaSeq cq = pa_seq<TP>(c, a, length(cs));
@@ -797,32 +794,36 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         // ---- state of the pair under way.  Queries: head g; scores and results: heads 2j and 2j + 1
         uint32_t qh[NMMA][2], ql[EX ? NMMA : 1][2];
         float o[NMMA][4], m[2], l[2], mw[2], qs[2];
-        auto begin_pair = [&]() {
+        constexpr int PIECE = FP8 ? 16 : 8;   // consecutive columns of a lane per 16-byte piece of a row
+        uint32_t raw[NMMA][EX ? 4 : 2];       // the lane's columns of query head g, as they lie in memory
+        auto load_queries = [&]() {
             const uint32_t h = cph / a.HT, hg = (cph - h * a.HT) * 8u + g;
-            const bool live = hg < a.G;
-            const uint8_t* q = a.q + (int64_t)cs * a.q_stride;
-            const uint32_t base = (h * a.G + hg) * HD;
-            float x[NMMA][4];
-            constexpr int PIECE = FP8 ? 16 : 8;   // consecutive columns of a lane per 16-byte piece of a row
-            float big = 0.f;
+            const uint8_t* q = a.q + (int64_t)cs * a.q_stride + (size_t)(h * a.G + hg) * HD * (EX ? 4 : 2);
 #pragma unroll
             for (int i = 0; i < NMMA; ++i) {
                 const uint32_t d = (i / (PIECE / 4)) * (4 * PIECE) + j * PIECE + (i % (PIECE / 4)) * 4;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][e] = 0.f;
-                if (live) {
+                for (int e = 0; e < (EX ? 4 : 2); ++e) raw[i][e] = 0u;
+                if (hg < a.G) {
                     if (EX) {
-                        const float4 f = *reinterpret_cast<const float4*>(q + (size_t)(base + d) * 4);
-                        x[i][0] = f.x; x[i][1] = f.y; x[i][2] = f.z; x[i][3] = f.w;
+                        const uint4 f = *reinterpret_cast<const uint4*>(q + d * 4);
+                        raw[i][0] = f.x; raw[i][1] = f.y; raw[i][EX ? 2 : 0] = f.z; raw[i][EX ? 3 : 0] = f.w;
                     } else {
-                        const uint2 f = *reinterpret_cast<const uint2*>(q + (size_t)(base + d) * 2);
-                        x[i][0] = bf_lo(f.x); x[i][1] = bf_hi(f.x); x[i][2] = bf_lo(f.y); x[i][3] = bf_hi(f.y);
+                        const uint2 f = *reinterpret_cast<const uint2*>(q + d * 2);
+                        raw[i][0] = f.x; raw[i][1] = f.y;
                     }
                 }
-                if (FP8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) big = fmaxf(big, fabsf(x[i][e]));
             }
+        };
+        auto begin_pair = [&]() {
+            float x[NMMA][4], big = 0.f;
+#pragma unroll
+            for (int i = 0; i < NMMA; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[i][e] = EX ? __uint_as_float(raw[i][e % (EX ? 4 : 2)]) : e & 1 ? bf_hi(raw[i][e / 2]) : bf_lo(raw[i][e / 2]);
+                    if (FP8) big = fmaxf(big, fabsf(x[i][e]));
+                }
             float mul = a.scale_log2, f = 1.f;
             if (FP8) {   // f16 operands: the head's largest query element comes to lie in [2^14, 2^15)
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
@@ -846,14 +847,15 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             m[0] = m[1] = mw[0] = mw[1] = -INFINITY;
             l[0] = l[1] = 0.f;
         };
-        // The pair's result over the tiles seen, relative to 2^m: emit(x, d, v0, v1) gets columns d and d + 1 of head 2j + x
-        // (e4m3), or d and d + 8 (bf16).
-        auto end_pair = [&](auto&& emit) {
+        // The pair's result over the tiles seen: emit(x, d, v0, v1) gets columns d and d + 1 (e4m3), or d and d + 8 (bf16), of
+        // head 2j + x; the sums themselves, relative to 2^m, or divided by l.
+        auto end_pair = [&](bool divide, auto&& emit) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
                 for (int k = 4; k < 32; k <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], k);
-                const float f = !FP8 ? 1.f : mw[x] == -INFINITY ? 0.f : pa_ex2(mw[x] - m[x] - 7.f);
+                float f = !FP8 ? 1.f : mw[x] == -INFINITY ? 0.f : pa_ex2(mw[x] - m[x] - 7.f);
+                if (divide) f = l[x] == 0.f ? 0.f : f / l[x];
                 constexpr int W16 = HD >= 128 ? 16 : 8;   // columns of a lane's V piece (e4m3)
 #pragma unroll
                 for (int i = 0; i < NMMA; ++i) {
@@ -868,8 +870,14 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         bool fresh = true;                            // the next tile starts a pair
         uint32_t to = 0;                              // ring slot of the next request
         uint32_t k = 0, st = 0;                       // tile of the range, and its slot
+        load_queries();
         for (uint32_t ahead = 0; k < total;) {
             if (ahead >= (uint32_t)ST - 1u) {
+                if (fresh) {   // while the tile is on its way
+                    if (k) load_queries();
+                    begin_pair();
+                    fresh = false;
+                }
                 asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
                 __syncwarp();   // the tile is there for every lane, and every lane is done with the previous one
             }
@@ -880,9 +888,6 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 ++ahead;
                 continue;
             }
-            if (fresh) begin_pair();
-            fresh = false;
-
             const uint32_t kd = ring + st * (2 * TILE), vd = kd + TILE;
             // scores: s[2x + e] is that of position 8x + g and head 2j + e
             float sc[NS][4], s[4 * NS], sv[4 * NS];
@@ -1043,42 +1048,45 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             ++ct;
             if (ct == cq.nt || k + 1u == total) {   // the pair ends here, for this warp at least
                 const uint32_t h = cph / a.HT, hg = (cph - h * a.HT) * 8u + 2u * j, hq = h * a.G + hg;
-                const bool whole = seg0 == 0u && ct == cq.nt, tail = k + 1u == total;
-                float* dst = nullptr;
-                float2* ml = nullptr;
-                if (!whole) {
+                const bool tail = k + 1u == total;
+                if (seg0 == 0u && ct == cq.nt) {
+                    end_pair(true, [&](int x, uint32_t d, float v0, float v1) {
+                        if (hg + x >= a.G) return;
+                        if (FP8) {
+                            pa_store2(c, a, cs, hq + x, d, v0, v1);
+                        } else {
+                            pa_store1(c, a, cs, hq + x, d, v0);
+                            pa_store1(c, a, cs, hq + x, d + 8u, v1);
+                        }
+                    });
+                    if (g == 0u && a.lse)
+                        for (int x = 0; x < 2; ++x)
+                            if (hg + x < a.G) pa_store_lse(a, cs, hq + x, m[x], l[x]);
+                } else {
                     Entry& e = tail ? last : first;
                     e = {1u, cs, cph, seg0 == 0u, ct == cq.nt};
+                    float* dst = a.head + ((size_t)blockIdx.x * NW + warp) * 8 * HD;
+                    float2* ml = reinterpret_cast<float2*>(a.head_ml) + ((size_t)blockIdx.x * NW + warp) * 8;
                     if (tail) {   // the ring has been read to the end
                         asm volatile("cp.async.wait_group 0;" ::: "memory");
                         __syncwarp();
                         dst = reinterpret_cast<float*>(pa_smem + warp * (ST * 2 * TILE));
                         ml = ml_all + warp * 8;
-                    } else {
-                        const size_t slot = (size_t)blockIdx.x * NW + warp;
-                        dst = a.head + slot * 8 * HD;
-                        ml = reinterpret_cast<float2*>(a.head_ml) + slot * 8;
+                    }
+                    end_pair(false, [&](int x, uint32_t d, float v0, float v1) {
+                        float* to = dst + (2 * j + x) * HD + d;
+                        if (FP8) {
+                            *reinterpret_cast<float2*>(to) = make_float2(v0, v1);
+                        } else {
+                            to[0] = v0;
+                            to[8] = v1;
+                        }
+                    });
+                    if (g == 0u) {
+                        ml[2 * j] = make_float2(m[0], l[0]);
+                        ml[2 * j + 1] = make_float2(m[1], l[1]);
                     }
                 }
-                end_pair([&](int x, uint32_t d, float v0, float v1) {
-                    if (!whole) {
-                        dst[(2 * j + x) * HD + d] = v0;
-                        dst[(2 * j + x) * HD + d + (FP8 ? 1 : 8)] = v1;
-                    } else if (hg + x < a.G) {
-                        const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
-                        if (FP8) {
-                            pa_store2(c, a, cs, hq + x, d, v0 * inv, v1 * inv);
-                        } else {
-                            pa_store1(c, a, cs, hq + x, d, v0 * inv);
-                            pa_store1(c, a, cs, hq + x, d + 8u, v1 * inv);
-                        }
-                    }
-                });
-                if (g == 0u)
-                    for (int x = 0; x < 2; ++x) {
-                        if (!whole) ml[2 * j + x] = make_float2(m[x], l[x]);
-                        else if (hg + x < a.G) pa_store_lse(a, cs, hq + x, m[x], l[x]);
-                    }
                 if (!tail) {
                     ct = seg0 = 0;
                     fresh = true;
@@ -1103,26 +1111,23 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     }
     __threadfence_block();   // the first results lie in global memory
     __syncthreads();
+    // lane e of every warp holds entry e; runs of valid entries of the same pair start at the bits of `starts`
+    const uint4 mine_e = lane < 2u * NW ? ent[lane] : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t valid = __ballot_sync(0xffffffffu, mine_e.x & 1u), below = valid & ((1u << lane) - 1u);
+    const int prev = below ? 31 - __clz(below) : 0;
+    const uint32_t ps = __shfl_sync(0xffffffffu, mine_e.y, prev), pph = __shfl_sync(0xffffffffu, mine_e.z, prev);
+    const uint32_t starts = __ballot_sync(0xffffffffu, (mine_e.x & 1u) && (!below || ps != mine_e.y || pph != mine_e.z));
     int4 meta = make_int4(0, 0, 0, 0);
-    for (uint32_t e0 = 0; e0 < 2u * NW;) {
-        const uint4 head = ent[e0];
-        if (!(head.x & 1u)) {
-            ++e0;
-            continue;
-        }
-        uint32_t mask = 1u << e0, e1 = e0 + 1u;   // entries of one pair
-        uint4 end = head;                         // the last of them
-        for (; e1 < 2u * NW; ++e1) {
-            const uint4 x = ent[e1];
-            if (!(x.x & 1u)) continue;
-            if (x.y != head.y || x.z != head.z) break;
-            mask |= 1u << e1;
-            end = x;
-        }
+    for (uint32_t rest = starts; rest; rest &= rest - 1u) {
+        const int e0 = __ffs(rest) - 1;
+        const uint32_t after = rest & (rest - 1u);
+        const uint32_t mask = valid & ~((1u << e0) - 1u) & (after ? (1u << (__ffs(after) - 1)) - 1u : 0xffffffffu);
+        const int e1 = 31 - __clz(mask);   // the run: bits e0 .. e1 of mask
+        const uint4 head = ent[e0], end = ent[e1];
         const uint32_t s = head.y, ph = head.z, h = ph / a.HT, h0 = (ph - h * a.HT) * 8u;
         const bool begins = head.x & 2u, whole = begins && (end.x & 4u);
         const size_t slot = (size_t)blockIdx.x * 2 + (begins ? 1 : 0);
-        if (begins && !whole) {   // the last block that shares the pair: the one that holds its last tile
+        if (begins && !whole && tid == 0u) {   // the last block that shares the pair: the one that holds its last tile
             const uint64_t last_tile = b_lo + b_n - 1u + end.w;
             const uint64_t wide = (share + 1u) * over;
             const uint64_t lb = last_tile < wide ? pa_div(last_tile, (uint32_t)share + 1u) : over + pa_div(last_tile - wide, (uint32_t)share);
@@ -1131,25 +1136,29 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         const uint32_t heads = min(8u, a.G - h0);
         for (uint32_t i = tid; i < heads * (HD / 2); i += NT) {
             const uint32_t hh = i / (HD / 2), d = i % (HD / 2) * 2u;
-            auto record = [&](uint32_t e, float2& ml) -> const float* {
-                if (e & 1u) {
-                    ml = ml_all[(e / 2u) * 8 + hh];
-                    return reinterpret_cast<const float*>(pa_smem + (e / 2u) * (ST * 2 * TILE)) + hh * HD + d;
-                }
-                const size_t gs = ((size_t)blockIdx.x * NW + e / 2u) * 8 + hh;
-                ml = reinterpret_cast<const float2*>(a.head_ml)[gs];
-                return a.head + gs * HD + d;
-            };
+            // the run: last[wa] .. last[wb], and first[wb + 1] where that warp goes on to another pair
+            float2 ml[NW], mf = make_float2(-INFINITY, 0.f);
             float M = -INFINITY, L = 0.f, v0 = 0.f, v1 = 0.f;
-            for (uint32_t x = mask; x; x &= x - 1u) {   // in the order of the list
-                float2 ml;
-                const float2 o = *reinterpret_cast<const float2*>(record(__ffs(x) - 1, ml));
-                const float mn = fmaxf(M, ml.x), mu = mn == -INFINITY ? 0.f : mn, f = pa_ex2(M - mu), w = pa_ex2(ml.x - mu);
-                M = mn;
-                L = L * f + ml.y * w;
-                v0 = v0 * f + o.x * w;
-                v1 = v1 * f + o.y * w;
+            const size_t fs = ((size_t)blockIdx.x * NW + e1 / 2) * 8 + hh;
+            if (!(e1 & 1)) mf = reinterpret_cast<const float2*>(a.head_ml)[fs];
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                ml[w] = mask >> (2 * w + 1) & 1u ? ml_all[w * 8 + hh] : make_float2(-INFINITY, 0.f);
+                M = fmaxf(M, ml[w].x);
             }
+            M = fmaxf(M, mf.x);
+            const float mu = M == -INFINITY ? 0.f : M;
+            auto add = [&](float2 x, const float* o) {
+                const float2 y = *reinterpret_cast<const float2*>(o);
+                const float f = pa_ex2(x.x - mu);
+                L += x.y * f;
+                v0 += y.x * f;
+                v1 += y.y * f;
+            };
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (mask >> (2 * w + 1) & 1u) add(ml[w], reinterpret_cast<const float*>(pa_smem + w * (ST * 2 * TILE)) + hh * HD + d);
+            if (!(e1 & 1)) add(mf, a.head + fs * HD + d);
             if (whole) {
                 const float inv = L == 0.f ? 0.f : 1.f / L;
                 pa_store2(c, a, s, h * a.G + h0 + hh, d, v0 * inv, v1 * inv);
@@ -1159,7 +1168,6 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 if (d == 0u) reinterpret_cast<float2*>(a.part_ml)[slot * 8 + hh] = make_float2(M, L);
             }
         }
-        e0 = e1;
     }
     if (tid == 0u) a.meta[blockIdx.x] = meta;
 }
@@ -1181,13 +1189,14 @@ __global__ void __launch_bounds__(PA_MERGE_THREADS) kl_paged_merge_kernel(const 
     auto slot = [&](int i) { return i == 0 ? (size_t)b * 2 + 1 : (size_t)(b + i) * 2; };
     for (int i = tid; i < cnt; i += PA_MERGE_THREADS) ml[i] = reinterpret_cast<const float2*>(a.part_ml)[slot(i) * 8 + hh];
     const uint32_t d = 2u * tid, dd = d < c.hd ? d : 0u;
-    constexpr int AHEAD = 16;   // records loaded before the maximum is known
+    constexpr int AHEAD = 24;   // records loaded before the maximum is known
     float2 x[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
         if (i < cnt) x[i] = *reinterpret_cast<const float2*>(a.part + (slot(i) * 8 + hh) * c.hd + dd);
     __syncthreads();
     float M = -INFINITY;
+#pragma unroll 8
     for (int i = 0; i < cnt; ++i) M = fmaxf(M, ml[i].x);
     const float mu = M == -INFINITY ? 0.f : M;
     float L = 0.f, v0 = 0.f, v1 = 0.f;
@@ -1198,8 +1207,10 @@ __global__ void __launch_bounds__(PA_MERGE_THREADS) kl_paged_merge_kernel(const 
         v1 += y.y * f;
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-        if (i < cnt) add(i, x[i]);
+    for (int i = 0; i < AHEAD; ++i) {
+        if (i >= cnt) break;
+        add(i, x[i]);
+    }
 #pragma unroll 8
     for (int i = AHEAD; i < cnt; ++i) add(i, *reinterpret_cast<const float2*>(a.part + (slot(i) * 8 + hh) * c.hd + dd));
     if (d >= c.hd) return;
