@@ -7,7 +7,10 @@ module raises at load time.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from pathlib import Path
+
+import torch
 
 _LIB_PATH = Path(__file__).resolve().parent / "libkl.so"
 
@@ -59,6 +62,9 @@ class PagedCacheDesc(C.Structure):
 class PagedSeqs(C.Structure):
     _fields_ = [("positions_d", C.c_void_p), ("page_table_d", C.c_void_p), ("table_stride", C.c_int64), ("table_pages", C.c_uint32),
                 ("n_seqs", C.c_uint32)]
+
+
+_PACK_SEQS = struct.Struct("@PPqII").pack   # a PagedSeqs as bytes: building the ctypes object costs more than the rest of a call
 
 
 _lib = None
@@ -130,7 +136,7 @@ def lib():
     l.kl_set_batched_path.restype = i32
     l.kl_set_dependent_launch.argtypes = [vp, C.c_int]
     l.kl_set_dependent_launch.restype = i32
-    pc, ps, i64 = C.POINTER(PagedCacheDesc), C.POINTER(PagedSeqs), C.c_int64
+    pc, ps, i64 = vp, vp, C.c_int64   # kl_paged_cache *, kl_paged_seqs * (a ctypes structure by reference, or its bytes)
     l.kl_paged_append.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp]
     l.kl_paged_append.restype = i32
     l.kl_paged_read.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp]
@@ -199,7 +205,6 @@ class PagedCache:
     k and v may be None (then page_size and kv_type say what bounds does not).  The tensors must stay alive and in place."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None, bounds=None, page_size=None, kv_type=None):
-        import torch
         self.tensors = (k, v, k_exp, v_exp, bounds)
         where = "PagedCache"
         d = PagedCacheDesc()
@@ -223,12 +228,13 @@ class PagedCache:
         self.device = (bounds if k is None else k).device
         _need(all(t is None or t.device == self.device for t in self.tensors), where)
         self.desc = d
+        self._index = self.device.index if self.device.type == "cuda" else -1
+        self._ref = C.byref(d)
 
     @classmethod
     def allocate(cls, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, kv_type: int = KL_KV_BF16, bounds: bool = False,
                  device="cuda"):
         """A zeroed pool of its own."""
-        import torch
         shape = (n_pages, n_kv_heads, page_size, head_dim)
         dt = torch.bfloat16 if kv_type == KL_KV_BF16 else torch.float8_e4m3fn
         k, v = torch.zeros(shape, dtype=dt, device=device), torch.zeros(shape, dtype=dt, device=device)
@@ -245,102 +251,116 @@ def _need(ok: bool, where: str) -> None:
         raise KlError(KL_ERR_INVALID_ARG, where)
 
 
-def _paged_seqs(cache: PagedCache, positions, page_table, where: str) -> PagedSeqs:
-    import torch
-    _need(positions.dtype == page_table.dtype == torch.int32 and page_table.dim() == 2 and positions.is_contiguous() and
-          page_table.stride(1) == 1 and positions.shape == page_table.shape[:1], where)
+_ROW_TYPES = {torch.float32: KL_F32, torch.bfloat16: KL_BF16}
+_I32, _U8, _F32 = torch.int32, torch.uint8, torch.float32
+
+
+def _here(cache: PagedCache) -> int:
+    """Index of the device the cache lives on if that is the current one (the library launches there); -2 otherwise."""
+    i = cache._index
+    return i if i >= 0 and i == torch.cuda.current_device() else -2
+
+
+def _paged_seqs(dev: int, positions, page_table, where: str):
+    """The sequences of a call as the bytes of a kl_paged_seqs, and their number."""
     n, pages = page_table.shape
-    return PagedSeqs(positions.data_ptr(), page_table.data_ptr(), max(page_table.stride(0), pages) if n <= 1 else page_table.stride(0), pages, n)
+    stride, one = page_table.stride()
+    _need(positions.dtype is _I32 and page_table.dtype is _I32 and one == 1 and positions.numel() == n and positions.is_contiguous() and
+          positions.get_device() == dev and page_table.get_device() == dev, where)
+    return _PACK_SEQS(positions.data_ptr(), page_table.data_ptr(), stride if n > 1 else max(stride, pages), pages, n), n
 
 
-def _row_type(t, where: str) -> int:
-    import torch
-    _need(t.dtype in (torch.float32, torch.bfloat16), where)
-    return KL_F32 if t.dtype == torch.float32 else KL_BF16
+def _flag(dev: int, status, where: str) -> int:
+    if status is None:
+        return 0
+    _need(status.dtype is _I32 and status.get_device() == dev and status.numel() >= 1, where)
+    return status.data_ptr()
 
 
-def _on_device(cache: PagedCache, where: str, *tensors) -> None:
-    """The library launches on the current device: everything has to live there."""
-    import torch
-    dev = cache.device
-    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device() and all(t is None or t.device == dev for t in tensors), where)
-
-
-def _paged_rows(fn: str, cache: PagedCache, k, v, positions, page_table, row_starts, status, stream) -> None:
-    import torch
-    _on_device(cache, fn, k, v, positions, page_table, row_starts, status)
-    d = cache.desc
-    _need(k.shape == v.shape and k.dtype == v.dtype and k.dim() == 3 and tuple(k.shape[1:]) == (d.n_kv_heads, d.head_dim), fn)
-    for t in (k, v):
-        _need(t.stride(2) == 1 and (t.stride(1) == d.head_dim or d.n_kv_heads == 1), fn)
-    n = k.shape[0]
+def _paged_rows(fn: str, call, cache: PagedCache, k, v, positions, page_table, row_starts, status, stream) -> None:
+    dev, d = _here(cache), cache.desc
+    rows, heads, width = shape = k.shape
+    k_row, k_head, k_one = k.stride()
+    v_row, v_head, v_one = v.stride()
+    t = _ROW_TYPES.get(k.dtype)
+    _need(t is not None and v.dtype is k.dtype and v.shape == shape and heads == d.n_kv_heads and width == d.head_dim and k_one == 1 and v_one == 1 and
+          (heads == 1 or (k_head == width and v_head == width)) and k.get_device() == dev and v.get_device() == dev, fn)
+    seqs, n = _paged_seqs(dev, positions, page_table, fn)
+    starts = 0
     if row_starts is not None:
-        _need(row_starts.dtype == torch.int32 and row_starts.is_contiguous() and row_starts.numel() == positions.numel() + 1, fn)
-    seqs = _paged_seqs(cache, positions, page_table, fn)
-    _check(getattr(lib(), fn)(C.byref(d), C.byref(seqs), _ptr(row_starts), n, _ptr(k), _ptr(v), _row_type(k, fn), k.stride(0), v.stride(0),
-                              _ptr(status), _stream_ptr(stream)), fn)
+        _need(row_starts.dtype is _I32 and row_starts.is_contiguous() and row_starts.numel() == n + 1 and row_starts.get_device() == dev, fn)
+        starts = row_starts.data_ptr()
+    rc = call(cache._ref, seqs, starts, rows, k.data_ptr(), v.data_ptr(), t, k_row, v_row, _flag(dev, status, fn),
+              0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
 
 
 def kl_paged_append(cache: PagedCache, k_rows, v_rows, positions, page_table, row_starts=None, status=None, stream=None) -> None:
     """New rows [n_rows, n_kv_heads, head_dim] (bf16 or fp32; rows may be strided) into the pages; positions int32 [n_seqs],
     page_table int32 [n_seqs, pages], row_starts int32 [n_seqs + 1] or None (one row per sequence)."""
-    _paged_rows("kl_paged_append", cache, k_rows, v_rows, positions, page_table, row_starts, status, stream)
+    _paged_rows("kl_paged_append", (_lib or lib()).kl_paged_append, cache, k_rows, v_rows, positions, page_table, row_starts, status, stream)
 
 
 def kl_paged_read(cache: PagedCache, k_out, v_out, positions, page_table, row_starts=None, status=None, stream=None) -> None:
     """The rows that kl_paged_append with the same arguments would write, copied out."""
-    _paged_rows("kl_paged_read", cache, k_out, v_out, positions, page_table, row_starts, status, stream)
+    _paged_rows("kl_paged_read", (_lib or lib()).kl_paged_read, cache, k_out, v_out, positions, page_table, row_starts, status, stream)
 
 
 def kl_paged_workspace_bytes(cache: PagedCache, n_q_heads: int, n_seqs: int, table_pages: int) -> int:
     b = C.c_size_t()
-    _check(lib().kl_paged_workspace_bytes(C.byref(cache.desc), n_q_heads, n_seqs, table_pages, C.byref(b)), "kl_paged_workspace_bytes")
+    _check(lib().kl_paged_workspace_bytes(cache._ref, n_q_heads, n_seqs, table_pages, C.byref(b)), "kl_paged_workspace_bytes")
     return b.value
 
 
-def _paged_queries(cache: PagedCache, q, positions, where: str) -> int:
-    d = cache.desc
-    _need(q.dim() == 3 and q.shape[0] == positions.numel() and q.shape[2] == d.head_dim and q.stride(2) == 1 and
-          (q.stride(1) == d.head_dim or q.shape[1] == 1), where)
-    return _row_type(q, where)
+def _paged_queries(cache: PagedCache, dev: int, q, n: int, where: str):
+    """(row type, row stride, query heads) of q [n, n_q_heads, head_dim]."""
+    rows, heads, width = q.shape
+    row, head, one = q.stride()
+    t = _ROW_TYPES.get(q.dtype)
+    _need(t is not None and rows == n and width == cache.desc.head_dim and one == 1 and (head == width or heads == 1) and q.get_device() == dev, where)
+    return t, row, heads
 
 
 def kl_paged_select(cache: PagedCache, q, positions, page_table, selected, workspace, keep_first: int = 1, keep_last: int = 1, status=None,
                     stream=None) -> None:
     """q [n_seqs, n_q_heads, head_dim] -> selected int32 [n_seqs, n_kv_heads, n_select]."""
-    import torch
     fn = "kl_paged_select"
-    _on_device(cache, fn, q, positions, page_table, selected, workspace, status)
-    t = _paged_queries(cache, q, positions, fn)
-    n = positions.numel()
-    _need(selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 3 and
-          tuple(selected.shape[:2]) == (n, cache.desc.n_kv_heads) and workspace.dtype == torch.uint8 and workspace.is_contiguous() and
-          keep_first >= 0 and keep_last >= 0, fn)
-    seqs = _paged_seqs(cache, positions, page_table, fn)
-    _check(lib().kl_paged_select(C.byref(cache.desc), C.byref(seqs), _ptr(q), t, q.stride(0), q.shape[1], keep_first, keep_last,
-                                 selected.shape[2], _ptr(selected), _ptr(workspace), workspace.numel(), _ptr(status), _stream_ptr(stream)), fn)
+    dev = _here(cache)
+    seqs, n = _paged_seqs(dev, positions, page_table, fn)
+    t, row, heads = _paged_queries(cache, dev, q, n, fn)
+    s_n, s_h, n_select = selected.shape
+    _need(selected.dtype is _I32 and selected.is_contiguous() and s_n == n and s_h == cache.desc.n_kv_heads and workspace.dtype is _U8 and
+          workspace.is_contiguous() and 0 <= keep_first < 1 << 31 and 0 <= keep_last < 1 << 31 and selected.get_device() == dev and workspace.get_device() == dev, fn)
+    rc = (_lib or lib()).kl_paged_select(cache._ref, seqs, q.data_ptr(), t, row, heads, keep_first, keep_last, n_select, selected.data_ptr(),
+                                         workspace.data_ptr(), workspace.numel(), _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
 
 
 def kl_paged_attention(cache: PagedCache, q, out, positions, page_table, workspace, scale: float = 0.0, window: int = 0, selected=None, lse=None,
                        status=None, stream=None) -> None:
     """q, out [n_seqs, n_q_heads, head_dim] of one type; selected int32 [n_seqs, n_kv_heads, n_select]; lse fp32 [n_seqs, n_q_heads]."""
-    import torch
     fn = "kl_paged_attention"
-    _on_device(cache, fn, q, out, positions, page_table, workspace, selected, lse, status)
-    t = _paged_queries(cache, q, positions, fn)
-    n = positions.numel()
-    _need(_paged_queries(cache, out, positions, fn) == t and out.shape == q.shape and workspace.dtype == torch.uint8 and
-          workspace.is_contiguous() and window >= 0, fn)
-    k = 0
+    dev = _here(cache)
+    seqs, n = _paged_seqs(dev, positions, page_table, fn)
+    t, row, heads = _paged_queries(cache, dev, q, n, fn)
+    t_out, out_row, out_heads = _paged_queries(cache, dev, out, n, fn)
+    _need(t_out == t and out_heads == heads and workspace.dtype is _U8 and workspace.is_contiguous() and 0 <= window < 1 << 31 and
+          workspace.get_device() == dev, fn)
+    n_select = sel = lse_d = 0
     if selected is not None:
-        _need(selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 3 and
-              tuple(selected.shape[:2]) == (n, cache.desc.n_kv_heads) and selected.shape[2] > 0, fn)
-        k = selected.shape[2]
+        s_n, s_h, n_select = selected.shape
+        _need(selected.dtype is _I32 and selected.is_contiguous() and s_n == n and s_h == cache.desc.n_kv_heads and n_select > 0 and
+              selected.get_device() == dev, fn)
+        sel = selected.data_ptr()
     if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2]), fn)
-    seqs = _paged_seqs(cache, positions, page_table, fn)
-    _check(lib().kl_paged_attention(C.byref(cache.desc), C.byref(seqs), _ptr(q), _ptr(out), t, q.stride(0), out.stride(0), q.shape[1], scale, window,
-                                    _ptr(selected), k, _ptr(lse), _ptr(workspace), workspace.numel(), _ptr(status), _stream_ptr(stream)), fn)
+        _need(lse.dtype is _F32 and lse.is_contiguous() and lse.shape == (n, heads) and lse.get_device() == dev, fn)
+        lse_d = lse.data_ptr()
+    rc = (_lib or lib()).kl_paged_attention(cache._ref, seqs, q.data_ptr(), out.data_ptr(), t, row, out_row, heads, scale, window, sel, n_select, lse_d,
+                                            workspace.data_ptr(), workspace.numel(), _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
 
 
 class Decoder:

@@ -141,6 +141,19 @@ kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
     return KL_OK;
 }
 
+// Scores: up to eight heads at once; two blocks per SM keep the 64-bit pipe and the loads busy.
+template <int HD>
+kl_status launch_score_hd(const PagedView& v, const PagedSelect& a, unsigned blocks, void* stream) {
+    if (a.G == 1) return launch(kl_paged_score_kernel<HD, 1>, dim3(blocks), PG_THREADS, 0, stream, v, a);
+    if (a.G == 2) return launch(kl_paged_score_kernel<HD, 2>, dim3(blocks), PG_THREADS, 0, stream, v, a);
+    if (a.G <= 4) return launch(kl_paged_score_kernel<HD, 4>, dim3(blocks), PG_THREADS, 0, stream, v, a);
+    return launch(kl_paged_score_kernel<HD, 8>, dim3(blocks), PG_THREADS, 0, stream, v, a);
+}
+kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
+    const unsigned blocks = 2u * (unsigned)sms;
+    return v.hd == 64 ? launch_score_hd<64>(v, a, blocks, stream) : v.hd == 128 ? launch_score_hd<128>(v, a, blocks, stream) : launch_score_hd<256>(v, a, blocks, stream);
+}
+
 template <int HD, bool FP8, int UR, bool EX>
 kl_status launch_attn_as(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
     using Cfg = PaCfg<HD, FP8, EX>;
@@ -193,8 +206,15 @@ kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
     const PagedView v = view(cache, seqs, status_d);
     const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
-    return row_type == KL_F32 ? launch(kl_paged_read_kernel<float>, dim3(n_rows), PG_THREADS, 0, stream, v, r)
-                              : launch(kl_paged_read_kernel<__nv_bfloat16>, dim3(n_rows), PG_THREADS, 0, stream, v, r);
+    const uint64_t per_block = (uint64_t)PG_THREADS / (cache->head_dim / (v.fp8 ? 16 : 8)) * PR_UNROLL;   // (row, head, K or V)
+    const uint64_t blocks = ((uint64_t)n_rows * 2 * cache->n_kv_heads + per_block - 1) / per_block;
+    if (blocks > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;
+    const dim3 grid((unsigned)blocks);
+    if (v.fp8)
+        return row_type == KL_F32 ? launch(kl_paged_read_kernel<float, true>, grid, PG_THREADS, 0, stream, v, r)
+                                  : launch(kl_paged_read_kernel<__nv_bfloat16, true>, grid, PG_THREADS, 0, stream, v, r);
+    return row_type == KL_F32 ? launch(kl_paged_read_kernel<float, false>, grid, PG_THREADS, 0, stream, v, r)
+                              : launch(kl_paged_read_kernel<__nv_bfloat16, false>, grid, PG_THREADS, 0, stream, v, r);
 }
 
 kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes) {
@@ -228,9 +248,15 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     a.keep_first = keep_first; a.keep_last = keep_last; a.n_select = n_select;
     a.selected = selected_d;
     a.scores = (float*)workspace_d;
-    const unsigned blocks = (seqs->table_pages + PG_THREADS / 32 - 1) / (PG_THREADS / 32);
-    if ((rc = launch(kl_paged_score_kernel, dim3(blocks, cache->n_kv_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a)) != KL_OK) return rc;
-    return launch(kl_paged_topk_kernel, dim3(cache->n_kv_heads, seqs->n_seqs), PG_THREADS, 0, stream, v, a);
+    const int sms = attn_blocks();
+    if (sms <= 0) return KL_ERR_CUDA;
+    if ((rc = launch_score(v, a, sms, stream)) != KL_OK) return rc;
+    // keys in registers where a block's threads can hold them, else read again for every step of the search
+    const dim3 grid(cache->n_kv_heads, seqs->n_seqs);
+    if (seqs->table_pages <= 2 * PT_THREADS) return launch(kl_paged_topk_kernel<2>, grid, PT_THREADS, 0, stream, v, a);
+    if (seqs->table_pages <= 8 * PT_THREADS) return launch(kl_paged_topk_kernel<8>, grid, PT_THREADS, 0, stream, v, a);
+    if (seqs->table_pages <= 16 * PT_THREADS) return launch(kl_paged_topk_kernel<16>, grid, PT_THREADS, 0, stream, v, a);
+    return launch(kl_paged_topk_kernel<0>, grid, PT_THREADS, 0, stream, v, a);
 }
 
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,

@@ -53,6 +53,9 @@ __device__ __forceinline__ uint32_t pg_length(const PagedView& c, uint32_t s) {
     return (uint32_t)pos + 1u;
 }
 
+// 64-bit division that is usually a 32-bit one (a 64-bit division is a few hundred cycles of a kernel that may last 5 us).
+__device__ __forceinline__ uint64_t pg_div(uint64_t x, uint32_t y) { return (x >> 32) == 0u ? (uint64_t)((uint32_t)x / y) : x / y; }
+
 // 2^(e - 127) of a scale byte, and its inverse for the exponents a row can have (e - 127 in [-127, 120]).
 __device__ __forceinline__ float pg_scale(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
 __device__ __forceinline__ float pg_inv_scale(int32_t e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
@@ -122,6 +125,39 @@ __device__ __forceinline__ void pg_load_cached8(const uint8_t* row, uint32_t col
     } else {
         pg_load8<__nv_bfloat16>(reinterpret_cast<const __nv_bfloat16*>(row) + col, x);
     }
+}
+
+// Prefix sums of count(s) over the n sequences, for a block of NW warps: pre[t] = sum over the sequences before thread t's
+// share (per = ceil(n / threads) sequences each); returns the sum over all of them.
+template <int NW, class Count>
+__device__ __forceinline__ uint64_t pg_prefix(uint32_t n, uint64_t* pre, uint64_t* wsum, Count&& count) {
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, per = (n + NW * 32u - 1u) / (NW * 32u);
+    uint64_t mine = 0;
+    for (uint32_t s = tid * per; s < min(n, (tid + 1u) * per); ++s) mine += count(s);
+    uint64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= (uint32_t)o) incl += y;
+    }
+    if (lane == 31u) wsum[warp] = incl;
+    __syncthreads();
+    uint64_t all = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < (int)warp) before += wsum[w];
+        all += wsum[w];
+    }
+    pre[tid] = before + incl - mine;
+    __syncthreads();
+    return all;
+}
+// The largest t with pre[t] <= x (pre[0] = 0): which of 32 groups of NW entries, then which entry.  Whole warps.
+template <int NW>
+__device__ __forceinline__ uint32_t pg_find(const uint64_t* pre, uint64_t x) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t i = (__popc(__ballot_sync(0xffffffffu, pre[lane * NW] <= x)) - 1) * NW;
+    return i + __popc(__ballot_sync(0xffffffffu, lane < (uint32_t)NW && pre[i + lane % NW] <= x)) - 1;
 }
 
 // ---- rows in and out
@@ -200,45 +236,55 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
         lo[i] = INFINITY;
         hi[i] = -INFINITY;
     }
-    for (uint32_t i0 = 0; i0 < cnt; i0 += groups) {   // every lane of a warp takes part in the shuffles
-        const uint32_t i = i0 + g;
-        const bool live = i < cnt;
-        float x[8] = {};
-        if (live) pg_load8<T>(reinterpret_cast<const T*>(src + (int64_t)(row0 + i) * src_stride) + (size_t)h * hd + col, x);
-        uint8_t* out = dst + (int64_t)(off0 + (live ? i : 0u)) * c.row_b;
-        if (c.fp8) {
-            float big = 0.f;
+    constexpr int U = 4;   // rows a lane has in flight
+    for (uint32_t i0 = 0; i0 < cnt; i0 += groups * U) {   // every lane of a warp takes part in the shuffles
+        float xs[U][8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float a = fabsf(x[q]);
-                if (a < INFINITY) big = fmaxf(big, a);
-            }
-            for (uint32_t o = lanes / 2u; o > 0u; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-            const int32_t e = pg_exponent(big);
-            const float inv = pg_inv_scale(e), scale = pg_scale((uint32_t)(e + 127));
-            uint32_t code[4];
+        for (int y = 0; y < U; ++y) {
+            const uint32_t i = i0 + y * groups + g;
+            if (i < cnt) pg_load8<T>(reinterpret_cast<const T*>(src + (int64_t)(row0 + i) * src_stride) + (size_t)h * hd + col, xs[y]);
+        }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                code[q] = pg_to_e4m3x2(x[2 * q] * inv, x[2 * q + 1] * inv);
-                const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[q]));
-                x[2 * q] = f.x * scale;
-                x[2 * q + 1] = f.y * scale;
+        for (int y = 0; y < U; ++y) {
+            if (i0 + y * groups >= cnt) break;   // the same for the whole block
+            const uint32_t i = i0 + y * groups + g;
+            const bool live = i < cnt;
+            float (&x)[8] = xs[y];
+            uint8_t* out = dst + (int64_t)(off0 + (live ? i : 0u)) * c.row_b;
+            if (c.fp8) {
+                float big = 0.f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float a = fabsf(x[q]);
+                    if (live && a < INFINITY) big = fmaxf(big, a);
+                }
+                for (uint32_t o = lanes / 2u; o > 0u; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                const int32_t e = pg_exponent(big);
+                const float inv = pg_inv_scale(e), scale = pg_scale((uint32_t)(e + 127));
+                uint32_t code[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    code[q] = pg_to_e4m3x2(x[2 * q] * inv, x[2 * q + 1] * inv);
+                    const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[q]));
+                    x[2 * q] = f.x * scale;
+                    x[2 * q + 1] = f.y * scale;
+                }
+                if (live) {
+                    *reinterpret_cast<uint2*>(out + col) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
+                    if (lane == 0u) exps[off0 + i] = (uint8_t)(e + 127);
+                }
+            } else if (live) {
+                const uint4 w = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+                *reinterpret_cast<uint4*>(out + col * 2u) = w;
+                x[0] = bf_lo(w.x); x[1] = bf_hi(w.x); x[2] = bf_lo(w.y); x[3] = bf_hi(w.y);
+                x[4] = bf_lo(w.z); x[5] = bf_hi(w.z); x[6] = bf_lo(w.w); x[7] = bf_hi(w.w);
             }
             if (live) {
-                *reinterpret_cast<uint2*>(out + col) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
-                if (lane == 0u) exps[off0 + i] = (uint8_t)(e + 127);
-            }
-        } else if (live) {
-            const uint4 w = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-            *reinterpret_cast<uint4*>(out + col * 2u) = w;
-            x[0] = bf_lo(w.x); x[1] = bf_hi(w.x); x[2] = bf_lo(w.y); x[3] = bf_hi(w.y);
-            x[4] = bf_lo(w.z); x[5] = bf_hi(w.z); x[6] = bf_lo(w.w); x[7] = bf_hi(w.w);
-        }
-        if (live) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {   // fminf and fmaxf leave NaN out
-                lo[q] = fminf(lo[q], x[q]);
-                hi[q] = fmaxf(hi[q], x[q]);
+                for (int q = 0; q < 8; ++q) {   // fminf and fmaxf leave NaN out
+                    lo[q] = fminf(lo[q], x[q]);
+                    hi[q] = fmaxf(hi[q], x[q]);
+                }
             }
         }
     }
@@ -275,42 +321,88 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
     return lo;
 }
 
-// Read back: hd / 8 lanes per (row, head, K or V).
-template <class T>
+// Read back.  A vector = one row of one head, K or V; hd / E lanes share it (E = 8 columns each, 16 of an e4m3 row: 16 bytes
+// of the cache either way).  A lane works on PR_UNROLL vectors at once: all their page look-ups, then all their rows.
+constexpr int PR_UNROLL = 4;
+template <class T, bool FP8>
 __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedView c, const PagedRows rows) {
+    constexpr uint32_t E = FP8 ? 16 : 8;
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint32_t lanes = c.hd / 8u, groups = PG_THREADS / lanes, grp = threadIdx.x / lanes, col = threadIdx.x % lanes * 8u;
-    const uint32_t row = blockIdx.x;
-    if (rows.row_starts && row == 0u)
+    const uint32_t lanes = c.hd / E, groups = PG_THREADS / lanes, grp = threadIdx.x / lanes, col = threadIdx.x % lanes * E;
+    if (rows.row_starts && blockIdx.x == 0u)
         for (uint32_t s = threadIdx.x; s < c.n_seqs; s += PG_THREADS) {
             const int32_t a = rows.row_starts[s], b = rows.row_starts[s + 1u];
             if (a < 0 || b < a || (uint32_t)b > rows.n_rows) pg_error(c);
         }
-    const uint32_t s = pg_seq_of_row(c, rows, row);
-    if (s >= c.n_seqs) return;
-    const uint32_t r0 = pg_row_start(c, rows, s), r1 = pg_row_start(c, rows, s + 1u);
-    const int32_t pos = c.positions[s];
-    if (pos < 0 || row < r0 || row >= r1) return;
-    const uint64_t at = (uint64_t)pos + (row - r0), lp = at / c.page;
-    if (lp >= c.table_pages) {
-        if (threadIdx.x == 0u) pg_error(c);
-        return;
+    const uint64_t v0 = (uint64_t)blockIdx.x * groups * PR_UNROLL + grp;
+    uint32_t row[PR_UNROLL], head[PR_UNROLL];   // head: nkv + head for values
+    int64_t src[PR_UNROLL], exp_at[PR_UNROLL];
+    bool live[PR_UNROLL];
+#pragma unroll
+    for (int u = 0; u < PR_UNROLL; ++u) {
+        const uint64_t vec = v0 + (uint64_t)u * groups;
+        const uint64_t r64 = pg_div(vec, 2u * c.nkv);
+        live[u] = r64 < rows.n_rows;
+        row[u] = live[u] ? (uint32_t)r64 : 0u;
+        head[u] = (uint32_t)(vec - r64 * 2u * c.nkv);
+        src[u] = exp_at[u] = 0;
+        if (!live[u]) continue;
+        const uint32_t s = pg_seq_of_row(c, rows, row[u]);
+        const uint32_t r0 = pg_row_start(c, rows, s), r1 = pg_row_start(c, rows, s + 1u);
+        const int32_t pos = c.positions[s];
+        live[u] = pos >= 0 && row[u] >= r0 && row[u] < r1;
+        if (!live[u]) continue;
+        const uint64_t at = (uint64_t)pos + (row[u] - r0);
+        const uint64_t lp = pg_div(at, c.page);
+        const int32_t phys = lp < c.table_pages ? pg_physical(c, s, (uint32_t)lp) : -1;
+        if (phys < 0) {
+            pg_error(c);
+            live[u] = false;
+            continue;
+        }
+        const uint32_t off = (uint32_t)(at - lp * c.page), h = head[u] >= c.nkv ? head[u] - c.nkv : head[u];
+        src[u] = (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off * c.row_b;
+        exp_at[u] = ((int64_t)phys * c.nkv + h) * c.page + off;
     }
-    const int32_t phys = pg_physical(c, s, (uint32_t)lp);
-    if (phys < 0) return;
-    const uint32_t off = (uint32_t)(at - lp * c.page);
-    for (uint32_t i = grp; i < 2u * c.nkv; i += groups) {
-        const bool is_v = i >= c.nkv;
-        const uint32_t h = is_v ? i - c.nkv : i;
-        const uint8_t* src = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off * c.row_b;
-        const float scale = c.fp8 ? pg_scale((is_v ? c.ve : c.ke)[((int64_t)phys * c.nkv + h) * c.page + off]) : 1.f;
-        float x[8];
-        pg_load_cached8(src, col, c.fp8, scale, x);
-        uint8_t* out = is_v ? rows.v + (int64_t)row * rows.v_stride : rows.k + (int64_t)row * rows.k_stride;
-        pg_store8<T>(reinterpret_cast<T*>(out) + (size_t)h * c.hd + col, x);
-    }
+    uint4 x[PR_UNROLL];
+    uint32_t e[PR_UNROLL];
+#pragma unroll
+    for (int u = 0; u < PR_UNROLL; ++u)
+        if (live[u]) {
+            const bool is_v = head[u] >= c.nkv;
+            x[u] = *reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + src[u] + col * (FP8 ? 1 : 2));
+            if (FP8) e[u] = (is_v ? c.ve : c.ke)[exp_at[u]];
+        }
+#pragma unroll
+    for (int u = 0; u < PR_UNROLL; ++u)
+        if (live[u]) {
+            const bool is_v = head[u] >= c.nkv;
+            uint8_t* to = is_v ? rows.v + (int64_t)row[u] * rows.v_stride : rows.k + (int64_t)row[u] * rows.k_stride;
+            T* out = reinterpret_cast<T*>(to) + (size_t)(is_v ? head[u] - c.nkv : head[u]) * c.hd + col;
+            const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+            float f[8];
+#pragma unroll
+            for (int hh = 0; hh < (FP8 ? 2 : 1); ++hh) {
+                if (FP8) {
+                    const float scale = pg_scale(e[u]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2((w[2 * hh + i / 2] >> (16 * (i & 1))) & 0xffffu));
+                        f[2 * i] = y.x * scale;
+                        f[2 * i + 1] = y.y * scale;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f[2 * i] = bf_lo(w[i]);
+                        f[2 * i + 1] = bf_hi(w[i]);
+                    }
+                }
+                pg_store8<T>(out + hh * 8, f);
+            }
+        }
 }
 
 // ---- page selection
@@ -327,47 +419,147 @@ __device__ __forceinline__ float pg_q(const uint8_t* row, uint32_t f32, uint32_t
     return f32 ? reinterpret_cast<const float*>(row)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[i]);
 }
 
-// A score as a whole number of the same order: NaN below everything.
+// A score as a whole number of the same order: at least 2, NaN 1, so that 0 is below every page.
 __device__ __forceinline__ uint32_t pg_key(float x) {
-    if (isnan(x)) return 0u;
+    if (isnan(x)) return 1u;
     const uint32_t u = __float_as_uint(x + 0.f);   // -0 becomes +0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One warp per page: scores in 64 bits (the products of a bf16 bound and a query are exact there), rounded once.
+constexpr int PS_PAGES = 4;                            // pages a group of eight lanes scores at a time
+constexpr int PS_BLOCK = PG_THREADS / 8 * PS_PAGES;    // pages per unit: 128
+
+// Scores.  Work is cut into units of PS_BLOCK pages of one (sequence, kv head); every block of the grid takes an equal,
+// contiguous range of all units.  Eight lanes share a page (16-byte pieces of its lower and upper bounds, both read once
+// for up to GT heads) and score PS_PAGES pages at once, so that a query element fetched from shared memory is used four
+// times.  The products of a bf16 bound and a query are exact in 64 bits, and so, but for extreme spreads, are their sums: the
+// rounded score does not depend on the order of additions.  What bounds it: with eight heads per kv head the 64-bit
+// pipe and the selects in front of it, not memory.
+template <int HD, int GT>
 __global__ void __launch_bounds__(PG_THREADS) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
+    constexpr int NW = PG_THREADS / 32, NC = HD / 64;   // 16-byte pieces of a bound per lane
+    __shared__ uint64_t pre[PG_THREADS], wsum[NW];
+    __shared__ double q_s[NC * 8][GT][8];               // [piece, element][head][lane of the group]
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint32_t s = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31u;
-    const uint32_t lp = blockIdx.x * (PG_THREADS / 32u) + (threadIdx.x >> 5);
-    const uint32_t n = (pg_length(c, s) + c.page - 1u) / c.page;
-    if (lp >= n) return;
-    const int32_t phys = pg_physical(c, s, lp);
-    float best = -INFINITY;
-    if (phys >= 0) {
-        const __nv_bfloat16* b = c.bounds + ((int64_t)phys * c.nkv + h) * 2 * c.hd;
-        bool first = true;
-        for (uint32_t g = 0; g < a.G; ++g) {
-            const uint8_t* q = a.q + (int64_t)s * a.q_stride;
-            double sum = 0.0;
-            for (uint32_t d = lane; d < c.hd; d += 32u) {
-                const float x = pg_q(q, a.q_f32, (h * a.G + g) * c.hd + d);
-                sum += (double)x * (double)__bfloat162float(x >= 0.f ? b[c.hd + d] : b[d]);
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, l8 = lane & 7u;
+    const uint32_t n = c.n_seqs, per = (n + PG_THREADS - 1u) / PG_THREADS, HT = (a.G + GT - 1u) / GT;
+    auto pages_of = [&](uint32_t s) { return (pg_length(c, s) + c.page - 1u) / c.page; };
+    const uint64_t W = pg_prefix<NW>(n, pre, wsum, [&](uint32_t s) { return (uint64_t)((pages_of(s) + PS_BLOCK - 1u) / PS_BLOCK) * c.nkv; });
+    const uint64_t share = pg_div(W, gridDim.x), over = W - share * gridDim.x;
+    const uint64_t lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), hi = lo + share + (blockIdx.x < over ? 1u : 0u);
+    if (lo >= hi) return;
+    const uint32_t i0 = pg_find<NW>(pre, lo);
+    uint64_t rem = lo - pre[i0];
+    uint32_t s = i0 * per, np = pages_of(s), nu = (np + PS_BLOCK - 1u) / PS_BLOCK;   // units per head of sequence s
+    while (rem >= (uint64_t)nu * c.nkv) {
+        rem -= (uint64_t)nu * c.nkv;
+        np = pages_of(++s);
+        nu = (np + PS_BLOCK - 1u) / PS_BLOCK;
+    }
+    uint32_t h = (uint32_t)pg_div(rem, nu), u = (uint32_t)(rem - (uint64_t)h * nu);
+    bool fresh = true;
+    for (uint64_t left = hi - lo; left; --left) {
+        const uint32_t p0 = u * PS_BLOCK + warp * (4 * PS_PAGES) + (lane >> 3) * PS_PAGES;   // this group's pages
+        const __nv_bfloat16* b[PS_PAGES];
+        bool live[PS_PAGES];
+#pragma unroll
+        for (int x = 0; x < PS_PAGES; ++x) {
+            live[x] = false;
+            b[x] = c.bounds;
+            if (p0 + x < np) {
+                const int32_t phys = pg_physical(c, s, p0 + x);
+                live[x] = phys >= 0;
+                b[x] = c.bounds + ((int64_t)max(phys, 0) * c.nkv + h) * 2 * HD + l8 * 8;
             }
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float sc = (float)sum;
-            best = first ? sc : (isnan(sc) || isnan(best) ? (isnan(best) ? sc : best) : fmaxf(best, sc));
-            first = false;
+        }
+        float best = __int_as_float(0x7fc00000);   // NaN; of page l8 >> 1 of the group, see the reduction
+        for (uint32_t ht = 0; ht < HT; ++ht) {
+            if (fresh || HT > 1u) {
+                __syncthreads();
+                for (uint32_t i = tid; i < (uint32_t)(HD * GT); i += PG_THREADS) {
+                    const uint32_t d = i % HD, gg = i / HD, head = min(ht * GT + gg, a.G - 1u);   // a missing head repeats the last
+                    q_s[(d / 64) * 8 + d % 8][gg][(d / 8) % 8] = (double)pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + head) * HD + d);
+                }
+                __syncthreads();
+                fresh = false;
+            }
+            double acc[PS_PAGES][GT];
+#pragma unroll
+            for (int x = 0; x < PS_PAGES; ++x)
+#pragma unroll
+                for (int gg = 0; gg < GT; ++gg) acc[x][gg] = 0.0;
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) {
+                uint32_t lw[PS_PAGES][4], hw[PS_PAGES][4];
+#pragma unroll
+                for (int x = 0; x < PS_PAGES; ++x) {
+                    uint4 l4 = make_uint4(0u, 0u, 0u, 0u), h4 = l4;
+                    if (live[x]) {
+                        l4 = *reinterpret_cast<const uint4*>(b[x] + cc * 64);
+                        h4 = *reinterpret_cast<const uint4*>(b[x] + HD + cc * 64);
+                    }
+                    lw[x][0] = l4.x; lw[x][1] = l4.y; lw[x][2] = l4.z; lw[x][3] = l4.w;
+                    hw[x][0] = h4.x; hw[x][1] = h4.y; hw[x][2] = h4.z; hw[x][3] = h4.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    double ld[PS_PAGES], hd[PS_PAGES];
+#pragma unroll
+                    for (int x = 0; x < PS_PAGES; ++x) {
+                        ld[x] = (double)(i & 1 ? bf_hi(lw[x][i / 2]) : bf_lo(lw[x][i / 2]));
+                        hd[x] = (double)(i & 1 ? bf_hi(hw[x][i / 2]) : bf_lo(hw[x][i / 2]));
+                    }
+#pragma unroll
+                    for (int gg = 0; gg < GT; ++gg) {
+                        const double q = q_s[cc * 8 + i][gg][l8];
+                        const bool up = q >= 0.0;
+#pragma unroll
+                        for (int x = 0; x < PS_PAGES; ++x) acc[x][gg] = fma(q, up ? hd[x] : ld[x], acc[x][gg]);
+                    }
+                }
+            }
+            // sums over the eight lanes, halving the pages a lane keeps in the first two steps
+            double r2[2][GT], r1[GT];
+#pragma unroll
+            for (int gg = 0; gg < GT; ++gg) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const double keep = l8 & 4u ? acc[x + 2][gg] : acc[x][gg], give = l8 & 4u ? acc[x][gg] : acc[x + 2][gg];
+                    r2[x][gg] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+                }
+                const double keep = l8 & 2u ? r2[1][gg] : r2[0][gg], give = l8 & 2u ? r2[0][gg] : r2[1][gg];
+                r1[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+                r1[gg] += __shfl_xor_sync(0xffffffffu, r1[gg], 1);
+                best = fmaxf(best, (float)r1[gg]);   // fmaxf leaves NaN out
+            }
+        }
+        const uint32_t page = p0 + (l8 >> 1);   // lanes 4.. hold pages 2, 3; of these, lanes 2, 3, 6, 7 the odd ones
+        if (!(l8 & 1u) && page < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + page] = best;
+        if (++u == nu) {
+            u = 0;
+            fresh = true;
+            if (++h == c.nkv && left > 1u) {
+                h = 0;
+                do {
+                    np = pages_of(++s);
+                    nu = (np + PS_BLOCK - 1u) / PS_BLOCK;
+                } while (nu == 0u);
+            }
         }
     }
-    if (lane == 0u) a.scores[((size_t)s * c.nkv + h) * c.table_pages + lp] = best;
 }
 
-// One block per (sequence, kv head): the n_select-th largest key by bisection over its bits, then the pages above it and
-// the first ones equal to it, in order.
-__global__ void __launch_bounds__(PG_THREADS) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
-    __shared__ uint32_t red[PG_THREADS / 32 * 2 + 4];
+// The choice: one block per (sequence, kv head).  The threshold -- the largest key t that at least `need` pages reach -- is found
+// bit by bit, starting below the bits all keys share and ending as soon as exactly `need` pages reach it (a dozen steps,
+// not 32).  KPT > 0: every thread keeps KPT neighbouring keys in registers, and one prefix sum puts the pages in order;
+// KPT == 0: any number of pages, read again for every step.
+constexpr int PT_THREADS = 512;
+template <int KPT>
+__global__ void __launch_bounds__(PT_THREADS) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
+    constexpr int NW = PT_THREADS / 32, NK = KPT ? KPT : 1;
+    __shared__ uint32_t red[2][NW][2];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
@@ -375,52 +567,119 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_topk_kernel(const PagedVi
     const uint32_t n = (pg_length(c, s) + c.page - 1u) / c.page;
     const float* sc = a.scores + ((size_t)s * c.nkv + h) * c.table_pages;
     int32_t* out = a.selected + ((size_t)s * c.nkv + h) * a.n_select;
-    auto key = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n ? 0xffffffffu : pg_key(sc[i]); };
-    auto count = [&](uint32_t t) {   // pages with key >= t
-        uint32_t x = 0;
-        for (uint32_t i = tid; i < n; i += PG_THREADS) x += key(i) >= t;
-        x = __reduce_add_sync(0xffffffffu, x);
-        __syncthreads();
-        if (lane == 0u) red[warp] = x;
-        __syncthreads();
-        uint32_t y = 0;
-        for (int w = 0; w < PG_THREADS / 32; ++w) y += red[w];
-        return y;
-    };
-    uint32_t t = 0, above = 0;
-    if (n > a.n_select) {
-        for (int b = 31; b >= 0; --b)   // the largest t with at least n_select keys >= t
-            if (count(t | 1u << b) >= a.n_select) t |= 1u << b;
-        above = t == 0xffffffffu ? 0u : count(t + 1u);
+    if (n <= a.n_select) {   // all of them
+        for (uint32_t i = tid; i < a.n_select; i += PT_THREADS) out[i] = i < n ? (int32_t)i : -1;
+        return;
     }
-    const uint32_t ties = n > a.n_select ? a.n_select - above : 0u;   // pages equal to t that still fit
-    uint32_t done = 0, tied = 0;
-    for (uint32_t i0 = 0; i0 < n; i0 += PG_THREADS) {
-        const uint32_t i = i0 + tid, k = i < n ? key(i) : 0u;
-        const bool eq = i < n && n > a.n_select && k == t, gt = i < n && (n <= a.n_select || k > t);
-        const uint32_t be = __ballot_sync(0xffffffffu, eq), bg = __ballot_sync(0xffffffffu, gt);
-        __syncthreads();
+    auto forced = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n; };
+    auto key_of = [&](uint32_t i) { return i >= n || forced(i) ? 0u : pg_key(sc[i]); };
+    uint32_t key[NK];
+    if (KPT)
+#pragma unroll
+        for (int r = 0; r < NK; ++r) key[r] = key_of(tid * NK + r);
+    const uint32_t need = a.n_select - min(n, a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
+    int turn = 0;
+    auto sum2 = [&](uint32_t x, uint32_t y, bool is_max) -> uint2 {   // block sums, or (maximum, minimum)
+        x = is_max ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
+        y = is_max ? __reduce_min_sync(0xffffffffu, y) : __reduce_add_sync(0xffffffffu, y);
         if (lane == 0u) {
-            red[2 * warp] = __popc(be);
-            red[2 * warp + 1] = __popc(bg);
+            red[turn][warp][0] = x;
+            red[turn][warp][1] = y;
         }
         __syncthreads();
-        uint32_t e = tied + __popc(be & ((1u << lane) - 1u)), ge = __popc(bg & ((1u << lane) - 1u)), et = 0, gt_ = 0;
-        for (uint32_t w = 0; w < PG_THREADS / 32; ++w) {
-            if (w < warp) {
-                e += red[2 * w];
-                ge += red[2 * w + 1];
-            }
-            et += red[2 * w];
-            gt_ += red[2 * w + 1];
+        uint2 t = make_uint2(red[turn][0][0], red[turn][0][1]);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            const uint32_t p = red[turn][w][0], q = red[turn][w][1];
+            t.x = is_max ? max(t.x, p) : t.x + p;
+            t.y = is_max ? min(t.y, q) : t.y + q;
         }
-        // chosen before this page: the larger ones and as many equal ones as fit
-        const uint32_t at = done + ge + min(e, ties) - min(tied, ties);
-        if ((gt || (eq && e < ties)) && at < a.n_select) out[at] = (int32_t)i;
-        done += gt_ + min(tied + et, ties) - min(tied, ties);
-        tied += et;
+        turn ^= 1;   // the next call writes the other half, and nobody is two calls behind
+        return t;
+    };
+    auto count = [&](uint32_t t) {   // pages with a key of at least t
+        uint32_t x = 0;
+        if (KPT) {
+#pragma unroll
+            for (int r = 0; r < NK; ++r) x += key[r] >= t;
+        } else {
+            for (uint32_t i = tid; i < n; i += PT_THREADS) x += key_of(i) >= t;
+        }
+        return sum2(x, 0u, false).x;
+    };
+    uint32_t t = 0xffffffffu, ties = 0xffffffffu;   // chosen: keys above t, and the first `ties` of those equal to it
+    if (need) {
+        uint32_t mx = 0, mn = 0xffffffffu;
+        auto see = [&](uint32_t k) {
+            mx = max(mx, k);
+            if (k) mn = min(mn, k);
+        };
+        if (KPT) {
+#pragma unroll
+            for (int r = 0; r < NK; ++r) see(key[r]);
+        } else {
+            for (uint32_t i = tid; i < n; i += PT_THREADS) see(key_of(i));
+        }
+        const uint2 mm = sum2(mx, mn, true);
+        const uint32_t differ = mm.x ^ mm.y;
+        bool exact = false;
+        int bit = differ ? 31 - __clz(differ) : -1;
+        t = bit >= 0 ? mm.y & ~((2u << bit) - 1u) : mm.y;
+        for (; bit >= 0 && !exact; --bit) {
+            const uint32_t x = count(t | 1u << bit);
+            if (x >= need) {
+                t |= 1u << bit;
+                exact = x == need;
+            }
+        }
+        if (!exact) ties = need - (t == 0xffffffffu ? 0u : count(t + 1u));
+    } else {
+        ties = 0;
     }
-    for (uint32_t i = done + tid; i < a.n_select; i += PG_THREADS) out[i] = -1;
+    // in order: a page is chosen if it is forced, above t, or one of the first equal ones
+    uint32_t done = 0, tied = 0;   // chosen pages without the equal ones, and equal ones, so far
+    auto place = [&](uint32_t i, bool sure, bool eq, uint32_t sure_before, uint32_t eq_before) {
+        const uint32_t at = sure_before + min(eq_before, ties);
+        if (i < n && (sure || (eq && eq_before < ties)) && at < a.n_select) out[at] = (int32_t)i;
+    };
+    constexpr uint32_t STEP = PT_THREADS * NK;
+    for (uint32_t i0 = 0; i0 < n; i0 += STEP) {   // once where the keys are in registers
+        bool sure[NK], eq[NK];
+        uint32_t ns = 0, ne = 0;
+#pragma unroll
+        for (int r = 0; r < NK; ++r) {
+            const uint32_t i = i0 + tid * NK + r, k = KPT ? key[r] : key_of(i);
+            eq[r] = need && k == t;
+            sure[r] = i < n && (k > t || forced(i));
+            ns += sure[r];
+            ne += eq[r];
+        }
+        uint32_t both = ns | ne << 16, incl = both;   // at most STEP <= 2^15 each
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= (uint32_t)o) incl += y;
+        }
+        if (lane == 31u) red[turn][warp][0] = incl;
+        __syncthreads();
+        uint32_t before = incl - both, all = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const uint32_t y = red[turn][w][0];
+            if (w < (int)warp) before += y;
+            all += y;
+        }
+        turn ^= 1;
+        uint32_t bs = done + (before & 0xffffu), be = tied + (before >> 16);
+#pragma unroll
+        for (int r = 0; r < NK; ++r) {
+            place(i0 + tid * NK + r, sure[r], eq[r], bs, be);
+            bs += sure[r];
+            be += eq[r];
+        }
+        done += all & 0xffffu;
+        tied += all >> 16;
+    }
 }
 
 // ---- attention
@@ -525,9 +784,6 @@ __device__ __forceinline__ void pa_store_lse(const PagedAttn& a, uint32_t s, uin
     if (a.lse) a.lse[(size_t)s * a.nq + hq] = (m + log2f(l)) * 0.6931471805599453f;   // l == 0: -inf
 }
 
-// 64-bit division that is usually a 32-bit one (a 64-bit division is a few hundred cycles of a kernel that may last 5 us).
-__device__ __forceinline__ uint64_t pa_div(uint64_t x, uint32_t y) { return (x >> 32) == 0u ? (uint64_t)((uint32_t)x / y) : x / y; }
-
 constexpr uint32_t PA_NONE = 0x7fffffffu;   // position of a row group that holds nothing to attend to
 constexpr int PA_MAX_WARPS = 16;
 constexpr int PA_LENS = 1024;               // sequences whose lengths are kept in shared memory
@@ -623,29 +879,12 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     if (pg_stopped(c)) return;
 
     // ---- the list of tiles: prefix sums over the sequences
-    const uint32_t PH = c.nkv * a.HT, n = c.n_seqs, per = (n + NT - 1u) / NT;
-    uint64_t mine = 0;
-    for (uint32_t s = tid * per; s < min(n, (tid + 1u) * per); ++s) {
+    const uint32_t PH = c.nkv * a.HT, n = c.n_seqs, per = (n + NT - 1u) / NT;   // per: see pg_prefix
+    const uint64_t W = pg_prefix<NW>(n, pre, wsum, [&](uint32_t s) {
         const uint32_t len = pg_length(c, s);
         if (s < (uint32_t)PA_LENS) lens[s] = len;
-        mine += (uint64_t)pa_seq<TP>(c, a, len).nt * PH;
-    }
-    uint64_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= (uint32_t)o) incl += y;
-    }
-    if (lane == 31u) wsum[warp] = incl;
-    __syncthreads();
-    uint64_t W = 0, before = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        if (w < (int)warp) before += wsum[w];
-        W += wsum[w];
-    }
-    pre[tid] = before + incl - mine;
-    __syncthreads();
+        return (uint64_t)pa_seq<TP>(c, a, len).nt * PH;
+    });
     auto length = [&](uint32_t s) { return s < (uint32_t)PA_LENS ? lens[s] : pg_length(c, s); };
 
     for (uint32_t s = blockIdx.x; s < n; s += gridDim.x)   // sequences without a position: zeros
@@ -660,9 +899,9 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         return;
     }
     // block b takes tiles [share * b + min(b, over), ...): the first `over` blocks one more than the others
-    const uint64_t share = pa_div(W, blocks), over = W - share * blocks;
+    const uint64_t share = pg_div(W, blocks), over = W - share * blocks;
     const uint64_t b_lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), b_n = share + (blockIdx.x < over ? 1u : 0u);
-    const uint64_t w_n = pa_div(b_n, NW), w_over = b_n - w_n * NW;
+    const uint64_t w_n = pg_div(b_n, NW), w_over = b_n - w_n * NW;
     const uint64_t lo = b_lo + w_n * warp + min((uint64_t)warp, w_over), hi = lo + w_n + (warp < w_over ? 1u : 0u);
 
     // ---- this warp's range
@@ -672,9 +911,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     const uint32_t exps = smem_u32(exps_all) + warp * (ST * 64);
     volatile uint32_t* lps = lps_all + warp * (ST * 12);
     if (lo < hi) {
-        // the largest i0 with pre[i0] <= lo: which of 32 groups of NW entries, then which entry
-        uint32_t i0 = (__popc(__ballot_sync(0xffffffffu, pre[lane * NW] <= lo)) - 1) * NW;
-        i0 += __popc(__ballot_sync(0xffffffffu, lane < (uint32_t)NW && pre[i0 + lane % NW] <= lo)) - 1;
+        const uint32_t i0 = pg_find<NW>(pre, lo);
         uint64_t rem = lo - pre[i0];
         uint32_t cs = i0 * per;                    // cursor of the tiles that are consumed
         PaSeq cq = pa_seq<TP>(c, a, length(cs));
@@ -682,7 +919,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             rem -= (uint64_t)cq.nt * PH;
             cq = pa_seq<TP>(c, a, length(++cs));
         }
-        uint32_t cph = (uint32_t)pa_div(rem, cq.nt), ct = (uint32_t)(rem - (uint64_t)cph * cq.nt);
+        uint32_t cph = (uint32_t)pg_div(rem, cq.nt), ct = (uint32_t)(rem - (uint64_t)cph * cq.nt);
 
         // cursor of the tiles that are requested, and the look-ups of its batch (this one and the next)
         uint32_t is = cs, iph = cph, it = ct;
@@ -1130,7 +1367,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         if (begins && !whole && tid == 0u) {   // the last block that shares the pair: the one that holds its last tile
             const uint64_t last_tile = b_lo + b_n - 1u + end.w;
             const uint64_t wide = (share + 1u) * over;
-            const uint64_t lb = last_tile < wide ? pa_div(last_tile, (uint32_t)share + 1u) : over + pa_div(last_tile - wide, (uint32_t)share);
+            const uint64_t lb = last_tile < wide ? pg_div(last_tile, (uint32_t)share + 1u) : over + pg_div(last_tile - wide, (uint32_t)share);
             meta = make_int4(1, (int)s, (int)ph, (int)lb);
         }
         const uint32_t heads = min(8u, a.G - h0);
