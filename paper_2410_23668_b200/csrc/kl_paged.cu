@@ -141,17 +141,18 @@ kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
     return KL_OK;
 }
 
-// Scores: up to eight heads at once; two blocks per SM keep the 64-bit pipe and the loads busy.
+// Scores: up to eight heads at once, as many blocks as the SMs hold.
 template <int HD>
-kl_status launch_score_hd(const PagedView& v, const PagedSelect& a, unsigned blocks, void* stream) {
+kl_status launch_score_hd(const PagedView& v, const PagedSelect& a, unsigned sms, void* stream) {
+    const unsigned blocks = (a.G <= 4 ? 3u : 2u) * sms;
     if (a.G == 1) return launch(kl_paged_score_kernel<HD, 1>, dim3(blocks), PG_THREADS, 0, stream, v, a);
     if (a.G == 2) return launch(kl_paged_score_kernel<HD, 2>, dim3(blocks), PG_THREADS, 0, stream, v, a);
     if (a.G <= 4) return launch(kl_paged_score_kernel<HD, 4>, dim3(blocks), PG_THREADS, 0, stream, v, a);
     return launch(kl_paged_score_kernel<HD, 8>, dim3(blocks), PG_THREADS, 0, stream, v, a);
 }
 kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
-    const unsigned blocks = 2u * (unsigned)sms;
-    return v.hd == 64 ? launch_score_hd<64>(v, a, blocks, stream) : v.hd == 128 ? launch_score_hd<128>(v, a, blocks, stream) : launch_score_hd<256>(v, a, blocks, stream);
+    const unsigned n = (unsigned)sms;
+    return v.hd == 64 ? launch_score_hd<64>(v, a, n, stream) : v.hd == 128 ? launch_score_hd<128>(v, a, n, stream) : launch_score_hd<256>(v, a, n, stream);
 }
 
 template <int HD, bool FP8, int UR, bool EX>

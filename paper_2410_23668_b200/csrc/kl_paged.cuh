@@ -86,21 +86,7 @@ __device__ __forceinline__ float2 pg_f16x2_to_float2(uint32_t h) {
     return __half22float2(v);
 }
 
-// Eight consecutive elements at src (16-byte aligned) as floats.
-template <class T>
-__device__ __forceinline__ void pg_load8(const T* src, float (&x)[8]);
-template <>
-__device__ __forceinline__ void pg_load8<float>(const float* src, float (&x)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(src)[0], b = reinterpret_cast<const float4*>(src)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-template <>
-__device__ __forceinline__ void pg_load8<__nv_bfloat16>(const __nv_bfloat16* src, float (&x)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4*>(src);
-    x[0] = bf_lo(u.x); x[1] = bf_hi(u.x); x[2] = bf_lo(u.y); x[3] = bf_hi(u.y);
-    x[4] = bf_lo(u.z); x[5] = bf_hi(u.z); x[6] = bf_lo(u.w); x[7] = bf_hi(u.w);
-}
+// Eight consecutive elements to dst (16-byte aligned).
 template <class T>
 __device__ __forceinline__ void pg_store8(T* dst, const float (&x)[8]);
 template <>
@@ -112,21 +98,6 @@ template <>
 __device__ __forceinline__ void pg_store8<__nv_bfloat16>(__nv_bfloat16* dst, const float (&x)[8]) {
     *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
-// Eight consecutive cached elements of a row (columns col .. col + 7) as floats.
-__device__ __forceinline__ void pg_load_cached8(const uint8_t* row, uint32_t col, bool fp8, float scale, float (&x)[8]) {
-    if (fp8) {
-        const uint2 u = *reinterpret_cast<const uint2*>(row + col);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(((i < 2 ? u.x : u.y) >> (16 * (i & 1))) & 0xffffu));
-            x[2 * i] = f.x * scale;
-            x[2 * i + 1] = f.y * scale;
-        }
-    } else {
-        pg_load8<__nv_bfloat16>(reinterpret_cast<const __nv_bfloat16*>(row) + col, x);
-    }
-}
-
 // Prefix sums of count(s) over the n sequences, for a block of NW warps: pre[t] = sum over the sequences before thread t's
 // share (per = ceil(n / threads) sequences each); returns the sum over all of them.
 template <int NW, class Count>
@@ -178,6 +149,14 @@ __device__ __forceinline__ uint32_t pg_row_start(const PagedView& c, const Paged
 
 constexpr int PG_THREADS = 256;
 
+// An array of row starts that descends or leaves [0, n_rows] is an error (one block of a call looks).
+__device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedRows& r) {
+    for (uint32_t s = threadIdx.x; s < c.n_seqs; s += PG_THREADS) {
+        const int32_t a = r.row_starts[s], b = r.row_starts[s + 1u];
+        if (a < 0 || b < a || (uint32_t)b > r.n_rows) pg_error(c);
+    }
+}
+
 // Append.  One block = the rows of one call that fall into one page, for one kv head, so that the page's bounds have one
 // writer and its rows are quantised where they pass by.  Sequence s touches at most rows / page + 2 pages, so block u of
 // the grid belongs to the sequence s with base(s) <= u < base(s + 1), base(s) = row_starts[s] / page + 2 s, and is its
@@ -190,24 +169,23 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
     griddep_wait();
     if (pg_stopped(c)) return;
     const uint32_t u = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
-    uint32_t s, j;
-    if (!rows.row_starts) {
-        s = u;
-        j = 0;
-    } else {
-        uint32_t lo = 0, hi = c.n_seqs;   // base(lo) <= u < base(hi)
-        while (hi - lo > 1u) {
-            const uint32_t mid = (lo + hi) / 2u;
-            if (pg_row_start(c, rows, mid) / c.page + 2u * mid <= u) lo = mid;
-            else hi = mid;
-        }
-        s = lo;
-        j = u - (pg_row_start(c, rows, s) / c.page + 2u * s);
-    }
-    const uint32_t r0 = pg_row_start(c, rows, s), r1 = pg_row_start(c, rows, s + 1u);
-    if (rows.row_starts && j == 0u && tid == 0u) {   // an array that descends or leaves [0, n_rows]
-        const int32_t a = rows.row_starts[s], b = rows.row_starts[s + 1u];
-        if (a < 0 || b < a || (uint32_t)b > rows.n_rows) pg_error(c);
+    uint32_t s = u, j = 0, r0 = u, r1 = u + 1u;
+    if (rows.row_starts) {
+        // the last s with base(s) <= u; all candidates are loaded at once (a search would be a chain of loads)
+        __shared__ uint32_t found[2];
+        if (u == 0u && h == 0u) pg_check_starts(c, rows);
+        int below = 0;
+        for (uint32_t t = tid; t < c.n_seqs; t += PG_THREADS) below += pg_row_start(c, rows, t) / c.page + 2u * t <= u;
+        if (tid < 2u) found[tid] = 0u;
+        __syncthreads();
+        below = __reduce_add_sync(0xffffffffu, below);
+        if ((tid & 31u) == 0u) atomicAdd(&found[0], (uint32_t)below);
+        __syncthreads();
+        s = found[0] - 1u;   // base(0) = row_starts[0] / page may lie above u: no sequence then
+        if (found[0] == 0u) return;
+        r0 = pg_row_start(c, rows, s);
+        r1 = pg_row_start(c, rows, s + 1u);
+        j = u - (r0 / c.page + 2u * s);
     }
     const int32_t pos = c.positions[s];
     if (pos < 0 || r1 <= r0) return;
@@ -238,18 +216,32 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
     }
     constexpr int U = 4;   // rows a lane has in flight
     for (uint32_t i0 = 0; i0 < cnt; i0 += groups * U) {   // every lane of a warp takes part in the shuffles
-        float xs[U][8];
+        uint4 raw[U][sizeof(T) / 2];
 #pragma unroll
         for (int y = 0; y < U; ++y) {
             const uint32_t i = i0 + y * groups + g;
-            if (i < cnt) pg_load8<T>(reinterpret_cast<const T*>(src + (int64_t)(row0 + i) * src_stride) + (size_t)h * hd + col, xs[y]);
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
+                raw[y][q] = make_uint4(0u, 0u, 0u, 0u);
+                if (i < cnt) raw[y][q] = reinterpret_cast<const uint4*>(src + (int64_t)(row0 + i) * src_stride + ((size_t)h * hd + col) * sizeof(T))[q];
+            }
         }
 #pragma unroll
         for (int y = 0; y < U; ++y) {
             if (i0 + y * groups >= cnt) break;   // the same for the whole block
             const uint32_t i = i0 + y * groups + g;
             const bool live = i < cnt;
-            float (&x)[8] = xs[y];
+            float x[8];
+            if (sizeof(T) == 2) {
+                const uint32_t w[4] = {raw[y][0].x, raw[y][0].y, raw[y][0].z, raw[y][0].w};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) x[q] = q & 1 ? bf_hi(w[q / 2]) : bf_lo(w[q / 2]);
+            } else {
+                const uint4 p = raw[y][0], q = raw[y][sizeof(T) / 2 - 1];
+                const uint32_t w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k]);
+            }
             uint8_t* out = dst + (int64_t)(off0 + (live ? i : 0u)) * c.row_b;
             if (c.fp8) {
                 float big = 0.f;
@@ -309,13 +301,14 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
     }
 }
 
-// Sequence a row belongs to: the largest s with row_starts[s] <= row (the last of several that start there).
-__device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const PagedRows& r, uint32_t row) {
+// Sequence a row belongs to: the largest s with row_starts[s] <= row (the last of several that start there).  `starts`:
+// the array in shared memory, or null.
+__device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const PagedRows& r, const uint32_t* starts, uint32_t row) {
     if (!r.row_starts) return row;
     uint32_t lo = 0, hi = c.n_seqs;
     while (hi - lo > 1u) {
         const uint32_t mid = (lo + hi) / 2u;
-        if (pg_row_start(c, r, mid) <= row) lo = mid;
+        if ((starts ? starts[mid] : pg_row_start(c, r, mid)) <= row) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -324,6 +317,7 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
 // Read back.  A vector = one row of one head, K or V; hd / E lanes share it (E = 8 columns each, 16 of an e4m3 row: 16 bytes
 // of the cache either way).  A lane works on PR_UNROLL vectors at once: all their page look-ups, then all their rows.
 constexpr int PR_UNROLL = 4;
+constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in shared memory
 template <class T, bool FP8>
 __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedView c, const PagedRows rows) {
     constexpr uint32_t E = FP8 ? 16 : 8;
@@ -331,11 +325,14 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedVi
     griddep_wait();
     if (pg_stopped(c)) return;
     const uint32_t lanes = c.hd / E, groups = PG_THREADS / lanes, grp = threadIdx.x / lanes, col = threadIdx.x % lanes * E;
-    if (rows.row_starts && blockIdx.x == 0u)
-        for (uint32_t s = threadIdx.x; s < c.n_seqs; s += PG_THREADS) {
-            const int32_t a = rows.row_starts[s], b = rows.row_starts[s + 1u];
-            if (a < 0 || b < a || (uint32_t)b > rows.n_rows) pg_error(c);
-        }
+    if (rows.row_starts && blockIdx.x == 0u) pg_check_starts(c, rows);
+    __shared__ uint32_t starts_s[PR_STARTS + 1];
+    const bool kept = rows.row_starts && c.n_seqs <= PR_STARTS;
+    if (kept) {
+        for (uint32_t s = threadIdx.x; s <= c.n_seqs; s += PG_THREADS) starts_s[s] = pg_row_start(c, rows, s);
+        __syncthreads();
+    }
+    const uint32_t* starts = kept ? starts_s : nullptr;
     const uint64_t v0 = (uint64_t)blockIdx.x * groups * PR_UNROLL + grp;
     uint32_t row[PR_UNROLL], head[PR_UNROLL];   // head: nkv + head for values
     int64_t src[PR_UNROLL], exp_at[PR_UNROLL];
@@ -349,8 +346,8 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedVi
         head[u] = (uint32_t)(vec - r64 * 2u * c.nkv);
         src[u] = exp_at[u] = 0;
         if (!live[u]) continue;
-        const uint32_t s = pg_seq_of_row(c, rows, row[u]);
-        const uint32_t r0 = pg_row_start(c, rows, s), r1 = pg_row_start(c, rows, s + 1u);
+        const uint32_t s = pg_seq_of_row(c, rows, starts, row[u]);
+        const uint32_t r0 = starts ? starts[s] : pg_row_start(c, rows, s), r1 = starts ? starts[s + 1u] : pg_row_start(c, rows, s + 1u);
         const int32_t pos = c.positions[s];
         live[u] = pos >= 0 && row[u] >= r0 && row[u] < r1;
         if (!live[u]) continue;
@@ -426,20 +423,21 @@ __device__ __forceinline__ uint32_t pg_key(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int PS_PAGES = 4;                            // pages a group of eight lanes scores at a time
-constexpr int PS_BLOCK = PG_THREADS / 8 * PS_PAGES;    // pages per unit: 128
+constexpr int PS_PAGES = 2;                            // pages a group of eight lanes scores at a time
+constexpr int PS_BLOCK = PG_THREADS / 8 * PS_PAGES;    // pages per unit: 64
 
 // Scores.  Work is cut into units of PS_BLOCK pages of one (sequence, kv head); every block of the grid takes an equal,
 // contiguous range of all units.  Eight lanes share a page (16-byte pieces of its lower and upper bounds, both read once
-// for up to GT heads) and score PS_PAGES pages at once, so that a query element fetched from shared memory is used four
-// times.  The products of a bf16 bound and a query are exact in 64 bits, and so, but for extreme spreads, are their sums: the
-// rounded score does not depend on the order of additions.  What bounds it: with eight heads per kv head the 64-bit
-// pipe and the selects in front of it, not memory.
+// for up to GT heads) and score PS_PAGES pages at once.  The products of a bf16 bound and a query are exact in 64 bits, and
+// so, but for extreme spreads, are their sums: the rounded score does not depend on the order of additions.
+// What bounds it: with eight heads per kv head not memory but the 64-bit pipe (16 lanes per clock and scheduler) and the
+// selects of upper or lower bound in front of it (two 32-bit ones per operand).  Half of the heads therefore select, the
+// other half issue both products under opposite predicates, which balances the two pipes.
 template <int HD, int GT>
-__global__ void __launch_bounds__(PG_THREADS) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
+__global__ void __launch_bounds__(PG_THREADS, GT == 8 ? 2 : 3) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
     constexpr int NW = PG_THREADS / 32, NC = HD / 64;   // 16-byte pieces of a bound per lane
     __shared__ uint64_t pre[PG_THREADS], wsum[NW];
-    __shared__ double q_s[NC * 8][GT][8];               // [piece, element][head][lane of the group]
+    __shared__ __align__(16) double q_s[NC * 8][(GT + 1) / 2][8][2];   // [piece, element][pair of heads][lane of the group][head]
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
@@ -474,13 +472,13 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_score_kernel(const PagedV
                 b[x] = c.bounds + ((int64_t)max(phys, 0) * c.nkv + h) * 2 * HD + l8 * 8;
             }
         }
-        float best = __int_as_float(0x7fc00000);   // NaN; of page l8 >> 1 of the group, see the reduction
+        float best = __int_as_float(0x7fc00000);   // NaN; of page l8 >> 2 of the group, see the reduction
         for (uint32_t ht = 0; ht < HT; ++ht) {
             if (fresh || HT > 1u) {
                 __syncthreads();
                 for (uint32_t i = tid; i < (uint32_t)(HD * GT); i += PG_THREADS) {
                     const uint32_t d = i % HD, gg = i / HD, head = min(ht * GT + gg, a.G - 1u);   // a missing head repeats the last
-                    q_s[(d / 64) * 8 + d % 8][gg][(d / 8) % 8] = (double)pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + head) * HD + d);
+                    q_s[(d / 64) * 8 + d % 8][gg / 2][(d / 8) % 8][gg % 2] = (double)pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + head) * HD + d);
                 }
                 __syncthreads();
                 fresh = false;
@@ -512,31 +510,48 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_score_kernel(const PagedV
                         hd[x] = (double)(i & 1 ? bf_hi(hw[x][i / 2]) : bf_lo(hw[x][i / 2]));
                     }
 #pragma unroll
-                    for (int gg = 0; gg < GT; ++gg) {
-                        const double q = q_s[cc * 8 + i][gg][l8];
-                        const bool up = q >= 0.0;
+                    for (int gp = 0; gp < (GT + 1) / 2; ++gp) {
+                        const double2 q2 = *reinterpret_cast<const double2*>(q_s[cc * 8 + i][gp][l8]);
+                        const bool up = q2.x >= 0.0;
 #pragma unroll
-                        for (int x = 0; x < PS_PAGES; ++x) acc[x][gg] = fma(q, up ? hd[x] : ld[x], acc[x][gg]);
+                        for (int x = 0; x < PS_PAGES; ++x) acc[x][2 * gp] = fma(q2.x, up ? hd[x] : ld[x], acc[x][2 * gp]);
+                        if (2 * gp + 1 < GT) {
+                            const int k = 2 * gp + 1 < GT ? 2 * gp + 1 : 0;
+                            static_assert(PS_PAGES == 2, "both pages in one block");
+                            asm("{\n\t.reg .pred p;\n\tsetp.ge.f64 p, %2, 0d0000000000000000;\n\t"
+                                "@p fma.rn.f64 %0, %2, %3, %0;\n\t@p fma.rn.f64 %1, %2, %4, %1;\n\t"
+                                "@!p fma.rn.f64 %0, %2, %5, %0;\n\t@!p fma.rn.f64 %1, %2, %6, %1;\n\t}"
+                                : "+d"(acc[0][k]), "+d"(acc[1][k])
+                                : "d"(q2.y), "d"(hd[0]), "d"(hd[1]), "d"(ld[0]), "d"(ld[1]));
+                        }
                     }
                 }
             }
-            // sums over the eight lanes, halving the pages a lane keeps in the first two steps
-            double r2[2][GT], r1[GT];
+            // sums over the eight lanes: every step halves what a lane keeps -- a page of two, then half of the heads twice
+            double r[GT];
+            constexpr int H2 = GT >= 2 ? GT / 2 : 1, H1 = GT >= 4 ? GT / 4 : 1;
 #pragma unroll
             for (int gg = 0; gg < GT; ++gg) {
+                const double keep = l8 & 4u ? acc[1][gg] : acc[0][gg], give = l8 & 4u ? acc[0][gg] : acc[1][gg];
+                r[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+            }
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const double keep = l8 & 4u ? acc[x + 2][gg] : acc[x][gg], give = l8 & 4u ? acc[x][gg] : acc[x + 2][gg];
-                    r2[x][gg] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
-                }
-                const double keep = l8 & 2u ? r2[1][gg] : r2[0][gg], give = l8 & 2u ? r2[0][gg] : r2[1][gg];
-                r1[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
-                r1[gg] += __shfl_xor_sync(0xffffffffu, r1[gg], 1);
-                best = fmaxf(best, (float)r1[gg]);   // fmaxf leaves NaN out
+            for (int gg = 0; gg < H2; ++gg) {
+                const int k = GT >= 2 ? gg + H2 : gg;
+                const double keep = l8 & 2u ? r[k] : r[gg], give = l8 & 2u ? r[gg] : r[k];
+                r[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+            }
+#pragma unroll
+            for (int gg = 0; gg < H1; ++gg) {
+                const int k = GT >= 4 ? gg + H1 : gg;
+                const double keep = l8 & 1u ? r[k] : r[gg], give = l8 & 1u ? r[gg] : r[k];
+                best = fmaxf(best, (float)(keep + __shfl_xor_sync(0xffffffffu, give, 1)));   // fmaxf leaves NaN out
             }
         }
-        const uint32_t page = p0 + (l8 >> 1);   // lanes 4.. hold pages 2, 3; of these, lanes 2, 3, 6, 7 the odd ones
-        if (!(l8 & 1u) && page < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + page] = best;
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+        const uint32_t page = p0 + (l8 >> 2);
+        if (!(l8 & 3u) && page < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + page] = best;
         if (++u == nu) {
             u = 0;
             fresh = true;
