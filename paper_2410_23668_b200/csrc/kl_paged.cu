@@ -96,7 +96,7 @@ PagedRows rows_of(const int32_t* row_starts_d, uint32_t n_rows, const void* k, c
 }
 
 size_t score_bytes(const kl_paged_cache* c, uint64_t n_seqs, uint64_t table_pages) {
-    return (size_t)((n_seqs * c->n_kv_heads * table_pages * 4 + 255) / 256 * 256);
+    return (size_t)((n_seqs * c->n_kv_heads * table_pages * 8 + 255) / 256 * 256);
 }
 
 kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_seqs) {
@@ -141,18 +141,14 @@ kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
     return KL_OK;
 }
 
-// Scores: up to eight heads at once, as many blocks as the SMs hold.
-template <int HD>
-kl_status launch_score_hd(const PagedView& v, const PagedSelect& a, unsigned sms, void* stream) {
-    const unsigned blocks = (a.G <= 4 ? 3u : 2u) * sms;
-    if (a.G == 1) return launch(kl_paged_score_kernel<HD, 1>, dim3(blocks), PG_THREADS, 0, stream, v, a);
-    if (a.G == 2) return launch(kl_paged_score_kernel<HD, 2>, dim3(blocks), PG_THREADS, 0, stream, v, a);
-    if (a.G <= 4) return launch(kl_paged_score_kernel<HD, 4>, dim3(blocks), PG_THREADS, 0, stream, v, a);
-    return launch(kl_paged_score_kernel<HD, 8>, dim3(blocks), PG_THREADS, 0, stream, v, a);
+template <int HD, bool F32>
+kl_status launch_score_as(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
+    return launch(kl_paged_score_kernel<HD, F32>, dim3((unsigned)(ps_blocks_per_sm<HD, F32>() * sms)), PG_THREADS, 0, stream, v, a);
 }
 kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
-    const unsigned n = (unsigned)sms;
-    return v.hd == 64 ? launch_score_hd<64>(v, a, n, stream) : v.hd == 128 ? launch_score_hd<128>(v, a, n, stream) : launch_score_hd<256>(v, a, n, stream);
+    if (v.hd == 64) return a.q_f32 ? launch_score_as<64, true>(v, a, sms, stream) : launch_score_as<64, false>(v, a, sms, stream);
+    if (v.hd == 128) return a.q_f32 ? launch_score_as<128, true>(v, a, sms, stream) : launch_score_as<128, false>(v, a, sms, stream);
+    return a.q_f32 ? launch_score_as<256, true>(v, a, sms, stream) : launch_score_as<256, false>(v, a, sms, stream);
 }
 
 template <int HD, bool FP8, int UR, bool EX>
@@ -248,7 +244,7 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     a.G = n_q_heads / cache->n_kv_heads;
     a.keep_first = keep_first; a.keep_last = keep_last; a.n_select = n_select;
     a.selected = selected_d;
-    a.scores = (float*)workspace_d;
+    a.scores = (float2*)workspace_d;
     const int sms = attn_blocks();
     if (sms <= 0) return KL_ERR_CUDA;
     if ((rc = launch_score(v, a, sms, stream)) != KL_OK) return rc;

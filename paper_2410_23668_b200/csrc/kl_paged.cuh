@@ -410,7 +410,7 @@ struct PagedSelect {
     uint32_t q_f32, nq, G;
     uint32_t keep_first, keep_last, n_select;
     int32_t* selected;
-    float* scores;         // [n_seqs][nkv][table_pages]
+    float2* scores;        // [n_seqs][nkv][table_pages]: score, largest magnitude among the bounds
 };
 __device__ __forceinline__ float pg_q(const uint8_t* row, uint32_t f32, uint32_t i) {
     return f32 ? reinterpret_cast<const float*>(row)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[i]);
@@ -423,180 +423,236 @@ __device__ __forceinline__ uint32_t pg_key(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int PS_PAGES = 2;                            // pages a group of eight lanes scores at a time
-constexpr int PS_BLOCK = PG_THREADS / 8 * PS_PAGES;    // pages per unit: 64
+// The exact score of a page, by one warp: sums in 64 bits (the products of a bf16 bound and a query are exact there, and so,
+// but for extreme spreads, are their sums), rounded once to 32.
+__device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect& a, uint32_t s, uint32_t h, int32_t phys) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const __nv_bfloat16* b = c.bounds + ((int64_t)phys * c.nkv + h) * 2 * c.hd;
+    const uint8_t* q = a.q + (int64_t)s * a.q_stride;
+    float best = __int_as_float(0x7fc00000);   // NaN
+    for (uint32_t g = 0; g < a.G; ++g) {
+        double sum = 0.0;
+        for (uint32_t d = lane; d < c.hd; d += 32u) {
+            const float x = pg_q(q, a.q_f32, (h * a.G + g) * c.hd + d);
+            sum += (double)x * (double)__bfloat162float(x >= 0.f ? b[c.hd + d] : b[d]);
+        }
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        best = fmaxf(best, (float)sum);        // fmaxf leaves NaN out
+    }
+    return best;
+}
 
-// Scores.  Work is cut into units of PS_BLOCK pages of one (sequence, kv head); every block of the grid takes an equal,
-// contiguous range of all units.  Eight lanes share a page (16-byte pieces of its lower and upper bounds, both read once
-// for up to GT heads) and score PS_PAGES pages at once.  The products of a bf16 bound and a query are exact in 64 bits, and
-// so, but for extreme spreads, are their sums: the rounded score does not depend on the order of additions.
-// What bounds it: with eight heads per kv head not memory but the 64-bit pipe (16 lanes per clock and scheduler) and the
-// selects of upper or lower bound in front of it (two 32-bit ones per operand).  Half of the heads therefore select, the
-// other half issue both products under opposite predicates, which balances the two pipes.
-template <int HD, int GT>
-__global__ void __launch_bounds__(PG_THREADS, GT == 8 ? 2 : 3) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
-    constexpr int NW = PG_THREADS / 32, NC = HD / 64;   // 16-byte pieces of a bound per lane
+// Scores good to a known bound, on the tensor cores: kl_paged_topk_kernel computes exact ones where the bound leaves the
+// choice open, which is a page or two of thousands (64-bit scores for every page kept the 64-bit pipe and the selects in
+// front of it busy for five times as long as reading the bounds takes).
+//   max(q lo, q hi) = min(q, 0) lo + max(q, 0) hi: with the bounds [lo | hi] of a page as a row of 2 hd numbers and
+//   [min(q, 0) | max(q, 0)] as columns it is one matrix product, pages x heads.  16 pages are the rows of mma.m16n8k16, up to
+//   eight heads its columns; the rows go from memory straight into the operand's registers (the order of the columns is
+//   free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
+//   all tiles of 16 pages.  Written per page: the score, and the largest magnitude among its bounds, for the error's bound.
+template <int HD, bool F32>
+constexpr int ps_blocks_per_sm() { return HD == 256 || (HD == 128 && F32) ? 1 : 2; }   // what the registers allow
+template <int HD, bool F32>   // F32: type of the queries
+__global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
+    constexpr int NW = PG_THREADS / 32, NC = HD / 16;   // 16-byte pieces of a row's 4 hd bytes per lane
+    constexpr int BATCH = NC > 8 ? 8 : NC;              // of them in flight at once
     __shared__ uint64_t pre[PG_THREADS], wsum[NW];
-    __shared__ __align__(16) double q_s[NC * 8][(GT + 1) / 2][8][2];   // [piece, element][pair of heads][lane of the group][head]
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, l8 = lane & 7u;
-    const uint32_t n = c.n_seqs, per = (n + PG_THREADS - 1u) / PG_THREADS, HT = (a.G + GT - 1u) / GT;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, j = lane & 3u;
+    const uint32_t n = c.n_seqs, per = (n + PG_THREADS - 1u) / PG_THREADS, HT = (a.G + 7u) / 8u;
     auto pages_of = [&](uint32_t s) { return (pg_length(c, s) + c.page - 1u) / c.page; };
-    const uint64_t W = pg_prefix<NW>(n, pre, wsum, [&](uint32_t s) { return (uint64_t)((pages_of(s) + PS_BLOCK - 1u) / PS_BLOCK) * c.nkv; });
-    const uint64_t share = pg_div(W, gridDim.x), over = W - share * gridDim.x;
-    const uint64_t lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), hi = lo + share + (blockIdx.x < over ? 1u : 0u);
+    const uint64_t W = pg_prefix<NW>(n, pre, wsum, [&](uint32_t s) { return (uint64_t)((pages_of(s) + 15u) / 16u) * c.nkv; });
+    const uint32_t warps = gridDim.x * NW, w = warp * gridDim.x + blockIdx.x;   // few tiles spread over the SMs
+    const uint64_t share = pg_div(W, warps), over = W - share * warps;
+    const uint64_t lo = share * w + min((uint64_t)w, over), hi = lo + share + (w < over ? 1u : 0u);
     if (lo >= hi) return;
     const uint32_t i0 = pg_find<NW>(pre, lo);
     uint64_t rem = lo - pre[i0];
-    uint32_t s = i0 * per, np = pages_of(s), nu = (np + PS_BLOCK - 1u) / PS_BLOCK;   // units per head of sequence s
-    while (rem >= (uint64_t)nu * c.nkv) {
-        rem -= (uint64_t)nu * c.nkv;
+    uint32_t s = i0 * per, np = pages_of(s), nt = (np + 15u) / 16u;   // pages and tiles per head of sequence s
+    while (rem >= (uint64_t)nt * c.nkv) {
+        rem -= (uint64_t)nt * c.nkv;
         np = pages_of(++s);
-        nu = (np + PS_BLOCK - 1u) / PS_BLOCK;
+        nt = (np + 15u) / 16u;
     }
-    uint32_t h = (uint32_t)pg_div(rem, nu), u = (uint32_t)(rem - (uint64_t)h * nu);
-    bool fresh = true;
+    uint32_t h = (uint32_t)pg_div(rem, nt), t = (uint32_t)(rem - (uint64_t)h * nt);
+    uint32_t qf[NC][2][2], ql[F32 ? NC : 1][2][2];   // B fragments of the current head tile, and what bf16 leaves of fp32 queries
+    auto look_up = [&](uint32_t ss, uint32_t tt, uint32_t pages) -> int32_t {   // lane l < 16: page 16 tt + l
+        const uint32_t p = tt * 16u + lane;
+        return lane < 16u && p < pages ? pg_physical(c, ss, p) : -1;
+    };
+    auto load_queries = [&](uint32_t ht) {
+        const uint32_t head = h * a.G + min(ht * 8u + g, a.G - 1u);   // a missing head repeats the last one
+        const uint8_t* q = a.q + (int64_t)s * a.q_stride + (size_t)head * HD * (F32 ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t d = (i % (NC / 2)) * 32 + j * 8 + x * 4;
+                float v[4];
+                if (F32) {
+                    const float4 f = *reinterpret_cast<const float4*>(q + d * 4);
+                    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+                } else {
+                    const uint2 f = *reinterpret_cast<const uint2*>(q + d * 2);
+                    v[0] = bf_lo(f.x); v[1] = bf_hi(f.x); v[2] = bf_lo(f.y); v[3] = bf_hi(f.y);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = i < NC / 2 ? fminf(v[e], 0.f) : fmaxf(v[e], 0.f);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    qf[i][x][e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                    if (F32) ql[F32 ? i : 0][x][e] = pack_bf16(v[2 * e] - bf_lo(qf[i][x][e]), v[2 * e + 1] - bf_hi(qf[i][x][e]));
+                }
+            }
+    };
+    int32_t ids = look_up(s, t, np);
+    if (HT == 1u) load_queries(0);
     for (uint64_t left = hi - lo; left; --left) {
-        const uint32_t p0 = u * PS_BLOCK + warp * (4 * PS_PAGES) + (lane >> 3) * PS_PAGES;   // this group's pages
-        const __nv_bfloat16* b[PS_PAGES];
-        bool live[PS_PAGES];
-#pragma unroll
-        for (int x = 0; x < PS_PAGES; ++x) {
-            live[x] = false;
-            b[x] = c.bounds;
-            if (p0 + x < np) {
-                const int32_t phys = pg_physical(c, s, p0 + x);
-                live[x] = phys >= 0;
-                b[x] = c.bounds + ((int64_t)max(phys, 0) * c.nkv + h) * 2 * HD + l8 * 8;
+        const int32_t p0 = __shfl_sync(0xffffffffu, ids, g), p1 = __shfl_sync(0xffffffffu, ids, g + 8u);
+        const uint4* r0 = reinterpret_cast<const uint4*>(c.bounds + ((int64_t)max(p0, 0) * c.nkv + h) * 2 * HD) + j;
+        const uint4* r1 = reinterpret_cast<const uint4*>(c.bounds + ((int64_t)max(p1, 0) * c.nkv + h) * 2 * HD) + j;
+        // the next tile, whose look-up travels with this one's rows
+        uint32_t ns = s, nh = h, ntile = t + 1u, npages = np;
+        if (ntile == nt) {
+            ntile = 0;
+            if (++nh == c.nkv && left > 1u) {
+                nh = 0;
+                do npages = pages_of(++ns);
+                while (npages == 0u);
             }
         }
-        float best = __int_as_float(0x7fc00000);   // NaN; of page l8 >> 2 of the group, see the reduction
+        if (left > 1u) ids = look_up(ns, ntile, npages);
+        float best0 = -INFINITY, best1 = -INFINITY;
+        uint32_t big0 = 0, big1 = 0;   // largest magnitudes, as bf16 bit patterns (two columns of them)
         for (uint32_t ht = 0; ht < HT; ++ht) {
-            if (fresh || HT > 1u) {
-                __syncthreads();
-                for (uint32_t i = tid; i < (uint32_t)(HD * GT); i += PG_THREADS) {
-                    const uint32_t d = i % HD, gg = i / HD, head = min(ht * GT + gg, a.G - 1u);   // a missing head repeats the last
-                    q_s[(d / 64) * 8 + d % 8][gg / 2][(d / 8) % 8][gg % 2] = (double)pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + head) * HD + d);
-                }
-                __syncthreads();
-                fresh = false;
-            }
-            double acc[PS_PAGES][GT];
+            if (HT > 1u) load_queries(ht);
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int x = 0; x < PS_PAGES; ++x)
+            for (int i0_ = 0; i0_ < NC; i0_ += BATCH) {
+                uint4 x[BATCH], y[BATCH];
 #pragma unroll
-                for (int gg = 0; gg < GT; ++gg) acc[x][gg] = 0.0;
-#pragma unroll
-            for (int cc = 0; cc < NC; ++cc) {
-                uint32_t lw[PS_PAGES][4], hw[PS_PAGES][4];
-#pragma unroll
-                for (int x = 0; x < PS_PAGES; ++x) {
-                    uint4 l4 = make_uint4(0u, 0u, 0u, 0u), h4 = l4;
-                    if (live[x]) {
-                        l4 = *reinterpret_cast<const uint4*>(b[x] + cc * 64);
-                        h4 = *reinterpret_cast<const uint4*>(b[x] + HD + cc * 64);
-                    }
-                    lw[x][0] = l4.x; lw[x][1] = l4.y; lw[x][2] = l4.z; lw[x][3] = l4.w;
-                    hw[x][0] = h4.x; hw[x][1] = h4.y; hw[x][2] = h4.z; hw[x][3] = h4.w;
+                for (int i = 0; i < BATCH; ++i) {
+                    x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (p0 >= 0) x[i] = r0[(i0_ + i) * 4];
+                    if (p1 >= 0) y[i] = r1[(i0_ + i) * 4];
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    double ld[PS_PAGES], hd[PS_PAGES];
-#pragma unroll
-                    for (int x = 0; x < PS_PAGES; ++x) {
-                        ld[x] = (double)(i & 1 ? bf_hi(lw[x][i / 2]) : bf_lo(lw[x][i / 2]));
-                        hd[x] = (double)(i & 1 ? bf_hi(hw[x][i / 2]) : bf_lo(hw[x][i / 2]));
+                for (int i = 0; i < BATCH; ++i) {
+                    const int k = i0_ + i;
+                    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                        : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
+                        : "r"(x[i].x), "r"(y[i].x), "r"(x[i].y), "r"(y[i].y), "r"(qf[k][0][0]), "r"(qf[k][0][1]));
+                    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                        : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
+                        : "r"(x[i].z), "r"(y[i].z), "r"(x[i].w), "r"(y[i].w), "r"(qf[k][1][0]), "r"(qf[k][1][1]));
+                    if (F32) {
+                        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                            : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
+                            : "r"(x[i].x), "r"(y[i].x), "r"(x[i].y), "r"(y[i].y), "r"(ql[F32 ? k : 0][0][0]), "r"(ql[F32 ? k : 0][0][1]));
+                        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                            : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
+                            : "r"(x[i].z), "r"(y[i].z), "r"(x[i].w), "r"(y[i].w), "r"(ql[F32 ? k : 0][1][0]), "r"(ql[F32 ? k : 0][1][1]));
                     }
-#pragma unroll
-                    for (int gp = 0; gp < (GT + 1) / 2; ++gp) {
-                        const double2 q2 = *reinterpret_cast<const double2*>(q_s[cc * 8 + i][gp][l8]);
-                        const bool up = q2.x >= 0.0;
-#pragma unroll
-                        for (int x = 0; x < PS_PAGES; ++x) acc[x][2 * gp] = fma(q2.x, up ? hd[x] : ld[x], acc[x][2 * gp]);
-                        if (2 * gp + 1 < GT) {
-                            const int k = 2 * gp + 1 < GT ? 2 * gp + 1 : 0;
-                            static_assert(PS_PAGES == 2, "both pages in one block");
-                            asm("{\n\t.reg .pred p;\n\tsetp.ge.f64 p, %2, 0d0000000000000000;\n\t"
-                                "@p fma.rn.f64 %0, %2, %3, %0;\n\t@p fma.rn.f64 %1, %2, %4, %1;\n\t"
-                                "@!p fma.rn.f64 %0, %2, %5, %0;\n\t@!p fma.rn.f64 %1, %2, %6, %1;\n\t}"
-                                : "+d"(acc[0][k]), "+d"(acc[1][k])
-                                : "d"(q2.y), "d"(hd[0]), "d"(hd[1]), "d"(ld[0]), "d"(ld[1]));
-                        }
+                    if (ht == 0u) {
+                        const uint32_t m = 0x7fff7fffu;
+                        big0 = __vmaxu2(__vmaxu2(big0, __vmaxu2(x[i].x & m, x[i].y & m)), __vmaxu2(x[i].z & m, x[i].w & m));
+                        big1 = __vmaxu2(__vmaxu2(big1, __vmaxu2(y[i].x & m, y[i].y & m)), __vmaxu2(y[i].z & m, y[i].w & m));
                     }
                 }
             }
-            // sums over the eight lanes: every step halves what a lane keeps -- a page of two, then half of the heads twice
-            double r[GT];
-            constexpr int H2 = GT >= 2 ? GT / 2 : 1, H1 = GT >= 4 ? GT / 4 : 1;
-#pragma unroll
-            for (int gg = 0; gg < GT; ++gg) {
-                const double keep = l8 & 4u ? acc[1][gg] : acc[0][gg], give = l8 & 4u ? acc[0][gg] : acc[1][gg];
-                r[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 4);
-            }
-#pragma unroll
-            for (int gg = 0; gg < H2; ++gg) {
-                const int k = GT >= 2 ? gg + H2 : gg;
-                const double keep = l8 & 2u ? r[k] : r[gg], give = l8 & 2u ? r[gg] : r[k];
-                r[gg] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
-            }
-#pragma unroll
-            for (int gg = 0; gg < H1; ++gg) {
-                const int k = GT >= 4 ? gg + H1 : gg;
-                const double keep = l8 & 1u ? r[k] : r[gg], give = l8 & 1u ? r[gg] : r[k];
-                best = fmaxf(best, (float)(keep + __shfl_xor_sync(0xffffffffu, give, 1)));   // fmaxf leaves NaN out
-            }
+            // (a NaN must not be lost in a maximum: it says that the score is not known)
+            auto larger = [](float u, float v) { return isnan(u) || isnan(v) ? __int_as_float(0x7fc00000) : fmaxf(u, v); };
+            best0 = larger(best0, larger(acc[0], acc[1]));
+            best1 = larger(best1, larger(acc[2], acc[3]));
         }
-        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
-        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
-        const uint32_t page = p0 + (l8 >> 2);
-        if (!(l8 & 3u) && page < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + page] = best;
-        if (++u == nu) {
-            u = 0;
-            fresh = true;
-            if (++h == c.nkv && left > 1u) {
-                h = 0;
-                do {
-                    np = pages_of(++s);
-                    nu = (np + PS_BLOCK - 1u) / PS_BLOCK;
-                } while (nu == 0u);
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            const float u = __shfl_xor_sync(0xffffffffu, best0, o), v = __shfl_xor_sync(0xffffffffu, best1, o);
+            best0 = isnan(u) || isnan(best0) ? __int_as_float(0x7fc00000) : fmaxf(best0, u);
+            best1 = isnan(v) || isnan(best1) ? __int_as_float(0x7fc00000) : fmaxf(best1, v);
+            big0 = __vmaxu2(big0, __shfl_xor_sync(0xffffffffu, big0, o));
+            big1 = __vmaxu2(big1, __shfl_xor_sync(0xffffffffu, big1, o));
+        }
+        if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
+            const uint32_t p = t * 16u + g + j * 8u, b = j ? big1 : big0;
+            const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
+            if (p < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + p] = make_float2(j ? best1 : best0, mag);
+        }
+        if (left > 1u) {
+            const bool other = ns != s || nh != h;
+            if (ns != s) {
+                np = npages;
+                nt = (np + 15u) / 16u;
             }
+            s = ns; h = nh; t = ntile;
+            if (other && HT == 1u) load_queries(0);
         }
     }
 }
 
-// The choice: one block per (sequence, kv head).  The threshold -- the largest key t that at least `need` pages reach -- is found
-// bit by bit, starting below the bits all keys share and ending as soon as exactly `need` pages reach it (a dozen steps,
-// not 32).  KPT > 0: every thread keeps KPT neighbouring keys in registers, and one prefix sum puts the pages in order;
-// KPT == 0: any number of pages, read again for every step.
+// The choice: one block per (sequence, kv head).
+//   1. T = the need-th largest of the approximate scores, found bit by bit from below the bits all of them share.
+//   2. With E a bound of their errors, pages above T + 2 E are chosen for certain and pages below T - 2 E are not.  What lies
+//      between is chosen too if there is room for all of it; otherwise its exact scores decide (equal ones by page).
+//   3. The chosen pages are put in order by a prefix sum.
+// Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
+// magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
+// queries also lose 2^-16 of themselves.  E = 2^-16 (2^-14) times the largest sum |q_d| of a head and the largest bound.
+// A score or bound that is not finite makes every page a candidate.
+// KPT > 0: every thread keeps KPT neighbouring keys in registers; KPT == 0: any number of pages, read again each time.
 constexpr int PT_THREADS = 512;
 template <int KPT>
-__global__ void __launch_bounds__(PT_THREADS) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
+__global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
     constexpr int NW = PT_THREADS / 32, NK = KPT ? KPT : 1;
+    constexpr uint32_t SURE = 0xffffffffu;   // key of a page that is chosen in any case; 0: of one that is not looked at
     __shared__ uint32_t red[2][NW][2];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
     const uint32_t s = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
     const uint32_t n = (pg_length(c, s) + c.page - 1u) / c.page;
-    const float* sc = a.scores + ((size_t)s * c.nkv + h) * c.table_pages;
+    float2* sc = a.scores + ((size_t)s * c.nkv + h) * c.table_pages;
     int32_t* out = a.selected + ((size_t)s * c.nkv + h) * a.n_select;
     if (n <= a.n_select) {   // all of them
         for (uint32_t i = tid; i < a.n_select; i += PT_THREADS) out[i] = i < n ? (int32_t)i : -1;
         return;
     }
     auto forced = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n; };
-    auto key_of = [&](uint32_t i) { return i >= n || forced(i) ? 0u : pg_key(sc[i]); };
-    uint32_t key[NK];
-    if (KPT)
+    uint32_t need = a.n_select - (a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
+
+    // keys: of the approximate scores first, then (KPT == 0: kept in the workspace) of what step 2 leaves of them
+    uint32_t key[NK], mx = 0, mn = 0xffffffffu, mag = 0, odd = 0;
+    float q1 = 0.f;
+    auto take = [&](uint32_t i) {
+        const float2 x = i < n ? sc[i] : make_float2(0.f, 0.f);
+        const uint32_t k = i >= n ? 0u : forced(i) ? SURE : pg_key(x.x);
+        if (k && k != SURE) {
+            mx = max(mx, k);
+            mn = min(mn, k);
+            mag = max(mag, __float_as_uint(x.y));   // not negative: ordered like whole numbers, NaN above infinity
+            odd |= !isfinite(x.x);
+        }
+        return k;
+    };
+    if (KPT) {
 #pragma unroll
-        for (int r = 0; r < NK; ++r) key[r] = key_of(tid * NK + r);
-    const uint32_t need = a.n_select - min(n, a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
+        for (int r = 0; r < NK; ++r) key[r] = take(tid * NK + r);
+    } else {
+        for (uint32_t i = tid; i < n; i += PT_THREADS) take(i);
+    }
+    for (uint32_t gg = warp; gg < a.G; gg += NW) {   // largest sum |q_d| of a head
+        float x = 0.f;
+        for (uint32_t d = lane; d < c.hd; d += 32u) x += fabsf(pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + gg) * c.hd + d));
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        q1 = x <= q1 ? q1 : x;   // keeps NaN
+        if (isnan(x)) odd = 1u;
+    }
     int turn = 0;
-    auto sum2 = [&](uint32_t x, uint32_t y, bool is_max) -> uint2 {   // block sums, or (maximum, minimum)
-        x = is_max ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
-        y = is_max ? __reduce_min_sync(0xffffffffu, y) : __reduce_add_sync(0xffffffffu, y);
+    auto reduce = [&](uint32_t x, uint32_t y, bool extremes) -> uint2 {   // block sums, or (maximum, minimum)
+        x = extremes ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
+        y = extremes ? __reduce_min_sync(0xffffffffu, y) : __reduce_add_sync(0xffffffffu, y);
         if (lane == 0u) {
             red[turn][warp][0] = x;
             red[turn][warp][1] = y;
@@ -606,66 +662,152 @@ __global__ void __launch_bounds__(PT_THREADS) kl_paged_topk_kernel(const PagedVi
 #pragma unroll
         for (int w = 1; w < NW; ++w) {
             const uint32_t p = red[turn][w][0], q = red[turn][w][1];
-            t.x = is_max ? max(t.x, p) : t.x + p;
-            t.y = is_max ? min(t.y, q) : t.y + q;
+            t.x = extremes ? max(t.x, p) : t.x + p;
+            t.y = extremes ? min(t.y, q) : t.y + q;
         }
         turn ^= 1;   // the next call writes the other half, and nobody is two calls behind
         return t;
     };
-    auto count = [&](uint32_t t) {   // pages with a key of at least t
-        uint32_t x = 0;
+    // f(key) for every page of this thread
+    auto each = [&](auto&& f) {
         if (KPT) {
 #pragma unroll
-            for (int r = 0; r < NK; ++r) x += key[r] >= t;
+            for (int r = 0; r < NK; ++r) f(key[r], tid * NK + r);
         } else {
-            for (uint32_t i = tid; i < n; i += PT_THREADS) x += key_of(i) >= t;
-        }
-        return sum2(x, 0u, false).x;
-    };
-    uint32_t t = 0xffffffffu, ties = 0xffffffffu;   // chosen: keys above t, and the first `ties` of those equal to it
-    if (need) {
-        uint32_t mx = 0, mn = 0xffffffffu;
-        auto see = [&](uint32_t k) {
-            mx = max(mx, k);
-            if (k) mn = min(mn, k);
-        };
-        if (KPT) {
-#pragma unroll
-            for (int r = 0; r < NK; ++r) see(key[r]);
-        } else {
-            for (uint32_t i = tid; i < n; i += PT_THREADS) see(key_of(i));
-        }
-        const uint2 mm = sum2(mx, mn, true);
-        const uint32_t differ = mm.x ^ mm.y;
-        bool exact = false;
-        int bit = differ ? 31 - __clz(differ) : -1;
-        t = bit >= 0 ? mm.y & ~((2u << bit) - 1u) : mm.y;
-        for (; bit >= 0 && !exact; --bit) {
-            const uint32_t x = count(t | 1u << bit);
-            if (x >= need) {
-                t |= 1u << bit;
-                exact = x == need;
+            for (uint32_t i = tid; i < n; i += PT_THREADS) {
+                uint32_t k = forced(i) ? SURE : pg_key(sc[i].x);
+                f(k, i);
             }
         }
-        if (!exact) ties = need - (t == 0xffffffffu ? 0u : count(t + 1u));
-    } else {
-        ties = 0;
-    }
-    // in order: a page is chosen if it is forced, above t, or one of the first equal ones
-    uint32_t done = 0, tied = 0;   // chosen pages without the equal ones, and equal ones, so far
-    auto place = [&](uint32_t i, bool sure, bool eq, uint32_t sure_before, uint32_t eq_before) {
-        const uint32_t at = sure_before + min(eq_before, ties);
-        if (i < n && (sure || (eq && eq_before < ties)) && at < a.n_select) out[at] = (int32_t)i;
     };
+    auto count = [&](uint32_t t) {   // pages with t <= key < SURE
+        uint32_t x = 0;
+        each([&](uint32_t k, uint32_t) { x += k >= t && k != SURE; });
+        return reduce(x, 0u, false).x;
+    };
+    // The largest t that at least `want` of the keys between `lo` and `hi` reach, or, as soon as a t is found that exactly
+    // `want` keys reach, that one (exact).
+    auto threshold = [&](uint32_t lo, uint32_t hi, uint32_t want, bool& exact) {
+        const uint32_t differ = lo ^ hi;
+        int bit = differ ? 31 - __clz(differ) : -1;
+        uint32_t t = bit >= 0 ? lo & ~((2u << bit) - 1u) : lo;
+        exact = false;
+        for (; bit >= 0 && !exact; --bit) {
+            const uint32_t x = count(t | 1u << bit);
+            if (x >= want) {
+                t |= 1u << bit;
+                exact = x == want;
+            }
+        }
+        return t;
+    };
+    uint32_t t = SURE - 1u, ties = 0;   // chosen: keys above t, and the first `ties` of those equal to it
+    float above = INFINITY, below = -INFINITY;   // approximate scores above `above` are chosen, those below `below` are not
+    if (need) {
+        const uint2 mm = reduce(mx, mn, true);
+        const uint2 mq = reduce(mag, 0u, true), oq = reduce(max(odd ? 0x7f800000u : 0u, __float_as_uint(q1) & 0x7fffffffu), 0u, true);
+        const float E = __uint_as_float(oq.x) * 1.001f * __uint_as_float(mq.x) * (a.q_f32 ? 0x1p-14f : 0x1p-16f);
+        uint32_t cand = 0, sure = 0;
+        if (isfinite(E)) {
+            bool exact;
+            const uint32_t t0 = threshold(mm.y, mm.x, need, exact);
+            uint32_t low = 0xffffffffu;   // the smallest key that reaches t0: the need-th largest
+            each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
+            const uint32_t kt = reduce(0u, low, true).y;
+            const float T = __uint_as_float(kt & 0x80000000u ? kt & 0x7fffffffu : ~kt);
+            above = __fadd_ru(T, 2.f * E);
+            below = __fadd_rd(T, -2.f * E);
+        }
+        each([&](uint32_t k, uint32_t i) {
+            if (!k || k == SURE) return;
+            const float x = __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);   // NaN: neither above nor below
+            const bool up = k != 1u && x > above, down = k != 1u && x < below;
+            sure += up;
+            cand += !up && !down;
+        });
+        const uint2 cs = reduce(cand, sure, false);
+        const uint32_t room = need - cs.y;       // for candidates
+        const bool open = cs.x > room;           // their exact scores decide
+        uint32_t cmx = 0, cmn = 0xffffffffu;
+        auto settle = [&](uint32_t k, bool& is_cand) -> uint32_t {   // SURE or 0 where that is certain
+            const float x = __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+            const bool seen = k && k != SURE, up = seen && k != 1u && x > above, down = seen && k != 1u && x < below;
+            is_cand = seen && !up && !down;
+            return up || (is_cand && !open) ? SURE : down ? 0u : k;
+        };
+        if (KPT && !open) {
+#pragma unroll
+            for (int r = 0; r < NK; ++r) {
+                bool is_cand;
+                key[r] = settle(key[r], is_cand);
+            }
+        } else {   // through the workspace, where a key takes the place of the magnitude; candidates get that of their exact score
+#pragma unroll 1
+            for (uint32_t i0 = 0; i0 < n; i0 += PT_THREADS) {
+                const uint32_t i = i0 + tid;
+                bool is_cand;
+                uint32_t k = settle(i >= n ? 0u : forced(i) ? SURE : pg_key(sc[i].x), is_cand);
+                const int32_t phys = open && is_cand ? pg_physical(c, s, i) : -1;
+                uint32_t todo = __ballot_sync(0xffffffffu, open && is_cand);
+                while (todo) {
+                    const int src = __ffs(todo) - 1;
+                    todo &= todo - 1u;
+                    const int32_t ph = __shfl_sync(0xffffffffu, phys, src);
+                    const uint32_t ek = ph >= 0 ? pg_key(ps_exact(c, a, s, h, ph)) : 1u;
+                    if ((int)lane == src) {
+                        k = ek;
+                        cmx = max(cmx, ek);
+                        cmn = min(cmn, ek);
+                    }
+                }
+                if (i < n) sc[i].y = __uint_as_float(k);
+            }
+            __syncthreads();
+            if (KPT)
+#pragma unroll
+                for (int r = 0; r < NK; ++r) key[r] = tid * NK + r < n ? __float_as_uint(sc[tid * NK + r].y) : 0u;
+        }
+        if (open) {
+            auto each2 = [&](auto&& f) {
+                if (KPT) {
+#pragma unroll
+                    for (int r = 0; r < NK; ++r) f(key[r]);
+                } else {
+                    for (uint32_t i = tid; i < n; i += PT_THREADS) f(__float_as_uint(sc[i].y));
+                }
+            };
+            auto count2 = [&](uint32_t x) {
+                uint32_t y = 0;
+                each2([&](uint32_t k) { y += k >= x && k != SURE; });
+                return reduce(y, 0u, false).x;
+            };
+            const uint2 ce = reduce(cmx, cmn, true);
+            const uint32_t differ = ce.x ^ ce.y;
+            int bit = differ ? 31 - __clz(differ) : -1;
+            t = bit >= 0 ? ce.y & ~((2u << bit) - 1u) : ce.y;
+            bool exact = false;
+            for (; bit >= 0 && !exact; --bit) {
+                const uint32_t x = count2(t | 1u << bit);
+                if (x >= room) {
+                    t |= 1u << bit;
+                    exact = x == room;
+                }
+            }
+            ties = exact ? 0xffffffffu : room - count2(t + 1u);
+        }
+    }
+    // in order
+    uint32_t done = 0, tied = 0;   // chosen pages without the equal ones, and equal ones, so far
     constexpr uint32_t STEP = PT_THREADS * NK;
     for (uint32_t i0 = 0; i0 < n; i0 += STEP) {   // once where the keys are in registers
         bool sure[NK], eq[NK];
         uint32_t ns = 0, ne = 0;
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
-            const uint32_t i = i0 + tid * NK + r, k = KPT ? key[r] : key_of(i);
-            eq[r] = need && k == t;
-            sure[r] = i < n && (k > t || forced(i));
+            const uint32_t i = i0 + tid * NK + r;
+            const uint32_t k = i >= n ? 0u : KPT ? key[r] : forced(i) ? SURE : need ? __float_as_uint(sc[i].y) : 0u;
+            eq[r] = ties && k == t;
+            sure[r] = k > t;
             ns += sure[r];
             ne += eq[r];
         }
@@ -688,7 +830,8 @@ __global__ void __launch_bounds__(PT_THREADS) kl_paged_topk_kernel(const PagedVi
         uint32_t bs = done + (before & 0xffffu), be = tied + (before >> 16);
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
-            place(i0 + tid * NK + r, sure[r], eq[r], bs, be);
+            const uint32_t at = bs + min(be, ties);
+            if ((sure[r] || (eq[r] && be < ties)) && at < a.n_select) out[at] = (int32_t)(i0 + tid * NK + r);
             bs += sure[r];
             be += eq[r];
         }
