@@ -446,6 +446,26 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
                              const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
                              int32_t* status_d, void* stream);
 
+/* One decode step of a batch on a paged cache: kl_decode_step's batched tensor-core path (kl_set_batched_path; the same
+ * projections, one launch per operator) with kl_paged_append, kl_paged_select and kl_paged_attention in the place of the
+ * contiguous cache's append and attention.  Sequences join, leave and share pages by their page table alone.
+ *   layers         HOST array of n_layers descriptors (copied); all with the model's heads and one page_size
+ *   page_table_d   [batch][table_stride], table_pages entries usable: positions 0 .. table_pages * page_size - 1 (max_ctx of the
+ *                  handle does not matter here); the table serves every layer
+ *   positions_d[b] as in kl_decode_step; negative: an empty slot, whose logits are finite but meaningless and whose cache is not
+ *                  touched (kl_argmax_advance adds one to every position: set empty slots back)
+ *   n_select       0: attention over all positions; >= 2: over this many pages per kv head (the first and the last always
+ *                  among them, chosen layer by layer; needs bounds_d)
+ *   workspace_d    kl_paged_step_bytes bytes (cache: any layer's descriptor), 256-byte aligned, need not be cleared
+ * batch 1 .. max_batch; needs a handle with the batched path (max_batch 2 .. 32, dense, head_dim 64 or 128), otherwise
+ * KL_ERR_UNSUPPORTED_SHAPE.  Tokens, positions and the page tables of the whole batch are checked before anything is written: one
+ * bad entry sets the handle's status word (KL_ERR_OUT_OF_RANGE) and makes the step a no-op.  Works on device buffers
+ * alone, so a stream capture of it and kl_argmax_advance can be replayed step after step.  kl_read_hidden follows it as usual. */
+kl_status kl_paged_step_bytes(const kl_handle* h, const kl_paged_cache* cache, uint32_t batch, uint32_t table_pages, uint32_t n_select, size_t* bytes);
+kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int32_t* positions_d, const kl_paged_cache* layers,
+                               const int32_t* page_table_d, int64_t table_stride, uint32_t table_pages, uint32_t n_select, float* logits_d,
+                               uint32_t batch, void* workspace_d, size_t workspace_bytes, void* stream);
+
 const char* kl_status_string(kl_status s);
 
 /* Releases host-side state only (the arenas belong to the caller). */

@@ -43,7 +43,8 @@ EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_by
            "kl_profile_read", "kl_set_trace", "kl_set_tensor_core_attention", "kl_stash_mode", "kl_argmax_advance_static", "kl_set_batched_path",
            "kl_set_dependent_launch", "kl_decode_greedy_host", "kl_decode_greedy", "kl_decode_greedy_tokens",
            "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights",
-           "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention")
+           "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention", "kl_paged_step_bytes",
+           "kl_decode_step_paged")
 
 
 class ModelDesc(C.Structure):
@@ -147,6 +148,10 @@ def lib():
     l.kl_paged_select.restype = i32
     l.kl_paged_attention.argtypes = [pc, ps, vp, vp, C.c_int, i64, i64, u32, C.c_float, u32, vp, u32, vp, vp, C.c_size_t, vp, vp]
     l.kl_paged_attention.restype = i32
+    l.kl_paged_step_bytes.argtypes = [vp, pc, u32, u32, u32, C.POINTER(C.c_size_t)]
+    l.kl_paged_step_bytes.restype = i32
+    l.kl_decode_step_paged.argtypes = [vp, vp, vp, vp, vp, i64, u32, u32, vp, u32, vp, C.c_size_t, vp]
+    l.kl_decode_step_paged.restype = i32
     l.kl_status_string.argtypes = [i32]
     l.kl_status_string.restype = C.c_char_p
     l.kl_destroy.argtypes = [vp]
@@ -436,6 +441,24 @@ class Decoder:
     def kl_decode_greedy_host(self, tokens_h, positions_h, kv_cache_d, next_tokens_h, batch: int, stream=None) -> None:
         _check(lib().kl_decode_greedy_host(self.handle, _ptr(tokens_h), _ptr(positions_h), _ptr(kv_cache_d),
                                            _ptr(next_tokens_h), batch, _stream_ptr(stream)), "kl_decode_greedy_host")
+
+    def kl_paged_step_bytes(self, cache: PagedCache, batch: int, table_pages: int, n_select: int = 0) -> int:
+        b = C.c_size_t()
+        _check(lib().kl_paged_step_bytes(self.handle, cache._ref, batch, table_pages, n_select, C.byref(b)), "kl_paged_step_bytes")
+        return b.value
+
+    def kl_decode_step_paged(self, tokens_d, positions_d, caches, page_table_d, logits_d, workspace_d, n_select: int = 0, stream=None) -> None:
+        """caches: one PagedCache per layer; page_table_d int32 [batch, pages]."""
+        fn = "kl_decode_step_paged"
+        batch, pages = page_table_d.shape
+        _need(len(caches) == self.shape.n_layers and tokens_d.numel() == batch and positions_d.numel() == batch and tokens_d.dtype is _I32 and
+              positions_d.dtype is _I32 and page_table_d.dtype is _I32 and page_table_d.stride(1) == 1 and logits_d.dtype is _F32 and
+              logits_d.numel() == batch * self.shape.vocab and logits_d.is_contiguous() and tokens_d.is_contiguous() and
+              positions_d.is_contiguous() and workspace_d.dtype is _U8 and workspace_d.is_contiguous() and 0 <= n_select < 1 << 31, fn)
+        layers = (PagedCacheDesc * len(caches))(*(c.desc for c in caches))
+        stride = page_table_d.stride(0) if batch > 1 else max(page_table_d.stride(0), pages)
+        _check(lib().kl_decode_step_paged(self.handle, _ptr(tokens_d), _ptr(positions_d), C.addressof(layers), _ptr(page_table_d), stride, pages,
+                                          n_select, _ptr(logits_d), batch, _ptr(workspace_d), workspace_d.numel(), _stream_ptr(stream)), fn)
 
     def kl_argmax_advance(self, logits_d, tokens_d, positions_d, batch: int, stream=None) -> None:
         _check(lib().kl_argmax_advance(self.handle, _ptr(logits_d), _ptr(tokens_d), _ptr(positions_d), batch,

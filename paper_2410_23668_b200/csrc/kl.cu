@@ -23,6 +23,7 @@
 #include <utility>
 
 #include "../../include/kl.h"
+#include "kl_paged_internal.h"
 
 namespace kl {
 
@@ -1555,6 +1556,107 @@ static kl_status decode_step_batched(kl_handle* h, const int32_t* tokens_d, cons
     if (ev && cudaEventRecord(ev[2], st) != cudaSuccess) return KL_ERR_CUDA;
 #undef KL_B_LAUNCH
     return KL_OK;
+}
+
+// Workspace of a step on a paged cache: that of the paged operators, the selected pages, the step's rows of k and v.
+struct PagedStepSpace { size_t ops, selected, rows, bytes; };
+static kl_status paged_step_space(const kl_handle* h, const kl_paged_cache* cache, uint32_t batch, uint32_t table_pages, uint32_t n_select,
+                                  PagedStepSpace* y) {
+    const kl_status rc = kl_paged_workspace_bytes(cache, h->prm.nq, batch, table_pages, &y->ops);
+    if (rc != KL_OK) return rc;
+    y->selected = y->ops;
+    y->rows = y->selected + align_up((size_t)batch * h->prm.nkv * n_select * 4);
+    y->bytes = y->rows + align_up((size_t)2 * 32 * h->prm.KVD * 4);
+    return KL_OK;
+}
+
+kl_status kl_paged_step_bytes(const kl_handle* h, const kl_paged_cache* cache, uint32_t batch, uint32_t table_pages, uint32_t n_select, size_t* bytes) {
+    if (!h || !cache || !bytes || batch == 0 || batch > h->desc.max_batch) return KL_ERR_INVALID_ARG;
+    PagedStepSpace y;
+    const kl_status rc = paged_step_space(h, cache, batch, table_pages, n_select, &y);
+    if (rc == KL_OK) *bytes = y.bytes;
+    return rc;
+}
+
+// The step of decode_step_batched with the paged operators in the place of the cache append, the attention stream and its merge.
+kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int32_t* positions_d, const kl_paged_cache* layers,
+                               const int32_t* page_table_d, int64_t table_stride, uint32_t table_pages, uint32_t n_select, float* logits_d,
+                               uint32_t batch, void* workspace_d, size_t workspace_bytes, void* stream) {
+    if (!h || !tokens_d || !positions_d || !layers || !page_table_d || !logits_d || !workspace_d) return KL_ERR_INVALID_ARG;
+    if (batch == 0 || batch > h->desc.max_batch) return KL_ERR_INVALID_ARG;
+    if (!h->bt_ok) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (n_select == 1) return KL_ERR_INVALID_ARG;   // the first and the last page are always chosen
+    if (!all_loaded(h)) return KL_ERR_NOT_LOADED;
+    const Params& p = h->prm;
+    uint32_t n_pages = 0xffffffffu;
+    for (uint32_t l = 0; l < p.L; ++l) {
+        const kl_paged_cache& c = layers[l];
+        if (c.n_kv_heads != p.nkv || c.head_dim != p.hd || c.page_size != layers[0].page_size || (n_select && !c.bounds_d)) return KL_ERR_INVALID_ARG;
+        if (c.n_pages < n_pages) n_pages = c.n_pages;
+    }
+    PagedStepSpace y;
+    kl_status rc = paged_step_space(h, &layers[0], batch, table_pages, n_select, &y);
+    if (rc != KL_OK) return rc;
+    if (((uintptr_t)workspace_d & 255u) || workspace_bytes < y.bytes) return KL_ERR_INVALID_ARG;
+    if (table_pages == 0 || (uint64_t)table_pages * layers[0].page_size > 0x7fffffffull || table_stride < (int64_t)table_pages) return KL_ERR_INVALID_ARG;
+    uint8_t* ws = (uint8_t*)workspace_d;
+    int32_t* selected = n_select ? (int32_t*)(ws + y.selected) : nullptr;
+    float* rows = (float*)(ws + y.rows);
+    kl_paged_seqs seqs;
+    seqs.positions_d = positions_d;
+    seqs.page_table_d = page_table_d;
+    seqs.table_stride = table_stride;
+    seqs.table_pages = table_pages;
+    seqs.n_seqs = batch;
+    // a descriptor that the operators would refuse is refused before anything is launched
+    for (uint32_t l = 0; l < p.L; ++l)
+        if ((rc = paged_check(&layers[l], &seqs)) != KL_OK) return rc;
+    cudaStream_t st = as_stream(stream);
+    h->chain_tok = nullptr;
+    h->last_batch = batch;
+    h->hidden_is_copy = 1;   // hidden_all holds it, for a single sequence too
+    BAttnView a = {};
+    a.rows = rows;
+    a.positions = positions_d;
+    a.cs = p.rope_cs;
+    a.q = h->bq;
+    a.QD = p.QD; a.KVD = p.KVD; a.nq = p.nq; a.nkv = p.nkv; a.G = p.G; a.hd = p.hd;
+    a.B = batch;
+    a.status = p.status;
+    a.wait_ns = p.wait_ns;
+    BgPartials parts = {};
+#define KL_B_LAUNCH(kernel, grid, block, ...)                                                                    \
+    do {                                                                                                         \
+        if (launch_dependent(h->use_pdl, kernel, dim3(grid), dim3(block), 0, st, __VA_ARGS__) != cudaSuccess) return KL_ERR_CUDA; \
+        ++h->launches;                                                                                           \
+    } while (0)
+    KL_B_LAUNCH(kl_b_embed_paged_kernel, batch, 256, tokens_d, positions_d, p.embed, h->bx, p.H, p.V, table_pages * layers[0].page_size,
+                p.inv_freq, p.rope_cs, p.hd / 2, p.status, page_table_d, table_stride, layers[0].page_size, n_pages);
+    const dim3 grid_h(batch, ceil_div(p.H, (uint32_t)BV_CHUNK)), grid_f(batch, ceil_div(p.F, (uint32_t)BV_CHUNK));
+    for (uint32_t l = 0; l < p.L; ++l) {
+        const size_t lo = (size_t)l * p.layer_stride;
+        a.layer = l;
+        a.bias = p.bqkv ? p.bqkv + lo : nullptr;
+        KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.g1 + lo, 0, p.H, h->bxop[0], h->bssq, p.status);
+        if ((rc = launch_bgemm(h, 0, l, h->bpart, batch, st, &a.qkv)) != KL_OK) return rc;
+        KL_B_LAUNCH(kl_b_rope_rows_kernel, dim3(batch, p.nq + 2 * p.nkv), 128, a);
+        if ((rc = kl_paged_append(&layers[l], &seqs, nullptr, batch, rows, rows + (size_t)32 * p.KVD, KL_F32, p.KVD, p.KVD, p.status, st)) != KL_OK) return rc;
+        ++h->launches;
+        if (n_select) {
+            if ((rc = kl_paged_select(&layers[l], &seqs, h->bq, KL_F32, p.QD, p.nq, 1, 1, n_select, selected, ws, y.ops, p.status, st)) != KL_OK) return rc;
+            h->launches += 2;
+        }
+        if ((rc = paged_attention_operand(&layers[l], &seqs, h->bq, h->bxop[1], p.nq, selected, n_select, ws, y.ops, p.status, st)) != KL_OK) return rc;
+        h->launches += 2;
+        if ((rc = launch_bgemm(h, 1, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;
+        KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.g2 + lo, 0, p.H, h->bxop[0], h->bssq, p.status);
+        if ((rc = launch_bgemm(h, 2, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;
+        KL_B_LAUNCH(kl_b_finish_kernel, grid_f, 256, parts, nullptr, nullptr, nullptr, 1, p.F, h->bxop[2], nullptr, p.status);
+        if ((rc = launch_bgemm(h, 3, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;
+    }
+    KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.gf, 0, p.H, h->bxop[0], h->bssq, p.status);
+#undef KL_B_LAUNCH
+    return launch_bgemm(h, 4, 0, logits_d, batch, st);
 }
 
 // Decode step of a batch as the looped kernel: one cooperative launch for the whole step (KL_MODE_LOOPED), or one

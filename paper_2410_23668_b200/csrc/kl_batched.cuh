@@ -600,12 +600,14 @@ __global__ void __launch_bounds__(256) kl_b_finish_kernel(const BgPartials part,
 
 // Token embedding of every sequence of the batch, the check of the whole batch, and the step's rotary table:
 // x[b] = E[token_b]; cs[b][i] = (cos, sin)(position_b * inv_freq[i]).  Grid (batch), 256 threads.
-template <int NT>
+// EMPTY: a negative position is an empty slot of the batch (token 0 at position 0 is computed for it, and not used) and not
+// an error.
+template <int NT, bool EMPTY = false>
 __device__ __forceinline__ void b_embed_item(const int32_t* tokens, const int32_t* positions, const __nv_bfloat16* embed, float* x,
                                              uint32_t H, uint32_t V, uint32_t max_ctx, const double* inv_freq, float* cs,
                                              uint32_t half, int32_t* status, uint32_t b, uint32_t tid) {
-    int32_t tok = tokens[b];
-    const int32_t pos = positions[b];
+    int32_t tok = tokens[b], pos = positions[b];
+    if (EMPTY && pos < 0) tok = pos = 0;
     if (tid == 0 && (tok < 0 || tok >= (int32_t)V || pos < 0 || pos >= (int32_t)max_ctx)) atomicCAS(status, 0, ERR_OUT_OF_RANGE);
     if (tok < 0 || tok >= (int32_t)V) tok = 0;
     for (uint32_t i = tid; i < half; i += NT) {
@@ -626,8 +628,25 @@ __global__ void __launch_bounds__(256) kl_b_embed_kernel(const int32_t* tokens, 
     b_embed_item<256>(tokens, positions, embed, x, H, V, max_ctx, inv_freq, cs, half, status, blockIdx.x, threadIdx.x);
 }
 
+// The same for a step on a paged cache.  The block of a sequence also looks at the page table: every page up to the one this
+// step writes must be one of the pool, before anything is written.
+__global__ void __launch_bounds__(256) kl_b_embed_paged_kernel(const int32_t* tokens, const int32_t* positions, const __nv_bfloat16* embed,
+                                                               float* x, uint32_t H, uint32_t V, uint32_t max_ctx, const double* inv_freq,
+                                                               float* cs, uint32_t half, int32_t* status, const int32_t* table,
+                                                               int64_t table_stride, uint32_t page, uint32_t n_pages) {
+    griddep_launch();
+    griddep_wait();
+    const uint32_t b = blockIdx.x;
+    const int32_t pos = positions[b];
+    if (pos >= 0 && pos < (int32_t)max_ctx)
+        for (uint32_t i = threadIdx.x; i <= (uint32_t)pos / page; i += 256u)
+            if ((uint32_t)table[(int64_t)b * table_stride + i] >= n_pages) atomicCAS(status, 0, ERR_OUT_OF_RANGE);
+    b_embed_item<256, true>(tokens, positions, embed, x, H, V, max_ctx, inv_freq, cs, half, status, b, threadIdx.x);
+}
+
 struct BAttnView {
     __nv_bfloat16* kv;
+    float* rows;              // paged cache: the step's keys [32][KVD] and values [32][KVD] go here instead of into kv
     const int32_t* positions;
     const float* cs;          // [32][hd / 2][2] (cos, sin) of the step's positions
     BgPartials qkv;           // partial results of the QKV projection
@@ -648,10 +667,11 @@ struct BAttnParams : BAttnView {
 // threads: sums the splits of the QKV projection, rotates a q head (and scales it by log2(e) / sqrt(hd) for the base-2
 // softmax) or a k head at the sequence's position, rounds k and v to bf16 and writes them into row `position` of the
 // sequence's cache slabs.  The attention kernel that follows reads that row from the cache like any other.
-template <int NT>   // threads that share the item
+// PAGED: the rows of k and v are left in fp32 (p.rows) for kl_paged_append.
+template <int NT, bool PAGED = false>   // threads that share the item
 __device__ __forceinline__ void b_rope_item(const BAttnView& p, uint32_t b, uint32_t head, uint32_t tid) {
     const uint32_t hd = p.hd, half = hd >> 1;
-    const int32_t pos = p.positions[b];
+    const int32_t pos = PAGED ? 0 : p.positions[b];
     const float* cs = p.cs + (size_t)b * hd;
     auto val = [&](uint32_t r) {   // row r of [q | k | v]: sum of the partial results, plus the projection's bias if any
         float v[1];
@@ -668,6 +688,15 @@ __device__ __forceinline__ void b_rope_item(const BAttnView& p, uint32_t b, uint
         }
     } else if (head < p.nq + p.nkv) {
         const uint32_t g = head - p.nq;
+        if (PAGED) {
+            float* to = p.rows + (size_t)b * p.KVD + g * hd;
+            for (uint32_t i = tid; i < half; i += NT) {
+                const float a = val(p.QD + g * hd + i), bb = val(p.QD + g * hd + i + half), c = cs[2 * i], sn = cs[2 * i + 1];
+                to[i] = a * c - bb * sn;
+                to[i + half] = bb * c + a * sn;
+            }
+            return;
+        }
         __nv_bfloat16* row = p.kv + ((((size_t)p.layer * 2 + 0) * p.B + b) * p.nkv + g) * slab + (size_t)pos * hd;
         for (uint32_t i = tid; i < half; i += NT) {
             const float a = val(p.QD + g * hd + i), bb = val(p.QD + g * hd + i + half), c = cs[2 * i], sn = cs[2 * i + 1];
@@ -676,6 +705,11 @@ __device__ __forceinline__ void b_rope_item(const BAttnView& p, uint32_t b, uint
         }
     } else {
         const uint32_t g = head - p.nq - p.nkv;
+        if (PAGED) {
+            float* to = p.rows + (size_t)(32 + b) * p.KVD + g * hd;
+            for (uint32_t d = tid; d < hd; d += NT) to[d] = val(p.QD + p.KVD + g * hd + d);
+            return;
+        }
         __nv_bfloat16* row = p.kv + ((((size_t)p.layer * 2 + 1) * p.B + b) * p.nkv + g) * slab + (size_t)pos * hd;
         for (uint32_t d = tid; d < hd; d += NT) row[d] = __float2bfloat16_rn(val(p.QD + p.KVD + g * hd + d));
     }
@@ -686,6 +720,13 @@ __global__ void __launch_bounds__(128) kl_b_rope_kernel(const BAttnParams p) {
     griddep_wait();
     if (*p.status != 0) return;
     b_rope_item<128>(p, blockIdx.x, blockIdx.y, threadIdx.x);
+}
+
+__global__ void __launch_bounds__(128) kl_b_rope_rows_kernel(const BAttnView p) {
+    griddep_launch();
+    griddep_wait();
+    if (*p.status != 0) return;
+    b_rope_item<128, true>(p, blockIdx.x, blockIdx.y, threadIdx.x);
 }
 
 constexpr int BA_WARPS = 11;     // independent warps per CTA; one persistent CTA per SM (the looped kernel's twelfth warp streams weights)

@@ -7,7 +7,7 @@
 #include <atomic>
 #include <utility>
 
-#include "../../include/kl.h"
+#include "kl_paged_internal.h"
 
 using namespace kl;
 
@@ -173,7 +173,58 @@ kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* 
     return v.fp8 ? launch_attn_hd<256, true>(v, a, blocks, stream) : launch_attn_hd<256, false>(v, a, blocks, stream);
 }
 
+// Both ways into the attention kernels.
+kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type, uint32_t out_mode,
+                        int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale_log2, uint32_t window,
+                        const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
+                        int32_t* status_d, void* stream) {
+    if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
+    const AttnSpace sp = attn_space(cache->head_dim);
+    if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
+    const int blocks = attn_blocks();
+    if (blocks <= 0) return KL_ERR_CUDA;
+    uint8_t* ws = (uint8_t*)workspace_d;
+    const PagedView v = view(cache, seqs, status_d);
+    PagedAttn a;
+    a.q = (const uint8_t*)q_d;
+    a.out = (uint8_t*)out_d;
+    a.q_stride = q_row_stride * elem(q_type);
+    a.out_stride = out_row_stride * elem(q_type);
+    a.out_mode = out_mode;
+    a.nq = n_q_heads;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.HT = (a.G + 7) / 8;
+    a.scale_log2 = scale_log2;
+    a.window = window;
+    a.selected = selected_d;
+    a.n_select = n_select;
+    a.lse = lse_d;
+    a.part = (float*)(ws + sp.part);
+    a.part_ml = (float*)(ws + sp.part_ml);
+    a.head = (float*)(ws + sp.head);
+    a.head_ml = (float*)(ws + sp.head_ml);
+    a.meta = (int4*)(ws + sp.meta);
+    const kl_status rc = launch_attn(v, a, blocks, stream);
+    if (rc != KL_OK) return rc;
+    return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
+}
+
 }  // namespace
+
+namespace kl {
+kl_status paged_check(const kl_paged_cache* cache, const kl_paged_seqs* seqs) {
+    const kl_status rc = check_cache(cache, true);
+    return rc != KL_OK ? rc : check_seqs(cache, seqs);
+}
+
+kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const float* q_d, __nv_bfloat16* operand_d,
+                                  uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
+                                  size_t workspace_bytes, int32_t* status_d, void* stream) {
+    const int64_t width = (int64_t)n_q_heads * cache->head_dim;
+    return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, selected_d, n_select, nullptr, workspace_d,
+                         workspace_bytes, status_d, stream);
+}
+}  // namespace kl
 
 extern "C" {
 
@@ -265,35 +316,10 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     if (seqs->n_seqs == 0) return KL_OK;
     if ((rc = check_queries(cache, q_d, q_type, q_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
     if ((rc = check_queries(cache, out_d, q_type, out_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
-    if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu || !(scale < INFINITY)) return KL_ERR_INVALID_ARG;
-    if (!workspace_d || ((uintptr_t)workspace_d & 255u)) return KL_ERR_INVALID_ARG;
-    uint8_t* ws = (uint8_t*)workspace_d;
-    const AttnSpace sp = attn_space(cache->head_dim);
-    if (workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
-    const int blocks = attn_blocks();
-    if (blocks <= 0) return KL_ERR_CUDA;
-    const PagedView v = view(cache, seqs, status_d);
-    PagedAttn a;
-    a.q = (const uint8_t*)q_d;
-    a.out = (uint8_t*)out_d;
-    a.q_stride = q_row_stride * elem(q_type);
-    a.out_stride = out_row_stride * elem(q_type);
-    a.out_mode = q_type == KL_F32 ? PA_F32 : PA_BF16;
-    a.nq = n_q_heads;
-    a.G = n_q_heads / cache->n_kv_heads;
-    a.HT = (a.G + 7) / 8;
-    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
-    a.window = window;
-    a.selected = selected_d;
-    a.n_select = n_select;
-    a.lse = lse_d;
-    a.part = (float*)(ws + sp.part);
-    a.part_ml = (float*)(ws + sp.part_ml);
-    a.head = (float*)(ws + sp.head);
-    a.head_ml = (float*)(ws + sp.head_ml);
-    a.meta = (int4*)(ws + sp.meta);
-    if ((rc = launch_attn(v, a, blocks, stream)) != KL_OK) return rc;
-    return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
+    if (!(scale < INFINITY)) return KL_ERR_INVALID_ARG;
+    const float scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
+    return run_attention(cache, seqs, q_d, out_d, q_type, q_type == KL_F32 ? PA_F32 : PA_BF16, q_row_stride, out_row_stride, n_q_heads, scale_log2,
+                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, stream);
 }
 
 }  // extern "C"

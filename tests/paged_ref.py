@@ -154,3 +154,64 @@ def select_ref(bounds, q, positions, table, page, keep_first, keep_last, n_selec
             keep = sorted(forced + rest[:max(0, n_select - len(forced))])[:n_select]
             out[s, h, :len(keep)] = torch.tensor(keep, dtype=torch.int32)
     return out
+
+
+class PlainDecoder:
+    """The decode step in 64 bits over a cache kept as lists of rows per (layer, sequence): what kl_decode_step_paged
+    computes, written out.  e4m3: rows are stored as the values their codes stand for.  n_select: 0, or pages per kv head."""
+
+    def __init__(self, shape, layers, glob, page, e4m3=False, n_select=0):
+        self.s, self.page, self.e4m3, self.n_select = shape, page, e4m3, n_select
+        self.layers = [{k: v.double() for k, v in l.items()} for l in layers]
+        self.glob = {k: v.double() for k, v in glob.items()}
+
+    def _norm(self, x, gain):
+        return x / torch.sqrt((x * x).mean(-1, keepdim=True) + self.s.rms_eps) * gain
+
+    def _rope(self, x, pos):
+        half = self.s.head_dim // 2
+        f = pos * self.s.rope_theta ** (-2.0 * torch.arange(half, dtype=torch.float64) / self.s.head_dim)
+        a, b = x[..., :half], x[..., half:]
+        return torch.cat([a * f.cos() - b * f.sin(), b * f.cos() + a * f.sin()], -1)
+
+    def held(self, x):
+        """Row(s) [nkv, hd] as the cache stands for them."""
+        if not self.e4m3:
+            return x.float().to(torch.bfloat16).double()
+        out = torch.empty_like(x)
+        for h in range(x.shape[0]):
+            e = row_exponent(float(x[h].abs().max()))
+            out[h] = e4m3_round(x[h] * 2.0 ** -e) * 2.0 ** e
+        return out
+
+    def step(self, cache, token, pos):
+        """One sequence; cache: per layer (k, v) tensors [nkv, rows, hd] of the rows before pos, extended in place.  Returns hidden, logits."""
+        s, G = self.s, self.s.n_q_heads // self.s.n_kv_heads
+        x = self.glob["embed"][token]
+        for l, w in enumerate(self.layers):
+            a = self._norm(x, w["norm1"])
+            q, k, v = w["wq"] @ a, w["wk"] @ a, w["wv"] @ a
+            if "bq" in w:
+                q, k, v = q + w["bq"], k + w["bk"], v + w["bv"]
+            q = self._rope(q.view(s.n_q_heads, s.head_dim), pos)
+            k = self.held(self._rope(k.view(s.n_kv_heads, s.head_dim), pos))
+            v = self.held(v.view(s.n_kv_heads, s.head_dim))
+            kk, vv = (torch.cat([c, r[:, None]], 1) for c, r in zip(cache[l], (k, v)))
+            cache[l] = (kk, vv)
+            o = torch.empty(s.n_q_heads, s.head_dim, dtype=torch.float64)
+            for h in range(s.n_kv_heads):
+                at = torch.arange(pos + 1)
+                pages = pos // self.page + 1
+                if self.n_select and pages > self.n_select:
+                    lo = torch.stack([kk[h, p * self.page:(p + 1) * self.page].amin(0) for p in range(pages)])
+                    hi = torch.stack([kk[h, p * self.page:(p + 1) * self.page].amax(0) for p in range(pages)])
+                    score = torch.stack([torch.maximum(y * lo, y * hi).sum(1) for y in q[h * G:(h + 1) * G]]).amax(0)
+                    rest = sorted(range(1, pages - 1), key=lambda p: (-float(score[p]), p))[:self.n_select - 2]
+                    at = torch.cat([at[p * self.page:(p + 1) * self.page] for p in sorted([0, pages - 1] + rest)])
+                sc = q[h * G:(h + 1) * G] @ kk[h, at].T / math.sqrt(s.head_dim)
+                o[h * G:(h + 1) * G] = torch.softmax(sc, 1) @ vv[h, at]
+            x = x + w["wo"] @ o.flatten()
+            a = self._norm(x, w["norm2"])
+            g = w["wgate"] @ a
+            x = x + w["wdown"] @ (g / (1 + torch.exp(-g)) * (w["wup"] @ a))
+        return x, self.glob["lm_head"] @ self._norm(x, self.glob["norm_f"])
