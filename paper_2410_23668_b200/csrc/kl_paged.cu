@@ -254,10 +254,10 @@ kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
     const PagedView v = view(cache, seqs, status_d);
     const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
-    const uint64_t per_block = (uint64_t)PG_THREADS / (cache->head_dim / (v.fp8 ? 16 : 8)) * PR_UNROLL;   // (row, head, K or V)
-    const uint64_t blocks = ((uint64_t)n_rows * 2 * cache->n_kv_heads + per_block - 1) / per_block;
-    if (blocks > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;
-    const dim3 grid((unsigned)blocks);
+    const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / (v.fp8 ? 16 : 8)), chunks = (n_rows + per - 1) / per;
+    const int sms = attn_blocks();
+    if (sms <= 0) return KL_ERR_CUDA;
+    const dim3 grid(chunks < 5u * (unsigned)sms ? chunks : 5u * (unsigned)sms);   // as many blocks as the SMs hold
     if (v.fp8)
         return row_type == KL_F32 ? launch(kl_paged_read_kernel<float, true>, grid, PG_THREADS, 0, stream, v, r)
                                   : launch(kl_paged_read_kernel<__nv_bfloat16, true>, grid, PG_THREADS, 0, stream, v, r);

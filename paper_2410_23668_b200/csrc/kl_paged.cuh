@@ -163,31 +163,44 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // page number u - base(s) (blocks without a page leave).  hd / 8 lanes share a row, eight columns each; half of the
 // lane groups take keys, the other half values.
 template <class T>
-__global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
+__global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
     extern __shared__ float pg_red[];   // [groups of K rows][2][hd] when the cache has bounds
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
     const uint32_t u = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
     uint32_t s = u, j = 0, r0 = u, r1 = u + 1u;
+    int32_t pos;
     if (rows.row_starts) {
-        // the last s with base(s) <= u; all candidates are loaded at once (a search would be a chain of loads)
-        __shared__ uint32_t found[2];
+        // the last s with base(s) <= u, and its position: all candidates are loaded at once (a search would be a chain of loads)
+        __shared__ uint32_t found[5];
         if (u == 0u && h == 0u) pg_check_starts(c, rows);
-        int below = 0;
-        for (uint32_t t = tid; t < c.n_seqs; t += PG_THREADS) below += pg_row_start(c, rows, t) / c.page + 2u * t <= u;
-        if (tid < 2u) found[tid] = 0u;
+        if (tid == 0u) found[0] = 0u;
         __syncthreads();
-        below = __reduce_add_sync(0xffffffffu, below);
-        if ((tid & 31u) == 0u) atomicAdd(&found[0], (uint32_t)below);
+        uint32_t best = 0, b0 = 0, b1 = 0;
+        int32_t bp = 0;
+        for (uint32_t t = tid; t < c.n_seqs; t += PG_THREADS) {
+            const uint32_t x = pg_row_start(c, rows, t), y = pg_row_start(c, rows, t + 1u);
+            const int32_t p = c.positions[t];
+            if (x / c.page + 2u * t <= u) {
+                best = t + 1u;
+                b0 = x; b1 = y; bp = p;
+            }
+        }
+        const uint32_t wbest = __reduce_max_sync(0xffffffffu, best);
+        if ((tid & 31u) == 0u && wbest) atomicMax(&found[0], wbest);
         __syncthreads();
-        s = found[0] - 1u;   // base(0) = row_starts[0] / page may lie above u: no sequence then
-        if (found[0] == 0u) return;
-        r0 = pg_row_start(c, rows, s);
-        r1 = pg_row_start(c, rows, s + 1u);
+        if (found[0] == 0u) return;   // base(0) = row_starts[0] / page may lie above u
+        if (best == found[0]) {
+            found[1] = b0; found[2] = b1; found[3] = (uint32_t)bp;
+        }
+        __syncthreads();
+        s = found[0] - 1u;
+        r0 = found[1]; r1 = found[2]; pos = (int32_t)found[3];
         j = u - (r0 / c.page + 2u * s);
+    } else {
+        pos = c.positions[s];
     }
-    const int32_t pos = c.positions[s];
     if (pos < 0 || r1 <= r0) return;
     const uint64_t n = r1 - r0, p0 = (uint64_t)pos, p1 = p0 + n;            // positions [p0, p1)
     const uint64_t lp = p0 / c.page + j, a0 = max(p0, lp * c.page), a1 = min(p1, (lp + 1u) * c.page);
@@ -208,6 +221,15 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
     const int64_t src_stride = is_v ? rows.v_stride : rows.k_stride;
     uint8_t* dst = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b;
     uint8_t* exps = c.fp8 ? (is_v ? c.ve : c.ke) + ((int64_t)phys * c.nkv + h) * c.page : nullptr;
+    // the page's bounds so far, requested ahead of the rows: thread t looks after columns t, t + PG_THREADS of [lo | hi]
+    __nv_bfloat16* bounds = c.bounds ? c.bounds + ((int64_t)phys * c.nkv + h) * 2 * hd : nullptr;
+    float old[2] = {INFINITY, INFINITY};
+    if (bounds)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t t = tid + i * PG_THREADS;
+            if (t < 2u * hd) old[i] = off0 == 0u ? (t >= hd ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
+        }
     float lo[8], hi[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -289,15 +311,17 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_append_kernel(const Paged
         }
     }
     __syncthreads();
-    for (uint32_t t = tid; t < 2u * hd; t += PG_THREADS) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t t = tid + i * PG_THREADS;
+        if (t >= 2u * hd) break;
         const bool up = t >= hd;
-        __nv_bfloat16* b = c.bounds + (((int64_t)phys * c.nkv + h) * 2) * hd + t;
-        float x = off0 == 0u ? (up ? -INFINITY : INFINITY) : __bfloat162float(*b);
+        float x = old[i];
         for (uint32_t k = 0; k < groups; ++k) {
             const float y = pg_red[k * 2u * hd + t];
             x = up ? fmaxf(x, y) : fminf(x, y);
         }
-        *b = __float2bfloat16_rn(x);
+        bounds[t] = __float2bfloat16_rn(x);
     }
 }
 
@@ -314,92 +338,103 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
     return lo;
 }
 
-// Read back.  A vector = one row of one head, K or V; hd / E lanes share it (E = 8 columns each, 16 of an e4m3 row: 16 bytes
-// of the cache either way).  A lane works on PR_UNROLL vectors at once: all their page look-ups, then all their rows.
+// Read back.  A block walks over chunks of R rows (as many as make PR_ITEMS 16-byte pieces).  R threads look up where the rows
+// of the next chunk lie -- a chain of dependent loads: sequence, position, page -- while the block copies this chunk's.  hd / E
+// lanes share a (row, head, K or V), E = 8 columns each (16 of an e4m3 row: 16 bytes of the cache either way), PR_UNROLL
+// of them in flight per lane.
 constexpr int PR_UNROLL = 4;
+constexpr uint32_t PR_ITEMS = 4096;
 constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in shared memory
+__host__ __device__ constexpr uint32_t pr_rows(uint32_t nkv, uint32_t lanes) {   // rows of a chunk
+    return 2u * nkv * lanes >= PR_ITEMS ? 1u : PR_ITEMS / (2u * nkv * lanes) < (uint32_t)PG_THREADS ? PR_ITEMS / (2u * nkv * lanes) : (uint32_t)PG_THREADS;
+}
 template <class T, bool FP8>
 __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedView c, const PagedRows rows) {
     constexpr uint32_t E = FP8 ? 16 : 8;
+    __shared__ uint32_t starts_s[PR_STARTS + 1];
+    __shared__ int64_t at_s[2][PG_THREADS], exp_s[2][PG_THREADS];   // offsets of a chunk's rows (head 0), -1: nothing to copy
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint32_t lanes = c.hd / E, groups = PG_THREADS / lanes, grp = threadIdx.x / lanes, col = threadIdx.x % lanes * E;
+    const uint32_t tid = threadIdx.x, lanes = c.hd / E, groups = PG_THREADS / lanes, grp = tid / lanes, col = tid % lanes * E;
+    const uint32_t R = pr_rows(c.nkv, lanes), nvec = R * 2u * c.nkv;
     if (rows.row_starts && blockIdx.x == 0u) pg_check_starts(c, rows);
-    __shared__ uint32_t starts_s[PR_STARTS + 1];
     const bool kept = rows.row_starts && c.n_seqs <= PR_STARTS;
     if (kept) {
-        for (uint32_t s = threadIdx.x; s <= c.n_seqs; s += PG_THREADS) starts_s[s] = pg_row_start(c, rows, s);
+        for (uint32_t s = tid; s <= c.n_seqs; s += PG_THREADS) starts_s[s] = pg_row_start(c, rows, s);
         __syncthreads();
     }
     const uint32_t* starts = kept ? starts_s : nullptr;
-    const uint64_t v0 = (uint64_t)blockIdx.x * groups * PR_UNROLL + grp;
-    uint32_t row[PR_UNROLL], head[PR_UNROLL];   // head: nkv + head for values
-    int64_t src[PR_UNROLL], exp_at[PR_UNROLL];
-    bool live[PR_UNROLL];
-#pragma unroll
-    for (int u = 0; u < PR_UNROLL; ++u) {
-        const uint64_t vec = v0 + (uint64_t)u * groups;
-        const uint64_t r64 = pg_div(vec, 2u * c.nkv);
-        live[u] = r64 < rows.n_rows;
-        row[u] = live[u] ? (uint32_t)r64 : 0u;
-        head[u] = (uint32_t)(vec - r64 * 2u * c.nkv);
-        src[u] = exp_at[u] = 0;
-        if (!live[u]) continue;
-        const uint32_t s = pg_seq_of_row(c, rows, starts, row[u]);
+    auto look_up = [&](uint64_t row0, int64_t& at, int64_t& ex) {   // row row0 + tid
+        at = ex = -1;
+        const uint64_t row64 = row0 + tid;
+        if (tid >= R || row64 >= rows.n_rows) return;
+        const uint32_t row = (uint32_t)row64, s = pg_seq_of_row(c, rows, starts, row);
         const uint32_t r0 = starts ? starts[s] : pg_row_start(c, rows, s), r1 = starts ? starts[s + 1u] : pg_row_start(c, rows, s + 1u);
         const int32_t pos = c.positions[s];
-        live[u] = pos >= 0 && row[u] >= r0 && row[u] < r1;
-        if (!live[u]) continue;
-        const uint64_t at = (uint64_t)pos + (row[u] - r0);
-        const uint64_t lp = pg_div(at, c.page);
+        if (pos < 0 || row < r0 || row >= r1) return;
+        const uint64_t p = (uint64_t)pos + (row - r0), lp = pg_div(p, c.page);
         const int32_t phys = lp < c.table_pages ? pg_physical(c, s, (uint32_t)lp) : -1;
         if (phys < 0) {
             pg_error(c);
-            live[u] = false;
-            continue;
+            return;
         }
-        const uint32_t off = (uint32_t)(at - lp * c.page), h = head[u] >= c.nkv ? head[u] - c.nkv : head[u];
-        src[u] = (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off * c.row_b;
-        exp_at[u] = ((int64_t)phys * c.nkv + h) * c.page + off;
-    }
-    uint4 x[PR_UNROLL];
-    uint32_t e[PR_UNROLL];
+        const uint32_t off = (uint32_t)(p - lp * c.page);
+        at = (int64_t)phys * c.page_b + (int64_t)off * c.row_b;
+        ex = (int64_t)phys * c.nkv * c.page + off;
+    };
+    const uint64_t step = (uint64_t)gridDim.x * R;
+    uint64_t row0 = (uint64_t)blockIdx.x * R;
+    int64_t at, ex;
+    look_up(row0, at, ex);
+    for (int buf = 0; row0 < rows.n_rows; row0 += step, buf ^= 1) {
+        at_s[buf][tid] = at;
+        exp_s[buf][tid] = ex;
+        __syncthreads();   // (the buffer's previous contents were read before the barrier of the round between)
+        look_up(row0 + step, at, ex);
+        for (uint32_t v0 = grp; v0 < nvec; v0 += groups * PR_UNROLL) {
+            uint4 x[PR_UNROLL];
+            uint32_t e[PR_UNROLL];
+            bool live[PR_UNROLL];
 #pragma unroll
-    for (int u = 0; u < PR_UNROLL; ++u)
-        if (live[u]) {
-            const bool is_v = head[u] >= c.nkv;
-            x[u] = *reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + src[u] + col * (FP8 ? 1 : 2));
-            if (FP8) e[u] = (is_v ? c.ve : c.ke)[exp_at[u]];
-        }
+            for (int u = 0; u < PR_UNROLL; ++u) {
+                const uint32_t v = v0 + u * groups, r = v / (2u * c.nkv), i = v - r * 2u * c.nkv, h = i >= c.nkv ? i - c.nkv : i;
+                live[u] = v < nvec && at_s[buf][min(r, R - 1u)] >= 0;
+                if (live[u]) {
+                    x[u] = *reinterpret_cast<const uint4*>((i >= c.nkv ? c.v : c.k) + at_s[buf][r] + (int64_t)h * c.head_b + col * (FP8 ? 1 : 2));
+                    if (FP8) e[u] = (i >= c.nkv ? c.ve : c.ke)[exp_s[buf][r] + (int64_t)h * c.page];
+                }
+            }
 #pragma unroll
-    for (int u = 0; u < PR_UNROLL; ++u)
-        if (live[u]) {
-            const bool is_v = head[u] >= c.nkv;
-            uint8_t* to = is_v ? rows.v + (int64_t)row[u] * rows.v_stride : rows.k + (int64_t)row[u] * rows.k_stride;
-            T* out = reinterpret_cast<T*>(to) + (size_t)(is_v ? head[u] - c.nkv : head[u]) * c.hd + col;
-            const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-            float f[8];
+            for (int u = 0; u < PR_UNROLL; ++u)
+                if (live[u]) {
+                    const uint32_t v = v0 + u * groups, r = v / (2u * c.nkv), i = v - r * 2u * c.nkv, h = i >= c.nkv ? i - c.nkv : i;
+                    const int64_t row = (int64_t)(row0 + r);
+                    T* out = reinterpret_cast<T*>(i >= c.nkv ? rows.v + row * rows.v_stride : rows.k + row * rows.k_stride) + (size_t)h * c.hd + col;
+                    const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                    float f[8];
 #pragma unroll
-            for (int hh = 0; hh < (FP8 ? 2 : 1); ++hh) {
-                if (FP8) {
-                    const float scale = pg_scale(e[u]);
+                    for (int hh = 0; hh < (FP8 ? 2 : 1); ++hh) {
+                        if (FP8) {
+                            const float scale = pg_scale(e[u]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 y = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2((w[2 * hh + i / 2] >> (16 * (i & 1))) & 0xffffu));
-                        f[2 * i] = y.x * scale;
-                        f[2 * i + 1] = y.y * scale;
-                    }
-                } else {
+                            for (int q = 0; q < 4; ++q) {
+                                const float2 y = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2((w[2 * hh + q / 2] >> (16 * (q & 1))) & 0xffffu));
+                                f[2 * q] = y.x * scale;
+                                f[2 * q + 1] = y.y * scale;
+                            }
+                        } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f[2 * i] = bf_lo(w[i]);
-                        f[2 * i + 1] = bf_hi(w[i]);
+                            for (int q = 0; q < 4; ++q) {
+                                f[2 * q] = bf_lo(w[q]);
+                                f[2 * q + 1] = bf_hi(w[q]);
+                            }
+                        }
+                        pg_store8<T>(out + hh * 8, f);
                     }
                 }
-                pg_store8<T>(out + hh * 8, f);
-            }
         }
+    }
 }
 
 // ---- page selection
@@ -410,7 +445,7 @@ struct PagedSelect {
     uint32_t q_f32, nq, G;
     uint32_t keep_first, keep_last, n_select;
     int32_t* selected;
-    float2* scores;        // [n_seqs][nkv][table_pages]: score, largest magnitude among the bounds
+    float2* scores;        // [n_seqs][nkv][table_pages]: score, bound of its error
 };
 __device__ __forceinline__ float pg_q(const uint8_t* row, uint32_t f32, uint32_t i) {
     return f32 ? reinterpret_cast<const float*>(row)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[i]);
@@ -427,15 +462,28 @@ __device__ __forceinline__ uint32_t pg_key(float x) {
 // but for extreme spreads, are their sums), rounded once to 32.
 __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect& a, uint32_t s, uint32_t h, int32_t phys) {
     const uint32_t lane = threadIdx.x & 31u;
-    const __nv_bfloat16* b = c.bounds + ((int64_t)phys * c.nkv + h) * 2 * c.hd;
+    const uint32_t* b = reinterpret_cast<const uint32_t*>(c.bounds + ((int64_t)phys * c.nkv + h) * 2 * c.hd);
     const uint8_t* q = a.q + (int64_t)s * a.q_stride;
+    uint32_t lo[4], hi[4];   // columns 2 lane + 64 i, + 1
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (64u * i < c.hd) {
+            lo[i] = b[lane + 32u * i];
+            hi[i] = b[c.hd / 2u + lane + 32u * i];
+        }
     float best = __int_as_float(0x7fc00000);   // NaN
+#pragma unroll 4
     for (uint32_t g = 0; g < a.G; ++g) {
         double sum = 0.0;
-        for (uint32_t d = lane; d < c.hd; d += 32u) {
-            const float x = pg_q(q, a.q_f32, (h * a.G + g) * c.hd + d);
-            sum += (double)x * (double)__bfloat162float(x >= 0.f ? b[c.hd + d] : b[d]);
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (64u * i < c.hd) {
+                const uint32_t d = (h * a.G + g) * c.hd + 2u * lane + 64u * i;
+                const float x = pg_q(q, a.q_f32, d), y = pg_q(q, a.q_f32, d + 1u);
+                sum += (double)x * (double)bf_lo(x >= 0.f ? hi[i] : lo[i]);
+                sum += (double)y * (double)bf_hi(y >= 0.f ? hi[i] : lo[i]);
+            }
+#pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         best = fmaxf(best, (float)sum);        // fmaxf leaves NaN out
     }
@@ -449,7 +497,11 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 //   [min(q, 0) | max(q, 0)] as columns it is one matrix product, pages x heads.  16 pages are the rows of mma.m16n8k16, up to
 //   eight heads its columns; the rows go from memory straight into the operand's registers (the order of the columns is
 //   free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
-//   all tiles of 16 pages.  Written per page: the score, and the largest magnitude among its bounds, for the error's bound.
+//   all tiles of 16 pages.  Written per page: the score and a bound of its error.
+// Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
+// magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
+// queries also lose 2^-16 of themselves.  Taken: 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest
+// bound; infinite where a score or bound is not finite.
 template <int HD, bool F32>
 constexpr int ps_blocks_per_sm() { return HD == 256 || (HD == 128 && F32) ? 1 : 2; }   // what the registers allow
 template <int HD, bool F32>   // F32: type of the queries
@@ -482,7 +534,9 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
         const uint32_t p = tt * 16u + lane;
         return lane < 16u && p < pages ? pg_physical(c, ss, p) : -1;
     };
+    float q1 = 0.f;   // largest sum |q_d| of the heads seen, infinite where one is NaN
     auto load_queries = [&](uint32_t ht) {
+        float sum = 0.f;
         const uint32_t head = h * a.G + min(ht * 8u + g, a.G - 1u);   // a missing head repeats the last one
         const uint8_t* q = a.q + (int64_t)s * a.q_stride + (size_t)head * HD * (F32 ? 4 : 2);
 #pragma unroll
@@ -499,13 +553,22 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
                     v[0] = bf_lo(f.x); v[1] = bf_hi(f.x); v[2] = bf_lo(f.y); v[3] = bf_hi(f.y);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = i < NC / 2 ? fminf(v[e], 0.f) : fmaxf(v[e], 0.f);
+                for (int e = 0; e < 4; ++e) {
+                    if (i < NC / 2) sum += fabsf(v[e]);
+                    v[e] = i < NC / 2 ? fminf(v[e], 0.f) : fmaxf(v[e], 0.f);
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     qf[i][x][e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                     if (F32) ql[F32 ? i : 0][x][e] = pack_bf16(v[2 * e] - bf_lo(qf[i][x][e]), v[2 * e + 1] - bf_hi(qf[i][x][e]));
                 }
             }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (isnan(sum)) sum = INFINITY;
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum = fmaxf(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+        q1 = ht ? fmaxf(q1, sum) : sum;
     };
     int32_t ids = look_up(s, t, np);
     if (HT == 1u) load_queries(0);
@@ -578,7 +641,9 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
         if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
             const uint32_t p = t * 16u + g + j * 8u, b = j ? big1 : big0;
             const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
-            if (p < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + p] = make_float2(j ? best1 : best0, mag);
+            const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? 0x1p-14f : 0x1p-16f);
+            // (infinite where nothing is known: 0 * infinity, a score that is not finite)
+            if (p < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + p] = make_float2(score, isfinite(score) && err >= 0.f ? err : INFINITY);
         }
         if (left > 1u) {
             const bool other = ns != s || nh != h;
@@ -593,21 +658,22 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
 }
 
 // The choice: one block per (sequence, kv head).
-//   1. T = the need-th largest of the approximate scores, found bit by bit from below the bits all of them share.
-//   2. With E a bound of their errors, pages above T + 2 E are chosen for certain and pages below T - 2 E are not.  What lies
-//      between is chosen too if there is room for all of it; otherwise its exact scores decide (equal ones by page).
+//   1. T = the need-th largest of the approximate scores, found from the top bit on, from below the bits all of them share.
+//   2. With E the largest bound of their errors, pages above T + 2 E are chosen for certain and pages below T - 2 E are not.
+//      What lies between is chosen too if there is room for all of it; otherwise exact scores decide (equal ones by page): for
+//      up to PT_LIST candidates a warp scores one each and they are ranked against one another, for more (many equal
+//      scores, or E infinite) step 1 is repeated on the exact scores.
 //   3. The chosen pages are put in order by a prefix sum.
-// Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
-// magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
-// queries also lose 2^-16 of themselves.  E = 2^-16 (2^-14) times the largest sum |q_d| of a head and the largest bound.
-// A score or bound that is not finite makes every page a candidate.
-// KPT > 0: every thread keeps KPT neighbouring keys in registers; KPT == 0: any number of pages, read again each time.
+// KPT > 0: every thread keeps KPT neighbouring keys in registers, and two bits are found per step; KPT == 0: any number of
+// pages, read again for each step.
 constexpr int PT_THREADS = 512;
+constexpr uint32_t PT_LIST = 128;
 template <int KPT>
 __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
     constexpr int NW = PT_THREADS / 32, NK = KPT ? KPT : 1;
     constexpr uint32_t SURE = 0xffffffffu;   // key of a page that is chosen in any case; 0: of one that is not looked at
-    __shared__ uint32_t red[2][NW][2];
+    __shared__ uint4 red[2][NW];
+    __shared__ uint32_t list_n, list_page[PT_LIST], list_key[PT_LIST];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
@@ -620,19 +686,83 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         return;
     }
     auto forced = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n; };
-    uint32_t need = a.n_select - (a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
+    const uint32_t need = a.n_select - (a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
+    if (tid == 0u) list_n = 0u;
 
-    // keys: of the approximate scores first, then (KPT == 0: kept in the workspace) of what step 2 leaves of them
-    uint32_t key[NK], mx = 0, mn = 0xffffffffu, mag = 0, odd = 0;
-    float q1 = 0.f;
+    int turn = 0;
+    // sums of x, y, or the maxima of x, z and the minimum of y, over the block
+    auto reduce = [&](uint32_t x, uint32_t y, uint32_t z, bool extremes) -> uint4 {
+        x = extremes ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
+        y = extremes ? __reduce_min_sync(0xffffffffu, y) : __reduce_add_sync(0xffffffffu, y);
+        if (extremes) z = __reduce_max_sync(0xffffffffu, z);
+        if (lane == 0u) red[turn][warp] = make_uint4(x, y, z, 0u);
+        __syncthreads();
+        uint4 t = red[turn][0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            const uint4 p = red[turn][w];
+            t.x = extremes ? max(t.x, p.x) : t.x + p.x;
+            t.y = extremes ? min(t.y, p.y) : t.y + p.y;
+            t.z = max(t.z, p.z);
+        }
+        turn ^= 1;   // the next call writes the other half, and nobody is two calls behind
+        return t;
+    };
+    // keys: of the approximate scores, or (from_exact) those that the workspace holds in the place of the error bounds
+    uint32_t key[NK];
+    bool from_exact = false;
+    auto key_at = [&](uint32_t i) { return forced(i) ? SURE : from_exact ? __float_as_uint(sc[i].y) : pg_key(sc[i].x); };
+    auto each = [&](auto&& f) {   // f(key, page) for every page of this thread (and for places behind the last one, with key 0)
+        if (KPT) {
+#pragma unroll
+            for (int r = 0; r < NK; ++r) f(key[r], tid * NK + r);
+        } else {
+            for (uint32_t i = tid; i < n; i += PT_THREADS) f(key_at(i), i);
+        }
+    };
+    // The largest t that at least `want` keys reach -- lo and hi: the smallest and the largest key but SURE and 0 -- or, as
+    // soon as a t is found that exactly `want` keys reach, that one (exact).
+    auto threshold = [&](uint32_t lo, uint32_t hi, uint32_t want, bool& exact) {
+        const uint32_t differ = lo ^ hi;
+        int bit = differ ? 31 - __clz(differ) : -1;
+        uint32_t t = bit >= 0 ? lo & ~((2u << bit) - 1u) : lo;
+        exact = false;
+        auto pick = [&](uint32_t with, uint32_t x) {   // x keys reach t | with
+            if (x < want) return false;
+            t |= with;
+            exact = x == want;
+            return true;
+        };
+        while (bit >= 0 && !exact) {
+            if (KPT && bit > 0) {   // three counts of at most 2^13 in two words
+                const uint32_t t1 = t | 1u << (bit - 1), t2 = t | 2u << (bit - 1), t3 = t | 3u << (bit - 1);
+                uint32_t x = 0, y = 0;
+                each([&](uint32_t k, uint32_t) {
+                    if (k == SURE) return;
+                    x += (k >= t1) + (k >= t2 ? 0x10000u : 0u);
+                    y += k >= t3;
+                });
+                const uint4 r = reduce(x, y, 0u, false);
+                if (!pick(3u << (bit - 1), r.y) && !pick(2u << (bit - 1), r.x >> 16)) pick(1u << (bit - 1), r.x & 0xffffu);
+                bit -= 2;
+            } else {
+                uint32_t x = 0;
+                each([&](uint32_t k, uint32_t) { x += k >= (t | 1u << bit) && k != SURE; });
+                pick(1u << bit, reduce(x, 0u, 0u, false).x);
+                --bit;
+            }
+        }
+        return t;
+    };
+
+    uint32_t mx = 0, mn = 0xffffffffu, mag = 0;
     auto take = [&](uint32_t i) {
         const float2 x = i < n ? sc[i] : make_float2(0.f, 0.f);
         const uint32_t k = i >= n ? 0u : forced(i) ? SURE : pg_key(x.x);
         if (k && k != SURE) {
             mx = max(mx, k);
             mn = min(mn, k);
-            mag = max(mag, __float_as_uint(x.y));   // not negative: ordered like whole numbers, NaN above infinity
-            odd |= !isfinite(x.x);
+            mag = max(mag, __float_as_uint(x.y));   // not negative: ordered like whole numbers
         }
         return k;
     };
@@ -642,116 +772,77 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
     } else {
         for (uint32_t i = tid; i < n; i += PT_THREADS) take(i);
     }
-    for (uint32_t gg = warp; gg < a.G; gg += NW) {   // largest sum |q_d| of a head
-        float x = 0.f;
-        for (uint32_t d = lane; d < c.hd; d += 32u) x += fabsf(pg_q(a.q + (int64_t)s * a.q_stride, a.q_f32, (h * a.G + gg) * c.hd + d));
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        q1 = x <= q1 ? q1 : x;   // keeps NaN
-        if (isnan(x)) odd = 1u;
-    }
-    int turn = 0;
-    auto reduce = [&](uint32_t x, uint32_t y, bool extremes) -> uint2 {   // block sums, or (maximum, minimum)
-        x = extremes ? __reduce_max_sync(0xffffffffu, x) : __reduce_add_sync(0xffffffffu, x);
-        y = extremes ? __reduce_min_sync(0xffffffffu, y) : __reduce_add_sync(0xffffffffu, y);
-        if (lane == 0u) {
-            red[turn][warp][0] = x;
-            red[turn][warp][1] = y;
-        }
-        __syncthreads();
-        uint2 t = make_uint2(red[turn][0][0], red[turn][0][1]);
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            const uint32_t p = red[turn][w][0], q = red[turn][w][1];
-            t.x = extremes ? max(t.x, p) : t.x + p;
-            t.y = extremes ? min(t.y, q) : t.y + q;
-        }
-        turn ^= 1;   // the next call writes the other half, and nobody is two calls behind
-        return t;
-    };
-    // f(key) for every page of this thread
-    auto each = [&](auto&& f) {
-        if (KPT) {
-#pragma unroll
-            for (int r = 0; r < NK; ++r) f(key[r], tid * NK + r);
-        } else {
-            for (uint32_t i = tid; i < n; i += PT_THREADS) {
-                uint32_t k = forced(i) ? SURE : pg_key(sc[i].x);
-                f(k, i);
-            }
-        }
-    };
-    auto count = [&](uint32_t t) {   // pages with t <= key < SURE
-        uint32_t x = 0;
-        each([&](uint32_t k, uint32_t) { x += k >= t && k != SURE; });
-        return reduce(x, 0u, false).x;
-    };
-    // The largest t that at least `want` of the keys between `lo` and `hi` reach, or, as soon as a t is found that exactly
-    // `want` keys reach, that one (exact).
-    auto threshold = [&](uint32_t lo, uint32_t hi, uint32_t want, bool& exact) {
-        const uint32_t differ = lo ^ hi;
-        int bit = differ ? 31 - __clz(differ) : -1;
-        uint32_t t = bit >= 0 ? lo & ~((2u << bit) - 1u) : lo;
-        exact = false;
-        for (; bit >= 0 && !exact; --bit) {
-            const uint32_t x = count(t | 1u << bit);
-            if (x >= want) {
-                t |= 1u << bit;
-                exact = x == want;
-            }
-        }
-        return t;
-    };
     uint32_t t = SURE - 1u, ties = 0;   // chosen: keys above t, and the first `ties` of those equal to it
-    float above = INFINITY, below = -INFINITY;   // approximate scores above `above` are chosen, those below `below` are not
     if (need) {
-        const uint2 mm = reduce(mx, mn, true);
-        const uint2 mq = reduce(mag, 0u, true), oq = reduce(max(odd ? 0x7f800000u : 0u, __float_as_uint(q1) & 0x7fffffffu), 0u, true);
-        const float E = __uint_as_float(oq.x) * 1.001f * __uint_as_float(mq.x) * (a.q_f32 ? 0x1p-14f : 0x1p-16f);
-        uint32_t cand = 0, sure = 0;
+        const uint4 all = reduce(mx, mn, mag, true);
+        const float E = __uint_as_float(all.z);
+        float above = INFINITY, below = -INFINITY;
         if (isfinite(E)) {
             bool exact;
-            const uint32_t t0 = threshold(mm.y, mm.x, need, exact);
-            uint32_t low = 0xffffffffu;   // the smallest key that reaches t0: the need-th largest
-            each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
-            const uint32_t kt = reduce(0u, low, true).y;
-            const float T = __uint_as_float(kt & 0x80000000u ? kt & 0x7fffffffu : ~kt);
+            const uint32_t t0 = threshold(all.y, all.x, need, exact);
+            uint32_t low = t0;
+            if (exact) {   // the smallest key that reaches t0 is the need-th largest
+                low = 0xffffffffu;
+                each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
+                low = reduce(0u, low, 0u, true).y;
+            }
+            const float T = __uint_as_float(low & 0x80000000u ? low & 0x7fffffffu : ~low);
             above = __fadd_ru(T, 2.f * E);
             below = __fadd_rd(T, -2.f * E);
         }
-        each([&](uint32_t k, uint32_t i) {
-            if (!k || k == SURE) return;
-            const float x = __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);   // NaN: neither above nor below
-            const bool up = k != 1u && x > above, down = k != 1u && x < below;
-            sure += up;
-            cand += !up && !down;
-        });
-        const uint2 cs = reduce(cand, sure, false);
-        const uint32_t room = need - cs.y;       // for candidates
-        const bool open = cs.x > room;           // their exact scores decide
-        uint32_t cmx = 0, cmn = 0xffffffffu;
-        auto settle = [&](uint32_t k, bool& is_cand) -> uint32_t {   // SURE or 0 where that is certain
+        auto where = [&](uint32_t k) {   // 0: not looked at, 1: out, 2: candidate, 3: chosen
+            if (!k || k == SURE) return 0;
             const float x = __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-            const bool seen = k && k != SURE, up = seen && k != 1u && x > above, down = seen && k != 1u && x < below;
-            is_cand = seen && !up && !down;
-            return up || (is_cand && !open) ? SURE : down ? 0u : k;
+            return k == 1u ? 2 : x > above ? 3 : x < below ? 1 : 2;   // 1: NaN
         };
-        if (KPT && !open) {
+        uint32_t cand = 0, sure = 0;
+        each([&](uint32_t k, uint32_t) {
+            cand += where(k) == 2;
+            sure += where(k) == 3;
+        });
+        const uint4 cs = reduce(cand, sure, 0u, false);
+        const uint32_t room = need - cs.y;       // for candidates
+        const bool open = cs.x > room, few = cs.x <= PT_LIST;
+        if (KPT && (!open || few)) {
+            const uint32_t slot0 = open && cand ? atomicAdd(&list_n, cand) : 0u;
+            uint32_t slot = slot0;
+            if (open) {
+#pragma unroll
+                for (int r = 0; r < NK; ++r)
+                    if (where(key[r]) == 2) list_page[slot++] = tid * NK + r;
+                __syncthreads();
+                for (uint32_t i = warp; i < cs.x; i += NW) {
+                    const int32_t phys = pg_physical(c, s, list_page[i]);
+                    const uint32_t k = phys >= 0 ? pg_key(ps_exact(c, a, s, h, phys)) : 1u;
+                    if (lane == 0u) list_key[i] = k;
+                }
+                __syncthreads();
+            }
+            slot = slot0;
 #pragma unroll
             for (int r = 0; r < NK; ++r) {
-                bool is_cand;
-                key[r] = settle(key[r], is_cand);
+                const int w = where(key[r]);
+                bool take_it = w == 3 || (w == 2 && !open);
+                if (w == 2 && open) {   // its rank among the candidates
+                    const uint32_t k = list_key[slot++], page = tid * NK + r;
+                    uint32_t rank = 0;
+                    for (uint32_t i = 0; i < cs.x; ++i) rank += list_key[i] > k || (list_key[i] == k && list_page[i] < page);
+                    take_it = rank < room;
+                }
+                if (w) key[r] = take_it ? SURE : 0u;
             }
-        } else {   // through the workspace, where a key takes the place of the magnitude; candidates get that of their exact score
+        } else {   // through the workspace, where a key takes the place of the error bound; candidates get that of their exact score
+            uint32_t cmx = 0, cmn = 0xffffffffu;
 #pragma unroll 1
             for (uint32_t i0 = 0; i0 < n; i0 += PT_THREADS) {
                 const uint32_t i = i0 + tid;
-                bool is_cand;
-                uint32_t k = settle(i >= n ? 0u : forced(i) ? SURE : pg_key(sc[i].x), is_cand);
-                const int32_t phys = open && is_cand ? pg_physical(c, s, i) : -1;
-                uint32_t todo = __ballot_sync(0xffffffffu, open && is_cand);
-                while (todo) {
+                uint32_t k = i >= n ? 0u : forced(i) ? SURE : pg_key(sc[i].x);
+                const int w = where(k);
+                const bool ask = open && w == 2;
+                if (w) k = w == 3 || (w == 2 && !open) ? SURE : 0u;
+                const int32_t phys = ask ? pg_physical(c, s, i) : -1;
+                for (uint32_t todo = __ballot_sync(0xffffffffu, ask); todo; todo &= todo - 1u) {
                     const int src = __ffs(todo) - 1;
-                    todo &= todo - 1u;
                     const int32_t ph = __shfl_sync(0xffffffffu, phys, src);
                     const uint32_t ek = ph >= 0 ? pg_key(ps_exact(c, a, s, h, ph)) : 1u;
                     if ((int)lane == src) {
@@ -763,37 +854,21 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
                 if (i < n) sc[i].y = __uint_as_float(k);
             }
             __syncthreads();
+            from_exact = true;
             if (KPT)
 #pragma unroll
-                for (int r = 0; r < NK; ++r) key[r] = tid * NK + r < n ? __float_as_uint(sc[tid * NK + r].y) : 0u;
-        }
-        if (open) {
-            auto each2 = [&](auto&& f) {
-                if (KPT) {
-#pragma unroll
-                    for (int r = 0; r < NK; ++r) f(key[r]);
-                } else {
-                    for (uint32_t i = tid; i < n; i += PT_THREADS) f(__float_as_uint(sc[i].y));
-                }
-            };
-            auto count2 = [&](uint32_t x) {
-                uint32_t y = 0;
-                each2([&](uint32_t k) { y += k >= x && k != SURE; });
-                return reduce(y, 0u, false).x;
-            };
-            const uint2 ce = reduce(cmx, cmn, true);
-            const uint32_t differ = ce.x ^ ce.y;
-            int bit = differ ? 31 - __clz(differ) : -1;
-            t = bit >= 0 ? ce.y & ~((2u << bit) - 1u) : ce.y;
-            bool exact = false;
-            for (; bit >= 0 && !exact; --bit) {
-                const uint32_t x = count2(t | 1u << bit);
-                if (x >= room) {
-                    t |= 1u << bit;
-                    exact = x == room;
+                for (int r = 0; r < NK; ++r) key[r] = tid * NK + r < n ? key_at(tid * NK + r) : 0u;
+            if (open) {
+                const uint4 ce = reduce(cmx, cmn, 0u, true);
+                bool exact;
+                t = threshold(ce.y, ce.x, room, exact);
+                ties = 0xffffffffu;
+                if (!exact) {
+                    uint32_t x = 0;
+                    each([&](uint32_t k, uint32_t) { x += k > t && k != SURE; });
+                    ties = room - reduce(x, 0u, 0u, false).x;
                 }
             }
-            ties = exact ? 0xffffffffu : room - count2(t + 1u);
         }
     }
     // in order
@@ -805,24 +880,24 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
 #pragma unroll
         for (int r = 0; r < NK; ++r) {
             const uint32_t i = i0 + tid * NK + r;
-            const uint32_t k = i >= n ? 0u : KPT ? key[r] : forced(i) ? SURE : need ? __float_as_uint(sc[i].y) : 0u;
+            const uint32_t k = i >= n ? 0u : KPT ? key[r] : need || forced(i) ? key_at(i) : 0u;
             eq[r] = ties && k == t;
             sure[r] = k > t;
             ns += sure[r];
             ne += eq[r];
         }
-        uint32_t both = ns | ne << 16, incl = both;   // at most STEP <= 2^15 each
+        uint32_t both = ns | ne << 16, incl = both;   // at most STEP <= 2^13 each
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= (uint32_t)o) incl += y;
         }
-        if (lane == 31u) red[turn][warp][0] = incl;
+        if (lane == 31u) red[turn][warp].x = incl;
         __syncthreads();
         uint32_t before = incl - both, all = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const uint32_t y = red[turn][w][0];
+            const uint32_t y = red[turn][w].x;
             if (w < (int)warp) before += y;
             all += y;
         }
