@@ -141,6 +141,23 @@ kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
     return KL_OK;
 }
 
+template <int HD>
+kl_status launch_append(int type, const PagedView& v, const PagedRows& r, dim3 grid, size_t smem, void* stream) {
+    if (v.fp8)
+        return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, true>, grid, PG_THREADS, smem, stream, v, r)
+                              : launch(kl_paged_append_kernel<__nv_bfloat16, HD, true>, grid, PG_THREADS, smem, stream, v, r);
+    return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, false>, grid, PG_THREADS, smem, stream, v, r)
+                          : launch(kl_paged_append_kernel<__nv_bfloat16, HD, false>, grid, PG_THREADS, smem, stream, v, r);
+}
+template <int HD>
+kl_status launch_read(int type, const PagedView& v, const PagedRows& r, dim3 grid, void* stream) {
+    if (v.fp8)
+        return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, true>, grid, PG_THREADS, 0, stream, v, r)
+                              : launch(kl_paged_read_kernel<__nv_bfloat16, HD, true>, grid, PG_THREADS, 0, stream, v, r);
+    return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, false>, grid, PG_THREADS, 0, stream, v, r)
+                          : launch(kl_paged_read_kernel<__nv_bfloat16, HD, false>, grid, PG_THREADS, 0, stream, v, r);
+}
+
 template <int HD, bool F32>
 kl_status launch_score_as(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
     return launch(kl_paged_score_kernel<HD, F32>, dim3((unsigned)(ps_blocks_per_sm<HD, F32>() * sms)), PG_THREADS, 0, stream, v, a);
@@ -241,8 +258,9 @@ kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     const PagedRows r = rows_of(row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride);
     const size_t smem = cache->bounds_d ? (size_t)(PG_THREADS / (cache->head_dim / 8) / 2) * 2 * cache->head_dim * 4 : 0;
     const dim3 grid((unsigned)units, cache->n_kv_heads);
-    return row_type == KL_F32 ? launch(kl_paged_append_kernel<float>, grid, PG_THREADS, smem, stream, v, r)
-                              : launch(kl_paged_append_kernel<__nv_bfloat16>, grid, PG_THREADS, smem, stream, v, r);
+    if (v.hd == 64) return launch_append<64>(row_type, v, r, grid, smem, stream);
+    if (v.hd == 128) return launch_append<128>(row_type, v, r, grid, smem, stream);
+    return launch_append<256>(row_type, v, r, grid, smem, stream);
 }
 
 kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
@@ -257,12 +275,10 @@ kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / (v.fp8 ? 16 : 8)), chunks = (n_rows + per - 1) / per;
     const int sms = attn_blocks();
     if (sms <= 0) return KL_ERR_CUDA;
-    const dim3 grid(chunks < 5u * (unsigned)sms ? chunks : 5u * (unsigned)sms);   // as many blocks as the SMs hold
-    if (v.fp8)
-        return row_type == KL_F32 ? launch(kl_paged_read_kernel<float, true>, grid, PG_THREADS, 0, stream, v, r)
-                                  : launch(kl_paged_read_kernel<__nv_bfloat16, true>, grid, PG_THREADS, 0, stream, v, r);
-    return row_type == KL_F32 ? launch(kl_paged_read_kernel<float, false>, grid, PG_THREADS, 0, stream, v, r)
-                              : launch(kl_paged_read_kernel<__nv_bfloat16, false>, grid, PG_THREADS, 0, stream, v, r);
+    const dim3 grid(chunks < 4u * (unsigned)sms ? chunks : 4u * (unsigned)sms);   // as many blocks as the SMs hold
+    if (v.hd == 64) return launch_read<64>(row_type, v, r, grid, stream);
+    if (v.hd == 128) return launch_read<128>(row_type, v, r, grid, stream);
+    return launch_read<256>(row_type, v, r, grid, stream);
 }
 
 kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes) {

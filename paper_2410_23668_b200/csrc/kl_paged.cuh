@@ -162,7 +162,7 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // the grid belongs to the sequence s with base(s) <= u < base(s + 1), base(s) = row_starts[s] / page + 2 s, and is its
 // page number u - base(s) (blocks without a page leave).  hd / 8 lanes share a row, eight columns each; half of the
 // lane groups take keys, the other half values.
-template <class T>
+template <class T, int HD, bool FP8>
 __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
     extern __shared__ float pg_red[];   // [groups of K rows][2][hd] when the cache has bounds
     griddep_launch();
@@ -212,23 +212,24 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
     const int32_t phys = pg_physical(c, s, (uint32_t)lp);
     if (phys < 0) return;
 
-    const uint32_t hd = c.hd, lanes = hd / 8u, groups = PG_THREADS / lanes / 2u;   // lane groups per side (K, V)
-    const uint32_t grp = tid / lanes, lane = tid % lanes, col = lane * 8u;
-    const bool is_v = grp >= groups;
-    const uint32_t g = is_v ? grp - groups : grp;
+    constexpr uint32_t LANES = HD / 8, GROUPS = PG_THREADS / LANES / 2;   // lanes per row, rows at a time per side (K, V)
+    const uint32_t grp = tid / LANES, lane = tid % LANES, col = lane * 8u;
+    const bool is_v = grp >= GROUPS;   // the same for a whole warp
+    const uint32_t g = is_v ? grp - GROUPS : grp;
     const uint32_t off0 = (uint32_t)(a0 - lp * c.page), cnt = (uint32_t)(a1 - a0), row0 = r0 + (uint32_t)(a0 - p0);
-    const uint8_t* src = is_v ? rows.v : rows.k;
     const int64_t src_stride = is_v ? rows.v_stride : rows.k_stride;
-    uint8_t* dst = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b;
-    uint8_t* exps = c.fp8 ? (is_v ? c.ve : c.ke) + ((int64_t)phys * c.nkv + h) * c.page : nullptr;
+    const uint8_t* src = (is_v ? rows.v : rows.k) + (int64_t)row0 * src_stride + ((size_t)h * HD + col) * sizeof(T);
+    uint8_t* dst = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off0 * c.row_b + col * (FP8 ? 1 : 2);
+    uint8_t* exps = FP8 ? (is_v ? c.ve : c.ke) + ((int64_t)phys * c.nkv + h) * c.page + off0 : nullptr;
     // the page's bounds so far, requested ahead of the rows: thread t looks after columns t, t + PG_THREADS of [lo | hi]
-    __nv_bfloat16* bounds = c.bounds ? c.bounds + ((int64_t)phys * c.nkv + h) * 2 * hd : nullptr;
+    __nv_bfloat16* bounds = c.bounds ? c.bounds + ((int64_t)phys * c.nkv + h) * 2 * HD : nullptr;
+    const bool bounded = bounds && !is_v;
     float old[2] = {INFINITY, INFINITY};
     if (bounds)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t t = tid + i * PG_THREADS;
-            if (t < 2u * hd) old[i] = off0 == 0u ? (t >= hd ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
+            if (t < 2u * HD) old[i] = off0 == 0u ? (t >= (uint32_t)HD ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
         }
     float lo[8], hi[8];
 #pragma unroll
@@ -236,64 +237,76 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
         lo[i] = INFINITY;
         hi[i] = -INFINITY;
     }
-    constexpr int U = 4;   // rows a lane has in flight
-    for (uint32_t i0 = 0; i0 < cnt; i0 += groups * U) {   // every lane of a warp takes part in the shuffles
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;   // rows a lane has in flight
+    for (uint32_t i0 = 0; i0 < cnt; i0 += GROUPS * U) {   // every lane of a warp takes part in the shuffles
         uint4 raw[U][sizeof(T) / 2];
 #pragma unroll
         for (int y = 0; y < U; ++y) {
-            const uint32_t i = i0 + y * groups + g;
+            const uint32_t i = i0 + y * GROUPS + g;
 #pragma unroll
             for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
                 raw[y][q] = make_uint4(0u, 0u, 0u, 0u);
-                if (i < cnt) raw[y][q] = reinterpret_cast<const uint4*>(src + (int64_t)(row0 + i) * src_stride + ((size_t)h * hd + col) * sizeof(T))[q];
+                if (i < cnt) raw[y][q] = reinterpret_cast<const uint4*>(src + (int64_t)i * src_stride)[q];
             }
         }
 #pragma unroll
         for (int y = 0; y < U; ++y) {
-            if (i0 + y * groups >= cnt) break;   // the same for the whole block
-            const uint32_t i = i0 + y * groups + g;
+            if (i0 + y * GROUPS >= cnt) break;   // the same for the whole block
+            const uint32_t i = i0 + y * GROUPS + g;
             const bool live = i < cnt;
+            const uint4 p = raw[y][0], p2 = raw[y][sizeof(T) / 2 - 1];
+            const uint32_t w[8] = {p.x, p.y, p.z, p.w, p2.x, p2.y, p2.z, p2.w};
             float x[8];
-            if (sizeof(T) == 2) {
-                const uint32_t w[4] = {raw[y][0].x, raw[y][0].y, raw[y][0].z, raw[y][0].w};
 #pragma unroll
-                for (int q = 0; q < 8; ++q) x[q] = q & 1 ? bf_hi(w[q / 2]) : bf_lo(w[q / 2]);
-            } else {
-                const uint4 p = raw[y][0], q = raw[y][sizeof(T) / 2 - 1];
-                const uint32_t w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+            for (int q = 0; q < 8; ++q) x[q] = sizeof(T) == 4 ? __uint_as_float(w[q]) : q & 1 ? bf_hi(w[q / 2]) : bf_lo(w[q / 2]);
+            uint8_t* out = dst + (int64_t)i * c.row_b;
+            if (FP8) {
+                uint32_t big = 0u;   // largest magnitude, as its bits (rows that do not exist are zeros)
+                if (sizeof(T) == 4) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k]);
-            }
-            uint8_t* out = dst + (int64_t)(off0 + (live ? i : 0u)) * c.row_b;
-            if (c.fp8) {
-                float big = 0.f;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float a = fabsf(x[q]);
-                    if (live && a < INFINITY) big = fmaxf(big, a);
+                    for (int q = 0; q < 8; ++q) big = max(big, w[q] & 0x7fffffffu);
+                } else {
+                    const uint32_t m = 0x7fff7fffu, v = __vmaxu2(__vmaxu2(w[0] & m, w[1] & m), __vmaxu2(w[2] & m, w[3] & m));
+                    big = max(v & 0xffff0000u, v << 16);
                 }
-                for (uint32_t o = lanes / 2u; o > 0u; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-                const int32_t e = pg_exponent(big);
-                const float inv = pg_inv_scale(e), scale = pg_scale((uint32_t)(e + 127));
+                if (big >= 0x7f800000u) {   // infinities and NaN do not count
+                    big = 0u;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const uint32_t u = __float_as_uint(x[q]) & 0x7fffffffu;
+                        if (u < 0x7f800000u) big = max(big, u);
+                    }
+                }
+#pragma unroll
+                for (uint32_t o = LANES / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                const int32_t e = pg_exponent(__uint_as_float(big));
+                const float inv = pg_inv_scale(e);
                 uint32_t code[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    code[q] = pg_to_e4m3x2(x[2 * q] * inv, x[2 * q + 1] * inv);
-                    const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[q]));
-                    x[2 * q] = f.x * scale;
-                    x[2 * q + 1] = f.y * scale;
-                }
+                for (int q = 0; q < 4; ++q) code[q] = pg_to_e4m3x2(x[2 * q] * inv, x[2 * q + 1] * inv);
                 if (live) {
-                    *reinterpret_cast<uint2*>(out + col) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
-                    if (lane == 0u) exps[off0 + i] = (uint8_t)(e + 127);
+                    *reinterpret_cast<uint2*>(out) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
+                    if (lane == 0u) exps[i] = (uint8_t)(e + 127);
+                }
+                if (bounded) {
+                    const float scale = pg_scale((uint32_t)(e + 127));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[q]));
+                        x[2 * q] = f.x * scale;
+                        x[2 * q + 1] = f.y * scale;
+                    }
                 }
             } else if (live) {
-                const uint4 w = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-                *reinterpret_cast<uint4*>(out + col * 2u) = w;
-                x[0] = bf_lo(w.x); x[1] = bf_hi(w.x); x[2] = bf_lo(w.y); x[3] = bf_hi(w.y);
-                x[4] = bf_lo(w.z); x[5] = bf_hi(w.z); x[6] = bf_lo(w.w); x[7] = bf_hi(w.w);
+                uint4 v = p;
+                if (sizeof(T) == 4) {
+                    v = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+                    x[0] = bf_lo(v.x); x[1] = bf_hi(v.x); x[2] = bf_lo(v.y); x[3] = bf_hi(v.y);
+                    x[4] = bf_lo(v.z); x[5] = bf_hi(v.z); x[6] = bf_lo(v.w); x[7] = bf_hi(v.w);
+                }
+                *reinterpret_cast<uint4*>(out) = v;
             }
-            if (live) {
+            if (live && bounded) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {   // fminf and fmaxf leave NaN out
                     lo[q] = fminf(lo[q], x[q]);
@@ -302,23 +315,24 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
             }
         }
     }
-    if (!c.bounds) return;
+    if (!bounds) return;
     if (!is_v) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            pg_red[(g * 2u) * hd + col + q] = lo[q];
-            pg_red[(g * 2u + 1u) * hd + col + q] = hi[q];
+            pg_red[(g * 2u) * HD + col + q] = lo[q];
+            pg_red[(g * 2u + 1u) * HD + col + q] = hi[q];
         }
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t t = tid + i * PG_THREADS;
-        if (t >= 2u * hd) break;
-        const bool up = t >= hd;
+        if (t >= 2u * HD) break;
+        const bool up = t >= (uint32_t)HD;
         float x = old[i];
-        for (uint32_t k = 0; k < groups; ++k) {
-            const float y = pg_red[k * 2u * hd + t];
+#pragma unroll
+        for (uint32_t k = 0; k < GROUPS; ++k) {
+            const float y = pg_red[k * 2u * HD + t];
             x = up ? fmaxf(x, y) : fminf(x, y);
         }
         bounds[t] = __float2bfloat16_rn(x);
@@ -348,16 +362,16 @@ constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in 
 __host__ __device__ constexpr uint32_t pr_rows(uint32_t nkv, uint32_t lanes) {   // rows of a chunk
     return 2u * nkv * lanes >= PR_ITEMS ? 1u : PR_ITEMS / (2u * nkv * lanes) < (uint32_t)PG_THREADS ? PR_ITEMS / (2u * nkv * lanes) : (uint32_t)PG_THREADS;
 }
-template <class T, bool FP8>
-__global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedView c, const PagedRows rows) {
-    constexpr uint32_t E = FP8 ? 16 : 8;
+template <class T, int HD, bool FP8>
+__global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_read_kernel(const PagedView c, const PagedRows rows) {
+    constexpr uint32_t E = FP8 ? 16 : 8, LANES = HD / E, GROUPS = PG_THREADS / LANES;
     __shared__ uint32_t starts_s[PR_STARTS + 1];
     __shared__ int64_t at_s[2][PG_THREADS], exp_s[2][PG_THREADS];   // offsets of a chunk's rows (head 0), -1: nothing to copy
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint32_t tid = threadIdx.x, lanes = c.hd / E, groups = PG_THREADS / lanes, grp = tid / lanes, col = tid % lanes * E;
-    const uint32_t R = pr_rows(c.nkv, lanes), nvec = R * 2u * c.nkv;
+    const uint32_t tid = threadIdx.x, grp = tid / LANES, col = tid % LANES * E;
+    const uint32_t R = pr_rows(c.nkv, LANES), per_row = 2u * c.nkv, di = GROUPS % per_row, dr = GROUPS / per_row;
     if (rows.row_starts && blockIdx.x == 0u) pg_check_starts(c, rows);
     const bool kept = rows.row_starts && c.n_seqs <= PR_STARTS;
     if (kept) {
@@ -392,26 +406,40 @@ __global__ void __launch_bounds__(PG_THREADS) kl_paged_read_kernel(const PagedVi
         exp_s[buf][tid] = ex;
         __syncthreads();   // (the buffer's previous contents were read before the barrier of the round between)
         look_up(row0 + step, at, ex);
-        for (uint32_t v0 = grp; v0 < nvec; v0 += groups * PR_UNROLL) {
+        uint32_t r = grp / per_row, i = grp - r * per_row;   // row of the chunk, head (values: nkv + head)
+        while (r < R) {
             uint4 x[PR_UNROLL];
-            uint32_t e[PR_UNROLL];
-            bool live[PR_UNROLL];
+            uint32_t e[PR_UNROLL], to_r[PR_UNROLL], to_i[PR_UNROLL];
 #pragma unroll
             for (int u = 0; u < PR_UNROLL; ++u) {
-                const uint32_t v = v0 + u * groups, r = v / (2u * c.nkv), i = v - r * 2u * c.nkv, h = i >= c.nkv ? i - c.nkv : i;
-                live[u] = v < nvec && at_s[buf][min(r, R - 1u)] >= 0;
-                if (live[u]) {
-                    x[u] = *reinterpret_cast<const uint4*>((i >= c.nkv ? c.v : c.k) + at_s[buf][r] + (int64_t)h * c.head_b + col * (FP8 ? 1 : 2));
-                    if (FP8) e[u] = (i >= c.nkv ? c.ve : c.ke)[exp_s[buf][r] + (int64_t)h * c.page];
+                const int64_t from = r < R ? at_s[buf][r] : -1;
+                to_r[u] = from >= 0 ? r : 0xffffffffu;
+                to_i[u] = i;
+                if (from >= 0) {
+                    const bool is_v = i >= c.nkv;
+                    const uint32_t h = is_v ? i - c.nkv : i;
+                    x[u] = *reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + from + (int64_t)h * c.head_b + col * (FP8 ? 1 : 2));
+                    if (FP8) e[u] = (is_v ? c.ve : c.ke)[exp_s[buf][r] + (int64_t)h * c.page];
+                }
+                i += di;
+                r += dr;
+                if (i >= per_row) {
+                    i -= per_row;
+                    ++r;
                 }
             }
 #pragma unroll
             for (int u = 0; u < PR_UNROLL; ++u)
-                if (live[u]) {
-                    const uint32_t v = v0 + u * groups, r = v / (2u * c.nkv), i = v - r * 2u * c.nkv, h = i >= c.nkv ? i - c.nkv : i;
-                    const int64_t row = (int64_t)(row0 + r);
-                    T* out = reinterpret_cast<T*>(i >= c.nkv ? rows.v + row * rows.v_stride : rows.k + row * rows.k_stride) + (size_t)h * c.hd + col;
+                if (to_r[u] != 0xffffffffu) {
+                    const bool is_v = to_i[u] >= c.nkv;
+                    const int64_t row = (int64_t)(row0 + to_r[u]);
+                    T* out = reinterpret_cast<T*>(is_v ? rows.v + row * rows.v_stride : rows.k + row * rows.k_stride) +
+                             (is_v ? to_i[u] - c.nkv : to_i[u]) * HD + col;
                     const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                    if (!FP8 && sizeof(T) == 2) {
+                        *reinterpret_cast<uint4*>(out) = x[u];
+                        continue;
+                    }
                     float f[8];
 #pragma unroll
                     for (int hh = 0; hh < (FP8 ? 2 : 1); ++hh) {
