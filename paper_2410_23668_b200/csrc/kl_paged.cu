@@ -272,7 +272,7 @@ kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
     const PagedView v = view(cache, seqs, status_d);
     const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
-    const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / (v.fp8 ? 16 : 8)), chunks = (n_rows + per - 1) / per;
+    const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / 8), chunks = (n_rows + per - 1) / per;
     const int sms = attn_blocks();
     if (sms <= 0) return KL_ERR_CUDA;
     const dim3 grid(chunks < 4u * (unsigned)sms ? chunks : 4u * (unsigned)sms);   // as many blocks as the SMs hold
