@@ -999,6 +999,9 @@ __device__ __forceinline__ uint32_t pa_rest(float x0, float x1, uint32_t hi) {
 __device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src, bool ok) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void pa_copy4(uint32_t dst, const void* src, bool ok) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
 }
@@ -1209,6 +1212,18 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             if (phys >= 0) lp = logical * c.page + row;
         };
         uint64_t left = hi - lo;   // tiles still to request
+        // Where a row's 16-byte pieces lie in its tile: piece ch of row r at ch ^ fk(r) (K) or ch ^ fv(r) (V), so that the pieces
+        // a warp reads together fall into different banks.  A lane copies piece ch of rows r0, r0 + RPP, ...
+        const uint32_t ch = lane % CPR, r0 = lane / CPR;
+        auto fk_of = [](uint32_t r) { return CPR >= 8 ? ((r & 1u) << 2 | ((r >> 1) & 3u)) : 0u; };
+        auto fv_of = [](uint32_t r) { return CPR < 8 ? ((r >> 1) & 3u) : FP8 ? (r & 7u) : ((r & 1u) << 2 | ((r >> 1) & 3u)); };
+        constexpr int NPAT = RPP >= 8 ? 1 : 8 / RPP;   // the pattern repeats every eight rows
+        uint32_t k_at[NPAT], v_at[NPAT];
+#pragma unroll
+        for (int i = 0; i < NPAT; ++i) {
+            k_at[i] = r0 * ROW + ((ch ^ fk_of(i * RPP + r0)) << 4);
+            v_at[i] = r0 * ROW + ((ch ^ fv_of(i * RPP + r0)) << 4);
+        }
         auto issue = [&](uint32_t st) {
             const uint32_t b = it / TPB, at = it - b * TPB;
             if (b != batch) {   // this batch, unless it has been looked up already, and the next one
@@ -1224,7 +1239,6 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             const uint32_t h = iph / a.HT;
             const uint32_t kd = ring + st * (2 * TILE), vd = kd + TILE;
             const int64_t hoff = (int64_t)h * c.head_b;
-            const uint32_t ch = lane % CPR, r0 = lane / CPR;
             bool full = true;   // every position of the tile counts
 #pragma unroll
             for (uint32_t v = 0; v < UPT; v += UR == 16 ? 1 : UPT) {   // UR == 16: unit after unit; UR == 4: the lanes' units at once
@@ -1233,17 +1247,24 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                     const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, at * UPT + v), row = __shfl_sync(0xffffffffu, b_row, at * UPT + v);
                     const int32_t r_lo = (int32_t)iq.lo - (int32_t)lp, r_hi = (int32_t)iq.len - (int32_t)lp;   // rows of the unit that count
                     full = full && r_lo <= 0 && r_hi >= 16;
-                    int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + r0) * c.row_b + ch * 16u;
-                    const int64_t step = (int64_t)RPP * c.row_b;
+                    const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + r0) * c.row_b + ch * 16u;
+                    const uint8_t *ks = c.k + off, *vs = c.v + off;
+                    if (r_lo <= 0 && r_hi >= 16 && c.row_b == ROW) {   // the usual unit: 16 rows in a row, all of which count
 #pragma unroll
-                    for (int i = 0; i < 16 / RPP; ++i) {
-                        const int32_t r = i * RPP + (int32_t)r0;
-                        const bool ok = r >= r_lo && r < r_hi;
-                        const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
-                        const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
-                        pa_copy16(kd + (v * 16 + r) * ROW + ((ch ^ fk) << 4), c.k + off, ok);
-                        pa_copy16(vd + (v * 16 + r) * ROW + ((ch ^ fv) << 4), c.v + off, ok);
-                        off += step;
+                        for (int i = 0; i < 16 / RPP; ++i) {
+                            pa_copy16(kd + k_at[i % NPAT] + (v * 16 + i * RPP) * ROW, ks + i * RPP * ROW);
+                            pa_copy16(vd + v_at[i % NPAT] + (v * 16 + i * RPP) * ROW, vs + i * RPP * ROW);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < 16 / RPP; ++i) {
+                            const int32_t r = i * RPP + (int32_t)r0;
+                            const bool ok = r >= r_lo && r < r_hi;
+                            pa_copy16(kd + (v * 16 + r) * ROW + ((ch ^ fk_of(r)) << 4), ks, ok);
+                            pa_copy16(vd + (v * 16 + r) * ROW + ((ch ^ fv_of(r)) << 4), vs, ok);
+                            ks += (int64_t)RPP * c.row_b;
+                            vs += (int64_t)RPP * c.row_b;
+                        }
                     }
                     if (FP8 && lane < 2u) {
                         const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
@@ -1260,10 +1281,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         const int32_t p = (int32_t)lp + (r & 3);
                         const bool ok = lp != PA_NONE && p >= (int32_t)iq.lo && p < (int32_t)iq.len;
                         const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + (r & 3)) * c.row_b + ch * 16u;
-                        const uint32_t fk = CPR >= 8 ? ((r & 1) << 2 | ((r >> 1) & 3)) : 0u;
-                        const uint32_t fv = CPR >= 8 ? (FP8 ? (r & 7) : fk) : ((r >> 1) & 3);
-                        pa_copy16(kd + r * ROW + ((ch ^ fk) << 4), c.k + off, ok);
-                        pa_copy16(vd + r * ROW + ((ch ^ fv) << 4), c.v + off, ok);
+                        pa_copy16(kd + r * ROW + ((ch ^ fk_of(r)) << 4), c.k + off, ok);
+                        pa_copy16(vd + r * ROW + ((ch ^ fv_of(r)) << 4), c.v + off, ok);
                     }
                     const uint32_t u = lane % UPT, src = at * UPT + u;
                     const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
