@@ -1069,11 +1069,11 @@ template <int HD, bool FP8, bool EX>
 struct PaCfg {
     static constexpr int ROW = FP8 ? HD : 2 * HD;            // bytes of a cached row
     static constexpr int NW = HD == 256 ? (FP8 ? 8 : 6) : EX && HD == 128 ? 8 : HD == 64 ? 12 : FP8 ? KL_PA_F8_NW : KL_PA_BF_NW;     // warps
-    static constexpr int TP = HD == 64 ? 32 : HD == 128 && FP8 ? KL_PA_F8_TP : 16;     // positions per tile
+    static constexpr int TP = HD == 64 ? 32 : HD == 128 && FP8 ? (EX ? 32 : KL_PA_F8_TP) : 16;     // positions per tile
     static constexpr int TILE = TP * ROW;                    // bytes of a K (or V) tile
     static constexpr int RING = 204800 / (NW * 2 * TILE);
     static constexpr int ST = RING > 8 ? 8 : RING;           // tiles of a warp's ring
-    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 64 + 48) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256;
+    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 2 * TP + TP) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256;
     static_assert(ST >= 2 && SMEM <= 232448, "ring");
 };
 
@@ -1124,6 +1124,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     using Cfg = PaCfg<HD, FP8, EX>;
     constexpr int NW = Cfg::NW, ST = Cfg::ST, ROW = Cfg::ROW, TILE = Cfg::TILE, NT = NW * 32;
     constexpr uint32_t TP = Cfg::TP, UPT = TP / UR;              // positions and page look-ups per tile
+    constexpr int EXB = 2 * TP, LPN = TP / 4;                    // scale bytes (K, V) and unit positions per tile
     constexpr int NS = TP / 16;                                  // MMA steps of 16 positions per tile
     constexpr uint32_t TPB = 32 / UPT;                           // tiles per batch of look-ups
     constexpr int CPR = ROW / 16, RPP = 32 / CPR;                // 16-byte pieces per row, rows per pass of a warp
@@ -1131,8 +1132,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     extern __shared__ __align__(128) uint8_t pa_smem[];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, j = lane & 3u;
     uint8_t* exps_all = pa_smem + (size_t)NW * ST * 2 * TILE;
-    uint32_t* lps_all = reinterpret_cast<uint32_t*>(exps_all + (size_t)NW * ST * 64);
-    float2* ml_all = reinterpret_cast<float2*>(lps_all + NW * ST * 12);          // [NW][8]
+    uint32_t* lps_all = reinterpret_cast<uint32_t*>(exps_all + (size_t)NW * ST * EXB);
+    float2* ml_all = reinterpret_cast<float2*>(lps_all + NW * ST * LPN);          // [NW][8]
     uint64_t* pre = reinterpret_cast<uint64_t*>(ml_all + NW * 8);               // [NT]
     uint32_t* lens = reinterpret_cast<uint32_t*>(pre + 512);                    // [PA_LENS]
     uint32_t* misc = lens + PA_LENS;
@@ -1171,8 +1172,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     struct Entry { uint32_t valid, s, ph, begins, ends; } first = {0, 0, 0, 0, 0}, last = {0, 0, 0, 0, 0};
     uint32_t last_tiles = 0;
     const uint32_t ring = smem_u32(pa_smem) + warp * (ST * 2 * TILE);
-    const uint32_t exps = smem_u32(exps_all) + warp * (ST * 64);
-    volatile uint32_t* lps = lps_all + warp * (ST * 12);
+    const uint32_t exps = smem_u32(exps_all) + warp * (ST * EXB);
+    volatile uint32_t* lps = lps_all + warp * (ST * LPN);
     if (lo < hi) {
         const uint32_t i0 = pg_find<NW>(pre, lo);
         uint64_t rem = lo - pre[i0];
@@ -1188,6 +1189,15 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
         uint32_t is = cs, iph = cph, it = ct;
         PaSeq iq = cq;
         uint32_t batch = 0xffffffffu;
+        const uint8_t *ik, *iv;   // the pair's head in page 0, this lane's piece of a row; and its scales
+        int64_t ie;
+        auto aim = [&]() {
+            const uint32_t h = iph / a.HT;
+            ik = c.k + (int64_t)h * c.head_b + lane % CPR * 16u;
+            iv = c.v + (int64_t)h * c.head_b + lane % CPR * 16u;
+            ie = (int64_t)h * c.page;
+        };
+        aim();
         int32_t b_phys = -1, n_phys = -1;
         uint32_t b_lp = PA_NONE, n_lp = PA_NONE, b_row = 0, n_row = 0;
         auto look_up = [&](uint32_t b, int32_t& phys, uint32_t& lp, uint32_t& row) {   // unit `lane` of batch b
@@ -1212,9 +1222,11 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             if (phys >= 0) lp = logical * c.page + row;
         };
         uint64_t left = hi - lo;   // tiles still to request
+        uint32_t whole = 0;        // ring slots whose tile has no position that does not count
         // Where a row's 16-byte pieces lie in its tile: piece ch of row r at ch ^ fk(r) (K) or ch ^ fv(r) (V), so that the pieces
         // a warp reads together fall into different banks.  A lane copies piece ch of rows r0, r0 + RPP, ...
         const uint32_t ch = lane % CPR, r0 = lane / CPR;
+        const int64_t e_page = (int64_t)c.nkv * c.page;   // scales of a page
         auto fk_of = [](uint32_t r) { return CPR >= 8 ? ((r & 1u) << 2 | ((r >> 1) & 3u)) : 0u; };
         auto fv_of = [](uint32_t r) { return CPR < 8 ? ((r >> 1) & 3u) : FP8 ? (r & 7u) : ((r & 1u) << 2 | ((r >> 1) & 3u)); };
         constexpr int NPAT = RPP >= 8 ? 1 : 8 / RPP;   // the pattern repeats every eight rows
@@ -1236,9 +1248,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 }
                 batch = b;
             }
-            const uint32_t h = iph / a.HT;
             const uint32_t kd = ring + st * (2 * TILE), vd = kd + TILE;
-            const int64_t hoff = (int64_t)h * c.head_b;
             bool full = true;   // every position of the tile counts
 #pragma unroll
             for (uint32_t v = 0; v < UPT; v += UR == 16 ? 1 : UPT) {   // UR == 16: unit after unit; UR == 4: the lanes' units at once
@@ -1247,8 +1257,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                     const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, at * UPT + v), row = __shfl_sync(0xffffffffu, b_row, at * UPT + v);
                     const int32_t r_lo = (int32_t)iq.lo - (int32_t)lp, r_hi = (int32_t)iq.len - (int32_t)lp;   // rows of the unit that count
                     full = full && r_lo <= 0 && r_hi >= 16;
-                    const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + r0) * c.row_b + ch * 16u;
-                    const uint8_t *ks = c.k + off, *vs = c.v + off;
+                    const int64_t off = (int64_t)max(phys, 0) * c.page_b + (int64_t)(row + r0) * c.row_b;
+                    const uint8_t *ks = ik + off, *vs = iv + off;
                     if (r_lo <= 0 && r_hi >= 16 && c.row_b == ROW) {   // the usual unit: 16 rows in a row, all of which count
 #pragma unroll
                         for (int i = 0; i < 16 / RPP; ++i) {
@@ -1267,10 +1277,10 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         }
                     }
                     if (FP8 && lane < 2u) {
-                        const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
-                        pa_copy16(exps + st * 64 + lane * 32 + v * 16, (lane ? c.ve : c.ke) + eoff, phys >= 0);
+                        const int64_t eoff = (int64_t)max(phys, 0) * e_page + ie + row;
+                        pa_copy16(exps + st * EXB + lane * TP + v * 16, (lane ? c.ve : c.ke) + eoff, phys >= 0);
                     }
-                    if (lane == 0u) lps[st * 12 + v] = lp;
+                    if (lane == 0u) lps[st * LPN + v] = lp;
                 } else {
 #pragma unroll
                     for (int i = 0; i < (int)TP / RPP; ++i) {
@@ -1280,22 +1290,22 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
                         const int32_t p = (int32_t)lp + (r & 3);
                         const bool ok = lp != PA_NONE && p >= (int32_t)iq.lo && p < (int32_t)iq.len;
-                        const int64_t off = (int64_t)max(phys, 0) * c.page_b + hoff + (int64_t)(row + (r & 3)) * c.row_b + ch * 16u;
-                        pa_copy16(kd + r * ROW + ((ch ^ fk_of(r)) << 4), c.k + off, ok);
-                        pa_copy16(vd + r * ROW + ((ch ^ fv_of(r)) << 4), c.v + off, ok);
+                        const int64_t off = (int64_t)max(phys, 0) * c.page_b + (int64_t)(row + (r & 3)) * c.row_b;
+                        pa_copy16(kd + r * ROW + ((ch ^ fk_of(r)) << 4), ik + off, ok);
+                        pa_copy16(vd + r * ROW + ((ch ^ fv_of(r)) << 4), iv + off, ok);
                     }
                     const uint32_t u = lane % UPT, src = at * UPT + u;
                     const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
                     const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
                     if (FP8 && lane < 2u * UPT) {
-                        const int64_t eoff = ((int64_t)max(phys, 0) * c.nkv + h) * c.page + row;
-                        pa_copy4(exps + st * 64 + lane / UPT * 32 + u * 4, (lane < UPT ? c.ke : c.ve) + eoff, phys >= 0);
+                        const int64_t eoff = (int64_t)max(phys, 0) * e_page + ie + row;
+                        pa_copy4(exps + st * EXB + lane / UPT * TP + u * 4, (lane < UPT ? c.ke : c.ve) + eoff, phys >= 0);
                     }
-                    if (lane < UPT) lps[st * 12 + lane] = lp;
+                    if (lane < UPT) lps[st * LPN + lane] = lp;
                     full = __all_sync(0xffffffffu, lp != PA_NONE && lp >= iq.lo && lp + UR <= iq.len);
                 }
             }
-            if (lane == 0u) lps[st * 12 + 8] = full;
+            whole = full ? whole | 1u << st : whole & ~(1u << st);
             --left;
             if (++it == iq.nt && left) {   // on to the next pair, perhaps of the next sequence that has any
                 it = 0;
@@ -1305,6 +1315,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                     do iq = pa_seq<TP>(c, a, length(++is));
                     while (iq.nt == 0u);
                 }
+                aim();
             }
         };
         // ---- state of the pair under way.  Queries: head g; scores and results: heads 2j and 2j + 1
@@ -1440,8 +1451,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 float f0 = qs[0], f1 = qs[1], ev = 0.f;
                 if (FP8) {
                     uint32_t ke, ve;
-                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ke) : "r"(exps + st * 64 + x * 8 + g));
-                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ve) : "r"(exps + st * 64 + 32 + x * 8 + g));
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ke) : "r"(exps + st * EXB + x * 8 + g));
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ve) : "r"(exps + st * EXB + TP + x * 8 + g));
                     f0 *= pg_scale(ke);
                     f1 *= pg_scale(ke);
                     ev = (float)(int)ve - 127.f;
@@ -1450,10 +1461,10 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 s[2 * x + 1] = sc[x / 2][x % 2 * 2 + 1] * f1;
                 if (FP8) sv[2 * x] = sv[2 * x + 1] = ev;
             }
-            if (!lps[st * 12 + 8]) {   // positions that do not count
+            if (!(whole >> st & 1u)) {   // positions that do not count
 #pragma unroll
                 for (int x = 0; x < 2 * NS; ++x) {
-                    const uint32_t r = x * 8 + g, lp = lps[st * 12 + r / UR], p = lp + r % UR;
+                    const uint32_t r = x * 8 + g, lp = lps[st * LPN + r / UR], p = lp + r % UR;
                     if (lp == PA_NONE || p < cq.lo || p >= cq.len) s[2 * x] = s[2 * x + 1] = -INFINITY;
                 }
             }
