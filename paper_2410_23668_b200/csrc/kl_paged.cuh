@@ -529,12 +529,24 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 // magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
 // queries also lose 2^-16 of themselves.  Taken: 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest
 // bound; infinite where a score or bound is not finite.
+#ifndef KL_PS_BATCH
+#define KL_PS_BATCH 8
+#endif
+#ifndef KL_PS_BPS
+#define KL_PS_BPS 2
+#endif
+// The number of the larger magnitude, bf16 by bf16 (NaN is left out: it makes the score NaN).
+__device__ __forceinline__ uint32_t ps_larger(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 template <int HD, bool F32>
-constexpr int ps_blocks_per_sm() { return HD == 256 || (HD == 128 && F32) ? 1 : 2; }   // what the registers allow
+constexpr int ps_blocks_per_sm() { return HD == 256 || (HD == 128 && F32) ? 1 : KL_PS_BPS; }   // what the registers allow
 template <int HD, bool F32>   // F32: type of the queries
 __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
     constexpr int NW = PG_THREADS / 32, NC = HD / 16;   // 16-byte pieces of a row's 4 hd bytes per lane
-    constexpr int BATCH = NC > 8 ? 8 : NC;              // of them in flight at once
+    constexpr int BATCH = NC > KL_PS_BATCH ? KL_PS_BATCH : NC;              // of them in flight at once
     __shared__ uint64_t pre[PG_THREADS], wsum[NW];
     griddep_launch();
     griddep_wait();
@@ -615,7 +627,7 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
         }
         if (left > 1u) ids = look_up(ns, ntile, npages);
         float best0 = -INFINITY, best1 = -INFINITY;
-        uint32_t big0 = 0, big1 = 0;   // largest magnitudes, as bf16 bit patterns (two columns of them)
+        uint32_t big0 = 0, big1 = 0;   // largest magnitudes, two columns of bf16 (their signs mean nothing)
         for (uint32_t ht = 0; ht < HT; ++ht) {
             if (HT > 1u) load_queries(ht);
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -646,9 +658,8 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
                             : "r"(x[i].z), "r"(y[i].z), "r"(x[i].w), "r"(y[i].w), "r"(ql[F32 ? k : 0][1][0]), "r"(ql[F32 ? k : 0][1][1]));
                     }
                     if (ht == 0u) {
-                        const uint32_t m = 0x7fff7fffu;
-                        big0 = __vmaxu2(__vmaxu2(big0, __vmaxu2(x[i].x & m, x[i].y & m)), __vmaxu2(x[i].z & m, x[i].w & m));
-                        big1 = __vmaxu2(__vmaxu2(big1, __vmaxu2(y[i].x & m, y[i].y & m)), __vmaxu2(y[i].z & m, y[i].w & m));
+                        big0 = ps_larger(ps_larger(big0, ps_larger(x[i].x, x[i].y)), ps_larger(x[i].z, x[i].w));
+                        big1 = ps_larger(ps_larger(big1, ps_larger(y[i].x, y[i].y)), ps_larger(y[i].z, y[i].w));
                     }
                 }
             }
@@ -662,11 +673,11 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
             const float u = __shfl_xor_sync(0xffffffffu, best0, o), v = __shfl_xor_sync(0xffffffffu, best1, o);
             best0 = isnan(u) || isnan(best0) ? __int_as_float(0x7fc00000) : fmaxf(best0, u);
             best1 = isnan(v) || isnan(best1) ? __int_as_float(0x7fc00000) : fmaxf(best1, v);
-            big0 = __vmaxu2(big0, __shfl_xor_sync(0xffffffffu, big0, o));
-            big1 = __vmaxu2(big1, __shfl_xor_sync(0xffffffffu, big1, o));
+            big0 = ps_larger(big0, __shfl_xor_sync(0xffffffffu, big0, o));
+            big1 = ps_larger(big1, __shfl_xor_sync(0xffffffffu, big1, o));
         }
         if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
-            const uint32_t p = t * 16u + g + j * 8u, b = j ? big1 : big0;
+            const uint32_t p = t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
             const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
             const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? 0x1p-14f : 0x1p-16f);
             // (infinite where nothing is known: 0 * infinity, a score that is not finite)
@@ -685,7 +696,8 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
 }
 
 // The choice: one block per (sequence, kv head).
-//   1. T = the need-th largest of the approximate scores, found from the top bit on, from below the bits all of them share.
+//   1. T = the need-th largest of the approximate scores: by a histogram and the ranks within one bin, or, where too many
+//      keys share the bin, from the top bit on (from below the bits all of them share).
 //   2. With E the largest bound of their errors, pages above T + 2 E are chosen for certain and pages below T - 2 E are not.
 //      What lies between is chosen too if there is room for all of it; otherwise exact scores decide (equal ones by page): for
 //      up to PT_LIST candidates a warp scores one each and they are ranked against one another, for more (many equal
@@ -700,7 +712,7 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
     constexpr int NW = PT_THREADS / 32, NK = KPT ? KPT : 1;
     constexpr uint32_t SURE = 0xffffffffu;   // key of a page that is chosen in any case; 0: of one that is not looked at
     __shared__ uint4 red[2][NW];
-    __shared__ uint32_t list_n, list_page[PT_LIST], list_key[PT_LIST];
+    __shared__ uint32_t list_n, list_page[PT_LIST], list_key[PT_LIST], found[4], hist[KPT ? PT_THREADS : 1];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
@@ -712,6 +724,7 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         for (uint32_t i = tid; i < a.n_select; i += PT_THREADS) out[i] = i < n ? (int32_t)i : -1;
         return;
     }
+    auto number = [](uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); };   // the score behind a key
     auto forced = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n; };
     const uint32_t need = a.n_select - (a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
     if (tid == 0u) list_n = 0u;
@@ -805,21 +818,71 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         const float E = __uint_as_float(all.z);
         float above = INFINITY, below = -INFINITY;
         if (isfinite(E)) {
-            bool exact;
-            const uint32_t t0 = threshold(all.y, all.x, need, exact);
-            uint32_t low = t0;
-            if (exact) {   // the smallest key that reaches t0 is the need-th largest
-                low = 0xffffffffu;
-                each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
-                low = reduce(0u, low, 0u, true).y;
+            // the need-th largest key: a histogram over bins of equal width finds its bin, the few keys of that bin are ranked
+            uint32_t low = 0u;
+            if (KPT) {
+                const float x0 = number(all.y), width = (PT_THREADS - 1) / (number(all.x) - x0);
+                auto bin_of = [&](uint32_t k) { return (uint32_t)min(PT_THREADS - 1, max(0, (int)((number(k) - x0) * width))); };
+                hist[tid] = 0u;
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < NK; ++r)
+                    if (key[r] && key[r] != SURE) atomicAdd(&hist[bin_of(key[r])], 1u);
+                __syncthreads();
+                // keys in this thread's bin and above: a sum from the last bin down
+                const uint32_t mine = hist[PT_THREADS - 1 - tid];
+                uint32_t sum = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= (uint32_t)o) sum += y;
+                }
+                if (lane == 31u) red[turn][warp].x = sum;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+                    if (w < (int)warp) sum += red[turn][w].x;
+                turn ^= 1;
+                if (sum >= need && sum - mine < need) {   // one thread
+                    found[0] = PT_THREADS - 1 - tid;
+                    found[1] = need - (sum - mine);       // rank within the bin, from 1
+                    found[2] = mine;
+                }
+                __syncthreads();
+                const uint32_t bin = found[0], rank = found[1], cnt = found[2];
+                if (cnt <= PT_LIST) {
+#pragma unroll
+                    for (int r = 0; r < NK; ++r)
+                        if (key[r] && key[r] != SURE && bin_of(key[r]) == bin) list_key[atomicAdd(&list_n, 1u)] = key[r];
+                    __syncthreads();
+                    if (tid < cnt) {
+                        const uint32_t k = list_key[tid];
+                        uint32_t before = 0;
+                        for (uint32_t i = 0; i < cnt; ++i) before += list_key[i] > k || (list_key[i] == k && i < tid);
+                        if (before + 1u == rank) found[3] = k;
+                    }
+                    __syncthreads();
+                    low = found[3];
+                    if (tid == 0u) list_n = 0u;   // (the next barrier comes before its next use)
+                }
             }
-            const float T = __uint_as_float(low & 0x80000000u ? low & 0x7fffffffu : ~low);
+            if (!low) {
+                bool exact;
+                const uint32_t t0 = threshold(all.y, all.x, need, exact);
+                low = t0;
+                if (exact) {   // the smallest key that reaches t0 is the need-th largest
+                    low = 0xffffffffu;
+                    each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
+                    low = reduce(0u, low, 0u, true).y;
+                }
+            }
+            const float T = number(low);
             above = __fadd_ru(T, 2.f * E);
             below = __fadd_rd(T, -2.f * E);
         }
         auto where = [&](uint32_t k) {   // 0: not looked at, 1: out, 2: candidate, 3: chosen
             if (!k || k == SURE) return 0;
-            const float x = __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+            const float x = number(k);
             return k == 1u ? 2 : x > above ? 3 : x < below ? 1 : 2;   // 1: NaN
         };
         uint32_t cand = 0, sure = 0;
