@@ -108,6 +108,18 @@ kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_
     return KL_OK;
 }
 
+// Function attributes hold per device: set them on a kernel's first launch there (`done`: one bit per device; devices
+// beyond 63 set them every time).
+kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KL_ERR_CUDA;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return KL_OK;
+    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return KL_ERR_CUDA;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return KL_OK;
+}
+
 // Workspace of kl_paged_attention (byte offsets): room for PA_MAX_BLOCKS blocks of PA_MAX_WARPS warps.
 struct AttnSpace { size_t part, part_ml, head, head_ml, meta, bytes; };
 AttnSpace attn_space(uint32_t head_dim) {
@@ -129,18 +141,6 @@ int attn_blocks() {
     return sms < PA_MAX_BLOCKS ? sms : PA_MAX_BLOCKS;
 }
 
-// Function attributes hold per device: set them on a kernel's first launch there (`done`: one bit per device; devices
-// beyond 63 set them every time).
-kl_status prepare(const void* f, int smem, std::atomic<uint64_t>& done) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return KL_ERR_CUDA;
-    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-    if (bit && (done.load(std::memory_order_relaxed) & bit)) return KL_OK;
-    if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return KL_ERR_CUDA;
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return KL_OK;
-}
-
 template <int HD>
 kl_status launch_append(int type, const PagedView& v, const PagedRows& r, dim3 grid, size_t smem, void* stream) {
     if (v.fp8)
@@ -160,7 +160,11 @@ kl_status launch_read(int type, const PagedView& v, const PagedRows& r, dim3 gri
 
 template <int HD, bool F32>
 kl_status launch_score_as(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
-    return launch(kl_paged_score_kernel<HD, F32>, dim3((unsigned)(ps_blocks_per_sm<HD, F32>() * sms)), PG_THREADS, 0, stream, v, a);
+    using Cfg = PsCfg<HD>;
+    auto* f = kl_paged_score_kernel<HD, F32>;
+    static std::atomic<uint64_t> done{0};
+    const kl_status rc = prepare((const void*)f, (int)Cfg::SMEM, done);
+    return rc != KL_OK ? rc : launch(f, dim3((unsigned)sms), Cfg::NW * 32, Cfg::SMEM, stream, v, a);
 }
 kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
     if (v.hd == 64) return a.q_f32 ? launch_score_as<64, true>(v, a, sms, stream) : launch_score_as<64, false>(v, a, sms, stream);
@@ -315,12 +319,12 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     const int sms = attn_blocks();
     if (sms <= 0) return KL_ERR_CUDA;
     if ((rc = launch_score(v, a, sms, stream)) != KL_OK) return rc;
-    // keys in registers where a block's threads can hold them, else read again for every step of the search
+    // keys in shared memory up to PT_KEYS pages, else in the workspace
     const dim3 grid(cache->n_kv_heads, seqs->n_seqs);
-    if (seqs->table_pages <= 2 * PT_THREADS) return launch(kl_paged_topk_kernel<2>, grid, PT_THREADS, 0, stream, v, a);
-    if (seqs->table_pages <= 8 * PT_THREADS) return launch(kl_paged_topk_kernel<8>, grid, PT_THREADS, 0, stream, v, a);
-    if (seqs->table_pages <= 16 * PT_THREADS) return launch(kl_paged_topk_kernel<16>, grid, PT_THREADS, 0, stream, v, a);
-    return launch(kl_paged_topk_kernel<0>, grid, PT_THREADS, 0, stream, v, a);
+    if (seqs->table_pages > PT_KEYS) return launch(kl_paged_topk_kernel<false>, grid, PT_THREADS, 0, stream, v, a);
+    static std::atomic<uint64_t> done{0};
+    if ((rc = prepare((const void*)kl_paged_topk_kernel<true>, (int)PT_KEYS * 4, done)) != KL_OK) return rc;
+    return launch(kl_paged_topk_kernel<true>, grid, PT_THREADS, (size_t)seqs->table_pages * 4, stream, v, a);
 }
 
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,

@@ -464,6 +464,39 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_read_kernel(const Page
     }
 }
 
+// 16 (or 4) bytes to shared memory, asynchronously; nothing is read and zeros are written when `ok` is false.
+__device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void pa_copy4(uint32_t dst, const void* src, bool ok) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 pa_lds16(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint2 pa_lds8(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    return v;
+}
+
+// D += A * B, one m16n8k16 tile of f16 (e4m3 caches) or bf16 operands.  Not volatile: the compiler may interleave chains.
+template <bool FP8>
+__device__ __forceinline__ void pa_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (FP8)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // ---- page selection
 
 struct PagedSelect {
@@ -486,8 +519,8 @@ __device__ __forceinline__ uint32_t pg_key(float x) {
 }
 
 // The exact score of a page, by one warp: sums in 64 bits (the products of a bf16 bound and a query are exact there, and so,
-// but for extreme spreads, are their sums), rounded once to 32.
-__device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect& a, uint32_t s, uint32_t h, int32_t phys) {
+// but for extreme spreads, are their sums), rounded once to 32; the largest over query heads [g0, g1) of kv head h.
+__device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect& a, uint32_t s, uint32_t h, int32_t phys, uint32_t g0, uint32_t g1) {
     const uint32_t lane = threadIdx.x & 31u;
     const uint32_t* b = reinterpret_cast<const uint32_t*>(c.bounds + ((int64_t)phys * c.nkv + h) * 2 * c.hd);
     const uint8_t* q = a.q + (int64_t)s * a.q_stride;
@@ -499,8 +532,8 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
             hi[i] = b[c.hd / 2u + lane + 32u * i];
         }
     float best = __int_as_float(0x7fc00000);   // NaN
-#pragma unroll 4
-    for (uint32_t g = 0; g < a.G; ++g) {
+#pragma unroll 1
+    for (uint32_t g = g0; g < g1; ++g) {
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -524,60 +557,101 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 //   [min(q, 0) | max(q, 0)] as columns it is one matrix product, pages x heads.  16 pages are the rows of mma.m16n8k16, up to
 //   eight heads its columns; the rows go from memory straight into the operand's registers (the order of the columns is
 //   free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
-//   all tiles of 16 pages.  Written per page: the score and a bound of its error.
+//   all tiles of 16 pages and brings them in through a ring of its own in shared memory (rows loaded straight into registers, two
+//   blocks per SM, left a third of the memory's rate unused).  Written per page: the score and a bound of its error.
 // Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
 // magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
 // queries also lose 2^-16 of themselves.  Taken: 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest
 // bound; infinite where a score or bound is not finite.
-#ifndef KL_PS_BATCH
-#define KL_PS_BATCH 8
-#endif
-#ifndef KL_PS_BPS
-#define KL_PS_BPS 2
-#endif
 // The number of the larger magnitude, bf16 by bf16 (NaN is left out: it makes the score NaN).
 __device__ __forceinline__ uint32_t ps_larger(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-template <int HD, bool F32>
-constexpr int ps_blocks_per_sm() { return HD == 256 || (HD == 128 && F32) ? 1 : KL_PS_BPS; }   // what the registers allow
+template <int HD>
+struct PsCfg {
+    static constexpr int ROW = 4 * HD, TILE = 16 * ROW;   // bytes of a page's bounds, of a tile's
+    static constexpr int NW = HD == 256 ? 6 : 12;         // warps
+    static constexpr int ST = 196608 / (NW * TILE);       // tiles of a warp's ring: 4, 2, 2
+    static constexpr size_t SMEM = (size_t)NW * ST * TILE;
+};
 template <int HD, bool F32>   // F32: type of the queries
-__global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
-    constexpr int NW = PG_THREADS / 32, NC = HD / 16;   // 16-byte pieces of a row's 4 hd bytes per lane
-    constexpr int BATCH = NC > KL_PS_BATCH ? KL_PS_BATCH : NC;              // of them in flight at once
-    __shared__ uint64_t pre[PG_THREADS], wsum[NW];
+__global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(const PagedView c, const PagedSelect a) {
+    using Cfg = PsCfg<HD>;
+    constexpr int NW = Cfg::NW, ST = Cfg::ST, ROW = Cfg::ROW, TILE = Cfg::TILE;
+    constexpr int NC = HD / 16;                         // 16-byte pieces of a row per lane
+    constexpr int CPR = ROW / 16, PASSES = 16 * CPR / 32;   // pieces of a row; copies of a lane per tile
+    extern __shared__ __align__(128) uint8_t ps_smem[];
+    __shared__ uint64_t pre[NW * 32], wsum[NW];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, g = lane >> 2, j = lane & 3u;
-    const uint32_t n = c.n_seqs, per = (n + PG_THREADS - 1u) / PG_THREADS, HT = (a.G + 7u) / 8u;
+    const uint32_t n = c.n_seqs, per = (n + NW * 32u - 1u) / (NW * 32u), HT = (a.G + 7u) / 8u;
     auto pages_of = [&](uint32_t s) { return (pg_length(c, s) + c.page - 1u) / c.page; };
     const uint64_t W = pg_prefix<NW>(n, pre, wsum, [&](uint32_t s) { return (uint64_t)((pages_of(s) + 15u) / 16u) * c.nkv; });
     const uint32_t warps = gridDim.x * NW, w = warp * gridDim.x + blockIdx.x;   // few tiles spread over the SMs
     const uint64_t share = pg_div(W, warps), over = W - share * warps;
     const uint64_t lo = share * w + min((uint64_t)w, over), hi = lo + share + (w < over ? 1u : 0u);
     if (lo >= hi) return;
-    const uint32_t i0 = pg_find<NW>(pre, lo);
-    uint64_t rem = lo - pre[i0];
-    uint32_t s = i0 * per, np = pages_of(s), nt = (np + 15u) / 16u;   // pages and tiles per head of sequence s
-    while (rem >= (uint64_t)nt * c.nkv) {
-        rem -= (uint64_t)nt * c.nkv;
-        np = pages_of(++s);
-        nt = (np + 15u) / 16u;
+    struct Cursor { uint32_t s, h, t, np, nt; };   // sequence, kv head, tile; pages and tiles per head of the sequence
+    Cursor cur;
+    {
+        const uint32_t i0 = pg_find<NW>(pre, lo);
+        uint64_t rem = lo - pre[i0];
+        cur.s = i0 * per;
+        cur.np = pages_of(cur.s);
+        cur.nt = (cur.np + 15u) / 16u;
+        while (rem >= (uint64_t)cur.nt * c.nkv) {
+            rem -= (uint64_t)cur.nt * c.nkv;
+            cur.np = pages_of(++cur.s);
+            cur.nt = (cur.np + 15u) / 16u;
+        }
+        cur.h = (uint32_t)pg_div(rem, cur.nt);
+        cur.t = (uint32_t)(rem - (uint64_t)cur.h * cur.nt);
     }
-    uint32_t h = (uint32_t)pg_div(rem, nt), t = (uint32_t)(rem - (uint64_t)h * nt);
-    uint32_t qf[NC][2][2], ql[F32 ? NC : 1][2][2];   // B fragments of the current head tile, and what bf16 leaves of fp32 queries
-    auto look_up = [&](uint32_t ss, uint32_t tt, uint32_t pages) -> int32_t {   // lane l < 16: page 16 tt + l
-        const uint32_t p = tt * 16u + lane;
-        return lane < 16u && p < pages ? pg_physical(c, ss, p) : -1;
+    auto advance = [&](Cursor& x) {   // to a tile that exists
+        if (++x.t < x.nt) return;
+        x.t = 0;
+        if (++x.h < c.nkv) return;
+        x.h = 0;
+        do {
+            x.np = pages_of(++x.s);
+            x.nt = (x.np + 15u) / 16u;
+        } while (x.nt == 0u);
     };
+    // Requests: lane l < 16 looks up where the bounds of page 16 t + l lie, one tile ahead of the copies.
+    Cursor req = cur;
+    uint64_t left = hi - lo;   // tiles still to request
+    int64_t at = -1;
+    auto look_up = [&]() {
+        const uint32_t p = req.t * 16u + lane;
+        const int32_t phys = lane < 16u && p < req.np ? pg_physical(c, req.s, p) : -1;
+        at = phys < 0 ? -1 : ((int64_t)phys * c.nkv + req.h) * ROW;
+    };
+    look_up();
+    const uint32_t ring = smem_u32(ps_smem) + warp * (ST * TILE);
+    auto swizzle = [](uint32_t r) { return (r & 1u) << 2 | ((r >> 1) & 3u); };   // as in the attention kernel's tiles
+    auto request = [&](uint32_t slot) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const uint32_t e = i * 32 + lane, r = e / CPR, piece = e % CPR;
+            const int64_t from = __shfl_sync(0xffffffffu, at, r);
+            pa_copy16(ring + slot * TILE + r * ROW + ((piece ^ swizzle(r)) << 4), reinterpret_cast<const uint8_t*>(c.bounds) + max(from, (int64_t)0) + piece * 16u,
+                      from >= 0);
+        }
+        if (--left) {
+            advance(req);
+            look_up();
+        }
+    };
+    uint32_t qf[NC][2][2], ql[F32 ? NC : 1][2][2];   // B fragments of the current head tile, and what bf16 leaves of fp32 queries
     float q1 = 0.f;   // largest sum |q_d| of the heads seen, infinite where one is NaN
     auto load_queries = [&](uint32_t ht) {
         float sum = 0.f;
-        const uint32_t head = h * a.G + min(ht * 8u + g, a.G - 1u);   // a missing head repeats the last one
-        const uint8_t* q = a.q + (int64_t)s * a.q_stride + (size_t)head * HD * (F32 ? 4 : 2);
+        const uint32_t head = cur.h * a.G + min(ht * 8u + g, a.G - 1u);   // a missing head repeats the last one
+        const uint8_t* q = a.q + (int64_t)cur.s * a.q_stride + (size_t)head * HD * (F32 ? 4 : 2);
 #pragma unroll
         for (int i = 0; i < NC; ++i)
 #pragma unroll
@@ -609,58 +683,41 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
         for (int o = 4; o < 32; o <<= 1) sum = fmaxf(sum, __shfl_xor_sync(0xffffffffu, sum, o));
         q1 = ht ? fmaxf(q1, sum) : sum;
     };
-    int32_t ids = look_up(s, t, np);
-    if (HT == 1u) load_queries(0);
-    for (uint64_t left = hi - lo; left; --left) {
-        const int32_t p0 = __shfl_sync(0xffffffffu, ids, g), p1 = __shfl_sync(0xffffffffu, ids, g + 8u);
-        const uint4* r0 = reinterpret_cast<const uint4*>(c.bounds + ((int64_t)max(p0, 0) * c.nkv + h) * 2 * HD) + j;
-        const uint4* r1 = reinterpret_cast<const uint4*>(c.bounds + ((int64_t)max(p1, 0) * c.nkv + h) * 2 * HD) + j;
-        // the next tile, whose look-up travels with this one's rows
-        uint32_t ns = s, nh = h, ntile = t + 1u, npages = np;
-        if (ntile == nt) {
-            ntile = 0;
-            if (++nh == c.nkv && left > 1u) {
-                nh = 0;
-                do npages = pages_of(++ns);
-                while (npages == 0u);
-            }
+    bool fresh = true;
+    uint32_t to = 0, slot = 0, ahead = 0;
+    for (uint64_t k = lo; k < hi;) {
+        if (ahead >= (uint32_t)ST - 1u) {
+            if (fresh && HT == 1u) load_queries(0);
+            fresh = false;
+            asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+            __syncwarp();   // the tile is there for every lane, and every lane is done with the previous one
         }
-        if (left > 1u) ids = look_up(ns, ntile, npages);
+        if (left) request(to);
+        if (++to == (uint32_t)ST) to = 0;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (ahead < (uint32_t)ST - 1u) {   // the first ST - 1 tiles are only requested
+            ++ahead;
+            continue;
+        }
+        const uint32_t rows = ring + slot * TILE + g * ROW, fk = swizzle(g);   // rows g and g + 8: the same swizzle
         float best0 = -INFINITY, best1 = -INFINITY;
         uint32_t big0 = 0, big1 = 0;   // largest magnitudes, two columns of bf16 (their signs mean nothing)
         for (uint32_t ht = 0; ht < HT; ++ht) {
             if (HT > 1u) load_queries(ht);
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i0_ = 0; i0_ < NC; i0_ += BATCH) {
-                uint4 x[BATCH], y[BATCH];
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (p0 >= 0) x[i] = r0[(i0_ + i) * 4];
-                    if (p1 >= 0) y[i] = r1[(i0_ + i) * 4];
+            for (int k4 = 0; k4 < NC; ++k4) {
+                const uint32_t piece = ((k4 * 4 + j) ^ fk) << 4;
+                const uint4 x = pa_lds16(rows + piece), y = pa_lds16(rows + 8 * ROW + piece);
+                pa_mma<false>(acc, x.x, y.x, x.y, y.y, qf[k4][0][0], qf[k4][0][1]);
+                pa_mma<false>(acc, x.z, y.z, x.w, y.w, qf[k4][1][0], qf[k4][1][1]);
+                if (F32) {
+                    pa_mma<false>(acc, x.x, y.x, x.y, y.y, ql[F32 ? k4 : 0][0][0], ql[F32 ? k4 : 0][0][1]);
+                    pa_mma<false>(acc, x.z, y.z, x.w, y.w, ql[F32 ? k4 : 0][1][0], ql[F32 ? k4 : 0][1][1]);
                 }
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int k = i0_ + i;
-                    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                        : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
-                        : "r"(x[i].x), "r"(y[i].x), "r"(x[i].y), "r"(y[i].y), "r"(qf[k][0][0]), "r"(qf[k][0][1]));
-                    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                        : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
-                        : "r"(x[i].z), "r"(y[i].z), "r"(x[i].w), "r"(y[i].w), "r"(qf[k][1][0]), "r"(qf[k][1][1]));
-                    if (F32) {
-                        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                            : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
-                            : "r"(x[i].x), "r"(y[i].x), "r"(x[i].y), "r"(y[i].y), "r"(ql[F32 ? k : 0][0][0]), "r"(ql[F32 ? k : 0][0][1]));
-                        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                            : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
-                            : "r"(x[i].z), "r"(y[i].z), "r"(x[i].w), "r"(y[i].w), "r"(ql[F32 ? k : 0][1][0]), "r"(ql[F32 ? k : 0][1][1]));
-                    }
-                    if (ht == 0u) {
-                        big0 = ps_larger(ps_larger(big0, ps_larger(x[i].x, x[i].y)), ps_larger(x[i].z, x[i].w));
-                        big1 = ps_larger(ps_larger(big1, ps_larger(y[i].x, y[i].y)), ps_larger(y[i].z, y[i].w));
-                    }
+                if (ht == 0u) {
+                    big0 = ps_larger(ps_larger(big0, ps_larger(x.x, x.y)), ps_larger(x.z, x.w));
+                    big1 = ps_larger(ps_larger(big1, ps_larger(y.x, y.y)), ps_larger(y.z, y.w));
                 }
             }
             // (a NaN must not be lost in a maximum: it says that the score is not known)
@@ -677,42 +734,41 @@ __global__ void __launch_bounds__(PG_THREADS, ps_blocks_per_sm<HD, F32>()) kl_pa
             big1 = ps_larger(big1, __shfl_xor_sync(0xffffffffu, big1, o));
         }
         if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
-            const uint32_t p = t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
+            const uint32_t p = cur.t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
             const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
             const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? 0x1p-14f : 0x1p-16f);
             // (infinite where nothing is known: 0 * infinity, a score that is not finite)
-            if (p < np) a.scores[((size_t)s * c.nkv + h) * c.table_pages + p] = make_float2(score, isfinite(score) && err >= 0.f ? err : INFINITY);
+            if (p < cur.np) a.scores[((size_t)cur.s * c.nkv + cur.h) * c.table_pages + p] = make_float2(score, isfinite(score) && err >= 0.f ? err : INFINITY);
         }
-        if (left > 1u) {
-            const bool other = ns != s || nh != h;
-            if (ns != s) {
-                np = npages;
-                nt = (np + 15u) / 16u;
-            }
-            s = ns; h = nh; t = ntile;
-            if (other && HT == 1u) load_queries(0);
+        if (++slot == (uint32_t)ST) slot = 0;
+        if (++k < hi) {
+            const uint32_t h = cur.h, s = cur.s;
+            advance(cur);
+            fresh = cur.h != h || cur.s != s;
         }
     }
 }
 
 // The choice: one block per (sequence, kv head).
 //   1. T = the need-th largest of the approximate scores: by a histogram and the ranks within one bin, or, where too many
-//      keys share the bin, from the top bit on (from below the bits all of them share).
+//      keys share the bin, bit by bit (from below the bits all of them share).
 //   2. With E the largest bound of their errors, pages above T + 2 E are chosen for certain and pages below T - 2 E are not.
 //      What lies between is chosen too if there is room for all of it; otherwise exact scores decide (equal ones by page): for
-//      up to PT_LIST candidates a warp scores one each and they are ranked against one another, for more (many equal
-//      scores, or E infinite) step 1 is repeated on the exact scores.
-//   3. The chosen pages are put in order by a prefix sum.
-// KPT > 0: every thread keeps KPT neighbouring keys in registers, and two bits are found per step; KPT == 0: any number of
-// pages, read again for each step.
+//      up to PT_LIST candidates a warp scores one query head of one each and they are ranked against one another, for more (many equal
+//      scores, or E infinite) a threshold is found bit by bit among the exact scores.
+//   3. The chosen pages are put in order by a prefix sum over groups of 32.
+// The keys lie in shared memory (SMEM), or, beyond PT_KEYS pages, in the workspace.  A block's time is latency -- barriers, and
+// fetching its own instructions, each of which runs a few times only -- so the loops are not unrolled (eight keys per thread in
+// registers and everything unrolled took twice as long).
 constexpr int PT_THREADS = 512;
-constexpr uint32_t PT_LIST = 128;
-template <int KPT>
+constexpr uint32_t PT_LIST = 128, PT_KEYS = 16384;
+template <bool SMEM>
 __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const PagedView c, const PagedSelect a) {
-    constexpr int NW = PT_THREADS / 32, NK = KPT ? KPT : 1;
-    constexpr uint32_t SURE = 0xffffffffu;   // key of a page that is chosen in any case; 0: of one that is not looked at
+    constexpr int NW = PT_THREADS / 32;
+    constexpr uint32_t SURE = 0xffffffffu;   // key of a page that is chosen in any case; 0: of one that is not
+    extern __shared__ uint32_t keys_s[];     // [pages of the longest sequence] (SMEM)
     __shared__ uint4 red[2][NW];
-    __shared__ uint32_t list_n, list_page[PT_LIST], list_key[PT_LIST], found[4], hist[KPT ? PT_THREADS : 1];
+    __shared__ uint32_t list_n, sure_n, list_page[PT_LIST], list_key[PT_LIST], found[4], hist[PT_THREADS];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
@@ -725,9 +781,10 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         return;
     }
     auto number = [](uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); };   // the score behind a key
-    auto forced = [&](uint32_t i) { return i < a.keep_first || i + a.keep_last >= n; };
+    auto key = [&](uint32_t i) -> uint32_t& { return SMEM ? keys_s[i] : reinterpret_cast<uint32_t*>(sc + i)[1]; };
     const uint32_t need = a.n_select - (a.keep_first + a.keep_last);   // n > n_select >= keep_first + keep_last
-    if (tid == 0u) list_n = 0u;
+    hist[tid] = 0u;
+    if (tid == 0u) list_n = sure_n = 0u;
 
     int turn = 0;
     // sums of x, y, or the maxima of x, z and the minimum of y, over the block
@@ -737,246 +794,17 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         if (extremes) z = __reduce_max_sync(0xffffffffu, z);
         if (lane == 0u) red[turn][warp] = make_uint4(x, y, z, 0u);
         __syncthreads();
-        uint4 t = red[turn][0];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            const uint4 p = red[turn][w];
-            t.x = extremes ? max(t.x, p.x) : t.x + p.x;
-            t.y = extremes ? min(t.y, p.y) : t.y + p.y;
-            t.z = max(t.z, p.z);
-        }
+        const uint4 p = red[turn][lane % NW];
         turn ^= 1;   // the next call writes the other half, and nobody is two calls behind
+        uint4 t;
+        t.x = extremes ? __reduce_max_sync(0xffffffffu, p.x) : __reduce_add_sync(0xffffffffu, lane < (uint32_t)NW ? p.x : 0u);
+        t.y = extremes ? __reduce_min_sync(0xffffffffu, p.y) : __reduce_add_sync(0xffffffffu, lane < (uint32_t)NW ? p.y : 0u);
+        t.z = extremes ? __reduce_max_sync(0xffffffffu, p.z) : 0u;
         return t;
     };
-    // keys: of the approximate scores, or (from_exact) those that the workspace holds in the place of the error bounds
-    uint32_t key[NK];
-    bool from_exact = false;
-    auto key_at = [&](uint32_t i) { return forced(i) ? SURE : from_exact ? __float_as_uint(sc[i].y) : pg_key(sc[i].x); };
-    auto each = [&](auto&& f) {   // f(key, page) for every page of this thread (and for places behind the last one, with key 0)
-        if (KPT) {
-#pragma unroll
-            for (int r = 0; r < NK; ++r) f(key[r], tid * NK + r);
-        } else {
-            for (uint32_t i = tid; i < n; i += PT_THREADS) f(key_at(i), i);
-        }
-    };
-    // The largest t that at least `want` keys reach -- lo and hi: the smallest and the largest key but SURE and 0 -- or, as
-    // soon as a t is found that exactly `want` keys reach, that one (exact).
-    auto threshold = [&](uint32_t lo, uint32_t hi, uint32_t want, bool& exact) {
-        const uint32_t differ = lo ^ hi;
-        int bit = differ ? 31 - __clz(differ) : -1;
-        uint32_t t = bit >= 0 ? lo & ~((2u << bit) - 1u) : lo;
-        exact = false;
-        auto pick = [&](uint32_t with, uint32_t x) {   // x keys reach t | with
-            if (x < want) return false;
-            t |= with;
-            exact = x == want;
-            return true;
-        };
-        while (bit >= 0 && !exact) {
-            if (KPT && bit > 0) {   // three counts of at most 2^13 in two words
-                const uint32_t t1 = t | 1u << (bit - 1), t2 = t | 2u << (bit - 1), t3 = t | 3u << (bit - 1);
-                uint32_t x = 0, y = 0;
-                each([&](uint32_t k, uint32_t) {
-                    if (k == SURE) return;
-                    x += (k >= t1) + (k >= t2 ? 0x10000u : 0u);
-                    y += k >= t3;
-                });
-                const uint4 r = reduce(x, y, 0u, false);
-                if (!pick(3u << (bit - 1), r.y) && !pick(2u << (bit - 1), r.x >> 16)) pick(1u << (bit - 1), r.x & 0xffffu);
-                bit -= 2;
-            } else {
-                uint32_t x = 0;
-                each([&](uint32_t k, uint32_t) { x += k >= (t | 1u << bit) && k != SURE; });
-                pick(1u << bit, reduce(x, 0u, 0u, false).x);
-                --bit;
-            }
-        }
-        return t;
-    };
-
-    uint32_t mx = 0, mn = 0xffffffffu, mag = 0;
-    auto take = [&](uint32_t i) {
-        const float2 x = i < n ? sc[i] : make_float2(0.f, 0.f);
-        const uint32_t k = i >= n ? 0u : forced(i) ? SURE : pg_key(x.x);
-        if (k && k != SURE) {
-            mx = max(mx, k);
-            mn = min(mn, k);
-            mag = max(mag, __float_as_uint(x.y));   // not negative: ordered like whole numbers
-        }
-        return k;
-    };
-    if (KPT) {
-#pragma unroll
-        for (int r = 0; r < NK; ++r) key[r] = take(tid * NK + r);
-    } else {
-        for (uint32_t i = tid; i < n; i += PT_THREADS) take(i);
-    }
-    uint32_t t = SURE - 1u, ties = 0;   // chosen: keys above t, and the first `ties` of those equal to it
-    if (need) {
-        const uint4 all = reduce(mx, mn, mag, true);
-        const float E = __uint_as_float(all.z);
-        float above = INFINITY, below = -INFINITY;
-        if (isfinite(E)) {
-            // the need-th largest key: a histogram over bins of equal width finds its bin, the few keys of that bin are ranked
-            uint32_t low = 0u;
-            if (KPT) {
-                const float x0 = number(all.y), width = (PT_THREADS - 1) / (number(all.x) - x0);
-                auto bin_of = [&](uint32_t k) { return (uint32_t)min(PT_THREADS - 1, max(0, (int)((number(k) - x0) * width))); };
-                hist[tid] = 0u;
-                __syncthreads();
-#pragma unroll
-                for (int r = 0; r < NK; ++r)
-                    if (key[r] && key[r] != SURE) atomicAdd(&hist[bin_of(key[r])], 1u);
-                __syncthreads();
-                // keys in this thread's bin and above: a sum from the last bin down
-                const uint32_t mine = hist[PT_THREADS - 1 - tid];
-                uint32_t sum = mine;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
-                    if (lane >= (uint32_t)o) sum += y;
-                }
-                if (lane == 31u) red[turn][warp].x = sum;
-                __syncthreads();
-#pragma unroll
-                for (int w = 0; w < NW; ++w)
-                    if (w < (int)warp) sum += red[turn][w].x;
-                turn ^= 1;
-                if (sum >= need && sum - mine < need) {   // one thread
-                    found[0] = PT_THREADS - 1 - tid;
-                    found[1] = need - (sum - mine);       // rank within the bin, from 1
-                    found[2] = mine;
-                }
-                __syncthreads();
-                const uint32_t bin = found[0], rank = found[1], cnt = found[2];
-                if (cnt <= PT_LIST) {
-#pragma unroll
-                    for (int r = 0; r < NK; ++r)
-                        if (key[r] && key[r] != SURE && bin_of(key[r]) == bin) list_key[atomicAdd(&list_n, 1u)] = key[r];
-                    __syncthreads();
-                    if (tid < cnt) {
-                        const uint32_t k = list_key[tid];
-                        uint32_t before = 0;
-                        for (uint32_t i = 0; i < cnt; ++i) before += list_key[i] > k || (list_key[i] == k && i < tid);
-                        if (before + 1u == rank) found[3] = k;
-                    }
-                    __syncthreads();
-                    low = found[3];
-                    if (tid == 0u) list_n = 0u;   // (the next barrier comes before its next use)
-                }
-            }
-            if (!low) {
-                bool exact;
-                const uint32_t t0 = threshold(all.y, all.x, need, exact);
-                low = t0;
-                if (exact) {   // the smallest key that reaches t0 is the need-th largest
-                    low = 0xffffffffu;
-                    each([&](uint32_t k, uint32_t) { if (k >= t0 && k != SURE) low = min(low, k); });
-                    low = reduce(0u, low, 0u, true).y;
-                }
-            }
-            const float T = number(low);
-            above = __fadd_ru(T, 2.f * E);
-            below = __fadd_rd(T, -2.f * E);
-        }
-        auto where = [&](uint32_t k) {   // 0: not looked at, 1: out, 2: candidate, 3: chosen
-            if (!k || k == SURE) return 0;
-            const float x = number(k);
-            return k == 1u ? 2 : x > above ? 3 : x < below ? 1 : 2;   // 1: NaN
-        };
-        uint32_t cand = 0, sure = 0;
-        each([&](uint32_t k, uint32_t) {
-            cand += where(k) == 2;
-            sure += where(k) == 3;
-        });
-        const uint4 cs = reduce(cand, sure, 0u, false);
-        const uint32_t room = need - cs.y;       // for candidates
-        const bool open = cs.x > room, few = cs.x <= PT_LIST;
-        if (KPT && (!open || few)) {
-            const uint32_t slot0 = open && cand ? atomicAdd(&list_n, cand) : 0u;
-            uint32_t slot = slot0;
-            if (open) {
-#pragma unroll
-                for (int r = 0; r < NK; ++r)
-                    if (where(key[r]) == 2) list_page[slot++] = tid * NK + r;
-                __syncthreads();
-                for (uint32_t i = warp; i < cs.x; i += NW) {
-                    const int32_t phys = pg_physical(c, s, list_page[i]);
-                    const uint32_t k = phys >= 0 ? pg_key(ps_exact(c, a, s, h, phys)) : 1u;
-                    if (lane == 0u) list_key[i] = k;
-                }
-                __syncthreads();
-            }
-            slot = slot0;
-#pragma unroll
-            for (int r = 0; r < NK; ++r) {
-                const int w = where(key[r]);
-                bool take_it = w == 3 || (w == 2 && !open);
-                if (w == 2 && open) {   // its rank among the candidates
-                    const uint32_t k = list_key[slot++], page = tid * NK + r;
-                    uint32_t rank = 0;
-                    for (uint32_t i = 0; i < cs.x; ++i) rank += list_key[i] > k || (list_key[i] == k && list_page[i] < page);
-                    take_it = rank < room;
-                }
-                if (w) key[r] = take_it ? SURE : 0u;
-            }
-        } else {   // through the workspace, where a key takes the place of the error bound; candidates get that of their exact score
-            uint32_t cmx = 0, cmn = 0xffffffffu;
-#pragma unroll 1
-            for (uint32_t i0 = 0; i0 < n; i0 += PT_THREADS) {
-                const uint32_t i = i0 + tid;
-                uint32_t k = i >= n ? 0u : forced(i) ? SURE : pg_key(sc[i].x);
-                const int w = where(k);
-                const bool ask = open && w == 2;
-                if (w) k = w == 3 || (w == 2 && !open) ? SURE : 0u;
-                const int32_t phys = ask ? pg_physical(c, s, i) : -1;
-                for (uint32_t todo = __ballot_sync(0xffffffffu, ask); todo; todo &= todo - 1u) {
-                    const int src = __ffs(todo) - 1;
-                    const int32_t ph = __shfl_sync(0xffffffffu, phys, src);
-                    const uint32_t ek = ph >= 0 ? pg_key(ps_exact(c, a, s, h, ph)) : 1u;
-                    if ((int)lane == src) {
-                        k = ek;
-                        cmx = max(cmx, ek);
-                        cmn = min(cmn, ek);
-                    }
-                }
-                if (i < n) sc[i].y = __uint_as_float(k);
-            }
-            __syncthreads();
-            from_exact = true;
-            if (KPT)
-#pragma unroll
-                for (int r = 0; r < NK; ++r) key[r] = tid * NK + r < n ? key_at(tid * NK + r) : 0u;
-            if (open) {
-                const uint4 ce = reduce(cmx, cmn, 0u, true);
-                bool exact;
-                t = threshold(ce.y, ce.x, room, exact);
-                ties = 0xffffffffu;
-                if (!exact) {
-                    uint32_t x = 0;
-                    each([&](uint32_t k, uint32_t) { x += k > t && k != SURE; });
-                    ties = room - reduce(x, 0u, 0u, false).x;
-                }
-            }
-        }
-    }
-    // in order
-    uint32_t done = 0, tied = 0;   // chosen pages without the equal ones, and equal ones, so far
-    constexpr uint32_t STEP = PT_THREADS * NK;
-    for (uint32_t i0 = 0; i0 < n; i0 += STEP) {   // once where the keys are in registers
-        bool sure[NK], eq[NK];
-        uint32_t ns = 0, ne = 0;
-#pragma unroll
-        for (int r = 0; r < NK; ++r) {
-            const uint32_t i = i0 + tid * NK + r;
-            const uint32_t k = i >= n ? 0u : KPT ? key[r] : need || forced(i) ? key_at(i) : 0u;
-            eq[r] = ties && k == t;
-            sure[r] = k > t;
-            ns += sure[r];
-            ne += eq[r];
-        }
-        uint32_t both = ns | ne << 16, incl = both;   // at most STEP <= 2^13 each
+    // exclusive prefix sum over the block's threads
+    auto scan = [&](uint32_t v) {
+        uint32_t incl = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
@@ -984,24 +812,203 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
         }
         if (lane == 31u) red[turn][warp].x = incl;
         __syncthreads();
-        uint32_t before = incl - both, all = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const uint32_t y = red[turn][w].x;
-            if (w < (int)warp) before += y;
-            all += y;
-        }
+        const uint32_t p = lane < warp ? red[turn][lane].x : 0u;   // warp < NW <= 32
         turn ^= 1;
-        uint32_t bs = done + (before & 0xffffu), be = tied + (before >> 16);
-#pragma unroll
-        for (int r = 0; r < NK; ++r) {
-            const uint32_t at = bs + min(be, ties);
-            if ((sure[r] || (eq[r] && be < ties)) && at < a.n_select) out[at] = (int32_t)(i0 + tid * NK + r);
-            bs += sure[r];
-            be += eq[r];
+        return incl - v + __reduce_add_sync(0xffffffffu, p);
+    };
+    // The largest t that at least `want` keys (but SURE) reach -- lo and hi: the smallest and the largest key but SURE and 0 --
+    // or, as soon as a t is found that exactly `want` keys reach, that one (exact).
+    auto threshold = [&](uint32_t lo, uint32_t hi, uint32_t want, bool& exact) {
+        const uint32_t differ = lo ^ hi;
+        int bit = differ ? 31 - __clz(differ) : -1;
+        uint32_t t = bit >= 0 ? lo & ~((2u << bit) - 1u) : lo;
+        exact = false;
+#pragma unroll 1
+        for (; bit >= 0 && !exact; --bit) {
+            uint32_t x = 0;
+#pragma unroll 1
+            for (uint32_t i = tid; i < n; i += PT_THREADS) x += key(i) >= (t | 1u << bit) && key(i) != SURE;
+            x = reduce(x, 0u, 0u, false).x;
+            if (x >= want) {
+                t |= 1u << bit;
+                exact = x == want;
+            }
         }
-        done += all & 0xffffu;
-        tied += all >> 16;
+        return t;
+    };
+
+    uint32_t mx = 0, mn = 0xffffffffu, err = 0;
+#pragma unroll 1
+    for (uint32_t i = tid; i < n; i += PT_THREADS) {
+        const float2 x = sc[i];
+        uint32_t k = SURE;
+        if (i >= a.keep_first && i + a.keep_last < n) {
+            k = pg_key(x.x);
+            mx = max(mx, k);
+            mn = min(mn, k);
+            err = max(err, __float_as_uint(x.y));   // not negative: ordered like whole numbers
+        }
+        key(i) = need || k == SURE ? k : 0u;
+    }
+    uint32_t t = SURE - 1u, ties = 0;   // chosen: keys above t, and the first `ties` of those equal to it
+    if (need) {
+        const uint4 all = reduce(mx, mn, err, true);
+        const float E = __uint_as_float(all.z);
+        float above = INFINITY, below = -INFINITY;
+        if (isfinite(E)) {
+            // bins of equal width between the smallest and the largest score
+            const float x0 = number(all.y), width = (PT_THREADS - 1) / (number(all.x) - x0);
+            auto bin_of = [&](uint32_t k) { return (uint32_t)min(PT_THREADS - 1, max(0, (int)((number(k) - x0) * width))); };
+#pragma unroll 1
+            for (uint32_t i = tid; i < n; i += PT_THREADS)
+                if (key(i) != SURE) atomicAdd(&hist[bin_of(key(i))], 1u);
+            __syncthreads();
+            const uint32_t mine = hist[PT_THREADS - 1 - tid], higher = scan(mine);   // from the last bin down
+            if (higher < need && higher + mine >= need) {   // one thread
+                found[0] = PT_THREADS - 1 - tid;
+                found[1] = need - higher;                   // rank within the bin, from 1
+                found[2] = mine;
+            }
+            __syncthreads();
+            const uint32_t bin = found[0], rank = found[1], cnt = found[2];
+            uint32_t low;
+            if (cnt <= PT_LIST) {
+#pragma unroll 1
+                for (uint32_t i = tid; i < n; i += PT_THREADS)
+                    if (key(i) != SURE && bin_of(key(i)) == bin) list_key[atomicAdd(&list_n, 1u)] = key(i);
+                __syncthreads();
+                if (tid < cnt) {
+                    const uint32_t k = list_key[tid];
+                    uint32_t before = 0;
+#pragma unroll 1
+                    for (uint32_t i = 0; i < cnt; ++i) before += list_key[i] > k || (list_key[i] == k && i < tid);
+                    if (before + 1u == rank) found[3] = k;
+                }
+                if (tid == PT_THREADS - 1) list_n = 0u;
+                __syncthreads();
+                low = found[3];
+            } else {
+                bool exact;
+                low = threshold(all.y, all.x, need, exact);
+                if (exact) {   // the smallest key that reaches it is the need-th largest
+                    uint32_t k = 0xffffffffu;
+#pragma unroll 1
+                    for (uint32_t i = tid; i < n; i += PT_THREADS)
+                        if (key(i) >= low) k = min(k, key(i));
+                    low = reduce(0u, k, 0u, true).y;
+                }
+            }
+            above = __fadd_ru(number(low), 2.f * E);
+            below = __fadd_rd(number(low), -2.f * E);
+        }
+        // certain ones, and the list of candidates
+        uint32_t sure = 0;
+#pragma unroll 1
+        for (uint32_t i = tid; i < n; i += PT_THREADS) {
+            const uint32_t k = key(i);
+            if (k == SURE) continue;
+            const float x = number(k);
+            if (k != 1u && x > above) {        // 1: NaN, always a candidate
+                key(i) = SURE;
+                ++sure;
+            } else if (k != 1u && x < below) {
+                key(i) = 0u;
+            } else {
+                const uint32_t at = atomicAdd(&list_n, 1u);
+                if (at < PT_LIST) list_page[at] = i;
+            }
+        }
+        sure = __reduce_add_sync(0xffffffffu, sure);
+        if (lane == 0u && sure) atomicAdd(&sure_n, sure);
+        __syncthreads();
+        const uint32_t cand = list_n, room = need - sure_n;   // room for candidates
+        if (cand <= PT_LIST) {
+            if (cand > room) {   // their exact scores decide
+                if (tid < cand) list_key[tid] = 0u;
+                __syncthreads();
+#pragma unroll 1
+                for (uint32_t i = warp; i < cand * a.G; i += NW) {   // a warp per candidate and query head
+                    const uint32_t x = i / a.G, g = i - x * a.G;
+                    const int32_t phys = pg_physical(c, s, list_page[x]);
+                    const uint32_t k = phys >= 0 ? pg_key(ps_exact(c, a, s, h, phys, g, g + 1u)) : 1u;
+                    if (lane == 0u) atomicMax(&list_key[x], k);
+                }
+                __syncthreads();
+            }
+            if (tid < cand) {
+                uint32_t before = 0;   // its rank among the candidates
+                if (cand > room) {
+                    const uint32_t k = list_key[tid], page = list_page[tid];
+#pragma unroll 1
+                    for (uint32_t i = 0; i < cand; ++i) before += list_key[i] > k || (list_key[i] == k && list_page[i] < page);
+                }
+                key(list_page[tid]) = before < room ? SURE : 0u;
+            }
+            __syncthreads();
+        } else {
+            uint32_t cmx = 0, cmn = 0xffffffffu;
+#pragma unroll 1
+            for (uint32_t i0 = 0; i0 < n; i0 += PT_THREADS) {   // whole warps: a warp scores its candidates one after another
+                const uint32_t i = i0 + tid;
+                const bool ask = i < n && key(i) != SURE && key(i) != 0u;
+                const int32_t phys = ask && cand > room ? pg_physical(c, s, i) : -1;
+                uint32_t k = SURE;
+                if (cand > room)
+                    for (uint32_t todo = __ballot_sync(0xffffffffu, ask); todo; todo &= todo - 1u) {
+                        const int src = __ffs(todo) - 1;
+                        const int32_t ph = __shfl_sync(0xffffffffu, phys, src);
+                        const uint32_t ek = ph >= 0 ? pg_key(ps_exact(c, a, s, h, ph, 0u, a.G)) : 1u;
+                        if ((int)lane == src) {
+                            k = ek;
+                            cmx = max(cmx, ek);
+                            cmn = min(cmn, ek);
+                        }
+                    }
+                if (ask) key(i) = k;
+            }
+            if (cand > room) {
+                const uint4 ce = reduce(cmx, cmn, 0u, true);
+                bool exact;
+                t = threshold(ce.y, ce.x, room, exact);
+                ties = 0xffffffffu;
+                if (!exact) {
+                    uint32_t x = 0;
+#pragma unroll 1
+                    for (uint32_t i = tid; i < n; i += PT_THREADS) x += key(i) > t && key(i) != SURE;
+                    ties = room - reduce(x, 0u, 0u, false).x;
+                }
+            }
+        }
+    }
+    // in order, PT_THREADS groups of 32 pages at a time
+    uint32_t done = 0, tied = 0;   // chosen pages without the equal ones, and equal ones, so far
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < n; i0 += PT_THREADS * 32u) {
+        const uint32_t end = min(n, i0 + PT_THREADS * 32u);
+        __syncthreads();   // hist takes the groups' counts, and then their sums
+#pragma unroll 1
+        for (uint32_t g = warp; g < (uint32_t)PT_THREADS; g += NW) {
+            const uint32_t i = i0 + g * 32u + lane, k = i < end ? key(i) : 0u;
+            const uint32_t bs = __ballot_sync(0xffffffffu, k > t), be = __ballot_sync(0xffffffffu, ties && k == t);
+            if (lane == 0u) hist[g] = __popc(bs) | __popc(be) << 16;   // sums of at most 2^14 each
+            if (i0 + g * 32u >= end) break;
+        }
+        __syncthreads();
+        const uint32_t groups = (end - i0 + 31u) / 32u, v = tid < groups ? hist[tid] : 0u, before = scan(v);
+        hist[tid] = before;
+        if (tid == PT_THREADS - 1) found[0] = before + v;
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t g = warp; g < groups; g += NW) {
+            const uint32_t i = i0 + g * 32u + lane, k = i < end ? key(i) : 0u, under = (1u << lane) - 1u;
+            const bool eq = ties && k == t;
+            const uint32_t bs = __ballot_sync(0xffffffffu, k > t), be = __ballot_sync(0xffffffffu, eq);
+            const uint32_t e = tied + (hist[g] >> 16) + __popc(be & under);
+            const uint32_t at = done + (hist[g] & 0xffffu) + __popc(bs & under) + min(e, ties);
+            if ((k > t || (eq && e < ties)) && at < a.n_select) out[at] = (int32_t)i;
+        }
+        done += found[0] & 0xffffu;
+        tied += found[0] >> 16;
     }
 }
 
@@ -1035,18 +1042,6 @@ __device__ __forceinline__ uint32_t pa_pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// D += A * B, one m16n8k16 tile of f16 (e4m3 caches) or bf16 operands.  Not volatile: the compiler may interleave chains.
-template <bool FP8>
-__device__ __forceinline__ void pa_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    if (FP8)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // Two numbers rounded to 16 bits (f16 with an e4m3 cache, bf16 else), and what that leaves of them.
 template <bool FP8>
 __device__ __forceinline__ uint32_t pa_round(float x0, float x1) {
@@ -1058,27 +1053,6 @@ __device__ __forceinline__ uint32_t pa_rest(float x0, float x1, uint32_t hi) {
     const float2 f = pg_f16x2_to_float2(hi);
     return pa_pack_f16(x0 - f.x, x1 - f.y);
 }
-// 16 (or 4) bytes to shared memory, asynchronously; nothing is read and zeros are written when `ok` is false.
-__device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src, bool ok) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void pa_copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void pa_copy4(uint32_t dst, const void* src, bool ok) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ uint4 pa_lds16(uint32_t a) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ uint2 pa_lds8(uint32_t a) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-    return v;
-}
-
 // Two neighbouring columns (d even) of query head hq of sequence s.
 __device__ __forceinline__ void pa_store2(const PagedView& c, const PagedAttn& a, uint32_t s, uint32_t hq, uint32_t d, float v0, float v1) {
     if (a.out_mode == PA_F32) {
