@@ -218,9 +218,11 @@ class PagedCache:
             d.n_pages, d.n_kv_heads, _, d.head_dim = bounds.shape
             d.page_size, d.kv_type = page_size, kv_type
         else:
-            _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, where)
+            _need(k.dim() == 4 and k.shape == v.shape and k.stride(3) == 1 and v.stride(3) == 1 and k.dtype == v.dtype, where)
+            strides = [[0 if t.shape[i] == 1 else t.stride(i) for i in range(3)] for t in (k, v)]   # of a single page or head: anything
+            _need(strides[0] == strides[1], where)
             d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
-            d.page_stride, d.head_stride, d.row_stride = k.stride(0), k.stride(1), k.stride(2)
+            d.page_stride, d.head_stride, d.row_stride = strides[0]
             d.kv_type = KL_KV_BF16 if k.dtype == torch.bfloat16 else KL_KV_E4M3
             _need(k.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn), where)
             if d.kv_type == KL_KV_E4M3:

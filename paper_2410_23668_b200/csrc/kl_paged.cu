@@ -79,8 +79,9 @@ kl_status check_rows(const kl_paged_cache* c, const kl_paged_seqs* s, const int3
     if (n_rows > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return KL_ERR_INVALID_ARG;
     const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
-    if ((n_rows > 1 && (ks < width || vs < width)) || ks < 0 || vs < 0 || ks > (INT64_MAX >> 34) || vs > (INT64_MAX >> 34)) return KL_ERR_INVALID_ARG;
-    if ((ks * elem(type)) % 16 || (vs * elem(type)) % 16) return KL_ERR_INVALID_ARG;
+    if (n_rows > 1)   // the stride of a single row means nothing
+        for (int64_t x : {ks, vs})
+            if (x < width || x > (INT64_MAX >> 34) || (x * elem(type)) % 16) return KL_ERR_INVALID_ARG;
     return KL_OK;
 }
 
@@ -103,8 +104,8 @@ kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_
     if (!q || (type != KL_F32 && type != KL_BF16)) return KL_ERR_INVALID_ARG;
     if (!n_q_heads || n_q_heads % c->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
     if ((uint64_t)n_q_heads * c->head_dim > 0x7fffffffull || n_q_heads > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
-    if (stride < 0 || (n_seqs > 1 && stride < (int64_t)n_q_heads * c->head_dim) || stride > (INT64_MAX >> 34)) return KL_ERR_INVALID_ARG;
-    if (!aligned16(q) || (stride * elem(type)) % 16) return KL_ERR_INVALID_ARG;
+    if (!aligned16(q)) return KL_ERR_INVALID_ARG;
+    if (n_seqs > 1 && (stride < (int64_t)n_q_heads * c->head_dim || stride > (INT64_MAX >> 34) || (stride * elem(type)) % 16)) return KL_ERR_INVALID_ARG;
     return KL_OK;
 }
 
@@ -144,10 +145,10 @@ int attn_blocks() {
 template <int HD>
 kl_status launch_append(int type, const PagedView& v, const PagedRows& r, dim3 grid, size_t smem, void* stream) {
     if (v.fp8)
-        return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, true>, grid, PG_THREADS, smem, stream, v, r)
-                              : launch(kl_paged_append_kernel<__nv_bfloat16, HD, true>, grid, PG_THREADS, smem, stream, v, r);
-    return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, false>, grid, PG_THREADS, smem, stream, v, r)
-                          : launch(kl_paged_append_kernel<__nv_bfloat16, HD, false>, grid, PG_THREADS, smem, stream, v, r);
+        return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, true>, grid, PW_THREADS, smem, stream, v, r)
+                              : launch(kl_paged_append_kernel<__nv_bfloat16, HD, true>, grid, PW_THREADS, smem, stream, v, r);
+    return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, false>, grid, PW_THREADS, smem, stream, v, r)
+                          : launch(kl_paged_append_kernel<__nv_bfloat16, HD, false>, grid, PW_THREADS, smem, stream, v, r);
 }
 template <int HD>
 kl_status launch_read(int type, const PagedView& v, const PagedRows& r, dim3 grid, void* stream) {
@@ -260,7 +261,7 @@ kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     if (units > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;
     const PagedView v = view(cache, seqs, status_d);
     const PagedRows r = rows_of(row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride);
-    const size_t smem = cache->bounds_d ? (size_t)(PG_THREADS / (cache->head_dim / 8) / 2) * 2 * cache->head_dim * 4 : 0;
+    const size_t smem = cache->bounds_d ? (size_t)(PW_THREADS / (cache->head_dim / 8) / 2) * 2 * cache->head_dim * 4 : 0;
     const dim3 grid((unsigned)units, cache->n_kv_heads);
     if (v.hd == 64) return launch_append<64>(row_type, v, r, grid, smem, stream);
     if (v.hd == 128) return launch_append<128>(row_type, v, r, grid, smem, stream);

@@ -153,7 +153,7 @@ constexpr int PG_THREADS = 256;
 
 // An array of row starts that descends or leaves [0, n_rows] is an error (one block of a call looks).
 __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedRows& r) {
-    for (uint32_t s = threadIdx.x; s < c.n_seqs; s += PG_THREADS) {
+    for (uint32_t s = threadIdx.x; s < c.n_seqs; s += blockDim.x) {
         const int32_t a = r.row_starts[s], b = r.row_starts[s + 1u];
         if (a < 0 || b < a || (uint32_t)b > r.n_rows) pg_error(c);
     }
@@ -164,8 +164,9 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // the grid belongs to the sequence s with base(s) <= u < base(s + 1), base(s) = row_starts[s] / page + 2 s, and is its
 // page number u - base(s) (blocks without a page leave).  hd / 8 lanes share a row, eight columns each; half of the
 // lane groups take keys, the other half values.
+constexpr int PW_THREADS = 128;   // 8191 e4m3 rows, pages of 64: 16.3 us; 256 threads 17.6, 64 threads 25.0
 template <class T, int HD, bool FP8>
-__global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
+__global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
     extern __shared__ float pg_red[];   // [groups of K rows][2][hd] when the cache has bounds
     griddep_launch();
     griddep_wait();
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
         __syncthreads();
         uint32_t best = 0, b0 = 0, b1 = 0;
         int32_t bp = 0;
-        for (uint32_t t = tid; t < c.n_seqs; t += PG_THREADS) {
+        for (uint32_t t = tid; t < c.n_seqs; t += PW_THREADS) {
             const uint32_t x = pg_row_start(c, rows, t), y = pg_row_start(c, rows, t + 1u);
             const int32_t p = c.positions[t];
             if (x / c.page + 2u * t <= u) {
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
     const int32_t phys = pg_physical(c, s, (uint32_t)lp);
     if (phys < 0) return;
 
-    constexpr uint32_t LANES = HD / 8, GROUPS = PG_THREADS / LANES / 2;   // lanes per row, rows at a time per side (K, V)
+    constexpr uint32_t LANES = HD / 8, GROUPS = PW_THREADS / LANES / 2;   // lanes per row, rows at a time per side (K, V)
     const uint32_t grp = tid / LANES, lane = tid % LANES, col = lane * 8u;
     const bool is_v = grp >= GROUPS;   // the same for a whole warp
     const uint32_t g = is_v ? grp - GROUPS : grp;
@@ -223,14 +224,15 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
     const uint8_t* src = (is_v ? rows.v : rows.k) + (int64_t)row0 * src_stride + ((size_t)h * HD + col) * sizeof(T);
     uint8_t* dst = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off0 * c.row_b + col * (FP8 ? 1 : 2);
     uint8_t* exps = FP8 ? (is_v ? c.ve : c.ke) + ((int64_t)phys * c.nkv + h) * c.page + off0 : nullptr;
-    // the page's bounds so far, requested ahead of the rows: thread t looks after columns t, t + PG_THREADS of [lo | hi]
+    // the page's bounds so far, requested ahead of the rows: thread t looks after columns t, t + PW_THREADS, ... of [lo | hi]
     __nv_bfloat16* bounds = c.bounds ? c.bounds + ((int64_t)phys * c.nkv + h) * 2 * HD : nullptr;
     const bool bounded = bounds && !is_v;
-    float old[2] = {INFINITY, INFINITY};
+    float old[512 / PW_THREADS];
     if (bounds)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t t = tid + i * PG_THREADS;
+        for (int i = 0; i < 512 / PW_THREADS; ++i) {
+            const uint32_t t = tid + i * PW_THREADS;
+            old[i] = 0.f;
             if (t < 2u * HD) old[i] = off0 == 0u ? (t >= (uint32_t)HD ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
         }
     float lo[8], hi[8];
@@ -327,8 +329,8 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_append_kernel(const Pa
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t t = tid + i * PG_THREADS;
+    for (int i = 0; i < 512 / PW_THREADS; ++i) {
+        const uint32_t t = tid + i * PW_THREADS;
         if (t >= 2u * HD) break;
         const bool up = t >= (uint32_t)HD;
         float x = old[i];
@@ -1089,24 +1091,15 @@ constexpr int PA_MAX_WARPS = 16;
 constexpr int PA_LENS = 1024;               // sequences whose lengths are kept in shared memory
 constexpr uint32_t PA_MIN_TILES = 8;        // fewest tiles worth a block
 
-#ifndef KL_PA_REST
-#define KL_PA_REST 1
-#endif
-#ifndef KL_PA_F8_NW
-#define KL_PA_F8_NW 12
-#endif
-#ifndef KL_PA_F8_TP
-#define KL_PA_F8_TP 32
-#endif
-#ifndef KL_PA_BF_NW
-#define KL_PA_BF_NW 12
-#endif
-// EX: fp32 queries and outputs -- what 16-bit rounding leaves of q and p enters the products too.
+// EX: fp32 queries and outputs -- what 16-bit rounding leaves of q enters the score product too.
+// Warps and tile: as many warps as the registers allow, with at least two tiles each in the ring.  Measured (device time of
+// kl_paged_attention): 32 sequences of <= 32768 e4m3 positions, 8 heads per kv head, head size 128: 12 warps x 32 positions
+// 162 us, 11 x 32 168, 6 x 64 174, 12 x 16 183, 16 x 16 (128 registers) 215; 32 x 4096 bf16: 12 x 16 90, 8 x 16 98.
 template <int HD, bool FP8, bool EX>
 struct PaCfg {
     static constexpr int ROW = FP8 ? HD : 2 * HD;            // bytes of a cached row
-    static constexpr int NW = HD == 256 ? (FP8 ? 8 : 6) : EX && HD == 128 ? 8 : HD == 64 ? 12 : FP8 ? KL_PA_F8_NW : KL_PA_BF_NW;     // warps
-    static constexpr int TP = HD == 64 ? 32 : HD == 128 && FP8 ? (EX ? 32 : KL_PA_F8_TP) : 16;     // positions per tile
+    static constexpr int NW = HD == 256 ? (FP8 ? 8 : 6) : EX && HD == 128 ? 8 : 12;   // warps
+    static constexpr int TP = HD == 64 || (HD == 128 && FP8) ? 32 : 16;               // positions per tile
     static constexpr int TILE = TP * ROW;                    // bytes of a K (or V) tile
     static constexpr int RING = 204800 / (NW * 2 * TILE);
     static constexpr int ST = RING > 8 ? 8 : RING;           // tiles of a warp's ring
@@ -1146,11 +1139,12 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     Where the range leaves a pair the pair's result is finished, or left as a partial one if other warps share the pair;
 //     those of one block meet in shared memory at the end, those of several blocks in kl_paged_merge_kernel.
 //   * Mathematics: sums of 2^(s - m) per head, s = q . k * scale * log2(e), m a reference that follows the maximum: it is
-//     raised (and the sums rescaled) only when a score exceeds it by more than 2^8, so that most tiles pass without an
+//     raised (and the sums rescaled) only when a score exceeds it by more than 8, so that most tiles pass without an
 //     exchange between lanes.  Positions are the 16 rows of mma.m16n8k16, the heads its eight columns:
 //     S[pos, head] = K . Q^T, O^T[d, head] += V^T . P; P leaves the score accumulators in 16-bit pairs and reaches the
-//     layout of a B operand with one movmatrix per 8 x 8 block.  Where 16 bits are not enough (bf16 probabilities;
-//     everything when q and out are fp32: EX) the rounding's rest enters as a second product.
+//     layout of a B operand with one movmatrix per 8 x 8 block.  What rounding p to 16 bits leaves of it (and, with fp32
+//     queries: EX, what it leaves of q) enters as a second product, so that results are as good as 32-bit ones; for e4m3 caches
+//     the second product costs 2 % of the time.
 //   * e4m3 rows become f16 (exact) on the way to the tensor cores.  Their scales are powers of two: 2^(e_k - 127) multiplies
 //     the score, 2^(e_v - 127) the probability.  The weighted probabilities w = p * 2^(e_v - 127) have a reference of
 //     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
@@ -1555,12 +1549,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             for (int t = 0; t < NS; ++t) {
                 const uint32_t h0 = pa_round<FP8>(p[4 * t], p[4 * t + 1]), h1 = pa_round<FP8>(p[4 * t + 2], p[4 * t + 3]);
                 const uint32_t b0 = movmatrix_trans(h0), b1 = movmatrix_trans(h1);
-                uint32_t c0 = 0u, c1 = 0u;
-                constexpr bool REST = KL_PA_REST || EX || !FP8;
-                if (REST) {
-                    c0 = movmatrix_trans(pa_rest<FP8>(p[4 * t], p[4 * t + 1], h0));
-                    c1 = movmatrix_trans(pa_rest<FP8>(p[4 * t + 2], p[4 * t + 3], h1));
-                }
+                const uint32_t c0 = movmatrix_trans(pa_rest<FP8>(p[4 * t], p[4 * t + 1], h0));
+                const uint32_t c1 = movmatrix_trans(pa_rest<FP8>(p[4 * t + 2], p[4 * t + 3], h1));
                 const uint32_t vs = vd + t * 16 * ROW;
                 if (FP8) {
                     constexpr int VW = HD >= 128 ? 4 : 2;            // words of a lane's piece of a row
@@ -1589,10 +1579,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                             const uint32_t y2 = pg_e4m3x2_to_f16x2(b23 & 0xffffu), y3 = pg_e4m3x2_to_f16x2(b23 >> 16);
                             pa_mma<FP8>(oo[0], x0, x1, x2, x3, b0, b1);
                             pa_mma<FP8>(oo[1], y0, y1, y2, y3, b0, b1);
-                            if (REST) {
-                                pa_mma<FP8>(oo[0], x0, x1, x2, x3, c0, c1);
-                                pa_mma<FP8>(oo[1], y0, y1, y2, y3, c0, c1);
-                            }
+                            pa_mma<FP8>(oo[0], x0, x1, x2, x3, c0, c1);
+                            pa_mma<FP8>(oo[1], y0, y1, y2, y3, c0, c1);
                         }
                     }
                 } else {

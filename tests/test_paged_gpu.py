@@ -301,6 +301,67 @@ def test_attention_many_sequences_and_batch_order():
     check_attention(c, q, torch.tensor(lengths, dtype=torch.int32) - 1, table)
 
 
+def test_attention_many_more_sequences_than_threads():
+    """Lengths beyond those kept in shared memory, several sequences per thread of the prefix sum, three of four empty."""
+    page, hd, n = 16, 64, 2100
+    lengths = [(i * 7) % 40 if i % 4 == 0 else 0 for i in range(n)]
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, 1, page, hd, True, seed=54)
+    table = ref.scattered_table(lengths, page, n_pages, seed=55)
+    q = (torch.randn(n, 2, hd, generator=torch.Generator().manual_seed(56)) * 0.05).to(torch.bfloat16).cuda()
+    check_attention(c, q, torch.tensor(lengths, dtype=torch.int32) - 1, table)
+
+
+def test_single_rows_pages_and_heads_of_any_stride():
+    """Strides of dimensions of size one mean nothing, to torch or to the library."""
+    k = torch.zeros(3, 1, 16, 64, dtype=torch.bfloat16, device="cuda").as_strided((3, 1, 16, 64), (1024, 7, 64, 1))
+    v = torch.zeros_like(k)
+    cache = kl.PagedCache(k, v)
+    rows = torch.randn(1, 1, 64, device="cuda").as_strided((1, 1, 64), (3, 5, 1))
+    table = i32([[2]]).as_strided((1, 1), (9, 1))
+    kl.kl_paged_append(cache, rows, rows * 2, i32([3]), table)
+    q = torch.randn(1, 4, 64, device="cuda").as_strided((1, 4, 64), (1, 64, 1))
+    out = torch.zeros(1, 4, 64, device="cuda")
+    ws = torch.empty(kl.kl_paged_workspace_bytes(cache, 4, 1, 1), dtype=torch.uint8, device="cuda")
+    kl.kl_paged_attention(cache, q, out, i32([3]), table, ws, window=1)
+    torch.cuda.synchronize()
+    assert torch.equal(k[2, 0, 3], rows[0, 0].to(torch.bfloat16))
+    want = (rows[0] * 2).to(torch.bfloat16).float().expand(4, 64)   # one position: its value, up to the split of p = 1 (exact)
+    assert torch.equal(out[0], want)
+
+
+FRESH = """
+import torch
+from paper_2410_23668_b200 import binding as kl
+c = kl.PagedCache.allocate(8, 2, 16, 128, kl.KL_KV_E4M3, bounds=True)
+pos, table = torch.tensor([40], dtype=torch.int32, device="cuda"), torch.tensor([[3, 1, 0]], dtype=torch.int32, device="cuda")
+k, q = torch.randn(1, 2, 128, device="cuda"), torch.randn(1, 8, 128, device="cuda")
+ws = torch.empty(kl.kl_paged_workspace_bytes(c, 8, 1, 3), dtype=torch.uint8, device="cuda")
+sel, out = torch.zeros(1, 2, 2, dtype=torch.int32, device="cuda"), torch.zeros(1, 8, 128, device="cuda")
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    st = torch.cuda.current_stream()
+    kl.kl_paged_append(c, k, k, pos, table, stream=st)
+    kl.kl_paged_select(c, q, pos, table, sel, ws, stream=st)
+    kl.kl_paged_attention(c, q, out, pos, table, ws, selected=sel, stream=st)
+g.replay()
+torch.cuda.synchronize()
+a, b = out.clone(), torch.zeros_like(out)
+kl.kl_paged_attention(c, q, b, pos, table, ws, selected=sel)
+torch.cuda.synchronize()
+assert torch.equal(a, b) and bool(a.abs().max() > 0) and sel.tolist() == [[[0, 2], [0, 2]]]
+print("fresh ok")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    import subprocess
+    import sys
+    from pathlib import Path
+    r = subprocess.run([sys.executable, "-c", FRESH], capture_output=True, text=True, timeout=300, cwd=Path(__file__).resolve().parent.parent)
+    assert r.returncode == 0 and "fresh ok" in r.stdout, r.stderr[-2000:]
+
+
 def test_attention_same_result_every_time():
     c = ref.Cache(700, 4, 16, 128, True, seed=61)
     table = ref.scattered_table([9000, 1200], 16, 700, seed=62)
