@@ -164,6 +164,11 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // the grid belongs to the sequence s with base(s) <= u < base(s + 1), base(s) = row_starts[s] / page + 2 s, and is its
 // page number u - base(s) (blocks without a page leave).  hd / 8 lanes share a row, eight columns each; half of the
 // lane groups take keys, the other half values.
+// Per row and head: largest magnitude over the lanes (as whole numbers: the bits of a float), the exponent from its bits, one
+// multiplication by a power of two per element (exact), rounding by the conversion instruction.
+// Measured, 8 kv heads of 128: one bf16 row 2.3 us (launch and a chain of three loads); 8191 bf16 rows to e4m3 16.3 us, 48 % of
+// the copy rate: the quantising itself (about 85 instructions per eight elements of a key, with its bounds) takes as long as
+// the memory does, and a block waits for its sequence, its page and its rows in turn.
 constexpr int PW_THREADS = 128;   // 8191 e4m3 rows, pages of 64: 16.3 us; 256 threads 17.6, 64 threads 25.0
 template <class T, int HD, bool FP8>
 __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
@@ -359,7 +364,8 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
 // Read back.  A block walks over chunks of R rows (as many as make PR_ITEMS 16-byte pieces).  R threads look up where the rows
 // of the next chunk lie -- a chain of dependent loads: sequence, position, page -- while the block copies this chunk's.  hd / 8
 // lanes share a (row, head, K or V), eight columns each: 16 bytes of a bf16 output, so that a warp's stores are contiguous
-// (16 columns of an e4m3 row per lane, 16-byte loads but 32-byte strides between the stores, were slower).
+// (16 columns of an e4m3 row per lane, 16-byte loads but 32-byte strides between the stores: 88 instead of 79 us).
+// Measured: 65537 e4m3 rows of 8 x 128 to bf16, 404 MB in all, 79 us, 79 % of the copy rate; 4096 bf16 rows 9.9 us.
 constexpr int PR_UNROLL = 4;   // pieces a lane has in flight (eight: no faster for e4m3, 13.2 instead of 9.9 us for 4096 bf16 rows)
 constexpr uint32_t PR_ITEMS = 4096;
 constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in shared memory
@@ -557,14 +563,15 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 // front of it busy for five times as long as reading the bounds takes).
 //   max(q lo, q hi) = min(q, 0) lo + max(q, 0) hi: with the bounds [lo | hi] of a page as a row of 2 hd numbers and
 //   [min(q, 0) | max(q, 0)] as columns it is one matrix product, pages x heads.  16 pages are the rows of mma.m16n8k16, up to
-//   eight heads its columns; the rows go from memory straight into the operand's registers (the order of the columns is
-//   free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
-//   all tiles of 16 pages and brings them in through a ring of its own in shared memory (rows loaded straight into registers, two
-//   blocks per SM, left a third of the memory's rate unused).  Written per page: the score and a bound of its error.
+//   eight heads its columns (the order of the 2 hd terms is free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
+//   all tiles of 16 pages and brings them in through a ring of its own in shared memory.  Written per page: the score and a bound
+//   of its error.
+// Measured: 397 thousand (page, head) pairs of 512 bytes, eight query heads each, 40.5 us (5.0 TB/s, what the kernel needs to
+// start and end included), 42.8 with rows loaded straight into registers.
 // Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
-// magnitudes (twice what the 32-bit accumulators show), and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32
-// queries also lose 2^-16 of themselves.  Taken: 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest
-// bound; infinite where a score or bound is not finite.
+// magnitudes, and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32 queries also lose 2^-16 of themselves.  Taken:
+// 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest bound, of which the errors seen (random, widely
+// spread, equal and cancelling terms) stay below 8 %; infinite where a score or bound is not finite.
 // The number of the larger magnitude, bf16 by bf16 (NaN is left out: it makes the score NaN).
 __device__ __forceinline__ uint32_t ps_larger(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -761,7 +768,7 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
 //   3. The chosen pages are put in order by a prefix sum over groups of 32.
 // The keys lie in shared memory (SMEM), or, beyond PT_KEYS pages, in the workspace.  A block's time is latency -- barriers, and
 // fetching its own instructions, each of which runs a few times only -- so the loops are not unrolled (eight keys per thread in
-// registers and everything unrolled took twice as long).
+// registers and everything unrolled took twice as long).  Measured: 5 us for 1024 pages, 4 to 10 us for 4096.
 constexpr int PT_THREADS = 512;
 constexpr uint32_t PT_LIST = 128, PT_KEYS = 16384;
 template <bool SMEM>
@@ -1150,6 +1157,10 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
 //   * Pages are looked up in units of UR rows (16 where the page size is a multiple of 16, else 4), one per lane, a batch of
 //     32 ahead of the copies.
+// What bounds it: bf16 caches, memory (32 x 4096 positions, 537 MB: 90 us, 93 % of the copy rate); e4m3 caches, half memory and
+// half instructions (32 sequences, 433 thousand positions, eight query heads per kv head, 894 MB: 162 us, 86 %: of some 800
+// instructions per 32 positions the conversions to f16 are a quarter); short calls, latency (1 x 333 positions: 9.4 us --
+// lengths, look-ups and first rows one after another 3 us, two tiles 1 us, joining 1 us, the merge kernel 3 us).
 template <int HD, bool FP8, int UR, bool EX>
 __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_kernel(const PagedView c, const PagedAttn a) {
     using Cfg = PaCfg<HD, FP8, EX>;
@@ -1725,7 +1736,9 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
 }
 
 // Joins the partial results of the pairs that several blocks of kl_paged_attn_kernel share, in the order of the blocks.
-// Block (b, h): head h of the pair that begins in block b and goes on in b + 1, if there is one.
+// Block (b, h): head h of the pair that begins in block b and goes on in b + 1, if there is one.  Latency: two rounds of loads,
+// about 3 us behind the last block of the attention kernel.  (Joining in the last block to arrive would save a launch, but
+// needs counters that start at zero, which no workspace of the caller's guarantees.)
 constexpr int PA_MERGE_THREADS = 128;
 constexpr int PA_MAX_BLOCKS = 256;
 __global__ void __launch_bounds__(PA_MERGE_THREADS) kl_paged_merge_kernel(const PagedView c, const PagedAttn a) {
