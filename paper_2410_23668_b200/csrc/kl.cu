@@ -1646,8 +1646,9 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
             if ((rc = kl_paged_select(&layers[l], &seqs, h->bq, KL_F32, p.QD, p.nq, 1, 1, n_select, selected, ws, y.ops, p.status, st)) != KL_OK) return rc;
             h->launches += 2;
         }
-        if ((rc = paged_attention_operand(&layers[l], &seqs, h->bq, h->bxop[1], p.nq, selected, n_select, ws, y.ops, p.status, st)) != KL_OK) return rc;
-        h->launches += 2;
+        uint64_t made = 0;
+        if ((rc = paged_attention_operand(&layers[l], &seqs, h->bq, h->bxop[1], p.nq, selected, n_select, ws, y.ops, p.status, &made, st)) != KL_OK) return rc;
+        h->launches += made;
         if ((rc = launch_bgemm(h, 1, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;
         KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.g2 + lo, 0, p.H, h->bxop[0], h->bssq, p.status);
         if ((rc = launch_bgemm(h, 2, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;

@@ -189,6 +189,13 @@ kl_status launch_attn_hd(const PagedView& v, const PagedAttn& a, int blocks, voi
     if (ex) return whole ? launch_attn_as<HD, FP8, 16, true>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, true>(v, a, blocks, stream);
     return whole ? launch_attn_as<HD, FP8, 16, false>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, false>(v, a, blocks, stream);
 }
+// Positions per tile of the kernel that a call takes.
+uint32_t attn_tile(const PagedView& v, uint32_t out_mode) {
+    const bool ex = out_mode != PA_BF16;
+    if (v.hd == 64) return v.fp8 ? PaCfg<64, true, false>::TP : PaCfg<64, false, false>::TP;
+    if (v.hd == 128) return v.fp8 ? (ex ? PaCfg<128, true, true>::TP : PaCfg<128, true, false>::TP) : PaCfg<128, false, false>::TP;
+    return v.fp8 ? PaCfg<256, true, false>::TP : PaCfg<256, false, false>::TP;
+}
 kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
     if (v.hd == 64) return v.fp8 ? launch_attn_hd<64, true>(v, a, blocks, stream) : launch_attn_hd<64, false>(v, a, blocks, stream);
     if (v.hd == 128) return v.fp8 ? launch_attn_hd<128, true>(v, a, blocks, stream) : launch_attn_hd<128, false>(v, a, blocks, stream);
@@ -199,7 +206,7 @@ kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* 
 kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type, uint32_t out_mode,
                         int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale_log2, uint32_t window,
                         const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
-                        int32_t* status_d, void* stream) {
+                        int32_t* status_d, uint64_t* launches, void* stream) {
     if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
     const AttnSpace sp = attn_space(cache->head_dim);
     if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
@@ -226,8 +233,15 @@ kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     a.head = (float*)(ws + sp.head);
     a.head_ml = (float*)(ws + sp.head_ml);
     a.meta = (int4*)(ws + sp.meta);
+    // the longest a pair can be, by the page table, the page list and the window
+    uint64_t most = (uint64_t)seqs->table_pages * cache->page_size;
+    if (selected_d && (uint64_t)n_select * cache->page_size < most) most = (uint64_t)n_select * cache->page_size;
+    if (!selected_d && window && (uint64_t)window + 64 < most) most = (uint64_t)window + 64;   // a window may begin inside a tile
+    const bool many = (uint64_t)seqs->n_seqs * cache->n_kv_heads * a.HT >= (uint64_t)blocks;
+    a.whole_pairs = most <= (uint64_t)(many ? PA_WHOLE_MANY : PA_WHOLE_FEW) * attn_tile(v, out_mode);
+    if (launches) *launches = a.whole_pairs ? 1 : 2;
     const kl_status rc = launch_attn(v, a, blocks, stream);
-    if (rc != KL_OK) return rc;
+    if (rc != KL_OK || a.whole_pairs) return rc;
     return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
 }
 
@@ -241,10 +255,10 @@ kl_status paged_check(const kl_paged_cache* cache, const kl_paged_seqs* seqs) {
 
 kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const float* q_d, __nv_bfloat16* operand_d,
                                   uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
-                                  size_t workspace_bytes, int32_t* status_d, void* stream) {
+                                  size_t workspace_bytes, int32_t* status_d, uint64_t* launches, void* stream) {
     const int64_t width = (int64_t)n_q_heads * cache->head_dim;
     return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, selected_d, n_select, nullptr, workspace_d,
-                         workspace_bytes, status_d, stream);
+                         workspace_bytes, status_d, launches, stream);
 }
 }  // namespace kl
 
@@ -340,7 +354,7 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     if (!(scale < INFINITY)) return KL_ERR_INVALID_ARG;
     const float scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
     return run_attention(cache, seqs, q_d, out_d, q_type, q_type == KL_F32 ? PA_F32 : PA_BF16, q_row_stride, out_row_stride, n_q_heads, scale_log2,
-                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, stream);
+                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, nullptr, stream);
 }
 
 }  // extern "C"

@@ -1034,6 +1034,7 @@ struct PagedAttn {
     const int32_t* selected;        // [n_seqs][nkv][n_select] or null
     uint32_t n_select;
     float* lse;                     // or null
+    uint32_t whole_pairs;           // 1: no pair is shared between blocks (and kl_paged_merge_kernel does not follow)
     // workspace: partial results, one record = [8 heads][hd] sums and [8 heads] (maximum, sum)
     float *part, *part_ml;          // [blocks][2]: the pair that began in an earlier block, the pair that goes on in the next one
     float *head, *head_ml;          // [blocks][warps]: a warp's first pair when it began in an earlier warp
@@ -1114,6 +1115,14 @@ struct PaCfg {
     static_assert(ST >= 2 && SMEM <= 232448, "ring");
 };
 
+// Short pairs are not shared between blocks, which makes the merge kernel unnecessary (3 us on the device, 3 us on the host) but
+// leaves a pair to one block: up to PA_WHOLE_FEW tiles always (one sequence, 8 kv heads of 128, bf16: 256 positions 8.3 us
+// against 8.8 shared, 512 9.8 against 9.0, 1024 12.3 against 9.4), up to PA_WHOLE_MANY tiles where there are as many
+// pairs as blocks (32 sequences: 512 positions 14.3 against 17.2, 1024 28.6 against 31.9; 128 sequences 54.6 against 58.6).  Longer
+// ones are shared although 32 x 2048 would gain 4 us too: lengths are not known on the host, and one long sequence among
+// short ones would leave its pairs to a block each.
+constexpr uint32_t PA_WHOLE_FEW = 24, PA_WHOLE_MANY = 64;
+
 // Positions of sequence s that take part, as tiles.
 struct PaSeq {
     uint32_t len, lo;   // positions [lo, len)
@@ -1159,8 +1168,8 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     32 ahead of the copies.
 // What bounds it: bf16 caches, memory (32 x 4096 positions, 537 MB: 90 us, 93 % of the copy rate); e4m3 caches, half memory and
 // half instructions (32 sequences, 433 thousand positions, eight query heads per kv head, 894 MB: 162 us, 86 %: of some 800
-// instructions per 32 positions the conversions to f16 are a quarter); short calls, latency (1 x 333 positions: 9.4 us --
-// lengths, look-ups and first rows one after another 3 us, two tiles 1 us, joining 1 us, the merge kernel 3 us).
+// instructions per 32 positions the conversions to f16 are a quarter); short calls, latency (1 x 333 positions: 8.7 us --
+// launch and the prefix of the lengths, look-ups, first rows and joining one after another, each a microsecond or two).
 template <int HD, bool FP8, int UR, bool EX>
 __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_kernel(const PagedView c, const PagedAttn a) {
     using Cfg = PaCfg<HD, FP8, EX>;
@@ -1201,12 +1210,30 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
 
     const uint32_t blocks = (uint32_t)min((uint64_t)gridDim.x, (W + PA_MIN_TILES - 1u) / PA_MIN_TILES);   // blocks at work
     if (blockIdx.x >= blocks) {
-        if (tid == 0u) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0u && !a.whole_pairs) a.meta[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     // block b takes tiles [share * b + min(b, over), ...): the first `over` blocks one more than the others
     const uint64_t share = pg_div(W, blocks), over = W - share * blocks;
-    const uint64_t b_lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), b_n = share + (blockIdx.x < over ? 1u : 0u);
+    uint64_t b_lo = share * blockIdx.x + min((uint64_t)blockIdx.x, over), b_n = share + (blockIdx.x < over ? 1u : 0u);
+    if (a.whole_pairs) {   // both ends move up to the start of a pair
+        auto up = [&](uint64_t x) {
+            if (x >= W) return W;
+            const uint32_t i = pg_find<NW>(pre, x);
+            uint64_t rem = x - pre[i];
+            uint32_t s = i * per, nt = pa_seq<TP>(c, a, length(s)).nt;
+            while (rem >= (uint64_t)nt * PH) {
+                rem -= (uint64_t)nt * PH;
+                nt = pa_seq<TP>(c, a, length(++s)).nt;
+            }
+            const uint32_t into = (uint32_t)(rem - pg_div(rem, nt) * nt);
+            return into ? x + nt - into : x;
+        };
+        const uint64_t to = up(b_lo + b_n);
+        b_lo = up(b_lo);
+        b_n = to - b_lo;
+        if (b_n == 0u) return;
+    }
     const uint64_t w_n = pg_div(b_n, NW), w_over = b_n - w_n * NW;
     const uint64_t lo = b_lo + w_n * warp + min((uint64_t)warp, w_over), hi = lo + w_n + (warp < w_over ? 1u : 0u);
 
@@ -1732,7 +1759,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             }
         }
     }
-    if (tid == 0u) a.meta[blockIdx.x] = meta;
+    if (tid == 0u && !a.whole_pairs) a.meta[blockIdx.x] = meta;
 }
 
 // Joins the partial results of the pairs that several blocks of kl_paged_attn_kernel share, in the order of the blocks.

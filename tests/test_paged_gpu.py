@@ -301,6 +301,31 @@ def test_attention_many_sequences_and_batch_order():
     check_attention(c, q, torch.tensor(lengths, dtype=torch.int32) - 1, table)
 
 
+@pytest.mark.parametrize("e4m3,dtype,hd,nq,nkv,page,lengths", [
+    (False, torch.bfloat16, 128, 32, 8, 16, [333]),
+    (True, torch.float32, 128, 10, 1, 4, [1, 100, 0, 700]),
+    (True, torch.bfloat16, 64, 8, 8, 64, [(37 * i) % 1000 for i in range(40)]),     # more pairs than blocks of the grid
+    (False, torch.float32, 256, 3, 3, 8, [(53 * i) % 400 for i in range(70)]),
+    (False, torch.bfloat16, 128, 16, 2, 16, [0, 0, 1200, 3, 0]),
+])
+@pytest.mark.parametrize("selected", [False, True])
+def test_attention_wider_tables(e4m3, dtype, hd, nq, nkv, page, lengths, selected):
+    """The width of the table, or of the page list, decides whether blocks share a (sequence, head) pair: both ways are right."""
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, nkv, page, hd, e4m3, seed=61)
+    g = torch.Generator().manual_seed(62)
+    q = (torch.randn(len(lengths), nq, hd, generator=g) * (0.02 if e4m3 else 1.0)).to(dtype).cuda()
+    for extra in (0, 16384 // page):
+        table = ref.scattered_table(lengths, page, n_pages, seed=63, extra=extra)
+        sel = None
+        if selected:   # every third page, then fillers up to the table's width
+            sel = torch.full((len(lengths), nkv, table.shape[1]), -1, dtype=torch.int32)
+            for i, x in enumerate(lengths):
+                pages = list(range(0, -(-x // page), 3))
+                sel[i, :, :len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        check_attention(c, q, torch.tensor(lengths, dtype=torch.int32) - 1, table, selected=sel)
+
+
 def test_attention_many_more_sequences_than_threads():
     """Lengths beyond those kept in shared memory, several sequences per thread of the prefix sum, three of four empty."""
     page, hd, n = 16, 64, 2100
