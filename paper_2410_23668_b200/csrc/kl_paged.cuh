@@ -571,7 +571,8 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 // Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
 // magnitudes, and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32 queries also lose 2^-16 of themselves.  Taken:
 // 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest bound, of which the errors seen (random, widely
-// spread, equal and cancelling terms) stay below 8 %; infinite where a score or bound is not finite.
+// spread, equal and cancelling terms) stay below 8 %; infinite where a score or bound is not finite, and below 2^-100: numbers
+// under 2^-126 have fewer bits (a rest of a query is off by up to 2^-134), which the bound does not count.
 // The number of the larger magnitude, bf16 by bf16 (NaN is left out: it makes the score NaN).
 __device__ __forceinline__ uint32_t ps_larger(uint32_t a, uint32_t b) {
     uint32_t r;
@@ -746,8 +747,10 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
             const uint32_t p = cur.t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
             const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
             const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? 0x1p-14f : 0x1p-16f);
-            // (infinite where nothing is known: 0 * infinity, a score that is not finite)
-            if (p < cur.np) a.scores[((size_t)cur.s * c.nkv + cur.h) * c.table_pages + p] = make_float2(score, isfinite(score) && err >= 0.f ? err : INFINITY);
+            // (infinite where nothing is known: 0 * infinity, a score that is not finite, queries whose halves and products
+            // whose sums reach down to where numbers have fewer bits; zeros are exact)
+            const bool known = isfinite(score) && (q1 == 0.f || mag == 0.f ? err == 0.f : q1 >= 0x1p-100f && err >= 0x1p-100f);
+            if (p < cur.np) a.scores[((size_t)cur.s * c.nkv + cur.h) * c.table_pages + p] = make_float2(score, known ? err : INFINITY);
         }
         if (++slot == (uint32_t)ST) slot = 0;
         if (++k < hi) {
@@ -884,7 +887,8 @@ __global__ void __launch_bounds__(PT_THREADS, 2) kl_paged_topk_kernel(const Page
             if (cnt <= PT_LIST) {
 #pragma unroll 1
                 for (uint32_t i = tid; i < n; i += PT_THREADS)
-                    if (key(i) != SURE && bin_of(key(i)) == bin) list_key[atomicAdd(&list_n, 1u)] = key(i);
+                    if (key(i) != SURE && bin_of(key(i)) == bin)   // (cnt of them, unless another call writes the workspace)
+                        list_key[min(atomicAdd(&list_n, 1u), PT_LIST - 1u)] = key(i);
                 __syncthreads();
                 if (tid < cnt) {
                     const uint32_t k = list_key[tid];
@@ -1777,6 +1781,8 @@ __global__ void __launch_bounds__(PA_MERGE_THREADS) kl_paged_merge_kernel(const 
     const int4 meta = a.meta[b];
     const uint32_t s = (uint32_t)meta.y, ph = (uint32_t)meta.z, h = ph / a.HT, h0 = (ph - h * a.HT) * 8u, hh = blockIdx.y;
     if (!meta.x || h0 + hh >= a.G) return;
+    // (a workspace that another call writes meanwhile leads to wrong results, not out of bounds)
+    if (s >= c.n_seqs || h >= c.nkv || meta.w < b || meta.w >= (int)gridDim.x) return;
     const int cnt = meta.w - b + 1;   // blocks b .. meta.w
     auto slot = [&](int i) { return i == 0 ? (size_t)b * 2 + 1 : (size_t)(b + i) * 2; };
     for (int i = tid; i < cnt; i += PA_MERGE_THREADS) ml[i] = reinterpret_cast<const float2*>(a.part_ml)[slot(i) * 8 + hh];

@@ -463,6 +463,23 @@ def test_select(dtype, hd, nq, nkv, page, n_select, keep, ties):
     assert torch.equal(got.cpu(), want)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("q_power,b_power", [(-124, 0), (-130, 20), (-118, 100), (-60, -70), (-75, -75), (100, 20), (0, -133)])
+def test_select_at_the_ends_of_the_exponents(dtype, q_power, b_power):
+    """Queries, bounds and products that 16-bit halves or 32-bit sums cannot hold."""
+    hd, nq, nkv, page, n_select, count = 128, 8, 2, 16, 20, 300
+    g = torch.Generator().manual_seed(86)
+    b = (torch.randn(count, nkv, 2, hd, generator=g) * 2.0 ** (b_power // 2) * 2.0 ** (b_power - b_power // 2)).sort(2).values.to(torch.bfloat16)
+    q = (torch.randn(1, nq, hd, generator=g) * 2.0 ** (q_power // 2) * 2.0 ** (q_power - q_power // 2)).to(dtype)
+    table = ref.scattered_table([count * page], page, count, seed=87)
+    cache = kl.PagedCache(None, None, bounds=b.cuda(), page_size=page, kv_type=kl.KL_KV_BF16)
+    ws = torch.empty(kl.kl_paged_workspace_bytes(cache, nq, 1, table.shape[1]), dtype=torch.uint8, device="cuda").fill_(0xff)
+    got = torch.full((1, nkv, n_select), 99, dtype=torch.int32, device="cuda")
+    kl.kl_paged_select(cache, q.cuda(), i32([count * page - 1]), table.cuda(), got, ws, keep_first=0, keep_last=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got.cpu(), ref.select_ref(b, q, [count * page - 1], table, page, 0, 0, n_select))
+
+
 def test_select_long_table():
     """More pages than one block keeps in registers, infinite bounds, NaN bounds and -0."""
     page, hd, n_pages = 4, 64, 40000
