@@ -58,23 +58,20 @@ __device__ __forceinline__ uint32_t pg_length(const PagedView& c, uint32_t s) {
 // 64-bit division that is usually a 32-bit one (a 64-bit division is a few hundred cycles of a kernel that may last 5 us).
 __device__ __forceinline__ uint64_t pg_div(uint64_t x, uint32_t y) { return (x >> 32) == 0u ? (uint64_t)((uint32_t)x / y) : x / y; }
 
-// 2^(e - 127) of a scale byte, and its inverse for the exponents a row can have (e - 127 in [-127, 120]).
+// 2^(e - 127) of a scale byte, and its inverse for the bytes a row can have (up to 247).
 __device__ __forceinline__ float pg_scale(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x00400000u); }
-__device__ __forceinline__ float pg_inv_scale(int32_t e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
+__device__ __forceinline__ float pg_inv_scale(uint32_t e) { return __uint_as_float((254u - e) << 23); }
 
-// Scale exponent of a row whose largest finite magnitude is `big`: the smallest e >= -127 with big <= 448 * 2^e.
-// big = m * 2^k with m in [1, 2): 448 = 1.75 * 2^8, so e = k - 8, or k - 7 where m > 1.75 (the 23 fraction bits of 1.75
-// are 0x600000).  Numbers below 2^-119 all get -127.
-__device__ __forceinline__ int32_t pg_exponent(float big) {
-    const uint32_t u = __float_as_uint(big);
-    const int32_t e = (int32_t)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return e < -127 ? -127 : e;
-}
+// Scale byte of a row whose largest finite magnitude has the bits `big`: e + 127 with the smallest e >= -127 with
+// magnitude <= 448 * 2^e.  m * 2^k with m in [1, 2): 448 = 1.75 * 2^8, so e = k - 8, or k - 7 where m > 1.75 (the 23 fraction
+// bits of 1.75 are 0x600000: adding 0x1fffff to larger ones carries into the exponent).  Numbers below 2^-119 all get -127.
+__device__ __forceinline__ uint32_t pg_exponent(uint32_t big) { return (uint32_t)max((int32_t)((big + 0x1fffffu) >> 23) - 8, 0); }
 
-// Two floats to two e4m3 codes (lo in the low byte), nearest even, saturating.
-__device__ __forceinline__ uint32_t pg_to_e4m3x2(float lo, float hi) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// Four floats to four e4m3 codes (x0 in the low byte), nearest even, saturating.
+__device__ __forceinline__ uint32_t pg_to_e4m3x4(float x0, float x1, float x2, float x3) {
+    uint32_t r;
+    asm("{.reg .b16 a, b; cvt.rn.satfinite.e4m3x2.f32 a, %2, %1; cvt.rn.satfinite.e4m3x2.f32 b, %4, %3; mov.b32 %0, {a, b};}"
+        : "=r"(r) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
     return r;
 }
 // Two e4m3 codes (low 16 bits) to two halves, exact.
@@ -86,6 +83,40 @@ __device__ __forceinline__ uint32_t pg_e4m3x2_to_f16x2(uint32_t codes) {
 __device__ __forceinline__ float2 pg_f16x2_to_float2(uint32_t h) {
     const __half2 v = *reinterpret_cast<const __half2*>(&h);
     return __half22float2(v);
+}
+
+// Two bf16 at a time: the number of the larger magnitude (its sign means nothing), product, smaller and larger one.  NaN is
+// left out where the other number is none.
+__device__ __forceinline__ uint32_t pg_larger(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pg_mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pg_min_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pg_max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The smallest and the largest of three floats; NaN is left out.
+__device__ __forceinline__ float pg_min3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float pg_max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 // Eight consecutive elements to dst (16-byte aligned).
@@ -164,12 +195,14 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // the grid belongs to the sequence s with base(s) <= u < base(s + 1), base(s) = row_starts[s] / page + 2 s, and is its
 // page number u - base(s) (blocks without a page leave).  hd / 8 lanes share a row, eight columns each; half of the
 // lane groups take keys, the other half values.
-// Per row and head: largest magnitude over the lanes (as whole numbers: the bits of a float), the exponent from its bits, one
-// multiplication by a power of two per element (exact), rounding by the conversion instruction.
-// Measured, 8 kv heads of 128: one bf16 row 2.3 us (launch and a chain of three loads); 8191 bf16 rows to e4m3 16.3 us, 48 % of
-// the copy rate: the quantising itself (about 85 instructions per eight elements of a key, with its bounds) takes as long as
-// the memory does, and a block waits for its sequence, its page and its rows in turn.
-constexpr int PW_THREADS = 128;   // 8191 e4m3 rows, pages of 64: 16.3 us; 256 threads 17.6, 64 threads 25.0
+// Per row and head: largest magnitude over the lanes (as whole numbers: the bits of a float; of bf16 rows two at a time in one
+// word), the exponent from its bits, one multiplication by a power of two per element (exact), rounding by the conversion
+// instruction.
+// Measured, 8 kv heads of 128: one bf16 row 2.1 us (launch and a chain of three loads); 8191 bf16 rows to e4m3 12.7 us, 62 % of
+// the copy rate.  What bounds it is instructions (some 75 per eight elements on average, half of the time) and a block's chain
+// of sequence, page and rows; two rows at a time, bf16 pairs and 32-bit strides took it there from 16.3 us.  Rows requested
+// asynchronously through shared memory: 12.1 us at best, not kept for that.
+constexpr int PW_THREADS = 128;   // (before the steps above: 16.3 us; 256 threads 17.6, 64 threads 25.0)
 template <class T, int HD, bool FP8>
 __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
     extern __shared__ float pg_red[];   // [groups of K rows][2][hd] when the cache has bounds
@@ -211,7 +244,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append
     }
     if (pos < 0 || r1 <= r0) return;
     const uint64_t n = r1 - r0, p0 = (uint64_t)pos, p1 = p0 + n;            // positions [p0, p1)
-    const uint64_t lp = p0 / c.page + j, a0 = max(p0, lp * c.page), a1 = min(p1, (lp + 1u) * c.page);
+    const uint64_t lp = (uint64_t)((uint32_t)pos / c.page) + j, a0 = max(p0, lp * c.page), a1 = min(p1, (lp + 1u) * c.page);
     if (a0 >= a1) return;
     if (lp >= c.table_pages) {
         if (tid == 0u) pg_error(c);
@@ -225,101 +258,139 @@ __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append
     const bool is_v = grp >= GROUPS;   // the same for a whole warp
     const uint32_t g = is_v ? grp - GROUPS : grp;
     const uint32_t off0 = (uint32_t)(a0 - lp * c.page), cnt = (uint32_t)(a1 - a0), row0 = r0 + (uint32_t)(a0 - p0);
-    const int64_t src_stride = is_v ? rows.v_stride : rows.k_stride;
-    const uint8_t* src = (is_v ? rows.v : rows.k) + (int64_t)row0 * src_stride + ((size_t)h * HD + col) * sizeof(T);
+    const uint32_t src_stride = (uint32_t)(is_v ? rows.v_stride : rows.k_stride), dst_stride = (uint32_t)c.row_b;   // at most 2^31
+    const uint8_t* src = (is_v ? rows.v : rows.k) + (uint64_t)row0 * src_stride + ((size_t)h * HD + col) * sizeof(T);
     uint8_t* dst = (is_v ? c.v : c.k) + (int64_t)phys * c.page_b + (int64_t)h * c.head_b + (int64_t)off0 * c.row_b + col * (FP8 ? 1 : 2);
     uint8_t* exps = FP8 ? (is_v ? c.ve : c.ke) + ((int64_t)phys * c.nkv + h) * c.page + off0 : nullptr;
     // the page's bounds so far, requested ahead of the rows: thread t looks after columns t, t + PW_THREADS, ... of [lo | hi]
     __nv_bfloat16* bounds = c.bounds ? c.bounds + ((int64_t)phys * c.nkv + h) * 2 * HD : nullptr;
     const bool bounded = bounds && !is_v;
-    float old[512 / PW_THREADS];
+    constexpr int COLS = 2 * HD / PW_THREADS;
+    static_assert(COLS * PW_THREADS == 2 * HD, "columns");
+    float old[COLS];
     if (bounds)
 #pragma unroll
-        for (int i = 0; i < 512 / PW_THREADS; ++i) {
+        for (int i = 0; i < COLS; ++i) {
             const uint32_t t = tid + i * PW_THREADS;
-            old[i] = 0.f;
-            if (t < 2u * HD) old[i] = off0 == 0u ? (t >= (uint32_t)HD ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
+            old[i] = off0 == 0u ? (t >= (uint32_t)HD ? -INFINITY : INFINITY) : __bfloat162float(bounds[t]);
         }
-    float lo[8], hi[8];
+    // bounds of the rows seen: eight columns in 32 bits (e4m3), or two in one word as the cache holds them (bf16)
+    float lo[FP8 ? 8 : 1], hi[FP8 ? 8 : 1];
+    uint32_t lo2[FP8 ? 1 : 4], hi2[FP8 ? 1 : 4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < (FP8 ? 8 : 1); ++i) {
         lo[i] = INFINITY;
         hi[i] = -INFINITY;
     }
-    constexpr int U = sizeof(T) == 2 ? 4 : 2;   // rows a lane has in flight
+#pragma unroll
+    for (int i = 0; i < (FP8 ? 1 : 4); ++i) {
+        lo2[i] = 0x7f807f80u;
+        hi2[i] = 0xff80ff80u;
+    }
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;   // rows a lane has in flight (bf16: two 14.3 us, eight 13.1)
     for (uint32_t i0 = 0; i0 < cnt; i0 += GROUPS * U) {   // every lane of a warp takes part in the shuffles
         uint4 raw[U][sizeof(T) / 2];
 #pragma unroll
         for (int y = 0; y < U; ++y) {
-            const uint32_t i = i0 + y * GROUPS + g;
+            const uint32_t i = min(i0 + y * GROUPS + g, cnt - 1u);   // past the end the last row again, which changes no maximum
 #pragma unroll
-            for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
-                raw[y][q] = make_uint4(0u, 0u, 0u, 0u);
-                if (i < cnt) raw[y][q] = reinterpret_cast<const uint4*>(src + (int64_t)i * src_stride)[q];
-            }
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q) raw[y][q] = reinterpret_cast<const uint4*>(src + (uint64_t)i * src_stride)[q];
         }
 #pragma unroll
-        for (int y = 0; y < U; ++y) {
+        for (int y = 0; y < U; y += 2) {   // two rows at a time
             if (i0 + y * GROUPS >= cnt) break;   // the same for the whole block
-            const uint32_t i = i0 + y * GROUPS + g;
-            const bool live = i < cnt;
-            const uint4 p = raw[y][0], p2 = raw[y][sizeof(T) / 2 - 1];
-            const uint32_t w[8] = {p.x, p.y, p.z, p.w, p2.x, p2.y, p2.z, p2.w};
-            float x[8];
+            const uint32_t i[2] = {i0 + y * GROUPS + g, i0 + (y + 1) * GROUPS + g};
+            uint32_t w[2][8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) x[q] = sizeof(T) == 4 ? __uint_as_float(w[q]) : q & 1 ? bf_hi(w[q / 2]) : bf_lo(w[q / 2]);
-            uint8_t* out = dst + (int64_t)i * c.row_b;
-            if (FP8) {
-                uint32_t big = 0u;   // largest magnitude, as its bits (rows that do not exist are zeros)
-                if (sizeof(T) == 4) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) big = max(big, w[q] & 0x7fffffffu);
-                } else {
-                    const uint32_t m = 0x7fff7fffu, v = __vmaxu2(__vmaxu2(w[0] & m, w[1] & m), __vmaxu2(w[2] & m, w[3] & m));
-                    big = max(v & 0xffff0000u, v << 16);
-                }
-                if (big >= 0x7f800000u) {   // infinities and NaN do not count
-                    big = 0u;
+            for (int r = 0; r < 2; ++r) {
+                const uint4 p = raw[y + r][0], p2 = raw[y + r][sizeof(T) / 2 - 1];
+                w[r][0] = p.x; w[r][1] = p.y; w[r][2] = p.z; w[r][3] = p.w;
+                w[r][4] = p2.x; w[r][5] = p2.y; w[r][6] = p2.z; w[r][7] = p2.w;
+            }
+            auto element = [&](int r, int q) { return sizeof(T) == 4 ? __uint_as_float(w[r][q]) : q & 1 ? bf_hi(w[r][q / 2]) : bf_lo(w[r][q / 2]); };
+            if constexpr (FP8) {
+                uint32_t big[2];   // largest magnitudes, as their bits; infinities and NaN do not count
+                auto finite = [&](int r) {   // (asked for by whole warps: a branch, not instructions that are skipped one by one)
+                    uint32_t b = 0u;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const uint32_t u = __float_as_uint(x[q]) & 0x7fffffffu;
-                        if (u < 0x7f800000u) big = max(big, u);
+                        const uint32_t u = __float_as_uint(element(r, q)) & 0x7fffffffu;
+                        if (u < 0x7f800000u) b = max(b, u);
                     }
+                    return b;
+                };
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        big[r] = 0u;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) big[r] = max(big[r], w[r][q] & 0x7fffffffu);
+                        if (__any_sync(0xffffffffu, big[r] >= 0x7f800000u)) big[r] = finite(r);
+#pragma unroll
+                        for (uint32_t o = LANES / 2u; o > 0u; o >>= 1) big[r] = max(big[r], __shfl_xor_sync(0xffffffffu, big[r], o));
+                    }
+                } else {   // both rows in one word: the first in its low half
+                    const uint32_t a = pg_larger(pg_larger(w[0][0], w[0][1]), pg_larger(w[0][2], w[0][3]));
+                    const uint32_t b = pg_larger(pg_larger(w[1][0], w[1][1]), pg_larger(w[1][2], w[1][3]));
+                    uint32_t m = pg_larger(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632)) & 0x7fff7fffu;
+                    if (__any_sync(0xffffffffu, (m + 0x00800080u) & 0x80008000u)) m = finite(0) >> 16 | (finite(1) & 0xffff0000u);
+#pragma unroll
+                    for (uint32_t o = LANES / 2u; o > 0u; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    big[0] = m << 16;
+                    big[1] = m & 0xffff0000u;
                 }
+                uint32_t code[2][2];
+                float scale[2];
 #pragma unroll
-                for (uint32_t o = LANES / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-                const int32_t e = pg_exponent(__uint_as_float(big));
-                const float inv = pg_inv_scale(e);
-                uint32_t code[4];
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t e = pg_exponent(big[r]);
+                    float x[8];
+                    if constexpr (sizeof(T) == 2) {   // products by a power of two: exact, or so small that the code is zero
+                        const uint32_t inv = (254u - e) * 0x00800080u;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) code[q] = pg_to_e4m3x2(x[2 * q] * inv, x[2 * q + 1] * inv);
-                if (live) {
-                    *reinterpret_cast<uint2*>(out) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
-                    if (lane == 0u) exps[i] = (uint8_t)(e + 127);
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t t = pg_mul_bf16x2(w[r][q], inv);
+                            x[2 * q] = bf_lo(t);
+                            x[2 * q + 1] = bf_hi(t);
+                        }
+                    } else {
+                        const float inv = pg_inv_scale(e);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) x[q] = element(r, q) * inv;
+                    }
+                    code[r][0] = pg_to_e4m3x4(x[0], x[1], x[2], x[3]);
+                    code[r][1] = pg_to_e4m3x4(x[4], x[5], x[6], x[7]);
+                    scale[r] = pg_scale(e);
+                    if (i[r] < cnt) {
+                        *reinterpret_cast<uint2*>(dst + (uint64_t)i[r] * dst_stride) = make_uint2(code[r][0], code[r][1]);
+                        if (lane == 0u) exps[i[r]] = (uint8_t)e;
+                    }
                 }
                 if (bounded) {
-                    const float scale = pg_scale((uint32_t)(e + 127));
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[q]));
-                        x[2 * q] = f.x * scale;
-                        x[2 * q + 1] = f.y * scale;
+                        const uint32_t shift = 16 * (q & 1);
+                        const float2 f = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[0][q / 2] >> shift & 0xffffu));
+                        const float2 h = pg_f16x2_to_float2(pg_e4m3x2_to_f16x2(code[1][q / 2] >> shift & 0xffffu));
+                        const float x0 = f.x * scale[0], x1 = f.y * scale[0], y0 = h.x * scale[1], y1 = h.y * scale[1];
+                        lo[2 * q] = pg_min3(lo[2 * q], x0, y0);
+                        hi[2 * q] = pg_max3(hi[2 * q], x0, y0);
+                        lo[2 * q + 1] = pg_min3(lo[2 * q + 1], x1, y1);
+                        hi[2 * q + 1] = pg_max3(hi[2 * q + 1], x1, y1);
                     }
                 }
-            } else if (live) {
-                uint4 v = p;
-                if (sizeof(T) == 4) {
-                    v = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-                    x[0] = bf_lo(v.x); x[1] = bf_hi(v.x); x[2] = bf_lo(v.y); x[3] = bf_hi(v.y);
-                    x[4] = bf_lo(v.z); x[5] = bf_hi(v.z); x[6] = bf_lo(v.w); x[7] = bf_hi(v.w);
-                }
-                *reinterpret_cast<uint4*>(out) = v;
-            }
-            if (live && bounded) {
+            } else {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {   // fminf and fmaxf leave NaN out
-                    lo[q] = fminf(lo[q], x[q]);
-                    hi[q] = fmaxf(hi[q], x[q]);
+                for (int r = 0; r < 2; ++r) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = sizeof(T) == 4 ? pack_bf16(element(r, 2 * q), element(r, 2 * q + 1)) : w[r][q];
+                    if (i[r] < cnt) *reinterpret_cast<uint4*>(dst + (uint64_t)i[r] * dst_stride) = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        lo2[q] = pg_min_bf16x2(lo2[q], v[q]);
+                        hi2[q] = pg_max_bf16x2(hi2[q], v[q]);
+                    }
                 }
             }
         }
@@ -327,16 +398,16 @@ __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append
     if (!bounds) return;
     if (!is_v) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            pg_red[(g * 2u) * HD + col + q] = lo[q];
-            pg_red[(g * 2u + 1u) * HD + col + q] = hi[q];
+        for (int q = 0; q < 4; ++q) {
+            float* to = pg_red + g * 2u * HD + col + 2 * q;
+            *reinterpret_cast<float2*>(to) = FP8 ? make_float2(lo[FP8 ? 2 * q : 0], lo[FP8 ? 2 * q + 1 : 0]) : make_float2(bf_lo(lo2[FP8 ? 0 : q]), bf_hi(lo2[FP8 ? 0 : q]));
+            *reinterpret_cast<float2*>(to + HD) = FP8 ? make_float2(hi[FP8 ? 2 * q : 0], hi[FP8 ? 2 * q + 1 : 0]) : make_float2(bf_lo(hi2[FP8 ? 0 : q]), bf_hi(hi2[FP8 ? 0 : q]));
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 512 / PW_THREADS; ++i) {
+    for (int i = 0; i < COLS; ++i) {
         const uint32_t t = tid + i * PW_THREADS;
-        if (t >= 2u * HD) break;
         const bool up = t >= (uint32_t)HD;
         float x = old[i];
 #pragma unroll
@@ -573,12 +644,6 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 // 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest bound, of which the errors seen (random, widely
 // spread, equal and cancelling terms) stay below 8 %; infinite where a score or bound is not finite, and below 2^-100: numbers
 // under 2^-126 have fewer bits (a rest of a query is off by up to 2^-134), which the bound does not count.
-// The number of the larger magnitude, bf16 by bf16 (NaN is left out: it makes the score NaN).
-__device__ __forceinline__ uint32_t ps_larger(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 template <int HD>
 struct PsCfg {
     static constexpr int ROW = 4 * HD, TILE = 16 * ROW;   // bytes of a page's bounds, of a tile's
@@ -726,8 +791,8 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
                     pa_mma<false>(acc, x.z, y.z, x.w, y.w, ql[F32 ? k4 : 0][1][0], ql[F32 ? k4 : 0][1][1]);
                 }
                 if (ht == 0u) {
-                    big0 = ps_larger(ps_larger(big0, ps_larger(x.x, x.y)), ps_larger(x.z, x.w));
-                    big1 = ps_larger(ps_larger(big1, ps_larger(y.x, y.y)), ps_larger(y.z, y.w));
+                    big0 = pg_larger(pg_larger(big0, pg_larger(x.x, x.y)), pg_larger(x.z, x.w));
+                    big1 = pg_larger(pg_larger(big1, pg_larger(y.x, y.y)), pg_larger(y.z, y.w));
                 }
             }
             // (a NaN must not be lost in a maximum: it says that the score is not known)
@@ -740,8 +805,8 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
             const float u = __shfl_xor_sync(0xffffffffu, best0, o), v = __shfl_xor_sync(0xffffffffu, best1, o);
             best0 = isnan(u) || isnan(best0) ? __int_as_float(0x7fc00000) : fmaxf(best0, u);
             best1 = isnan(v) || isnan(best1) ? __int_as_float(0x7fc00000) : fmaxf(best1, v);
-            big0 = ps_larger(big0, __shfl_xor_sync(0xffffffffu, big0, o));
-            big1 = ps_larger(big1, __shfl_xor_sync(0xffffffffu, big1, o));
+            big0 = pg_larger(big0, __shfl_xor_sync(0xffffffffu, big0, o));
+            big1 = pg_larger(big1, __shfl_xor_sync(0xffffffffu, big1, o));
         }
         if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
             const uint32_t p = cur.t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
