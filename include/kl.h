@@ -448,7 +448,8 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
 
 /* One decode step of a batch on a paged cache: kl_decode_step's batched tensor-core path (kl_set_batched_path; the same
  * projections, one launch per operator) with kl_paged_append, kl_paged_select and kl_paged_attention in the place of the
- * contiguous cache's append and attention.  Sequences join, leave and share pages by their page table alone.
+ * contiguous cache's append and attention.  Sequences join, leave and share pages by their page table alone (all but the page
+ * that holds the newest position, which this step writes; pad a batch with empty slots).
  *   layers         HOST array of n_layers descriptors (copied); all with the model's heads and one page_size
  *   page_table_d   [batch][table_stride], table_pages entries usable: positions 0 .. table_pages * page_size - 1 (max_ctx of the
  *                  handle does not matter here); the table serves every layer

@@ -436,7 +436,7 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
 // of the next chunk lie -- a chain of dependent loads: sequence, position, page -- while the block copies this chunk's.  hd / 8
 // lanes share a (row, head, K or V), eight columns each: 16 bytes of a bf16 output, so that a warp's stores are contiguous
 // (16 columns of an e4m3 row per lane, 16-byte loads but 32-byte strides between the stores: 88 instead of 79 us).
-// Measured: 65537 e4m3 rows of 8 x 128 to bf16, 404 MB in all, 79 us, 79 % of the copy rate; 4096 bf16 rows 9.9 us.
+// Measured: 65537 e4m3 rows of 8 x 128 to bf16, 404 MB in all, 78 us, 80 % of the copy rate; 4096 bf16 rows 9.9 us.
 constexpr int PR_UNROLL = 4;   // pieces a lane has in flight (eight: no faster for e4m3, 13.2 instead of 9.9 us for 4096 bf16 rows)
 constexpr uint32_t PR_ITEMS = 4096;
 constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in shared memory
@@ -479,6 +479,7 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_read_kernel(const Page
         at = (int64_t)phys * c.page_b + (int64_t)off * c.row_b;
         ex = (int64_t)phys * c.nkv * c.page + off;
     };
+    const uint32_t head_b = (uint32_t)c.head_b, k_stride = (uint32_t)rows.k_stride, v_stride = (uint32_t)rows.v_stride;   // at most 2^31
     const uint64_t step = (uint64_t)gridDim.x * R;
     uint64_t row0 = (uint64_t)blockIdx.x * R;
     int64_t at, ex;
@@ -500,8 +501,8 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_read_kernel(const Page
                 if (from >= 0) {
                     const bool is_v = i >= c.nkv;
                     const uint32_t h = is_v ? i - c.nkv : i;
-                    x[u] = *reinterpret_cast<const Piece*>((is_v ? c.v : c.k) + from + (int64_t)h * c.head_b + col * (FP8 ? 1 : 2));
-                    if (FP8) e[u] = (is_v ? c.ve : c.ke)[exp_s[buf][r] + (int64_t)h * c.page];
+                    x[u] = *reinterpret_cast<const Piece*>((is_v ? c.v : c.k) + from + (uint64_t)h * head_b + col * (FP8 ? 1 : 2));
+                    if (FP8) e[u] = (is_v ? c.ve : c.ke)[exp_s[buf][r] + h * c.page];
                 }
                 i += di;
                 r += dr;
@@ -514,8 +515,8 @@ __global__ void __launch_bounds__(PG_THREADS, 4) kl_paged_read_kernel(const Page
             for (int u = 0; u < PR_UNROLL; ++u)
                 if (to_r[u] != 0xffffffffu) {
                     const bool is_v = to_i[u] >= c.nkv;
-                    const int64_t row = (int64_t)(row0 + to_r[u]);
-                    T* out = reinterpret_cast<T*>(is_v ? rows.v + row * rows.v_stride : rows.k + row * rows.k_stride) +
+                    const uint32_t row = (uint32_t)row0 + to_r[u];
+                    T* out = reinterpret_cast<T*>((is_v ? rows.v : rows.k) + (uint64_t)row * (is_v ? v_stride : k_stride)) +
                              (is_v ? to_i[u] - c.nkv : to_i[u]) * HD + col;
                     float f[8];
                     if constexpr (FP8) {
