@@ -440,7 +440,8 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
  * and a selection combine.  q and out: [n_seqs][n_q_heads][head_dim] of q_type; scale <= 0: 1 / sqrt(head_dim).  lse_d
  * (optional): fp32 [n_seqs][n_q_heads], the natural logarithm of the softmax's denominator sum_p exp(scale * q . k_p), which is
  * what joining the results of several caches needs.  A sequence without positions to attend to gets zeros, and -inf.
- * n_q_heads is a multiple of n_kv_heads, any group size. */
+ * n_q_heads is a multiple of n_kv_heads, any group size.  Scores, the softmax and all sums are held in 32 bits; in the two
+ * products fp32 queries and the probabilities take part with 24 bits (KL_KV_BF16) or 22 (KL_KV_E4M3). */
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,
                              int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
                              const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,

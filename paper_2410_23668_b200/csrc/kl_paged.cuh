@@ -1122,7 +1122,8 @@ __device__ __forceinline__ uint32_t pa_pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Two numbers rounded to 16 bits (f16 with an e4m3 cache, bf16 else), and what that leaves of them.
+// Two numbers rounded to 16 bits (f16 with an e4m3 cache, bf16 else), what that leaves of them, and what the two leave where
+// they are bf16 (eight bits each: 24 with a third).
 template <bool FP8>
 __device__ __forceinline__ uint32_t pa_round(float x0, float x1) {
     return FP8 ? pa_pack_f16(x0, x1) : pack_bf16(x0, x1);
@@ -1132,6 +1133,9 @@ __device__ __forceinline__ uint32_t pa_rest(float x0, float x1, uint32_t hi) {
     if (!FP8) return pack_bf16(x0 - bf_lo(hi), x1 - bf_hi(hi));
     const float2 f = pg_f16x2_to_float2(hi);
     return pa_pack_f16(x0 - f.x, x1 - f.y);
+}
+__device__ __forceinline__ uint32_t pa_rest2(float x0, float x1, uint32_t hi, uint32_t lo) {   // both differences are exact
+    return pack_bf16(x0 - bf_lo(hi) - bf_lo(lo), x1 - bf_hi(hi) - bf_hi(lo));
 }
 // Two neighbouring columns (d even) of query head hq of sequence s.
 __device__ __forceinline__ void pa_store2(const PagedView& c, const PagedAttn& a, uint32_t s, uint32_t hq, uint32_t d, float v0, float v1) {
@@ -1181,7 +1185,10 @@ struct PaCfg {
     static constexpr int TILE = TP * ROW;                    // bytes of a K (or V) tile
     static constexpr int RING = 204800 / (NW * 2 * TILE);
     static constexpr int ST = RING > 8 ? 8 : RING;           // tiles of a warp's ring
-    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 2 * TP + TP) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256;
+    // fp32 queries and a bf16 cache: the queries' third parts, 8 bytes of a lane per 16 columns, lie in shared memory where
+    // registers do not suffice (32 x 4096, 16 heads of 256: 178 us spilled, 101 us so, 100 us without a third part)
+    static constexpr bool QM = EX && !FP8 && HD == 256;
+    static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 2 * TP + TP) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256 + (QM ? NW * 32 * HD / 2 : 0);
     static_assert(ST >= 2 && SMEM <= 232448, "ring");
 };
 
@@ -1229,8 +1236,9 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     exchange between lanes.  Positions are the 16 rows of mma.m16n8k16, the heads its eight columns:
 //     S[pos, head] = K . Q^T, O^T[d, head] += V^T . P; P leaves the score accumulators in 16-bit pairs and reaches the
 //     layout of a B operand with one movmatrix per 8 x 8 block.  What rounding p to 16 bits leaves of it (and, with fp32
-//     queries: EX, what it leaves of q) enters as a second product, so that results are as good as 32-bit ones; for e4m3 caches
-//     the second product costs 2 % of the time.
+//     queries: EX, what it leaves of q) enters as a second product, and, where the 16 bits are bf16, what that leaves as a
+//     third: 22 bits with an e4m3 cache (two f16), 24 with a bf16 one.  The second product costs e4m3 caches 2 % of the time,
+//     the third one bf16 caches 0.5 % (fp32 queries 2 %; of a short call 0.2 and 0.7 us).
 //   * e4m3 rows become f16 (exact) on the way to the tensor cores.  Their scales are powers of two: 2^(e_k - 127) multiplies
 //     the score, 2^(e_v - 127) the probability.  The weighted probabilities w = p * 2^(e_v - 127) have a reference of
 //     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
@@ -1458,7 +1466,9 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             }
         };
         // ---- state of the pair under way.  Queries: head g; scores and results: heads 2j and 2j + 1
-        uint32_t qh[NMMA][2], ql[EX ? NMMA : 1][2];
+        constexpr bool THIRD = EX && !FP8;
+        uint32_t qh[NMMA][2], ql[EX ? NMMA : 1][2], qm[THIRD && !Cfg::QM ? NMMA : 1][2];
+        uint2* qm_s = reinterpret_cast<uint2*>(misc + 64) + warp * (NMMA * 32) + lane;   // (Cfg::QM)
         float o[NMMA][4], m[2], l[2], mw[2], qs[2];
         constexpr int PIECE = FP8 ? 16 : 8;   // consecutive columns of a lane per 16-byte piece of a row
         uint32_t raw[NMMA][EX ? 4 : 2];       // the lane's columns of query head g, as they lie in memory
@@ -1501,13 +1511,22 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             qs[0] = __shfl_sync(0xffffffffu, mul, j * 8u);
             qs[1] = __shfl_sync(0xffffffffu, mul, j * 8u + 4u);
 #pragma unroll
-            for (int i = 0; i < NMMA; ++i)
+            for (int i = 0; i < NMMA; ++i) {
+                uint32_t third[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float x0 = x[i][2 * e] * f, x1 = x[i][2 * e + 1] * f;
                     qh[i][e] = pa_round<FP8>(x0, x1);
                     if (EX) ql[i % (EX ? NMMA : 1)][e] = pa_rest<FP8>(x0, x1, qh[i][e]);
+                    if (THIRD) third[e] = pa_rest2(x0, x1, qh[i][e], ql[i % (EX ? NMMA : 1)][e]);
                 }
+                if (Cfg::QM) {
+                    qm_s[i * 32] = make_uint2(third[0], third[1]);
+                } else if (THIRD) {
+                    qm[i % (THIRD && !Cfg::QM ? NMMA : 1)][0] = third[0];
+                    qm[i % (THIRD && !Cfg::QM ? NMMA : 1)][1] = third[1];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < NMMA; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
             m[0] = m[1] = mw[0] = mw[1] = -INFINITY;
@@ -1582,6 +1601,11 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                             const int i = (q * 2 + x) % NMMA;
                             pa_mma<FP8>(sc[t], wa[2 * x], ya[2 * x], wa[2 * x + 1], ya[2 * x + 1], qh[i][0], qh[i][1]);
                             if (EX) pa_mma<FP8>(sc[t], wa[2 * x], ya[2 * x], wa[2 * x + 1], ya[2 * x + 1], ql[i % (EX ? NMMA : 1)][0], ql[i % (EX ? NMMA : 1)][1]);
+                            if (THIRD) {
+                                uint2 w3 = make_uint2(qm[i % (THIRD && !Cfg::QM ? NMMA : 1)][0], qm[i % (THIRD && !Cfg::QM ? NMMA : 1)][1]);
+                                if (Cfg::QM) w3 = qm_s[i * 32];   // the lane's own
+                                pa_mma<FP8>(sc[t], wa[2 * x], ya[2 * x], wa[2 * x + 1], ya[2 * x + 1], w3.x, w3.y);
+                            }
                         }
                     }
                 }
@@ -1657,8 +1681,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             for (int t = 0; t < NS; ++t) {
                 const uint32_t h0 = pa_round<FP8>(p[4 * t], p[4 * t + 1]), h1 = pa_round<FP8>(p[4 * t + 2], p[4 * t + 3]);
                 const uint32_t b0 = movmatrix_trans(h0), b1 = movmatrix_trans(h1);
-                const uint32_t c0 = movmatrix_trans(pa_rest<FP8>(p[4 * t], p[4 * t + 1], h0));
-                const uint32_t c1 = movmatrix_trans(pa_rest<FP8>(p[4 * t + 2], p[4 * t + 3], h1));
+                const uint32_t l0 = pa_rest<FP8>(p[4 * t], p[4 * t + 1], h0), l1 = pa_rest<FP8>(p[4 * t + 2], p[4 * t + 3], h1);
+                const uint32_t c0 = movmatrix_trans(l0), c1 = movmatrix_trans(l1);
                 const uint32_t vs = vd + t * 16 * ROW;
                 if (FP8) {
                     constexpr int VW = HD >= 128 ? 4 : 2;            // words of a lane's piece of a row
@@ -1692,6 +1716,8 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         }
                     }
                 } else {
+                    const uint32_t e0 = movmatrix_trans(pa_rest2(p[4 * t], p[4 * t + 1], h0, l0));
+                    const uint32_t e1 = movmatrix_trans(pa_rest2(p[4 * t + 2], p[4 * t + 3], h1, l1));
                     // matrices of a load: positions 0..7 and 8..15 of two neighbouring pieces of eight columns
                     const uint32_t row = (lane >> 4) * 8u + (lane & 7u), base = vs + row * ROW, fv = (row & 1u) << 2 | ((row >> 1) & 3u);
 #pragma unroll
@@ -1700,6 +1726,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         ldmatrix_x4_trans(r, base + (((i * 2 + (lane >> 3 & 1u)) ^ fv) << 4));
                         pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], b0, b1);
                         pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], c0, c1);
+                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], e0, e1);
                     }
                 }
             }
