@@ -437,9 +437,10 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
  * sequence s -- all of them (window == 0), the last `window`, or, when selected_d is given, those of the listed pages
  * (kl_paged_select's output, or any [n_seqs][n_kv_heads][n_select] list of distinct logical pages; of a sequence with
  * fewer than n_select pages only the first entries, one per page, are looked at; a negative entry is no page).  A window
- * and a selection combine.  q and out: [n_seqs][n_q_heads][head_dim] of q_type; scale <= 0: 1 / sqrt(head_dim).  lse_d
- * (optional): fp32 [n_seqs][n_q_heads], the natural logarithm of the softmax's denominator sum_p exp(scale * q . k_p), which is
- * what joining the results of several caches needs.  A sequence without positions to attend to gets zeros, and -inf.
+ * and a selection combine; pages that lie wholly before the window are not looked up (their entries may name no page).
+ * q and out: [n_seqs][n_q_heads][head_dim] of q_type; scale <= 0: 1 / sqrt(head_dim).  lse_d (optional): fp32 [n_seqs]
+ * [n_q_heads], the natural logarithm of the softmax's denominator sum_p exp(scale * q . k_p), which is what joining the results
+ * of several caches needs.  A sequence without positions to attend to gets zeros, and -inf.
  * n_q_heads is a multiple of n_kv_heads, any group size.  Scores, the softmax and all sums are held in 32 bits; in the two
  * products fp32 queries and the probabilities take part with 24 bits (KL_KV_BF16) or 22 (KL_KV_E4M3). */
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,

@@ -1365,6 +1365,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 logical = u * UR / c.page;
                 row = u * UR - logical * c.page;
             }
+            if (logical * c.page + row + UR <= iq.lo) return;   // before the window: the page may be gone
             phys = pg_physical(c, is, logical);
             if (phys >= 0) lp = logical * c.page + row;
         };

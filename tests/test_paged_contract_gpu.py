@@ -4,7 +4,7 @@ import torch
 
 from paper_2410_23668_b200 import binding as kl, build
 from tests import paged_ref as ref
-from tests.test_paged_gpu import i32
+from tests.test_paged_gpu import check_attention, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,39 @@ def test_bf16_caches_keep_24_bits(hd, page, dtype, reach):
         tol = ((2 * (11 * s + 4) + 6 + n + 3) * 2.0 ** -24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)) * want.abs() + 1e-37
         worst = max(worst, float(((out.cpu().double() - want).abs() / tol).max()))
     assert worst <= 1.0, worst
+
+
+@pytest.mark.parametrize("e4m3,dtype,hd", [(False, torch.bfloat16, 128), (False, torch.float32, 64), (True, torch.bfloat16, 128), (True, torch.bfloat16, 64),
+                                           (True, torch.float32, 256)])
+@pytest.mark.parametrize("page", [4, 8, 16, 24])
+@pytest.mark.parametrize("listed", [False, True])
+def test_a_window_needs_no_pages_before_it(e4m3, dtype, hd, page, listed):
+    """A program that slides a window along gives back the pages behind it: their table entries name no page."""
+    nkv, nq, window = 2, 6, 50
+    positions = [180 + i for i in range(0, 2 * page + 1, max(1, page // 8))] + [20, window - 1, window]
+    lengths = [p + 1 for p in positions]
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, nkv, page, hd, e4m3, seed=1)
+    table = ref.scattered_table(lengths, page, n_pages, seed=2)
+    q = (torch.randn(len(positions), nq, hd, generator=torch.Generator().manual_seed(3)) * (0.02 if e4m3 else 1.0)).to(dtype).cuda()
+    sel = None
+    if listed:   # every page, those before the window among them
+        sel = torch.arange(table.shape[1], dtype=torch.int32).expand(len(positions), nkv, -1).contiguous()
+    first = torch.tensor([max(0, x - window) // page for x in lengths])
+    gone = torch.arange(table.shape[1])[None, :] < first[:, None]
+    assert gone.any()
+    want = check_attention(c, q, torch.tensor(positions, dtype=torch.int32), table, window=window, selected=sel)
+    got = check_attention(c, q, torch.tensor(positions, dtype=torch.int32), table.masked_fill(gone, -1), window=window, selected=sel)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_window_that_blocks_share(e4m3):
+    page, hd, nkv, nq, window = 16, 128, 2, 4, 5000
+    positions = [19999, 31, 7000]
+    lengths = [p + 1 for p in positions]
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, nkv, page, hd, e4m3, seed=4)
+    table = ref.scattered_table(lengths, page, n_pages, seed=5)
+    q = (torch.randn(3, nq, hd, generator=torch.Generator().manual_seed(6)) * (0.02 if e4m3 else 1.0)).to(torch.bfloat16).cuda()
+    check_attention(c, q, torch.tensor(positions, dtype=torch.int32), table, window=window)
