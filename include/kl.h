@@ -226,7 +226,8 @@ kl_status kl_decode_greedy_host(kl_handle* h, const int32_t* tokens_h, const int
 
 /* Sampling block, the last of the four calls per token of Section 2's looped schedule (Embedding, looped Decoder,
  * Classifier, Sampling), as greedy sampling: tokens_d[b] = argmax_v logits_d[b, v] (lowest index on ties);
- * positions_d[b] += 1. */
+ * positions_d[b] += 1.  A sequence at a negative position -- an empty slot of the batch, see kl_decode_step_paged --
+ * keeps its token and its position. */
 kl_status kl_argmax_advance(kl_handle* h, const float* logits_d, int32_t* tokens_d, int32_t* positions_d,
                             uint32_t batch, void* stream);
 
@@ -241,7 +242,7 @@ kl_status kl_argmax_advance(kl_handle* h, const float* logits_d, int32_t* tokens
  * inside the CUDA runtime routines this call uses (a symbol-address query, a memset node and a kernel launch).
  *   logits_d    [batch, vocab] fp32 on the current device
  *   tokens_d    [batch] int32, written: argmax (lowest index on ties)
- *   positions_d [batch] int32, incremented
+ *   positions_d [batch] int32, incremented; a negative one stays, and its token too
  *   batch       1..KL_STATIC_ARGMAX_MAX_BATCH; larger -> KL_ERR_TOO_LARGE, nothing is launched
  * The first call on a device looks up the array's address (with that device current): make that first call outside
  * any stream capture, before the latency-critical part of the program.  Every call on a device shares the one
@@ -456,7 +457,7 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
  *   page_table_d   [batch][table_stride], table_pages entries usable: positions 0 .. table_pages * page_size - 1 (max_ctx of the
  *                  handle does not matter here); the table serves every layer
  *   positions_d[b] as in kl_decode_step; negative: an empty slot, whose logits are finite but meaningless and whose cache is not
- *                  touched (kl_argmax_advance adds one to every position: set empty slots back)
+ *                  touched (kl_argmax_advance leaves it empty)
  *   n_select       0: attention over all positions; >= 2: over this many pages per kv head (the first and the last always
  *                  among them, chosen layer by layer; needs bounds_d)
  *   workspace_d    kl_paged_step_bytes bytes (cache: any layer's descriptor), 256-byte aligned, need not be cleared

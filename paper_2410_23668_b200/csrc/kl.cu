@@ -356,8 +356,10 @@ __global__ void __launch_bounds__(256) kl_argmax_kernel(const float* logits, uin
         for (int o = 16; o > 0; o >>= 1)
             argmax_merge(bv, bi, __shfl_xor_sync(0xffffffffu, bv, o), __shfl_xor_sync(0xffffffffu, bi, o));
         if (tid == 0) {
-            tokens[b] = (int32_t)(bi == 0xffffffffu ? 0u : bi);
-            positions[b] += 1;
+            if (positions[b] >= 0) {   // an empty slot of the batch stays one
+                tokens[b] = (int32_t)(bi == 0xffffffffu ? 0u : bi);
+                positions[b] += 1;
+            }
             tickets[b] = 0u;  // ready for the next call (calls on one handle do not overlap)
         }
     }

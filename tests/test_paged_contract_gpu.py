@@ -2,8 +2,9 @@
 import pytest
 import torch
 
-from paper_2410_23668_b200 import binding as kl, build
-from tests import paged_ref as ref
+from paper_2410_23668_b200 import binding as kl, build, inputs as gen
+from tests import helpers, paged_ref as ref
+from tests.test_paged_decode_gpu import Setup
 from tests.test_paged_gpu import check_attention, i32
 
 pytestmark = pytest.mark.gpu
@@ -88,3 +89,51 @@ def test_a_window_that_blocks_share(e4m3):
     table = ref.scattered_table(lengths, page, n_pages, seed=5)
     q = (torch.randn(3, nq, hd, generator=torch.Generator().manual_seed(6)) * (0.02 if e4m3 else 1.0)).to(torch.bfloat16).cuda()
     check_attention(c, q, torch.tensor(positions, dtype=torch.int32), table, window=window)
+
+
+@pytest.mark.parametrize("static", [False, True])
+def test_sampling_leaves_empty_slots_alone(static):
+    shape, n = gen.TINY, 5
+    logits = torch.randn(n, shape.vocab, generator=torch.Generator().manual_seed(1)).cuda()
+    tok, pos = i32([7, 8, 9, 10, 11]), i32([3, -1, 0, -2 ** 31, 2 ** 20])
+    dec = helpers.make_decoder(shape, n, 16, 0)
+    for t in range(3):
+        if static:
+            kl.kl_argmax_advance_static(logits, tok, pos, n)
+        else:
+            dec.kl_argmax_advance(logits, tok, pos, n)
+        torch.cuda.synchronize()
+        best = logits.cpu().argmax(1).tolist()
+        assert tok.tolist() == [best[0], 8, best[2], 10, best[4]]
+        assert pos.tolist() == [4 + t, -1, 1 + t, -2 ** 31, 2 ** 20 + 1 + t]
+    dec.close()
+
+
+@pytest.mark.parametrize("fill", [-1, 0])
+def test_replayed_steps_keep_empty_slots_empty(fill):
+    """A capture of the step and the sampling, replayed: an empty slot stays one, whatever its row of the page table holds."""
+    shape, contexts = gen.TINY, [30, -1, 12]
+    a, b = (Setup(shape, contexts, 16, kl.KL_KV_E4M3, n_select=3) for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    a.table[1] = fill
+    b.table[1] = -1
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        st = torch.cuda.current_stream()
+        a.step(stream=st)
+        a.dec.kl_argmax_advance(a.logits, a.tok, a.pos, 3, stream=st)
+    for t in range(4):
+        graph.replay()
+        b.step()
+        b.dec.kl_argmax_advance(b.logits, b.tok, b.pos, 3)
+        b.pos[1] = -1
+        torch.cuda.synchronize()
+        assert a.dec.kl_last_status() == 0 and b.dec.kl_last_status() == 0
+        assert a.pos.tolist() == [31 + t, -1, 13 + t]
+        for i in (0, 2):
+            assert torch.equal(a.logits[i], b.logits[i]) and a.tok[i] == b.tok[i]
+        for x, y in zip(a.caches, b.caches):
+            assert all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(x.tensors, y.tensors))
+    del graph
+    a.dec.close()
+    b.dec.close()
