@@ -1614,6 +1614,7 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
     for (uint32_t l = 0; l < p.L; ++l)
         if ((rc = paged_check(&layers[l], &seqs)) != KL_OK) return rc;
     cudaStream_t st = as_stream(stream);
+    const PagedOrder order = {stream, h->use_pdl != 0};
     h->chain_tok = nullptr;
     h->last_batch = batch;
     h->hidden_is_copy = 1;   // hidden_all holds it, for a single sequence too
@@ -1642,14 +1643,14 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
         KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.g1 + lo, 0, p.H, h->bxop[0], h->bssq, p.status);
         if ((rc = launch_bgemm(h, 0, l, h->bpart, batch, st, &a.qkv)) != KL_OK) return rc;
         KL_B_LAUNCH(kl_b_rope_rows_kernel, dim3(batch, p.nq + 2 * p.nkv), 128, a);
-        if ((rc = kl_paged_append(&layers[l], &seqs, nullptr, batch, rows, rows + (size_t)32 * p.KVD, KL_F32, p.KVD, p.KVD, p.status, st)) != KL_OK) return rc;
+        if ((rc = paged_append(&layers[l], &seqs, nullptr, batch, rows, rows + (size_t)32 * p.KVD, KL_F32, p.KVD, p.KVD, p.status, order)) != KL_OK) return rc;
         ++h->launches;
         if (n_select) {
-            if ((rc = kl_paged_select(&layers[l], &seqs, h->bq, KL_F32, p.QD, p.nq, 1, 1, n_select, selected, ws, y.ops, p.status, st)) != KL_OK) return rc;
+            if ((rc = paged_select(&layers[l], &seqs, h->bq, KL_F32, p.QD, p.nq, 1, 1, n_select, selected, ws, y.ops, p.status, order)) != KL_OK) return rc;
             h->launches += 2;
         }
         uint64_t made = 0;
-        if ((rc = paged_attention_operand(&layers[l], &seqs, h->bq, h->bxop[1], p.nq, selected, n_select, ws, y.ops, p.status, &made, st)) != KL_OK) return rc;
+        if ((rc = paged_attention_operand(&layers[l], &seqs, h->bq, h->bxop[1], p.nq, selected, n_select, ws, y.ops, p.status, &made, order)) != KL_OK) return rc;
         h->launches += made;
         if ((rc = launch_bgemm(h, 1, l, h->bpart, batch, st, &parts)) != KL_OK) return rc;
         KL_B_LAUNCH(kl_b_finish_kernel, grid_h, 256, parts, h->bx, h->bx, p.g2 + lo, 0, p.H, h->bxop[0], h->bssq, p.status);

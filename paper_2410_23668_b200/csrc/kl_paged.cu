@@ -13,17 +13,18 @@ using namespace kl;
 
 namespace {
 
-// Launch with programmatic stream serialisation (see griddep_wait): set-up overlaps the end of the stream's previous kernel.
+// With `early` a kernel is launched with programmatic stream serialisation (see griddep_wait): its set-up overlaps the end of the
+// stream's previous kernel.
 template <typename... KArgs, typename... Args>
-kl_status launch(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, void* stream, Args&&... args) {
+kl_status launch(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, PagedOrder order, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
-    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cfg.stream = reinterpret_cast<cudaStream_t>(order.stream);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].val.programmaticStreamSerializationAllowed = order.early ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(std::forward<Args>(args))...) == cudaSuccess ? KL_OK : KL_ERR_CUDA;
@@ -143,51 +144,51 @@ int attn_blocks() {
 }
 
 template <int HD>
-kl_status launch_append(int type, const PagedView& v, const PagedRows& r, dim3 grid, size_t smem, void* stream) {
+kl_status launch_append(int type, const PagedView& v, const PagedRows& r, dim3 grid, size_t smem, PagedOrder order) {
     if (v.fp8)
-        return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, true>, grid, PW_THREADS, smem, stream, v, r)
-                              : launch(kl_paged_append_kernel<__nv_bfloat16, HD, true>, grid, PW_THREADS, smem, stream, v, r);
-    return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, false>, grid, PW_THREADS, smem, stream, v, r)
-                          : launch(kl_paged_append_kernel<__nv_bfloat16, HD, false>, grid, PW_THREADS, smem, stream, v, r);
+        return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, true>, grid, PW_THREADS, smem, order, v, r)
+                              : launch(kl_paged_append_kernel<__nv_bfloat16, HD, true>, grid, PW_THREADS, smem, order, v, r);
+    return type == KL_F32 ? launch(kl_paged_append_kernel<float, HD, false>, grid, PW_THREADS, smem, order, v, r)
+                          : launch(kl_paged_append_kernel<__nv_bfloat16, HD, false>, grid, PW_THREADS, smem, order, v, r);
 }
 template <int HD>
-kl_status launch_read(int type, const PagedView& v, const PagedRows& r, dim3 grid, void* stream) {
+kl_status launch_read(int type, const PagedView& v, const PagedRows& r, dim3 grid, PagedOrder order) {
     if (v.fp8)
-        return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, true>, grid, PG_THREADS, 0, stream, v, r)
-                              : launch(kl_paged_read_kernel<__nv_bfloat16, HD, true>, grid, PG_THREADS, 0, stream, v, r);
-    return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, false>, grid, PG_THREADS, 0, stream, v, r)
-                          : launch(kl_paged_read_kernel<__nv_bfloat16, HD, false>, grid, PG_THREADS, 0, stream, v, r);
+        return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, true>, grid, PG_THREADS, 0, order, v, r)
+                              : launch(kl_paged_read_kernel<__nv_bfloat16, HD, true>, grid, PG_THREADS, 0, order, v, r);
+    return type == KL_F32 ? launch(kl_paged_read_kernel<float, HD, false>, grid, PG_THREADS, 0, order, v, r)
+                          : launch(kl_paged_read_kernel<__nv_bfloat16, HD, false>, grid, PG_THREADS, 0, order, v, r);
 }
 
 template <int HD, bool F32>
-kl_status launch_score_as(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
+kl_status launch_score_as(const PagedView& v, const PagedSelect& a, int sms, PagedOrder order) {
     using Cfg = PsCfg<HD>;
     auto* f = kl_paged_score_kernel<HD, F32>;
     static std::atomic<uint64_t> done{0};
     const kl_status rc = prepare((const void*)f, (int)Cfg::SMEM, done);
-    return rc != KL_OK ? rc : launch(f, dim3((unsigned)sms), Cfg::NW * 32, Cfg::SMEM, stream, v, a);
+    return rc != KL_OK ? rc : launch(f, dim3((unsigned)sms), Cfg::NW * 32, Cfg::SMEM, order, v, a);
 }
-kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, void* stream) {
-    if (v.hd == 64) return a.q_f32 ? launch_score_as<64, true>(v, a, sms, stream) : launch_score_as<64, false>(v, a, sms, stream);
-    if (v.hd == 128) return a.q_f32 ? launch_score_as<128, true>(v, a, sms, stream) : launch_score_as<128, false>(v, a, sms, stream);
-    return a.q_f32 ? launch_score_as<256, true>(v, a, sms, stream) : launch_score_as<256, false>(v, a, sms, stream);
+kl_status launch_score(const PagedView& v, const PagedSelect& a, int sms, PagedOrder order) {
+    if (v.hd == 64) return a.q_f32 ? launch_score_as<64, true>(v, a, sms, order) : launch_score_as<64, false>(v, a, sms, order);
+    if (v.hd == 128) return a.q_f32 ? launch_score_as<128, true>(v, a, sms, order) : launch_score_as<128, false>(v, a, sms, order);
+    return a.q_f32 ? launch_score_as<256, true>(v, a, sms, order) : launch_score_as<256, false>(v, a, sms, order);
 }
 
 template <int HD, bool FP8, int UR, bool EX>
-kl_status launch_attn_as(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
+kl_status launch_attn_as(const PagedView& v, const PagedAttn& a, int blocks, PagedOrder order) {
     using Cfg = PaCfg<HD, FP8, EX>;
     auto* f = kl_paged_attn_kernel<HD, FP8, UR, EX>;
     static std::atomic<uint64_t> done{0};
     const kl_status rc = prepare((const void*)f, (int)Cfg::SMEM, done);
     if (rc != KL_OK) return rc;
-    return launch(f, dim3((unsigned)blocks), Cfg::NW * 32, Cfg::SMEM, stream, v, a);
+    return launch(f, dim3((unsigned)blocks), Cfg::NW * 32, Cfg::SMEM, order, v, a);
 }
 template <int HD, bool FP8>
-kl_status launch_attn_hd(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
+kl_status launch_attn_hd(const PagedView& v, const PagedAttn& a, int blocks, PagedOrder order) {
     // pages are looked up in units of 16 rows where they consist of such units, else of four
     const bool whole = v.page % 16 == 0, ex = a.out_mode != PA_BF16;
-    if (ex) return whole ? launch_attn_as<HD, FP8, 16, true>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, true>(v, a, blocks, stream);
-    return whole ? launch_attn_as<HD, FP8, 16, false>(v, a, blocks, stream) : launch_attn_as<HD, FP8, 4, false>(v, a, blocks, stream);
+    if (ex) return whole ? launch_attn_as<HD, FP8, 16, true>(v, a, blocks, order) : launch_attn_as<HD, FP8, 4, true>(v, a, blocks, order);
+    return whole ? launch_attn_as<HD, FP8, 16, false>(v, a, blocks, order) : launch_attn_as<HD, FP8, 4, false>(v, a, blocks, order);
 }
 // Positions per tile of the kernel that a call takes.
 uint32_t attn_tile(const PagedView& v, uint32_t out_mode) {
@@ -196,17 +197,17 @@ uint32_t attn_tile(const PagedView& v, uint32_t out_mode) {
     if (v.hd == 128) return v.fp8 ? (ex ? PaCfg<128, true, true>::TP : PaCfg<128, true, false>::TP) : PaCfg<128, false, false>::TP;
     return v.fp8 ? PaCfg<256, true, false>::TP : PaCfg<256, false, false>::TP;
 }
-kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, void* stream) {
-    if (v.hd == 64) return v.fp8 ? launch_attn_hd<64, true>(v, a, blocks, stream) : launch_attn_hd<64, false>(v, a, blocks, stream);
-    if (v.hd == 128) return v.fp8 ? launch_attn_hd<128, true>(v, a, blocks, stream) : launch_attn_hd<128, false>(v, a, blocks, stream);
-    return v.fp8 ? launch_attn_hd<256, true>(v, a, blocks, stream) : launch_attn_hd<256, false>(v, a, blocks, stream);
+kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, PagedOrder order) {
+    if (v.hd == 64) return v.fp8 ? launch_attn_hd<64, true>(v, a, blocks, order) : launch_attn_hd<64, false>(v, a, blocks, order);
+    if (v.hd == 128) return v.fp8 ? launch_attn_hd<128, true>(v, a, blocks, order) : launch_attn_hd<128, false>(v, a, blocks, order);
+    return v.fp8 ? launch_attn_hd<256, true>(v, a, blocks, order) : launch_attn_hd<256, false>(v, a, blocks, order);
 }
 
 // Both ways into the attention kernels.
 kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type, uint32_t out_mode,
                         int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale_log2, uint32_t window,
                         const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
-                        int32_t* status_d, uint64_t* launches, void* stream) {
+                        int32_t* status_d, uint64_t* launches, PagedOrder order) {
     if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
     const AttnSpace sp = attn_space(cache->head_dim);
     if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
@@ -240,9 +241,9 @@ kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     const bool many = (uint64_t)seqs->n_seqs * cache->n_kv_heads * a.HT >= (uint64_t)blocks;
     a.whole_pairs = most <= (uint64_t)(many ? PA_WHOLE_MANY : PA_WHOLE_FEW) * attn_tile(v, out_mode);
     if (launches) *launches = a.whole_pairs ? 1 : 2;
-    const kl_status rc = launch_attn(v, a, blocks, stream);
+    const kl_status rc = launch_attn(v, a, blocks, order);
     if (rc != KL_OK || a.whole_pairs) return rc;
-    return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, stream, v, a);
+    return launch(kl_paged_merge_kernel, dim3((unsigned)blocks, a.G < 8 ? a.G : 8), PA_MERGE_THREADS, 0, order, v, a);
 }
 
 }  // namespace
@@ -253,20 +254,9 @@ kl_status paged_check(const kl_paged_cache* cache, const kl_paged_seqs* seqs) {
     return rc != KL_OK ? rc : check_seqs(cache, seqs);
 }
 
-kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const float* q_d, __nv_bfloat16* operand_d,
-                                  uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
-                                  size_t workspace_bytes, int32_t* status_d, uint64_t* launches, void* stream) {
-    const int64_t width = (int64_t)n_q_heads * cache->head_dim;
-    return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, selected_d, n_select, nullptr, workspace_d,
-                         workspace_bytes, status_d, launches, stream);
-}
-}  // namespace kl
-
-extern "C" {
-
-kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
-                          const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
-                          int32_t* status_d, void* stream) {
+kl_status paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                       const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                       int32_t* status_d, PagedOrder order) {
     kl_status rc;
     if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
     if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
@@ -277,42 +267,14 @@ kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     const PagedRows r = rows_of(row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride);
     const size_t smem = cache->bounds_d ? (size_t)(PW_THREADS / (cache->head_dim / 8) / 2) * 2 * cache->head_dim * 4 : 0;
     const dim3 grid((unsigned)units, cache->n_kv_heads);
-    if (v.hd == 64) return launch_append<64>(row_type, v, r, grid, smem, stream);
-    if (v.hd == 128) return launch_append<128>(row_type, v, r, grid, smem, stream);
-    return launch_append<256>(row_type, v, r, grid, smem, stream);
+    if (v.hd == 64) return launch_append<64>(row_type, v, r, grid, smem, order);
+    if (v.hd == 128) return launch_append<128>(row_type, v, r, grid, smem, order);
+    return launch_append<256>(row_type, v, r, grid, smem, order);
 }
 
-kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
-                        void* k_out_d, void* v_out_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
-                        int32_t* status_d, void* stream) {
-    kl_status rc;
-    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
-    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
-    if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
-    const PagedView v = view(cache, seqs, status_d);
-    const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
-    const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / 8), chunks = (n_rows + per - 1) / per;
-    const int sms = attn_blocks();
-    if (sms <= 0) return KL_ERR_CUDA;
-    const dim3 grid(chunks < 4u * (unsigned)sms ? chunks : 4u * (unsigned)sms);   // as many blocks as the SMs hold
-    if (v.hd == 64) return launch_read<64>(row_type, v, r, grid, stream);
-    if (v.hd == 128) return launch_read<128>(row_type, v, r, grid, stream);
-    return launch_read<256>(row_type, v, r, grid, stream);
-}
-
-kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes) {
-    if (!bytes) return KL_ERR_INVALID_ARG;
-    const kl_status rc = check_cache(cache, false);
-    if (rc != KL_OK) return rc;
-    if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
-    const size_t sel = score_bytes(cache, n_seqs, table_pages), att = attn_space(cache->head_dim).bytes;
-    *bytes = sel > att ? sel : att;
-    return KL_OK;
-}
-
-kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
-                          uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
-                          void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream) {
+kl_status paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
+                       uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
+                       void* workspace_d, size_t workspace_bytes, int32_t* status_d, PagedOrder order) {
     kl_status rc;
     if ((rc = check_cache(cache, false)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
     if (seqs->n_seqs == 0) return KL_OK;
@@ -333,13 +295,66 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
     a.scores = (float2*)workspace_d;
     const int sms = attn_blocks();
     if (sms <= 0) return KL_ERR_CUDA;
-    if ((rc = launch_score(v, a, sms, stream)) != KL_OK) return rc;
+    if ((rc = launch_score(v, a, sms, order)) != KL_OK) return rc;
     // keys in shared memory up to PT_KEYS pages, else in the workspace
     const dim3 grid(cache->n_kv_heads, seqs->n_seqs);
-    if (seqs->table_pages > PT_KEYS) return launch(kl_paged_topk_kernel<false>, grid, PT_THREADS, 0, stream, v, a);
+    if (seqs->table_pages > PT_KEYS) return launch(kl_paged_topk_kernel<false>, grid, PT_THREADS, 0, order, v, a);
     static std::atomic<uint64_t> done{0};
     if ((rc = prepare((const void*)kl_paged_topk_kernel<true>, (int)PT_KEYS * 4, done)) != KL_OK) return rc;
-    return launch(kl_paged_topk_kernel<true>, grid, PT_THREADS, (size_t)seqs->table_pages * 4, stream, v, a);
+    return launch(kl_paged_topk_kernel<true>, grid, PT_THREADS, (size_t)seqs->table_pages * 4, order, v, a);
+}
+
+kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const float* q_d, __nv_bfloat16* operand_d,
+                                  uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
+                                  size_t workspace_bytes, int32_t* status_d, uint64_t* launches, PagedOrder order) {
+    const int64_t width = (int64_t)n_q_heads * cache->head_dim;
+    return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, selected_d, n_select, nullptr, workspace_d,
+                         workspace_bytes, status_d, launches, order);
+}
+}  // namespace kl
+
+extern "C" {
+
+kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                          const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                          int32_t* status_d, void* stream) {
+    return paged_append(cache, seqs, row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride, status_d, {stream, true});
+}
+
+kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                        void* k_out_d, void* v_out_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                        int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
+    if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
+    const PagedView v = view(cache, seqs, status_d);
+    const PagedOrder order = {stream, true};
+    const PagedRows r = rows_of(row_starts_d, n_rows, k_out_d, v_out_d, row_type, k_row_stride, v_row_stride);
+    const uint32_t per = pr_rows(cache->n_kv_heads, cache->head_dim / 8), chunks = (n_rows + per - 1) / per;
+    const int sms = attn_blocks();
+    if (sms <= 0) return KL_ERR_CUDA;
+    const dim3 grid(chunks < 4u * (unsigned)sms ? chunks : 4u * (unsigned)sms);   // as many blocks as the SMs hold
+    if (v.hd == 64) return launch_read<64>(row_type, v, r, grid, order);
+    if (v.hd == 128) return launch_read<128>(row_type, v, r, grid, order);
+    return launch_read<256>(row_type, v, r, grid, order);
+}
+
+kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, uint32_t n_seqs, uint32_t table_pages, size_t* bytes) {
+    if (!bytes) return KL_ERR_INVALID_ARG;
+    const kl_status rc = check_cache(cache, false);
+    if (rc != KL_OK) return rc;
+    if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
+    const size_t sel = score_bytes(cache, n_seqs, table_pages), att = attn_space(cache->head_dim).bytes;
+    *bytes = sel > att ? sel : att;
+    return KL_OK;
+}
+
+kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
+                          uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
+                          void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream) {
+    return paged_select(cache, seqs, q_d, q_type, q_row_stride, n_q_heads, keep_first, keep_last, n_select, selected_d, workspace_d, workspace_bytes,
+                        status_d, {stream, true});
 }
 
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,
@@ -354,7 +369,7 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     if (!(scale < INFINITY)) return KL_ERR_INVALID_ARG;
     const float scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
     return run_attention(cache, seqs, q_d, out_d, q_type, q_type == KL_F32 ? PA_F32 : PA_BF16, q_row_stride, out_row_stride, n_q_heads, scale_log2,
-                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, nullptr, stream);
+                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, nullptr, {stream, true});
 }
 
 }  // extern "C"

@@ -1,4 +1,6 @@
 """Properties the paged operators promise beyond ordinary batches."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -137,3 +139,48 @@ def test_replayed_steps_keep_empty_slots_empty(fill):
     del graph
     a.dec.close()
     b.dec.close()
+
+
+def programmatic_edges(graph):
+    """(edges, how many of them let a kernel start before the one in front of it has ended)"""
+    cu = C.CDLL("libcuda.so.1")
+    get = cu.cuGraphGetEdges_v2
+    get.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+    n = C.c_size_t()
+    assert get(graph.raw_cuda_graph(), None, None, None, C.byref(n)) == 0
+    a, b = ((C.c_void_p * n.value)() for _ in range(2))
+    data = (C.c_uint8 * (8 * n.value))()   # CUgraphEdgeData: the type is its third byte, 1 = programmatic
+    assert get(graph.raw_cuda_graph(), a, b, data, C.byref(n)) == 0
+    return n.value, sum(data[8 * i + 2] == 1 for i in range(n.value))
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("n_select", [0, 3])
+def test_plain_stream_order_holds_for_the_whole_paged_step(wide, n_select):
+    """kl_set_dependent_launch(0): every kernel of the step starts when the one before it has ended, those of the paged operators too."""
+    shape, contexts = gen.TINY, [30, 12]
+    s = Setup(shape, contexts, 16, kl.KL_KV_BF16, n_select)
+    if wide:   # attention over all positions joins with a kernel of its own
+        table = torch.full((2, 4096), -1, dtype=torch.int32, device="cuda")
+        table[:, :s.table.shape[1]] = s.table
+        s.table = table
+        s.ws = torch.empty(s.dec.kl_paged_step_bytes(s.caches[0], 2, 4096, n_select), dtype=torch.uint8, device="cuda").fill_(0xff)
+    made, logits = {}, {}
+    torch.cuda.synchronize()
+    for on in (True, False):
+        s.dec.kl_set_dependent_launch(on)
+        graph = torch.cuda.CUDAGraph(keep_graph=True)
+        before = s.dec.kl_launch_count()
+        with torch.cuda.graph(graph):
+            s.step(stream=torch.cuda.current_stream())
+        made[on] = s.dec.kl_launch_count() - before
+        edges, early = programmatic_edges(graph)
+        assert edges == made[on] - 1 and early == (edges if on else 0)
+        graph.instantiate()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert s.dec.kl_last_status() == 0
+        logits[on] = s.logits.clone()
+        del graph
+    assert made[True] == made[False] and torch.equal(logits[True], logits[False])
+    s.dec.close()
