@@ -457,6 +457,9 @@ class Decoder:
               positions_d.dtype is _I32 and page_table_d.dtype is _I32 and page_table_d.stride(1) == 1 and logits_d.dtype is _F32 and
               logits_d.numel() == batch * self.shape.vocab and logits_d.is_contiguous() and tokens_d.is_contiguous() and
               positions_d.is_contiguous() and workspace_d.dtype is _U8 and workspace_d.is_contiguous() and 0 <= n_select < 1 << 31, fn)
+        dev = self.weight_arena.get_device()   # the library launches on the current device, and its weights lie there
+        _need(dev >= 0 and dev == torch.cuda.current_device() and all(c._index == dev for c in caches) and
+              all(t.get_device() == dev for t in (tokens_d, positions_d, page_table_d, logits_d, workspace_d)), fn)
         layers = (PagedCacheDesc * len(caches))(*(c.desc for c in caches))
         stride = page_table_d.stride(0) if batch > 1 else max(page_table_d.stride(0), pages)
         _check(lib().kl_decode_step_paged(self.handle, _ptr(tokens_d), _ptr(positions_d), C.addressof(layers), _ptr(page_table_d), stride, pages,

@@ -184,3 +184,15 @@ def test_plain_stream_order_holds_for_the_whole_paged_step(wide, n_select):
         del graph
     assert made[True] == made[False] and torch.equal(logits[True], logits[False])
     s.dec.close()
+
+
+def test_step_refuses_caches_of_the_host():
+    s = Setup(gen.TINY, [30, 12], 16, kl.KL_KV_BF16)
+    k = torch.zeros(4, gen.TINY.n_kv_heads, 16, gen.TINY.head_dim, dtype=torch.bfloat16)
+    made = s.dec.kl_launch_count()
+    for caches in ([kl.PagedCache(k, k.clone())] * gen.TINY.n_layers, s.caches[:-1] + [kl.PagedCache(k, k.clone())]):
+        with pytest.raises(kl.KlError) as e:
+            s.dec.kl_decode_step_paged(s.tok, s.pos, caches, s.table, s.logits, s.ws)
+        assert e.value.code == kl.KL_ERR_INVALID_ARG
+    assert s.dec.kl_launch_count() == made
+    s.dec.close()

@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
-from paper_2410_23668_b200 import binding as kl, build
+from paper_2410_23668_b200 import binding as kl, build, inputs as gen
 
 OK, BAD, SHAPE = kl.KL_OK, kl.KL_ERR_INVALID_ARG, kl.KL_ERR_UNSUPPORTED_SHAPE
 P = 4096   # stands for a device pointer; a refused call never follows it
@@ -109,3 +109,46 @@ def test_binding_checks():
     q = torch.zeros(1, 8, 128)
     with pytest.raises(kl.KlError):   # tensors of the host: the library launches on the current device
         kl.kl_paged_attention(c, q, q, torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), torch.zeros(9, dtype=torch.uint8))
+
+
+def test_step_refuses_tensors_of_another_device(monkeypatch):
+    """The step's buffers, the caches of its layers and the model lie on the current device, or the library is not called."""
+    class Library:
+        def kl_decode_step_paged(self, *args):
+            raise AssertionError("the library was called")
+
+        def kl_status_string(self, code):
+            return b""
+
+    shape = gen.TINY
+    monkeypatch.setattr(kl, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    class Here:   # what the binding asks of a tensor of device 0
+        def __init__(self, t):
+            self.t = t
+
+        def get_device(self):
+            return 0
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+    k = torch.zeros(4, shape.n_kv_heads, 16, shape.head_dim, dtype=torch.bfloat16)
+    host, there = kl.PagedCache(k, k.clone()), kl.PagedCache(k, k.clone())
+    there._index = 0
+    i32 = lambda *size: torch.zeros(size, dtype=torch.int32)
+    args = dict(tok=i32(2), pos=i32(2), table=i32(2, 3), logits=torch.zeros(2, shape.vocab), ws=torch.zeros(256, dtype=torch.uint8))
+
+    def step(arena=0, caches=None, **host_ones):
+        dec = object.__new__(kl.Decoder)
+        dec.shape, dec.handle, dec.weight_arena = shape, None, Here(k) if arena == 0 else k
+        a = {n: host_ones.get(n, Here(t)) for n, t in args.items()}
+        dec.kl_decode_step_paged(a["tok"], a["pos"], caches or [there] * shape.n_layers, a["table"], a["logits"], a["ws"])
+
+    with pytest.raises(AssertionError):   # everything where it should be
+        step()
+    for over in ([dict(arena=-1), dict(caches=[there] * (shape.n_layers - 1) + [host])] + [{n: t} for n, t in args.items()]):
+        with pytest.raises(kl.KlError) as e:
+            step(**over)
+        assert e.value.code == BAD, over
