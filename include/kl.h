@@ -404,7 +404,9 @@ typedef struct {
  * KL_KV_BF16: rounded to nearest even.  KL_KV_E4M3: per row and head, e = the smallest integer >= -127 with
  * (largest finite magnitude) <= 448 * 2^e, scale byte e + 127, codes x / 2^e rounded to nearest even (infinities
  * saturate, NaN stays NaN).  The scale is a power of two: e4m3 is itself a floating-point format, a finer scale would
- * gain no precision, and this one makes quantising, reading back and the page bounds exact.
+ * gain no precision, and this one makes quantising, reading back and the page bounds exact -- but for rows whose largest
+ * magnitude is at most 448 * 2^-125 (scale bytes 0 .. 2), which stand for multiples of 2^-136 .. 2^-134 while bf16 ends at
+ * 2^-133: fp32 holds those, bounds are rounded outwards, kl_paged_read rounds to nearest for bf16 outputs.
  * bounds_d (if any): a row 0 of a page starts the page's bounds anew, other rows widen them; overwriting a row in the
  * middle of a page leaves bounds that still hold, perhaps wider than need be.
  * Two sequences of a call must not write the same page. */
@@ -413,7 +415,8 @@ kl_status kl_paged_append(const kl_paged_cache* cache, const kl_paged_seqs* seqs
                           int32_t* status_d, void* stream);
 
 /* The way back: the rows that kl_paged_append with the same arguments would write are copied out of the cache, as bf16
- * (exact for both cache types) or fp32.  Output rows that belong to no sequence or to an empty slot are left as they were. */
+ * (exact for both cache types, but for the smallest scales, see above) or fp32 (exact).  Output rows that belong to no sequence
+ * or to an empty slot are left as they were. */
 kl_status kl_paged_read(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
                         void* k_out_d, void* v_out_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
                         int32_t* status_d, void* stream);

@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append
             const float y = pg_red[k * 2u * HD + t];
             x = up ? fmaxf(x, y) : fminf(x, y);
         }
-        bounds[t] = __float2bfloat16_rn(x);
+        bounds[t] = up ? __float2bfloat16_ru(x) : __float2bfloat16_rd(x);   // exact but for e4m3 rows of scale bytes 0 .. 2
     }
 }
 

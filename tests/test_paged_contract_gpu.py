@@ -196,3 +196,35 @@ def test_step_refuses_caches_of_the_host():
         assert e.value.code == kl.KL_ERR_INVALID_ARG
     assert s.dec.kl_launch_count() == made
     s.dec.close()
+
+
+def test_bounds_hold_where_bf16_has_no_number():
+    """e4m3 rows of the smallest scales stand for numbers that bf16 does not hold (down to 2^-136): their bounds are rounded outwards."""
+    nkv, hd, page, n = 2, 64, 8, 13
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(n, 2, nkv, hd, generator=g) * 2.0 ** -134
+    x[page:] *= 2.0 ** 20                                   # a page of scales that leave bf16 numbers only
+    x[:, :, :, 0] = x[:, :, :, 0].sign() * 2.0 ** -124      # the largest of the first page's rows
+    x = x.cuda()
+    c = ref.Cache(3, nkv, page, hd, True, bounds=True, seed=2)
+    table = ref.scattered_table([n + 5], page, 3, seed=3, extra=0)
+    c.bounds.zero_()
+    for k0, k1 in ((0, 4), (4, n)):   # a page goes on
+        kl.kl_paged_append(c.handle, x[k0:k1, 0], x[k0:k1, 1], i32([k0]), table.cuda(), row_starts=i32([0, k1 - k0]))
+    ko, vo = (torch.zeros(n, nkv, hd, device="cuda") for _ in range(2))
+    kl.kl_paged_read(c.handle, ko, vo, i32([0]), table.cuda(), row_starts=i32([0, n]))
+    torch.cuda.synchronize()
+    inexact = 0
+    for lp in range(2):
+        phys = int(table[0, lp])
+        held = c.values("k")[phys, :, :min(page, n - lp * page)]
+        assert torch.equal(ko[lp * page:lp * page + held.shape[1]].cpu().double().transpose(0, 1), held)   # fp32 holds them all
+        b = c.bounds[phys].cpu().double()
+        lo, hi = held.amin(1), held.amax(1)
+        assert bool((b[:, 0] <= lo).all()) and bool((b[:, 1] >= hi).all())
+        step = 2.0 ** -133   # between the bf16 numbers at zero
+        assert bool((lo - b[:, 0] < step).all()) and bool((b[:, 1] - hi < step).all())
+        exact = (lo / step == (lo / step).round()) | (lo.abs() > 2.0 ** -120)
+        assert torch.equal(b[:, 0][exact], lo[exact])
+        inexact += int((~exact).sum())
+    assert inexact > 50
