@@ -640,11 +640,12 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 //   of its error.
 // Measured: 397 thousand (page, head) pairs of 512 bytes, eight query heads each, 40.5 us (5.0 TB/s, what the kernel needs to
 // start and end included), 42.8 with rows loaded straight into registers.
-// Error bound: a matrix-product step adds 16 exact products to the sum, with an error of at most 2^-22 of the sum of all
-// magnitudes, and there are hd / 8 <= 32 steps: 2^-17 of sum |q_d| max|b|; fp32 queries also lose 2^-16 of themselves.  Taken:
-// 2^-16 (2^-14) times the largest sum |q_d| of a head and the page's largest bound, of which the errors seen (random, widely
-// spread, equal and cancelling terms) stay below 8 %; infinite where a score or bound is not finite, and below 2^-100: numbers
-// under 2^-126 have fewer bits (a rest of a query is off by up to 2^-134), which the bound does not count.
+// Error bound: a product of two bf16 is exact, and the matrix instruction adds with at least single precision, in an order of
+// its own: each addition is off by at most a unit, 2^-23, of the sum of all magnitudes.  A step adds 16 products and there are hd / 8 of
+// them (fp32 queries: twice as many, and the two parts leave 2^-16 of a query): hd * 2^-22 (hd * 2^-21 + 2^-16) of the
+// largest sum |q_d| of a head times the page's largest bound; infinite where a score or bound is not finite, and below 2^-100:
+// numbers under 2^-126 have fewer bits (a rest of a query is off by up to 2^-134), which the bound does not count.  Errors seen
+// (random, widely spread, equal, cancelling terms, a large one among small ones) stay below 9 % of it.
 template <int HD>
 struct PsCfg {
     static constexpr int ROW = 4 * HD, TILE = 16 * ROW;   // bytes of a page's bounds, of a tile's
@@ -812,7 +813,7 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
         if (j < 2u) {   // lane 0 of the quad stores page g, lane 1 page g + 8
             const uint32_t p = cur.t * 16u + g + j * 8u, b = (j ? big1 : big0) & 0x7fff7fffu;
             const float mag = __uint_as_float(max(b >> 16, b & 0xffffu) << 16);
-            const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? 0x1p-14f : 0x1p-16f);
+            const float score = j ? best1 : best0, err = q1 * 1.001f * mag * (F32 ? HD * 0x1p-21f + 0x1p-16f : HD * 0x1p-22f);
             // (infinite where nothing is known: 0 * infinity, a score that is not finite, queries whose halves and products
             // whose sums reach down to where numbers have fewer bits; zeros are exact)
             const bool known = isfinite(score) && (q1 == 0.f || mag == 0.f ? err == 0.f : q1 >= 0x1p-100f && err >= 0x1p-100f);

@@ -228,3 +228,60 @@ def test_bounds_hold_where_bf16_has_no_number():
         assert torch.equal(b[:, 0][exact], lo[exact])
         inexact += int((~exact).sum())
     assert inexact > 50
+
+
+SPREADS = ["one large, equal small ones", "one large, small ones of both signs", "falling by halves", "cancelling", "wide"]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("spread", SPREADS)
+@pytest.mark.parametrize("power", [-20, -23, -25, -27])
+def test_select_hard_spreads(dtype, hd, spread, power):
+    """Pages whose scores differ only by terms that a 32-bit sum loses: the choice is that of the exact scores, and the scores the
+    workspace holds ([n_seqs][n_kv_heads][pages] of score, bound) are off by no more than the bound beside them."""
+    nkv, G, page, pages, n_select = 2, 3, 4, 300, 40
+    g = torch.Generator().manual_seed(1000 * hd + 10 * SPREADS.index(spread) - power)
+    c = ref.Cache(pages, nkv, page, hd, False, bounds=True, seed=1)
+    q = torch.zeros(1, nkv * G, hd)
+    b = torch.zeros(pages, nkv, hd)
+    small = 2.0 ** power
+    if spread == "one large, equal small ones":
+        q[:] = small
+        b[:] = (torch.rand(pages, nkv, hd, generator=g) < torch.rand(pages, nkv, 1, generator=g)).float()
+    elif spread == "one large, small ones of both signs":
+        q[:] = small * (1 + torch.rand(q.shape, generator=g))
+        b[:] = torch.randint(-1, 2, b.shape, generator=g).float()
+    elif spread == "falling by halves":
+        q[:] = 2.0 ** -(torch.arange(hd) % 30).float() * torch.sign(torch.randn(q.shape, generator=g))
+        b[:] = 1 + torch.rand(b.shape, generator=g) * small
+    elif spread == "cancelling":
+        q[:] = 1.0
+        q[..., 1::2] = -1.0
+        b[:] = 1.0 + 0.25 * torch.rand(pages, nkv, 1, generator=g)
+        b[..., ::2] += torch.randint(0, 2, (pages, nkv, hd // 2), generator=g) * 2.0 ** -7
+    else:
+        q[:] = torch.randn(q.shape, generator=g) * torch.exp(4 * torch.randn(q.shape, generator=g))
+        b[:] = torch.randn(b.shape, generator=g) * torch.exp(4 * torch.randn(b.shape, generator=g))
+    if spread.startswith("one large"):
+        at = int(torch.randint(0, hd, (1,), generator=g))
+        q[..., at] = 1.0
+        b[..., at] = 1.0
+    q = q.to(dtype)
+    b = b.to(torch.bfloat16)
+    c.bounds.copy_(torch.stack([b, b], 2))   # lo = hi: the score is a plain product sum
+    table = ref.scattered_table([pages * page], page, pages, seed=2)
+    sel = torch.full((1, nkv, n_select), 9, dtype=torch.int32, device="cuda")
+    ws = torch.empty(kl.kl_paged_workspace_bytes(c.handle, nkv * G, 1, table.shape[1]), dtype=torch.uint8, device="cuda").fill_(0xff)
+    kl.kl_paged_select(c.handle, q.cuda(), i32([pages * page - 1]), table.cuda(), sel, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(sel.cpu(), ref.select_ref(c.bounds.cpu(), q, [pages * page - 1], table, page, 1, 1, n_select))
+    held = ws[:nkv * table.shape[1] * 8].view(torch.float32).view(nkv, table.shape[1], 2)[:, :pages].cpu().double()
+    v = b[table[0, :pages].long()].double()
+    exact = torch.stack([torch.einsum("gd,pd->gp", q[0, h * G:(h + 1) * G].double(), v[:, h]).amax(0) for h in range(nkv)])
+    off = (held[..., 0] - exact).abs() / held[..., 1]
+    assert bool((off <= 1.0).all()), float(off.max())
+    reach = torch.stack([torch.einsum("gd,pd->gp", q[0, h * G:(h + 1) * G].double().abs(), v[:, h].abs()).amax(0) for h in range(nkv)])
+    # hd / 16 products of 16 terms for lo and as many for hi (fp32 queries: twice), each addition off by a unit of 32 bits at most
+    need = hd * 2.0 ** -22 if dtype == torch.bfloat16 else hd * 2.0 ** -21 + 2.0 ** -16
+    assert bool((held[..., 1] >= need * reach).all())
