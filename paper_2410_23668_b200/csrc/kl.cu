@@ -1587,7 +1587,7 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
     if (!h || !tokens_d || !positions_d || !layers || !page_table_d || !logits_d || !workspace_d) return KL_ERR_INVALID_ARG;
     if (batch == 0 || batch > h->desc.max_batch) return KL_ERR_INVALID_ARG;
     if (!h->bt_ok) return KL_ERR_UNSUPPORTED_SHAPE;
-    if (n_select == 1) return KL_ERR_INVALID_ARG;   // the first and the last page are always chosen
+    if (n_select == 1 || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;   // the first and the last page are always chosen
     if (!all_loaded(h)) return KL_ERR_NOT_LOADED;
     const Params& p = h->prm;
     uint32_t n_pages = 0xffffffffu;

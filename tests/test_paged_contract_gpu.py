@@ -285,3 +285,16 @@ def test_select_hard_spreads(dtype, hd, spread, power):
     # hd / 16 products of 16 terms for lo and as many for hi (fp32 queries: twice), each addition off by a unit of 32 bits at most
     need = hd * 2.0 ** -22 if dtype == torch.bfloat16 else hd * 2.0 ** -21 + 2.0 ** -16
     assert bool((held[..., 1] >= need * reach).all())
+
+
+def test_step_refuses_more_pages_than_a_list_can_name():
+    """Refused before anything is launched, whatever the workspace claims to hold."""
+    s = Setup(gen.TINY, [30, 12], 16, kl.KL_KV_BF16, 3)
+    layers = (kl.PagedCacheDesc * len(s.caches))(*(c.desc for c in s.caches))
+    made = s.dec.kl_launch_count()
+    for n_select in (1, 2 ** 31, 2 ** 32 - 1):
+        rc = kl.lib().kl_decode_step_paged(s.dec.handle, s.tok.data_ptr(), s.pos.data_ptr(), C.addressof(layers), s.table.data_ptr(), s.table.stride(0),
+                                           s.table.shape[1], n_select, s.logits.data_ptr(), 2, s.ws.data_ptr(), 1 << 62, None)
+        assert rc == kl.KL_ERR_INVALID_ARG
+    assert s.dec.kl_launch_count() == made
+    s.dec.close()
