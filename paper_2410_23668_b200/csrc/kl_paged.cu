@@ -97,8 +97,12 @@ PagedRows rows_of(const int32_t* row_starts_d, uint32_t n_rows, const void* k, c
     return r;
 }
 
-size_t score_bytes(const kl_paged_cache* c, uint64_t n_seqs, uint64_t table_pages) {
-    return (size_t)((n_seqs * c->n_kv_heads * table_pages * 8 + 255) / 256 * 256);
+// Workspace of kl_paged_select; false where no address space holds it.
+bool score_bytes(const kl_paged_cache* c, uint64_t n_seqs, uint64_t table_pages, size_t* bytes) {
+    const uint64_t pairs = n_seqs * c->n_kv_heads;   // below 2^48
+    if (table_pages && pairs > (1ull << 56) / table_pages) return false;
+    *bytes = (size_t)((pairs * table_pages * 8 + 255) / 256 * 256);
+    return true;
 }
 
 kl_status check_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_seqs) {
@@ -281,8 +285,9 @@ kl_status paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, c
     if ((rc = check_queries(cache, q_d, q_type, q_row_stride, n_q_heads, seqs->n_seqs)) != KL_OK) return rc;
     if (!cache->bounds_d || !selected_d) return KL_ERR_INVALID_ARG;
     if (!n_select || (uint64_t)keep_first + keep_last > n_select || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
-    if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < score_bytes(cache, seqs->n_seqs, seqs->table_pages)) return KL_ERR_INVALID_ARG;
-    if (seqs->n_seqs > 65535u) return KL_ERR_UNSUPPORTED_SHAPE;
+    size_t need;
+    if (seqs->n_seqs > 65535u || !score_bytes(cache, seqs->n_seqs, seqs->table_pages, &need)) return KL_ERR_UNSUPPORTED_SHAPE;
+    if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < need) return KL_ERR_INVALID_ARG;
     const PagedView v = view(cache, seqs, status_d);
     PagedSelect a;
     a.q = (const uint8_t*)q_d;
@@ -345,7 +350,9 @@ kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_hea
     const kl_status rc = check_cache(cache, false);
     if (rc != KL_OK) return rc;
     if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
-    const size_t sel = score_bytes(cache, n_seqs, table_pages), att = attn_space(cache->head_dim).bytes;
+    size_t sel;
+    if (!score_bytes(cache, n_seqs, table_pages, &sel)) return KL_ERR_UNSUPPORTED_SHAPE;
+    const size_t att = attn_space(cache->head_dim).bytes;
     *bytes = sel > att ? sel : att;
     return KL_OK;
 }

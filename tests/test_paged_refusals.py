@@ -152,3 +152,15 @@ def test_step_refuses_tensors_of_another_device(monkeypatch):
         with pytest.raises(kl.KlError) as e:
             step(**over)
         assert e.value.code == BAD, over
+
+
+def test_sizes_beyond_any_workspace(lib):
+    """Products of sizes that leave 64 bits are refused, not cut off to something small."""
+    b = C.c_size_t()
+    many = cache(n_kv_heads=65535, page_size=4)
+    assert lib.kl_paged_workspace_bytes(C.byref(many), 65535, 65536, 1 << 29, C.byref(b)) == SHAPE
+    assert lib.kl_paged_workspace_bytes(C.byref(cache()), 8, 1 << 31, 1 << 31, C.byref(b)) == SHAPE
+    assert lib.kl_paged_workspace_bytes(C.byref(cache()), 8, 65535, 1 << 27, C.byref(b)) == OK and b.value == 65535 * 2 * (1 << 27) * 8
+    s = seqs(n_seqs=65535, table_pages=(1 << 29) - 1, table_stride=(1 << 29) - 1)
+    assert select_call(lib, many, s, nq=65535, qs=65535 * 128, wb=(1 << 64) - 1) == SHAPE
+    assert select_call(lib, cache(page_size=4), s, wb=1 << 40) == BAD
