@@ -1,5 +1,6 @@
 """Properties the paged operators promise beyond ordinary batches."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -7,7 +8,7 @@ import torch
 from paper_2410_23668_b200 import binding as kl, build, inputs as gen
 from tests import helpers, paged_ref as ref
 from tests.test_paged_decode_gpu import Setup
-from tests.test_paged_gpu import check_attention, i32
+from tests.test_paged_gpu import check_attention, i32, rows_like
 
 pytestmark = pytest.mark.gpu
 
@@ -298,3 +299,171 @@ def test_step_refuses_more_pages_than_a_list_can_name():
         assert rc == kl.KL_ERR_INVALID_ARG
     assert s.dec.kl_launch_count() == made
     s.dec.close()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_sequences_share_the_pages_of_a_prefix(e4m3):
+    """Three sequences with the same first pages: read, select and attention see the prefix in each, append writes their own pages."""
+    page, hd, nkv, nq, prefix, own = 16, 128, 2, 8, 8, [3, 1, 5]
+    lengths = [(prefix + x) * page - 5 for x in own]
+    n_pages = prefix + sum(own)
+    c = ref.Cache(n_pages, nkv, page, hd, e4m3, bounds=True, seed=1)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(2)).to(torch.int32)
+    table = torch.full((3, prefix + max(own)), -1, dtype=torch.int32)
+    table[:, :prefix] = order[:prefix]
+    at = prefix
+    for s, x in enumerate(own):
+        table[s, prefix:prefix + x] = order[at:at + x]
+        at += x
+    tab = table.cuda()
+    k, v = rows_like(prefix * page, nkv, hd, torch.bfloat16, 3)
+    kl.kl_paged_append(c.handle, k, v, i32([0]), tab[:1].contiguous(), row_starts=i32([0, prefix * page]))
+    shared = [t[order[:prefix].long().cuda()].view(torch.uint8).clone() for t in (c.k, c.v, c.bounds)]
+    starts = [0]
+    for x in lengths:
+        starts.append(starts[-1] + x - prefix * page)
+    k, v = rows_like(starts[-1], nkv, hd, torch.bfloat16, 4)
+    kl.kl_paged_append(c.handle, k, v, i32([prefix * page] * 3), tab, row_starts=i32(starts))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, t[order[:prefix].long().cuda()].view(torch.uint8)) for x, t in zip(shared, (c.k, c.v, c.bounds)))
+    pos = [x - 1 for x in lengths]
+    q = (torch.randn(3, nq, hd, generator=torch.Generator().manual_seed(5)) * 0.2).to(torch.bfloat16).cuda()
+    check_attention(c, q, torch.tensor(pos, dtype=torch.int32), table)
+    sel = torch.zeros(3, nkv, 6, dtype=torch.int32, device="cuda")
+    ws = torch.empty(kl.kl_paged_workspace_bytes(c.handle, nq, 3, table.shape[1]), dtype=torch.uint8, device="cuda")
+    kl.kl_paged_select(c.handle, q, i32(pos), tab, sel, ws)
+    torch.cuda.synchronize()
+    want = ref.select_ref(c.bounds.cpu(), q.cpu(), pos, table, page, 1, 1, 6)
+    assert torch.equal(sel.cpu(), want)
+    check_attention(c, q, torch.tensor(pos, dtype=torch.int32), table, selected=want)
+    n = prefix * page
+    ko, vo = (torch.zeros(3 * n, nkv, hd, device="cuda") for _ in range(2))
+    kl.kl_paged_read(c.handle, ko, vo, i32([0, 0, 0]), tab, row_starts=i32([0, n, 2 * n, 3 * n]))
+    torch.cuda.synchronize()
+    for got, held in ((ko, c.values("k")), (vo, c.values("v"))):
+        rows = held[order[:prefix].long()].transpose(1, 2).reshape(n, nkv, hd)
+        assert torch.equal(got.cpu().double(), rows.repeat(3, 1, 1))
+
+
+@pytest.mark.parametrize("n_select", [0, 3])
+def test_steps_on_a_shared_prefix_equal_steps_on_copies(n_select):
+    """Two sequences that share the pages of a prefix, and the same two with a copy of it each: the same logits, bit for bit."""
+    shape, page, prefix = gen.TINY, 16, 3
+    logits = []
+    for shared in (False, True):
+        s = Setup(shape, [prefix * page + 5, prefix * page + 2], page, kl.KL_KV_E4M3, n_select)
+        for c in s.caches:   # the second sequence's prefix is the first one's
+            for t in c.tensors:
+                t.view(torch.uint8)[s.table[1, :prefix].long()] = t.view(torch.uint8)[s.table[0, :prefix].long()]
+        if shared:
+            s.table[1, :prefix] = s.table[0, :prefix]
+        run = []
+        for t in range(3):
+            s.step()
+            torch.cuda.synchronize()
+            assert s.dec.kl_last_status() == 0
+            run.append(s.logits.clone())
+            s.dec.kl_argmax_advance(s.logits, s.tok, s.pos, 2)
+        logits.append(run)
+        s.dec.close()
+    assert all(torch.equal(x, y) for x, y in zip(*logits))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows", [torch.bfloat16, torch.float32])
+def test_rows_of_700_sequences(e4m3, rows):
+    """More sequences than a block of append or read holds at once, some without rows, some of them empty slots."""
+    nkv, hd, page, n = 2, 64, 8, 700
+    g = torch.Generator().manual_seed(1)
+    cnt = torch.randint(0, 12, (n,), generator=g).tolist()
+    pos = torch.randint(0, 20, (n,), generator=g).tolist()
+    for s in range(0, n, 7):
+        pos[s] = -1
+    cnt[:3], cnt[-3:] = [0, 0, 5], [0, 9, 0]
+    starts = [2]   # rows in front of the first sequence
+    for x in cnt:
+        starts.append(starts[-1] + x)
+    total = starts[-1] + 3
+    lengths = [max(p, 0) + x if p >= 0 else 0 for p, x in zip(pos, cnt)]
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, nkv, page, hd, e4m3, bounds=True, seed=2)
+    table = ref.scattered_table(lengths, page, n_pages, seed=3)
+    before = {x: getattr(c, x).cpu().clone() for x in ("k", "v", "ke", "ve", "bounds") if getattr(c, x) is not None}
+    k, v = rows_like(total, nkv, hd, rows, 4)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    kl.kl_paged_append(c.handle, k, v, i32(pos), table.cuda(), row_starts=i32(starts), status=status)
+    torch.cuda.synchronize()
+    seq = torch.tensor([s for s in range(n) for _ in range(cnt[s] if pos[s] >= 0 else 0)])
+    row = torch.tensor([starts[s] + i for s in range(n) for i in range(cnt[s] if pos[s] >= 0 else 0)])
+    at = torch.tensor([pos[s] + i for s in range(n) for i in range(cnt[s] if pos[s] >= 0 else 0)])
+    phys, off = table[seq, at // page].long(), at % page
+    expected = {}
+    for which, x in (("k", k), ("v", v)):
+        x = x.cpu()[row]
+        if e4m3:
+            y = x.double()
+            e = torch.tensor([ref.row_exponent(float(m)) for m in y.abs().amax(-1).flatten()]).view(len(row), nkv)
+            held = ref.e4m3_round(y * torch.pow(torch.tensor(2.0, dtype=torch.float64), -e)[..., None]) * torch.pow(torch.tensor(2.0, dtype=torch.float64), e)[..., None]
+            before[which + "e"][phys, :, off] = (e + 127).to(torch.uint8)
+            assert torch.equal(getattr(c, which + "e").cpu(), before[which + "e"])
+        else:
+            held = x.to(torch.bfloat16).double()
+        expected[which] = held
+        assert torch.equal(c.values(which)[phys, :, off], held)
+        rest = torch.ones(n_pages, page, dtype=torch.bool)
+        rest[phys, off] = False
+        for t, old in ((getattr(c, which), before[which]),):
+            assert torch.equal(t.cpu().view(torch.uint8).transpose(1, 2)[rest], old.view(torch.uint8).transpose(1, 2)[rest])
+    b = before["bounds"].double()
+    for i in range(len(row)):
+        p, y = int(phys[i]), expected["k"][i]
+        if off[i] == 0:
+            b[p, :, 0], b[p, :, 1] = math.inf, -math.inf
+        b[p, :, 0], b[p, :, 1] = torch.minimum(b[p, :, 0], y), torch.maximum(b[p, :, 1], y)
+    assert torch.equal(c.bounds.cpu().double(), b)
+    for out_type in (torch.bfloat16, torch.float32):
+        ko, vo = (torch.full((total, nkv, hd), 5.0, dtype=out_type, device="cuda") for _ in range(2))
+        kl.kl_paged_read(c.handle, ko, vo, i32(pos), table.cuda(), row_starts=i32(starts), status=status)
+        torch.cuda.synchronize()
+        for which, o in (("k", ko), ("v", vo)):
+            want = torch.full((total, nkv, hd), 5.0, dtype=torch.float64)
+            want[row] = expected[which]
+            assert torch.equal(o.cpu().double(), want)
+    assert status.item() == 0
+
+
+def test_attention_of_a_batch_in_another_order():
+    """More sequences than blocks of the grid, in two orders: each is right, and equal calls give equal bits."""
+    page, hd, nkv, nq, n = 16, 64, 2, 8, 500
+    g = torch.Generator().manual_seed(51)
+    lengths = [int(x) for x in torch.randint(0, 120, (n,), generator=g)]
+    n_pages = sum(-(-x // page) for x in lengths)
+    c = ref.Cache(n_pages, nkv, page, hd, False, seed=52)
+    table = ref.scattered_table(lengths, page, n_pages, seed=53)
+    q = torch.randn(n, nq, hd, generator=g).cuda()
+    pos = torch.tensor(lengths, dtype=torch.int32) - 1
+    for order in (torch.arange(n), torch.randperm(n, generator=g)):
+        a, b = (check_attention(c, q[order.cuda()].contiguous(), pos[order], table[order].contiguous()) for _ in range(2))
+        assert torch.equal(a, b)
+
+
+def test_append_and_attention_on_a_stream_of_their_own():
+    """Rows, positions and tables stay alive until the stream has read them: what is written is what was handed in."""
+    page, hd, nkv, nq = 8, 128, 2, 8
+    lengths = [30, 3, 57]
+    c = ref.Cache(20, nkv, page, hd, True, bounds=True, seed=1)
+    table = ref.scattered_table(lengths, page, 20, seed=2)
+    starts, zero, tab = i32([0, 30, 33, 90]), i32([0, 0, 0]), table.cuda()
+    k, v = rows_like(90, nkv, hd, torch.bfloat16, 3)
+    q = (torch.randn(3, nq, hd, generator=torch.Generator().manual_seed(4)) * 0.2).to(torch.bfloat16).cuda()
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    kl.kl_paged_append(c.handle, k, v, zero, tab, row_starts=starts, stream=st)
+    st.synchronize()
+    for s in range(3):
+        for i in range(lengths[s]):
+            got = c.k[int(table[s, i // page]), :, i % page].cpu()
+            for h in range(nkv):
+                x = k[int([0, 30, 33][s]) + i, h].cpu().double()
+                assert torch.equal(ref.e4m3_values(got[h]), ref.e4m3_round(x * 2.0 ** -ref.row_exponent(float(x.abs().max()))))
+    check_attention(c, q, torch.tensor(lengths, dtype=torch.int32) - 1, table, stream=st)
