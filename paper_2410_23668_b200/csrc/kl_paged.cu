@@ -293,7 +293,6 @@ kl_status paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, c
     a.q = (const uint8_t*)q_d;
     a.q_stride = q_row_stride * elem(q_type);
     a.q_f32 = q_type == KL_F32;
-    a.nq = n_q_heads;
     a.G = n_q_heads / cache->n_kv_heads;
     a.keep_first = keep_first; a.keep_last = keep_last; a.n_select = n_select;
     a.selected = selected_d;

@@ -582,7 +582,7 @@ __device__ __forceinline__ void pa_mma(float (&d)[4], uint32_t a0, uint32_t a1, 
 struct PagedSelect {
     const uint8_t* q;
     int64_t q_stride;      // bytes
-    uint32_t q_f32, nq, G;
+    uint32_t q_f32, G;
     uint32_t keep_first, keep_last, n_select;
     int32_t* selected;
     float2* scores;        // [n_seqs][nkv][table_pages]: score, bound of its error
@@ -1170,7 +1170,7 @@ __device__ __forceinline__ void pa_store_lse(const PagedAttn& a, uint32_t s, uin
 }
 
 constexpr uint32_t PA_NONE = 0x7fffffffu;   // position of a row group that holds nothing to attend to
-constexpr int PA_MAX_WARPS = 16;
+constexpr int PA_MAX_WARPS = 12;
 constexpr int PA_LENS = 1024;               // sequences whose lengths are kept in shared memory
 constexpr uint32_t PA_MIN_TILES = 8;        // fewest tiles worth a block
 
@@ -1191,6 +1191,7 @@ struct PaCfg {
     static constexpr bool QM = EX && !FP8 && HD == 256;
     static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 2 * TP + TP) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256 + (QM ? NW * 32 * HD / 2 : 0);
     static_assert(ST >= 2 && SMEM <= 232448, "ring");
+    static_assert(NW <= PA_MAX_WARPS, "workspace");
 };
 
 // Short pairs are not shared between blocks, which makes the merge kernel unnecessary (3 us on the device, 3 us on the host) but
