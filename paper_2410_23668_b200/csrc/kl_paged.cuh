@@ -1241,6 +1241,10 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     queries: EX, what it leaves of q) enters as a second product, and, where the 16 bits are bf16, what that leaves as a
 //     third: 22 bits with an e4m3 cache (two f16), 24 with a bf16 one.  The second product costs e4m3 caches 2 % of the time,
 //     the third one bf16 caches 0.5 % (fp32 queries 2 %; of a short call 0.2 and 0.7 us).
+//   * The matrix instruction cuts its sums off to 32 bits instead of rounding them, always towards zero.  With a bf16 cache the
+//     products of 16 positions are therefore summed by themselves and added to the result by an ordinary addition: relative error
+//     against 64 bits, fp32 queries, 16 sequences of 65536: 2.0e-6 (2.0e-5 without), for 1 % of the time.  e4m3 caches, whose rows
+//     have three fraction bits, go without (4e-6 for 32 of 65536; instructions are what bounds them).
 //   * e4m3 rows become f16 (exact) on the way to the tensor cores.  Their scales are powers of two: 2^(e_k - 127) multiplies
 //     the score, 2^(e_v - 127) the probability.  The weighted probabilities w = p * 2^(e_v - 127) have a reference of
 //     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
@@ -1727,9 +1731,12 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                     for (int i = 0; i < NMMA; ++i) {
                         uint32_t r[4];
                         ldmatrix_x4_trans(r, base + (((i * 2 + (lane >> 3 & 1u)) ^ fv) << 4));
-                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], b0, b1);
-                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], c0, c1);
-                        pa_mma<FP8>(o[i], r[0], r[1], r[2], r[3], e0, e1);
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                        pa_mma<FP8>(sum, r[0], r[1], r[2], r[3], e0, e1);
+                        pa_mma<FP8>(sum, r[0], r[1], r[2], r[3], c0, c1);
+                        pa_mma<FP8>(sum, r[0], r[1], r[2], r[3], b0, b1);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[i][e] += sum[e];
                     }
                 }
             }

@@ -58,6 +58,29 @@ def test_bf16_caches_keep_24_bits(hd, page, dtype, reach):
     assert worst <= 1.0, worst
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_long_sums_on_bf16_caches_have_no_drift(hd, dtype):
+    """Values that are all 1: the result is 1, however many tiles a warp adds up.  Additions to nearest have no direction; what is left
+    is the 48 additions within a tile of 16 positions, single precision, half a unit off on average: 48 * 2^-24 of the mean of
+    many results.  (Sums that are cut off instead lose half a unit per product and tile: 1.2e-5 here.)"""
+    n, nkv, G, page, ctx = 32, 4, 4, 16, 65536
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    k = torch.randn(ctx // page, nkv, page, hd, generator=g, device="cuda").to(torch.bfloat16)
+    c = kl.PagedCache(k, torch.ones_like(k))
+    table = torch.arange(ctx // page, dtype=torch.int32, device="cuda").expand(n, -1).contiguous()   # the sequences share their pages
+    q = torch.randn(n, nkv * G, hd, generator=g, device="cuda").to(dtype)
+    out = torch.zeros_like(q)
+    ws = torch.empty(kl.kl_paged_workspace_bytes(c, nkv * G, n, ctx // page), dtype=torch.uint8, device="cuda")
+    kl.kl_paged_attention(c, q, out, i32([ctx - 1] * n), table, ws)
+    torch.cuda.synchronize()
+    off = out.double() - 1
+    if dtype == torch.bfloat16:   # rounded to 1 unless off by a quarter of the step below it
+        assert bool((off == 0).all())
+    else:
+        assert abs(float(off.mean())) <= 48 * 2.0 ** -24, float(off.mean())
+
+
 @pytest.mark.parametrize("e4m3,dtype,hd", [(False, torch.bfloat16, 128), (False, torch.float32, 64), (True, torch.bfloat16, 128), (True, torch.bfloat16, 64),
                                            (True, torch.float32, 256)])
 @pytest.mark.parametrize("page", [4, 8, 16, 24])
