@@ -429,10 +429,11 @@ kl_status kl_paged_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_hea
 /* Chooses, for the newest token of every sequence and every kv head, the pages worth attending to.  q_d: [n_seqs]
  * [n_q_heads][head_dim] of q_type, rows q_row_stride elements apart; query heads h * G .. h * G + G - 1 share kv head h.
  * The score of a page is the largest, over these G heads, of sum_d max(q_d * lo_d, q_d * hi_d) -- no key of the page has a
- * larger product with q -- summed in 64 bits and rounded to 32.  The first keep_first and the last keep_last pages of a
- * sequence are always chosen, then the best scores until n_select (>= keep_first + keep_last, >= 1) are (the lower page
- * first among equals, NaN last).  selected_d: [n_seqs][n_kv_heads][n_select] logical page numbers in ascending order,
- * filled up with -1. */
+ * larger product with q -- summed in 64 bits and rounded to 32 (q_d * hi_d where q_d >= 0, else q_d * lo_d: a column that
+ * holds no number, lo > hi, counts as -infinity; NaN scores are left out of the largest).  The first keep_first and the last
+ * keep_last pages of a sequence are always chosen, then the best scores until n_select (>= keep_first + keep_last, >= 1) are
+ * (the lower page first among equals, NaN last).  selected_d: [n_seqs][n_kv_heads][n_select] logical page numbers in
+ * ascending order, filled up with -1. */
 kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, int q_type, int64_t q_row_stride,
                           uint32_t n_q_heads, uint32_t keep_first, uint32_t keep_last, uint32_t n_select, int32_t* selected_d,
                           void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream);
@@ -445,8 +446,10 @@ kl_status kl_paged_select(const kl_paged_cache* cache, const kl_paged_seqs* seqs
  * q and out: [n_seqs][n_q_heads][head_dim] of q_type; scale <= 0: 1 / sqrt(head_dim).  lse_d (optional): fp32 [n_seqs]
  * [n_q_heads], the natural logarithm of the softmax's denominator sum_p exp(scale * q . k_p), which is what joining the results
  * of several caches needs.  A sequence without positions to attend to gets zeros, and -inf.
- * n_q_heads is a multiple of n_kv_heads, any group size.  Scores, the softmax and all sums are held in 32 bits; in the two
- * products fp32 queries and the probabilities take part with 24 bits (KL_KV_BF16) or 22 (KL_KV_E4M3). */
+ * n_q_heads is a multiple of n_kv_heads, any group size (a kv head's rows are read once for every eight query heads).
+ * Scores, the softmax and all sums are held in 32 bits; in the two products fp32 queries and the probabilities take part
+ * with 24 bits (KL_KV_BF16) or 22 (KL_KV_E4M3; fewer for elements of a query head below 2^-29 of its largest, and for
+ * positions whose probability times value scale is below 2^-29 of the largest such product). */
 kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type,
                              int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
                              const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,

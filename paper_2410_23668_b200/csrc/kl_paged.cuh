@@ -198,10 +198,11 @@ __device__ __forceinline__ void pg_check_starts(const PagedView& c, const PagedR
 // Per row and head: largest magnitude over the lanes (as whole numbers: the bits of a float; of bf16 rows two at a time in one
 // word), the exponent from its bits, one multiplication by a power of two per element (exact), rounding by the conversion
 // instruction.
-// Measured, 8 kv heads of 128: one bf16 row 2.1 us (launch and a chain of three loads); 8191 bf16 rows to e4m3 12.7 us, 62 % of
-// the copy rate.  What bounds it is instructions (some 75 per eight elements on average, half of the time) and a block's chain
+// Measured, 8 kv heads of 128: one bf16 row 2.1 us (launch and a chain of three loads); 8191 bf16 rows to e4m3 12.7 us, 61 % of
+// the copy rate.  What bounds it is instructions (some 96 per eight elements on average, half of the time) and a block's chain
 // of sequence, page and rows; two rows at a time, bf16 pairs and 32-bit strides took it there from 16.3 us.  Rows requested
-// asynchronously through shared memory: 12.1 us at best, not kept for that.
+// asynchronously through shared memory: 12.1 us at best, not kept for that.  8191 fp32 rows to e4m3 18.2 us (72 %), bf16 rows to a
+// bf16 cache 14.8 (70 %), fp32 rows to a bf16 cache 19.0 (82 %).
 constexpr int PW_THREADS = 128;   // (before the steps above: 16.3 us; 256 threads 17.6, 64 threads 25.0)
 template <class T, int HD, bool FP8>
 __global__ void __launch_bounds__(PW_THREADS, 1024 / PW_THREADS) kl_paged_append_kernel(const PagedView c, const PagedRows rows) {
@@ -436,7 +437,8 @@ __device__ __forceinline__ uint32_t pg_seq_of_row(const PagedView& c, const Page
 // of the next chunk lie -- a chain of dependent loads: sequence, position, page -- while the block copies this chunk's.  hd / 8
 // lanes share a (row, head, K or V), eight columns each: 16 bytes of a bf16 output, so that a warp's stores are contiguous
 // (16 columns of an e4m3 row per lane, 16-byte loads but 32-byte strides between the stores: 88 instead of 79 us).
-// Measured: 65537 e4m3 rows of 8 x 128 to bf16, 404 MB in all, 78 us, 80 % of the copy rate; 4096 bf16 rows 9.9 us.
+// Measured: 65537 e4m3 rows of 8 x 128 to bf16, 404 MB in all, 78.5 us, 80 % of the copy rate (to fp32 144 us, 72 %); 4096 bf16 rows
+// 10.0 us (to fp32 20.6).
 constexpr int PR_UNROLL = 4;   // pieces a lane has in flight (eight: no faster for e4m3, 13.2 instead of 9.9 us for 4096 bf16 rows)
 constexpr uint32_t PR_ITEMS = 4096;
 constexpr uint32_t PR_STARTS = 512;   // sequences whose first rows are kept in shared memory
@@ -631,8 +633,8 @@ __device__ __forceinline__ float ps_exact(const PagedView& c, const PagedSelect&
 }
 
 // Scores good to a known bound, on the tensor cores: kl_paged_topk_kernel computes exact ones where the bound leaves the
-// choice open, which is a page or two of thousands (64-bit scores for every page kept the 64-bit pipe and the selects in
-// front of it busy for five times as long as reading the bounds takes).
+// choice open, which is a few pages of thousands where pages differ (64-bit scores for every page kept the 64-bit pipe and the
+// selects in front of it busy for five times as long as reading the bounds takes).
 //   max(q lo, q hi) = min(q, 0) lo + max(q, 0) hi: with the bounds [lo | hi] of a page as a row of 2 hd numbers and
 //   [min(q, 0) | max(q, 0)] as columns it is one matrix product, pages x heads.  16 pages are the rows of mma.m16n8k16, up to
 //   eight heads its columns (the order of the 2 hd terms is free, so a lane takes 16 contiguous bytes of its two rows at a time).  Every warp takes an equal, contiguous range of
@@ -838,7 +840,11 @@ __global__ void __launch_bounds__(PsCfg<HD>::NW * 32, 1) kl_paged_score_kernel(c
 //   3. The chosen pages are put in order by a prefix sum over groups of 32.
 // The keys lie in shared memory (SMEM), or, beyond PT_KEYS pages, in the workspace.  A block's time is latency -- barriers, and
 // fetching its own instructions, each of which runs a few times only -- so the loops are not unrolled (eight keys per thread in
-// registers and everything unrolled took twice as long).  Measured: 5 us for 1024 pages, 4 to 10 us for 4096.
+// registers and everything unrolled took twice as long).  Measured: 5 us for 1024 pages, 4 to 11 us for 4096.
+// E is that of the (sequence, head)'s worst page.  One page of unknown score (a bound that is infinite) makes every page a
+// candidate, and so do equal pages; beyond PT_LIST of them a warp scores its candidates one after another.  Both calls together, 8 kv heads of
+// 128, 4 query heads each: one sequence of 4096 pages 675 us instead of 19, 32 of 1024 211 instead of 37; one page 64 times as loud as the
+// others 46 and 63.
 constexpr int PT_THREADS = 512;
 constexpr uint32_t PT_LIST = 128, PT_KEYS = 16384;
 template <bool SMEM>
@@ -1177,7 +1183,9 @@ constexpr uint32_t PA_MIN_TILES = 8;        // fewest tiles worth a block
 // EX: fp32 queries and outputs -- what 16-bit rounding leaves of q enters the score product too.
 // Warps and tile: as many warps as the registers allow, with at least two tiles each in the ring.  Measured (device time of
 // kl_paged_attention): 32 sequences of <= 32768 e4m3 positions, 8 heads per kv head, head size 128: 12 warps x 32 positions
-// 162 us, 11 x 32 168, 6 x 64 174, 12 x 16 183, 16 x 16 (128 registers) 215; 32 x 4096 bf16: 12 x 16 90, 8 x 16 98.
+// 162 us, 11 x 32 168, 6 x 64 174, 12 x 16 183, 16 x 16 (128 registers) 215; 32 x 4096 bf16, when probabilities had two parts: 12 x 16
+// 90, 8 x 16 98.  Registers spilled, in bytes: e4m3 of 128 with bf16 queries 44 (pages not of 16 rows: 92), head size 256 with fp32 queries 218 to
+// 298, bf16 of 64 with fp32 queries 16, bf16 of 256 with bf16 queries and pages not of 16 rows 8.
 template <int HD, bool FP8, bool EX>
 struct PaCfg {
     static constexpr int ROW = FP8 ? HD : 2 * HD;            // bytes of a cached row
@@ -1187,7 +1195,7 @@ struct PaCfg {
     static constexpr int RING = 204800 / (NW * 2 * TILE);
     static constexpr int ST = RING > 8 ? 8 : RING;           // tiles of a warp's ring
     // fp32 queries and a bf16 cache: the queries' third parts, 8 bytes of a lane per 16 columns, lie in shared memory where
-    // registers do not suffice (32 x 4096, 16 heads of 256: 178 us spilled, 101 us so, 100 us without a third part)
+    // registers do not suffice (32 x 4096, 16 heads of 256: 178 us spilled, 102 so, 100 without a third part)
     static constexpr bool QM = EX && !FP8 && HD == 256;
     static constexpr size_t SMEM = (size_t)NW * ST * (2 * TILE + 2 * TP + TP) + NW * 8 * 8 + 512 * 8 + PA_LENS * 4 + 256 + (QM ? NW * 32 * HD / 2 : 0);
     static_assert(ST >= 2 && SMEM <= 232448, "ring");
@@ -1195,11 +1203,15 @@ struct PaCfg {
 };
 
 // Short pairs are not shared between blocks, which makes the merge kernel unnecessary (3 us on the device, 3 us on the host) but
-// leaves a pair to one block: up to PA_WHOLE_FEW tiles always (one sequence, 8 kv heads of 128, bf16: 256 positions 8.3 us
-// against 8.8 shared, 512 9.8 against 9.0, 1024 12.3 against 9.4), up to PA_WHOLE_MANY tiles where there are as many
-// pairs as blocks (32 sequences: 512 positions 14.3 against 17.2, 1024 28.6 against 31.9; 128 sequences 54.6 against 58.6).  Longer
-// ones are shared although 32 x 2048 would gain 4 us too: lengths are not known on the host, and one long sequence among
-// short ones would leave its pairs to a block each.
+// leaves a pair to one block: up to PA_WHOLE_FEW tiles always, up to PA_WHOLE_MANY tiles where there are as many pairs as blocks.
+// Measured, whole against shared, 8 kv heads (4 of 256).  One sequence: bf16 of 128 (tiles of 16) 256 positions 8.7 us against 9.2, 384 9.5 against
+// 9.2, 512 10.4 against 9.4, 1024 13.6 against 9.8; bf16 of 256 (16) 256 10.5 against 10.7, 384 12.5 against 10.8, e4m3 12.5 against 11.4; e4m3 of 128
+// (32) 384 9.8 against 10.9, 512 10.7 against 10.4, 768 11.6 against 10.8; bf16 of 64 (32) 768 8.4 against 8.9, 1024 9.4 against 9.1, e4m3 8.9
+// against 9.2 and 9.9 against 9.4.  So 24 tiles are where the two meet, give or take a third, and cost 16 % at most where they are too many.
+// 32 sequences: bf16 of 128 512 positions 19.3 against 22.6, 1024 29.2 against 32.7; e4m3 of 128 2048 33.4 against 35.6; of 64 27.9 against
+// 31.1 (e4m3 23.1 against 25.1); bf16 of 256 1024 28.2 against 33.4; 128 sequences of 1024 95.0 against 101.2, e4m3 60.0 against 63.4.
+// Longer ones are shared although 32 x 2048 bf16 would gain 4 us too: lengths are not known on the host, and one long sequence
+// among short ones would leave its pairs to a block each.
 constexpr uint32_t PA_WHOLE_FEW = 24, PA_WHOLE_MANY = 64;
 
 // Positions of sequence s that take part, as tiles.
@@ -1250,10 +1262,11 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
 //     their own, so that f16 holds them whatever the scales (w * 2^7 at most 2^15).
 //   * Pages are looked up in units of UR rows (16 where the page size is a multiple of 16, else 4), one per lane, a batch of
 //     32 ahead of the copies.
-// What bounds it: bf16 caches, memory (32 x 4096 positions, 537 MB: 90 us, 93 % of the copy rate); e4m3 caches, half memory and
-// half instructions (32 sequences, 433 thousand positions, eight query heads per kv head, 894 MB: 162 us, 86 %: of some 800
-// instructions per 32 positions the conversions to f16 are a quarter); short calls, latency (1 x 333 positions: 8.7 us --
-// launch and the prefix of the lengths, look-ups, first rows and joining one after another, each a microsecond or two).
+// What bounds it: bf16 caches, memory (32 x 4096 positions, 537 MB: 91.8 us, 91 % of the copy rate; fp32 queries 97.9); e4m3 caches,
+// half memory and half instructions (32 sequences, 433 thousand positions, eight query heads per kv head, 894 MB: 161.5 us, 86 %: of some
+// 800 instructions per 32 positions the conversions to f16 are a quarter); short calls, latency (1 x 333 positions: 9.1 us --
+// launch and the prefix of the lengths, look-ups, first rows and joining one after another, each a microsecond or two); more
+// than eight query heads per kv head, the cache read once per eight (16: 32 x 4096 bf16 176 us, e4m3 107 against 56).
 template <int HD, bool FP8, int UR, bool EX>
 __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_kernel(const PagedView c, const PagedAttn a) {
     using Cfg = PaCfg<HD, FP8, EX>;
