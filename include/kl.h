@@ -476,6 +476,26 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
                                const int32_t* page_table_d, int64_t table_stride, uint32_t table_pages, uint32_t n_select, float* logits_d,
                                uint32_t batch, void* workspace_d, size_t workspace_bytes, void* stream);
 
+/* ---- Sampling without a handle, next to kl_argmax_advance: one token per row of logits from a given random number.
+ *   logits_d       fp32 [n_rows][vocab], rows row_stride (>= vocab) elements apart; vocab 1 .. 327680.  -infinity: a token that is
+ *                  not allowed; NaN counts as -infinity; the largest being +infinity: equal chances for all such tokens
+ *   uniforms_d     [n_rows] random numbers in [0, 1) (others count as the nearer end; NaN as 0)
+ *   temperature_d, top_k_d, top_p_d, min_p_d   one value per row each, or NULL (1, off, off, off).  Temperature not above 0 (or
+ *                  NaN): the largest logit, the lower token first.  top_k <= 0 or >= vocab, top_p not below 1 and min_p not above 0: off
+ * With w = exp((logit - largest) / temperature), tokens in order of falling logit, the lower token first among equals: those of
+ * rank below top_k stay; of these, those with less than top_p times their mass in front of them; of these, those with w >= min_p;
+ * the first of the order always.  Then, in order of the tokens' numbers, the first one at which the cumulative mass exceeds
+ * uniforms_d[row] times the mass of all that stayed.  Weights and sums are held in 64 bits.
+ *   tokens_d       [n_rows] the token, or -1 where no token is allowed
+ *   logprobs_d     [n_rows] natural logarithm of the probability it was drawn with (0 when there was no choice, -infinity with
+ *                  token -1), or NULL
+ *   positions_d    [n_rows] or NULL: incremented, as in kl_argmax_advance; a negative entry is an empty slot of the batch, whose token,
+ *                  log-probability and position stay; a row without a token keeps its position
+ * Launches one kernel on `stream`, allocates nothing, needs no workspace; calls may overlap. */
+kl_status kl_sample(const float* logits_d, int64_t row_stride, uint32_t n_rows, uint32_t vocab, const float* uniforms_d, const float* temperature_d,
+                    const int32_t* top_k_d, const float* top_p_d, const float* min_p_d, int32_t* tokens_d, float* logprobs_d, int32_t* positions_d,
+                    void* stream);
+
 const char* kl_status_string(kl_status s);
 
 /* Releases host-side state only (the arenas belong to the caller). */

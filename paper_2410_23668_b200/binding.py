@@ -44,7 +44,7 @@ EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_by
            "kl_set_dependent_launch", "kl_decode_greedy_host", "kl_decode_greedy", "kl_decode_greedy_tokens",
            "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights",
            "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention", "kl_paged_step_bytes",
-           "kl_decode_step_paged")
+           "kl_decode_step_paged", "kl_sample")
 
 
 class ModelDesc(C.Structure):
@@ -152,6 +152,8 @@ def lib():
     l.kl_paged_step_bytes.restype = i32
     l.kl_decode_step_paged.argtypes = [vp, vp, vp, vp, vp, i64, u32, u32, vp, u32, vp, C.c_size_t, vp]
     l.kl_decode_step_paged.restype = i32
+    l.kl_sample.argtypes = [vp, i64, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    l.kl_sample.restype = i32
     l.kl_status_string.argtypes = [i32]
     l.kl_status_string.restype = C.c_char_p
     l.kl_destroy.argtypes = [vp]
@@ -366,6 +368,30 @@ def kl_paged_attention(cache: PagedCache, q, out, positions, page_table, workspa
         lse_d = lse.data_ptr()
     rc = (_lib or lib()).kl_paged_attention(cache._ref, seqs, q.data_ptr(), out.data_ptr(), t, row, out_row, heads, scale, window, sel, n_select, lse_d,
                                             workspace.data_ptr(), workspace.numel(), _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
+
+
+def _per_row(t, dtype, n: int, dev: int, where: str) -> int:
+    """Address of one value per row; 0 without any."""
+    if t is None:
+        return 0
+    _need(t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == dev, where)
+    return t.data_ptr()
+
+
+def kl_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=None, positions=None, stream=None) -> None:
+    """logits fp32 [n_rows, vocab] (rows may be strided), uniforms fp32 [n_rows] -> tokens int32 [n_rows], logprobs fp32 [n_rows];
+    temperature, top_p, min_p fp32 and top_k int32, each [n_rows] or None (off); positions int32 [n_rows] are advanced."""
+    fn = "kl_sample"
+    n, vocab = logits.shape
+    row, one = logits.stride()
+    dev = logits.get_device()
+    _need(logits.dtype is _F32 and (one == 1 or vocab == 1) and dev >= 0 and dev == torch.cuda.current_device() and uniforms is not None and tokens is not None, fn)
+    rc = (_lib or lib()).kl_sample(logits.data_ptr(), row, n, vocab, _per_row(uniforms, _F32, n, dev, fn), _per_row(temperature, _F32, n, dev, fn),
+                                   _per_row(top_k, _I32, n, dev, fn), _per_row(top_p, _F32, n, dev, fn), _per_row(min_p, _F32, n, dev, fn),
+                                   _per_row(tokens, _I32, n, dev, fn), _per_row(logprobs, _F32, n, dev, fn), _per_row(positions, _I32, n, dev, fn),
+                                   0 if stream is None else stream.cuda_stream)
     if rc:
         raise KlError(rc, fn)
 

@@ -1,0 +1,746 @@
+// Sampling from given random numbers: temperature, top-k, top-p and min-p per row of logits (contract in include/kl.h).
+//
+// w_i = exp((x_i - max) / T).  Tokens in order of falling logit (the lower token first among equals): those of rank < k stay, of
+// these those with less than p of their mass in front of them, of these those with w >= min_p; then the first token, in order of
+// its number, at which the cumulative mass exceeds u times the mass of all that stayed.  Which token that is hangs on comparisons
+// of sums of up to some 10^5 weights: weights and sums are held in 64 bits, so that it is the token of the definition (32 bits
+// would err in one of ten draws from a flat row of 128256).
+//
+// One cluster of thread blocks = one row, whose logits are read once and stay in the blocks' shared memory.  A row is not sorted:
+//   * a histogram over (max - x) / T, 32 bins to the unit, finds the bin that a cut falls into -- by counts for top-k, by mass for
+//     top-p (a bin's members differ by 3 % at most, so their weights relative to the bin's largest fit whole numbers of 16 bits) --
+//     and only that bin's members are put in order, by the first block;
+//   * approximate masses only say which bin to look at: the mass in front of it and its own are then summed in 64 bits, and the
+//     neighbouring bin is taken where they say so;
+//   * a bin of too many members (equal logits) is cut again by their bits, until it is small or holds equal logits alone;
+//   * for k up to SP_LIST all that can stay goes to the first block, which finishes alone.
+#include "kl_device.cuh"
+
+#include <atomic>
+
+#include "../../include/kl.h"
+
+using namespace kl;
+
+namespace {
+
+constexpr int SP_THREADS = 512, SP_WARPS = SP_THREADS / 32;
+constexpr int SP_BINS = 2048;             // 32 to the unit of (max - x) / T; the last one holds all that lies further down
+constexpr float SP_BINS_PER_UNIT = 32.f;
+constexpr uint32_t SP_LIST = 2048;        // members of a bin that are put in order; also the largest k that one block finishes alone
+constexpr uint32_t SP_SLICE = 40960;      // most logits of a block
+constexpr int SP_MAX_CLUSTER = 8;
+constexpr uint32_t SP_SLICE_FEW = 16384;  // logits of a block beyond which a row is spread over more blocks
+
+struct SampleArgs {
+    const float* logits;
+    int64_t stride;
+    uint32_t n_rows, vocab, slice;
+    const float *uniforms, *temperature, *top_p, *min_p;
+    const int32_t* top_k;
+    int32_t *tokens, *positions;
+    float* logprobs;
+};
+
+// Shared memory behind the slice of logits.
+struct SampleShared {
+    uint64_t list[SP_LIST];               // first block: members of a bin, (complement of the key, token)
+    double listw[SP_LIST];
+    uint32_t hist[SP_BINS];
+    // written by every block of the cluster; two of each in turn, so that a block may go on while another still reads
+    double sums[2][SP_MAX_CLUSTER][3];
+    uint64_t best[2][SP_MAX_CLUSTER];
+    double warp_sum[SP_WARPS];
+    uint64_t warp_u64[SP_WARPS];
+    uint64_t cut;                         // first block: what the other blocks read
+    uint64_t found64[2];
+    uint32_t found, n_list;
+};
+
+__device__ __forceinline__ uint32_t cl_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cl_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cl_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Address of this block's shared variable in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t cl_map(const void* p, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cl_st64(uint32_t a, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
+__device__ __forceinline__ uint64_t cl_ld64(uint32_t a) { uint64_t v; asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory"); return v; }
+__device__ __forceinline__ uint4 cl_ld128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t cl_add(uint32_t a, uint32_t v) {
+    uint32_t old;
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
+    return old;
+}
+
+// Whole numbers in the order of the floats they stand for, and back.
+__device__ __forceinline__ uint32_t sp_key(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float sp_unkey(uint32_t k) { return __uint_as_float(k ^ ((int32_t)k < 0 ? 0x80000000u : 0xffffffffu)); }
+// Places in the order of falling logits: the lower the number, the earlier.
+__device__ __forceinline__ uint64_t sp_place(float x, uint32_t token) { return (uint64_t)(~sp_key(x)) << 32 | token; }
+
+__device__ __forceinline__ double sp_weight(float x, float m, double inv_t) {
+    if (x == m) return 1.0;
+    const double y = ((double)x - (double)m) * inv_t;
+    return y > -80.0 ? exp(y) : 0.0;   // (an empty token's y is -infinity; the rest is less than 2^-115 of the largest)
+}
+
+struct Sampler {
+    float* x;                 // this block's slice
+    SampleShared& s;
+    uint32_t base, n;         // first token of the slice, and how many
+    uint32_t rank, C, tid, warp, lane;
+    float m, scale;
+    double inv_t;
+    uint32_t turn;            // of the cluster's exchanges
+
+    __device__ __forceinline__ uint32_t bin(float v) const { return (uint32_t)fminf((m - v) * scale, (float)(SP_BINS - 1)); }
+
+    __device__ __forceinline__ double block_sum(double v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        __syncthreads();
+        if (lane == 0u) s.warp_sum[warp] = v;
+        __syncthreads();
+        double all = 0;
+#pragma unroll
+        for (int w = 0; w < SP_WARPS; ++w) all += s.warp_sum[w];
+        return all;
+    }
+    // Inclusive sum over the threads of the block.
+    __device__ __forceinline__ double block_scan(double v, double& before) {
+        double incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= (uint32_t)o) incl += y;
+        }
+        __syncthreads();
+        if (lane == 31u) s.warp_sum[warp] = incl;
+        __syncthreads();
+        double b = 0;
+        for (uint32_t w = 0; w < warp; ++w) b += s.warp_sum[w];
+        before = b + (incl - v);
+        return b + incl;
+    }
+    // Three sums over the cluster, the same in every block.
+    __device__ __forceinline__ void cluster_sums(double& a, double& b, double& c) {
+        a = block_sum(a);
+        b = block_sum(b);
+        c = block_sum(c);
+        const uint32_t half = turn++ & 1u;
+        if (tid < C) {
+            const uint32_t to = cl_map(&s.sums[half][rank][0], tid);
+            cl_st64(to, __double_as_longlong(a));
+            cl_st64(to + 8u, __double_as_longlong(b));
+            cl_st64(to + 16u, __double_as_longlong(c));
+        }
+        cl_sync();
+        a = b = c = 0;
+        for (uint32_t r = 0; r < C; ++r) {
+            a += s.sums[half][r][0];
+            b += s.sums[half][r][1];
+            c += s.sums[half][r][2];
+        }
+    }
+    __device__ __forceinline__ uint64_t block_min(uint64_t v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v = min(v, (uint64_t)__shfl_xor_sync(0xffffffffu, (unsigned long long)v, o));
+        __syncthreads();
+        if (lane == 0u) s.warp_u64[warp] = v;
+        __syncthreads();
+        uint64_t all = s.warp_u64[0];
+#pragma unroll
+        for (int w = 1; w < SP_WARPS; ++w) all = min(all, s.warp_u64[w]);
+        return all;
+    }
+    __device__ __forceinline__ uint64_t cluster_min(uint64_t v) {
+        v = block_min(v);
+        const uint32_t half = turn++ & 1u;
+        if (tid < C) cl_st64(cl_map(&s.best[half][rank], tid), v);
+        cl_sync();
+        for (uint32_t r = 0; r < C; ++r) v = min(v, s.best[half][r]);
+        return v;
+    }
+
+    // Histogram over the whole row, in every thread's hands: thread t gets bins 4 t .. 4 t + 3.
+    // value(x, token, bin) says which bin (< SP_BINS) and how much; false: left out.
+    template <class Value>
+    __device__ __forceinline__ void histogram(Value&& value, uint64_t (&mine)[4]) {
+        static_assert(SP_BINS == 4 * SP_THREADS, "four bins to a thread");
+        __syncthreads();
+        reinterpret_cast<uint4*>(s.hist)[tid] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        for (uint32_t i = tid; i < n; i += SP_THREADS) {
+            uint32_t b, v;
+            if (value(x[i], base + i, b, v)) atomicAdd(&s.hist[b], v);
+        }
+        cl_sync();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mine[q] = 0;
+        for (uint32_t r = 0; r < C; ++r) {
+            const uint4 h = cl_ld128(cl_map(&s.hist[4 * tid], r));
+            mine[0] += h.x; mine[1] += h.y; mine[2] += h.z; mine[3] += h.w;
+        }
+        cl_sync();   // the histograms may be cleared again
+    }
+
+    // The tokens that `in` names, in any order, in the first block's list; returns how many there are (more than SP_LIST: some are
+    // missing) in the first block, 0 in the others.  Between two calls lies another exchange of the cluster.
+    template <class In>
+    __device__ __forceinline__ uint32_t gather(In&& in) {
+        if (rank == 0u && tid == 0u) s.n_list = 0u;
+        cl_sync();
+        const uint32_t count = cl_map(&s.n_list, 0), list = cl_map(s.list, 0);
+        for (uint32_t i0 = 0; i0 < n; i0 += SP_THREADS) {
+            const uint32_t i = i0 + tid;
+            uint64_t p = 0;
+            bool yes = false;
+            if (i < n && x[i] > -INFINITY) {
+                p = sp_place(x[i], base + i);
+                yes = in(x[i], p);
+            }
+            const uint32_t who = __ballot_sync(0xffffffffu, yes);
+            if (!who) continue;
+            uint32_t at = 0;
+            if (lane == 0u) at = cl_add(count, __popc(who));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+            if (yes && at < SP_LIST) cl_st64(list + at * 8u, p);
+        }
+        cl_sync();
+        return rank == 0u ? s.n_list : 0u;
+    }
+    // Bitonic sort of the first n entries of the list, ascending (first block; n <= SP_LIST).
+    __device__ __forceinline__ uint32_t sort_list(uint32_t cnt) {
+        uint32_t len = 2;
+        while (len < cnt) len <<= 1;
+        for (uint32_t i = cnt + tid; i < len; i += SP_THREADS) s.list[i] = ~0ull;
+        __syncthreads();
+        for (uint32_t k = 2; k <= len; k <<= 1)
+            for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+                for (uint32_t t = tid; t < len / 2; t += SP_THREADS) {
+                    const uint32_t i = 2 * t - (t & (j - 1)), l = i + j;
+                    const uint64_t a = s.list[i], b = s.list[l];
+                    if ((a > b) == ((i & k) == 0u)) {
+                        s.list[i] = b;
+                        s.list[l] = a;
+                    }
+                }
+                __syncthreads();
+            }
+        return len;
+    }
+    __device__ __forceinline__ uint64_t broadcast(uint64_t v) {   // of the first block's thread 0
+        if (rank == 0u && tid == 0u) s.cut = v;
+        cl_sync();
+        v = cl_ld64(cl_map(&s.cut, 0));
+        cl_sync();
+        return v;
+    }
+};
+
+// The bin whose running sum first reaches `want` (> 0), the sum in front of it and its own; bins are four to a thread.  Whole block.
+__device__ __forceinline__ bool sp_find(Sampler& q, const uint64_t (&mine)[4], uint64_t want, uint32_t& bin, uint64_t& before, uint64_t& own) {
+    SampleShared& s = q.s;
+    const uint64_t sum = mine[0] + mine[1] + mine[2] + mine[3];
+    uint64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t y = __shfl_up_sync(0xffffffffu, (unsigned long long)incl, o);
+        if (q.lane >= (uint32_t)o) incl += y;
+    }
+    __syncthreads();
+    if (q.lane == 31u) s.warp_u64[q.warp] = incl;
+    if (q.tid == 0u) s.found = SP_BINS;
+    __syncthreads();
+    uint64_t b = 0;
+    for (uint32_t w = 0; w < q.warp; ++w) b += s.warp_u64[w];
+    uint64_t at = b + incl - sum;
+    if (at < want && want <= at + sum) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (at < want && want <= at + mine[i]) {
+                s.found = 4 * q.tid + i;
+                s.found64[0] = at;
+                s.found64[1] = mine[i];
+            }
+            at += mine[i];
+        }
+    }
+    __syncthreads();
+    bin = s.found;
+    before = s.found64[0];
+    own = s.found64[1];
+    __syncthreads();
+    return bin < SP_BINS;
+}
+
+// A run of places that a cut falls into: bin `b` of the row's first histogram, or the places lo .. hi.
+struct SampleRegion {
+    uint32_t b;           // SP_BINS: lo and hi say it
+    uint64_t lo, hi;
+    // -1: the token comes before the region, 0: it belongs to it, 1: behind it
+    __device__ __forceinline__ int side(const Sampler& q, float x, uint64_t place) const {
+        if (b < SP_BINS) {
+            const uint32_t at = q.bin(x);
+            return at < b ? -1 : at > b;
+        }
+        return place < lo ? -1 : place > hi;
+    }
+};
+
+// A region of too many tokens is cut into SP_BINS runs of places, 2^shift each from the first place that it holds.
+__device__ __forceinline__ void sp_split(Sampler& q, const SampleRegion& g, uint64_t& lo, uint64_t& hi, uint32_t& shift) {
+    uint64_t first = ~0ull, last = ~0ull;   // last: its complement
+    for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+        if (!(q.x[i] > -INFINITY)) continue;
+        const uint64_t p = sp_place(q.x[i], q.base + i);
+        if (g.side(q, q.x[i], p) == 0) {
+            first = min(first, p);
+            last = min(last, ~p);
+        }
+    }
+    lo = q.cluster_min(first);
+    hi = ~q.cluster_min(last);
+    shift = 0;
+    while (((hi - lo) >> shift) >= SP_BINS) ++shift;
+}
+
+// The place of rank k - 1 (ranks from zero): the last one that stays.
+__device__ __forceinline__ uint64_t sp_cut_by_rank(Sampler& q, SampleRegion g, uint64_t before, uint64_t own, uint64_t k) {
+    while (own > SP_LIST) {
+        uint64_t lo, hi, mine[4], b4;
+        uint32_t shift, bin;
+        sp_split(q, g, lo, hi, shift);
+        q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
+            const uint64_t p = sp_place(x, token);
+            if (!(x > -INFINITY) || p < lo || p > hi) return false;
+            b = (uint32_t)((p - lo) >> shift);
+            v = 1u;
+            return true;
+        }, mine);
+        if (!sp_find(q, mine, k - before, bin, b4, own)) return hi;
+        before += b4;
+        g.b = SP_BINS;
+        g.lo = lo + ((uint64_t)bin << shift);
+        g.hi = min(hi, g.lo + (((uint64_t)1 << shift) - 1u));
+    }
+    const uint32_t cnt = q.gather([&](float x, uint64_t p) { return g.side(q, x, p) == 0; });
+    uint64_t cut = 0;
+    if (q.rank == 0u) {   // own >= k - before >= 1
+        q.sort_list(cnt);
+        cut = q.s.list[min((uint32_t)(k - before), cnt) - 1u];
+    }
+    return q.broadcast(cut);
+}
+
+// The last place that stays when those stay with less than p of the mass of all places up to `cut` in front of them.
+__device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, double p) {
+    SampleShared& s = q.s;
+    uint64_t mine[4], before, own;
+    uint32_t bin;
+    // approximate masses, in units of 2^-43 of the largest weight: sums of at most 2^19 tokens stay below 2^62
+    q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
+        if (!(x > -INFINITY) || sp_place(x, token) > cut) return false;
+        const float t = fminf((q.m - x) * q.scale, (float)(SP_BINS - 1));
+        b = (uint32_t)t;
+        v = (uint32_t)(65536.f * exp2f((float)b * (1.4426950408889634f / SP_BINS_PER_UNIT) - t * (1.4426950408889634f / SP_BINS_PER_UNIT)));
+        return true;
+    }, mine);
+    uint64_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine[i] = (uint64_t)((double)mine[i] * exp2((4 * q.tid + i) * (-1.4426950408889634 / SP_BINS_PER_UNIT) + 27.0));
+    {
+        const double part = (double)(mine[0] + mine[1] + mine[2] + mine[3]);   // (rounded: approximate anyway)
+        all = (uint64_t)q.block_sum(part);
+    }
+    uint64_t want = (uint64_t)(p * (double)all);
+    if (want < 1ull) want = 1ull;
+    if (!sp_find(q, mine, want, bin, before, own)) bin = 0u;
+    double total = 0, goal = 0, front, inside;
+    SampleRegion g = {bin, 0, 0};
+    uint64_t lo = 0, hi = 0;   // of the runs of places that a region has been cut into, if it has
+    uint32_t shift = 0, last = SP_BINS - 1;
+    int went = 0;
+    bool settled = false;
+    for (;;) {
+        front = inside = 0;
+        double sum = 0;
+        for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+            const float x = q.x[i];
+            if (!(x > -INFINITY)) continue;
+            const uint64_t place = sp_place(x, q.base + i);
+            if (place > cut) continue;
+            const int side = g.side(q, x, place);
+            if (side > 0 && goal > 0) continue;
+            const double w = sp_weight(x, q.m, q.inv_t);
+            sum += w;
+            if (side < 0) front += w;
+            if (side == 0) inside += w;
+        }
+        q.cluster_sums(sum, front, inside);
+        if (goal == 0) {
+            total = sum;
+            goal = p * total;
+        }
+        // towards the region where the mass in front first reaches the goal; where two neighbours point at each other (their sums
+        // round apart) the one that was left again is taken
+        const int go = front >= goal ? -1 : front + inside < goal ? 1 : 0;
+        if (!settled && go != 0 && (go < 0 ? bin > 0u : bin < last)) {
+            settled = go == -went;
+            went = go;
+            bin += go;
+        } else {
+            uint32_t cnt = q.gather([&](float x, uint64_t place) { return place <= cut && g.side(q, x, place) == 0; });
+            cnt = (uint32_t)q.broadcast(cnt);
+            if (cnt <= SP_LIST) {
+                uint64_t end = 0;
+                if (q.rank == 0u) {
+                    q.sort_list(cnt);
+                    double w[SP_LIST / SP_THREADS], sum4 = 0, ahead;
+#pragma unroll
+                    for (uint32_t i = 0; i < SP_LIST / SP_THREADS; ++i) {
+                        const uint32_t at = q.tid * (SP_LIST / SP_THREADS) + i;
+                        w[i] = at < cnt ? sp_weight(sp_unkey(~(uint32_t)(s.list[at] >> 32)), q.m, q.inv_t) : 0.0;
+                        sum4 += w[i];
+                    }
+                    q.block_scan(sum4, ahead);
+                    uint32_t stay = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < SP_LIST / SP_THREADS; ++i) {
+                        const uint32_t at = q.tid * (SP_LIST / SP_THREADS) + i;
+                        if (at < cnt && front + ahead < goal) stay = at + 1u;
+                        ahead += w[i];
+                    }
+                    const uint32_t most = (uint32_t)~q.block_min(~(uint64_t)stay);
+                    end = cnt ? s.list[most ? most - 1u : 0u] : cut;
+                }
+                return q.broadcast(end);
+            }
+            sp_split(q, g, lo, hi, shift);
+            if (hi > cut) hi = cut;
+            went = 0;
+            settled = false;
+            const float first = sp_unkey(~(uint32_t)(lo >> 32));
+            q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
+                const uint64_t place = sp_place(x, token);
+                if (!(x > -INFINITY) || place < lo || place > hi) return false;
+                b = (uint32_t)((place - lo) >> shift);
+                v = (uint32_t)(65536.f * __expf((float)(((double)x - (double)first) * q.inv_t)));
+                return true;
+            }, mine);
+            last = (uint32_t)((hi - lo) >> shift);
+            const double unit = sp_weight(first, q.m, q.inv_t) / 65536.0;
+            want = unit > 0 ? (uint64_t)fmax(fmin((goal - front) / unit, 9e18), 1.0) : 1ull;
+            if (!sp_find(q, mine, want, bin, before, own)) bin = last;
+        }
+        if (hi) {
+            g.b = SP_BINS;
+            g.lo = lo + ((uint64_t)bin << shift);
+            g.hi = min(hi, g.lo + (((uint64_t)1 << shift) - 1u));
+        } else {
+            g.b = bin;
+        }
+    }
+}
+
+__device__ __forceinline__ void sp_write(const SampleArgs& a, uint32_t row, int32_t token, double w, double total) {
+    a.tokens[row] = token;
+    if (a.logprobs) a.logprobs[row] = token < 0 ? -INFINITY : (float)log(w / total);
+    if (a.positions && token >= 0) ++a.positions[row];
+}
+
+// The first block alone: `cnt` tokens in its list, of which the first k by rank stay.
+__device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, uint32_t row, uint32_t cnt, uint32_t k, double p, double min_p, double u) {
+    SampleShared& s = q.s;
+    constexpr uint32_t PER = SP_LIST / SP_THREADS;
+    q.sort_list(cnt);
+    cnt = min(cnt, k);
+    double w[PER], sum = 0, ahead;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t at = q.tid * PER + i;
+        w[i] = at < cnt ? sp_weight(sp_unkey(~(uint32_t)(s.list[at] >> 32)), q.m, q.inv_t) : 0.0;
+        sum += w[i];
+    }
+    q.block_scan(sum, ahead);
+    const double mass = q.block_sum(sum);
+    uint64_t item[PER];
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t at = q.tid * PER + i;
+        const bool stays = at < cnt && (at == 0u || ((p >= 1.0 || ahead < p * mass) && w[i] >= min_p));
+        item[i] = stays ? (uint64_t)(uint32_t)s.list[at] << 32 | at : ~0ull;
+        ahead += w[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t at = q.tid * PER + i;
+        if (at < cnt) {
+            s.list[at] = item[i];
+            s.listw[at] = w[i];
+        }
+    }
+    __syncthreads();
+    q.sort_list(cnt);   // by token
+    sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t at = q.tid * PER + i;
+        item[i] = at < cnt ? s.list[at] : ~0ull;
+        w[i] = item[i] != ~0ull ? s.listw[(uint32_t)item[i]] : 0.0;
+        sum += w[i];
+    }
+    q.block_scan(sum, ahead);
+    const double total = q.block_sum(sum), goal = u * total;
+    // the first token at which the running mass exceeds the goal; the last one of any mass where rounding lets none
+    uint64_t first = ~0ull, last = ~0ull;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        ahead += w[i];
+        if (w[i] > 0) {
+            if (ahead > goal) first = min(first, item[i]);
+            last = min(last, ~item[i]);
+        }
+    }
+    first = q.block_min(first);
+    last = ~q.block_min(last);
+    if (q.tid == 0u) {
+        const uint64_t it = first != ~0ull ? first : last;
+        sp_write(a, row, (int32_t)(it >> 32), s.listw[(uint32_t)it], total);
+    }
+}
+
+__global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs a) {
+    extern __shared__ __align__(16) uint8_t sp_smem[];
+    SampleShared& s = *reinterpret_cast<SampleShared*>(sp_smem);
+    const uint32_t C = cl_size(), row = blockIdx.x / C;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // every block of the cluster has begun: see the wait
+    griddep_launch();
+    griddep_wait();
+    Sampler q = {reinterpret_cast<float*>(sp_smem + sizeof(SampleShared)), s};
+    q.rank = cl_rank();
+    q.C = C;
+    q.tid = threadIdx.x;
+    q.warp = threadIdx.x >> 5;
+    q.lane = threadIdx.x & 31u;
+    q.base = q.rank * a.slice;
+    q.n = q.base < a.vocab ? min(a.slice, a.vocab - q.base) : 0u;
+    q.turn = 0;
+    const bool idle = a.positions && a.positions[row] < 0;   // an empty slot of the batch: the same for the whole cluster
+    const float T = a.temperature ? a.temperature[row] : 1.f;
+    const float top_p = a.top_p ? a.top_p[row] : 1.f, min_pf = a.min_p ? a.min_p[row] : 0.f;
+    int32_t top_k = a.top_k ? a.top_k[row] : 0;
+    const double p = top_p < 1.f ? (double)top_p : 1.0, min_p = min_pf > 0.f ? (double)min_pf : 0.0;
+    if (!(T > 0.f) || p <= 0.0 || min_p > 1.0) top_k = 1;
+    const double u = a.uniforms[row] > 0.f ? (double)fminf(a.uniforms[row], 1.f) : 0.0;
+
+    uint64_t best = ~0ull;   // the first place of the row
+    if (!idle) {
+        const float* src = a.logits + (int64_t)row * a.stride + q.base;
+        constexpr int U = 8;
+        for (uint32_t i0 = q.tid; i0 < q.n; i0 += SP_THREADS * U) {
+            float v[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) v[j] = i0 + j * SP_THREADS < q.n ? src[i0 + j * SP_THREADS] : 0.f;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const uint32_t i = i0 + j * SP_THREADS;
+                if (i < q.n) {
+                    const float y = v[j] == v[j] ? v[j] + 0.f : -INFINITY;   // NaN: no token; -0 counts as 0
+                    q.x[i] = y;
+                    if (y > -INFINITY) best = min(best, sp_place(y, q.base + i));
+                }
+            }
+        }
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (idle) return;
+    best = q.cluster_min(best);
+    if (best == ~0ull || top_k == 1) {   // nothing to choose from, or nothing to choose
+        if (q.rank == 0u && q.tid == 0u) sp_write(a, row, best == ~0ull ? -1 : (int32_t)(uint32_t)best, 1.0, 1.0);
+        return;
+    }
+    q.m = sp_unkey(~(uint32_t)(best >> 32));
+    if (q.m == INFINITY) {   // equal chances for the infinite ones, none for the rest
+        for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) q.x[i] = q.x[i] == INFINITY ? 0.f : -INFINITY;
+        q.m = 0.f;
+    }
+    q.scale = SP_BINS_PER_UNIT / T;
+    q.inv_t = 1.0 / (double)T;
+
+    uint64_t cut = ~0ull - 1ull;   // the last place that stays
+    if (top_k > 0 && (uint32_t)top_k < a.vocab) {
+        uint64_t mine[4], before, own;
+        uint32_t bin;
+        q.histogram([&](float x, uint32_t, uint32_t& b, uint32_t& v) {
+            if (!(x > -INFINITY)) return false;
+            b = q.bin(x);
+            v = 1u;
+            return true;
+        }, mine);
+        const bool enough = sp_find(q, mine, (uint64_t)top_k, bin, before, own);
+        if (enough && before + own <= SP_LIST) {
+            const uint32_t cnt = q.gather([&](float x, uint64_t) { return q.bin(x) <= bin; });
+            if (q.rank == 0u) sp_finish_list(q, a, row, cnt, (uint32_t)top_k, p, min_p, u);
+            return;
+        }
+        if (enough) cut = sp_cut_by_rank(q, {bin, 0, 0}, before, own, (uint64_t)top_k);
+    }
+    if (p < 1.0) cut = sp_cut_by_mass(q, cut, p);
+
+    // the draw: sums of the runs of tokens of every warp, then the run that the goal falls into once more
+    auto weight = [&](uint32_t i) {
+        const float x = q.x[i];
+        if (!(x > -INFINITY) || sp_place(x, q.base + i) > cut) return 0.0;
+        const double w = sp_weight(x, q.m, q.inv_t);
+        return w >= min_p ? w : 0.0;
+    };
+    const uint32_t run = (q.n + SP_WARPS * 32u - 1u) / (SP_WARPS * 32u) * 32u, i0 = q.warp * run, i1 = min(q.n, i0 + run);
+    double mine = 0;
+    for (uint32_t i = i0 + q.lane; i < i1; i += 32u) mine += weight(i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    __syncthreads();
+    if (q.lane == 0u) s.warp_sum[q.warp] = mine;
+    __syncthreads();
+    double sums[SP_WARPS], own = 0;
+#pragma unroll
+    for (int w = 0; w < SP_WARPS; ++w) own += sums[w] = s.warp_sum[w];
+    if (q.tid < C) cl_st64(cl_map(&s.sums[q.turn & 1u][q.rank][0], q.tid), __double_as_longlong(own));
+    cl_sync();
+    double total = 0;
+    for (uint32_t r = 0; r < C; ++r) total += s.sums[q.turn & 1u][r][0];
+    const double goal = u * total;
+    // the first part whose end lies beyond the goal, else the last one that has any mass
+    double ahead = 0, at = 0, front = 0;
+    uint32_t who = C;
+    bool beyond = false;
+    for (uint32_t r = 0; r < C; ++r) {
+        const double x = s.sums[q.turn & 1u][r][0];
+        if (x > 0 && !beyond) {
+            who = r;
+            front = at;
+            beyond = at + x > goal;
+        }
+        at += x;
+    }
+    if (who != q.rank) return;
+    at = front;
+    beyond = false;
+    uint32_t in = 0;
+#pragma unroll
+    for (int w = 0; w < SP_WARPS; ++w) {
+        if (sums[w] > 0 && !beyond) {
+            in = w;
+            ahead = at;
+            beyond = at + sums[w] > goal;
+        }
+        at += sums[w];
+    }
+    if (in != q.warp) return;
+    // every lane a run of its own of the warp's (read from a place that goes by the lane, so that the banks differ)
+    const uint32_t part = run / 32u, j0 = i0 + q.lane * part;
+    double sum = 0;
+    for (uint32_t j = 0; j < part; ++j) {
+        uint32_t i = j + q.lane % part;
+        i = j0 + (i >= part ? i - part : i);
+        if (i < i1) sum += weight(i);
+    }
+    auto pick = [&](double v, double start, double& before_it) {   // the lane that the goal falls into
+        double incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (q.lane >= (uint32_t)o) incl += y;
+        }
+        const uint32_t any = __ballot_sync(0xffffffffu, v > 0), over = __ballot_sync(0xffffffffu, v > 0 && start + incl > goal);
+        const uint32_t l = over ? __ffs(over) - 1 : any ? 31 - __clz(any) : 32;
+        before_it = start + __shfl_sync(0xffffffffu, incl - v, l & 31u);
+        return over ? l : l | 64u;   // 64: none lies beyond the goal
+    };
+    double start;
+    const uint32_t l = pick(sum, ahead, start) & 31u;
+    const uint32_t k0 = i0 + l * part, k1 = min(i1, k0 + part);
+    uint32_t token = 0;
+    double w_token = 1;
+    for (uint32_t k = k0; k < k1; k += 32u) {
+        const double w = k + q.lane < k1 ? weight(k + q.lane) : 0.0;
+        double before_it;
+        const uint32_t got = pick(w, start, before_it);
+        if ((got & 63u) < 32u) {
+            token = q.base + k + (got & 31u);
+            w_token = __shfl_sync(0xffffffffu, w, got & 31u);
+        }
+        if (got < 32u) break;
+        double all = w;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        start += all;
+    }
+    if (q.lane == 0u) sp_write(a, row, (int32_t)token, w_token, total);
+}
+
+}  // namespace
+
+extern "C" kl_status kl_sample(const float* logits_d, int64_t row_stride, uint32_t n_rows, uint32_t vocab, const float* uniforms_d,
+                               const float* temperature_d, const int32_t* top_k_d, const float* top_p_d, const float* min_p_d, int32_t* tokens_d,
+                               float* logprobs_d, int32_t* positions_d, void* stream) {
+    if (n_rows == 0) return KL_OK;
+    if (!logits_d || !uniforms_d || !tokens_d || vocab == 0) return KL_ERR_INVALID_ARG;
+    if (n_rows > 1 && (row_stride < (int64_t)vocab || row_stride > (INT64_MAX >> 34))) return KL_ERR_INVALID_ARG;
+    if (vocab > SP_SLICE * SP_MAX_CLUSTER || n_rows > (1u << 24)) return KL_ERR_UNSUPPORTED_SHAPE;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return KL_ERR_CUDA;
+    // blocks of a row: as many as hold it, and while the GPU is not full, twice as many as long as each has SP_SLICE_FEW / 8 logits to do
+    uint32_t C = 1;
+    while (C < SP_MAX_CLUSTER && vocab > (uint64_t)C * SP_SLICE_FEW) C *= 2;
+    while (C < SP_MAX_CLUSTER && (uint64_t)n_rows * C * 2 <= (uint64_t)sms && vocab >= C * 2 * (SP_SLICE_FEW / 8)) C *= 2;
+    SampleArgs a;
+    a.logits = logits_d;
+    a.stride = row_stride;
+    a.n_rows = n_rows;
+    a.vocab = vocab;
+    a.slice = (vocab + C - 1) / C;
+    a.uniforms = uniforms_d;
+    a.temperature = temperature_d;
+    a.top_p = top_p_d;
+    a.min_p = min_p_d;
+    a.top_k = top_k_d;
+    a.tokens = tokens_d;
+    a.positions = positions_d;
+    a.logprobs = logprobs_d;
+    static std::atomic<uint64_t> done{0};   // one bit per device whose kernel attribute is set
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (!bit || !(done.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(kl_sample_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(SampleShared) + SP_SLICE * 4)) != cudaSuccess)
+            return KL_ERR_CUDA;
+        done.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n_rows * C);
+    cfg.blockDim = dim3(SP_THREADS);
+    cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)a.slice * 4;
+    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kl_sample_kernel, a) == cudaSuccess ? KL_OK : KL_ERR_CUDA;
+}
