@@ -476,6 +476,27 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
                                const int32_t* page_table_d, int64_t table_stride, uint32_t table_pages, uint32_t n_select, float* logits_d,
                                uint32_t batch, void* workspace_d, size_t workspace_bytes, void* stream);
 
+/* ---- Drafted tokens on a paged cache: several new tokens of a sequence in one pass, a chain or a tree of them.
+ *
+ * The new tokens of sequence s are rows row_starts_d[s] .. row_starts_d[s + 1] - 1 of a call (row_starts_d == NULL: one row per
+ * sequence), and lie at positions positions_d[s], positions_d[s] + 1, ... of it, as in kl_paged_append; positions before
+ * positions_d[s] are the sequence's cached ones, a negative entry is an empty slot.  row_positions_d ([n_rows] or NULL) says
+ * where the tokens stand in the text, which for the nodes of a tree is not where they lie: cached positions plus depth. */
+
+/* kl_paged_append with the position rotation on the way: k_rows_d are keys before their rotation, and with q_d the queries of the
+ * same rows are turned in the same launch.  Pair (i, i + head_dim / 2) of a key or query turns by the angle position * freqs_d[i]
+ * (freqs_d: fp64 [head_dim / 2], device; theta^(-2 i / head_dim) gives the rotation of kl_decode_step), position = row_positions_d
+ * of its row, or where the row lies.
+ *   q_d, q_out_d   [n_rows][n_q_heads][head_dim] of row_type, rows q_row_stride and q_out_row_stride elements apart (16-byte
+ *                  alignment as above); both NULL: no queries; q_out_d == q_d with equal strides turns them in place
+ * Angles, and the products of a key, are held in 64 bits, and a key is rounded once, to what the cache holds; queries turn in 32
+ * bits.  Values are written as they are.  Query rows that belong to no sequence or to an empty slot are left as they were.
+ * Everything else is as in kl_paged_append. */
+kl_status kl_paged_append_rotated(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                                  const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                                  const double* freqs_d, const int32_t* row_positions_d, const void* q_d, void* q_out_d, int64_t q_row_stride,
+                                  int64_t q_out_row_stride, uint32_t n_q_heads, int32_t* status_d, void* stream);
+
 /* ---- Sampling without a handle, next to kl_argmax_advance: one token per row of logits from a given random number.
  *   logits_d       fp32 [n_rows][vocab], rows row_stride (>= vocab) elements apart; vocab 1 .. 327680.  -infinity: a token that is
  *                  not allowed; NaN counts as -infinity; the largest being +infinity: equal chances for all such tokens

@@ -44,7 +44,7 @@ EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_by
            "kl_set_dependent_launch", "kl_decode_greedy_host", "kl_decode_greedy", "kl_decode_greedy_tokens",
            "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights",
            "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention", "kl_paged_step_bytes",
-           "kl_decode_step_paged", "kl_sample")
+           "kl_decode_step_paged", "kl_paged_append_rotated", "kl_sample")
 
 
 class ModelDesc(C.Structure):
@@ -152,6 +152,8 @@ def lib():
     l.kl_paged_step_bytes.restype = i32
     l.kl_decode_step_paged.argtypes = [vp, vp, vp, vp, vp, i64, u32, u32, vp, u32, vp, C.c_size_t, vp]
     l.kl_decode_step_paged.restype = i32
+    l.kl_paged_append_rotated.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp, vp, vp, i64, i64, u32, vp, vp]
+    l.kl_paged_append_rotated.restype = i32
     l.kl_sample.argtypes = [vp, i64, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     l.kl_sample.restype = i32
     l.kl_status_string.argtypes = [i32]
@@ -368,6 +370,41 @@ def kl_paged_attention(cache: PagedCache, q, out, positions, page_table, workspa
         lse_d = lse.data_ptr()
     rc = (_lib or lib()).kl_paged_attention(cache._ref, seqs, q.data_ptr(), out.data_ptr(), t, row, out_row, heads, scale, window, sel, n_select, lse_d,
                                             workspace.data_ptr(), workspace.numel(), _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
+
+
+def _starts(row_starts, n: int, dev: int, where: str) -> int:
+    if row_starts is None:
+        return 0
+    _need(row_starts.dtype is _I32 and row_starts.is_contiguous() and row_starts.numel() == n + 1 and row_starts.get_device() == dev, where)
+    return row_starts.data_ptr()
+
+
+def kl_paged_append_rotated(cache: PagedCache, k_rows, v_rows, positions, page_table, freqs, row_starts=None, row_positions=None, q=None, q_out=None,
+                            status=None, stream=None) -> None:
+    """kl_paged_append of keys that are turned on the way; freqs fp64 [head_dim / 2], row_positions int32 [n_rows] or None; q and q_out
+    [n_rows, n_q_heads, head_dim] of the rows' type: queries turned too (q_out may be q)."""
+    fn = "kl_paged_append_rotated"
+    dev, d = _here(cache), cache.desc
+    rows, heads, width = shape = k_rows.shape
+    k_row, k_head, k_one = k_rows.stride()
+    v_row, v_head, v_one = v_rows.stride()
+    t = _ROW_TYPES.get(k_rows.dtype)
+    _need(t is not None and v_rows.dtype is k_rows.dtype and v_rows.shape == shape and heads == d.n_kv_heads and width == d.head_dim and k_one == 1 and
+          v_one == 1 and (heads == 1 or (k_head == width and v_head == width)) and k_rows.get_device() == dev and v_rows.get_device() == dev, fn)
+    _need(freqs.dtype is torch.float64 and freqs.numel() * 2 == width and freqs.is_contiguous() and freqs.get_device() == dev, fn)
+    seqs, n = _paged_seqs(dev, positions, page_table, fn)
+    q_at = o_at = q_row = o_row = nq = 0
+    if q is not None or q_out is not None:
+        _need(q is not None and q_out is not None, fn)
+        q_type, q_row, nq = _paged_queries(cache, dev, q, rows, fn)
+        o_type, o_row, o_heads = _paged_queries(cache, dev, q_out, rows, fn)
+        q_at, o_at = q.data_ptr(), q_out.data_ptr()
+        _need(q_type == t and o_type == t and o_heads == nq and (q_at != o_at or q_row == o_row or rows < 2), fn)
+    rc = (_lib or lib()).kl_paged_append_rotated(cache._ref, seqs, _starts(row_starts, n, dev, fn), rows, k_rows.data_ptr(), v_rows.data_ptr(), t, k_row, v_row,
+                                                 freqs.data_ptr(), _per_row(row_positions, _I32, rows, dev, fn), q_at, o_at, q_row, o_row, nq,
+                                                 _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
     if rc:
         raise KlError(rc, fn)
 

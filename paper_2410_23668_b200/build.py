@@ -9,8 +9,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libkl.so"
-SOURCES = [CSRC / "kl.cu", CSRC / "kl_paged.cu", CSRC / "kl_sample.cu"]
-HEADERS = [CSRC / "kl_device.cuh", CSRC / "kl_attention_tc.cuh", CSRC / "kl_batched.cuh", CSRC / "kl_bloop.cuh", CSRC / "kl_paged.cuh", CSRC / "kl_paged_internal.h",
+SOURCES = [CSRC / "kl.cu", CSRC / "kl_paged.cu", CSRC / "kl_drafted.cu", CSRC / "kl_sample.cu"]
+HEADERS = [CSRC / "kl_device.cuh", CSRC / "kl_attention_tc.cuh", CSRC / "kl_batched.cuh", CSRC / "kl_bloop.cuh", CSRC / "kl_paged.cuh", CSRC / "kl_paged_internal.h", CSRC / "kl_paged_common.cuh", CSRC / "kl_paged_host.h", CSRC / "kl_drafted.cuh",
            PKG.parent / "include" / "kl.h"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]

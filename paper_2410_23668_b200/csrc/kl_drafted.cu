@@ -1,0 +1,83 @@
+// Host side of the operators for drafted tokens on a paged cache (contracts in include/kl.h, kernels in kl_drafted.cuh).
+#include "kl_drafted.cuh"
+
+#include <math.h>
+
+#include "kl_paged_host.h"
+
+using namespace kl;
+
+namespace {
+
+template <class T, int HD>
+kl_status launch_rotate(const PagedView& v, const PagedRows& r, const RotateArgs& a, unsigned blocks, PagedOrder order) {
+    constexpr size_t smem = rt_smem_bytes<HD>();
+    static_assert(smem <= 48 * 1024, "no attribute needed");
+    return v.fp8 ? launch(kl_paged_append_rotated_kernel<T, HD, true>, dim3(blocks), RT_THREADS, smem, order, v, r, a)
+                 : launch(kl_paged_append_rotated_kernel<T, HD, false>, dim3(blocks), RT_THREADS, smem, order, v, r, a);
+}
+
+int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms;
+}
+
+// Queries of new rows, or what takes their place in the output.
+kl_status check_row_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_rows) {
+    return check_queries(c, q, type, stride, n_q_heads, n_rows);
+}
+
+}  // namespace
+
+extern "C" {
+
+kl_status kl_paged_append_rotated(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows,
+                                  const void* k_rows_d, const void* v_rows_d, int row_type, int64_t k_row_stride, int64_t v_row_stride,
+                                  const double* freqs_d, const int32_t* row_positions_d, const void* q_d, void* q_out_d, int64_t q_row_stride,
+                                  int64_t q_out_row_stride, uint32_t n_q_heads, int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
+    if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
+    if (!freqs_d || ((uintptr_t)freqs_d & 7u) || (q_d != nullptr) != (q_out_d != nullptr)) return KL_ERR_INVALID_ARG;
+    if (q_d) {
+        if ((rc = check_row_queries(cache, q_d, row_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+        if ((rc = check_row_queries(cache, q_out_d, row_type, q_out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+    }
+    const int sms = sm_count();
+    if (sms <= 0) return KL_ERR_CUDA;
+    const uint64_t units = row_starts_d ? (uint64_t)n_rows / cache->page_size + 2ull * seqs->n_seqs : seqs->n_seqs;
+    RotateArgs a = {};
+    a.freqs = freqs_d;
+    a.row_positions = row_positions_d;
+    // kv heads of a block: up to eight share the angles of their rows, fewer where that leaves SMs without a block
+    a.heads = 8;
+    while (a.heads > 1 && (a.heads > cache->n_kv_heads || units * ((cache->n_kv_heads + a.heads - 1) / a.heads) < 2ull * sms)) a.heads /= 2;
+    a.head_groups = (cache->n_kv_heads + a.heads - 1) / a.heads;
+    uint64_t blocks = units * a.head_groups;
+    a.q_groups = 1;
+    if (q_d) {
+        a.q = (const uint8_t*)q_d;
+        a.q_out = (uint8_t*)q_out_d;
+        a.q_stride = q_row_stride * elem(row_type);
+        a.q_out_stride = q_out_row_stride * elem(row_type);
+        a.nq = n_q_heads;
+        const uint64_t runs = (n_rows + RT_ROWS - 1) / RT_ROWS;
+        a.q_heads = n_q_heads;
+        while (a.q_heads > 4 && runs * ((n_q_heads + a.q_heads - 1) / a.q_heads) < 2ull * sms) a.q_heads = (a.q_heads + 1) / 2;
+        a.q_groups = (n_q_heads + a.q_heads - 1) / a.q_heads;
+        blocks += runs * a.q_groups;
+    }
+    if (blocks > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;
+    a.kv_blocks = (uint32_t)(units * a.head_groups);
+    const PagedView v = view(cache, seqs, status_d);
+    const PagedRows r = rows_of(row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride);
+    const PagedOrder order = {stream, true};
+    const bool f32 = row_type == KL_F32;
+    if (v.hd == 64) return f32 ? launch_rotate<float, 64>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 64>(v, r, a, (unsigned)blocks, order);
+    if (v.hd == 128) return f32 ? launch_rotate<float, 128>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 128>(v, r, a, (unsigned)blocks, order);
+    return f32 ? launch_rotate<float, 256>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 256>(v, r, a, (unsigned)blocks, order);
+}
+
+}  // extern "C"
