@@ -497,6 +497,33 @@ kl_status kl_paged_append_rotated(const kl_paged_cache* cache, const kl_paged_se
                                   const double* freqs_d, const int32_t* row_positions_d, const void* q_d, void* q_out_d, int64_t q_row_stride,
                                   int64_t q_out_row_stride, uint32_t n_q_heads, int32_t* status_d, void* stream);
 
+/* Bytes of workspace kl_paged_tree_attention needs (256-byte aligned, need not be cleared; calls that may run at the same time --
+ * graphs captured from them included -- need workspaces of their own). */
+kl_status kl_paged_tree_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, size_t* bytes);
+
+/* Attention of all new tokens of every sequence, whose rows the cache holds already (kl_paged_append_rotated with the same seqs and
+ * row_starts_d, or kl_paged_append): out[r][h] = sum_p softmax_p(scale * q[r][h] . k_p) v_p over the positions that the token of
+ * row r, number i of its sequence, sees:
+ *   - of the cached positions p < positions_d[s], all (window == 0), or those with p < n_sinks or p > at - window, at being
+ *     row_positions_d[r] (positions_d[s] where that is larger; without row_positions_d: positions_d[s] + i).  Pages that hold neither
+ *     a first position nor one behind positions_d[s] - window are not looked up (their entries may name no page).  n_sinks
+ *     means nothing without a window.
+ *   - of the sequence's new tokens, those j whose bit is set in the row's mask (mask_d: [n_rows][mask_words] words of 32 bits, bit j % 32
+ *     of word j / 32; bits behind the sequence's last token, and words that are not there, name nothing).  Without mask_d: all j <= i, with a
+ *     window those with i - j < window.
+ * window = W and one row per sequence is a decode step with a sliding window and n_sinks first positions that stay visible.
+ * q_d and out_d: bf16 [n_rows][n_q_heads][head_dim] (KL_F32: KL_ERR_UNSUPPORTED_SHAPE), rows q_row_stride and out_row_stride elements
+ * apart; scale <= 0: 1 / sqrt(head_dim); lse_d as in kl_paged_attention, [n_rows][n_q_heads].  A token that sees nothing gets zeros, and
+ * -inf; rows that belong to no sequence or to an empty slot are left as they were.  Any number of new tokens and any group size; a
+ * cached row is read once for every 128 (token, query head) pairs of its kv head.  What a token does not see has no part in its result,
+ * whatever it holds; a token that sees an infinity or NaN gets no number in the columns it reaches.
+ * Scores, the softmax and all sums are held in 32 bits; in the second product a probability takes part with 16 bits (KL_KV_BF16) or 11
+ * (KL_KV_E4M3; fewer for positions whose probability times value scale is below 2^-24 of the largest value scale of the sequence). */
+kl_status kl_paged_tree_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows, const void* q_d,
+                                  void* out_d, int q_type, int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
+                                  uint32_t n_sinks, const int32_t* row_positions_d, const uint32_t* mask_d, uint32_t mask_words, float* lse_d,
+                                  void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream);
+
 /* ---- Sampling without a handle, next to kl_argmax_advance: one token per row of logits from a given random number.
  *   logits_d       fp32 [n_rows][vocab], rows row_stride (>= vocab) elements apart; vocab 1 .. 327680.  -infinity: a token that is
  *                  not allowed; NaN counts as -infinity; the largest being +infinity: equal chances for all such tokens

@@ -44,7 +44,7 @@ EXPORTS = ("kl_workspace_bytes", "kl_create", "kl_load_weights", "kl_kv_cache_by
            "kl_set_dependent_launch", "kl_decode_greedy_host", "kl_decode_greedy", "kl_decode_greedy_tokens",
            "kl_decode_greedy_tokens_host", "kl_debug_set_step", "kl_debug_set_jitter", "kl_load_expert_weights",
            "kl_paged_append", "kl_paged_read", "kl_paged_workspace_bytes", "kl_paged_select", "kl_paged_attention", "kl_paged_step_bytes",
-           "kl_decode_step_paged", "kl_paged_append_rotated", "kl_sample")
+           "kl_decode_step_paged", "kl_paged_append_rotated", "kl_paged_tree_workspace_bytes", "kl_paged_tree_attention", "kl_sample")
 
 
 class ModelDesc(C.Structure):
@@ -154,6 +154,10 @@ def lib():
     l.kl_decode_step_paged.restype = i32
     l.kl_paged_append_rotated.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, vp, vp, vp, vp, i64, i64, u32, vp, vp]
     l.kl_paged_append_rotated.restype = i32
+    l.kl_paged_tree_workspace_bytes.argtypes = [pc, u32, C.POINTER(C.c_size_t)]
+    l.kl_paged_tree_workspace_bytes.restype = i32
+    l.kl_paged_tree_attention.argtypes = [pc, ps, vp, u32, vp, vp, C.c_int, i64, i64, u32, C.c_float, u32, u32, vp, vp, u32, vp, vp, C.c_size_t, vp, vp]
+    l.kl_paged_tree_attention.restype = i32
     l.kl_sample.argtypes = [vp, i64, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     l.kl_sample.restype = i32
     l.kl_status_string.argtypes = [i32]
@@ -405,6 +409,39 @@ def kl_paged_append_rotated(cache: PagedCache, k_rows, v_rows, positions, page_t
     rc = (_lib or lib()).kl_paged_append_rotated(cache._ref, seqs, _starts(row_starts, n, dev, fn), rows, k_rows.data_ptr(), v_rows.data_ptr(), t, k_row, v_row,
                                                  freqs.data_ptr(), _per_row(row_positions, _I32, rows, dev, fn), q_at, o_at, q_row, o_row, nq,
                                                  _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
+    if rc:
+        raise KlError(rc, fn)
+
+
+def kl_paged_tree_workspace_bytes(cache: PagedCache, n_q_heads: int) -> int:
+    b = C.c_size_t()
+    _check(lib().kl_paged_tree_workspace_bytes(cache._ref, n_q_heads, C.byref(b)), "kl_paged_tree_workspace_bytes")
+    return b.value
+
+
+def kl_paged_tree_attention(cache: PagedCache, q, out, positions, page_table, workspace, row_starts=None, row_positions=None, mask=None, scale: float = 0.0,
+                            window: int = 0, n_sinks: int = 0, lse=None, status=None, stream=None) -> None:
+    """q, out bf16 [n_rows, n_q_heads, head_dim]; row_starts int32 [n_seqs + 1] or None (one row per sequence), row_positions int32
+    [n_rows] or None, mask int32 [n_rows, words] or None (a chain); lse fp32 [n_rows, n_q_heads]."""
+    fn = "kl_paged_tree_attention"
+    dev = _here(cache)
+    seqs, n = _paged_seqs(dev, positions, page_table, fn)
+    rows = q.shape[0]
+    t, row, heads = _paged_queries(cache, dev, q, rows, fn)
+    t_out, out_row, out_heads = _paged_queries(cache, dev, out, rows, fn)
+    _need(t_out == t and out_heads == heads and workspace.dtype is _U8 and workspace.is_contiguous() and 0 <= window < 1 << 31 and 0 <= n_sinks < 1 << 31 and
+          workspace.get_device() == dev, fn)
+    words = mask_d = lse_d = 0
+    if mask is not None:
+        m_rows, words = mask.shape
+        _need(mask.dtype is _I32 and mask.is_contiguous() and m_rows == rows and words > 0 and mask.get_device() == dev, fn)
+        mask_d = mask.data_ptr()
+    if lse is not None:
+        _need(lse.dtype is _F32 and lse.is_contiguous() and lse.shape == (rows, heads) and lse.get_device() == dev, fn)
+        lse_d = lse.data_ptr()
+    rc = (_lib or lib()).kl_paged_tree_attention(cache._ref, seqs, _starts(row_starts, n, dev, fn), rows, q.data_ptr(), out.data_ptr(), t, row, out_row, heads,
+                                                 scale, window, n_sinks, _per_row(row_positions, _I32, rows, dev, fn), mask_d, words, lse_d,
+                                                 workspace.data_ptr(), workspace.numel(), _flag(dev, status, fn), 0 if stream is None else stream.cuda_stream)
     if rc:
         raise KlError(rc, fn)
 

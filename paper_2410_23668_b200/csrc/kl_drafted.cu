@@ -23,6 +23,29 @@ int sm_count() {
     return sms;
 }
 
+// Workspace of kl_paged_tree_attention (byte offsets): two parts of a unit for every block.
+struct TreeSpace { size_t part_ml, bytes; };
+TreeSpace tree_space(uint32_t head_dim) {
+    TreeSpace s;
+    s.part_ml = (size_t)2 * TA_MAX_BLOCKS * 128 * head_dim * 4;
+    s.bytes = s.part_ml + (size_t)2 * TA_MAX_BLOCKS * 128 * 8;
+    return s;
+}
+
+template <int HD, bool FP8>
+kl_status launch_tree(const PagedView& v, const TreeArgs& a, unsigned blocks, PagedOrder order) {
+    using Cfg = TaCfg<HD, FP8>;
+    auto* f = kl_paged_tree_kernel<HD, FP8>;
+    constexpr size_t smem = ta_smem<HD, FP8>();
+    static_assert(smem <= 227 * 1024, "shared memory of a block");
+    static std::atomic<uint64_t> done{0};
+    kl_status rc = prepare((const void*)f, (int)smem, done);
+    if (rc != KL_OK || (rc = launch(f, dim3(blocks), Cfg::NW * 32, smem, order, v, a)) != KL_OK) return rc;
+    // tables of one tile leave no unit to cut
+    if ((uint64_t)v.table_pages * v.page <= (uint64_t)Cfg::NK || blocks < 2) return KL_OK;
+    return launch(kl_paged_tree_merge_kernel<HD, Cfg::NK>, dim3(blocks - 1, 16), TA_MERGE_THREADS, 0, order, v, a, (uint32_t)blocks);
+}
+
 // Queries of new rows, or what takes their place in the output.
 kl_status check_row_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_rows) {
     return check_queries(c, q, type, stride, n_q_heads, n_rows);
@@ -78,6 +101,58 @@ kl_status kl_paged_append_rotated(const kl_paged_cache* cache, const kl_paged_se
     if (v.hd == 64) return f32 ? launch_rotate<float, 64>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 64>(v, r, a, (unsigned)blocks, order);
     if (v.hd == 128) return f32 ? launch_rotate<float, 128>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 128>(v, r, a, (unsigned)blocks, order);
     return f32 ? launch_rotate<float, 256>(v, r, a, (unsigned)blocks, order) : launch_rotate<__nv_bfloat16, 256>(v, r, a, (unsigned)blocks, order);
+}
+
+kl_status kl_paged_tree_workspace_bytes(const kl_paged_cache* cache, uint32_t n_q_heads, size_t* bytes) {
+    if (!bytes) return KL_ERR_INVALID_ARG;
+    const kl_status rc = check_cache(cache, false);
+    if (rc != KL_OK) return rc;
+    if (!n_q_heads || n_q_heads % cache->n_kv_heads) return KL_ERR_UNSUPPORTED_SHAPE;
+    *bytes = tree_space(cache->head_dim).bytes;
+    return KL_OK;
+}
+
+kl_status kl_paged_tree_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows, const void* q_d,
+                                  void* out_d, int q_type, int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
+                                  uint32_t n_sinks, const int32_t* row_positions_d, const uint32_t* mask_d, uint32_t mask_words, float* lse_d,
+                                  void* workspace_d, size_t workspace_bytes, int32_t* status_d, void* stream) {
+    kl_status rc;
+    if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
+    if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
+    if (!row_starts_d && n_rows != seqs->n_seqs) return KL_ERR_INVALID_ARG;
+    if (q_type != KL_F32 && q_type != KL_BF16) return KL_ERR_INVALID_ARG;
+    if (q_type != KL_BF16 || n_rows > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
+    if ((rc = check_row_queries(cache, q_d, q_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+    if ((rc = check_row_queries(cache, out_d, q_type, out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+    if (!(scale < INFINITY) || (mask_d != nullptr) != (mask_words != 0) || mask_words > (1u << 26)) return KL_ERR_INVALID_ARG;
+    const TreeSpace sp = tree_space(cache->head_dim);
+    if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms <= 0) return KL_ERR_CUDA;
+    const unsigned blocks = (unsigned)(sms < TA_MAX_BLOCKS ? sms : TA_MAX_BLOCKS);
+    const PagedView v = view(cache, seqs, status_d);
+    TreeArgs a = {};
+    a.row_starts = row_starts_d;
+    a.n_rows = n_rows;
+    a.q = (const uint8_t*)q_d;
+    a.out = (uint8_t*)out_d;
+    a.q_stride = q_row_stride * 2;
+    a.out_stride = out_row_stride * 2;
+    a.nq = n_q_heads;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
+    a.window = window;
+    a.sinks = n_sinks;
+    a.row_positions = row_positions_d;
+    a.mask = mask_d;
+    a.mask_words = mask_words;
+    a.lse = lse_d;
+    a.part = (float*)workspace_d;
+    a.part_ml = (float2*)((uint8_t*)workspace_d + sp.part_ml);
+    const PagedOrder order = {stream, true};
+    if (v.hd == 64) return v.fp8 ? launch_tree<64, true>(v, a, blocks, order) : launch_tree<64, false>(v, a, blocks, order);
+    if (v.hd == 128) return v.fp8 ? launch_tree<128, true>(v, a, blocks, order) : launch_tree<128, false>(v, a, blocks, order);
+    return v.fp8 ? launch_tree<256, true>(v, a, blocks, order) : launch_tree<256, false>(v, a, blocks, order);
 }
 
 }  // extern "C"

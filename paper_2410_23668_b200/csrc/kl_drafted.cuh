@@ -312,4 +312,911 @@ constexpr size_t rt_smem_bytes() {
                                                                                         : (size_t)RT_THREADS / (HD / 16) * 2 * HD * 4;
 }
 
+
+// ---- attention of new tokens, a tree or a chain of them, over a paged cache
+//
+// For a (sequence, kv head) the queries of all new tokens and all G query heads of the group are rows of one matrix product with
+// the cached keys, 128 at a time: S = Q K^T on the tensor cores (accumulators in TMEM), the softmax on S by the threads that own the
+// rows, O += P V on the tensor cores again, with P read from TMEM.  A cached row thus leaves memory once for 128 (token, head) pairs.
+//
+// One pass over the keys with a running reference m of the exponent and the running sum l: p = 2^(s - m), l += p, O += p v; m is
+// raised, and l and O scaled, only when a score exceeds it by TA_RAISE binades -- until then p is larger than one, which 32-bit sums and
+// the 16-bit types of P bear.
+//
+// The work of a call is one list of key tiles: sequences, kv heads, runs of 128 rows, tiles; every block of the grid (one per SM) takes an
+// equal share of it.  A unit (sequence, head, run of rows) cut by the border between two blocks leaves its parts (O, m, l) in the
+// workspace, and kl_paged_tree_merge_kernel joins them in order.
+//
+// Types.  bf16 caches: Q, K, V as they are, P as two bf16 halves (16 bits of it), both multiplied with V.  e4m3 caches: K's codes as
+// bf16 (exact), its scales applied to the scores in 32 bits; V's codes as f16 (exact), its scales applied to P, which enters as one f16
+// (11 bits) scaled by a power of two common to all columns so far (the largest value scale seen).
+//
+// Few rows.  With at most 64 (32) rows the queries lie in TMEM's lanes twice (four times), and each copy looks at one half (quarter) of
+// a tile's keys only: P is zero elsewhere, the copies' results are joined at the end of the unit.  So all four softmax warps share the
+// exponentials of a single row's worth of queries.
+
+struct TreeArgs {
+    const int32_t* row_starts;      // [n_seqs + 1] or null: one row per sequence
+    uint32_t n_rows;
+    const uint8_t* q;               // bf16 [n_rows][nq][hd], strides in bytes
+    uint8_t* out;
+    int64_t q_stride, out_stride;
+    uint32_t nq, G;
+    float scale_log2;
+    uint32_t window, sinks;
+    const int32_t* row_positions;   // or null
+    const uint32_t* mask;           // [n_rows][mask_words] or null
+    uint32_t mask_words;
+    float* lse;                     // [n_rows][nq] or null
+    float* part;                    // [2 blocks][128][hd]
+    float2* part_ml;                // [2 blocks][128]
+};
+
+constexpr int TA_MAX_BLOCKS = 160;
+constexpr uint64_t TA_WAIT_NS = 2000000000ull;
+constexpr int TA_RING = 8;          // tiles whose scale bytes (e4m3) are kept; also pieces whose ends are told apart
+
+template <int HD, bool FP8>
+struct TaCfg {
+    static constexpr int NK = HD == 256 ? 64 : 128;           // keys of a tile
+    static constexpr int PW = FP8 ? 8 : 4;                    // producer warps
+    static constexpr int NW = 4 + 1 + PW;                     // softmax, MMA, producers
+    static constexpr int SLABS = HD / 64;                     // runs of 64 columns (128 bytes, one swizzle row)
+    static constexpr int SLOT = NK * HD * 2;
+    static constexpr int NS = HD == 64 ? 8 : HD == 128 ? 5 : 4;
+    static constexpr int QBYTES = 128 * HD * 2;
+    static constexpr uint32_t S_COL = 0, LO_COL = 2 * NK, O_COL = 3 * NK;   // TMEM columns: two score buffers (P's high halves on them), P's low halves, O
+    static constexpr int RAISE = FP8 ? 4 : 8;
+};
+constexpr float TA_HEAD = 10.f;     // e4m3: binades between P's largest (2^RAISE) and the largest f16 that stay free
+
+struct TaShared {
+    float x[128 * 33];                       // exchange between the copies of a row, and staging of the output
+    float factor[4][2][128];                 // per softmax warp: key scales (with the score scale), value scales
+    uint8_t exps[TA_RING][2][128];
+    uint64_t pre[13 * 32];
+    uint64_t wsum[13];
+    float2 ml[128];
+    uint64_t kv_full[8], kv_empty[8], exp_full[TA_RING], piece_end[TA_RING];
+    uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done[2], o_empty;   // [2]: tiles in turn, so that a wait is never two phases behind
+    uint32_t bad[TA_RING];                   // pieces whose partly visible tiles hold values that are no numbers
+    uint32_t tmem;
+    int abort;
+};
+template <int HD, bool FP8>
+constexpr size_t ta_smem() {
+    return 1024 + TaCfg<HD, FP8>::QBYTES + (size_t)TaCfg<HD, FP8>::NS * TaCfg<HD, FP8>::SLOT + sizeof(TaShared);
+}
+
+// A bounded wait of a whole warp; every lane gets the same answer.
+__device__ __forceinline__ bool ta_wait(uint64_t* bar, uint32_t parity, TaShared& s, int32_t* status) {
+    const uint32_t b = smem_u32(bar);
+    bool done = mbar_try_wait(b, parity);
+    if (!__all_sync(0xffffffffu, done)) {
+        const uint64_t t0 = globaltimer_ns();
+        for (uint32_t it = 1; !done; ++it) {
+            done = mbar_try_wait(b, parity);
+            if (!done && (it & 63u) == 0u) {
+                if (*(volatile int*)&s.abort) break;
+                if (globaltimer_ns() - t0 > TA_WAIT_NS) {
+                    if (status) atomicCAS(status, 0, ERR_SYNC_TIMEOUT);
+                    *(volatile int*)&s.abort = 1;
+                    break;
+                }
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, done);
+}
+__device__ __forceinline__ void tm_commit_to(uint64_t* bar) { tm_commit(smem_u32(bar)); }
+__device__ __forceinline__ void ta_named_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // the softmax warps
+__device__ __forceinline__ bool ta_named_all(bool x) {   // ... whether it holds for all of them
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(x ? 1u : 0u) : "memory");
+    return r != 0u;
+}
+__device__ __forceinline__ void ta_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void ta_cp16(uint32_t dst, const void* src, uint32_t bytes) {   // bytes: 16, or 0 for zeros
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ta_st16(uint32_t dst, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void ta_tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void ta_tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void ta_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A B with both operands in shared memory, and with A in TMEM (lane = row, one column = two values of K).
+__device__ __forceinline__ void ta_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+        "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void ta_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+        "r"(acc)
+        : "memory");
+}
+// Descriptors of tiles stored as runs of 64 columns: [row][128 bytes], 16-byte pieces exchanged by the 128-byte swizzle, eight rows =
+// 1024 bytes.  K-major (Q, K: the contraction runs along the 128 bytes): stride between groups of eight rows 1024.  MN-major (V: the
+// contraction runs along the rows): `lead` bytes between runs of 64 columns, 1024 between groups of eight rows.
+__device__ __forceinline__ uint64_t ta_desc(uint32_t smem_addr, uint32_t lead) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3ffffu) >> 4);
+    d |= (uint64_t)(lead >> 4) << 16;
+    d |= (uint64_t)(1024u >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// kind::f16, fp32 accumulators, M = 128; type 1: bf16, 0: f16; B MN-major for V.
+__device__ __forceinline__ constexpr uint32_t ta_idesc(uint32_t type, uint32_t N, bool b_mn) {
+    return (1u << 4) | (type << 7) | (type << 10) | (b_mn ? 1u << 16 : 0u) | ((N >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ float ta_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// A sequence of the call.
+struct TaSeq {
+    uint32_t T, r0, base, len, lo;   // new tokens, their first row, cached positions, positions in all, first position of the window
+    uint32_t tiles, head_tiles, first_tile, runs;   // key tiles: head_tiles from position 0 on (sinks), the others from first_tile on
+};
+template <int NK>
+__device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, uint32_t s) {
+    TaSeq q;
+    q.T = 1u;
+    q.r0 = s;
+    if (a.row_starts) {
+        const int32_t x = a.row_starts[s], y = a.row_starts[s + 1u];
+        q.r0 = x < 0 ? 0u : min((uint32_t)x, a.n_rows);
+        const uint32_t r1 = y < 0 ? 0u : min((uint32_t)y, a.n_rows);
+        q.T = r1 > q.r0 ? r1 - q.r0 : 0u;
+    }
+    const int32_t pos = c.positions[s];
+    q.base = pos < 0 ? 0u : (uint32_t)pos;
+    if (pos < 0) q.T = 0u;
+    const uint32_t most = c.table_pages * c.page;
+    if (q.T > 0u && ((uint64_t)q.base + q.T > most)) {
+        pg_error(c);
+        q.base = min(q.base, most);
+        q.T = min(q.T, most - q.base);
+    }
+    q.len = q.base + q.T;
+    q.lo = a.window && q.base + 1u > a.window ? q.base + 1u - a.window : 0u;
+    q.first_tile = q.lo / NK;
+    q.head_tiles = q.lo ? min((min(a.sinks, q.base) + NK - 1u) / NK, q.first_tile) : 0u;
+    q.tiles = q.T ? q.head_tiles + (q.len + NK - 1u) / NK - q.first_tile : 0u;
+    q.runs = (uint32_t)(((uint64_t)q.T * a.G + 127u) / 128u);
+    return q;
+}
+__device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.runs; }
+
+// First tile of block b's share of the list.
+__device__ __forceinline__ uint64_t ta_border(uint64_t work, uint32_t b, uint32_t blocks) {
+    return work / blocks * b + work % blocks * b / blocks;
+}
+
+// One block's share of the list, piece by piece.
+struct TaPiece {
+    TaSeq q;
+    uint32_t h, run, t0, t1;   // kv head, run of 128 rows, tiles
+    uint32_t rows, split, slot;   // rows of the run, copies of a row, part in the workspace (~0: the whole unit is here)
+};
+template <int NK, int NW>
+struct TaIter {
+    uint32_t s, n;
+    uint64_t off, left;
+    bool begun;
+    TaSeq q;
+    // `g`: first tile of the share; all lanes of a warp
+    __device__ __forceinline__ TaIter(const PagedView& c, const TreeArgs& a, const uint64_t* pre, uint64_t g, uint64_t count) : left(count), begun(false) {
+        s = 0;
+        off = 0;
+        if (!count) return;
+        const uint32_t share = pg_find<NW>(pre, g), per = (c.n_seqs + NW * 32u - 1u) / (NW * 32u);
+        s = share * per;
+        off = g - pre[share];
+        q = ta_seq<NK>(c, a, s);
+    }
+    __device__ __forceinline__ bool next(const PagedView& c, const TreeArgs& a, TaPiece& p) {
+        if (!left) return false;
+        while (off >= ta_work(c, q)) {
+            off -= ta_work(c, q);
+            if (++s >= c.n_seqs) return false;
+            q = ta_seq<NK>(c, a, s);
+        }
+        const uint64_t u = pg_div(off, q.tiles);
+        p.q = q;
+        p.t0 = (uint32_t)(off - u * q.tiles);
+        p.h = (uint32_t)pg_div(u, q.runs);
+        p.run = (uint32_t)(u - (uint64_t)p.h * q.runs);
+        p.t1 = (uint32_t)min((uint64_t)q.tiles, p.t0 + left);
+        p.rows = (uint32_t)min((uint64_t)128u, (uint64_t)q.T * a.G - (uint64_t)p.run * 128u);
+        p.split = p.rows <= 32u && NK == 128 ? 4u : p.rows <= 64u ? 2u : 1u;   // a copy looks at 32 keys or more
+        p.slot = p.t0 == 0u && p.t1 == q.tiles ? ~0u : 2u * blockIdx.x + (begun ? 1u : 0u);
+        begun = true;
+        off += p.t1 - p.t0;
+        left -= p.t1 - p.t0;
+        return true;
+    }
+};
+__device__ __forceinline__ uint32_t ta_tile_pos(const TaSeq& q, uint32_t t, uint32_t nk) {   // first position of tile t
+    return (t < q.head_tiles ? t : q.first_tile + t - q.head_tiles) * nk;
+}
+// Whether the tokens of a sequence may see different parts of the tile at `pos`; far: largest position in the text minus the window.
+__device__ __forceinline__ bool ta_mixed(const TreeArgs& a, const TaSeq& q, uint32_t pos, uint32_t nk, int64_t far) {
+    return q.T > 1u && (pos + nk > q.base || (a.window && (int64_t)pos <= far));
+}
+// Largest position in the text of a sequence's tokens, minus the window (whole warps).
+__device__ __forceinline__ int64_t ta_far(const TreeArgs& a, const TaSeq& q) {
+    if (!a.window) return 0;
+    int32_t m = (int32_t)(q.base + q.T - 1u);
+    if (a.row_positions) {
+        m = 0;
+        for (uint32_t i = threadIdx.x & 31u; i < q.T; i += 32u) m = max(m, a.row_positions[q.r0 + i]);
+        m = __reduce_max_sync(0xffffffffu, m);
+    }
+    return (int64_t)m - (int64_t)a.window;
+}
+
+// What a row sees.
+struct TaRow {
+    uint32_t base, T, i;            // cached positions, new tokens, the row's own number (T == 0: not a row)
+    int64_t after;                  // cached positions up to this one are behind the window
+    uint32_t sinks, window;
+    const uint32_t* mask;
+    uint32_t mask_words;
+    // bits of positions p .. p + 31
+    __device__ __forceinline__ uint32_t sees(uint32_t p) const {
+        if (!T) return 0u;
+        uint32_t bits = 0xffffffffu;
+        if (p + 32u > base) bits = p >= base ? 0u : 0xffffffffu >> (p + 32u - base);
+        if ((int64_t)p <= after) {
+            uint32_t old = (int64_t)p + 31 <= after ? 0u : 0xffffffffu << (uint32_t)(after + 1 - (int64_t)p);
+            if (p < sinks) old |= p + 32u <= sinks ? 0xffffffffu : 0xffffffffu >> (p + 32u - sinks);
+            bits &= old;
+        }
+        if (p + 32u > base && p < base + T) {   // new tokens j = j0 .. j0 + 31
+            const int64_t j0 = (int64_t)p - base;
+            uint32_t b;
+            if (mask) {
+                const int64_t w = j0 >> 5;      // floor
+                const uint32_t lo = w >= 0 && w < mask_words ? mask[w] : 0u, hi = w + 1 >= 0 && w + 1 < mask_words ? mask[w + 1] : 0u;
+                b = __funnelshift_r(lo, hi, (uint32_t)j0 & 31u);
+            } else {
+                const int64_t d = (int64_t)i - j0;   // j <= i
+                b = d < 0 ? 0u : d >= 31 ? 0xffffffffu : 0xffffffffu >> (31u - (uint32_t)d);
+                const int64_t e = d - (int64_t)window;   // j > i - window
+                if (window && e >= 0) b &= e >= 31 ? 0u : 0xffffffffu << (uint32_t)(e + 1);
+            }
+            const int64_t end = (int64_t)T - j0;   // j < T
+            if (end < 32) b &= 0xffffffffu >> (uint32_t)(32 - end);
+            bits |= b & (j0 >= 0 ? 0xffffffffu : 0xffffffffu << (uint32_t)(-j0));
+        }
+        return bits;
+    }
+};
+__device__ __forceinline__ TaRow ta_row(const TreeArgs& a, const TaPiece& p, uint32_t r) {
+    TaRow w = {};
+    w.base = p.q.base;
+    w.sinks = a.sinks;
+    w.window = a.window;
+    w.mask_words = a.mask_words;
+    w.after = -1;
+    if (r < p.rows) {
+        w.T = p.q.T;
+        w.i = (p.run * 128u + r) / a.G;
+        if (a.mask) w.mask = a.mask + (size_t)(p.q.r0 + w.i) * a.mask_words;
+        if (a.window) {
+            const int64_t at = a.row_positions ? max((int64_t)a.row_positions[p.q.r0 + w.i], (int64_t)w.base) : (int64_t)w.base + w.i;
+            w.after = at - (int64_t)a.window;
+        }
+    }
+    return w;
+}
+
+// e4m3 codes, sixteen at a time, as bf16 or f16; `tidy`: codes that are no numbers become zero and are told of.
+template <bool BF16>
+__device__ __forceinline__ bool ta_widen(const uint4& raw, uint4 (&to)[2], bool tidy) {
+    uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w}, r[8];
+    bool bad = false;
+    if (tidy) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t nan = ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x7f alone carries into the sign
+            if (nan) {
+                bad = true;
+                w[i] &= ~((nan >> 7) * 0xffu);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t h = pg_e4m3x2_to_f16x2(w[i / 2] >> 16 * (i & 1) & 0xffffu);
+        if constexpr (BF16) {
+            const float2 f = pg_f16x2_to_float2(h);
+            r[i] = pack_bf16(f.x, f.y);
+        } else {
+            r[i] = h;
+        }
+    }
+    to[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    to[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    return bad;
+}
+
+template <int HD, bool FP8>
+__global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kernel(const PagedView c, const TreeArgs a) {
+    using Cfg = TaCfg<HD, FP8>;
+    constexpr int NK = Cfg::NK, PW = Cfg::PW, NW = Cfg::NW, SLABS = Cfg::SLABS, NS = Cfg::NS;
+    extern __shared__ uint8_t ta_raw[];
+    const uint32_t raw = smem_u32(ta_raw), q_s = (raw + 1023u) & ~1023u, ring_s = q_s + Cfg::QBYTES;
+    TaShared& s = *reinterpret_cast<TaShared*>(ta_raw + (ring_s - raw) + (size_t)NS * Cfg::SLOT);
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+    griddep_launch();
+    if (tid == 0u) {
+        for (int i = 0; i < 8; ++i) {
+            mbar_init(smem_u32(&s.kv_full[i]), PW);
+            mbar_init(smem_u32(&s.kv_empty[i]), 1);
+            mbar_init(smem_u32(&s.exp_full[i]), PW);
+            mbar_init(smem_u32(&s.piece_end[i]), PW);
+            s.bad[i] = 0u;
+        }
+        mbar_init(smem_u32(&s.q_full), PW);
+        mbar_init(smem_u32(&s.q_empty), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&s.s_full[i]), 1);
+            mbar_init(smem_u32(&s.p_full[i]), 4);
+            mbar_init(smem_u32(&s.pv_done[i]), 1);
+        }
+        mbar_init(smem_u32(&s.o_empty), 4);
+        s.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        ta_fence_async();
+    }
+    if (warp == 4u) tm_alloc(smem_u32(&s.tmem), 512);
+    griddep_wait();
+    if (a.row_starts && blockIdx.x == 0u) {
+        for (uint32_t i = tid; i < c.n_seqs; i += NW * 32) {
+            const int32_t x = a.row_starts[i], y = a.row_starts[i + 1u];
+            if (x < 0 || y < x || (uint32_t)y > a.n_rows) pg_error(c);
+        }
+    }
+    const bool stopped = pg_stopped(c);   // (a barrier of the whole block where there is a status word)
+    const uint64_t work = stopped ? 0ull : pg_prefix<NW>(c.n_seqs, s.pre, s.wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK>(c, a, i)); });
+    __syncthreads();
+    tm_fence_after();
+    const uint32_t tmem = s.tmem;
+    const uint64_t g0 = ta_border(work, blockIdx.x, gridDim.x), g1 = ta_border(work, blockIdx.x + 1u, gridDim.x);
+    TaIter<NK, NW> iter(c, a, s.pre, g0, g1 - g0);
+    TaPiece p;
+
+    if (warp >= 5u) {   // ---- producers: queries, keys, values into shared memory
+        const uint32_t pw = warp - 5u;
+        constexpr uint32_t RPW = NK / PW;                  // rows of a tile per warp, one per lane
+        constexpr uint32_t CH = FP8 ? HD / 16 : HD / 8;    // 16-byte pieces of a row in the cache
+        constexpr uint32_t STEPS = RPW * CH / 32;          // pieces per lane
+        uint32_t slot = 0, use = 0, ntile = 0, npiece = 0, pending = 0, arrived = 0;   // pending: groups of copies not yet announced
+        // announces the copies of all but the newest `keep` slots
+        auto announce = [&](uint32_t keep) {
+            if (pending <= keep) return;
+            if (keep == 0u) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            else asm volatile("cp.async.wait_group 2;" ::: "memory");
+            ta_fence_async();
+            __syncwarp();
+            while (pending > keep) {
+                if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[arrived]));
+                if (++arrived == NS) arrived = 0;
+                --pending;
+            }
+        };
+        auto take_slot = [&]() {   // waits until the slot may be written
+            if (use == 0u) return true;
+            if (!FP8 && !__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&s.kv_empty[slot]), (use - 1u) & 1u))) announce(0u);
+            return ta_wait(&s.kv_empty[slot], (use - 1u) & 1u, s, c.status);
+        };
+        auto next_slot = [&]() {
+            if (++slot == NS) {
+                slot = 0;
+                ++use;
+            }
+        };
+        // where row RPW * pw + lane of the tile at position pos lies (lanes below RPW): offset of its 16-byte pieces, -1: nothing to read
+        auto look_up = [&](const TaPiece& p, uint32_t pos, int64_t& at, int64_t& ex) {
+            at = ex = -1;
+            const uint32_t x = pos + pw * RPW + lane;
+            if (lane >= RPW || x >= p.q.len || (x < p.q.lo && x >= a.sinks)) return;
+            const uint32_t lp = x / c.page, off = x - lp * c.page;
+            const int32_t phys = pg_physical(c, iter.s, lp);
+            if (phys < 0) return;
+            at = (int64_t)phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)off * c.row_b;
+            if (FP8) ex = ((int64_t)phys * c.nkv + p.h) * c.page + off;
+        };
+        bool ok = true;
+        while (ok && iter.next(c, a, p)) {
+            // queries: lane row L holds row L % (128 / split) of the run
+            if (npiece > 0u) {
+                if (!FP8) announce(0u);
+                ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status);
+                if (!ok) break;
+            }
+            {
+                constexpr uint32_t QC = HD / 8;
+                const uint32_t R = 128u / p.split;
+                for (uint32_t i = pw * 32u + lane; i < 128u * QC; i += PW * 32u) {
+                    const uint32_t L = i / QC, ch = i % QC, r = L % R;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (r < p.rows) {
+                        const uint32_t gr = p.run * 128u + r, tok = gr / a.G, g = gr - tok * a.G;
+                        v = *reinterpret_cast<const uint4*>(a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + g) * HD + ch * 8u) * 2u);
+                    }
+                    ta_st16(q_s + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v);
+                }
+                ta_fence_async();
+                __syncwarp();
+                if (lane == 0u) mbar_arrive(smem_u32(&s.q_full));
+            }
+            const int64_t far = ta_far(a, p.q);
+            bool bad = false;
+            if constexpr (!FP8) {
+                for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
+                    const uint32_t pos = ta_tile_pos(p.q, t, NK);
+                    const bool mixed = ta_mixed(a, p.q, pos, NK, far);
+                    int64_t at, ex;
+                    look_up(p, pos, at, ex);
+                    for (int kv = 0; ok && kv < 2; ++kv) {
+                        ok = take_slot();
+                        if (!ok) break;
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+                        const uint8_t* src = kv ? c.v : c.k;
+#pragma unroll
+                        for (uint32_t i = 0; i < STEPS; ++i) {
+                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
+                            const int64_t o = __shfl_sync(0xffffffffu, at, r);
+                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4);
+                            if (kv == 0 || !mixed) {
+                                ta_cp16(d, src + (o < 0 ? 0 : o + ch * 16u), o < 0 ? 0u : 16u);
+                            } else {   // values that some row must not see: what is no number becomes zero here
+                                uint4 v = make_uint4(0, 0, 0, 0);
+                                if (o >= 0) v = *reinterpret_cast<const uint4*>(src + o + ch * 16u);
+                                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u, bad = true;
+                                    if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu, bad = true;
+                                }
+                                ta_st16(d, make_uint4(w[0], w[1], w[2], w[3]));
+                            }
+                        }
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        ++pending;
+                        next_slot();
+                        announce(2u);
+                    }
+                }
+            } else {
+                // two tiles' worth of loads: the next tile's are under way while this one's are widened
+                uint4 kraw[STEPS], vraw[STEPS];
+                int64_t at, ex;
+                uint32_t ke = 0, ve = 0;
+                auto request = [&](const uint8_t* src, uint4 (&to)[STEPS]) {
+#pragma unroll
+                    for (uint32_t i = 0; i < STEPS; ++i) {
+                        const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH;
+                        const int64_t o = __shfl_sync(0xffffffffu, at, r);
+                        to[i] = o >= 0 ? *reinterpret_cast<const uint4*>(src + o + ch * 16u) : make_uint4(0, 0, 0, 0);
+                    }
+                };
+                auto request_scales = [&]() {
+                    ke = ve = 0;
+                    if (ex >= 0) {
+                        ke = c.ke[ex];
+                        ve = c.ve[ex];
+                    }
+                };
+                look_up(p, ta_tile_pos(p.q, p.t0, NK), at, ex);
+                request(c.k, kraw);
+                request_scales();
+                request(c.v, vraw);
+                for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
+                    const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far), more = t + 1u < p.t1;
+                    // scale bytes; a row that nobody sees gets the smallest
+                    if (lane < RPW) {
+                        s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke;
+                        s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve;
+                    }
+                    __syncwarp();
+                    if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
+                    if (more) look_up(p, ta_tile_pos(p.q, t + 1u, NK), at, ex);
+                    for (int kv = 0; ok && kv < 2; ++kv) {
+                        ok = take_slot();
+                        if (!ok) break;
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+#pragma unroll
+                        for (uint32_t i = 0; i < STEPS; ++i) {
+                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
+                            uint4 w[2];
+                            if (kv == 0) ta_widen<true>(kraw[i], w, false);
+                            else bad |= ta_widen<false>(vraw[i], w, mixed);
+                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
+                            ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
+                            ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
+                        }
+                        if (more) {
+                            if (kv == 0) {
+                                request(c.k, kraw);
+                                request_scales();
+                            } else {
+                                request(c.v, vraw);
+                            }
+                        }
+                        ta_fence_async();
+                        __syncwarp();
+                        if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
+                        next_slot();
+                    }
+                    ++ntile;
+                }
+            }
+            if (bad) atomicOr(&s.bad[npiece % TA_RING], 1u);
+            __syncwarp();
+            if (lane == 0u) mbar_arrive(smem_u32(&s.piece_end[npiece % TA_RING]));
+            ++npiece;
+        }
+        if (!FP8) announce(0u);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp == 4u) {   // ---- MMA
+        constexpr uint32_t qk_idesc = ta_idesc(1u, NK, false), pv_idesc = ta_idesc(FP8 ? 0u : 1u, HD, true);
+        uint32_t slot = 0, use = 0, nt = 0, npiece = 0;
+        bool ok = true;
+        uint32_t v_slot = 0, v_use = 0;
+        auto pv = [&](uint32_t tile, uint32_t acc) {   // the tile's number among all of this block
+            const uint32_t b = tile & 1u;
+            if (!ta_wait(&s.p_full[b], (tile >> 1) & 1u, s, c.status) || !ta_wait(&s.kv_full[v_slot], v_use & 1u, s, c.status)) return false;
+            tm_fence_after();
+            if (lane == 0u) {
+                const uint32_t vb = ring_s + v_slot * Cfg::SLOT, d = tmem + Cfg::O_COL, hi = tmem + Cfg::S_COL + b * NK, lo = tmem + Cfg::LO_COL + b * (NK / 2);
+#pragma unroll
+                for (uint32_t k = 0; k < NK / 16; ++k) {
+                    const uint64_t bd = ta_desc(vb + k * 2048u, NK * 128u);
+                    ta_mma_ts(d, hi + k * 8u, bd, pv_idesc, acc | (k > 0u));
+                    if (!FP8) ta_mma_ts(d, lo + k * 8u, bd, pv_idesc, 1u);
+                }
+                tm_commit_to(&s.kv_empty[v_slot]);
+                tm_commit_to(&s.pv_done[b]);
+            }
+            __syncwarp();
+            return true;
+        };
+        auto advance = [&](uint32_t& sl, uint32_t& us) {
+            if (++sl == NS) {
+                sl = 0;
+                ++us;
+            }
+        };
+        while (ok && iter.next(c, a, p)) {
+            ok = ta_wait(&s.q_full, npiece & 1u, s, c.status);
+            for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++nt) {
+                ok = ta_wait(&s.kv_full[slot], use & 1u, s, c.status);
+                if (!ok) break;
+                tm_fence_after();
+                if (lane == 0u) {
+                    const uint32_t kb = ring_s + slot * Cfg::SLOT, d = tmem + Cfg::S_COL + (nt & 1u) * NK;
+#pragma unroll
+                    for (uint32_t k = 0; k < HD / 16; ++k)
+                        ta_mma_ss(d, ta_desc(q_s + k / 4u * (128u * 128u) + k % 4u * 32u, 16u), ta_desc(kb + k / 4u * (NK * 128u) + k % 4u * 32u, 16u), qk_idesc, k > 0u);
+                    tm_commit_to(&s.s_full[nt & 1u]);
+                    tm_commit_to(&s.kv_empty[slot]);
+                    if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
+                }
+                __syncwarp();
+                advance(slot, use);
+                // the values of this tile lie in the next slot
+                if (t > p.t0) ok = pv(nt - 1u, t - 1u > p.t0);
+                else if (npiece > 0u) ok = ta_wait(&s.o_empty, (npiece - 1u) & 1u, s, c.status);   // the last unit's result has been read
+                v_slot = slot;
+                v_use = use;
+                advance(slot, use);
+            }
+            if (ok) ok = pv(nt - 1u, p.t1 - 1u > p.t0);
+            ++npiece;
+        }
+        if (nt > 0u) ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status);
+    } else {   // ---- softmax and results: thread L owns TMEM lane L
+        const uint32_t L = tid, lane_base = tmem + (warp * 32u << 16);
+        uint32_t nt = 0, npiece = 0;
+        bool ok = true;
+        while (ok && iter.next(c, a, p)) {
+            const uint32_t R = 128u / p.split, r = L % R, col0 = L / R * (NK / p.split), ncol = NK / p.split;
+            const TaRow row = ta_row(a, p, r);
+            const bool active = __any_sync(0xffffffffu, row.T > 0u);
+            float m = -INFINITY, l = 0.f;
+            int ev_ref = -1;   // e4m3: the largest value scale byte so far
+            for (uint32_t t = p.t0; t < p.t1; ++t, ++nt) {
+                const uint32_t b = nt & 1u, pos = ta_tile_pos(p.q, t, NK), s_at = lane_base + Cfg::S_COL + b * NK;
+                if (FP8 && !(ok = ta_wait(&s.exp_full[nt % TA_RING], (nt / TA_RING) & 1u, s, c.status))) break;
+                if (!(ok = ta_wait(&s.s_full[b], (nt >> 1) & 1u, s, c.status))) break;
+                tm_fence_after();
+                if (active) {
+                    float raise = 1.f;   // of O and l: by a new reference of the values' scales
+                    if constexpr (FP8) {
+                        const uint32_t kw = *reinterpret_cast<const uint32_t*>(&s.exps[nt % TA_RING][0][lane * 4u % NK]);
+                        const uint32_t vw = *reinterpret_cast<const uint32_t*>(&s.exps[nt % TA_RING][1][lane * 4u % NK]);
+                        int mx = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mx = max(mx, (int)(vw >> 8 * j & 0xffu));
+                        mx = (int)__reduce_max_sync(0xffffffffu, (unsigned)mx);
+                        if (mx > ev_ref) {
+                            raise = ev_ref < 0 ? 0.f : ta_exp2((float)(ev_ref - mx));
+                            ev_ref = mx;
+                        }
+                        __syncwarp();
+                        if (lane * 4u < (uint32_t)NK) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                s.factor[warp][0][lane * 4u + j] = pg_scale(kw >> 8 * j & 0xffu) * a.scale_log2;
+                                s.factor[warp][1][lane * 4u + j] = ta_exp2((float)((int)(vw >> 8 * j & 0xffu) - ev_ref) + TA_HEAD);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    // largest score of the tile
+                    float mx = -INFINITY;
+                    for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
+                        uint32_t x[32];
+                        tm_ld32(s_at + c0, x);
+                        tm_ld_wait();
+                        const uint32_t sees = row.sees(pos + c0);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float y = __uint_as_float(x[j]) * (FP8 ? s.factor[warp][0][c0 + j] : a.scale_log2);
+                            if (sees >> j & 1u) mx = fmaxf(mx, y);
+                        }
+                    }
+                    float f = 1.f;
+                    if (mx > m + (float)Cfg::RAISE) {
+                        f = m == -INFINITY ? 0.f : ta_exp2(m - mx);
+                        m = mx;
+                    }
+                    l *= f;
+                    f *= FP8 ? raise : 1.f;
+                    if (t > p.t0 && __any_sync(0xffffffffu, f != 1.f)) {   // O so far, in the new references
+                        if (!(ok = ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status))) break;
+                        tm_fence_after();
+                        for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 32u) {
+                            uint32_t x[32];
+                            tm_ld32(lane_base + Cfg::O_COL + c0, x);
+                            tm_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
+                            ta_tmem_st32(lane_base + Cfg::O_COL + c0, x);
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (uint32_t c0 = 0; c0 < (uint32_t)NK; c0 += 32u) {
+                        uint32_t hi[16], lo[16];
+                        if (c0 < col0 || c0 >= col0 + ncol) {   // another copy's columns
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) hi[j] = lo[j] = 0u;
+                        } else {
+                            uint32_t x[32];
+                            tm_ld32(s_at + c0, x);
+                            tm_ld_wait();
+                            const uint32_t sees = row.sees(pos + c0);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const float e = ta_exp2(fmaf(__uint_as_float(x[j]), FP8 ? s.factor[warp][0][c0 + j] : a.scale_log2, -ref));
+                                const float y = sees >> j & 1u ? e : 0.f;
+                                sum[j & 3] += y;
+                                x[j] = __float_as_uint(FP8 ? y * s.factor[warp][1][c0 + j] : y);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float u = __uint_as_float(x[2 * j]), v = __uint_as_float(x[2 * j + 1]);
+                                if constexpr (FP8) {
+                                    const __half2 h = __floats2half2_rn(u, v);
+                                    hi[j] = *reinterpret_cast<const uint32_t*>(&h);
+                                } else {
+                                    hi[j] = pack_bf16(u, v);
+                                    lo[j] = pack_bf16(u - bf_lo(hi[j]), v - bf_hi(hi[j]));
+                                }
+                            }
+                        }
+                        // P's high halves lie on the scores that have been read: columns c0 / 2 .. are behind those still to come
+                        ta_tmem_st16(s_at + c0 / 2u, hi);
+                        if (!FP8) ta_tmem_st16(lane_base + Cfg::LO_COL + b * (NK / 2) + c0 / 2u, lo);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    ta_tmem_st_wait();
+                }
+                tm_fence_before();
+                __syncwarp();
+                if (lane == 0u) mbar_arrive(smem_u32(&s.p_full[b]));
+            }
+            ok = ok && ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status) && ta_wait(&s.piece_end[npiece % TA_RING], (npiece / TA_RING) & 1u, s, c.status);
+            if (!(ok = ta_named_all(ok))) break;   // (no softmax warp waits for one that has given up)
+            tm_fence_after();
+            const bool bad = *(volatile uint32_t*)&s.bad[npiece % TA_RING] != 0u;
+            // the copies of a row: one reference, one sum
+            const float unit = FP8 && ev_ref >= 0 ? ta_exp2((float)(ev_ref - 127) - TA_HEAD) : 1.f;   // of the values
+            float mm = m, ll = l, f = 1.f;
+            s.ml[L] = make_float2(m, FP8 ? unit : 0.f);
+            ta_named_sync();
+            if (bad && L == 0u) s.bad[npiece % TA_RING] = 0u;
+            if (p.split > 1u) {
+                for (uint32_t k = 0; k < p.split; ++k) mm = fmaxf(mm, s.ml[r + k * R].x);
+                f = m == -INFINITY ? 0.f : ta_exp2(m - mm);
+                ta_named_sync();
+                s.ml[L] = make_float2(l * f, 0.f);
+                ta_named_sync();
+                ll = 0.f;
+                for (uint32_t k = 0; k < p.split; ++k) ll += s.ml[r + k * R].x;
+            }
+            const bool whole = p.slot == ~0u;
+            const uint32_t gr = p.run * 128u + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
+            if (r < p.rows && L < R) {
+                if (whole) {
+                    if (a.lse) a.lse[(size_t)(p.q.r0 + tok) * a.nq + head] = ll > 0.f || ll != ll ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
+                } else {
+                    a.part_ml[(size_t)p.slot * 128u + r] = make_float2(mm, ll);
+                }
+            }
+            const float g = (whole ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f) * f * unit;
+            const uint32_t cols = 32u / p.split;   // of a chunk of 32: what this thread writes of row r
+            const uint32_t mine = L / R * cols;
+            for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 32u) {
+                uint32_t x[32];
+                tm_ld32(lane_base + Cfg::O_COL + c0, x);
+                tm_ld_wait();
+                if (bad && r < p.rows) {   // values that are no numbers, for the rows that see them
+                    for (uint32_t t = p.t0; t < p.t1; ++t) {
+                        const uint32_t pos = ta_tile_pos(p.q, t, NK);
+                        if (!ta_mixed(a, p.q, pos, NK, INT32_MAX)) continue;
+                        for (uint32_t k0 = col0; k0 < col0 + ncol; k0 += 32u) {
+                            uint32_t sees = row.sees(pos + k0);
+                            while (sees) {
+                                const uint32_t at = pos + k0 + __ffs(sees) - 1u;
+                                sees &= sees - 1u;
+                                const int32_t phys = pg_physical(c, iter.s, at / c.page);
+                                if (phys < 0) continue;
+                                const uint8_t* v = c.v + (int64_t)phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)(at % c.page) * c.row_b;
+                                for (int j = 0; j < 32; ++j) {
+                                    if (FP8 ? (v[c0 + j] & 0x7f) == 0x7f : (reinterpret_cast<const uint16_t*>(v)[c0 + j] & 0x7f80) == 0x7f80)
+                                        x[j] = __float_as_uint(__uint_as_float(x[j]) + (FP8 ? NAN : __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(v)[c0 + j] << 16)));
+                                }
+                            }
+                        }
+                    }
+                }
+                ta_named_sync();   // the buffer's last readers are done
+#pragma unroll
+                for (int j = 0; j < 32; ++j) s.x[L * 33u + j] = f == 0.f ? 0.f : __uint_as_float(x[j]) * g;
+                ta_named_sync();
+                if (r < p.rows) {
+                    for (uint32_t j = mine; j < mine + cols; j += 8u) {
+                        float o[8];
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            o[y] = 0.f;
+                            for (uint32_t k = 0; k < p.split; ++k) o[y] += s.x[(r + k * R) * 33u + j + y];
+                        }
+                        if (whole)
+                            pg_store8<__nv_bfloat16>(reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD + c0 + j, o);
+                        else
+                            pg_store8<float>(a.part + ((size_t)p.slot * 128u + r) * HD + c0 + j, o);
+                    }
+                }
+            }
+            tm_fence_before();
+            __syncwarp();
+            if (lane == 0u) mbar_arrive(smem_u32(&s.o_empty));
+            ++npiece;
+        }
+    }
+    tm_fence_before();
+    __syncthreads();
+    if (warp == 4u) tm_dealloc(tmem, 512);
+}
+
+// Joins the parts of the units that borders between blocks cut: block (b - 1, y) of the grid has border b, and does nothing unless it is the
+// first border inside its unit.  A warp takes a row: weights 2^(m - largest m), sums in the order of the parts.
+constexpr int TA_MERGE_THREADS = 128;
+template <int HD, int NK>
+__global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(const PagedView c, const TreeArgs a, const uint32_t blocks) {
+    constexpr int NW = TA_MERGE_THREADS / 32, COLS = HD / 32;
+    __shared__ uint64_t pre[NW * 32], wsum[NW];
+    griddep_launch();
+    griddep_wait();
+    if (pg_stopped(c)) return;
+    const uint64_t work = pg_prefix<NW>(c.n_seqs, pre, wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK>(c, a, i)); });
+    const uint32_t b = blockIdx.x + 1u, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint64_t g = ta_border(work, b, blocks);
+    if (g == 0u || g >= work) return;
+    const uint32_t share = pg_find<NW>(pre, g), per = (c.n_seqs + NW * 32u - 1u) / (NW * 32u);
+    uint32_t s = share * per;
+    uint64_t off = g - pre[share];
+    TaSeq q = ta_seq<NK>(c, a, s);
+    while (off >= ta_work(c, q)) {
+        off -= ta_work(c, q);
+        if (++s >= c.n_seqs) return;
+        q = ta_seq<NK>(c, a, s);
+    }
+    const uint64_t u = pg_div(off, q.tiles), begin = g - (off - u * q.tiles), end = begin + q.tiles;
+    const uint32_t first = b - 1u, h = (uint32_t)pg_div(u, q.runs), run = (uint32_t)(u - (uint64_t)h * q.runs);
+    if (g == begin || ta_border(work, first, blocks) > begin) return;
+    const uint32_t first_slot = 2u * first + (ta_border(work, first, blocks) < begin ? 1u : 0u);
+    uint32_t last = b;
+    while (last + 1u < blocks && ta_border(work, last + 1u, blocks) < end) ++last;
+    const uint32_t rows = (uint32_t)min((uint64_t)128u, (uint64_t)q.T * a.G - (uint64_t)run * 128u);
+    for (uint32_t r = blockIdx.y * NW + warp; r < rows; r += gridDim.y * NW) {
+        auto slot_of = [&](uint32_t k) { return k == first ? first_slot : 2u * k; };
+        auto holds = [&](uint32_t k) { return ta_border(work, k, blocks) < ta_border(work, k + 1u, blocks); };   // blocks without work left nothing
+        float m = -INFINITY;
+        for (uint32_t k = first + lane; k <= last; k += 32u)
+            if (holds(k)) m = fmaxf(m, a.part_ml[(size_t)slot_of(k) * 128u + r].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float l = 0.f, sum[COLS];
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
+        for (uint32_t k0 = first; k0 <= last; k0 += 32u) {
+            float w = 0.f, part = 0.f;
+            if (k0 + lane <= last && holds(k0 + lane)) {
+                const float2 ml = a.part_ml[(size_t)slot_of(k0 + lane) * 128u + r];
+                w = ml.x == -INFINITY ? 0.f : ta_exp2(ml.x - m);
+                part = ml.y;
+            }
+            const uint32_t n = min(32u, last - k0 + 1u);
+            for (uint32_t k = 0; k < n; ++k) {
+                const float wk = __shfl_sync(0xffffffffu, w, k), lk = __shfl_sync(0xffffffffu, part, k);
+                if (wk == 0.f) continue;   // (the same for the whole warp)
+                l += wk * lk;
+                const float* src = a.part + ((size_t)slot_of(k0 + k) * 128u + r) * HD + lane * COLS;
+                float x[COLS];
+                if constexpr (COLS == 2) {
+                    const float2 v = *reinterpret_cast<const float2*>(src);
+                    x[0] = v.x; x[1] = v.y;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < COLS / 4; ++j) {
+                        const float4 v = reinterpret_cast<const float4*>(src)[j];
+                        x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < COLS; ++j) sum[j] += wk * x[j];
+            }
+        }
+        const uint32_t gr = run * 128u + r, tok = gr / a.G, head = h * a.G + gr - tok * a.G;
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+        if (a.lse && lane == 0u) a.lse[(size_t)(q.r0 + tok) * a.nq + head] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        uint32_t* out = reinterpret_cast<uint32_t*>(a.out + (int64_t)(q.r0 + tok) * a.out_stride + ((size_t)head * HD + lane * COLS) * 2u);
+        uint32_t o[COLS / 2];
+#pragma unroll
+        for (int j = 0; j < COLS / 2; ++j) o[j] = pack_bf16(sum[2 * j] * inv, sum[2 * j + 1] * inv);
+        if constexpr (COLS == 2) *out = o[0];
+        else if constexpr (COLS == 4) *reinterpret_cast<uint2*>(out) = make_uint2(o[0], o[1]);
+        else *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
 }  // namespace kl
