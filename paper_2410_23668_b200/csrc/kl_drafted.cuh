@@ -361,7 +361,6 @@ struct TaCfg {
     static constexpr int NK = HD == 256 ? 64 : 128;           // keys of a tile
     static constexpr int PW = FP8 ? 8 : 4;                    // producer warps
     static constexpr int NW = 4 + 1 + PW;                     // softmax, MMA, producers
-    static constexpr int SLABS = HD / 64;                     // runs of 64 columns (128 bytes, one swizzle row)
     static constexpr int SLOT = NK * HD * 2;
     static constexpr int NS = HD == 64 ? 8 : HD == 128 ? 5 : 4;
     static constexpr int QBYTES = 128 * HD * 2;
@@ -372,7 +371,7 @@ constexpr float TA_HEAD = 10.f;     // e4m3: binades between P's largest (2^RAIS
 
 struct TaShared {
     float x[128 * 33];                       // exchange between the copies of a row, and staging of the output
-    float factor[4][2][128];                 // per softmax warp: key scales (with the score scale), value scales
+    alignas(16) float factor[4][2][128];                 // per softmax warp: key scales (with the score scale), value scales
     uint8_t exps[TA_RING][2][128];
     uint64_t pre[13 * 32];
     uint64_t wsum[13];
@@ -471,6 +470,35 @@ __device__ __forceinline__ constexpr uint32_t ta_idesc(uint32_t type, uint32_t N
 __device__ __forceinline__ float ta_exp2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Two floats as f16 (x0 in the low half), nearest, saturating.
+__device__ __forceinline__ uint32_t ta_pack_f16(float x0, float x1) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(x0), "f"(x1));
+    return r;
+}
+// Two floats in one register pair.
+__device__ __forceinline__ uint64_t ta_pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void ta_unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t ta_fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t ta_mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 
@@ -666,7 +694,7 @@ __device__ __forceinline__ bool ta_widen(const uint4& raw, uint4 (&to)[2], bool 
 template <int HD, bool FP8>
 __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kernel(const PagedView c, const TreeArgs a) {
     using Cfg = TaCfg<HD, FP8>;
-    constexpr int NK = Cfg::NK, PW = Cfg::PW, NW = Cfg::NW, SLABS = Cfg::SLABS, NS = Cfg::NS;
+    constexpr int NK = Cfg::NK, PW = Cfg::PW, NW = Cfg::NW, NS = Cfg::NS;
     extern __shared__ uint8_t ta_raw[];
     const uint32_t raw = smem_u32(ta_raw), q_s = (raw + 1023u) & ~1023u, ring_s = q_s + Cfg::QBYTES;
     TaShared& s = *reinterpret_cast<TaShared*>(ta_raw + (ring_s - raw) + (size_t)NS * Cfg::SLOT);
@@ -674,7 +702,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
     griddep_launch();
     if (tid == 0u) {
         for (int i = 0; i < 8; ++i) {
-            mbar_init(smem_u32(&s.kv_full[i]), PW);
+            mbar_init(smem_u32(&s.kv_full[i]), FP8 ? PW : PW * 32);   // bf16: every producer thread's copies
             mbar_init(smem_u32(&s.kv_empty[i]), 1);
             mbar_init(smem_u32(&s.exp_full[i]), PW);
             mbar_init(smem_u32(&s.piece_end[i]), PW);
@@ -714,53 +742,46 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         constexpr uint32_t RPW = NK / PW;                  // rows of a tile per warp, one per lane
         constexpr uint32_t CH = FP8 ? HD / 16 : HD / 8;    // 16-byte pieces of a row in the cache
         constexpr uint32_t STEPS = RPW * CH / 32;          // pieces per lane
-        uint32_t slot = 0, use = 0, ntile = 0, npiece = 0, pending = 0, arrived = 0;   // pending: groups of copies not yet announced
-        // announces the copies of all but the newest `keep` slots
-        auto announce = [&](uint32_t keep) {
-            if (pending <= keep) return;
-            if (keep == 0u) asm volatile("cp.async.wait_group 0;" ::: "memory");
-            else asm volatile("cp.async.wait_group 2;" ::: "memory");
-            ta_fence_async();
-            __syncwarp();
-            while (pending > keep) {
-                if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[arrived]));
-                if (++arrived == NS) arrived = 0;
-                --pending;
-            }
-        };
-        auto take_slot = [&]() {   // waits until the slot may be written
-            if (use == 0u) return true;
-            if (!FP8 && !__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&s.kv_empty[slot]), (use - 1u) & 1u))) announce(0u);
-            return ta_wait(&s.kv_empty[slot], (use - 1u) & 1u, s, c.status);
-        };
+        uint32_t slot = 0, use = 0, ntile = 0, npiece = 0;
+        auto take_slot = [&]() { return use == 0u || ta_wait(&s.kv_empty[slot], (use - 1u) & 1u, s, c.status); };   // until it may be written
         auto next_slot = [&]() {
             if (++slot == NS) {
                 slot = 0;
                 ++use;
             }
         };
-        // where row RPW * pw + lane of the tile at position pos lies (lanes below RPW): offset of its 16-byte pieces, -1: nothing to read
-        auto look_up = [&](const TaPiece& p, uint32_t pos, int64_t& at, int64_t& ex) {
+        // Row RPW * pw + lane of a tile (lanes below RPW): its page is asked for a tile or two ahead of its use.
+        struct Look { int32_t phys; uint32_t off; bool any; };
+        auto look_up = [&](uint32_t t) {
+            Look k = {0, 0u, false};
+            const uint32_t x = ta_tile_pos(p.q, t, NK) + pw * RPW + lane;
+            if (t >= p.t1 || lane >= RPW || x >= p.q.len || (x < p.q.lo && x >= a.sinks)) return k;
+            const uint32_t lp = x / c.page;
+            k.off = x - lp * c.page;
+            k.phys = lp < c.table_pages ? c.table[(int64_t)iter.s * c.table_stride + lp] : -1;
+            k.any = true;
+            return k;
+        };
+        // where its 16-byte pieces (and its scale bytes) lie; -1: nothing to read
+        auto place = [&](const Look& k, int64_t& at, int64_t& ex) {
             at = ex = -1;
-            const uint32_t x = pos + pw * RPW + lane;
-            if (lane >= RPW || x >= p.q.len || (x < p.q.lo && x >= a.sinks)) return;
-            const uint32_t lp = x / c.page, off = x - lp * c.page;
-            const int32_t phys = pg_physical(c, iter.s, lp);
-            if (phys < 0) return;
-            at = (int64_t)phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)off * c.row_b;
-            if (FP8) ex = ((int64_t)phys * c.nkv + p.h) * c.page + off;
+            if (!k.any) return;
+            if ((uint32_t)k.phys >= c.n_pages) {
+                pg_error(c);
+                return;
+            }
+            at = (int64_t)k.phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)k.off * c.row_b;
+            if (FP8) ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
         };
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
+            Look next = look_up(p.t0);
             // queries: lane row L holds row L % (128 / split) of the run
-            if (npiece > 0u) {
-                if (!FP8) announce(0u);
-                ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status);
-                if (!ok) break;
-            }
+            if (npiece > 0u && !(ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status))) break;
             {
                 constexpr uint32_t QC = HD / 8;
                 const uint32_t R = 128u / p.split;
+#pragma unroll 4
                 for (uint32_t i = pw * 32u + lane; i < 128u * QC; i += PW * 32u) {
                     const uint32_t L = i / QC, ch = i % QC, r = L % R;
                     uint4 v = make_uint4(0, 0, 0, 0);
@@ -778,23 +799,28 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             bool bad = false;
             if constexpr (!FP8) {
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
-                    const uint32_t pos = ta_tile_pos(p.q, t, NK);
-                    const bool mixed = ta_mixed(a, p.q, pos, NK, far);
+                    const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
                     int64_t at, ex;
-                    look_up(p, pos, at, ex);
+                    place(next, at, ex);
+                    next = look_up(t + 1u);
                     for (int kv = 0; ok && kv < 2; ++kv) {
                         ok = take_slot();
                         if (!ok) break;
-                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT, bar = smem_u32(&s.kv_full[slot]);
                         const uint8_t* src = kv ? c.v : c.k;
+                        if (kv == 0 || !mixed) {
 #pragma unroll
-                        for (uint32_t i = 0; i < STEPS; ++i) {
-                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
-                            const int64_t o = __shfl_sync(0xffffffffu, at, r);
-                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4);
-                            if (kv == 0 || !mixed) {
-                                ta_cp16(d, src + (o < 0 ? 0 : o + ch * 16u), o < 0 ? 0u : 16u);
-                            } else {   // values that some row must not see: what is no number becomes zero here
+                            for (uint32_t i = 0; i < STEPS; ++i) {
+                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
+                                const int64_t o = __shfl_sync(0xffffffffu, at, r);
+                                ta_cp16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), src + (o < 0 ? 0 : o + ch * 16u), o < 0 ? 0u : 16u);
+                            }
+                            // every thread's arrival comes when its copies have
+                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                        } else {   // values that some row must not see: what is no number becomes zero here
+                            for (uint32_t i = 0; i < STEPS; ++i) {
+                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
+                                const int64_t o = __shfl_sync(0xffffffffu, at, r);
                                 uint4 v = make_uint4(0, 0, 0, 0);
                                 if (o >= 0) v = *reinterpret_cast<const uint4*>(src + o + ch * 16u);
                                 uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -803,77 +829,86 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                     if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u, bad = true;
                                     if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu, bad = true;
                                 }
-                                ta_st16(d, make_uint4(w[0], w[1], w[2], w[3]));
+                                ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                             }
+                            mbar_arrive(bar);
                         }
-                        asm volatile("cp.async.commit_group;" ::: "memory");
-                        ++pending;
                         next_slot();
-                        announce(2u);
                     }
                 }
             } else {
-                // two tiles' worth of loads: the next tile's are under way while this one's are widened
-                uint4 kraw[STEPS], vraw[STEPS];
-                int64_t at, ex;
-                uint32_t ke = 0, ve = 0;
-                auto request = [&](const uint8_t* src, uint4 (&to)[STEPS]) {
+                // Two tiles' loads are under way while a third is widened, and the pages of the one after are looked up.
+                uint4 kraw[2][STEPS], vraw[2][STEPS];
+                uint32_t ke[2], ve[2];
+                int64_t at[2], ex[2];
+                auto request = [&](const uint8_t* src, int64_t from, uint4 (&to)[STEPS]) {
 #pragma unroll
                     for (uint32_t i = 0; i < STEPS; ++i) {
                         const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH;
-                        const int64_t o = __shfl_sync(0xffffffffu, at, r);
+                        const int64_t o = __shfl_sync(0xffffffffu, from, r);
                         to[i] = o >= 0 ? *reinterpret_cast<const uint4*>(src + o + ch * 16u) : make_uint4(0, 0, 0, 0);
                     }
                 };
-                auto request_scales = [&]() {
-                    ke = ve = 0;
-                    if (ex >= 0) {
-                        ke = c.ke[ex];
-                        ve = c.ve[ex];
+                auto request_scales = [&](int z) {
+                    ke[z] = ve[z] = 0;
+                    if (ex[z] >= 0) {
+                        ke[z] = c.ke[ex[z]];
+                        ve[z] = c.ve[ex[z]];
                     }
                 };
-                look_up(p, ta_tile_pos(p.q, p.t0, NK), at, ex);
-                request(c.k, kraw);
-                request_scales();
-                request(c.v, vraw);
-                for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
-                    const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far), more = t + 1u < p.t1;
-                    // scale bytes; a row that nobody sees gets the smallest
-                    if (lane < RPW) {
-                        s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke;
-                        s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve;
-                    }
-                    __syncwarp();
-                    if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
-                    if (more) look_up(p, ta_tile_pos(p.q, t + 1u, NK), at, ex);
-                    for (int kv = 0; ok && kv < 2; ++kv) {
-                        ok = take_slot();
-                        if (!ok) break;
-                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+                Look after = look_up(p.t0 + 1u);
+                place(next, at[0], ex[0]);
+                next = look_up(p.t0 + 2u);
+                request(c.k, at[0], kraw[0]);
+                request_scales(0);
+                request(c.v, at[0], vraw[0]);
+                place(after, at[1], ex[1]);
+                request(c.k, at[1], kraw[1]);
+                request_scales(1);
+                request(c.v, at[1], vraw[1]);
+                for (uint32_t t0 = p.t0; ok && t0 < p.t1; t0 += 2u) {
 #pragma unroll
-                        for (uint32_t i = 0; i < STEPS; ++i) {
-                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
-                            uint4 w[2];
-                            if (kv == 0) ta_widen<true>(kraw[i], w, false);
-                            else bad |= ta_widen<false>(vraw[i], w, mixed);
-                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
-                            ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
-                            ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
+                    for (int z = 0; z < 2; ++z) {
+                        const uint32_t t = t0 + z;
+                        if (!ok || t >= p.t1) break;
+                        const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
+                        // scale bytes; a row that nobody sees gets the smallest
+                        if (lane < RPW) {
+                            s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke[z];
+                            s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve[z];
                         }
-                        if (more) {
-                            if (kv == 0) {
-                                request(c.k, kraw);
-                                request_scales();
-                            } else {
-                                request(c.v, vraw);
-                            }
-                        }
-                        ta_fence_async();
                         __syncwarp();
-                        if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
-                        next_slot();
+                        if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
+                        place(next, at[z], ex[z]);   // of tile t + 2
+                        next = look_up(t + 3u);
+#pragma unroll
+                        for (int kv = 0; kv < 2; ++kv) {
+                            ok = ok && take_slot();
+                            if (!ok) break;
+                            const uint32_t dst = ring_s + slot * Cfg::SLOT;
+#pragma unroll
+                            for (uint32_t i = 0; i < STEPS; ++i) {
+                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
+                                uint4 w[2];
+                                if (kv == 0) ta_widen<true>(kraw[z][i], w, false);
+                                else bad |= ta_widen<false>(vraw[z][i], w, mixed);
+                                const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
+                                ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
+                                ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
+                            }
+                            if (kv == 0) {
+                                request(c.k, at[z], kraw[z]);
+                                request_scales(z);
+                            } else {
+                                request(c.v, at[z], vraw[z]);
+                            }
+                            ta_fence_async();
+                            __syncwarp();
+                            if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
+                            next_slot();
+                        }
+                        ++ntile;
                     }
-                    ++ntile;
                 }
             }
             if (bad) atomicOr(&s.bad[npiece % TA_RING], 1u);
@@ -881,7 +916,6 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             if (lane == 0u) mbar_arrive(smem_u32(&s.piece_end[npiece % TA_RING]));
             ++npiece;
         }
-        if (!FP8) announce(0u);
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == 4u) {   // ---- MMA
         constexpr uint32_t qk_idesc = ta_idesc(1u, NK, false), pv_idesc = ta_idesc(FP8 ? 0u : 1u, HD, true);
@@ -891,14 +925,15 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         auto pv = [&](uint32_t tile, uint32_t acc) {   // the tile's number among all of this block
             const uint32_t b = tile & 1u;
             if (!ta_wait(&s.p_full[b], (tile >> 1) & 1u, s, c.status) || !ta_wait(&s.kv_full[v_slot], v_use & 1u, s, c.status)) return false;
+            if (!FP8) ta_fence_async();
             tm_fence_after();
             if (lane == 0u) {
                 const uint32_t vb = ring_s + v_slot * Cfg::SLOT, d = tmem + Cfg::O_COL, hi = tmem + Cfg::S_COL + b * NK, lo = tmem + Cfg::LO_COL + b * (NK / 2);
 #pragma unroll
                 for (uint32_t k = 0; k < NK / 16; ++k) {
                     const uint64_t bd = ta_desc(vb + k * 2048u, NK * 128u);
-                    ta_mma_ts(d, hi + k * 8u, bd, pv_idesc, acc | (k > 0u));
-                    if (!FP8) ta_mma_ts(d, lo + k * 8u, bd, pv_idesc, 1u);
+                    if (!FP8) ta_mma_ts(d, hi + k * 8u, bd, pv_idesc, acc | (k > 0u));
+                    ta_mma_ts(d, lo + k * 8u, bd, pv_idesc, FP8 ? acc | (k > 0u) : 1u);
                 }
                 tm_commit_to(&s.kv_empty[v_slot]);
                 tm_commit_to(&s.pv_done[b]);
@@ -917,6 +952,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++nt) {
                 ok = ta_wait(&s.kv_full[slot], use & 1u, s, c.status);
                 if (!ok) break;
+                if (!FP8) ta_fence_async();   // the copies behind the barrier were the threads' own, not the copy engine's
                 tm_fence_after();
                 if (lane == 0u) {
                     const uint32_t kb = ring_s + slot * Cfg::SLOT, d = tmem + Cfg::S_COL + (nt & 1u) * NK;
@@ -978,28 +1014,45 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         }
                         __syncwarp();
                     }
-                    // largest score of the tile
-                    float mx = -INFINITY;
-                    for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
-                        uint32_t x[32];
+                    const uint32_t p_at = lane_base + Cfg::LO_COL + b * (NK / 2);   // P's low halves (bf16), or P (f16)
+                    // a chunk of 32 scores; what the row does not see becomes -infinity
+                    auto scores = [&](uint32_t c0, uint32_t (&x)[32]) {
                         tm_ld32(s_at + c0, x);
-                        tm_ld_wait();
                         const uint32_t sees = row.sees(pos + c0);
+                        tm_ld_wait();
+                        if (!__all_sync(0xffffffffu, sees == 0xffffffffu))
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float y = __uint_as_float(x[j]) * (FP8 ? s.factor[warp][0][c0 + j] : a.scale_log2);
-                            if (sees >> j & 1u) mx = fmaxf(mx, y);
+                            for (int j = 0; j < 32; ++j)
+                                if (!(sees >> j & 1u)) x[j] = 0xff800000u;
+                    };
+                    // largest score of the tile, in binades
+                    auto largest = [&]() {
+                        float mx[2] = {-INFINITY, -INFINITY};
+                        for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
+                            uint32_t x[32];
+                            scores(c0, x);
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                float y[4];
+                                if constexpr (FP8) {   // (a key's scale is positive: -infinity stays)
+                                    const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][0][c0 + j]);
+                                    ta_unpair(ta_mul2(ta_pair(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), ks.x), y[0], y[1]);
+                                    ta_unpair(ta_mul2(ta_pair(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), ks.y), y[2], y[3]);
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(x[j + i]);
+                                }
+                                mx[0] = pg_max3(mx[0], y[0], y[1]);
+                                mx[1] = pg_max3(mx[1], y[2], y[3]);
+                            }
                         }
-                    }
-                    float f = 1.f;
-                    if (mx > m + (float)Cfg::RAISE) {
-                        f = m == -INFINITY ? 0.f : ta_exp2(m - mx);
-                        m = mx;
-                    }
-                    l *= f;
-                    f *= FP8 ? raise : 1.f;
-                    if (t > p.t0 && __any_sync(0xffffffffu, f != 1.f)) {   // O so far, in the new references
-                        if (!(ok = ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status))) break;
+                        return fmaxf(mx[0], mx[1]) * (FP8 ? 1.f : a.scale_log2);
+                    };
+                    // l and O in new references: O times f (which also holds the values' new scale), l times g
+                    auto rescale = [&](float f, float g) {
+                        l *= g;
+                        if (t == p.t0 || !__any_sync(0xffffffffu, f != 1.f)) return true;
+                        if (!ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status)) return false;
                         tm_fence_after();
                         for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 32u) {
                             uint32_t x[32];
@@ -1009,43 +1062,98 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                             for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
                             ta_tmem_st32(lane_base + Cfg::O_COL + c0, x);
                         }
-                    }
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (uint32_t c0 = 0; c0 < (uint32_t)NK; c0 += 32u) {
-                        uint32_t hi[16], lo[16];
-                        if (c0 < col0 || c0 >= col0 + ncol) {   // another copy's columns
+                        return true;
+                    };
+                    auto raise_to = [&](float mx) {   // the factor of l when the reference rises to mx, if it has to
+                        if (!(mx > m + (float)Cfg::RAISE)) return 1.f;
+                        const float g = m == -INFINITY ? 0.f : ta_exp2(m - mx);
+                        m = mx;
+                        return g;
+                    };
+                    // another copy's columns are zero
+                    if (p.split > 1u) {
+                        uint32_t zero[16];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) hi[j] = lo[j] = 0u;
-                        } else {
-                            uint32_t x[32];
-                            tm_ld32(s_at + c0, x);
-                            tm_ld_wait();
-                            const uint32_t sees = row.sees(pos + c0);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                const float e = ta_exp2(fmaf(__uint_as_float(x[j]), FP8 ? s.factor[warp][0][c0 + j] : a.scale_log2, -ref));
-                                const float y = sees >> j & 1u ? e : 0.f;
-                                sum[j & 3] += y;
-                                x[j] = __float_as_uint(FP8 ? y * s.factor[warp][1][c0 + j] : y);
+                        for (int j = 0; j < 16; ++j) zero[j] = 0u;
+                        for (uint32_t c0 = 0; c0 < (uint32_t)NK; c0 += 32u)
+                            if (c0 < col0 || c0 >= col0 + ncol) {
+                                // (P's high halves lie on the scores: this thread's own columns lie behind those it writes here, or are read by now)
+                                if (!FP8 && c0 < col0) ta_tmem_st16(s_at + c0 / 2u, zero);
+                                if (t < p.t0 + 2u) ta_tmem_st16(p_at + c0 / 2u, zero);
                             }
+                    }
+                    uint64_t sum[2];
+                    if constexpr (FP8) {
+                        // scores are turned into probabilities with the reference so far, and once more if that was too low
+                        float g = 1.f;
+                        if (__any_sync(0xffffffffu, row.T > 0u && m == -INFINITY)) g = raise_to(largest());
+                        if (!(ok = rescale(g * raise, g))) break;
+                        for (int again = 0;; ++again) {
+                            const float ref = m == -INFINITY ? 0.f : m;
+                            const uint64_t ref2 = ta_pair(-ref, -ref);
+                            float mx[2] = {-INFINITY, -INFINITY};
+                            sum[0] = sum[1] = 0ull;
+                            for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
+                                uint32_t x[32], h[16];
+                                scores(c0, x);
+#pragma unroll
+                                for (int j = 0; j < 32; j += 4) {
+                                    const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][0][c0 + j]);
+                                    const ulonglong2 vs = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][1][c0 + j]);
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        float y0, y1;
+                                        ta_unpair(ta_fma2(ta_pair(__uint_as_float(x[j + 2 * i]), __uint_as_float(x[j + 2 * i + 1])), i ? ks.y : ks.x, ref2), y0, y1);
+                                        mx[i] = pg_max3(mx[i], y0, y1);
+                                        const uint64_t e = ta_pair(ta_exp2(y0), ta_exp2(y1));
+                                        sum[i] = ta_add2(sum[i], e);
+                                        ta_unpair(ta_mul2(e, i ? vs.y : vs.x), y0, y1);
+                                        h[j / 2 + i] = ta_pack_f16(y0, y1);
+                                    }
+                                }
+                                ta_tmem_st16(p_at + c0 / 2u, h);
+                            }
+                            const float top = fmaxf(mx[0], mx[1]);
+                            // (once: scores beyond 2^26 may differ from any 32-bit reference by more; P then saturates)
+                            if (again || !__any_sync(0xffffffffu, row.T > 0u && m > -INFINITY && top > (float)Cfg::RAISE)) break;
+                            g = raise_to(m + top);
+                            if (!(ok = rescale(g, g))) break;
+                        }
+                        if (!ok) break;
+                    } else {
+                        const float g = raise_to(largest());
+                        if (!(ok = rescale(g, g))) break;
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        const uint64_t ref2 = ta_pair(-ref, -ref), sc2 = ta_pair(a.scale_log2, a.scale_log2), minus = ta_pair(-1.f, -1.f);
+                        sum[0] = sum[1] = 0ull;
+                        for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
+                            uint32_t x[32], hi[16], lo[16];
+                            scores(c0, x);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) {
-                                const float u = __uint_as_float(x[2 * j]), v = __uint_as_float(x[2 * j + 1]);
-                                if constexpr (FP8) {
-                                    const __half2 h = __floats2half2_rn(u, v);
-                                    hi[j] = *reinterpret_cast<const uint32_t*>(&h);
-                                } else {
-                                    hi[j] = pack_bf16(u, v);
-                                    lo[j] = pack_bf16(u - bf_lo(hi[j]), v - bf_hi(hi[j]));
-                                }
+                                float y0, y1;
+                                ta_unpair(ta_fma2(ta_pair(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), sc2, ref2), y0, y1);
+                                const uint64_t e = ta_pair(ta_exp2(y0), ta_exp2(y1));
+                                sum[j & 1] = ta_add2(sum[j & 1], e);
+                                ta_unpair(e, y0, y1);
+                                hi[j] = pack_bf16(y0, y1);
+                                ta_unpair(ta_fma2(ta_pair(bf_lo(hi[j]), bf_hi(hi[j])), minus, e), y0, y1);
+                                lo[j] = pack_bf16(y0, y1);
                             }
+                            // P's high halves lie on scores that have been read
+                            ta_tmem_st16(s_at + c0 / 2u, hi);
+                            ta_tmem_st16(p_at + c0 / 2u, lo);
                         }
-                        // P's high halves lie on the scores that have been read: columns c0 / 2 .. are behind those still to come
-                        ta_tmem_st16(s_at + c0 / 2u, hi);
-                        if (!FP8) ta_tmem_st16(lane_base + Cfg::LO_COL + b * (NK / 2) + c0 / 2u, lo);
+                        if (p.split > 1u) {   // the columns behind this thread's own
+                            uint32_t zero[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) zero[j] = 0u;
+                            for (uint32_t c0 = col0 + ncol; c0 < (uint32_t)NK; c0 += 32u) ta_tmem_st16(s_at + c0 / 2u, zero);
+                        }
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    float s0, s1;
+                    ta_unpair(ta_add2(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
                     ta_tmem_st_wait();
                 }
                 tm_fence_before();
