@@ -27,8 +27,8 @@ int sm_count() {
 struct TreeSpace { size_t part_ml, bytes; };
 TreeSpace tree_space(uint32_t head_dim) {
     TreeSpace s;
-    s.part_ml = (size_t)2 * TA_MAX_BLOCKS * 128 * head_dim * 4;
-    s.bytes = s.part_ml + (size_t)2 * TA_MAX_BLOCKS * 128 * 8;
+    s.part_ml = (size_t)2 * TA_MAX_BLOCKS * TA_RECORD * head_dim * 4;
+    s.bytes = s.part_ml + (size_t)2 * TA_MAX_BLOCKS * TA_RECORD * 8;
     return s;
 }
 
@@ -43,7 +43,7 @@ kl_status launch_tree(const PagedView& v, const TreeArgs& a, unsigned blocks, Pa
     if (rc != KL_OK || (rc = launch(f, dim3(blocks), Cfg::NW * 32, smem, order, v, a)) != KL_OK) return rc;
     // tables of one tile leave no unit to cut
     if ((uint64_t)v.table_pages * v.page <= (uint64_t)Cfg::NK || blocks < 2) return KL_OK;
-    return launch(kl_paged_tree_merge_kernel<HD, Cfg::NK>, dim3(blocks - 1, 16), TA_MERGE_THREADS, 0, order, v, a, (uint32_t)blocks);
+    return launch(kl_paged_tree_merge_kernel<HD, Cfg::NK, Cfg::NG * 128>, dim3(blocks - 1, 16), TA_MERGE_THREADS, 0, order, v, a, (uint32_t)blocks);
 }
 
 // Queries of new rows, or what takes their place in the output.

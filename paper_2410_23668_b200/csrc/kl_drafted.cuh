@@ -327,13 +327,15 @@ constexpr size_t rt_smem_bytes() {
 // equal share of it.  A unit (sequence, head, run of rows) cut by the border between two blocks leaves its parts (O, m, l) in the
 // workspace, and kl_paged_tree_merge_kernel joins them in order.
 //
-// Types.  bf16 caches: Q, K, V as they are, P as two bf16 halves (16 bits of it), both multiplied with V.  e4m3 caches: K's codes as
+// Types.  bf16 caches: Q, K, V as they are, P as two bf16 parts (15 bits of it), both multiplied with V.  e4m3 caches: K's codes as
 // bf16 (exact), its scales applied to the scores in 32 bits; V's codes as f16 (exact), its scales applied to P, which enters as one f16
 // (11 bits) scaled by a power of two common to all columns so far (the largest value scale seen).
 //
-// Few rows.  With at most 64 (32) rows the queries lie in TMEM's lanes twice (four times), and each copy looks at one half (quarter) of
-// a tile's keys only: P is zero elsewhere, the copies' results are joined at the end of the unit.  So all four softmax warps share the
-// exponentials of a single row's worth of queries.
+// Two groups of four softmax warps.  Where a unit has at most 128 rows, each group takes one half of every tile's keys, with a
+// reference, a sum and an O of its own, joined at the end of the unit (with at most 64 rows each row lies in TMEM's lanes twice, and a copy
+// takes a quarter); where it has up to 256, each group takes 128 rows, and the tensor cores work for one while the other has its
+// softmax.  Either way no two warps have to agree on anything within a tile, and a tile's keys and values serve up to 256 rows.  (Head
+// size 256: O alone fills half of TMEM, one group of warps, 128 rows.)
 
 struct TreeArgs {
     const int32_t* row_starts;      // [n_seqs + 1] or null: one row per sequence
@@ -348,8 +350,8 @@ struct TreeArgs {
     const uint32_t* mask;           // [n_rows][mask_words] or null
     uint32_t mask_words;
     float* lse;                     // [n_rows][nq] or null
-    float* part;                    // [2 blocks][128][hd]
-    float2* part_ml;                // [2 blocks][128]
+    float* part;                    // [2 blocks][TA_RECORD][hd]
+    float2* part_ml;                // [2 blocks][TA_RECORD]
 };
 
 constexpr int TA_MAX_BLOCKS = 160;
@@ -358,33 +360,39 @@ constexpr int TA_RING = 8;          // tiles whose scale bytes (e4m3) are kept; 
 
 template <int HD, bool FP8>
 struct TaCfg {
+    static constexpr int NG = HD == 256 ? 1 : 2;              // groups of softmax warps
     static constexpr int NK = HD == 256 ? 64 : 128;           // keys of a tile
     static constexpr int PW = FP8 ? 8 : 4;                    // producer warps
-    static constexpr int NW = 4 + 1 + PW;                     // softmax, MMA, producers
+    static constexpr int NW = 4 * NG + 2 + PW;                // softmax, two that issue matrix instructions, producers
+    static constexpr int QK_WARP = 4 * NG, PV_WARP = 4 * NG + 1;
     static constexpr int SLOT = NK * HD * 2;
-    static constexpr int NS = HD == 64 ? 8 : HD == 128 ? 5 : 4;
-    static constexpr int QBYTES = 128 * HD * 2;
-    static constexpr uint32_t S_COL = 0, LO_COL = 2 * NK, O_COL = 3 * NK;   // TMEM columns: two score buffers (P's high halves on them), P's low halves, O
+    static constexpr int NS = HD == 64 ? 8 : 4;
+    static constexpr int QBYTES = 128 * HD * 2;               // of 128 rows
+    static constexpr uint32_t O_COL = 2 * NK;                 // TMEM columns: two score buffers (P on them), an O for every group
     static constexpr int RAISE = FP8 ? 4 : 8;
 };
 constexpr float TA_HEAD = 10.f;     // e4m3: binades between P's largest (2^RAISE) and the largest f16 that stay free
+constexpr int TA_RECORD = 256;      // rows of a part in the workspace
 
 struct TaShared {
-    float x[128 * 33];                       // exchange between the copies of a row, and staging of the output
-    alignas(16) float factor[4][2][128];                 // per softmax warp: key scales (with the score scale), value scales
+    alignas(16) float x[256 * 16];           // exchange between the parts of a row; before the first piece: prefix sums over the sequences
+    alignas(16) float factor[8][2][128];     // per softmax warp: key scales (with the score scale), value scales
+    float qscale[4][2][128];                 // e4m3: what a row's queries were divided by; pieces in turn (scores run up to two short pieces ahead)
     uint8_t exps[TA_RING][2][128];
-    uint64_t pre[13 * 32];
-    uint64_t wsum[13];
-    float2 ml[128];
+    uint64_t wsum[18];
+    float ml[2][256];
     uint64_t kv_full[8], kv_empty[8], exp_full[TA_RING], piece_end[TA_RING];
-    uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done[2], o_empty;   // [2]: tiles in turn, so that a wait is never two phases behind
+    uint64_t q_full, q_empty, qs_full[4], o_empty, end;
+    // Waits go by parity and must never be two phases behind, so barriers are told apart by tile ([2]: tiles in turn), group and kind of unit.
+    uint64_t h_scores[2], h_probs[2][2], h_done[2][2];   // units of one run of rows: [tile][group]
+    uint64_t r_scores[2], r_probs[2], r_done[2];         // units of two runs: [group]; r_done: of a tile
     uint32_t bad[TA_RING];                   // pieces whose partly visible tiles hold values that are no numbers
     uint32_t tmem;
     int abort;
 };
 template <int HD, bool FP8>
 constexpr size_t ta_smem() {
-    return 1024 + TaCfg<HD, FP8>::QBYTES + (size_t)TaCfg<HD, FP8>::NS * TaCfg<HD, FP8>::SLOT + sizeof(TaShared);
+    return 1024 + (size_t)TaCfg<HD, FP8>::NG * TaCfg<HD, FP8>::QBYTES + (size_t)TaCfg<HD, FP8>::NS * TaCfg<HD, FP8>::SLOT + sizeof(TaShared);
 }
 
 // A bounded wait of a whole warp; every lane gets the same answer.
@@ -408,10 +416,12 @@ __device__ __forceinline__ bool ta_wait(uint64_t* bar, uint32_t parity, TaShared
     return __all_sync(0xffffffffu, done);
 }
 __device__ __forceinline__ void tm_commit_to(uint64_t* bar) { tm_commit(smem_u32(bar)); }
-__device__ __forceinline__ void ta_named_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }   // the softmax warps
-__device__ __forceinline__ bool ta_named_all(bool x) {   // ... whether it holds for all of them
+// Barriers of the softmax warps: group g alone (1 + g), all of them (3).
+__device__ __forceinline__ void ta_named_sync(uint32_t id, uint32_t threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ bool ta_named_all(uint32_t id, uint32_t threads, bool x) {   // ... and whether x holds for all of them
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(x ? 1u : 0u) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(id), "r"(threads), "r"(x ? 1u : 0u) : "memory");
     return r != 0u;
 }
 __device__ __forceinline__ void ta_fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -436,6 +446,11 @@ __device__ __forceinline__ void ta_tmem_st32(uint32_t taddr, const uint32_t (&r)
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
         "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
+}
+__device__ __forceinline__ void ta_tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 __device__ __forceinline__ void ta_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D[tmem] (+)= A B with both operands in shared memory, and with A in TMEM (lane = row, one column = two values of K).
@@ -505,9 +520,9 @@ __device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b) {
 // A sequence of the call.
 struct TaSeq {
     uint32_t T, r0, base, len, lo;   // new tokens, their first row, cached positions, positions in all, first position of the window
-    uint32_t tiles, head_tiles, first_tile, runs;   // key tiles: head_tiles from position 0 on (sinks), the others from first_tile on
+    uint32_t tiles, head_tiles, first_tile, runs;   // key tiles: head_tiles from position 0 on (sinks), the others from first_tile on; runs of UR rows
 };
-template <int NK>
+template <int NK, int UR>
 __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, uint32_t s) {
     TaSeq q;
     q.T = 1u;
@@ -532,7 +547,7 @@ __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, u
     q.first_tile = q.lo / NK;
     q.head_tiles = q.lo ? min((min(a.sinks, q.base) + NK - 1u) / NK, q.first_tile) : 0u;
     q.tiles = q.T ? q.head_tiles + (q.len + NK - 1u) / NK - q.first_tile : 0u;
-    q.runs = (uint32_t)(((uint64_t)q.T * a.G + 127u) / 128u);
+    q.runs = (uint32_t)(((uint64_t)q.T * a.G + UR - 1u) / UR);
     return q;
 }
 __device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.runs; }
@@ -545,12 +560,14 @@ __device__ __forceinline__ uint64_t ta_border(uint64_t work, uint32_t b, uint32_
 // One block's share of the list, piece by piece.
 struct TaPiece {
     TaSeq q;
-    uint32_t h, run, t0, t1;   // kv head, run of 128 rows, tiles
-    uint32_t rows, split, slot;   // rows of the run, copies of a row, part in the workspace (~0: the whole unit is here)
+    uint32_t h, row0, t0, t1;   // kv head, first row of the unit among the (token, head) pairs, tiles
+    uint32_t rows, slot;        // rows of the unit, part in the workspace (~0: the whole unit is here)
+    bool two;                   // two runs of rows
+    uint32_t split, R;          // parts of a group's columns, rows that lie next to one another in TMEM's lanes
 };
-template <int NK, int NW>
+template <int NK, int NW, int UR>
 struct TaIter {
-    uint32_t s, n;
+    uint32_t s;
     uint64_t off, left;
     bool begun;
     TaSeq q;
@@ -562,23 +579,26 @@ struct TaIter {
         const uint32_t share = pg_find<NW>(pre, g), per = (c.n_seqs + NW * 32u - 1u) / (NW * 32u);
         s = share * per;
         off = g - pre[share];
-        q = ta_seq<NK>(c, a, s);
+        q = ta_seq<NK, UR>(c, a, s);
     }
     __device__ __forceinline__ bool next(const PagedView& c, const TreeArgs& a, TaPiece& p) {
         if (!left) return false;
         while (off >= ta_work(c, q)) {
             off -= ta_work(c, q);
             if (++s >= c.n_seqs) return false;
-            q = ta_seq<NK>(c, a, s);
+            q = ta_seq<NK, UR>(c, a, s);
         }
         const uint64_t u = pg_div(off, q.tiles);
         p.q = q;
         p.t0 = (uint32_t)(off - u * q.tiles);
         p.h = (uint32_t)pg_div(u, q.runs);
-        p.run = (uint32_t)(u - (uint64_t)p.h * q.runs);
+        const uint32_t run = (uint32_t)(u - (uint64_t)p.h * q.runs);
+        p.row0 = run * UR;
         p.t1 = (uint32_t)min((uint64_t)q.tiles, p.t0 + left);
-        p.rows = (uint32_t)min((uint64_t)128u, (uint64_t)q.T * a.G - (uint64_t)p.run * 128u);
-        p.split = p.rows <= 32u && NK == 128 ? 4u : p.rows <= 64u ? 2u : 1u;   // a copy looks at 32 keys or more
+        p.rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - p.row0);
+        p.two = p.rows > 128u;
+        p.split = p.rows <= 64u ? 2u : 1u;
+        p.R = p.rows <= 32u && UR == 256 ? 32u : 128u / p.split;
         p.slot = p.t0 == 0u && p.t1 == q.tiles ? ~0u : 2u * blockIdx.x + (begun ? 1u : 0u);
         begun = true;
         off += p.t1 - p.t0;
@@ -608,17 +628,17 @@ __device__ __forceinline__ int64_t ta_far(const TreeArgs& a, const TaSeq& q) {
 // What a row sees.
 struct TaRow {
     uint32_t base, T, i;            // cached positions, new tokens, the row's own number (T == 0: not a row)
-    int64_t after;                  // cached positions up to this one are behind the window
+    int32_t after;                  // cached positions up to this one are behind the window (-1: none)
     uint32_t sinks, window;
     const uint32_t* mask;
     uint32_t mask_words;
     // bits of positions p .. p + 31
-    __device__ __forceinline__ uint32_t sees(uint32_t p) const {
+    __device__ __noinline__ uint32_t sees(uint32_t p) const {
         if (!T) return 0u;
         uint32_t bits = 0xffffffffu;
         if (p + 32u > base) bits = p >= base ? 0u : 0xffffffffu >> (p + 32u - base);
-        if ((int64_t)p <= after) {
-            uint32_t old = (int64_t)p + 31 <= after ? 0u : 0xffffffffu << (uint32_t)(after + 1 - (int64_t)p);
+        if ((int32_t)p <= after) {
+            uint32_t old = (int32_t)p + 31 <= after ? 0u : 0xffffffffu << (uint32_t)(after + 1 - (int32_t)p);
             if (p < sinks) old |= p + 32u <= sinks ? 0xffffffffu : 0xffffffffu >> (p + 32u - sinks);
             bits &= old;
         }
@@ -651,18 +671,17 @@ __device__ __forceinline__ TaRow ta_row(const TreeArgs& a, const TaPiece& p, uin
     w.after = -1;
     if (r < p.rows) {
         w.T = p.q.T;
-        w.i = (p.run * 128u + r) / a.G;
+        w.i = (p.row0 + r) / a.G;
         if (a.mask) w.mask = a.mask + (size_t)(p.q.r0 + w.i) * a.mask_words;
         if (a.window) {
             const int64_t at = a.row_positions ? max((int64_t)a.row_positions[p.q.r0 + w.i], (int64_t)w.base) : (int64_t)w.base + w.i;
-            w.after = at - (int64_t)a.window;
+            w.after = (int32_t)max(at - (int64_t)a.window, (int64_t)-1);
         }
     }
     return w;
 }
 
-// e4m3 codes, sixteen at a time, as bf16 or f16; `tidy`: codes that are no numbers become zero and are told of.
-template <bool BF16>
+// e4m3 codes, sixteen at a time, as f16 (exact); `tidy`: codes that are no numbers become zero and are told of.
 __device__ __forceinline__ bool ta_widen(const uint4& raw, uint4 (&to)[2], bool tidy) {
     uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w}, r[8];
     bool bad = false;
@@ -677,15 +696,7 @@ __device__ __forceinline__ bool ta_widen(const uint4& raw, uint4 (&to)[2], bool 
         }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t h = pg_e4m3x2_to_f16x2(w[i / 2] >> 16 * (i & 1) & 0xffffu);
-        if constexpr (BF16) {
-            const float2 f = pg_f16x2_to_float2(h);
-            r[i] = pack_bf16(f.x, f.y);
-        } else {
-            r[i] = h;
-        }
-    }
+    for (int i = 0; i < 8; ++i) r[i] = pg_e4m3x2_to_f16x2(w[i / 2] >> 16 * (i & 1) & 0xffffu);
     to[0] = make_uint4(r[0], r[1], r[2], r[3]);
     to[1] = make_uint4(r[4], r[5], r[6], r[7]);
     return bad;
@@ -694,9 +705,9 @@ __device__ __forceinline__ bool ta_widen(const uint4& raw, uint4 (&to)[2], bool 
 template <int HD, bool FP8>
 __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kernel(const PagedView c, const TreeArgs a) {
     using Cfg = TaCfg<HD, FP8>;
-    constexpr int NK = Cfg::NK, PW = Cfg::PW, NW = Cfg::NW, NS = Cfg::NS;
+    constexpr int NG = Cfg::NG, NK = Cfg::NK, PW = Cfg::PW, NW = Cfg::NW, NS = Cfg::NS, UR = NG * 128;
     extern __shared__ uint8_t ta_raw[];
-    const uint32_t raw = smem_u32(ta_raw), q_s = (raw + 1023u) & ~1023u, ring_s = q_s + Cfg::QBYTES;
+    const uint32_t raw = smem_u32(ta_raw), q_s = (raw + 1023u) & ~1023u, ring_s = q_s + NG * Cfg::QBYTES;
     TaShared& s = *reinterpret_cast<TaShared*>(ta_raw + (ring_s - raw) + (size_t)NS * Cfg::SLOT);
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
     griddep_launch();
@@ -710,17 +721,24 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         }
         mbar_init(smem_u32(&s.q_full), PW);
         mbar_init(smem_u32(&s.q_empty), 1);
+        mbar_init(smem_u32(&s.end), 2);
+        mbar_init(smem_u32(&s.o_empty), 4 * NG);
+        for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&s.qs_full[i]), PW);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&s.s_full[i]), 1);
-            mbar_init(smem_u32(&s.p_full[i]), 4);
-            mbar_init(smem_u32(&s.pv_done[i]), 1);
+            mbar_init(smem_u32(&s.h_scores[i]), 1);
+            mbar_init(smem_u32(&s.r_scores[i]), 1);
+            mbar_init(smem_u32(&s.r_probs[i]), 4);
+            mbar_init(smem_u32(&s.r_done[i]), 1);
+            for (int g = 0; g < 2; ++g) {
+                mbar_init(smem_u32(&s.h_probs[i][g]), 4);
+                mbar_init(smem_u32(&s.h_done[i][g]), 1);
+            }
         }
-        mbar_init(smem_u32(&s.o_empty), 4);
         s.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         ta_fence_async();
     }
-    if (warp == 4u) tm_alloc(smem_u32(&s.tmem), 512);
+    if (warp == (uint32_t)Cfg::QK_WARP) tm_alloc(smem_u32(&s.tmem), 512);
     griddep_wait();
     if (a.row_starts && blockIdx.x == 0u) {
         for (uint32_t i = tid; i < c.n_seqs; i += NW * 32) {
@@ -728,17 +746,20 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             if (x < 0 || y < x || (uint32_t)y > a.n_rows) pg_error(c);
         }
     }
+    uint64_t* const pre = reinterpret_cast<uint64_t*>(s.x);
+    static_assert(sizeof(s.x) >= NW * 32 * 8 && alignof(TaShared) >= 16, "prefix sums");
     const bool stopped = pg_stopped(c);   // (a barrier of the whole block where there is a status word)
-    const uint64_t work = stopped ? 0ull : pg_prefix<NW>(c.n_seqs, s.pre, s.wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK>(c, a, i)); });
+    const uint64_t work = stopped ? 0ull : pg_prefix<NW>(c.n_seqs, pre, s.wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK, UR>(c, a, i)); });
     __syncthreads();
     tm_fence_after();
     const uint32_t tmem = s.tmem;
     const uint64_t g0 = ta_border(work, blockIdx.x, gridDim.x), g1 = ta_border(work, blockIdx.x + 1u, gridDim.x);
-    TaIter<NK, NW> iter(c, a, s.pre, g0, g1 - g0);
+    TaIter<NK, NW, UR> iter(c, a, pre, g0, g1 - g0);
+    __syncthreads();   // the prefix sums have been read
     TaPiece p;
 
-    if (warp >= 5u) {   // ---- producers: queries, keys, values into shared memory
-        const uint32_t pw = warp - 5u;
+    if (warp > (uint32_t)Cfg::PV_WARP) {   // ---- producers: queries, keys, values into shared memory
+        const uint32_t pw = warp - Cfg::PV_WARP - 1u;
         constexpr uint32_t RPW = NK / PW;                  // rows of a tile per warp, one per lane
         constexpr uint32_t CH = FP8 ? HD / 16 : HD / 8;    // 16-byte pieces of a row in the cache
         constexpr uint32_t STEPS = RPW * CH / 32;          // pieces per lane
@@ -776,24 +797,46 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
             Look next = look_up(p.t0);
-            // queries: lane row L holds row L % (128 / split) of the run
+            // queries: row L of the first (second) 128 is row L % R (128 + L) of the unit
             if (npiece > 0u && !(ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status))) break;
             {
                 constexpr uint32_t QC = HD / 8;
-                const uint32_t R = 128u / p.split;
+                const uint32_t R = p.R, pieces = (p.two ? 256u : 128u) * QC;
 #pragma unroll 4
-                for (uint32_t i = pw * 32u + lane; i < 128u * QC; i += PW * 32u) {
-                    const uint32_t L = i / QC, ch = i % QC, r = L % R;
+                for (uint32_t i = pw * 32u + lane; i < pieces; i += PW * 32u) {
+                    const uint32_t half = i / (128u * QC), L = i / QC % 128u, ch = i % QC, r = p.two ? half * 128u + L : L % R;
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (r < p.rows) {
-                        const uint32_t gr = p.run * 128u + r, tok = gr / a.G, g = gr - tok * a.G;
+                        const uint32_t gr = p.row0 + r, tok = gr / a.G, g = gr - tok * a.G;
                         v = *reinterpret_cast<const uint4*>(a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + g) * HD + ch * 8u) * 2u);
                     }
-                    ta_st16(q_s + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v);
+                    if constexpr (FP8) {   // as f16, divided by a power of two that brings the row's largest to 2^14 .. 2^15
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, big = 0u;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) big = pg_larger(big, w[j]);
+                        big = max(big & 0x7fffu, big >> 16 & 0x7fffu);
+                        if (((v.x & 0x7f807f80u) + 0x00800080u | (v.y & 0x7f807f80u) + 0x00800080u | (v.z & 0x7f807f80u) + 0x00800080u | (v.w & 0x7f807f80u) + 0x00800080u) & 0x80008000u)
+                            big = 0x7f80u;   // infinities and NaN stay what they are
+#pragma unroll
+                        for (uint32_t o = QC / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                        const int e = (int)(big >> 7);   // 1 .. 254 for numbers that are not tiny
+                        const float inv = e == 255 || e == 0 ? 1.f : pg_scale((uint32_t)min(268 - e, 254));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const __half2 h = __floats2half2_rn(bf_lo(w[j]) * inv, bf_hi(w[j]) * inv);
+                            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        v = make_uint4(w[0], w[1], w[2], w[3]);
+                        if (ch == 0u) s.qscale[npiece & 3u][half][L] = 1.f / inv;
+                    }
+                    ta_st16(q_s + half * Cfg::QBYTES + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v);
                 }
                 ta_fence_async();
                 __syncwarp();
-                if (lane == 0u) mbar_arrive(smem_u32(&s.q_full));
+                if (lane == 0u) {
+                    mbar_arrive(smem_u32(&s.q_full));
+                    mbar_arrive(smem_u32(&s.qs_full[npiece & 3u]));
+                }
             }
             const int64_t far = ta_far(a, p.q);
             bool bad = false;
@@ -803,6 +846,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                     int64_t at, ex;
                     place(next, at, ex);
                     next = look_up(t + 1u);
+#pragma unroll 1
                     for (int kv = 0; ok && kv < 2; ++kv) {
                         ok = take_slot();
                         if (!ok) break;
@@ -837,78 +881,68 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                     }
                 }
             } else {
-                // Two tiles' loads are under way while a third is widened, and the pages of the one after are looked up.
-                uint4 kraw[2][STEPS], vraw[2][STEPS];
-                uint32_t ke[2], ve[2];
-                int64_t at[2], ex[2];
-                auto request = [&](const uint8_t* src, int64_t from, uint4 (&to)[STEPS]) {
+                // The next tile's loads are under way while one is widened, and the pages of the one after are looked up.
+                uint4 kraw[STEPS], vraw[STEPS];
+                uint32_t ke = 0, ve = 0;
+                int64_t at, ex;
+                auto request = [&](const uint8_t* src, uint4 (&to)[STEPS]) {
 #pragma unroll
                     for (uint32_t i = 0; i < STEPS; ++i) {
                         const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH;
-                        const int64_t o = __shfl_sync(0xffffffffu, from, r);
+                        const int64_t o = __shfl_sync(0xffffffffu, at, r);
                         to[i] = o >= 0 ? *reinterpret_cast<const uint4*>(src + o + ch * 16u) : make_uint4(0, 0, 0, 0);
                     }
                 };
-                auto request_scales = [&](int z) {
-                    ke[z] = ve[z] = 0;
-                    if (ex[z] >= 0) {
-                        ke[z] = c.ke[ex[z]];
-                        ve[z] = c.ve[ex[z]];
+                auto request_scales = [&]() {
+                    ke = ve = 0;
+                    if (ex >= 0) {
+                        ke = c.ke[ex];
+                        ve = c.ve[ex];
                     }
                 };
-                Look after = look_up(p.t0 + 1u);
-                place(next, at[0], ex[0]);
-                next = look_up(p.t0 + 2u);
-                request(c.k, at[0], kraw[0]);
-                request_scales(0);
-                request(c.v, at[0], vraw[0]);
-                place(after, at[1], ex[1]);
-                request(c.k, at[1], kraw[1]);
-                request_scales(1);
-                request(c.v, at[1], vraw[1]);
-                for (uint32_t t0 = p.t0; ok && t0 < p.t1; t0 += 2u) {
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const uint32_t t = t0 + z;
-                        if (!ok || t >= p.t1) break;
-                        const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
-                        // scale bytes; a row that nobody sees gets the smallest
-                        if (lane < RPW) {
-                            s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke[z];
-                            s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve[z];
-                        }
-                        __syncwarp();
-                        if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
-                        place(next, at[z], ex[z]);   // of tile t + 2
-                        next = look_up(t + 3u);
-#pragma unroll
-                        for (int kv = 0; kv < 2; ++kv) {
-                            ok = ok && take_slot();
-                            if (!ok) break;
-                            const uint32_t dst = ring_s + slot * Cfg::SLOT;
-#pragma unroll
-                            for (uint32_t i = 0; i < STEPS; ++i) {
-                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
-                                uint4 w[2];
-                                if (kv == 0) ta_widen<true>(kraw[z][i], w, false);
-                                else bad |= ta_widen<false>(vraw[z][i], w, mixed);
-                                const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
-                                ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
-                                ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
-                            }
-                            if (kv == 0) {
-                                request(c.k, at[z], kraw[z]);
-                                request_scales(z);
-                            } else {
-                                request(c.v, at[z], vraw[z]);
-                            }
-                            ta_fence_async();
-                            __syncwarp();
-                            if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
-                            next_slot();
-                        }
-                        ++ntile;
+                place(next, at, ex);
+                next = look_up(p.t0 + 1u);
+                request(c.k, kraw);
+                request_scales();
+                request(c.v, vraw);
+                for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
+                    const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
+                    // scale bytes; a row that nobody sees gets the smallest
+                    if (lane < RPW) {
+                        s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke;
+                        s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve;
                     }
+                    __syncwarp();
+                    if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
+                    place(next, at, ex);   // of tile t + 1
+                    next = look_up(t + 2u);
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        ok = ok && take_slot();
+                        if (!ok) break;
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+#pragma unroll
+                        for (uint32_t i = 0; i < STEPS; ++i) {
+                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
+                            uint4 w[2];
+                            if (kv == 0) ta_widen(kraw[i], w, false);
+                            else bad |= ta_widen(vraw[i], w, mixed);
+                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
+                            ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
+                            ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
+                        }
+                        if (kv == 0) {
+                            request(c.k, kraw);
+                            request_scales();
+                        } else {
+                            request(c.v, vraw);
+                        }
+                        ta_fence_async();
+                        __syncwarp();
+                        if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
+                        next_slot();
+                    }
+                    ++ntile;
                 }
             }
             if (bad) atomicOr(&s.bad[npiece % TA_RING], 1u);
@@ -917,82 +951,141 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             ++npiece;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp == 4u) {   // ---- MMA
-        constexpr uint32_t qk_idesc = ta_idesc(1u, NK, false), pv_idesc = ta_idesc(FP8 ? 0u : 1u, HD, true);
-        uint32_t slot = 0, use = 0, nt = 0, npiece = 0;
-        bool ok = true;
-        uint32_t v_slot = 0, v_use = 0;
-        auto pv = [&](uint32_t tile, uint32_t acc) {   // the tile's number among all of this block
-            const uint32_t b = tile & 1u;
-            if (!ta_wait(&s.p_full[b], (tile >> 1) & 1u, s, c.status) || !ta_wait(&s.kv_full[v_slot], v_use & 1u, s, c.status)) return false;
-            if (!FP8) ta_fence_async();
+    } else if (warp >= (uint32_t)Cfg::QK_WARP) {   // ---- matrix instructions: one warp for Q K^T, one for P V
+        // A lone warp takes some five cycles per instruction, and 64 a matrix instruction: hence two warps, descriptors made once per
+        // tile, and no loops around the instructions.
+        constexpr uint32_t type = FP8 ? 0u : 1u, qk_idesc = ta_idesc(type, NK, false), pv_idesc = ta_idesc(type, HD, true);
+        uint32_t tile = 0, nh = 0, nr = 0, npiece = 0;   // tiles so far: all, of units of one run, of units of two
+        bool ok = true, two = false;
+        auto landed = [&](uint32_t n) {   // slot of the ring that is the n-th to be filled
+            if (!ta_wait(&s.kv_full[n % NS], n / NS & 1u, s, c.status)) return false;
+            if (!FP8) ta_fence_async();   // the copies behind the barrier were the threads' own, not the copy engine's
             tm_fence_after();
-            if (lane == 0u) {
-                const uint32_t vb = ring_s + v_slot * Cfg::SLOT, d = tmem + Cfg::O_COL, hi = tmem + Cfg::S_COL + b * NK, lo = tmem + Cfg::LO_COL + b * (NK / 2);
-#pragma unroll
-                for (uint32_t k = 0; k < NK / 16; ++k) {
-                    const uint64_t bd = ta_desc(vb + k * 2048u, NK * 128u);
-                    if (!FP8) ta_mma_ts(d, hi + k * 8u, bd, pv_idesc, acc | (k > 0u));
-                    ta_mma_ts(d, lo + k * 8u, bd, pv_idesc, FP8 ? acc | (k > 0u) : 1u);
-                }
-                tm_commit_to(&s.kv_empty[v_slot]);
-                tm_commit_to(&s.pv_done[b]);
-            }
-            __syncwarp();
             return true;
         };
-        auto advance = [&](uint32_t& sl, uint32_t& us) {
-            if (++sl == NS) {
-                sl = 0;
-                ++us;
-            }
-        };
-        while (ok && iter.next(c, a, p)) {
-            ok = ta_wait(&s.q_full, npiece & 1u, s, c.status);
-            for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++nt) {
-                ok = ta_wait(&s.kv_full[slot], use & 1u, s, c.status);
-                if (!ok) break;
-                if (!FP8) ta_fence_async();   // the copies behind the barrier were the threads' own, not the copy engine's
-                tm_fence_after();
-                if (lane == 0u) {
-                    const uint32_t kb = ring_s + slot * Cfg::SLOT, d = tmem + Cfg::S_COL + (nt & 1u) * NK;
+        if (warp == (uint32_t)Cfg::QK_WARP) {
+            auto qk = [&](uint32_t d, uint32_t half, uint32_t sl) {   // scores of queries `half` and the keys in slot sl into score buffer d
+                const uint64_t qd = ta_desc(q_s + half * Cfg::QBYTES, 16u), kd = ta_desc(ring_s + sl * Cfg::SLOT, 16u);
+                const uint32_t to = tmem + d * NK;
 #pragma unroll
-                    for (uint32_t k = 0; k < HD / 16; ++k)
-                        ta_mma_ss(d, ta_desc(q_s + k / 4u * (128u * 128u) + k % 4u * 32u, 16u), ta_desc(kb + k / 4u * (NK * 128u) + k % 4u * 32u, 16u), qk_idesc, k > 0u);
-                    tm_commit_to(&s.s_full[nt & 1u]);
-                    tm_commit_to(&s.kv_empty[slot]);
-                    if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
+                for (uint32_t k = 0; k < HD / 16; ++k)   // 32 bytes along the swizzled rows, then the next 64 columns
+                    ta_mma_ss(to, qd + (k / 4u * (128u * 128u / 16u) + k % 4u * 2u), kd + (k / 4u * (NK * 128u / 16u) + k % 4u * 2u), qk_idesc, k > 0u);
+            };
+            while (ok && iter.next(c, a, p)) {
+                // the other kind of unit used the score buffers last: both have been read
+                if (npiece > 0u && p.two != two) {
+                    if (two) {
+                        for (uint32_t g = 0; ok && g < 2u; ++g) ok = ta_wait(&s.r_done[g], (nr - 1u) & 1u, s, c.status);
+                    } else {
+                        for (uint32_t back = nh > 1u ? 2u : 1u; back > 0u; --back)
+                            for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) ok = ta_wait(&s.h_done[(nh - back) & 1u][g], (nh - back) >> 1 & 1u, s, c.status);
+                    }
                 }
-                __syncwarp();
-                advance(slot, use);
-                // the values of this tile lie in the next slot
-                if (t > p.t0) ok = pv(nt - 1u, t - 1u > p.t0);
-                else if (npiece > 0u) ok = ta_wait(&s.o_empty, (npiece - 1u) & 1u, s, c.status);   // the last unit's result has been read
-                v_slot = slot;
-                v_use = use;
-                advance(slot, use);
+                two = p.two;
+                ok = ok && ta_wait(&s.q_full, npiece & 1u, s, c.status);
+                for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++tile) {
+                    if (!(ok = landed(2u * tile))) break;
+                    const uint32_t sl = 2u * tile % NS;
+                    if (!two) {
+                        if (nh >= 2u)   // P of the last tile but one, which lies on this score buffer, has been read
+                            for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) ok = ta_wait(&s.h_done[nh & 1u][g], (nh - 2u) >> 1 & 1u, s, c.status);
+                        if (!ok) break;
+                        tm_fence_after();
+                        if (lane == 0u) {
+                            qk(nh & 1u, 0u, sl);
+                            tm_commit_to(&s.h_scores[nh & 1u]);
+                            tm_commit_to(&s.kv_empty[sl]);
+                            if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
+                        }
+                        ++nh;
+                    } else {
+#pragma unroll 1
+                        for (uint32_t g = 0; ok && g < 2u; ++g) {
+                            if (nr > 0u && !(ok = ta_wait(&s.r_done[g], (nr - 1u) & 1u, s, c.status))) break;
+                            tm_fence_after();
+                            if (lane == 0u) {
+                                qk(g, g, sl);
+                                tm_commit_to(&s.r_scores[g]);
+                                if (g == 1u) {
+                                    tm_commit_to(&s.kv_empty[sl]);
+                                    if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        ++nr;
+                    }
+                    __syncwarp();
+                }
+                ++npiece;
             }
-            if (ok) ok = pv(nt - 1u, p.t1 - 1u > p.t0);
-            ++npiece;
+        } else {
+            // O += P V over 16 * n keys, from the first of which P lies at pa and V at vd
+            auto pv = [&](uint32_t o, uint32_t pa, uint64_t vd, auto n, uint32_t acc) {
+                const uint32_t d = tmem + Cfg::O_COL + o * HD;
+#pragma unroll
+                for (uint32_t k = 0; k < decltype(n)::value; ++k) {
+                    ta_mma_ts(d, pa + k * 16u, vd + k * (2048u / 16u), pv_idesc, k > 0u ? 1u : acc);
+                    if (!FP8) ta_mma_ts(d, pa + k * 16u + 8u, vd + k * (2048u / 16u), pv_idesc, 1u);
+                }
+            };
+            while (ok && iter.next(c, a, p)) {
+                if (npiece > 0u) ok = ta_wait(&s.o_empty, (npiece - 1u) & 1u, s, c.status);   // the last unit's result has been read
+                for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++tile) {
+                    const uint32_t n = 2u * tile + 1u, sl = n % NS;
+                    const uint64_t vd = ta_desc(ring_s + sl * Cfg::SLOT, NK * 128u);
+                    if (!(ok = landed(n))) break;
+                    const uint32_t b = nh & 1u;
+#pragma unroll 1
+                    for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) {
+                        if (!(ok = p.two ? ta_wait(&s.r_probs[g], nr & 1u, s, c.status) : ta_wait(&s.h_probs[b][g], nh >> 1 & 1u, s, c.status))) break;
+                        tm_fence_after();
+                        if (lane == 0u) {
+                            if (p.two) pv(g, tmem + g * NK, vd, std::integral_constant<uint32_t, NK / 16>{}, t > p.t0);
+                            else pv(g, tmem + b * NK + g * (NK / NG), vd + g * (NK / NG * 128u / 16u), std::integral_constant<uint32_t, NK / 16 / NG>{}, t > p.t0);
+                            if (g + 1u == (uint32_t)NG) tm_commit_to(&s.kv_empty[sl]);
+                            tm_commit_to(p.two ? &s.r_done[g] : &s.h_done[b][g]);
+                        }
+                        __syncwarp();
+                    }
+                    if (p.two) ++nr;
+                    else ++nh;
+                }
+                ++npiece;
+            }
         }
-        if (nt > 0u) ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status);
-    } else {   // ---- softmax and results: thread L owns TMEM lane L
-        const uint32_t L = tid, lane_base = tmem + (warp * 32u << 16);
-        uint32_t nt = 0, npiece = 0;
+        // nothing may still be under way when TMEM is given back
+        if (lane == 0u) tm_commit_to(&s.end);
+        __syncwarp();
+        ta_wait(&s.end, 0u, s, c.status);
+    } else {   // ---- softmax and results: thread L of a group owns TMEM lane L
+        const uint32_t grp = warp >> 2, L = tid & 127u, lane_base = tmem + ((warp & 3u) * 32u << 16), o_at = lane_base + Cfg::O_COL + grp * HD;
+        float(&kf)[128] = s.factor[warp][0];
+        float(&vf)[128] = s.factor[warp][1];
+        uint32_t nt = 0, nh = 0, nr = 0, npiece = 0;
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
-            const uint32_t R = 128u / p.split, r = L % R, col0 = L / R * (NK / p.split), ncol = NK / p.split;
-            const TaRow row = ta_row(a, p, r);
+            // units of one run: the group's columns in `split` parts, each in another quarter (half) of the lanes; where every quarter holds
+            // all rows (R = 32), the groups take every other one, so that all four schedulers have one warp of each at work
+            const uint32_t R = p.R, r = p.two ? grp * 128u + L : L % R, quarter = L >> 5;
+            const uint32_t ncol = p.two ? (uint32_t)NK : (uint32_t)NK / NG / p.split, share = R == 32u ? quarter >> 1 : L / R;
+            const uint32_t col0 = p.two ? 0u : grp * (NK / NG) + share * ncol, col1 = col0 + ncol;
+            const bool idle = !p.two && R == 32u && (quarter & 1u) != grp;
+            const TaRow row = ta_row(a, p, idle ? ~0u : r);
             const bool active = __any_sync(0xffffffffu, row.T > 0u);
-            float m = -INFINITY, l = 0.f;
+            float m = -INFINITY, l = 0.f, qs = 1.f;
             int ev_ref = -1;   // e4m3: the largest value scale byte so far
-            for (uint32_t t = p.t0; t < p.t1; ++t, ++nt) {
-                const uint32_t b = nt & 1u, pos = ta_tile_pos(p.q, t, NK), s_at = lane_base + Cfg::S_COL + b * NK;
+            if (FP8) {
+                ok = ta_wait(&s.qs_full[npiece & 3u], npiece >> 2 & 1u, s, c.status);
+                qs = s.qscale[npiece & 3u][p.two ? grp : 0u][L];
+            }
+            for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++nt) {
+                const uint32_t buf = p.two ? grp : nh & 1u, pos = ta_tile_pos(p.q, t, NK), s_at = lane_base + buf * NK;
                 if (FP8 && !(ok = ta_wait(&s.exp_full[nt % TA_RING], (nt / TA_RING) & 1u, s, c.status))) break;
-                if (!(ok = ta_wait(&s.s_full[b], (nt >> 1) & 1u, s, c.status))) break;
+                if (!(ok = p.two ? ta_wait(&s.r_scores[grp], nr & 1u, s, c.status) : ta_wait(&s.h_scores[buf], (nh >> 1) & 1u, s, c.status))) break;
                 tm_fence_after();
                 if (active) {
-                    float raise = 1.f;   // of O and l: by a new reference of the values' scales
+                    float raise = 1.f;   // of O: by a new reference of the values' scales
                     if constexpr (FP8) {
                         const uint32_t kw = *reinterpret_cast<const uint32_t*>(&s.exps[nt % TA_RING][0][lane * 4u % NK]);
                         const uint32_t vw = *reinterpret_cast<const uint32_t*>(&s.exps[nt % TA_RING][1][lane * 4u % NK]);
@@ -1006,150 +1099,128 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         }
                         __syncwarp();
                         if (lane * 4u < (uint32_t)NK) {
+                            float k4[4], v4[4];
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                s.factor[warp][0][lane * 4u + j] = pg_scale(kw >> 8 * j & 0xffu) * a.scale_log2;
-                                s.factor[warp][1][lane * 4u + j] = ta_exp2((float)((int)(vw >> 8 * j & 0xffu) - ev_ref) + TA_HEAD);
+                                k4[j] = pg_scale(kw >> 8 * j & 0xffu) * a.scale_log2;
+                                v4[j] = ta_exp2((float)((int)(vw >> 8 * j & 0xffu) - ev_ref) + TA_HEAD);
                             }
+                            *reinterpret_cast<float4*>(&kf[lane * 4u]) = make_float4(k4[0], k4[1], k4[2], k4[3]);
+                            *reinterpret_cast<float4*>(&vf[lane * 4u]) = make_float4(v4[0], v4[1], v4[2], v4[3]);
                         }
                         __syncwarp();
                     }
-                    const uint32_t p_at = lane_base + Cfg::LO_COL + b * (NK / 2);   // P's low halves (bf16), or P (f16)
-                    // a chunk of 32 scores; what the row does not see becomes -infinity
+                    // whether every row of the warp sees all of the tile
+                    const bool full = __all_sync(0xffffffffu, row.T == 0u || (pos + NK <= row.base && (int32_t)pos > row.after));
+                    // 32 scores; what the row does not see is -infinity.  e4m3: times the keys' scales
                     auto scores = [&](uint32_t c0, uint32_t (&x)[32]) {
                         tm_ld32(s_at + c0, x);
-                        const uint32_t sees = row.sees(pos + c0);
                         tm_ld_wait();
-                        if (!__all_sync(0xffffffffu, sees == 0xffffffffu))
+                        if (!full) {
+                            const uint32_t sees = row.sees(pos + c0);
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
                                 if (!(sees >> j & 1u)) x[j] = 0xff800000u;
-                    };
-                    // largest score of the tile, in binades
-                    auto largest = [&]() {
-                        float mx[2] = {-INFINITY, -INFINITY};
-                        for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
-                            uint32_t x[32];
-                            scores(c0, x);
+                        }
+                        if constexpr (FP8) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                float y[4];
-                                if constexpr (FP8) {   // (a key's scale is positive: -infinity stays)
-                                    const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][0][c0 + j]);
-                                    ta_unpair(ta_mul2(ta_pair(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), ks.x), y[0], y[1]);
-                                    ta_unpair(ta_mul2(ta_pair(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), ks.y), y[2], y[3]);
-                                } else {
+                            for (int j = 0; j < 32; j += 4) {   // (scales are positive: -infinity stays)
+                                const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(&kf[c0 + j]);
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(x[j + i]);
+                                for (int i = 0; i < 4; i += 2) {
+                                    float y0, y1;
+                                    ta_unpair(ta_mul2(ta_pair(__uint_as_float(x[j + i]), __uint_as_float(x[j + i + 1])), i ? ks.y : ks.x), y0, y1);
+                                    x[j + i] = __float_as_uint(y0);
+                                    x[j + i + 1] = __float_as_uint(y1);
                                 }
-                                mx[0] = pg_max3(mx[0], y[0], y[1]);
-                                mx[1] = pg_max3(mx[1], y[2], y[3]);
                             }
                         }
-                        return fmaxf(mx[0], mx[1]) * (FP8 ? 1.f : a.scale_log2);
                     };
+                    // the largest of the own columns' scores, in binades; the last 32 stay in x
+                    uint32_t x[32];
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (uint32_t c0 = col0; c0 < col1; c0 += 32u) {
+                        scores(c0, x);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            top[0] = pg_max3(top[0], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+                            top[1] = pg_max3(top[1], __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]));
+                        }
+                    }
+                    const float unit_s = FP8 ? qs : a.scale_log2;
                     // l and O in new references: O times f (which also holds the values' new scale), l times g
                     auto rescale = [&](float f, float g) {
                         l *= g;
                         if (t == p.t0 || !__any_sync(0xffffffffu, f != 1.f)) return true;
-                        if (!ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status)) return false;
+                        // (units of two runs: the scores came behind the last product)
+                        if (!p.two && !ta_wait(&s.h_done[(nh - 1u) & 1u][grp], ((nh - 1u) >> 1) & 1u, s, c.status)) return false;
                         tm_fence_after();
-                        for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 32u) {
-                            uint32_t x[32];
-                            tm_ld32(lane_base + Cfg::O_COL + c0, x);
+#pragma unroll 1
+                        for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
+                            uint32_t x[16];
+                            tm_ld16(o_at + c0, x);
                             tm_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
-                            ta_tmem_st32(lane_base + Cfg::O_COL + c0, x);
+                            for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
+                            ta_tmem_st16(o_at + c0, x);
                         }
                         return true;
                     };
                     auto raise_to = [&](float mx) {   // the factor of l when the reference rises to mx, if it has to
-                        if (!(mx > m + (float)Cfg::RAISE)) return 1.f;
+                        // (scores of 2^22 and more: a step of the reference is as large as the slack, and no score may lie above it)
+                        if (!(mx > m + (fabsf(m) < 4194304.f ? (float)Cfg::RAISE : 0.f))) return 1.f;
+                        if (fabsf(mx) >= 4194304.f) mx = fmaf(fabsf(mx), 1.2e-7f, mx);
                         const float g = m == -INFINITY ? 0.f : ta_exp2(m - mx);
                         m = mx;
                         return g;
                     };
-                    // another copy's columns are zero
-                    if (p.split > 1u) {
+                    const float g = raise_to(fmaxf(top[0], top[1]) * unit_s);
+                    if (!(ok = rescale(g * raise, g))) break;
+                    // P on the scores that have been read: of 16 columns the first eight hold the high halves (f16: all), the others the low ones
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    const uint64_t ref2 = ta_pair(-ref, -ref), sc2 = ta_pair(unit_s, unit_s), minus = ta_pair(-1.f, -1.f);
+                    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll 1
+                    for (uint32_t c0 = col1 - 32u;; c0 -= 32u) {
+                        if (c0 + 32u != col1) scores(c0, x);
+                        uint32_t h[FP8 ? 16 : 32];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float y0, y1;
+                            ta_unpair(ta_fma2(ta_pair(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), sc2, ref2), y0, y1);
+                            const uint64_t e = ta_pair(ta_exp2(y0), ta_exp2(y1));
+                            sum[j & 1] = ta_add2(sum[j & 1], e);
+                            if constexpr (FP8) {
+                                const uint64_t vs = *reinterpret_cast<const uint64_t*>(&vf[c0 + 2 * j]);
+                                ta_unpair(ta_mul2(e, vs), y0, y1);
+                                h[j] = ta_pack_f16(y0, y1);
+                            } else {
+                                ta_unpair(e, y0, y1);
+                                // the upper 16 bits of p, and what they leave, rounded (no conversion instructions: they run on the unit that has
+                                // the exponentials to do)
+                                const uint32_t u0 = __float_as_uint(y0), u1 = __float_as_uint(y1);
+                                h[j / 8 * 16 + j % 8] = __byte_perm(u0, u1, 0x7632);
+                                ta_unpair(ta_fma2(ta_pair(__uint_as_float(u0 & 0xffff0000u), __uint_as_float(u1 & 0xffff0000u)), minus, e), y0, y1);
+                                h[j / 8 * 16 + 8 + j % 8] = __byte_perm(__float_as_uint(y0) + 0x8000u, __float_as_uint(y1) + 0x8000u, 0x7632);
+                            }
+                        }
+                        if constexpr (FP8) {
+                            const uint32_t h0[8] = {h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]}, h1[8] = {h[8], h[9], h[10], h[11], h[12], h[13], h[14], h[15]};
+                            ta_tmem_st8(s_at + c0, h0);
+                            ta_tmem_st8(s_at + c0 + 16u, h1);
+                        } else {
+                            ta_tmem_st32(s_at + c0, h);
+                        }
+                        if (c0 == col0) break;
+                    }
+                    if (p.split > 1u) {   // the other copies' columns of this group are zero
                         uint32_t zero[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) zero[j] = 0u;
-                        for (uint32_t c0 = 0; c0 < (uint32_t)NK; c0 += 32u)
-                            if (c0 < col0 || c0 >= col0 + ncol) {
-                                // (P's high halves lie on the scores: this thread's own columns lie behind those it writes here, or are read by now)
-                                if (!FP8 && c0 < col0) ta_tmem_st16(s_at + c0 / 2u, zero);
-                                if (t < p.t0 + 2u) ta_tmem_st16(p_at + c0 / 2u, zero);
-                            }
-                    }
-                    uint64_t sum[2];
-                    if constexpr (FP8) {
-                        // scores are turned into probabilities with the reference so far, and once more if that was too low
-                        float g = 1.f;
-                        if (__any_sync(0xffffffffu, row.T > 0u && m == -INFINITY)) g = raise_to(largest());
-                        if (!(ok = rescale(g * raise, g))) break;
-                        for (int again = 0;; ++again) {
-                            const float ref = m == -INFINITY ? 0.f : m;
-                            const uint64_t ref2 = ta_pair(-ref, -ref);
-                            float mx[2] = {-INFINITY, -INFINITY};
-                            sum[0] = sum[1] = 0ull;
-                            for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
-                                uint32_t x[32], h[16];
-                                scores(c0, x);
-#pragma unroll
-                                for (int j = 0; j < 32; j += 4) {
-                                    const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][0][c0 + j]);
-                                    const ulonglong2 vs = *reinterpret_cast<const ulonglong2*>(&s.factor[warp][1][c0 + j]);
-#pragma unroll
-                                    for (int i = 0; i < 2; ++i) {
-                                        float y0, y1;
-                                        ta_unpair(ta_fma2(ta_pair(__uint_as_float(x[j + 2 * i]), __uint_as_float(x[j + 2 * i + 1])), i ? ks.y : ks.x, ref2), y0, y1);
-                                        mx[i] = pg_max3(mx[i], y0, y1);
-                                        const uint64_t e = ta_pair(ta_exp2(y0), ta_exp2(y1));
-                                        sum[i] = ta_add2(sum[i], e);
-                                        ta_unpair(ta_mul2(e, i ? vs.y : vs.x), y0, y1);
-                                        h[j / 2 + i] = ta_pack_f16(y0, y1);
-                                    }
-                                }
-                                ta_tmem_st16(p_at + c0 / 2u, h);
-                            }
-                            const float top = fmaxf(mx[0], mx[1]);
-                            // (once: scores beyond 2^26 may differ from any 32-bit reference by more; P then saturates)
-                            if (again || !__any_sync(0xffffffffu, row.T > 0u && m > -INFINITY && top > (float)Cfg::RAISE)) break;
-                            g = raise_to(m + top);
-                            if (!(ok = rescale(g, g))) break;
-                        }
-                        if (!ok) break;
-                    } else {
-                        const float g = raise_to(largest());
-                        if (!(ok = rescale(g, g))) break;
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        const uint64_t ref2 = ta_pair(-ref, -ref), sc2 = ta_pair(a.scale_log2, a.scale_log2), minus = ta_pair(-1.f, -1.f);
-                        sum[0] = sum[1] = 0ull;
-                        for (uint32_t c0 = col0; c0 < col0 + ncol; c0 += 32u) {
-                            uint32_t x[32], hi[16], lo[16];
-                            scores(c0, x);
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                float y0, y1;
-                                ta_unpair(ta_fma2(ta_pair(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), sc2, ref2), y0, y1);
-                                const uint64_t e = ta_pair(ta_exp2(y0), ta_exp2(y1));
-                                sum[j & 1] = ta_add2(sum[j & 1], e);
-                                ta_unpair(e, y0, y1);
-                                hi[j] = pack_bf16(y0, y1);
-                                ta_unpair(ta_fma2(ta_pair(bf_lo(hi[j]), bf_hi(hi[j])), minus, e), y0, y1);
-                                lo[j] = pack_bf16(y0, y1);
-                            }
-                            // P's high halves lie on scores that have been read
-                            ta_tmem_st16(s_at + c0 / 2u, hi);
-                            ta_tmem_st16(p_at + c0 / 2u, lo);
-                        }
-                        if (p.split > 1u) {   // the columns behind this thread's own
-                            uint32_t zero[16];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) zero[j] = 0u;
-                            for (uint32_t c0 = col0 + ncol; c0 < (uint32_t)NK; c0 += 32u) ta_tmem_st16(s_at + c0 / 2u, zero);
-                        }
+#pragma unroll 1
+                        for (uint32_t c0 = grp * (NK / NG); c0 < (grp + 1u) * (NK / NG); c0 += 16u)
+                            if (c0 < col0 || c0 >= col1) ta_tmem_st16(s_at + c0, zero);
                     }
                     float s0, s1;
                     ta_unpair(ta_add2(sum[0], sum[1]), s0, s1);
@@ -1158,48 +1229,60 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 }
                 tm_fence_before();
                 __syncwarp();
-                if (lane == 0u) mbar_arrive(smem_u32(&s.p_full[b]));
+                if (lane == 0u) mbar_arrive(smem_u32(p.two ? &s.r_probs[grp] : &s.h_probs[buf][grp]));
+                if (p.two) ++nr;
+                else ++nh;
             }
-            ok = ok && ta_wait(&s.pv_done[(nt - 1u) & 1u], ((nt - 1u) >> 1) & 1u, s, c.status) && ta_wait(&s.piece_end[npiece % TA_RING], (npiece / TA_RING) & 1u, s, c.status);
-            if (!(ok = ta_named_all(ok))) break;   // (no softmax warp waits for one that has given up)
+            if (ok) ok = p.two ? ta_wait(&s.r_done[grp], (nr - 1u) & 1u, s, c.status) : ta_wait(&s.h_done[(nh - 1u) & 1u][grp], ((nh - 1u) >> 1) & 1u, s, c.status);
+            ok = ok && ta_wait(&s.piece_end[npiece % TA_RING], (npiece / TA_RING) & 1u, s, c.status);
+            if (!(ok = ta_named_all(3u, NG * 128u, ok))) break;   // (no softmax warp waits for one that has given up)
             tm_fence_after();
             const bool bad = *(volatile uint32_t*)&s.bad[npiece % TA_RING] != 0u;
-            // the copies of a row: one reference, one sum
             const float unit = FP8 && ev_ref >= 0 ? ta_exp2((float)(ev_ref - 127) - TA_HEAD) : 1.f;   // of the values
+            // the parts of a row: one reference, one sum
+            const uint32_t me = grp * 128u + L, parts = p.two ? 1u : NG * p.split;
+            auto part = [&](uint32_t k) {   // thread that holds part k of row r (units of one run)
+                const uint32_t g = k / p.split, j = k % p.split;
+                return g * 128u + (R == 32u ? (2u * j + g) * 32u : j * R) + r;
+            };
             float mm = m, ll = l, f = 1.f;
-            s.ml[L] = make_float2(m, FP8 ? unit : 0.f);
-            ta_named_sync();
-            if (bad && L == 0u) s.bad[npiece % TA_RING] = 0u;
-            if (p.split > 1u) {
-                for (uint32_t k = 0; k < p.split; ++k) mm = fmaxf(mm, s.ml[r + k * R].x);
-                f = m == -INFINITY ? 0.f : ta_exp2(m - mm);
-                ta_named_sync();
-                s.ml[L] = make_float2(l * f, 0.f);
-                ta_named_sync();
+            s.ml[0][me] = m;
+            s.ml[1][me] = l;
+            ta_named_sync(3u, NG * 128u);
+            if (bad && me == 0u) s.bad[npiece % TA_RING] = 0u;
+            if (parts > 1u) {
+                for (uint32_t k = 0; k < parts; ++k) mm = fmaxf(mm, s.ml[0][part(k)]);
                 ll = 0.f;
-                for (uint32_t k = 0; k < p.split; ++k) ll += s.ml[r + k * R].x;
+                for (uint32_t k = 0; k < parts; ++k) {
+                    const float mk = s.ml[0][part(k)];
+                    if (mk > -INFINITY) ll += s.ml[1][part(k)] * ta_exp2(mk - mm);
+                }
+                f = m == -INFINITY ? 0.f : ta_exp2(m - mm);
             }
-            const bool whole = p.slot == ~0u;
-            const uint32_t gr = p.run * 128u + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
-            if (r < p.rows && L < R) {
+            const bool whole = p.slot == ~0u, valid = r < p.rows;
+            const uint32_t gr = p.row0 + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
+            if (valid && (p.two || me == part(0u))) {
                 if (whole) {
                     if (a.lse) a.lse[(size_t)(p.q.r0 + tok) * a.nq + head] = ll > 0.f || ll != ll ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
                 } else {
-                    a.part_ml[(size_t)p.slot * 128u + r] = make_float2(mm, ll);
+                    a.part_ml[(size_t)p.slot * TA_RECORD + r] = make_float2(mm, ll);
                 }
             }
             const float g = (whole ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f) * f * unit;
-            const uint32_t cols = 32u / p.split;   // of a chunk of 32: what this thread writes of row r
-            const uint32_t mine = L / R * cols;
-            for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 32u) {
-                uint32_t x[32];
-                tm_ld32(lane_base + Cfg::O_COL + c0, x);
+            __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD;
+            float* const rec = a.part + ((size_t)(whole ? 0u : p.slot) * TA_RECORD + r) * HD;
+            auto at16 = [](uint32_t thread, uint32_t j) { return thread * 16u + ((j / 4u ^ (thread >> 1 & 3u)) << 2); };   // (eight threads' four columns lie in all banks)
+            const uint32_t cols = 16u / parts, mine = p.two ? 0u : (grp * p.split + share) * cols;   // of a chunk of 16: what this thread writes of row r
+#pragma unroll 1
+            for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
+                uint32_t x[16];
+                tm_ld16(o_at + c0, x);
                 tm_ld_wait();
-                if (bad && r < p.rows) {   // values that are no numbers, for the rows that see them
+                if (bad && valid && !idle) {   // values that are no numbers, for the rows that see them
                     for (uint32_t t = p.t0; t < p.t1; ++t) {
                         const uint32_t pos = ta_tile_pos(p.q, t, NK);
                         if (!ta_mixed(a, p.q, pos, NK, INT32_MAX)) continue;
-                        for (uint32_t k0 = col0; k0 < col0 + ncol; k0 += 32u) {
+                        for (uint32_t k0 = col0; k0 < col1; k0 += 32u) {
                             uint32_t sees = row.sees(pos + k0);
                             while (sees) {
                                 const uint32_t at = pos + k0 + __ffs(sees) - 1u;
@@ -1207,30 +1290,45 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                 const int32_t phys = pg_physical(c, iter.s, at / c.page);
                                 if (phys < 0) continue;
                                 const uint8_t* v = c.v + (int64_t)phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)(at % c.page) * c.row_b;
-                                for (int j = 0; j < 32; ++j) {
-                                    if (FP8 ? (v[c0 + j] & 0x7f) == 0x7f : (reinterpret_cast<const uint16_t*>(v)[c0 + j] & 0x7f80) == 0x7f80)
-                                        x[j] = __float_as_uint(__uint_as_float(x[j]) + (FP8 ? NAN : __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(v)[c0 + j] << 16)));
+                                for (int j = 0; j < 16; ++j) {
+                                    const uint32_t w = FP8 ? v[c0 + j] : reinterpret_cast<const uint16_t*>(v)[c0 + j];
+                                    if (FP8 ? (w & 0x7fu) == 0x7fu : (w & 0x7f80u) == 0x7f80u)
+                                        x[j] = __float_as_uint(__uint_as_float(x[j]) + (FP8 ? NAN : __uint_as_float(w << 16)));
                                 }
                             }
                         }
                     }
                 }
-                ta_named_sync();   // the buffer's last readers are done
+                float o[16];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) s.x[L * 33u + j] = f == 0.f ? 0.f : __uint_as_float(x[j]) * g;
-                ta_named_sync();
-                if (r < p.rows) {
-                    for (uint32_t j = mine; j < mine + cols; j += 8u) {
-                        float o[8];
+                for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(x[j]) * g;
+                if (p.two) {
+                    if (valid) {
 #pragma unroll
-                        for (int y = 0; y < 8; ++y) {
-                            o[y] = 0.f;
-                            for (uint32_t k = 0; k < p.split; ++k) o[y] += s.x[(r + k * R) * 33u + j + y];
+                        for (int j = 0; j < 16; j += 8) {
+                            const float y[8] = {o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]};
+                            if (whole) pg_store8<__nv_bfloat16>(out + c0 + j, y);
+                            else pg_store8<float>(rec + c0 + j, y);
                         }
-                        if (whole)
-                            pg_store8<__nv_bfloat16>(reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD + c0 + j, o);
-                        else
-                            pg_store8<float>(a.part + ((size_t)p.slot * 128u + r) * HD + c0 + j, o);
+                    }
+                    continue;
+                }
+                ta_named_sync(3u, NG * 128u);   // the buffer's last readers are done
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&s.x[at16(me, j)]) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                ta_named_sync(3u, NG * 128u);
+                if (valid && !idle) {
+                    for (uint32_t j = mine; j < mine + cols; j += 4u) {
+                        float4 y = *reinterpret_cast<const float4*>(&s.x[at16(part(0u), j)]);
+                        for (uint32_t k = 1; k < parts; ++k) {
+                            const float4 z = *reinterpret_cast<const float4*>(&s.x[at16(part(k), j)]);
+                            y.x += z.x;
+                            y.y += z.y;
+                            y.z += z.z;
+                            y.w += z.w;
+                        }
+                        if (whole) *reinterpret_cast<uint2*>(out + c0 + j) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+                        else *reinterpret_cast<float4*>(rec + c0 + j) = y;
                     }
                 }
             }
@@ -1242,31 +1340,31 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
     }
     tm_fence_before();
     __syncthreads();
-    if (warp == 4u) tm_dealloc(tmem, 512);
+    if (warp == (uint32_t)Cfg::QK_WARP) tm_dealloc(tmem, 512);
 }
 
 // Joins the parts of the units that borders between blocks cut: block (b - 1, y) of the grid has border b, and does nothing unless it is the
 // first border inside its unit.  A warp takes a row: weights 2^(m - largest m), sums in the order of the parts.
 constexpr int TA_MERGE_THREADS = 128;
-template <int HD, int NK>
+template <int HD, int NK, int UR>
 __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(const PagedView c, const TreeArgs a, const uint32_t blocks) {
     constexpr int NW = TA_MERGE_THREADS / 32, COLS = HD / 32;
     __shared__ uint64_t pre[NW * 32], wsum[NW];
     griddep_launch();
     griddep_wait();
     if (pg_stopped(c)) return;
-    const uint64_t work = pg_prefix<NW>(c.n_seqs, pre, wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK>(c, a, i)); });
+    const uint64_t work = pg_prefix<NW>(c.n_seqs, pre, wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK, UR>(c, a, i)); });
     const uint32_t b = blockIdx.x + 1u, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint64_t g = ta_border(work, b, blocks);
     if (g == 0u || g >= work) return;
     const uint32_t share = pg_find<NW>(pre, g), per = (c.n_seqs + NW * 32u - 1u) / (NW * 32u);
     uint32_t s = share * per;
     uint64_t off = g - pre[share];
-    TaSeq q = ta_seq<NK>(c, a, s);
+    TaSeq q = ta_seq<NK, UR>(c, a, s);
     while (off >= ta_work(c, q)) {
         off -= ta_work(c, q);
         if (++s >= c.n_seqs) return;
-        q = ta_seq<NK>(c, a, s);
+        q = ta_seq<NK, UR>(c, a, s);
     }
     const uint64_t u = pg_div(off, q.tiles), begin = g - (off - u * q.tiles), end = begin + q.tiles;
     const uint32_t first = b - 1u, h = (uint32_t)pg_div(u, q.runs), run = (uint32_t)(u - (uint64_t)h * q.runs);
@@ -1274,13 +1372,13 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
     const uint32_t first_slot = 2u * first + (ta_border(work, first, blocks) < begin ? 1u : 0u);
     uint32_t last = b;
     while (last + 1u < blocks && ta_border(work, last + 1u, blocks) < end) ++last;
-    const uint32_t rows = (uint32_t)min((uint64_t)128u, (uint64_t)q.T * a.G - (uint64_t)run * 128u);
+    const uint32_t rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - (uint64_t)run * UR);
     for (uint32_t r = blockIdx.y * NW + warp; r < rows; r += gridDim.y * NW) {
         auto slot_of = [&](uint32_t k) { return k == first ? first_slot : 2u * k; };
         auto holds = [&](uint32_t k) { return ta_border(work, k, blocks) < ta_border(work, k + 1u, blocks); };   // blocks without work left nothing
         float m = -INFINITY;
         for (uint32_t k = first + lane; k <= last; k += 32u)
-            if (holds(k)) m = fmaxf(m, a.part_ml[(size_t)slot_of(k) * 128u + r].x);
+            if (holds(k)) m = fmaxf(m, a.part_ml[(size_t)slot_of(k) * TA_RECORD + r].x);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         float l = 0.f, sum[COLS];
@@ -1289,7 +1387,7 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
         for (uint32_t k0 = first; k0 <= last; k0 += 32u) {
             float w = 0.f, part = 0.f;
             if (k0 + lane <= last && holds(k0 + lane)) {
-                const float2 ml = a.part_ml[(size_t)slot_of(k0 + lane) * 128u + r];
+                const float2 ml = a.part_ml[(size_t)slot_of(k0 + lane) * TA_RECORD + r];
                 w = ml.x == -INFINITY ? 0.f : ta_exp2(ml.x - m);
                 part = ml.y;
             }
@@ -1298,7 +1396,7 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
                 const float wk = __shfl_sync(0xffffffffu, w, k), lk = __shfl_sync(0xffffffffu, part, k);
                 if (wk == 0.f) continue;   // (the same for the whole warp)
                 l += wk * lk;
-                const float* src = a.part + ((size_t)slot_of(k0 + k) * 128u + r) * HD + lane * COLS;
+                const float* src = a.part + ((size_t)slot_of(k0 + k) * TA_RECORD + r) * HD + lane * COLS;
                 float x[COLS];
                 if constexpr (COLS == 2) {
                     const float2 v = *reinterpret_cast<const float2*>(src);
@@ -1314,7 +1412,7 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
                 for (int j = 0; j < COLS; ++j) sum[j] += wk * x[j];
             }
         }
-        const uint32_t gr = run * 128u + r, tok = gr / a.G, head = h * a.G + gr - tok * a.G;
+        const uint32_t gr = run * UR + r, tok = gr / a.G, head = h * a.G + gr - tok * a.G;
         const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
         if (a.lse && lane == 0u) a.lse[(size_t)(q.r0 + tok) * a.nq + head] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         uint32_t* out = reinterpret_cast<uint32_t*>(a.out + (int64_t)(q.r0 + tok) * a.out_stride + ((size_t)head * HD + lane * COLS) * 2u);

@@ -191,8 +191,9 @@ def test_append_rotated_reports_bad_pages():
 # Tolerances, derived: the tensor cores add 16 products at a time to a 32-bit sum and cut off what does not fit, which costs at most
 # 2^-22 of the sum of magnitudes per step: (hd / 16 + 2) steps of a score, N / 16 + 2 of a result over N positions.  A score's error
 # (relative to `reach`, the largest scale * sum |q k|) is a relative error of a probability; the exponential adds 2^-21 and the rounding of
-# its argument reach * 2^-23.  A probability enters the second product with 2^-16 (bf16 caches: two halves of 8 bits) or 2^-11 (e4m3: half a
-# step of f16, twice where its largest scale moved) left out.  Errors of probabilities count twice, in the numerator and in the denominator.
+# its argument reach * 2^-23.  A probability enters the second product with 2^-15 (bf16 caches: its upper 8 bits cut off, which leaves
+# less than 2^-7 of it, and that rounded to 8 bits, half a step of which is 2^-8) or 2^-11 (e4m3: half a step of f16, twice where its largest
+# scale moved) left out.  Errors of probabilities count twice, in the numerator and in the denominator.
 # The sum of probabilities: N * 2^-24 at most.  The result is rounded to bf16, half a step of which is 2^-8 of it.
 
 def tree_ref(c, q, seqs, starts, table, at, mask, window, sinks, scale):
@@ -267,7 +268,7 @@ def check_tree(c, q, seqs, table, form="causal", window=0, sinks=0, scale=0.0, s
     want, want_lse, mass, reach = tree_ref(c, q.cpu(), seqs, starts, table, at, mask, window, sinks, sc)
     N = max(b + t for b, t in seqs)
     score = reach * ((hd / 16 + 2) * 2.0 ** -22 + 2.0 ** -23) + 2.0 ** -21
-    err = (2 * (score + 2.0 ** (-11 if c.e4m3 else -16))[..., None] + (N / 16 + 2) * 2.0 ** -22 + N * 2.0 ** -24) * mass + 2.0 ** -8 * want.abs() + 1e-30
+    err = (2 * (score + 2.0 ** (-11 if c.e4m3 else -15))[..., None] + (N / 16 + 2) * 2.0 ** -22 + N * 2.0 ** -24) * mass + 2.0 ** -8 * want.abs() + 1e-30
     live = torch.zeros(n, dtype=torch.bool)
     for s, (base, T) in enumerate(seqs):
         live[starts[s]:starts[s] + T] = base >= 0
@@ -477,8 +478,8 @@ def test_single_tokens_agree_with_paged_attention():
             ws = torch.empty(max(kl.kl_paged_workspace_bytes(c.handle, 16, 5, table.shape[1]), kl.kl_paged_tree_workspace_bytes(c.handle, 16)), dtype=torch.uint8, device="cuda")
             kl.kl_paged_attention(c.handle, q, a, i32(pos), table.cuda(), ws, window=window)
             kl.kl_paged_tree_attention(c.handle, q, b, i32(pos), table.cuda(), ws, window=window)
-            # two roundings to bf16, and the e4m3 form's 2^-11 (twice) of sum p |v|, at most the largest |v|
-            tol = 2.0 ** -7 * a.abs() + (2.0 ** -10 * 448 * 2.0 ** -5 if e4m3 else 2.0 ** -15 * 5)
+            # two roundings to bf16, and the e4m3 form's 2^-11 (twice; bf16 2^-15) of sum p |v|, at most the largest |v|
+            tol = 2.0 ** -7 * a.abs() + (2.0 ** -10 * 448 * 2.0 ** -5 if e4m3 else 2.0 ** -14 * 5)
             assert bool(((a.float() - b.float()).abs() <= tol.float()).all())
             assert not b[3].any()
 
@@ -524,7 +525,7 @@ def test_captured_on_a_stream_and_replayed_while_the_sequences_grow():
             assert bool(((qo.cpu().double() - want_q).abs() <= 2.0 ** -8 * want_q.abs() + 2.0 ** -20)[live].all())
             want, _, mass, reach = tree_ref(c, qo.cpu(), seqs, starts_of(seqs), table.cpu(), None, None, 0, 0, 1 / math.sqrt(hd))
             score = reach * ((hd / 16 + 2) * 2.0 ** -22 + 2.0 ** -23) + 2.0 ** -21
-            err = (2 * (score + 2.0 ** -16)[..., None] + 15 * 2.0 ** -22 + 200 * 2.0 ** -24) * mass + 2.0 ** -8 * want.abs() + 1e-30
+            err = (2 * (score + 2.0 ** -15)[..., None] + 15 * 2.0 ** -22 + 200 * 2.0 ** -24) * mass + 2.0 ** -8 * want.abs() + 1e-30
             assert bool(((out.cpu().double() - want).abs() <= err)[live].all())
             for r in range(n):
                 w = torch.softmax(logits[r].cpu().double(), 0)
