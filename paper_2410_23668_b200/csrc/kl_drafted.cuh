@@ -331,11 +331,12 @@ constexpr size_t rt_smem_bytes() {
 // bf16 (exact), its scales applied to the scores in 32 bits; V's codes as f16 (exact), its scales applied to P, which enters as one f16
 // (11 bits) scaled by a power of two common to all columns so far (the largest value scale seen).
 //
-// Two groups of four softmax warps.  Where a unit has at most 128 rows, each group takes one half of every tile's keys, with a
-// reference, a sum and an O of its own, joined at the end of the unit (with at most 64 rows each row lies in TMEM's lanes twice, and a copy
-// takes a quarter); where it has up to 256, each group takes 128 rows, and the tensor cores work for one while the other has its
-// softmax.  Either way no two warps have to agree on anything within a tile, and a tile's keys and values serve up to 256 rows.  (Head
-// size 256: O alone fills half of TMEM, one group of warps, 128 rows.)
+// Two streams.  There are two score buffers and two groups of four softmax warps, each with a reference, a sum and an O of its own.  Where a
+// unit has at most 128 rows, the groups take its tiles in turn and are joined at its end; where it has up to 256, each group
+// takes 128 rows of every tile.  Either way the tensor cores work for one group while the other has its softmax, no two groups have
+// to agree on anything, and a tile's keys and values serve up to 256 rows.  With at most 64 (32) rows each row lies in TMEM's lanes
+// twice (four times), and a copy takes one half (quarter) of the tile's keys -- P is zero elsewhere -- so that all warps share a
+// single row's exponentials.  (Head size 256: O fills half of TMEM, one group of warps takes the buffers in turn, 128 rows.)
 
 struct TreeArgs {
     const int32_t* row_starts;      // [n_seqs + 1] or null: one row per sequence
@@ -383,9 +384,7 @@ struct TaShared {
     float ml[2][256];
     uint64_t kv_full[8], kv_empty[8], exp_full[TA_RING], piece_end[TA_RING];
     uint64_t q_full, q_empty, qs_full[4], o_empty, end;
-    // Waits go by parity and must never be two phases behind, so barriers are told apart by tile ([2]: tiles in turn), group and kind of unit.
-    uint64_t h_scores[2], h_probs[2][2], h_done[2][2];   // units of one run of rows: [tile][group]
-    uint64_t r_scores[2], r_probs[2], r_done[2];         // units of two runs: [group]; r_done: of a tile
+    uint64_t scores[2], probs[2], done[2];   // per stream: Q K^T has landed, P is written, P V has landed
     uint32_t bad[TA_RING];                   // pieces whose partly visible tiles hold values that are no numbers
     uint32_t tmem;
     int abort;
@@ -396,27 +395,29 @@ constexpr size_t ta_smem() {
 }
 
 // A bounded wait of a whole warp; every lane gets the same answer.
-__device__ __forceinline__ bool ta_wait(uint64_t* bar, uint32_t parity, TaShared& s, int32_t* status) {
-    const uint32_t b = smem_u32(bar);
-    bool done = mbar_try_wait(b, parity);
-    if (!__all_sync(0xffffffffu, done)) {
-        const uint64_t t0 = globaltimer_ns();
-        for (uint32_t it = 1; !done; ++it) {
-            done = mbar_try_wait(b, parity);
-            if (!done && (it & 63u) == 0u) {
-                if (*(volatile int*)&s.abort) break;
-                if (globaltimer_ns() - t0 > TA_WAIT_NS) {
-                    if (status) atomicCAS(status, 0, ERR_SYNC_TIMEOUT);
-                    *(volatile int*)&s.abort = 1;
-                    break;
-                }
+__device__ __noinline__ bool ta_wait_on(uint32_t bar, uint32_t parity, int* abort, int32_t* status) {
+    const uint64_t t0 = globaltimer_ns();
+    bool done = false;
+    for (uint32_t it = 1; !done; ++it) {
+        done = mbar_try_wait(bar, parity);
+        if (!done && (it & 63u) == 0u) {
+            if (*(volatile int*)abort) break;
+            if (globaltimer_ns() - t0 > TA_WAIT_NS) {
+                if (status) atomicCAS(status, 0, ERR_SYNC_TIMEOUT);
+                *(volatile int*)abort = 1;
+                break;
             }
         }
     }
     return __all_sync(0xffffffffu, done);
 }
+__device__ __forceinline__ bool ta_wait(uint64_t* bar, uint32_t parity, TaShared& s, int32_t* status) {
+    const uint32_t b = smem_u32(bar);
+    if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
+    return ta_wait_on(b, parity, &s.abort, status);
+}
 __device__ __forceinline__ void tm_commit_to(uint64_t* bar) { tm_commit(smem_u32(bar)); }
-// Barriers of the softmax warps: group g alone (1 + g), all of them (3).
+// A barrier of the softmax warps, by its number.
 __device__ __forceinline__ void ta_named_sync(uint32_t id, uint32_t threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ bool ta_named_all(uint32_t id, uint32_t threads, bool x) {   // ... and whether x holds for all of them
     uint32_t r;
@@ -563,7 +564,7 @@ struct TaPiece {
     uint32_t h, row0, t0, t1;   // kv head, first row of the unit among the (token, head) pairs, tiles
     uint32_t rows, slot;        // rows of the unit, part in the workspace (~0: the whole unit is here)
     bool two;                   // two runs of rows
-    uint32_t split, R;          // parts of a group's columns, rows that lie next to one another in TMEM's lanes
+    uint32_t split, R;          // copies of a row in TMEM's lanes, rows between them
 };
 template <int NK, int NW, int UR>
 struct TaIter {
@@ -597,8 +598,8 @@ struct TaIter {
         p.t1 = (uint32_t)min((uint64_t)q.tiles, p.t0 + left);
         p.rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - p.row0);
         p.two = p.rows > 128u;
-        p.split = p.rows <= 64u ? 2u : 1u;
-        p.R = p.rows <= 32u && UR == 256 ? 32u : 128u / p.split;
+        p.split = p.rows <= 32u && NK == 128 ? 4u : p.rows <= 64u ? 2u : 1u;   // a copy takes 32 keys or more
+        p.R = 128u / p.split;
         p.slot = p.t0 == 0u && p.t1 == q.tiles ? ~0u : 2u * blockIdx.x + (begun ? 1u : 0u);
         begun = true;
         off += p.t1 - p.t0;
@@ -629,45 +630,44 @@ __device__ __forceinline__ int64_t ta_far(const TreeArgs& a, const TaSeq& q) {
 struct TaRow {
     uint32_t base, T, i;            // cached positions, new tokens, the row's own number (T == 0: not a row)
     int32_t after;                  // cached positions up to this one are behind the window (-1: none)
-    uint32_t sinks, window;
     const uint32_t* mask;
-    uint32_t mask_words;
-    // bits of positions p .. p + 31
-    __device__ __noinline__ uint32_t sees(uint32_t p) const {
-        if (!T) return 0u;
-        uint32_t bits = 0xffffffffu;
-        if (p + 32u > base) bits = p >= base ? 0u : 0xffffffffu >> (p + 32u - base);
-        if ((int32_t)p <= after) {
-            uint32_t old = (int32_t)p + 31 <= after ? 0u : 0xffffffffu << (uint32_t)(after + 1 - (int32_t)p);
-            if (p < sinks) old |= p + 32u <= sinks ? 0xffffffffu : 0xffffffffu >> (p + 32u - sinks);
-            bits &= old;
-        }
-        if (p + 32u > base && p < base + T) {   // new tokens j = j0 .. j0 + 31
-            const int64_t j0 = (int64_t)p - base;
-            uint32_t b;
-            if (mask) {
-                const int64_t w = j0 >> 5;      // floor
-                const uint32_t lo = w >= 0 && w < mask_words ? mask[w] : 0u, hi = w + 1 >= 0 && w + 1 < mask_words ? mask[w + 1] : 0u;
-                b = __funnelshift_r(lo, hi, (uint32_t)j0 & 31u);
-            } else {
-                const int64_t d = (int64_t)i - j0;   // j <= i
-                b = d < 0 ? 0u : d >= 31 ? 0xffffffffu : 0xffffffffu >> (31u - (uint32_t)d);
-                const int64_t e = d - (int64_t)window;   // j > i - window
-                if (window && e >= 0) b &= e >= 31 ? 0u : 0xffffffffu << (uint32_t)(e + 1);
-            }
-            const int64_t end = (int64_t)T - j0;   // j < T
-            if (end < 32) b &= 0xffffffffu >> (uint32_t)(32 - end);
-            bits |= b & (j0 >= 0 ? 0xffffffffu : 0xffffffffu << (uint32_t)(-j0));
-        }
-        return bits;
-    }
 };
+// What a row sees of positions p .. p + 31, as bits.
+__device__ __noinline__ uint32_t ta_sees(uint32_t p, uint32_t base, uint32_t T, uint32_t i, int32_t after, uint32_t sinks, uint32_t window, const uint32_t* mask,
+                                         uint32_t mask_words) {
+    if (!T) return 0u;
+    uint32_t bits = 0xffffffffu;
+    if (p + 32u > base) bits = p >= base ? 0u : 0xffffffffu >> (p + 32u - base);
+    if ((int32_t)p <= after) {
+        uint32_t old = (int32_t)p + 31 <= after ? 0u : 0xffffffffu << (uint32_t)(after + 1 - (int32_t)p);
+        if (p < sinks) old |= p + 32u <= sinks ? 0xffffffffu : 0xffffffffu >> (p + 32u - sinks);
+        bits &= old;
+    }
+    if (p + 32u > base && p < base + T) {   // new tokens j = j0 .. j0 + 31
+        const int64_t j0 = (int64_t)p - base;
+        uint32_t b;
+        if (mask) {
+            const int64_t w = j0 >> 5;      // floor
+            const uint32_t lo = w >= 0 && w < mask_words ? mask[w] : 0u, hi = w + 1 >= 0 && w + 1 < mask_words ? mask[w + 1] : 0u;
+            b = __funnelshift_r(lo, hi, (uint32_t)j0 & 31u);
+        } else {
+            const int64_t d = (int64_t)i - j0;   // j <= i
+            b = d < 0 ? 0u : d >= 31 ? 0xffffffffu : 0xffffffffu >> (31u - (uint32_t)d);
+            const int64_t e = d - (int64_t)window;   // j > i - window
+            if (window && e >= 0) b &= e >= 31 ? 0u : 0xffffffffu << (uint32_t)(e + 1);
+        }
+        const int64_t end = (int64_t)T - j0;   // j < T
+        if (end < 32) b &= 0xffffffffu >> (uint32_t)(32 - end);
+        bits |= b & (j0 >= 0 ? 0xffffffffu : 0xffffffffu << (uint32_t)(-j0));
+    }
+    return bits;
+}
+__device__ __forceinline__ uint32_t ta_sees(const TreeArgs& a, const TaRow& w, uint32_t p) {
+    return ta_sees(p, w.base, w.T, w.i, w.after, a.sinks, a.window, w.mask, a.mask_words);
+}
 __device__ __forceinline__ TaRow ta_row(const TreeArgs& a, const TaPiece& p, uint32_t r) {
     TaRow w = {};
     w.base = p.q.base;
-    w.sinks = a.sinks;
-    w.window = a.window;
-    w.mask_words = a.mask_words;
     w.after = -1;
     if (r < p.rows) {
         w.T = p.q.T;
@@ -725,14 +725,9 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         mbar_init(smem_u32(&s.o_empty), 4 * NG);
         for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&s.qs_full[i]), PW);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&s.h_scores[i]), 1);
-            mbar_init(smem_u32(&s.r_scores[i]), 1);
-            mbar_init(smem_u32(&s.r_probs[i]), 4);
-            mbar_init(smem_u32(&s.r_done[i]), 1);
-            for (int g = 0; g < 2; ++g) {
-                mbar_init(smem_u32(&s.h_probs[i][g]), 4);
-                mbar_init(smem_u32(&s.h_done[i][g]), 1);
-            }
+            mbar_init(smem_u32(&s.scores[i]), 1);
+            mbar_init(smem_u32(&s.probs[i]), 4);
+            mbar_init(smem_u32(&s.done[i]), 1);
         }
         s.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -955,101 +950,69 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         // A lone warp takes some five cycles per instruction, and 64 a matrix instruction: hence two warps, descriptors made once per
         // tile, and no loops around the instructions.
         constexpr uint32_t type = FP8 ? 0u : 1u, qk_idesc = ta_idesc(type, NK, false), pv_idesc = ta_idesc(type, HD, true);
-        uint32_t tile = 0, nh = 0, nr = 0, npiece = 0;   // tiles so far: all, of units of one run, of units of two
-        bool ok = true, two = false;
+        uint32_t tile = 0, npiece = 0, n0 = 0, n1 = 0;   // tiles, units and every stream's tiles so far
+        bool ok = true;
         auto landed = [&](uint32_t n) {   // slot of the ring that is the n-th to be filled
             if (!ta_wait(&s.kv_full[n % NS], n / NS & 1u, s, c.status)) return false;
             if (!FP8) ta_fence_async();   // the copies behind the barrier were the threads' own, not the copy engine's
-            tm_fence_after();
             return true;
         };
         if (warp == (uint32_t)Cfg::QK_WARP) {
-            auto qk = [&](uint32_t d, uint32_t half, uint32_t sl) {   // scores of queries `half` and the keys in slot sl into score buffer d
-                const uint64_t qd = ta_desc(q_s + half * Cfg::QBYTES, 16u), kd = ta_desc(ring_s + sl * Cfg::SLOT, 16u);
-                const uint32_t to = tmem + d * NK;
-#pragma unroll
-                for (uint32_t k = 0; k < HD / 16; ++k)   // 32 bytes along the swizzled rows, then the next 64 columns
-                    ta_mma_ss(to, qd + (k / 4u * (128u * 128u / 16u) + k % 4u * 2u), kd + (k / 4u * (NK * 128u / 16u) + k % 4u * 2u), qk_idesc, k > 0u);
-            };
             while (ok && iter.next(c, a, p)) {
-                // the other kind of unit used the score buffers last: both have been read
-                if (npiece > 0u && p.two != two) {
-                    if (two) {
-                        for (uint32_t g = 0; ok && g < 2u; ++g) ok = ta_wait(&s.r_done[g], (nr - 1u) & 1u, s, c.status);
-                    } else {
-                        for (uint32_t back = nh > 1u ? 2u : 1u; back > 0u; --back)
-                            for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) ok = ta_wait(&s.h_done[(nh - back) & 1u][g], (nh - back) >> 1 & 1u, s, c.status);
-                    }
-                }
-                two = p.two;
-                ok = ok && ta_wait(&s.q_full, npiece & 1u, s, c.status);
+                ok = ta_wait(&s.q_full, npiece & 1u, s, c.status);
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++tile) {
                     if (!(ok = landed(2u * tile))) break;
-                    const uint32_t sl = 2u * tile % NS;
-                    if (!two) {
-                        if (nh >= 2u)   // P of the last tile but one, which lies on this score buffer, has been read
-                            for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) ok = ta_wait(&s.h_done[nh & 1u][g], (nh - 2u) >> 1 & 1u, s, c.status);
-                        if (!ok) break;
+                    const uint32_t sl = 2u * tile % NS, b0 = p.two ? 0u : t - p.t0 & 1u, b1 = p.two ? 1u : b0;
+                    const uint64_t kd = ta_desc(ring_s + sl * Cfg::SLOT, 16u);
+#pragma unroll 1
+                    for (uint32_t b = b0; b <= b1; ++b) {
+                        uint32_t& n = b ? n1 : n0;
+                        if (n > 0u && !(ok = ta_wait(&s.done[b], n - 1u & 1u, s, c.status))) break;   // P on this score buffer has been read
+                        ++n;
                         tm_fence_after();
                         if (lane == 0u) {
-                            qk(nh & 1u, 0u, sl);
-                            tm_commit_to(&s.h_scores[nh & 1u]);
-                            tm_commit_to(&s.kv_empty[sl]);
-                            if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
-                        }
-                        ++nh;
-                    } else {
-#pragma unroll 1
-                        for (uint32_t g = 0; ok && g < 2u; ++g) {
-                            if (nr > 0u && !(ok = ta_wait(&s.r_done[g], (nr - 1u) & 1u, s, c.status))) break;
-                            tm_fence_after();
-                            if (lane == 0u) {
-                                qk(g, g, sl);
-                                tm_commit_to(&s.r_scores[g]);
-                                if (g == 1u) {
-                                    tm_commit_to(&s.kv_empty[sl]);
-                                    if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
-                                }
+                            const uint64_t qd = ta_desc(q_s + (p.two ? b : 0u) * Cfg::QBYTES, 16u);
+                            const uint32_t to = tmem + b * NK;
+#pragma unroll
+                            for (uint32_t k = 0; k < HD / 16; ++k)   // 32 bytes along the swizzled rows, then the next 64 columns
+                                ta_mma_ss(to, qd + (k / 4u * (128u * 128u / 16u) + k % 4u * 2u), kd + (k / 4u * (NK * 128u / 16u) + k % 4u * 2u), qk_idesc, k > 0u);
+                            tm_commit_to(&s.scores[b]);
+                            if (b == b1) {
+                                tm_commit_to(&s.kv_empty[sl]);
+                                if (t + 1u == p.t1) tm_commit_to(&s.q_empty);
                             }
-                            __syncwarp();
                         }
-                        ++nr;
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
                 ++npiece;
             }
         } else {
-            // O += P V over 16 * n keys, from the first of which P lies at pa and V at vd
-            auto pv = [&](uint32_t o, uint32_t pa, uint64_t vd, auto n, uint32_t acc) {
-                const uint32_t d = tmem + Cfg::O_COL + o * HD;
-#pragma unroll
-                for (uint32_t k = 0; k < decltype(n)::value; ++k) {
-                    ta_mma_ts(d, pa + k * 16u, vd + k * (2048u / 16u), pv_idesc, k > 0u ? 1u : acc);
-                    if (!FP8) ta_mma_ts(d, pa + k * 16u + 8u, vd + k * (2048u / 16u), pv_idesc, 1u);
-                }
-            };
             while (ok && iter.next(c, a, p)) {
                 if (npiece > 0u) ok = ta_wait(&s.o_empty, (npiece - 1u) & 1u, s, c.status);   // the last unit's result has been read
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++tile) {
-                    const uint32_t n = 2u * tile + 1u, sl = n % NS;
+                    const uint32_t sl = (2u * tile + 1u) % NS, b0 = p.two ? 0u : t - p.t0 & 1u, b1 = p.two ? 1u : b0;
                     const uint64_t vd = ta_desc(ring_s + sl * Cfg::SLOT, NK * 128u);
-                    if (!(ok = landed(n))) break;
-                    const uint32_t b = nh & 1u;
+                    const uint32_t acc = t > p.t0 + (p.two || NG == 1 ? 0u : 1u);
+                    if (!(ok = landed(2u * tile + 1u))) break;
 #pragma unroll 1
-                    for (uint32_t g = 0; ok && g < (uint32_t)NG; ++g) {
-                        if (!(ok = p.two ? ta_wait(&s.r_probs[g], nr & 1u, s, c.status) : ta_wait(&s.h_probs[b][g], nh >> 1 & 1u, s, c.status))) break;
+                    for (uint32_t b = b0; b <= b1; ++b) {
+                        uint32_t& n = b ? n1 : n0;
+                        if (!(ok = ta_wait(&s.probs[b], n & 1u, s, c.status))) break;
+                        ++n;
                         tm_fence_after();
                         if (lane == 0u) {
-                            if (p.two) pv(g, tmem + g * NK, vd, std::integral_constant<uint32_t, NK / 16>{}, t > p.t0);
-                            else pv(g, tmem + b * NK + g * (NK / NG), vd + g * (NK / NG * 128u / 16u), std::integral_constant<uint32_t, NK / 16 / NG>{}, t > p.t0);
-                            if (g + 1u == (uint32_t)NG) tm_commit_to(&s.kv_empty[sl]);
-                            tm_commit_to(p.two ? &s.r_done[g] : &s.h_done[b][g]);
+                            const uint32_t d = tmem + Cfg::O_COL + (NG == 2 ? b * HD : 0u), pa = tmem + b * NK;
+#pragma unroll
+                            for (uint32_t k = 0; k < NK / 16; ++k) {
+                                ta_mma_ts(d, pa + k * 16u, vd + k * (2048u / 16u), pv_idesc, k > 0u ? 1u : acc);
+                                if (!FP8) ta_mma_ts(d, pa + k * 16u + 8u, vd + k * (2048u / 16u), pv_idesc, 1u);
+                            }
+                            if (b == b1) tm_commit_to(&s.kv_empty[sl]);
+                            tm_commit_to(&s.done[b]);
                         }
                         __syncwarp();
                     }
-                    if (p.two) ++nr;
-                    else ++nh;
                 }
                 ++npiece;
             }
@@ -1062,16 +1025,12 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         const uint32_t grp = warp >> 2, L = tid & 127u, lane_base = tmem + ((warp & 3u) * 32u << 16), o_at = lane_base + Cfg::O_COL + grp * HD;
         float(&kf)[128] = s.factor[warp][0];
         float(&vf)[128] = s.factor[warp][1];
-        uint32_t nt = 0, nh = 0, nr = 0, npiece = 0;
+        uint32_t tile = 0, npiece = 0, n0 = 0, n1 = 0;   // tiles of the block, units and every stream's tiles so far
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
-            // units of one run: the group's columns in `split` parts, each in another quarter (half) of the lanes; where every quarter holds
-            // all rows (R = 32), the groups take every other one, so that all four schedulers have one warp of each at work
-            const uint32_t R = p.R, r = p.two ? grp * 128u + L : L % R, quarter = L >> 5;
-            const uint32_t ncol = p.two ? (uint32_t)NK : (uint32_t)NK / NG / p.split, share = R == 32u ? quarter >> 1 : L / R;
-            const uint32_t col0 = p.two ? 0u : grp * (NK / NG) + share * ncol, col1 = col0 + ncol;
-            const bool idle = !p.two && R == 32u && (quarter & 1u) != grp;
-            const TaRow row = ta_row(a, p, idle ? ~0u : r);
+            const uint32_t R = p.R, r = p.two ? grp * 128u + L : L % R, share = L / R;
+            const uint32_t ncol = p.two ? (uint32_t)NK : (uint32_t)NK / p.split, col0 = p.two ? 0u : share * ncol, col1 = col0 + ncol;
+            const TaRow row = ta_row(a, p, r);
             const bool active = __any_sync(0xffffffffu, row.T > 0u);
             float m = -INFINITY, l = 0.f, qs = 1.f;
             int ev_ref = -1;   // e4m3: the largest value scale byte so far
@@ -1079,10 +1038,15 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 ok = ta_wait(&s.qs_full[npiece & 3u], npiece >> 2 & 1u, s, c.status);
                 qs = s.qscale[npiece & 3u][p.two ? grp : 0u][L];
             }
-            for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++nt) {
-                const uint32_t buf = p.two ? grp : nh & 1u, pos = ta_tile_pos(p.q, t, NK), s_at = lane_base + buf * NK;
+            const float unit_s = FP8 ? qs : a.scale_log2;
+            const uint64_t sc2 = ta_pair(unit_s, unit_s), minus = ta_pair(-1.f, -1.f);
+            const uint32_t step = p.two || NG == 1 ? 1u : 2u, first = p.two || NG == 1 ? p.t0 : p.t0 + grp;   // this group's tiles
+            for (uint32_t t = first; ok && t < p.t1; t += step) {
+                const uint32_t b = NG == 2 ? grp : t - p.t0 & 1u, pos = ta_tile_pos(p.q, t, NK), s_at = lane_base + b * NK, nt = tile + (t - p.t0);
+                uint32_t& n = b ? n1 : n0;
                 if (FP8 && !(ok = ta_wait(&s.exp_full[nt % TA_RING], (nt / TA_RING) & 1u, s, c.status))) break;
-                if (!(ok = p.two ? ta_wait(&s.r_scores[grp], nr & 1u, s, c.status) : ta_wait(&s.h_scores[buf], (nh >> 1) & 1u, s, c.status))) break;
+                if (!(ok = ta_wait(&s.scores[b], n & 1u, s, c.status))) break;
+                ++n;
                 tm_fence_after();
                 if (active) {
                     float raise = 1.f;   // of O: by a new reference of the values' scales
@@ -1110,14 +1074,34 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         }
                         __syncwarp();
                     }
+                    auto ta_scale_o = [&](float f) {   // O times f; the last product must have landed (two groups: these scores came behind it)
+                        if (NG == 1 && !ta_wait(&s.done[b ^ 1u], (b ? n0 : n1) - 1u & 1u, s, c.status)) return false;
+                        tm_fence_after();
+#pragma unroll 1
+                        for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
+                            uint32_t x[16];
+                            tm_ld16(o_at + c0, x);
+                            tm_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
+                            ta_tmem_st16(o_at + c0, x);
+                        }
+                        return true;
+                    };
                     // whether every row of the warp sees all of the tile
                     const bool full = __all_sync(0xffffffffu, row.T == 0u || (pos + NK <= row.base && (int32_t)pos > row.after));
-                    // 32 scores; what the row does not see is -infinity.  e4m3: times the keys' scales
-                    auto scores = [&](uint32_t c0, uint32_t (&x)[32]) {
+                    // 32 columns at a time: scores to probabilities, on which P is written: of 16 columns the first eight hold the high halves
+                    // (f16: all), the others the low ones
+                    uint64_t sum[2] = {0ull, 0ull};
+                    uint64_t ref2 = ta_pair(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m);
+                    if (FP8 && raise != 1.f && t > first) ok = ta_scale_o(raise);
+#pragma unroll 1
+                    for (uint32_t c0 = col0; ok && c0 < col1; c0 += 32u) {
+                        uint32_t x[32];
                         tm_ld32(s_at + c0, x);
                         tm_ld_wait();
-                        if (!full) {
-                            const uint32_t sees = row.sees(pos + c0);
+                        if (!full) {   // what the row does not see is -infinity
+                            const uint32_t sees = ta_sees(a, row, pos + c0);
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
                                 if (!(sees >> j & 1u)) x[j] = 0xff800000u;
@@ -1135,55 +1119,49 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                 }
                             }
                         }
-                    };
-                    // the largest of the own columns' scores, in binades; the last 32 stay in x
-                    uint32_t x[32];
-                    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll 1
-                    for (uint32_t c0 = col0; c0 < col1; c0 += 32u) {
-                        scores(c0, x);
+                        float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
                             top[0] = pg_max3(top[0], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
                             top[1] = pg_max3(top[1], __uint_as_float(x[j + 2]), __uint_as_float(x[j + 3]));
                         }
-                    }
-                    const float unit_s = FP8 ? qs : a.scale_log2;
-                    // l and O in new references: O times f (which also holds the values' new scale), l times g
-                    auto rescale = [&](float f, float g) {
-                        l *= g;
-                        if (t == p.t0 || !__any_sync(0xffffffffu, f != 1.f)) return true;
-                        // (units of two runs: the scores came behind the last product)
-                        if (!p.two && !ta_wait(&s.h_done[(nh - 1u) & 1u][grp], ((nh - 1u) >> 1) & 1u, s, c.status)) return false;
-                        tm_fence_after();
-#pragma unroll 1
-                        for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
-                            uint32_t x[16];
-                            tm_ld16(o_at + c0, x);
-                            tm_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(x[j]) * f);
-                            ta_tmem_st16(o_at + c0, x);
-                        }
-                        return true;
-                    };
-                    auto raise_to = [&](float mx) {   // the factor of l when the reference rises to mx, if it has to
+                        const float mx = fmaxf(top[0], top[1]) * unit_s;
                         // (scores of 2^22 and more: a step of the reference is as large as the slack, and no score may lie above it)
-                        if (!(mx > m + (fabsf(m) < 4194304.f ? (float)Cfg::RAISE : 0.f))) return 1.f;
-                        if (fabsf(mx) >= 4194304.f) mx = fmaf(fabsf(mx), 1.2e-7f, mx);
-                        const float g = m == -INFINITY ? 0.f : ta_exp2(m - mx);
-                        m = mx;
-                        return g;
-                    };
-                    const float g = raise_to(fmaxf(top[0], top[1]) * unit_s);
-                    if (!(ok = rescale(g * raise, g))) break;
-                    // P on the scores that have been read: of 16 columns the first eight hold the high halves (f16: all), the others the low ones
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    const uint64_t ref2 = ta_pair(-ref, -ref), sc2 = ta_pair(unit_s, unit_s), minus = ta_pair(-1.f, -1.f);
-                    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll 1
-                    for (uint32_t c0 = col1 - 32u;; c0 -= 32u) {
-                        if (c0 + 32u != col1) scores(c0, x);
+                        const bool rise = mx > m + (fabsf(m) < 4194304.f ? (float)Cfg::RAISE : 0.f);
+                        if (__any_sync(0xffffffffu, rise)) {   // seldom but for the first tile
+                            float g = 1.f;
+                            if (rise) {
+                                if (m == -INFINITY || fabsf(mx) >= 4194304.f) {
+                                    g = 0.f;
+                                    if (m > -INFINITY) g = ta_exp2(m - mx);
+                                    m = fabsf(mx) >= 4194304.f ? fmaf(fabsf(mx), 1.2e-7f, mx) : mx;
+                                } else {   // by whole binades: what is written of P stays exact
+                                    const float k = ceilf(mx - m);
+                                    m += k;
+                                    g = ta_exp2(-k);
+                                }
+                            }
+                            ref2 = ta_pair(m == -INFINITY ? 0.f : -m, m == -INFINITY ? 0.f : -m);
+                            l *= g;
+                            sum[0] = ta_mul2(sum[0], ta_pair(g, g));
+                            sum[1] = ta_mul2(sum[1], ta_pair(g, g));
+                            for (uint32_t d0 = col0; d0 < c0; d0 += 16u) {   // P of this tile so far
+                                uint32_t w[16];
+                                tm_ld16(s_at + d0, w);
+                                tm_ld_wait();
+#pragma unroll
+                                for (int j = 0; j < (FP8 ? 8 : 16); ++j) {
+                                    if constexpr (FP8) {
+                                        const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&w[j]), __float2half2_rn(g));
+                                        w[j] = *reinterpret_cast<const uint32_t*>(&h);
+                                    } else {
+                                        w[j] = pg_mul_bf16x2(w[j], __float_as_uint(g) >> 16 | (__float_as_uint(g) & 0xffff0000u));
+                                    }
+                                }
+                                ta_tmem_st16(s_at + d0, w);
+                            }
+                            if (t > first && !(ok = ta_scale_o(g))) break;
+                        }
                         uint32_t h[FP8 ? 16 : 32];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
@@ -1212,14 +1190,14 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         } else {
                             ta_tmem_st32(s_at + c0, h);
                         }
-                        if (c0 == col0) break;
                     }
-                    if (p.split > 1u) {   // the other copies' columns of this group are zero
+                    if (!ok) break;
+                    if (p.split > 1u) {   // the other copies' columns are zero
                         uint32_t zero[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) zero[j] = 0u;
 #pragma unroll 1
-                        for (uint32_t c0 = grp * (NK / NG); c0 < (grp + 1u) * (NK / NG); c0 += 16u)
+                        for (uint32_t c0 = 0; c0 < (uint32_t)NK; c0 += 16u)
                             if (c0 < col0 || c0 >= col1) ta_tmem_st16(s_at + c0, zero);
                     }
                     float s0, s1;
@@ -1229,11 +1207,14 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 }
                 tm_fence_before();
                 __syncwarp();
-                if (lane == 0u) mbar_arrive(smem_u32(p.two ? &s.r_probs[grp] : &s.h_probs[buf][grp]));
-                if (p.two) ++nr;
-                else ++nh;
+                if (lane == 0u) mbar_arrive(smem_u32(&s.probs[b]));
             }
-            if (ok) ok = p.two ? ta_wait(&s.r_done[grp], (nr - 1u) & 1u, s, c.status) : ta_wait(&s.h_done[(nh - 1u) & 1u][grp], ((nh - 1u) >> 1) & 1u, s, c.status);
+            tile += p.t1 - p.t0;
+            const bool any = first < p.t1;   // whether this group had a tile
+            if (ok && any) {
+                const uint32_t b = NG == 2 ? grp : p.t1 - 1u - p.t0 & 1u;
+                ok = ta_wait(&s.done[b], (b ? n1 : n0) - 1u & 1u, s, c.status);
+            }
             ok = ok && ta_wait(&s.piece_end[npiece % TA_RING], (npiece / TA_RING) & 1u, s, c.status);
             if (!(ok = ta_named_all(3u, NG * 128u, ok))) break;   // (no softmax warp waits for one that has given up)
             tm_fence_after();
@@ -1242,8 +1223,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             // the parts of a row: one reference, one sum
             const uint32_t me = grp * 128u + L, parts = p.two ? 1u : NG * p.split;
             auto part = [&](uint32_t k) {   // thread that holds part k of row r (units of one run)
-                const uint32_t g = k / p.split, j = k % p.split;
-                return g * 128u + (R == 32u ? (2u * j + g) * 32u : j * R) + r;
+                return k / p.split * 128u + k % p.split * R + r;
             };
             float mm = m, ll = l, f = 1.f;
             s.ml[0][me] = m;
@@ -1272,18 +1252,18 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD;
             float* const rec = a.part + ((size_t)(whole ? 0u : p.slot) * TA_RECORD + r) * HD;
             auto at16 = [](uint32_t thread, uint32_t j) { return thread * 16u + ((j / 4u ^ (thread >> 1 & 3u)) << 2); };   // (eight threads' four columns lie in all banks)
-            const uint32_t cols = 16u / parts, mine = p.two ? 0u : (grp * p.split + share) * cols;   // of a chunk of 16: what this thread writes of row r
+            const uint32_t cols = parts > 4u ? 4u : 16u / parts, mine = p.two ? 0u : (grp * p.split + share) * cols;   // of a chunk of 16: what this thread writes of row r
 #pragma unroll 1
             for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
                 uint32_t x[16];
                 tm_ld16(o_at + c0, x);
                 tm_ld_wait();
-                if (bad && valid && !idle) {   // values that are no numbers, for the rows that see them
-                    for (uint32_t t = p.t0; t < p.t1; ++t) {
+                if (bad && valid && any) {   // values that are no numbers, for the rows that see them
+                    for (uint32_t t = first; t < p.t1; t += step) {
                         const uint32_t pos = ta_tile_pos(p.q, t, NK);
                         if (!ta_mixed(a, p.q, pos, NK, INT32_MAX)) continue;
                         for (uint32_t k0 = col0; k0 < col1; k0 += 32u) {
-                            uint32_t sees = row.sees(pos + k0);
+                            uint32_t sees = ta_sees(a, row, pos + k0);
                             while (sees) {
                                 const uint32_t at = pos + k0 + __ffs(sees) - 1u;
                                 sees &= sees - 1u;
@@ -1301,7 +1281,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 }
                 float o[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(x[j]) * g;
+                for (int j = 0; j < 16; ++j) o[j] = any ? __uint_as_float(x[j]) * g : 0.f;
                 if (p.two) {
                     if (valid) {
 #pragma unroll
@@ -1317,7 +1297,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&s.x[at16(me, j)]) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                 ta_named_sync(3u, NG * 128u);
-                if (valid && !idle) {
+                if (valid && mine < 16u) {
                     for (uint32_t j = mine; j < mine + cols; j += 4u) {
                         float4 y = *reinterpret_cast<const float4*>(&s.x[at16(part(0u), j)]);
                         for (uint32_t k = 1; k < parts; ++k) {
