@@ -29,6 +29,7 @@ constexpr int SP_BINS = 2048;             // 32 to the unit of (max - x) / T; th
 constexpr float SP_BINS_PER_UNIT = 32.f;
 constexpr uint32_t SP_LIST = 2048;        // members of a bin that are put in order; also the largest k that one block finishes alone
 constexpr uint32_t SP_SLICE = 40960;      // most logits of a block
+constexpr int SP_POW = 64;                // entries of the table of powers of two
 constexpr int SP_MAX_CLUSTER = 8;
 constexpr uint32_t SP_SLICE_FEW = 16384;  // logits of a block beyond which a row is spread over more blocks
 
@@ -42,11 +43,15 @@ struct SampleArgs {
     float* logprobs;
 };
 
-// Shared memory behind the slice of logits.
-struct SampleShared {
-    uint64_t list[SP_LIST];               // first block: members of a bin, (complement of the key, token)
-    double listw[SP_LIST];
-    uint32_t hist[SP_BINS];
+// Shared memory in front of the slice of logits.
+struct alignas(16) SampleShared {
+    uint64_t list[SP_LIST];               // members of a bin, (complement of the key, token): a block's own, in the first block all of them
+    union {
+        double listw[SP_LIST];
+        uint64_t bins[SP_BINS];           // a histogram of the whole row
+    };
+    uint32_t hist[SP_BINS];               // a block's own
+    double pow2[SP_POW];                  // 2^(j / SP_POW)
     // written by every block of the cluster; two of each in turn, so that a block may go on while another still reads
     double sums[2][SP_MAX_CLUSTER][3];
     uint64_t best[2][SP_MAX_CLUSTER];
@@ -54,7 +59,7 @@ struct SampleShared {
     uint64_t warp_u64[SP_WARPS];
     uint64_t cut;                         // first block: what the other blocks read
     uint64_t found64[2];
-    uint32_t found, n_list;
+    uint32_t found, n_list, n_own;
 };
 
 __device__ __forceinline__ uint32_t cl_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
@@ -69,18 +74,15 @@ __device__ __forceinline__ uint32_t cl_map(const void* p, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void cl_st64(uint32_t a, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
+__device__ __forceinline__ void cl_st128(uint32_t a, uint64_t v, uint64_t w) {
+    asm volatile("st.shared::cluster.v2.u64 [%0], {%1, %2};" ::"r"(a), "l"(v), "l"(w) : "memory");
+}
 __device__ __forceinline__ uint64_t cl_ld64(uint32_t a) { uint64_t v; asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory"); return v; }
 __device__ __forceinline__ uint4 cl_ld128(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t cl_add(uint32_t a, uint32_t v) {
-    uint32_t old;
-    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(v) : "memory");
-    return old;
-}
-
 // Whole numbers in the order of the floats they stand for, and back.
 __device__ __forceinline__ uint32_t sp_key(float x) {
     const uint32_t u = __float_as_uint(x);
@@ -90,21 +92,34 @@ __device__ __forceinline__ float sp_unkey(uint32_t k) { return __uint_as_float(k
 // Places in the order of falling logits: the lower the number, the earlier.
 __device__ __forceinline__ uint64_t sp_place(float x, uint32_t token) { return (uint64_t)(~sp_key(x)) << 32 | token; }
 
-__device__ __forceinline__ double sp_weight(float x, float m, double inv_t) {
-    if (x == m) return 1.0;
-    const double y = ((double)x - (double)m) * inv_t;
-    return y > -80.0 ? exp(y) : 0.0;   // (an empty token's y is -infinity; the rest is less than 2^-115 of the largest)
-}
-
 struct Sampler {
     float* x;                 // this block's slice
     SampleShared& s;
     uint32_t base, n;         // first token of the slice, and how many
     uint32_t rank, C, tid, warp, lane;
     float m, scale;
-    double inv_t;
+    double c64;               // 64 log2(e) / T
+    double md;                // m
     uint32_t turn;            // of the cluster's exchanges
 
+    // exp((v - m) / T), by Tang's table method: t = 64 (v - m) log2(e) / T = n + r, 2^(n / 64) from a table of 64 powers and the exponent, 2^(r / 64)
+    // from six terms of its series (|r| <= 1/2: the seventh is below 2^-54).  What is wrong with t counts most, 2^-46 at t = -80 * 92.
+    __device__ __forceinline__ double weight(float v) const {
+        const double t = ((double)v - md) * c64;
+        if (!(t > -7400.0)) return 0.0;   // (an empty token's t is -infinity; the rest is less than 2^-115 of the largest)
+        const double shifted = t + 6755399441055744.0;   // 1.5 * 2^52: the sum's last bit is 1
+        const double r = t - (shifted - 6755399441055744.0);
+        const int32_t n = __double2loint(shifted);
+        constexpr double L = 0.010830424696249145;   // ln 2 / 64
+        double q = L * L * L * L * L / 120;
+        q = fma(q, r, L * L * L * L / 24);
+        q = fma(q, r, L * L * L / 6);
+        q = fma(q, r, L * L / 2);
+        q = fma(q, r, L);
+        q = fma(q, r, 1.0);
+        q *= s.pow2[n & 63];
+        return __hiloint2double(__double2hiint(q) + (n >> 6) * (1 << 20), __double2loint(q));
+    }
     __device__ __forceinline__ uint32_t bin(float v) const { return (uint32_t)fminf((m - v) * scale, (float)(SP_BINS - 1)); }
 
     __device__ __forceinline__ double block_sum(double v) {
@@ -118,8 +133,8 @@ struct Sampler {
         for (int w = 0; w < SP_WARPS; ++w) all += s.warp_sum[w];
         return all;
     }
-    // Inclusive sum over the threads of the block.
-    __device__ __forceinline__ double block_scan(double v, double& before) {
+    // Inclusive sum over the threads of the block, what lies before this thread, and all of it.
+    __device__ __forceinline__ double block_scan(double v, double& before, double& total) {
         double incl = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -130,7 +145,12 @@ struct Sampler {
         if (lane == 31u) s.warp_sum[warp] = incl;
         __syncthreads();
         double b = 0;
-        for (uint32_t w = 0; w < warp; ++w) b += s.warp_sum[w];
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < SP_WARPS; ++w) {
+            if (w < (int)warp) b += s.warp_sum[w];
+            total += s.warp_sum[w];
+        }
         before = b + (incl - v);
         return b + incl;
     }
@@ -175,55 +195,85 @@ struct Sampler {
     }
 
     // Histogram over the whole row, in every thread's hands: thread t gets bins 4 t .. 4 t + 3.
-    // value(x, token, bin) says which bin (< SP_BINS) and how much; false: left out.
-    template <class Value>
-    __device__ __forceinline__ void histogram(Value&& value, uint64_t (&mine)[4]) {
+    // each(add) calls add(bin, amount) for what this thread contributes.
+    template <class Each>
+    __device__ __forceinline__ void histogram(Each&& each, uint64_t (&mine)[4]) {
         static_assert(SP_BINS == 4 * SP_THREADS, "four bins to a thread");
         __syncthreads();
         reinterpret_cast<uint4*>(s.hist)[tid] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (uint32_t i = tid; i < n; i += SP_THREADS) {
-            uint32_t b, v;
-            if (value(x[i], base + i, b, v)) atomicAdd(&s.hist[b], v);
-        }
-        cl_sync();
+        each([&](uint32_t b, uint32_t v) { atomicAdd(&s.hist[b], v); });
+        if (C > 1u) {
+            cl_sync();
+            // every block adds up its share of the bins and hands the sums to all
+            const uint32_t per = SP_BINS / C, b4 = rank * per + 4u * tid;
+            if (4u * tid < per) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mine[q] = 0;
-        for (uint32_t r = 0; r < C; ++r) {
-            const uint4 h = cl_ld128(cl_map(&s.hist[4 * tid], r));
-            mine[0] += h.x; mine[1] += h.y; mine[2] += h.z; mine[3] += h.w;
+                for (int i = 0; i < 4; ++i) mine[i] = 0;
+                for (uint32_t r = 0; r < C; ++r) {
+                    const uint4 h = cl_ld128(cl_map(&s.hist[b4], r));
+                    mine[0] += h.x; mine[1] += h.y; mine[2] += h.z; mine[3] += h.w;
+                }
+                for (uint32_t r = 0; r < C; ++r) {
+                    const uint32_t to = cl_map(&s.bins[b4], r);
+                    cl_st128(to, mine[0], mine[1]);
+                    cl_st128(to + 16u, mine[2], mine[3]);
+                }
+            }
+            cl_sync();
+            const ulonglong2 a = reinterpret_cast<const ulonglong2*>(s.bins)[2 * tid], b = reinterpret_cast<const ulonglong2*>(s.bins)[2 * tid + 1];
+            mine[0] = a.x; mine[1] = a.y; mine[2] = b.x; mine[3] = b.y;
+        } else {
+            __syncthreads();
+            const uint4 h = reinterpret_cast<const uint4*>(s.hist)[tid];
+            mine[0] = h.x; mine[1] = h.y; mine[2] = h.z; mine[3] = h.w;
         }
-        cl_sync();   // the histograms may be cleared again
     }
 
     // The tokens that `in` names, in any order, in the first block's list; returns how many there are (more than SP_LIST: some are
-    // missing) in the first block, 0 in the others.  Between two calls lies another exchange of the cluster.
+    // missing), the same in every block.  Between two calls lies another exchange of the cluster.
     template <class In>
     __device__ __forceinline__ uint32_t gather(In&& in) {
-        if (rank == 0u && tid == 0u) s.n_list = 0u;
+        if (tid == 0u) s.n_own = 0u;
+        __syncthreads();
+        for (uint32_t i = tid; i < n; i += SP_THREADS) {
+            const float v = x[i];
+            if (!in(v, base + i)) continue;
+            const uint32_t at = atomicAdd(&s.n_own, 1u);
+            if (at < SP_LIST) s.list[at] = sp_place(v, base + i);
+        }
+        if (C == 1u) {
+            __syncthreads();
+            return s.n_own;
+        }
+        __syncthreads();
+        const uint32_t own = s.n_own, half = turn++ & 1u;
+        if (tid < C) cl_st64(cl_map(&s.best[half][rank], tid), own);
         cl_sync();
-        const uint32_t count = cl_map(&s.n_list, 0), list = cl_map(s.list, 0);
-        for (uint32_t i0 = 0; i0 < n; i0 += SP_THREADS) {
-            const uint32_t i = i0 + tid;
-            uint64_t p = 0;
-            bool yes = false;
-            if (i < n && x[i] > -INFINITY) {
-                p = sp_place(x[i], base + i);
-                yes = in(x[i], p);
-            }
-            const uint32_t who = __ballot_sync(0xffffffffu, yes);
-            if (!who) continue;
-            uint32_t at = 0;
-            if (lane == 0u) at = cl_add(count, __popc(who));
-            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-            if (yes && at < SP_LIST) cl_st64(list + at * 8u, p);
+        uint32_t before = 0, all = 0;
+        for (uint32_t r = 0; r < C; ++r) {
+            const uint32_t c = (uint32_t)s.best[half][r];
+            if (r < rank) before += c;
+            all += c;
+        }
+        if (rank > 0u && all <= SP_LIST) {
+            const uint32_t to = cl_map(&s.list[before], 0);
+            for (uint32_t i = tid; i < own; i += SP_THREADS) cl_st64(to + i * 8u, s.list[i]);
         }
         cl_sync();
-        return rank == 0u ? s.n_list : 0u;
+        return all;
     }
-    // Bitonic sort of the first n entries of the list, ascending (first block; n <= SP_LIST).
-    __device__ __forceinline__ uint32_t sort_list(uint32_t cnt) {
-        uint32_t len = 2;
+    // The first cnt entries of the list in ascending order (first block; cnt <= SP_LIST, all different).
+    __device__ __forceinline__ void sort_list(uint32_t cnt) {
+        if (cnt <= SP_THREADS) {   // every thread counts what comes before its own entry
+            const uint64_t own = tid < cnt ? s.list[tid] : ~0ull;
+            const uint32_t at = count_before(own, cnt);
+            __syncthreads();
+            if (tid < cnt) s.list[at] = own;
+            __syncthreads();
+            return;
+        }
+        uint32_t len = 2;   // bitonic
         while (len < cnt) len <<= 1;
         for (uint32_t i = cnt + tid; i < len; i += SP_THREADS) s.list[i] = ~0ull;
         __syncthreads();
@@ -239,7 +289,18 @@ struct Sampler {
                 }
                 __syncthreads();
             }
-        return len;
+    }
+    __device__ __forceinline__ uint32_t count_before(uint64_t own, uint32_t cnt) const {
+        uint32_t at = 0;
+        if (warp * 32u < cnt) {
+#pragma unroll 4
+            for (uint32_t j = 0; j + 1u < cnt; j += 2u) {
+                const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&s.list[j]);
+                at += (v.x < own) + (v.y < own);
+            }
+            if (cnt & 1u) at += s.list[cnt - 1u] < own;
+        }
+        return at;
     }
     __device__ __forceinline__ uint64_t broadcast(uint64_t v) {   // of the first block's thread 0
         if (rank == 0u && tid == 0u) s.cut = v;
@@ -323,12 +384,11 @@ __device__ __forceinline__ uint64_t sp_cut_by_rank(Sampler& q, SampleRegion g, u
         uint64_t lo, hi, mine[4], b4;
         uint32_t shift, bin;
         sp_split(q, g, lo, hi, shift);
-        q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
-            const uint64_t p = sp_place(x, token);
-            if (!(x > -INFINITY) || p < lo || p > hi) return false;
-            b = (uint32_t)((p - lo) >> shift);
-            v = 1u;
-            return true;
+        q.histogram([&](auto&& add) {
+            for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+                const uint64_t p = sp_place(q.x[i], q.base + i);
+                if (q.x[i] > -INFINITY && p >= lo && p <= hi) add((uint32_t)((p - lo) >> shift), 1u);
+            }
         }, mine);
         if (!sp_find(q, mine, k - before, bin, b4, own)) return hi;
         before += b4;
@@ -336,7 +396,7 @@ __device__ __forceinline__ uint64_t sp_cut_by_rank(Sampler& q, SampleRegion g, u
         g.lo = lo + ((uint64_t)bin << shift);
         g.hi = min(hi, g.lo + (((uint64_t)1 << shift) - 1u));
     }
-    const uint32_t cnt = q.gather([&](float x, uint64_t p) { return g.side(q, x, p) == 0; });
+    const uint32_t cnt = q.gather([&](float x, uint32_t token) { return x > -INFINITY && g.side(q, x, sp_place(x, token)) == 0; });
     uint64_t cut = 0;
     if (q.rank == 0u) {   // own >= k - before >= 1
         q.sort_list(cnt);
@@ -351,12 +411,14 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
     uint64_t mine[4], before, own;
     uint32_t bin;
     // approximate masses, in units of 2^-43 of the largest weight: sums of at most 2^19 tokens stay below 2^62
-    q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
-        if (!(x > -INFINITY) || sp_place(x, token) > cut) return false;
-        const float t = fminf((q.m - x) * q.scale, (float)(SP_BINS - 1));
-        b = (uint32_t)t;
-        v = (uint32_t)(65536.f * exp2f((float)b * (1.4426950408889634f / SP_BINS_PER_UNIT) - t * (1.4426950408889634f / SP_BINS_PER_UNIT)));
-        return true;
+    q.histogram([&](auto&& add) {
+        for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+            const float x = q.x[i];
+            if (!(x > -INFINITY) || sp_place(x, q.base + i) > cut) continue;
+            const float t = fminf((q.m - x) * q.scale, (float)(SP_BINS - 1));
+            const uint32_t b = (uint32_t)t;
+            add(b, (uint32_t)(65536.f * exp2f(((float)b - t) * (1.4426950408889634f / SP_BINS_PER_UNIT))));
+        }
     }, mine);
     uint64_t all = 0;
 #pragma unroll
@@ -384,7 +446,7 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
             if (place > cut) continue;
             const int side = g.side(q, x, place);
             if (side > 0 && goal > 0) continue;
-            const double w = sp_weight(x, q.m, q.inv_t);
+            const double w = q.weight(x);
             sum += w;
             if (side < 0) front += w;
             if (side == 0) inside += w;
@@ -402,20 +464,22 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
             went = go;
             bin += go;
         } else {
-            uint32_t cnt = q.gather([&](float x, uint64_t place) { return place <= cut && g.side(q, x, place) == 0; });
-            cnt = (uint32_t)q.broadcast(cnt);
+            const uint32_t cnt = q.gather([&](float x, uint32_t token) {
+                const uint64_t place = sp_place(x, token);
+                return x > -INFINITY && place <= cut && g.side(q, x, place) == 0;
+            });
             if (cnt <= SP_LIST) {
                 uint64_t end = 0;
                 if (q.rank == 0u) {
                     q.sort_list(cnt);
-                    double w[SP_LIST / SP_THREADS], sum4 = 0, ahead;
+                    double w[SP_LIST / SP_THREADS], sum4 = 0, ahead, all4;
 #pragma unroll
                     for (uint32_t i = 0; i < SP_LIST / SP_THREADS; ++i) {
                         const uint32_t at = q.tid * (SP_LIST / SP_THREADS) + i;
-                        w[i] = at < cnt ? sp_weight(sp_unkey(~(uint32_t)(s.list[at] >> 32)), q.m, q.inv_t) : 0.0;
+                        w[i] = at < cnt ? q.weight(sp_unkey(~(uint32_t)(s.list[at] >> 32))) : 0.0;
                         sum4 += w[i];
                     }
-                    q.block_scan(sum4, ahead);
+                    q.block_scan(sum4, ahead, all4);
                     uint32_t stay = 0;
 #pragma unroll
                     for (uint32_t i = 0; i < SP_LIST / SP_THREADS; ++i) {
@@ -433,15 +497,16 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
             went = 0;
             settled = false;
             const float first = sp_unkey(~(uint32_t)(lo >> 32));
-            q.histogram([&](float x, uint32_t token, uint32_t& b, uint32_t& v) {
-                const uint64_t place = sp_place(x, token);
-                if (!(x > -INFINITY) || place < lo || place > hi) return false;
-                b = (uint32_t)((place - lo) >> shift);
-                v = (uint32_t)(65536.f * __expf((float)(((double)x - (double)first) * q.inv_t)));
-                return true;
+            q.histogram([&](auto&& add) {
+                for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+                const float x = q.x[i];
+                const uint64_t place = sp_place(x, q.base + i);
+                if (!(x > -INFINITY) || place < lo || place > hi) continue;
+                add((uint32_t)((place - lo) >> shift), (uint32_t)(65536.f * exp2f((float)(((double)x - (double)first) * q.c64) * (1.f / 64.f))));
+                }
             }, mine);
             last = (uint32_t)((hi - lo) >> shift);
-            const double unit = sp_weight(first, q.m, q.inv_t) / 65536.0;
+            const double unit = q.weight(first) / 65536.0;
             want = unit > 0 ? (uint64_t)fmax(fmin((goal - front) / unit, 9e18), 1.0) : 1ull;
             if (!sp_find(q, mine, want, bin, before, own)) bin = last;
         }
@@ -464,6 +529,40 @@ __device__ __forceinline__ void sp_write(const SampleArgs& a, uint32_t row, int3
 // The first block alone: `cnt` tokens in its list, of which the first k by rank stay.
 __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, uint32_t row, uint32_t cnt, uint32_t k, double p, double min_p, double u) {
     SampleShared& s = q.s;
+    if (cnt <= SP_THREADS) {   // a token to a thread; orders by counting
+        const uint64_t own = q.tid < cnt ? s.list[q.tid] : ~0ull;
+        const double w = q.tid < cnt ? q.weight(sp_unkey(~(uint32_t)(own >> 32))) : 0.0;
+        const uint32_t rank = q.count_before(own, cnt), most = min(cnt, k);
+        if (q.tid < cnt) s.listw[rank] = w;
+        __syncthreads();
+        const double in_order = q.tid < most ? s.listw[q.tid] : 0.0;
+        double ahead, mass, total;
+        q.block_scan(in_order, ahead, mass);
+        // (what stays is the beginning of the order)
+        const uint32_t stay = (uint32_t)__syncthreads_count(q.tid < most && (q.tid == 0u || ((p >= 1.0 || ahead < p * mass) && in_order >= min_p)));
+        const uint32_t token = q.tid < cnt && rank < stay ? (uint32_t)own : ~0u;
+        uint32_t* tokens = s.hist;
+        if (q.tid < (cnt + 3u) / 4u * 4u) tokens[q.tid] = token;
+        __syncthreads();
+        uint32_t at = 0;
+        if (q.warp * 32u < cnt)
+#pragma unroll 4
+            for (uint32_t j = 0; j < cnt; j += 4u) {
+                const uint4 v = *reinterpret_cast<const uint4*>(&tokens[j]);
+                at += (v.x < token) + (v.y < token) + (v.z < token) + (v.w < token);
+            }
+        if (token != ~0u) {
+            s.listw[SP_THREADS + at] = w;
+            s.hist[SP_THREADS + at] = token;
+        }
+        __syncthreads();
+        const double mine = q.tid < stay ? s.listw[SP_THREADS + q.tid] : 0.0;
+        const double up_to = q.block_scan(mine, ahead, total), goal = u * total;
+        // the first token at which the running mass exceeds the goal; the last one of any mass where rounding lets none
+        const uint64_t first = q.block_min(mine > 0 && up_to > goal ? q.tid : ~0ull), last = ~q.block_min(mine > 0 ? ~(uint64_t)q.tid : ~0ull);
+        if (q.tid == (uint32_t)(first != ~0ull ? first : last)) sp_write(a, row, (int32_t)s.hist[SP_THREADS + q.tid], mine, total);
+        return;
+    }
     constexpr uint32_t PER = SP_LIST / SP_THREADS;
     q.sort_list(cnt);
     cnt = min(cnt, k);
@@ -471,11 +570,11 @@ __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, 
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i) {
         const uint32_t at = q.tid * PER + i;
-        w[i] = at < cnt ? sp_weight(sp_unkey(~(uint32_t)(s.list[at] >> 32)), q.m, q.inv_t) : 0.0;
+        w[i] = at < cnt ? q.weight(sp_unkey(~(uint32_t)(s.list[at] >> 32))) : 0.0;
         sum += w[i];
     }
-    q.block_scan(sum, ahead);
-    const double mass = q.block_sum(sum);
+    double mass, total;
+    q.block_scan(sum, ahead, mass);
     uint64_t item[PER];
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i) {
@@ -503,8 +602,8 @@ __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, 
         w[i] = item[i] != ~0ull ? s.listw[(uint32_t)item[i]] : 0.0;
         sum += w[i];
     }
-    q.block_scan(sum, ahead);
-    const double total = q.block_sum(sum), goal = u * total;
+    q.block_scan(sum, ahead, total);
+    const double goal = u * total;
     // the first token at which the running mass exceeds the goal; the last one of any mass where rounding lets none
     uint64_t first = ~0ull, last = ~0ull;
 #pragma unroll
@@ -547,25 +646,49 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     if (!(T > 0.f) || p <= 0.0 || min_p > 1.0) top_k = 1;
     const double u = a.uniforms[row] > 0.f ? (double)fminf(a.uniforms[row], 1.f) : 0.0;
 
-    uint64_t best = ~0ull;   // the first place of the row
+    if (q.tid < SP_POW) s.pow2[q.tid] = exp2((double)q.tid / SP_POW);
+    // NaN is no token; -0 counts as 0.  This thread's largest logit, the lowest token among equals.
+    float most = -INFINITY;
+    uint32_t most_at = 0;
+    auto keep = [&](float v, uint32_t i) {
+        const float y = v == v ? v + 0.f : -INFINITY;
+        if (y > most) {
+            most = y;
+            most_at = i;
+        }
+        return y;
+    };
     if (!idle) {
         const float* src = a.logits + (int64_t)row * a.stride + q.base;
+        const uint32_t n4 = ((uintptr_t)src & 15u) == 0 ? q.n / 4u : 0u;   // pieces of 16 bytes
         constexpr int U = 8;
-        for (uint32_t i0 = q.tid; i0 < q.n; i0 += SP_THREADS * U) {
-            float v[U];
+        for (uint32_t i0 = q.tid; i0 < n4; i0 += SP_THREADS * U) {
+            float4 v[U];
 #pragma unroll
-            for (int j = 0; j < U; ++j) v[j] = i0 + j * SP_THREADS < q.n ? src[i0 + j * SP_THREADS] : 0.f;
+            for (int j = 0; j < U; ++j)
+                if (i0 + j * SP_THREADS < n4) v[j] = reinterpret_cast<const float4*>(src)[i0 + j * SP_THREADS];
 #pragma unroll
             for (int j = 0; j < U; ++j) {
                 const uint32_t i = i0 + j * SP_THREADS;
-                if (i < q.n) {
-                    const float y = v[j] == v[j] ? v[j] + 0.f : -INFINITY;   // NaN: no token; -0 counts as 0
-                    q.x[i] = y;
-                    if (y > -INFINITY) best = min(best, sp_place(y, q.base + i));
+                if (i < n4) {
+                    const float4 y = make_float4(keep(v[j].x, 4 * i), keep(v[j].y, 4 * i + 1), keep(v[j].z, 4 * i + 2), keep(v[j].w, 4 * i + 3));
+                    reinterpret_cast<float4*>(q.x)[i] = y;
                 }
             }
         }
+        for (uint32_t i0 = 4 * n4 + q.tid; i0 < q.n; i0 += SP_THREADS * 2 * U) {
+            float v[2 * U];
+#pragma unroll
+            for (int j = 0; j < 2 * U; ++j)
+                if (i0 + j * SP_THREADS < q.n) v[j] = src[i0 + j * SP_THREADS];
+#pragma unroll
+            for (int j = 0; j < 2 * U; ++j) {
+                const uint32_t i = i0 + j * SP_THREADS;
+                if (i < q.n) q.x[i] = keep(v[j], i);
+            }
+        }
     }
+    uint64_t best = most > -INFINITY ? sp_place(most, q.base + most_at) : ~0ull;
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (idle) return;
     best = q.cluster_min(best);
@@ -576,24 +699,38 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     q.m = sp_unkey(~(uint32_t)(best >> 32));
     if (q.m == INFINITY) {   // equal chances for the infinite ones, none for the rest
         for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) q.x[i] = q.x[i] == INFINITY ? 0.f : -INFINITY;
+        most = most == INFINITY ? 0.f : -INFINITY;
         q.m = 0.f;
+        __syncthreads();
     }
     q.scale = SP_BINS_PER_UNIT / T;
-    q.inv_t = 1.0 / (double)T;
+    q.md = (double)q.m;
+    q.c64 = 92.33248261893449 / (double)T;   // 64 log2(e)
 
     uint64_t cut = ~0ull - 1ull;   // the last place that stays
     if (top_k > 0 && (uint32_t)top_k < a.vocab) {
         uint64_t mine[4], before, own;
         uint32_t bin;
-        q.histogram([&](float x, uint32_t, uint32_t& b, uint32_t& v) {
-            if (!(x > -INFINITY)) return false;
-            b = q.bin(x);
-            v = 1u;
-            return true;
+        // The k-th largest of the threads' largest logits is a lower bound of the k-th largest of all, and few others lie above it.
+        if ((uint32_t)top_k <= C * (SP_THREADS / 4)) {
+            q.histogram([&](auto&& add) {
+                if (most > -INFINITY) add(q.bin(most), 1u);
+            }, mine);
+            if (sp_find(q, mine, (uint64_t)top_k, bin, before, own)) {
+                const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.bin(x) <= bin; });
+                if (cnt <= SP_LIST) {
+                    if (q.rank == 0u) sp_finish_list(q, a, row, cnt, (uint32_t)top_k, p, min_p, u);
+                    return;
+                }
+            }
+        }
+        q.histogram([&](auto&& add) {
+            for (uint32_t i = q.tid; i < q.n; i += SP_THREADS)
+                if (q.x[i] > -INFINITY) add(q.bin(q.x[i]), 1u);
         }, mine);
         const bool enough = sp_find(q, mine, (uint64_t)top_k, bin, before, own);
         if (enough && before + own <= SP_LIST) {
-            const uint32_t cnt = q.gather([&](float x, uint64_t) { return q.bin(x) <= bin; });
+            const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.bin(x) <= bin; });
             if (q.rank == 0u) sp_finish_list(q, a, row, cnt, (uint32_t)top_k, p, min_p, u);
             return;
         }
@@ -601,35 +738,40 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     }
     if (p < 1.0) cut = sp_cut_by_mass(q, cut, p);
 
-    // the draw: sums of the runs of tokens of every warp, then the run that the goal falls into once more
+    // The draw: every thread sums up a run of its own (of odd length, so that 32 of them lie in different banks), then the run that the
+    // goal falls into is looked at once more.
+    const bool all_stay = cut == ~0ull - 1ull;
+    const float cut_x = all_stay ? -INFINITY : sp_unkey(~(uint32_t)(cut >> 32));
+    const uint32_t cut_token = all_stay ? 0u : (uint32_t)cut;
+    // what is certainly below min_p need not be weighed: 32 bits with room to spare
+    const float sure = min_p > 0 ? q.m + 1.0001f * T * logf(min_pf) - 1e-5f * fabsf(q.m) : -INFINITY;
     auto weight = [&](uint32_t i) {
         const float x = q.x[i];
-        if (!(x > -INFINITY) || sp_place(x, q.base + i) > cut) return 0.0;
-        const double w = sp_weight(x, q.m, q.inv_t);
+        if (!(x > cut_x || (x == cut_x && q.base + i <= cut_token && !all_stay)) || x < sure) return 0.0;
+        const double w = q.weight(x);
         return w >= min_p ? w : 0.0;
     };
-    const uint32_t run = (q.n + SP_WARPS * 32u - 1u) / (SP_WARPS * 32u) * 32u, i0 = q.warp * run, i1 = min(q.n, i0 + run);
-    double mine = 0;
-    for (uint32_t i = i0 + q.lane; i < i1; i += 32u) mine += weight(i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    __syncthreads();
-    if (q.lane == 0u) s.warp_sum[q.warp] = mine;
-    __syncthreads();
-    double sums[SP_WARPS], own = 0;
-#pragma unroll
-    for (int w = 0; w < SP_WARPS; ++w) own += sums[w] = s.warp_sum[w];
-    if (q.tid < C) cl_st64(cl_map(&s.sums[q.turn & 1u][q.rank][0], q.tid), __double_as_longlong(own));
-    cl_sync();
+    const uint32_t run = (q.n + SP_THREADS - 1u) / SP_THREADS | 1u, i0 = min(q.n, q.tid * run), i1 = min(q.n, i0 + run);
+    double mine = 0, before, own;
+    for (uint32_t i = i0; i < i1; ++i) mine += weight(i);
+    q.block_scan(mine, before, own);
+    const uint32_t half = q.turn++ & 1u;
+    if (C > 1u) {
+        if (q.tid < C) cl_st64(cl_map(&s.sums[half][q.rank][0], q.tid), __double_as_longlong(own));
+        cl_sync();
+    } else {
+        if (q.tid == 0u) s.sums[half][0][0] = own;
+        __syncthreads();
+    }
     double total = 0;
-    for (uint32_t r = 0; r < C; ++r) total += s.sums[q.turn & 1u][r][0];
+    for (uint32_t r = 0; r < C; ++r) total += s.sums[half][r][0];
     const double goal = u * total;
-    // the first part whose end lies beyond the goal, else the last one that has any mass
-    double ahead = 0, at = 0, front = 0;
+    // the first block whose end lies beyond the goal, else the last one that has any mass
+    double at = 0, front = 0;
     uint32_t who = C;
     bool beyond = false;
     for (uint32_t r = 0; r < C; ++r) {
-        const double x = s.sums[q.turn & 1u][r][0];
+        const double x = s.sums[half][r][0];
         if (x > 0 && !beyond) {
             who = r;
             front = at;
@@ -638,57 +780,33 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
         at += x;
     }
     if (who != q.rank) return;
-    at = front;
-    beyond = false;
-    uint32_t in = 0;
-#pragma unroll
-    for (int w = 0; w < SP_WARPS; ++w) {
-        if (sums[w] > 0 && !beyond) {
-            in = w;
-            ahead = at;
-            beyond = at + sums[w] > goal;
-        }
-        at += sums[w];
-    }
-    if (in != q.warp) return;
-    // every lane a run of its own of the warp's (read from a place that goes by the lane, so that the banks differ)
-    const uint32_t part = run / 32u, j0 = i0 + q.lane * part;
-    double sum = 0;
-    for (uint32_t j = 0; j < part; ++j) {
-        uint32_t i = j + q.lane % part;
-        i = j0 + (i >= part ? i - part : i);
-        if (i < i1) sum += weight(i);
-    }
-    auto pick = [&](double v, double start, double& before_it) {   // the lane that the goal falls into
-        double incl = v;
+    // the same among the threads' runs
+    const uint64_t first = q.block_min(mine > 0 && front + before + mine > goal ? q.tid : ~0ull), last = ~q.block_min(mine > 0 ? ~(uint64_t)q.tid : ~0ull);
+    const uint32_t t = (uint32_t)(first != ~0ull ? first : last);
+    if (q.tid == t) s.found64[0] = __double_as_longlong(front + before);
+    __syncthreads();
+    if (q.warp != 0u) return;
+    // and among the tokens of that run, 32 at a time
+    double start = __longlong_as_double(s.found64[0]);
+    const uint32_t k0 = min(q.n, t * run), k1 = min(q.n, k0 + run);
+    uint32_t token = 0;
+    double w_token = 1;
+    for (uint32_t k = k0; k < k1; k += 32u) {
+        const double w = k + q.lane < k1 ? weight(k + q.lane) : 0.0;
+        double incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const double y = __shfl_up_sync(0xffffffffu, incl, o);
             if (q.lane >= (uint32_t)o) incl += y;
         }
-        const uint32_t any = __ballot_sync(0xffffffffu, v > 0), over = __ballot_sync(0xffffffffu, v > 0 && start + incl > goal);
-        const uint32_t l = over ? __ffs(over) - 1 : any ? 31 - __clz(any) : 32;
-        before_it = start + __shfl_sync(0xffffffffu, incl - v, l & 31u);
-        return over ? l : l | 64u;   // 64: none lies beyond the goal
-    };
-    double start;
-    const uint32_t l = pick(sum, ahead, start) & 31u;
-    const uint32_t k0 = i0 + l * part, k1 = min(i1, k0 + part);
-    uint32_t token = 0;
-    double w_token = 1;
-    for (uint32_t k = k0; k < k1; k += 32u) {
-        const double w = k + q.lane < k1 ? weight(k + q.lane) : 0.0;
-        double before_it;
-        const uint32_t got = pick(w, start, before_it);
-        if ((got & 63u) < 32u) {
-            token = q.base + k + (got & 31u);
-            w_token = __shfl_sync(0xffffffffu, w, got & 31u);
+        const uint32_t any = __ballot_sync(0xffffffffu, w > 0), over = __ballot_sync(0xffffffffu, w > 0 && start + incl > goal);
+        if (any) {
+            const uint32_t l = over ? __ffs(over) - 1 : 31 - __clz(any);
+            token = q.base + k + l;
+            w_token = __shfl_sync(0xffffffffu, w, l);
         }
-        if (got < 32u) break;
-        double all = w;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-        start += all;
+        if (over) break;
+        start += __shfl_sync(0xffffffffu, incl, 31);
     }
     if (q.lane == 0u) sp_write(a, row, (int32_t)token, w_token, total);
 }
@@ -713,7 +831,7 @@ extern "C" kl_status kl_sample(const float* logits_d, int64_t row_stride, uint32
     a.stride = row_stride;
     a.n_rows = n_rows;
     a.vocab = vocab;
-    a.slice = (vocab + C - 1) / C;
+    a.slice = (vocab + 4 * C - 1) / (4 * C) * 4;   // pieces of 16 bytes
     a.uniforms = uniforms_d;
     a.temperature = temperature_d;
     a.top_p = top_p_d;
