@@ -7,8 +7,8 @@
 // would err in one of ten draws from a flat row of 128256).
 //
 // One cluster of thread blocks = one row, whose logits are read once and stay in the blocks' shared memory.  A row is not sorted:
-//   * a histogram over (max - x) / T, 32 bins to the unit, finds the bin that a cut falls into -- by counts for top-k, by mass for
-//     top-p (a bin's members differ by 3 % at most, so their weights relative to the bin's largest fit whole numbers of 16 bits) --
+//   * a histogram over (max - x) / T, 64 bins to the unit, finds the bin that a cut falls into -- by counts for top-k, by mass for
+//     top-p (a bin's members differ by 1.6 % at most, so their weights relative to the bin's largest fit whole numbers of 16 bits) --
 //     and only that bin's members are put in order, by the first block;
 //   * approximate masses only say which bin to look at: the mass in front of it and its own are then summed in 64 bits, and the
 //     neighbouring bin is taken where they say so;
@@ -25,8 +25,8 @@ using namespace kl;
 namespace {
 
 constexpr int SP_THREADS = 512, SP_WARPS = SP_THREADS / 32;
-constexpr int SP_BINS = 2048;             // 32 to the unit of (max - x) / T; the last one holds all that lies further down
-constexpr float SP_BINS_PER_UNIT = 32.f;
+constexpr int SP_BINS = 2048;             // 64 to the unit of (max - x) / T; the last one holds all that lies further down
+constexpr float SP_BINS_PER_UNIT = 64.f;
 constexpr uint32_t SP_LIST = 2048;        // members of a bin that are put in order; also the largest k that one block finishes alone
 constexpr uint32_t SP_SLICE = 40960;      // most logits of a block
 constexpr int SP_POW = 64;                // entries of the table of powers of two
@@ -120,7 +120,9 @@ struct Sampler {
         q *= s.pow2[n & 63];
         return __hiloint2double(__double2hiint(q) + (n >> 6) * (1 << 20), __double2loint(q));
     }
-    __device__ __forceinline__ uint32_t bin(float v) const { return (uint32_t)fminf((m - v) * scale, (float)(SP_BINS - 1)); }
+    uint32_t i0, i1;          // this thread's run of the slice: of odd length, so that the runs of a warp lie in different banks
+    __device__ __forceinline__ float at(float v) const { return (m - v) * scale; }   // in bins; infinite where there is no token
+    __device__ __forceinline__ uint32_t bin(float v) const { return (uint32_t)fminf(at(v), (float)(SP_BINS - 1)); }
 
     __device__ __forceinline__ double block_sum(double v) {
 #pragma unroll
@@ -236,6 +238,7 @@ struct Sampler {
     __device__ __forceinline__ uint32_t gather(In&& in) {
         if (tid == 0u) s.n_own = 0u;
         __syncthreads();
+#pragma unroll 4
         for (uint32_t i = tid; i < n; i += SP_THREADS) {
             const float v = x[i];
             if (!in(v, base + i)) continue;
@@ -347,19 +350,32 @@ __device__ __forceinline__ bool sp_find(Sampler& q, const uint64_t (&mine)[4], u
     return bin < SP_BINS;
 }
 
-// A run of places that a cut falls into: bin `b` of the row's first histogram, or the places lo .. hi.
+// The tokens that stay: those before the place (x, token) and it.
+struct SampleCut {
+    float x;              // -infinity: all that are tokens
+    uint32_t end;         // of the tokens with this logit, those below
+    __device__ __forceinline__ bool stays(float v, uint32_t token) const { return v > x || (v == x && token < end); }
+    __device__ __forceinline__ uint64_t place() const { return end ? sp_place(x, end - 1u) : ~0ull - 1ull; }
+};
+__device__ __forceinline__ SampleCut sp_cut_at(uint64_t place) { return {sp_unkey(~(uint32_t)(place >> 32)), (uint32_t)place + 1u}; }
+
+// A run of places that a cut falls into: a bin of the row's first histogram, or the places lo .. hi.
 struct SampleRegion {
-    uint32_t b;           // SP_BINS: lo and hi say it
+    float from, to;       // the bin, as the least and the largest number of bins; from < 0: lo and hi say it
     uint64_t lo, hi;
     // -1: the token comes before the region, 0: it belongs to it, 1: behind it
-    __device__ __forceinline__ int side(const Sampler& q, float x, uint64_t place) const {
-        if (b < SP_BINS) {
-            const uint32_t at = q.bin(x);
-            return at < b ? -1 : at > b;
+    __device__ __forceinline__ int side(const Sampler& q, float x, uint32_t token) const {
+        if (from >= 0.f) {
+            const float t = q.at(x);
+            return t < from ? -1 : t > to;
         }
+        const uint64_t place = sp_place(x, token);
         return place < lo ? -1 : place > hi;
     }
 };
+__device__ __forceinline__ SampleRegion sp_bin(uint32_t b) {   // (the number below b + 1, as a float; the last bin has no end)
+    return {(float)b, b + 1u < (uint32_t)SP_BINS ? __uint_as_float(__float_as_uint((float)(b + 1u)) - 1u) : INFINITY, 0, 0};
+}
 
 // A region of too many tokens is cut into SP_BINS runs of places, 2^shift each from the first place that it holds.
 __device__ __forceinline__ void sp_split(Sampler& q, const SampleRegion& g, uint64_t& lo, uint64_t& hi, uint32_t& shift) {
@@ -367,7 +383,7 @@ __device__ __forceinline__ void sp_split(Sampler& q, const SampleRegion& g, uint
     for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
         if (!(q.x[i] > -INFINITY)) continue;
         const uint64_t p = sp_place(q.x[i], q.base + i);
-        if (g.side(q, q.x[i], p) == 0) {
+        if (g.side(q, q.x[i], q.base + i) == 0) {
             first = min(first, p);
             last = min(last, ~p);
         }
@@ -379,7 +395,7 @@ __device__ __forceinline__ void sp_split(Sampler& q, const SampleRegion& g, uint
 }
 
 // The place of rank k - 1 (ranks from zero): the last one that stays.
-__device__ __forceinline__ uint64_t sp_cut_by_rank(Sampler& q, SampleRegion g, uint64_t before, uint64_t own, uint64_t k) {
+__device__ __forceinline__ SampleCut sp_cut_by_rank(Sampler& q, SampleRegion g, uint64_t before, uint64_t own, uint64_t k) {
     while (own > SP_LIST) {
         uint64_t lo, hi, mine[4], b4;
         uint32_t shift, bin;
@@ -390,34 +406,36 @@ __device__ __forceinline__ uint64_t sp_cut_by_rank(Sampler& q, SampleRegion g, u
                 if (q.x[i] > -INFINITY && p >= lo && p <= hi) add((uint32_t)((p - lo) >> shift), 1u);
             }
         }, mine);
-        if (!sp_find(q, mine, k - before, bin, b4, own)) return hi;
+        if (!sp_find(q, mine, k - before, bin, b4, own)) return sp_cut_at(hi);
         before += b4;
-        g.b = SP_BINS;
+        g.from = -1.f;
         g.lo = lo + ((uint64_t)bin << shift);
         g.hi = min(hi, g.lo + (((uint64_t)1 << shift) - 1u));
     }
-    const uint32_t cnt = q.gather([&](float x, uint32_t token) { return x > -INFINITY && g.side(q, x, sp_place(x, token)) == 0; });
+    const uint32_t cnt = q.gather([&](float x, uint32_t token) { return x > -INFINITY && g.side(q, x, token) == 0; });
     uint64_t cut = 0;
     if (q.rank == 0u) {   // own >= k - before >= 1
         q.sort_list(cnt);
         cut = q.s.list[min((uint32_t)(k - before), cnt) - 1u];
     }
-    return q.broadcast(cut);
+    return sp_cut_at(q.broadcast(cut));
 }
 
-// The last place that stays when those stay with less than p of the mass of all places up to `cut` in front of them.
-__device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, double p) {
+// What stays of `cut` when those stay with less than p of its mass in front of them.  g: the region that the new cut falls into, run_front:
+// the mass of this thread's run that lies in front of it.
+__device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut cut, double p, SampleRegion& g, double& run_front) {
     SampleShared& s = q.s;
     uint64_t mine[4], before, own;
     uint32_t bin;
     // approximate masses, in units of 2^-43 of the largest weight: sums of at most 2^19 tokens stay below 2^62
     q.histogram([&](auto&& add) {
+#pragma unroll 4
         for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
             const float x = q.x[i];
-            if (!(x > -INFINITY) || sp_place(x, q.base + i) > cut) continue;
-            const float t = fminf((q.m - x) * q.scale, (float)(SP_BINS - 1));
-            const uint32_t b = (uint32_t)t;
-            add(b, (uint32_t)(65536.f * exp2f(((float)b - t) * (1.4426950408889634f / SP_BINS_PER_UNIT))));
+            if (!cut.stays(x, q.base + i)) continue;
+            // bins and their fraction f; the weight relative to the bin's largest is exp(-f / 64), to third order
+            const uint32_t u = (uint32_t)(fminf(q.at(x), (float)SP_BINS - 0.01f) * 65536.f), f = u & 0xffffu;
+            add(u >> 16, 65536u - (f >> 6) + (f * f >> 29));
         }
     }, mine);
     uint64_t all = 0;
@@ -431,26 +449,26 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
     if (want < 1ull) want = 1ull;
     if (!sp_find(q, mine, want, bin, before, own)) bin = 0u;
     double total = 0, goal = 0, front, inside;
-    SampleRegion g = {bin, 0, 0};
+    g = sp_bin(bin);
     uint64_t lo = 0, hi = 0;   // of the runs of places that a region has been cut into, if it has
     uint32_t shift = 0, last = SP_BINS - 1;
     int went = 0;
     bool settled = false;
     for (;;) {
+        double behind = 0;
         front = inside = 0;
-        double sum = 0;
-        for (uint32_t i = q.tid; i < q.n; i += SP_THREADS) {
+        for (uint32_t i = q.i0; i < q.i1; ++i) {
             const float x = q.x[i];
-            if (!(x > -INFINITY)) continue;
-            const uint64_t place = sp_place(x, q.base + i);
-            if (place > cut) continue;
-            const int side = g.side(q, x, place);
+            if (!cut.stays(x, q.base + i)) continue;
+            const int side = g.side(q, x, q.base + i);
             if (side > 0 && goal > 0) continue;
             const double w = q.weight(x);
-            sum += w;
             if (side < 0) front += w;
-            if (side == 0) inside += w;
+            else if (side == 0) inside += w;
+            else behind += w;
         }
+        run_front = front;
+        double sum = front + inside + behind;
         q.cluster_sums(sum, front, inside);
         if (goal == 0) {
             total = sum;
@@ -465,8 +483,7 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
             bin += go;
         } else {
             const uint32_t cnt = q.gather([&](float x, uint32_t token) {
-                const uint64_t place = sp_place(x, token);
-                return x > -INFINITY && place <= cut && g.side(q, x, place) == 0;
+                return cut.stays(x, token) && g.side(q, x, token) == 0;
             });
             if (cnt <= SP_LIST) {
                 uint64_t end = 0;
@@ -488,12 +505,12 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
                         ahead += w[i];
                     }
                     const uint32_t most = (uint32_t)~q.block_min(~(uint64_t)stay);
-                    end = cnt ? s.list[most ? most - 1u : 0u] : cut;
+                    end = cnt ? s.list[most ? most - 1u : 0u] : cut.place();
                 }
-                return q.broadcast(end);
+                return sp_cut_at(q.broadcast(end));
             }
             sp_split(q, g, lo, hi, shift);
-            if (hi > cut) hi = cut;
+            hi = min(hi, cut.place());
             went = 0;
             settled = false;
             const float first = sp_unkey(~(uint32_t)(lo >> 32));
@@ -511,11 +528,11 @@ __device__ __forceinline__ uint64_t sp_cut_by_mass(Sampler& q, uint64_t cut, dou
             if (!sp_find(q, mine, want, bin, before, own)) bin = last;
         }
         if (hi) {
-            g.b = SP_BINS;
+            g.from = -1.f;
             g.lo = lo + ((uint64_t)bin << shift);
             g.hi = min(hi, g.lo + (((uint64_t)1 << shift) - 1u));
         } else {
-            g.b = bin;
+            g = sp_bin(bin);
         }
     }
 }
@@ -638,6 +655,9 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     q.base = q.rank * a.slice;
     q.n = q.base < a.vocab ? min(a.slice, a.vocab - q.base) : 0u;
     q.turn = 0;
+    const uint32_t run = (q.n + SP_THREADS - 1u) / SP_THREADS | 1u;
+    q.i0 = min(q.n, q.tid * run);
+    q.i1 = min(q.n, q.i0 + run);
     const bool idle = a.positions && a.positions[row] < 0;   // an empty slot of the batch: the same for the whole cluster
     const float T = a.temperature ? a.temperature[row] : 1.f;
     const float top_p = a.top_p ? a.top_p[row] : 1.f, min_pf = a.min_p ? a.min_p[row] : 0.f;
@@ -703,11 +723,11 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
         q.m = 0.f;
         __syncthreads();
     }
-    q.scale = SP_BINS_PER_UNIT / T;
+    q.scale = fminf(SP_BINS_PER_UNIT / T, 3e38f);
     q.md = (double)q.m;
     q.c64 = 92.33248261893449 / (double)T;   // 64 log2(e)
 
-    uint64_t cut = ~0ull - 1ull;   // the last place that stays
+    SampleCut cut = {-INFINITY, 0u};
     if (top_k > 0 && (uint32_t)top_k < a.vocab) {
         uint64_t mine[4], before, own;
         uint32_t bin;
@@ -717,7 +737,8 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
                 if (most > -INFINITY) add(q.bin(most), 1u);
             }, mine);
             if (sp_find(q, mine, (uint64_t)top_k, bin, before, own)) {
-                const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.bin(x) <= bin; });
+                const float to = sp_bin(bin).to;
+                const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.at(x) <= to; });
                 if (cnt <= SP_LIST) {
                     if (q.rank == 0u) sp_finish_list(q, a, row, cnt, (uint32_t)top_k, p, min_p, u);
                     return;
@@ -730,30 +751,34 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
         }, mine);
         const bool enough = sp_find(q, mine, (uint64_t)top_k, bin, before, own);
         if (enough && before + own <= SP_LIST) {
-            const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.bin(x) <= bin; });
+            const float to = sp_bin(bin).to;
+            const uint32_t cnt = q.gather([&](float x, uint32_t) { return x > -INFINITY && q.at(x) <= to; });
             if (q.rank == 0u) sp_finish_list(q, a, row, cnt, (uint32_t)top_k, p, min_p, u);
             return;
         }
-        if (enough) cut = sp_cut_by_rank(q, {bin, 0, 0}, before, own, (uint64_t)top_k);
+        if (enough) cut = sp_cut_by_rank(q, sp_bin(bin), before, own, (uint64_t)top_k);
     }
-    if (p < 1.0) cut = sp_cut_by_mass(q, cut, p);
+    SampleRegion g;
+    double run_front = 0;
+    if (p < 1.0) cut = sp_cut_by_mass(q, cut, p, g, run_front);
 
-    // The draw: every thread sums up a run of its own (of odd length, so that 32 of them lie in different banks), then the run that the
-    // goal falls into is looked at once more.
-    const bool all_stay = cut == ~0ull - 1ull;
-    const float cut_x = all_stay ? -INFINITY : sp_unkey(~(uint32_t)(cut >> 32));
-    const uint32_t cut_token = all_stay ? 0u : (uint32_t)cut;
-    // what is certainly below min_p need not be weighed: 32 bits with room to spare
+    // The draw: every thread sums up its run, then the run that the goal falls into is looked at once more.
+    // What is certainly below min_p need not be weighed: 32 bits with room to spare.
     const float sure = min_p > 0 ? q.m + 1.0001f * T * logf(min_pf) - 1e-5f * fabsf(q.m) : -INFINITY;
     auto weight = [&](uint32_t i) {
         const float x = q.x[i];
-        if (!(x > cut_x || (x == cut_x && q.base + i <= cut_token && !all_stay)) || x < sure) return 0.0;
+        if (!cut.stays(x, q.base + i) || x < sure) return 0.0;
         const double w = q.weight(x);
         return w >= min_p ? w : 0.0;
     };
-    const uint32_t run = (q.n + SP_THREADS - 1u) / SP_THREADS | 1u, i0 = min(q.n, q.tid * run), i1 = min(q.n, i0 + run);
     double mine = 0, before, own;
-    for (uint32_t i = i0; i < i1; ++i) mine += weight(i);
+    if (p < 1.0 && !(min_p > 0)) {   // the mass in front of the cut's region is known
+        mine = run_front;
+        for (uint32_t i = q.i0; i < q.i1; ++i)
+            if (cut.stays(q.x[i], q.base + i) && g.side(q, q.x[i], q.base + i) == 0) mine += q.weight(q.x[i]);
+    } else {
+        for (uint32_t i = q.i0; i < q.i1; ++i) mine += weight(i);
+    }
     q.block_scan(mine, before, own);
     const uint32_t half = q.turn++ & 1u;
     if (C > 1u) {
