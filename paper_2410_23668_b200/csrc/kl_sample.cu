@@ -124,6 +124,19 @@ struct Sampler {
     __device__ __forceinline__ float at(float v) const { return (m - v) * scale; }   // in bins; infinite where there is no token
     __device__ __forceinline__ uint32_t bin(float v) const { return (uint32_t)fminf(at(v), (float)(SP_BINS - 1)); }
 
+    // f(logit, place in the slice) for this thread's run
+    template <class F>
+    __device__ __forceinline__ void over_run(F&& f) const {
+        uint32_t i = i0;
+        for (; i + 8u <= i1; i += 8u) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = x[i + j];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f(v[j], i + j);
+        }
+        for (; i < i1; ++i) f(x[i], i);
+    }
     __device__ __forceinline__ double block_sum(double v) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -268,11 +281,12 @@ struct Sampler {
     }
     // The first cnt entries of the list in ascending order (first block; cnt <= SP_LIST, all different).
     __device__ __forceinline__ void sort_list(uint32_t cnt) {
-        if (cnt <= SP_THREADS) {   // every thread counts what comes before its own entry
-            const uint64_t own = tid < cnt ? s.list[tid] : ~0ull;
-            const uint32_t at = count_before(own, cnt);
+        if (cnt <= 2 * SP_THREADS) {   // every thread counts what comes before its own entries
+            const uint64_t own = tid < cnt ? s.list[tid] : ~0ull, second = tid + SP_THREADS < cnt ? s.list[tid + SP_THREADS] : ~0ull;
+            const uint32_t at = count_before(own, cnt), at2 = cnt > SP_THREADS ? count_before(second, cnt) : 0u;
             __syncthreads();
             if (tid < cnt) s.list[at] = own;
+            if (tid + SP_THREADS < cnt) s.list[at2] = second;
             __syncthreads();
             return;
         }
@@ -295,7 +309,7 @@ struct Sampler {
     }
     __device__ __forceinline__ uint32_t count_before(uint64_t own, uint32_t cnt) const {
         uint32_t at = 0;
-        if (warp * 32u < cnt) {
+        if (__any_sync(0xffffffffu, own != ~0ull)) {
 #pragma unroll 4
             for (uint32_t j = 0; j + 1u < cnt; j += 2u) {
                 const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&s.list[j]);
@@ -457,16 +471,15 @@ __device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut 
     for (;;) {
         double behind = 0;
         front = inside = 0;
-        for (uint32_t i = q.i0; i < q.i1; ++i) {
-            const float x = q.x[i];
-            if (!cut.stays(x, q.base + i)) continue;
+        q.over_run([&](float x, uint32_t i) {
+            if (!cut.stays(x, q.base + i)) return;
             const int side = g.side(q, x, q.base + i);
-            if (side > 0 && goal > 0) continue;
+            if (side > 0 && goal > 0) return;
             const double w = q.weight(x);
             if (side < 0) front += w;
             else if (side == 0) inside += w;
             else behind += w;
-        }
+        });
         run_front = front;
         double sum = front + inside + behind;
         q.cluster_sums(sum, front, inside);
@@ -597,7 +610,7 @@ __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, 
     for (uint32_t i = 0; i < PER; ++i) {
         const uint32_t at = q.tid * PER + i;
         const bool stays = at < cnt && (at == 0u || ((p >= 1.0 || ahead < p * mass) && w[i] >= min_p));
-        item[i] = stays ? (uint64_t)(uint32_t)s.list[at] << 32 | at : ~0ull;
+        item[i] = (uint64_t)(stays ? (uint32_t)s.list[at] : ~0u) << 32 | at;   // (what does not stay: behind all tokens)
         ahead += w[i];
     }
     __syncthreads();
@@ -616,7 +629,7 @@ __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, 
     for (uint32_t i = 0; i < PER; ++i) {
         const uint32_t at = q.tid * PER + i;
         item[i] = at < cnt ? s.list[at] : ~0ull;
-        w[i] = item[i] != ~0ull ? s.listw[(uint32_t)item[i]] : 0.0;
+        w[i] = item[i] >> 32 != 0xffffffffull ? s.listw[(uint32_t)item[i]] : 0.0;
         sum += w[i];
     }
     q.block_scan(sum, ahead, total);
@@ -764,20 +777,22 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
 
     // The draw: every thread sums up its run, then the run that the goal falls into is looked at once more.
     // What is certainly below min_p need not be weighed: 32 bits with room to spare.
-    const float sure = min_p > 0 ? q.m + 1.0001f * T * logf(min_pf) - 1e-5f * fabsf(q.m) : -INFINITY;
-    auto weight = [&](uint32_t i) {
-        const float x = q.x[i];
-        if (!cut.stays(x, q.base + i) || x < sure) return 0.0;
+    const float sure = min_p > 0 ? q.m + 1.0001f * T * logf(min_pf) - 1e-5f * fabsf(q.m) : -INFINITY, least = fmaxf(cut.x, sure);
+    auto weight = [&](float x, uint32_t i) {
+        if (!cut.stays(x, q.base + i)) return 0.0;
         const double w = q.weight(x);
         return w >= min_p ? w : 0.0;
     };
     double mine = 0, before, own;
     if (p < 1.0 && !(min_p > 0)) {   // the mass in front of the cut's region is known
         mine = run_front;
-        for (uint32_t i = q.i0; i < q.i1; ++i)
-            if (cut.stays(q.x[i], q.base + i) && g.side(q, q.x[i], q.base + i) == 0) mine += q.weight(q.x[i]);
+        q.over_run([&](float x, uint32_t i) {
+            if (x >= cut.x && cut.stays(x, q.base + i) && g.side(q, x, q.base + i) == 0) mine += q.weight(x);
+        });
     } else {
-        for (uint32_t i = q.i0; i < q.i1; ++i) mine += weight(i);
+        q.over_run([&](float x, uint32_t i) {
+            if (x >= least) mine += weight(x, i);
+        });
     }
     q.block_scan(mine, before, own);
     const uint32_t half = q.turn++ & 1u;
@@ -817,7 +832,7 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     uint32_t token = 0;
     double w_token = 1;
     for (uint32_t k = k0; k < k1; k += 32u) {
-        const double w = k + q.lane < k1 ? weight(k + q.lane) : 0.0;
+        const double w = k + q.lane < k1 ? weight(q.x[k + q.lane], k + q.lane) : 0.0;
         double incl = w;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
