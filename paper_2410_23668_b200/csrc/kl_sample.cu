@@ -245,19 +245,25 @@ struct Sampler {
         }
     }
 
-    // The tokens that `in` names, in any order, in the first block's list; returns how many there are (more than SP_LIST: some are
-    // missing), the same in every block.  Between two calls lies another exchange of the cluster.
-    template <class In>
-    __device__ __forceinline__ uint32_t gather(In&& in) {
+    // A list of tokens, in any order: every block's own (list_begin, then list_add), joined in the first block's by list_end, which returns
+    // how many there are in all (more than SP_LIST: some are missing).  Between two lists lies another exchange of the cluster.
+    __device__ __forceinline__ void list_begin() {
         if (tid == 0u) s.n_own = 0u;
         __syncthreads();
-#pragma unroll 4
-        for (uint32_t i = tid; i < n; i += SP_THREADS) {
-            const float v = x[i];
-            if (!in(v, base + i)) continue;
-            const uint32_t at = atomicAdd(&s.n_own, 1u);
-            if (at < SP_LIST) s.list[at] = sp_place(v, base + i);
-        }
+    }
+    __device__ __forceinline__ void list_add(float v, uint32_t token) {
+        const uint32_t at = atomicAdd(&s.n_own, 1u);
+        if (at < SP_LIST) s.list[at] = sp_place(v, token);
+    }
+    template <class In>
+    __device__ __forceinline__ uint32_t gather(In&& in) {   // those that `in` names
+        list_begin();
+        over_run([&](float v, uint32_t i) {
+            if (in(v, base + i)) list_add(v, base + i);
+        });
+        return list_end();
+    }
+    __device__ __forceinline__ uint32_t list_end() {
         if (C == 1u) {
             __syncthreads();
             return s.n_own;
@@ -436,8 +442,8 @@ __device__ __forceinline__ SampleCut sp_cut_by_rank(Sampler& q, SampleRegion g, 
 }
 
 // What stays of `cut` when those stay with less than p of its mass in front of them.  g: the region that the new cut falls into, run_front:
-// the mass of this thread's run that lies in front of it.
-__device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut cut, double p, SampleRegion& g, double& run_front) {
+// the mass of this thread's run that lies in front of it; hits: how many of the run belong to it, hit: the first of them.
+__device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut cut, double p, SampleRegion& g, double& run_front, uint32_t& hits, uint32_t& hit) {
     SampleShared& s = q.s;
     uint64_t mine[4], before, own;
     uint32_t bin;
@@ -454,7 +460,7 @@ __device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut 
     }, mine);
     uint64_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mine[i] = (uint64_t)((double)mine[i] * exp2((4 * q.tid + i) * (-1.4426950408889634 / SP_BINS_PER_UNIT) + 27.0));
+    for (int i = 0; i < 4; ++i) mine[i] = (uint64_t)((float)mine[i] * exp2f((4 * q.tid + i) * (-1.4426950408889634f / SP_BINS_PER_UNIT) + 27.f));
     {
         const double part = (double)(mine[0] + mine[1] + mine[2] + mine[3]);   // (rounded: approximate anyway)
         all = (uint64_t)q.block_sum(part);
@@ -469,16 +475,25 @@ __device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut 
     int went = 0;
     bool settled = false;
     for (;;) {
+        // the masses in front of the region, in it and behind it, and a list of its members
         double behind = 0;
         front = inside = 0;
+        hits = 0;
+        q.list_begin();
         q.over_run([&](float x, uint32_t i) {
             if (!cut.stays(x, q.base + i)) return;
             const int side = g.side(q, x, q.base + i);
             if (side > 0 && goal > 0) return;
             const double w = q.weight(x);
-            if (side < 0) front += w;
-            else if (side == 0) inside += w;
-            else behind += w;
+            if (side < 0) {
+                front += w;
+            } else if (side == 0) {
+                inside += w;
+                if (hits++ == 0u) hit = i;
+                q.list_add(x, q.base + i);
+            } else {
+                behind += w;
+            }
         });
         run_front = front;
         double sum = front + inside + behind;
@@ -495,9 +510,7 @@ __device__ __forceinline__ SampleCut sp_cut_by_mass(Sampler& q, const SampleCut 
             went = go;
             bin += go;
         } else {
-            const uint32_t cnt = q.gather([&](float x, uint32_t token) {
-                return cut.stays(x, token) && g.side(q, x, token) == 0;
-            });
+            const uint32_t cnt = q.list_end();
             if (cnt <= SP_LIST) {
                 uint64_t end = 0;
                 if (q.rank == 0u) {
@@ -652,7 +665,7 @@ __device__ __forceinline__ void sp_finish_list(Sampler& q, const SampleArgs& a, 
     }
 }
 
-__global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(SP_THREADS, 2) kl_sample_kernel(const SampleArgs a) {
     extern __shared__ __align__(16) uint8_t sp_smem[];
     SampleShared& s = *reinterpret_cast<SampleShared*>(sp_smem);
     const uint32_t C = cl_size(), row = blockIdx.x / C;
@@ -773,7 +786,8 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     }
     SampleRegion g;
     double run_front = 0;
-    if (p < 1.0) cut = sp_cut_by_mass(q, cut, p, g, run_front);
+    uint32_t hits = 0, hit = 0;
+    if (p < 1.0) cut = sp_cut_by_mass(q, cut, p, g, run_front, hits, hit);
 
     // The draw: every thread sums up its run, then the run that the goal falls into is looked at once more.
     // What is certainly below min_p need not be weighed: 32 bits with room to spare.
@@ -786,9 +800,13 @@ __global__ void __launch_bounds__(SP_THREADS) kl_sample_kernel(const SampleArgs 
     double mine = 0, before, own;
     if (p < 1.0 && !(min_p > 0)) {   // the mass in front of the cut's region is known
         mine = run_front;
-        q.over_run([&](float x, uint32_t i) {
-            if (x >= cut.x && cut.stays(x, q.base + i) && g.side(q, x, q.base + i) == 0) mine += q.weight(x);
-        });
+        if (hits == 1u) {
+            if (cut.stays(q.x[hit], q.base + hit)) mine += q.weight(q.x[hit]);
+        } else if (hits) {
+            q.over_run([&](float x, uint32_t i) {
+                if (x >= cut.x && cut.stays(x, q.base + i) && g.side(q, x, q.base + i) == 0) mine += q.weight(x);
+            });
+        }
     } else {
         q.over_run([&](float x, uint32_t i) {
             if (x >= least) mine += weight(x, i);
