@@ -553,10 +553,13 @@ __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, u
 }
 __device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.runs; }
 
-// First tile of block b's share of the list.
-__device__ __forceinline__ uint64_t ta_border(uint64_t work, uint32_t b, uint32_t blocks) {
-    return work / blocks * b + work % blocks * b / blocks;
-}
+// Equal shares of the list; border(b) is the first tile of block b's.
+struct TaShares {
+    uint64_t per;
+    uint32_t rest, blocks;
+    __device__ __forceinline__ TaShares(uint64_t work, uint32_t n) : per(pg_div(work, n)), blocks(n) { rest = (uint32_t)(work - per * n); }
+    __device__ __forceinline__ uint64_t border(uint32_t b) const { return per * b + rest * b / blocks; }   // (rest and b below TA_MAX_BLOCKS + 1)
+};
 
 // One block's share of the list, piece by piece.
 struct TaPiece {
@@ -748,7 +751,8 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
     __syncthreads();
     tm_fence_after();
     const uint32_t tmem = s.tmem;
-    const uint64_t g0 = ta_border(work, blockIdx.x, gridDim.x), g1 = ta_border(work, blockIdx.x + 1u, gridDim.x);
+    const TaShares shares(work, gridDim.x);
+    const uint64_t g0 = shares.border(blockIdx.x), g1 = shares.border(blockIdx.x + 1u);
     TaIter<NK, NW, UR> iter(c, a, pre, g0, g1 - g0);
     __syncthreads();   // the prefix sums have been read
     TaPiece p;
@@ -857,18 +861,28 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                             // every thread's arrival comes when its copies have
                             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
                         } else {   // values that some row must not see: what is no number becomes zero here
-                            for (uint32_t i = 0; i < STEPS; ++i) {
-                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
-                                const int64_t o = __shfl_sync(0xffffffffu, at, r);
-                                uint4 v = make_uint4(0, 0, 0, 0);
-                                if (o >= 0) v = *reinterpret_cast<const uint4*>(src + o + ch * 16u);
-                                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                            constexpr uint32_t Z = STEPS < 8u ? STEPS : 8u;   // pieces under way
+#pragma unroll 1
+                            for (uint32_t i0 = 0; i0 < STEPS; i0 += Z) {
+                                uint4 v[Z];
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u, bad = true;
-                                    if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu, bad = true;
+                                for (uint32_t z = 0; z < Z; ++z) {
+                                    const uint32_t e = (i0 + z) * 32u + lane;
+                                    const int64_t o = __shfl_sync(0xffffffffu, at, e / CH);
+                                    v[z] = make_uint4(0, 0, 0, 0);
+                                    if (o >= 0) v[z] = *reinterpret_cast<const uint4*>(src + o + e % CH * 16u);
                                 }
-                                ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                                for (uint32_t z = 0; z < Z; ++z) {
+                                    const uint32_t e = (i0 + z) * 32u + lane, ch = e % CH, row = pw * RPW + e / CH;
+                                    uint32_t w[4] = {v[z].x, v[z].y, v[z].z, v[z].w};
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) {
+                                        if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u, bad = true;
+                                        if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu, bad = true;
+                                    }
+                                    ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                                }
                             }
                             mbar_arrive(bar);
                         }
@@ -1222,26 +1236,26 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             const float unit = FP8 && ev_ref >= 0 ? ta_exp2((float)(ev_ref - 127) - TA_HEAD) : 1.f;   // of the values
             // the parts of a row: one reference, one sum
             const uint32_t me = grp * 128u + L, parts = p.two ? 1u : NG * p.split;
-            auto part = [&](uint32_t k) {   // thread that holds part k of row r (units of one run)
-                return k / p.split * 128u + k % p.split * R + r;
-            };
+            // (units of one run: thread g * 128 + j * R + r holds part (g, j) of row r)
             float mm = m, ll = l, f = 1.f;
             s.ml[0][me] = m;
             s.ml[1][me] = l;
             ta_named_sync(3u, NG * 128u);
             if (bad && me == 0u) s.bad[npiece % TA_RING] = 0u;
             if (parts > 1u) {
-                for (uint32_t k = 0; k < parts; ++k) mm = fmaxf(mm, s.ml[0][part(k)]);
+                for (uint32_t g = 0; g < NG * 128u; g += 128u)
+                    for (uint32_t j = r; j < 128u; j += R) mm = fmaxf(mm, s.ml[0][g + j]);
                 ll = 0.f;
-                for (uint32_t k = 0; k < parts; ++k) {
-                    const float mk = s.ml[0][part(k)];
-                    if (mk > -INFINITY) ll += s.ml[1][part(k)] * ta_exp2(mk - mm);
-                }
+                for (uint32_t g = 0; g < NG * 128u; g += 128u)
+                    for (uint32_t j = r; j < 128u; j += R) {
+                        const float mk = s.ml[0][g + j];
+                        if (mk > -INFINITY) ll += s.ml[1][g + j] * ta_exp2(mk - mm);
+                    }
                 f = m == -INFINITY ? 0.f : ta_exp2(m - mm);
             }
             const bool whole = p.slot == ~0u, valid = r < p.rows;
             const uint32_t gr = p.row0 + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
-            if (valid && (p.two || me == part(0u))) {
+            if (valid && (p.two || me == r)) {
                 if (whole) {
                     if (a.lse) a.lse[(size_t)(p.q.r0 + tok) * a.nq + head] = ll > 0.f || ll != ll ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
                 } else {
@@ -1251,7 +1265,10 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             const float g = (whole ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f) * f * unit;
             __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD;
             float* const rec = a.part + ((size_t)(whole ? 0u : p.slot) * TA_RECORD + r) * HD;
-            auto at16 = [](uint32_t thread, uint32_t j) { return thread * 16u + ((j / 4u ^ (thread >> 1 & 3u)) << 2); };   // (eight threads' four columns lie in all banks)
+            // (the exchange: 16 columns of a thread side by side, their fours exchanged so that eight threads' lie in all banks)
+            float* const xs = s.x + me * 16u;
+            const float* const xr = s.x + r * 16u;
+            const uint32_t turn = r >> 1 & 3u;   // of all parts of the row: R is a multiple of eight
             const uint32_t cols = parts > 4u ? 4u : 16u / parts, mine = p.two ? 0u : (grp * p.split + share) * cols;   // of a chunk of 16: what this thread writes of row r
 #pragma unroll 1
             for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
@@ -1295,18 +1312,20 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 }
                 ta_named_sync(3u, NG * 128u);   // the buffer's last readers are done
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(&s.x[at16(me, j)]) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(xs + ((j / 4 ^ turn) << 2)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                 ta_named_sync(3u, NG * 128u);
                 if (valid && mine < 16u) {
                     for (uint32_t j = mine; j < mine + cols; j += 4u) {
-                        float4 y = *reinterpret_cast<const float4*>(&s.x[at16(part(0u), j)]);
-                        for (uint32_t k = 1; k < parts; ++k) {
-                            const float4 z = *reinterpret_cast<const float4*>(&s.x[at16(part(k), j)]);
-                            y.x += z.x;
-                            y.y += z.y;
-                            y.z += z.z;
-                            y.w += z.w;
-                        }
+                        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (uint32_t g = 0; g < NG * 128u; g += 128u)
+#pragma unroll 4
+                            for (uint32_t k = 0; k < 128u; k += R) {
+                                const float4 z = *reinterpret_cast<const float4*>(xr + (g + k) * 16u + ((j / 4u ^ turn) << 2));
+                                y.x += z.x;
+                                y.y += z.y;
+                                y.z += z.z;
+                                y.w += z.w;
+                            }
                         if (whole) *reinterpret_cast<uint2*>(out + c0 + j) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
                         else *reinterpret_cast<float4*>(rec + c0 + j) = y;
                     }
@@ -1335,7 +1354,8 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
     if (pg_stopped(c)) return;
     const uint64_t work = pg_prefix<NW>(c.n_seqs, pre, wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK, UR>(c, a, i)); });
     const uint32_t b = blockIdx.x + 1u, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    const uint64_t g = ta_border(work, b, blocks);
+    const TaShares shares(work, blocks);
+    const uint64_t g = shares.border(b);
     if (g == 0u || g >= work) return;
     const uint32_t share = pg_find<NW>(pre, g), per = (c.n_seqs + NW * 32u - 1u) / (NW * 32u);
     uint32_t s = share * per;
@@ -1348,48 +1368,61 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
     }
     const uint64_t u = pg_div(off, q.tiles), begin = g - (off - u * q.tiles), end = begin + q.tiles;
     const uint32_t first = b - 1u, h = (uint32_t)pg_div(u, q.runs), run = (uint32_t)(u - (uint64_t)h * q.runs);
-    if (g == begin || ta_border(work, first, blocks) > begin) return;
-    const uint32_t first_slot = 2u * first + (ta_border(work, first, blocks) < begin ? 1u : 0u);
+    if (g == begin || shares.border(first) > begin) return;
+    const uint32_t first_slot = 2u * first + (shares.border(first) < begin ? 1u : 0u);
     uint32_t last = b;
-    while (last + 1u < blocks && ta_border(work, last + 1u, blocks) < end) ++last;
+    while (last + 1u < blocks && shares.border(last + 1u) < end) ++last;
     const uint32_t rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - (uint64_t)run * UR);
     for (uint32_t r = blockIdx.y * NW + warp; r < rows; r += gridDim.y * NW) {
         auto slot_of = [&](uint32_t k) { return k == first ? first_slot : 2u * k; };
-        auto holds = [&](uint32_t k) { return ta_border(work, k, blocks) < ta_border(work, k + 1u, blocks); };   // blocks without work left nothing
-        float m = -INFINITY;
-        for (uint32_t k = first + lane; k <= last; k += 32u)
-            if (holds(k)) m = fmaxf(m, a.part_ml[(size_t)slot_of(k) * TA_RECORD + r].x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float l = 0.f, sum[COLS];
+        auto holds = [&](uint32_t k) { return shares.border(k) < shares.border(k + 1u); };   // blocks without work left nothing
+        float m = -INFINITY, l = 0.f, sum[COLS];
 #pragma unroll
         for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
-        for (uint32_t k0 = first; k0 <= last; k0 += 32u) {
-            float w = 0.f, part = 0.f;
-            if (k0 + lane <= last && holds(k0 + lane)) {
-                const float2 ml = a.part_ml[(size_t)slot_of(k0 + lane) * TA_RECORD + r];
-                w = ml.x == -INFINITY ? 0.f : ta_exp2(ml.x - m);
-                part = ml.y;
-            }
-            const uint32_t n = min(32u, last - k0 + 1u);
-            for (uint32_t k = 0; k < n; ++k) {
-                const float wk = __shfl_sync(0xffffffffu, w, k), lk = __shfl_sync(0xffffffffu, part, k);
-                if (wk == 0.f) continue;   // (the same for the whole warp)
-                l += wk * lk;
-                const float* src = a.part + ((size_t)slot_of(k0 + k) * TA_RECORD + r) * HD + lane * COLS;
-                float x[COLS];
-                if constexpr (COLS == 2) {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
-                    x[0] = v.x; x[1] = v.y;
-                } else {
+        for (uint32_t k0 = first; k0 <= last; k0 += 32u) {   // 32 parts at a time, each lane with the reference and sum of one
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (k0 + lane <= last && holds(k0 + lane)) ml = a.part_ml[(size_t)slot_of(k0 + lane) * TA_RECORD + r];
+            float mx = fmaxf(m, ml.x);
 #pragma unroll
-                    for (int j = 0; j < COLS / 4; ++j) {
-                        const float4 v = reinterpret_cast<const float4*>(src)[j];
-                        x[4 * j] = v.x; x[4 * j + 1] = v.y; x[4 * j + 2] = v.z; x[4 * j + 3] = v.w;
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float old = m == -INFINITY ? 0.f : ta_exp2(m - mx), w = ml.x == -INFINITY ? 0.f : ta_exp2(ml.x - mx);
+            m = mx;
+            l *= old;
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) sum[j] *= old;
+            const float wl = w * ml.y;
+            uint32_t todo = __ballot_sync(0xffffffffu, w > 0.f);
+            while (todo) {   // four parts' loads under way
+                float x[4][COLS], wk[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    wk[z] = 0.f;
+                    const uint32_t k = todo ? __ffs(todo) - 1u : 0u;
+                    const float wz = __shfl_sync(0xffffffffu, w, k), lz = __shfl_sync(0xffffffffu, wl, k);
+                    if (!todo) {
+#pragma unroll
+                        for (int j = 0; j < COLS; ++j) x[z][j] = 0.f;
+                        continue;
+                    }
+                    todo &= todo - 1u;
+                    wk[z] = wz;
+                    l += lz;
+                    const float* src = a.part + ((size_t)slot_of(k0 + k) * TA_RECORD + r) * HD + lane * COLS;
+                    if constexpr (COLS == 2) {
+                        const float2 v = *reinterpret_cast<const float2*>(src);
+                        x[z][0] = v.x; x[z][1] = v.y;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < COLS / 4; ++j) {
+                            const float4 v = reinterpret_cast<const float4*>(src)[j];
+                            x[z][4 * j] = v.x; x[z][4 * j + 1] = v.y; x[z][4 * j + 2] = v.z; x[z][4 * j + 3] = v.w;
+                        }
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < COLS; ++j) sum[j] += wk * x[j];
+                for (int z = 0; z < 4; ++z)
+#pragma unroll
+                    for (int j = 0; j < COLS; ++j) sum[j] += wk[z] * x[z][j];
             }
         }
         const uint32_t gr = run * UR + r, tok = gr / a.G, head = h * a.G + gr - tok * a.G;
