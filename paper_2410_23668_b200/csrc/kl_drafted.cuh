@@ -381,7 +381,7 @@ struct TaShared {
     float qscale[4][2][128];                 // e4m3: what a row's queries were divided by; pieces in turn (scores run up to two short pieces ahead)
     uint8_t exps[TA_RING][2][128];
     uint64_t wsum[18];
-    float ml[2][256];
+    float ml[3][256];                        // reference, sum and unit of the values of every softmax thread
     uint64_t kv_full[8], kv_empty[8], exp_full[TA_RING], piece_end[TA_RING];
     uint64_t q_full, q_empty, qs_full[4], o_empty, end;
     uint64_t scores[2], probs[2], done[2];   // per stream: Q K^T has landed, P is written, P V has landed
@@ -1234,15 +1234,16 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             tm_fence_after();
             const bool bad = *(volatile uint32_t*)&s.bad[npiece % TA_RING] != 0u;
             const float unit = FP8 && ev_ref >= 0 ? ta_exp2((float)(ev_ref - 127) - TA_HEAD) : 1.f;   // of the values
-            // the parts of a row: one reference, one sum
-            const uint32_t me = grp * 128u + L, parts = p.two ? 1u : NG * p.split;
-            // (units of one run: thread g * 128 + j * R + r holds part (g, j) of row r)
-            float mm = m, ll = l, f = 1.f;
+            // the parts of a row: one reference, one sum (units of one run: thread g * 128 + j * R + r holds part (g, j) of row r)
+            const uint32_t me = grp * 128u + L;
+            float mm = m, ll = l;
             s.ml[0][me] = m;
             s.ml[1][me] = l;
+            s.ml[2][me] = unit;
             ta_named_sync(3u, NG * 128u);
             if (bad && me == 0u) s.bad[npiece % TA_RING] = 0u;
-            if (parts > 1u) {
+            if (!p.two) {
+                mm = -INFINITY;
                 for (uint32_t g = 0; g < NG * 128u; g += 128u)
                     for (uint32_t j = r; j < 128u; j += R) mm = fmaxf(mm, s.ml[0][g + j]);
                 ll = 0.f;
@@ -1251,7 +1252,6 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         const float mk = s.ml[0][g + j];
                         if (mk > -INFINITY) ll += s.ml[1][g + j] * ta_exp2(mk - mm);
                     }
-                f = m == -INFINITY ? 0.f : ta_exp2(m - mm);
             }
             const bool whole = p.slot == ~0u, valid = r < p.rows;
             const uint32_t gr = p.row0 + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
@@ -1262,21 +1262,44 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                     a.part_ml[(size_t)p.slot * TA_RECORD + r] = make_float2(mm, ll);
                 }
             }
-            const float g = (whole ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f) * f * unit;
+            const float norm = whole ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f;
             __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(a.out + (int64_t)(p.q.r0 + tok) * a.out_stride) + (size_t)head * HD;
             float* const rec = a.part + ((size_t)(whole ? 0u : p.slot) * TA_RECORD + r) * HD;
-            // (the exchange: 16 columns of a thread side by side, their fours exchanged so that eight threads' lie in all banks)
+            auto put = [&](uint32_t at, const float (&y)[8]) {
+                if (whole) pg_store8<__nv_bfloat16>(out + at, y);
+                else pg_store8<float>(rec + at, y);
+            };
+            // Units of one run: both groups' O of a lane can be read by either, so each takes half of the columns of both.
+            const bool pair = NG == 2 && !p.two, other = pair && p.t1 - p.t0 > 1u;   // (a single tile is the first group's)
+            float f[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t w = pair ? k * 128u + L : me;
+                f[k] = s.ml[0][w] == -INFINITY ? 0.f : ta_exp2(s.ml[0][w] - mm) * s.ml[2][w] * norm;
+            }
+            const uint32_t first_o = pair ? lane_base + Cfg::O_COL : o_at, c_end = pair ? (grp + 1u) * (HD / 2) : (uint32_t)HD;
+            // (the exchange between copies: 16 columns of a thread side by side, their fours exchanged so that eight threads' lie in all banks)
             float* const xs = s.x + me * 16u;
-            const float* const xr = s.x + r * 16u;
-            const uint32_t turn = r >> 1 & 3u;   // of all parts of the row: R is a multiple of eight
-            const uint32_t cols = parts > 4u ? 4u : 16u / parts, mine = p.two ? 0u : (grp * p.split + share) * cols;   // of a chunk of 16: what this thread writes of row r
+            const float* const xr = s.x + (grp * 128u + r) * 16u;
+            const uint32_t turn = r >> 1 & 3u;   // of all copies of the row: R is a multiple of eight
 #pragma unroll 1
-            for (uint32_t c0 = 0; c0 < (uint32_t)HD; c0 += 16u) {
+            for (uint32_t c0 = pair ? grp * (HD / 2) : 0u; c0 < c_end; c0 += 16u) {
                 uint32_t x[16];
-                tm_ld16(o_at + c0, x);
-                tm_ld_wait();
-                if (bad && valid && any) {   // values that are no numbers, for the rows that see them
-                    for (uint32_t t = first; t < p.t1; t += step) {
+                float o[16];
+                tm_ld16(first_o + c0, x);
+                if (other) {
+                    uint32_t y[16];
+                    tm_ld16(first_o + HD + c0, y);
+                    tm_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(x[j]) * f[0] + __uint_as_float(y[j]) * f[1];
+                } else {
+                    tm_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(x[j]) * f[0];
+                }
+                if (bad && valid) {   // values that are no numbers, for the rows that see them
+                    for (uint32_t t = p.t0; t < p.t1; ++t) {
                         const uint32_t pos = ta_tile_pos(p.q, t, NK);
                         if (!ta_mixed(a, p.q, pos, NK, INT32_MAX)) continue;
                         for (uint32_t k0 = col0; k0 < col1; k0 += 32u) {
@@ -1287,45 +1310,41 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                 const int32_t phys = pg_physical(c, iter.s, at / c.page);
                                 if (phys < 0) continue;
                                 const uint8_t* v = c.v + (int64_t)phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)(at % c.page) * c.row_b;
+#pragma unroll
                                 for (int j = 0; j < 16; ++j) {
                                     const uint32_t w = FP8 ? v[c0 + j] : reinterpret_cast<const uint16_t*>(v)[c0 + j];
-                                    if (FP8 ? (w & 0x7fu) == 0x7fu : (w & 0x7f80u) == 0x7f80u)
-                                        x[j] = __float_as_uint(__uint_as_float(x[j]) + (FP8 ? NAN : __uint_as_float(w << 16)));
+                                    if (FP8 ? (w & 0x7fu) == 0x7fu : (w & 0x7f80u) == 0x7f80u) o[j] += FP8 ? NAN : __uint_as_float(w << 16);
                                 }
                             }
                         }
                     }
                 }
-                float o[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = any ? __uint_as_float(x[j]) * g : 0.f;
-                if (p.two) {
+                if (p.two || p.split == 1u) {
                     if (valid) {
 #pragma unroll
                         for (int j = 0; j < 16; j += 8) {
                             const float y[8] = {o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]};
-                            if (whole) pg_store8<__nv_bfloat16>(out + c0 + j, y);
-                            else pg_store8<float>(rec + c0 + j, y);
+                            put(c0 + j, y);
                         }
                     }
                     continue;
                 }
-                ta_named_sync(3u, NG * 128u);   // the buffer's last readers are done
+                ta_named_sync(1u + grp, 128u);   // the buffer's last readers are done
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(xs + ((j / 4 ^ turn) << 2)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-                ta_named_sync(3u, NG * 128u);
-                if (valid && mine < 16u) {
-                    for (uint32_t j = mine; j < mine + cols; j += 4u) {
+                ta_named_sync(1u + grp, 128u);
+                if (valid) {
+                    const uint32_t cols = 16u / p.split;
+                    for (uint32_t j = share * cols; j < (share + 1u) * cols; j += 4u) {
                         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (uint32_t g = 0; g < NG * 128u; g += 128u)
 #pragma unroll 4
-                            for (uint32_t k = 0; k < 128u; k += R) {
-                                const float4 z = *reinterpret_cast<const float4*>(xr + (g + k) * 16u + ((j / 4u ^ turn) << 2));
-                                y.x += z.x;
-                                y.y += z.y;
-                                y.z += z.z;
-                                y.w += z.w;
-                            }
+                        for (uint32_t k = 0; k < 128u; k += R) {
+                            const float4 z = *reinterpret_cast<const float4*>(xr + k * 16u + ((j / 4u ^ turn) << 2));
+                            y.x += z.x;
+                            y.y += z.y;
+                            y.z += z.z;
+                            y.w += z.w;
+                        }
                         if (whole) *reinterpret_cast<uint2*>(out + c0 + j) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
                         else *reinterpret_cast<float4*>(rec + c0 + j) = y;
                     }
@@ -1370,7 +1389,9 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
     const uint32_t first = b - 1u, h = (uint32_t)pg_div(u, q.runs), run = (uint32_t)(u - (uint64_t)h * q.runs);
     if (g == begin || shares.border(first) > begin) return;
     const uint32_t first_slot = 2u * first + (shares.border(first) < begin ? 1u : 0u);
-    uint32_t last = b;
+    uint32_t last = min(blocks - 1u, (uint32_t)pg_div(end * blocks - 1u, (uint32_t)min(work, (uint64_t)0xffffffffu)));   // nearly: the last block whose share begins before the unit's end
+    last = max(last, b);
+    while (last > b && shares.border(last) >= end) --last;
     while (last + 1u < blocks && shares.border(last + 1u) < end) ++last;
     const uint32_t rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - (uint64_t)run * UR);
     for (uint32_t r = blockIdx.y * NW + warp; r < rows; r += gridDim.y * NW) {
