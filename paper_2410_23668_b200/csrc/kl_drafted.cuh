@@ -799,42 +799,57 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             // queries: row L of the first (second) 128 is row L % R (128 + L) of the unit
             if (npiece > 0u && !(ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status))) break;
             {
-                constexpr uint32_t QC = HD / 8;
-                const uint32_t R = p.R, pieces = (p.two ? 256u : 128u) * QC;
-#pragma unroll 4
-                for (uint32_t i = pw * 32u + lane; i < pieces; i += PW * 32u) {
-                    const uint32_t half = i / (128u * QC), L = i / QC % 128u, ch = i % QC, r = p.two ? half * 128u + L : L % R;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (r < p.rows) {
-                        const uint32_t gr = p.row0 + r, tok = gr / a.G, g = gr - tok * a.G;
-                        v = *reinterpret_cast<const uint4*>(a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + g) * HD + ch * 8u) * 2u);
-                    }
+                // PT threads to a row: its address is worked out once, and its pieces are under way together
+                constexpr uint32_t PT = PW * 32 / 128, QC = HD / 8 / PT, B = QC < 8u ? QC : 8u;
+                const uint32_t me = pw * 32u + lane, L = me / PT, ch0 = me % PT * QC;
+#pragma unroll 1
+                for (uint32_t half = 0; half < (p.two ? 2u : 1u); ++half) {
+                    const uint32_t r = p.two ? half * 128u + L : L & p.R - 1u, gr = p.row0 + r, tok = gr / a.G;
+                    const uint8_t* src = r < p.rows ? a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + gr - tok * a.G) * HD + ch0 * 8u) * 2u : nullptr;
+                    float inv = 1.f;
                     if constexpr (FP8) {   // as f16, divided by a power of two that brings the row's largest to 2^14 .. 2^15
-                        uint32_t w[4] = {v.x, v.y, v.z, v.w}, big = 0u;
+                        uint32_t big = 0u, odd = 0u;
+                        if (src)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) big = pg_larger(big, w[j]);
+                            for (uint32_t i = 0; i < QC; ++i) {
+                                const uint4 v = reinterpret_cast<const uint4*>(src)[i];
+                                big = pg_larger(pg_larger(big, v.x), pg_larger(v.y, pg_larger(v.z, v.w)));
+                                odd |= (v.x & 0x7f807f80u) + 0x00800080u | (v.y & 0x7f807f80u) + 0x00800080u | (v.z & 0x7f807f80u) + 0x00800080u | (v.w & 0x7f807f80u) + 0x00800080u;
+                            }
                         big = max(big & 0x7fffu, big >> 16 & 0x7fffu);
-                        if (((v.x & 0x7f807f80u) + 0x00800080u | (v.y & 0x7f807f80u) + 0x00800080u | (v.z & 0x7f807f80u) + 0x00800080u | (v.w & 0x7f807f80u) + 0x00800080u) & 0x80008000u)
-                            big = 0x7f80u;   // infinities and NaN stay what they are
+                        if (odd & 0x80008000u) big = 0x7f80u;   // infinities and NaN stay what they are
 #pragma unroll
-                        for (uint32_t o = QC / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                        for (uint32_t o = PT / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
                         const int e = (int)(big >> 7);   // 1 .. 254 for numbers that are not tiny
-                        const float inv = e == 255 || e == 0 ? 1.f : pg_scale((uint32_t)min(268 - e, 254));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const __half2 h = __floats2half2_rn(bf_lo(w[j]) * inv, bf_hi(w[j]) * inv);
-                            w[j] = *reinterpret_cast<const uint32_t*>(&h);
-                        }
-                        v = make_uint4(w[0], w[1], w[2], w[3]);
-                        if (ch == 0u) s.qscale[npiece & 3u][half][L] = 1.f / inv;
+                        if (e != 255 && e != 0) inv = pg_scale((uint32_t)min(268 - e, 254));
+                        if (ch0 == 0u) s.qscale[npiece & 3u][half][L] = 1.f / inv;
                     }
-                    ta_st16(q_s + half * Cfg::QBYTES + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v);
+#pragma unroll 1
+                    for (uint32_t i0 = 0; i0 < QC; i0 += B) {
+                        uint4 v[B];
+#pragma unroll
+                        for (uint32_t i = 0; i < B; ++i) v[i] = src ? reinterpret_cast<const uint4*>(src)[i0 + i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (uint32_t i = 0; i < B; ++i) {
+                            const uint32_t ch = ch0 + i0 + i;
+                            if constexpr (FP8) {
+                                uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const __half2 h = __floats2half2_rn(bf_lo(w[j]) * inv, bf_hi(w[j]) * inv);
+                                    w[j] = *reinterpret_cast<const uint32_t*>(&h);
+                                }
+                                v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                            ta_st16(q_s + half * Cfg::QBYTES + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v[i]);
+                        }
+                    }
                 }
                 ta_fence_async();
                 __syncwarp();
                 if (lane == 0u) {
                     mbar_arrive(smem_u32(&s.q_full));
-                    mbar_arrive(smem_u32(&s.qs_full[npiece & 3u]));
+                    if (FP8) mbar_arrive(smem_u32(&s.qs_full[npiece & 3u]));
                 }
             }
             const int64_t far = ta_far(a, p.q);
@@ -940,16 +955,17 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                             ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
                             ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
                         }
+                        // (the fence waits for loads as well: the next ones begin behind it)
+                        ta_fence_async();
+                        __syncwarp();
+                        if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
+                        next_slot();
                         if (kv == 0) {
                             request(c.k, kraw);
                             request_scales();
                         } else {
                             request(c.v, vraw);
                         }
-                        ta_fence_async();
-                        __syncwarp();
-                        if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
-                        next_slot();
                     }
                     ++ntile;
                 }
