@@ -793,65 +793,66 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             at = (int64_t)k.phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)k.off * c.row_b;
             if (FP8) ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
         };
+        // the unit's queries: row L of the first (second) 128 is row L % R (128 + L) of it
+        auto load_queries = [&]() {
+            if (npiece > 0u && !ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status)) return false;
+            // PT threads to a row: its address is worked out once, and its pieces are under way together
+            constexpr uint32_t PT = PW * 32 / 128, QC = HD / 8 / PT, B = FP8 ? 4u : 8u;
+            const uint32_t me = pw * 32u + lane, L = me / PT, ch0 = me % PT * QC;
+#pragma unroll 1
+            for (uint32_t half = 0; half < (p.two ? 2u : 1u); ++half) {
+                const uint32_t r = p.two ? half * 128u + L : L & p.R - 1u, gr = p.row0 + r, tok = gr / a.G;
+                const uint8_t* src = r < p.rows ? a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + gr - tok * a.G) * HD + ch0 * 8u) * 2u : nullptr;
+                float inv = 1.f;
+                if constexpr (FP8) {   // as f16, divided by a power of two that brings the row's largest to 2^14 .. 2^15
+                    uint32_t big = 0u, odd = 0u;
+                    if (src)
+#pragma unroll
+                        for (uint32_t i = 0; i < QC; ++i) {
+                            const uint4 v = reinterpret_cast<const uint4*>(src)[i];
+                            big = pg_larger(pg_larger(big, v.x), pg_larger(v.y, pg_larger(v.z, v.w)));
+                            odd |= (v.x & 0x7f807f80u) + 0x00800080u | (v.y & 0x7f807f80u) + 0x00800080u | (v.z & 0x7f807f80u) + 0x00800080u | (v.w & 0x7f807f80u) + 0x00800080u;
+                        }
+                    big = max(big & 0x7fffu, big >> 16 & 0x7fffu);
+                    if (odd & 0x80008000u) big = 0x7f80u;   // infinities and NaN stay what they are
+#pragma unroll
+                    for (uint32_t o = PT / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                    const int e = (int)(big >> 7);   // 1 .. 254 for numbers that are not tiny
+                    if (e != 255 && e != 0) inv = pg_scale((uint32_t)min(268 - e, 254));
+                    if (ch0 == 0u) s.qscale[npiece & 3u][half][L] = 1.f / inv;
+                }
+#pragma unroll 1
+                for (uint32_t i0 = 0; i0 < QC; i0 += B) {
+                    uint4 v[B];
+#pragma unroll
+                    for (uint32_t i = 0; i < B; ++i) v[i] = src ? reinterpret_cast<const uint4*>(src)[i0 + i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (uint32_t i = 0; i < B; ++i) {
+                        const uint32_t ch = ch0 + i0 + i;
+                        if constexpr (FP8) {
+                            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const __half2 h = __floats2half2_rn(bf_lo(w[j]) * inv, bf_hi(w[j]) * inv);
+                                w[j] = *reinterpret_cast<const uint32_t*>(&h);
+                            }
+                            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        ta_st16(q_s + half * Cfg::QBYTES + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v[i]);
+                    }
+                }
+            }
+            ta_fence_async();
+            __syncwarp();
+            if (lane == 0u) {
+                mbar_arrive(smem_u32(&s.q_full));
+                if (FP8) mbar_arrive(smem_u32(&s.qs_full[npiece & 3u]));
+            }
+            return true;
+        };
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
             Look next = look_up(p.t0);
-            // queries: row L of the first (second) 128 is row L % R (128 + L) of the unit
-            if (npiece > 0u && !(ok = ta_wait(&s.q_empty, (npiece - 1u) & 1u, s, c.status))) break;
-            {
-                // PT threads to a row: its address is worked out once, and its pieces are under way together
-                constexpr uint32_t PT = PW * 32 / 128, QC = HD / 8 / PT, B = QC < 8u ? QC : 8u;
-                const uint32_t me = pw * 32u + lane, L = me / PT, ch0 = me % PT * QC;
-#pragma unroll 1
-                for (uint32_t half = 0; half < (p.two ? 2u : 1u); ++half) {
-                    const uint32_t r = p.two ? half * 128u + L : L & p.R - 1u, gr = p.row0 + r, tok = gr / a.G;
-                    const uint8_t* src = r < p.rows ? a.q + (int64_t)(p.q.r0 + tok) * a.q_stride + ((size_t)(p.h * a.G + gr - tok * a.G) * HD + ch0 * 8u) * 2u : nullptr;
-                    float inv = 1.f;
-                    if constexpr (FP8) {   // as f16, divided by a power of two that brings the row's largest to 2^14 .. 2^15
-                        uint32_t big = 0u, odd = 0u;
-                        if (src)
-#pragma unroll
-                            for (uint32_t i = 0; i < QC; ++i) {
-                                const uint4 v = reinterpret_cast<const uint4*>(src)[i];
-                                big = pg_larger(pg_larger(big, v.x), pg_larger(v.y, pg_larger(v.z, v.w)));
-                                odd |= (v.x & 0x7f807f80u) + 0x00800080u | (v.y & 0x7f807f80u) + 0x00800080u | (v.z & 0x7f807f80u) + 0x00800080u | (v.w & 0x7f807f80u) + 0x00800080u;
-                            }
-                        big = max(big & 0x7fffu, big >> 16 & 0x7fffu);
-                        if (odd & 0x80008000u) big = 0x7f80u;   // infinities and NaN stay what they are
-#pragma unroll
-                        for (uint32_t o = PT / 2u; o > 0u; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-                        const int e = (int)(big >> 7);   // 1 .. 254 for numbers that are not tiny
-                        if (e != 255 && e != 0) inv = pg_scale((uint32_t)min(268 - e, 254));
-                        if (ch0 == 0u) s.qscale[npiece & 3u][half][L] = 1.f / inv;
-                    }
-#pragma unroll 1
-                    for (uint32_t i0 = 0; i0 < QC; i0 += B) {
-                        uint4 v[B];
-#pragma unroll
-                        for (uint32_t i = 0; i < B; ++i) v[i] = src ? reinterpret_cast<const uint4*>(src)[i0 + i] : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                        for (uint32_t i = 0; i < B; ++i) {
-                            const uint32_t ch = ch0 + i0 + i;
-                            if constexpr (FP8) {
-                                uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const __half2 h = __floats2half2_rn(bf_lo(w[j]) * inv, bf_hi(w[j]) * inv);
-                                    w[j] = *reinterpret_cast<const uint32_t*>(&h);
-                                }
-                                v[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                            ta_st16(q_s + half * Cfg::QBYTES + ch / 8u * (128u * 128u) + L * 128u + ((ch % 8u ^ (L & 7u)) << 4), v[i]);
-                        }
-                    }
-                }
-                ta_fence_async();
-                __syncwarp();
-                if (lane == 0u) {
-                    mbar_arrive(smem_u32(&s.q_full));
-                    if (FP8) mbar_arrive(smem_u32(&s.qs_full[npiece & 3u]));
-                }
-            }
             const int64_t far = ta_far(a, p.q);
             bool bad = false;
             if constexpr (!FP8) {
@@ -890,19 +891,26 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
 #pragma unroll
                                 for (uint32_t z = 0; z < Z; ++z) {
                                     const uint32_t e = (i0 + z) * 32u + lane, ch = e % CH, row = pw * RPW + e / CH;
-                                    uint32_t w[4] = {v[z].x, v[z].y, v[z].z, v[z].w};
+                                    auto odd = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };   // carries where an exponent is all ones
+                                    if ((odd(v[z].x) | odd(v[z].y) | odd(v[z].z) | odd(v[z].w)) & 0x80008000u) {
+                                        uint32_t w[4] = {v[z].x, v[z].y, v[z].z, v[z].w};
 #pragma unroll
-                                    for (int j = 0; j < 4; ++j) {
-                                        if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u, bad = true;
-                                        if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu, bad = true;
+                                        for (int j = 0; j < 4; ++j) {
+                                            if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+                                            if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0xffffu;
+                                        }
+                                        v[z] = make_uint4(w[0], w[1], w[2], w[3]);
+                                        bad = true;
                                     }
-                                    ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                                    ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), v[z]);
                                 }
                             }
                             mbar_arrive(bar);
                         }
                         next_slot();
                     }
+                    // (behind the first tile's copies, which are then under way)
+                    if (t == p.t0) ok = ok && load_queries();
                 }
             } else {
                 // The next tile's loads are under way while one is widened, and the pages of the one after are looked up.
@@ -929,6 +937,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 request(c.k, kraw);
                 request_scales();
                 request(c.v, vraw);
+                ok = load_queries();   // (while the first tile's loads are under way)
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
                     const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
                     // scale bytes; a row that nobody sees gets the smallest
