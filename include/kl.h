@@ -518,7 +518,9 @@ kl_status kl_paged_tree_workspace_bytes(const kl_paged_cache* cache, uint32_t n_
  * cached row is read once for every 128 (token, query head) pairs of its kv head.  What a token does not see has no part in its result,
  * whatever it holds; a token that sees an infinity or NaN gets no number in the columns it reaches.
  * Scores, the softmax and all sums are held in 32 bits; in the second product a probability takes part with 15 bits (KL_KV_BF16) or 11
- * (KL_KV_E4M3; fewer for positions whose probability times value scale is below 2^-24 of the largest value scale of the sequence). */
+ * (KL_KV_E4M3; fewer for positions whose probability times value scale is below 2^-24 of the largest value scale of the sequence, and
+ * for elements of a query below 2^-28 of its largest).  Every wait inside the kernels is bounded: should one run out, the status word becomes
+ * KL_ERR_SYNC_TIMEOUT and the call's results are undefined. */
 kl_status kl_paged_tree_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const int32_t* row_starts_d, uint32_t n_rows, const void* q_d,
                                   void* out_d, int q_type, int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale, uint32_t window,
                                   uint32_t n_sinks, const int32_t* row_positions_d, const uint32_t* mask_d, uint32_t mask_words, float* lse_d,

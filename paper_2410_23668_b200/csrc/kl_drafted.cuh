@@ -20,7 +20,7 @@ struct RotateArgs {
     uint32_t q_heads, q_groups;     // query heads of a block, blocks of a run of rows
 };
 
-constexpr int RT_THREADS = 256;
+constexpr int RT_MANY = 512, RT_FEW = 256;   // threads of a block: several rows of a sequence, one row of each
 constexpr int RT_ROWS = 16;   // rows whose angles a block holds at a time
 
 // Rounded to 32 bits towards zero, the last bit set where something was cut off: a number that rounds to any type of fewer bits
@@ -64,8 +64,8 @@ struct RtPiece {
 // (i, i + hd / 2) that turns together is in one lane's hands.  Cosines and sines of RT_ROWS rows are computed once for all heads.
 // Angles, cosines, sines and the two products of a key are held in 64 bits and the key is rounded once: a scale byte is a whole
 // number, and whether a key passes a border between two scales or codes is a comparison that 32 bits get wrong now and then.
-template <class T, int HD, bool FP8>
-__global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(const PagedView c, const PagedRows rows, const RotateArgs a) {
+template <class T, int HD, bool FP8, int RT_THREADS>
+__global__ void __launch_bounds__(RT_THREADS, 1) kl_paged_append_rotated_kernel(const PagedView c, const PagedRows rows, const RotateArgs a) {
     constexpr uint32_t LANES = HD / 16, GROUPS = RT_THREADS / LANES, HALF = HD / 2;
     extern __shared__ __align__(16) uint8_t rt_smem[];   // cosines and sines; at the end the groups' bounds
     __shared__ uint32_t found[4];
@@ -110,25 +110,36 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
         }
         __syncthreads();
         const uint32_t items = n * nh;
-        for (uint32_t it = grp; it < items; it += GROUPS) {
-            const uint32_t r = it / nh, h = h0 + it % nh;
-            if (!live_s[r]) continue;
-            const uint8_t* src = a.q + (int64_t)(row0 + r) * a.q_stride + ((size_t)h * HD + col) * sizeof(T);
-            T* dst = reinterpret_cast<T*>(a.q_out + (int64_t)(row0 + r) * a.q_out_stride) + (size_t)h * HD + col;
-            RtPiece<T> lo, hi;
-            lo.load(src);
-            hi.load(src + HALF * sizeof(T));
-            float x[8], y[8], u[8], v[8];
-            lo.get(x);
-            hi.get(y);
+        for (uint32_t it0 = grp; it0 < items; it0 += 2u * GROUPS) {   // two rows' loads under way
+            RtPiece<T> lo[2], hi[2];
+            uint32_t r[2];
+            T* dst[2];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float2 t = cs[r * HALF + col + q];
-                u[q] = x[q] * t.x - y[q] * t.y;
-                v[q] = y[q] * t.x + x[q] * t.y;
+            for (int z = 0; z < 2; ++z) {
+                const uint32_t it = it0 + z * GROUPS, h = h0 + it % nh;
+                r[z] = it / nh;
+                dst[z] = nullptr;
+                if (it >= items || !live_s[r[z]]) continue;
+                const uint8_t* src = a.q + (int64_t)(row0 + r[z]) * a.q_stride + ((size_t)h * HD + col) * sizeof(T);
+                dst[z] = reinterpret_cast<T*>(a.q_out + (int64_t)(row0 + r[z]) * a.q_out_stride) + (size_t)h * HD + col;
+                lo[z].load(src);
+                hi[z].load(src + HALF * sizeof(T));
             }
-            pg_store8<T>(dst, u);
-            pg_store8<T>(dst + HALF, v);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                if (!dst[z]) continue;
+                float x[8], y[8], u[8], v[8];
+                lo[z].get(x);
+                hi[z].get(y);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float2 t = cs[r[z] * HALF + col + q];
+                    u[q] = x[q] * t.x - y[q] * t.y;
+                    v[q] = y[q] * t.x + x[q] * t.y;
+                }
+                pg_store8<T>(dst[z], u);
+                pg_store8<T>(dst[z] + HALF, v);
+            }
         }
         return;
     }
@@ -233,6 +244,18 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
             }
         }
     };
+    // a row of keys and of values, requested while the angles (or the row before) are worked on
+    RtPiece<T> k0, k1, v0, v1;
+    const size_t hat = mine ? row_at : 0;
+    auto request = [&](uint32_t i) {
+        const uint8_t* ks = rows.k + (int64_t)(row0 + i) * rows.k_stride + hat;
+        const uint8_t* vs = rows.v + (int64_t)(row0 + i) * rows.v_stride + hat;
+        k0.load(ks);
+        k1.load(ks + HALF * sizeof(T));
+        v0.load(vs);
+        v1.load(vs + HALF * sizeof(T));
+    };
+    request(min(rs, cnt - 1u));
     double2* cs = reinterpret_cast<double2*>(rt_smem);   // [row][hd / 2]
     for (uint32_t c0 = 0; c0 < cnt; c0 += RT_ROWS) {
         const uint32_t n = min((uint32_t)RT_ROWS, cnt - c0);
@@ -248,14 +271,6 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
         for (uint32_t i0 = 0; i0 < n; i0 += slots) {   // every lane of a warp takes part in the shuffles
             const uint32_t r = min(i0 + rs, n - 1u), i = c0 + r;
             const bool keep = mine && i0 + rs < n;
-            const size_t hat = mine ? row_at : 0;
-            RtPiece<T> k0, k1, v0, v1;
-            const uint8_t* ks = rows.k + (int64_t)(row0 + i) * rows.k_stride + hat;
-            const uint8_t* vs = rows.v + (int64_t)(row0 + i) * rows.v_stride + hat;
-            k0.load(ks);
-            k1.load(ks + HALF * sizeof(T));
-            v0.load(vs);
-            v1.load(vs + HALF * sizeof(T));
             float x[8], y[8], w[16];
             k0.get(x);
             k1.get(y);
@@ -266,6 +281,10 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
                 w[q] = rt_sticky(fma(dx, t.x, -(dy * t.y)));
                 w[8 + q] = rt_sticky(fma(dy, t.x, dx * t.y));
             }
+            float vx[8], vy[8];
+            v0.get(vx);
+            v1.get(vy);
+            request(min(i0 + slots < n ? c0 + min(i0 + slots + rs, n - 1u) : c0 + RT_ROWS + rs, cnt - 1u));   // the next one
             put(w, kd, FP8 ? c.ke + exp_at : nullptr, i, keep);
             if (bounds && keep)
 #pragma unroll
@@ -273,12 +292,10 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
                     lo[q] = fminf(lo[q], w[q]);
                     hi[q] = fmaxf(hi[q], w[q]);
                 }
-            v0.get(x);
-            v1.get(y);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                w[q] = x[q];
-                w[8 + q] = y[q];
+                w[q] = vx[q];
+                w[8 + q] = vy[q];
             }
             put(w, vd, FP8 ? c.ve + exp_at : nullptr, i, keep);
         }
@@ -306,7 +323,7 @@ __global__ void __launch_bounds__(RT_THREADS) kl_paged_append_rotated_kernel(con
         bounds[t] = up ? __float2bfloat16_ru(x) : __float2bfloat16_rd(x);   // exact but for e4m3 rows of scale bytes 0 .. 2
     }
 }
-template <int HD>
+template <int HD, int RT_THREADS>
 constexpr size_t rt_smem_bytes() {
     return (size_t)RT_ROWS * (HD / 2) * 16 > (size_t)RT_THREADS / (HD / 16) * 2 * HD * 4 ? (size_t)RT_ROWS * (HD / 2) * 16
                                                                                         : (size_t)RT_THREADS / (HD / 16) * 2 * HD * 4;

@@ -68,7 +68,7 @@ def test_tree_attention(lib):
     for over in (dict(q=None), dict(o=None), dict(q=P + 8), dict(t=7), dict(qs=1020), dict(os=512), dict(scale=float("inf")), dict(scale=float("nan")), dict(mask=P),
                  dict(words=2), dict(mask=P, words=1 << 27), dict(ws=None), dict(ws=P + 16), dict(wb=1000)):
         assert tree_call(lib, cache(), seqs(), **over) == BAD, over
-    for over in (dict(nq=7), dict(nq=0), dict(nq=65536), dict(t=kl.KL_F32)):
+    for over in (dict(nq=7), dict(nq=0), dict(nq=65536), dict(t=kl.KL_F32), dict(n=1 << 29), dict(n=1 << 31)):
         assert tree_call(lib, cache(), seqs(), **over) == SHAPE, over
     b = C.c_size_t()
     assert lib.kl_paged_tree_workspace_bytes(C.byref(cache()), 7, C.byref(b)) == SHAPE and lib.kl_paged_tree_workspace_bytes(C.byref(cache()), 8, None) == BAD
