@@ -730,7 +730,6 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
     const uint32_t raw = smem_u32(ta_raw), q_s = (raw + 1023u) & ~1023u, ring_s = q_s + NG * Cfg::QBYTES;
     TaShared& s = *reinterpret_cast<TaShared*>(ta_raw + (ring_s - raw) + (size_t)NS * Cfg::SLOT);
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
-    griddep_launch();
     if (tid == 0u) {
         for (int i = 0; i < 8; ++i) {
             mbar_init(smem_u32(&s.kv_full[i]), FP8 ? PW : PW * 32);   // bf16: every producer thread's copies
@@ -753,8 +752,10 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         ta_fence_async();
     }
-    if (warp == (uint32_t)Cfg::QK_WARP) tm_alloc(smem_u32(&s.tmem), 512);
     griddep_wait();
+    // All of TMEM is taken only when the kernel before has left its own, and the next one may begin only once this block has it: either
+    // would otherwise wait for columns that the other holds while it waits for its end.
+    if (warp == (uint32_t)Cfg::QK_WARP) tm_alloc(smem_u32(&s.tmem), 512);
     if (a.row_starts && blockIdx.x == 0u) {
         for (uint32_t i = tid; i < c.n_seqs; i += NW * 32) {
             const int32_t x = a.row_starts[i], y = a.row_starts[i + 1u];
@@ -766,6 +767,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
     const bool stopped = pg_stopped(c);   // (a barrier of the whole block where there is a status word)
     const uint64_t work = stopped ? 0ull : pg_prefix<NW>(c.n_seqs, pre, s.wsum, [&](uint32_t i) { return ta_work(c, ta_seq<NK, UR>(c, a, i)); });
     __syncthreads();
+    griddep_launch();
     tm_fence_after();
     const uint32_t tmem = s.tmem;
     const TaShares shares(work, gridDim.x);
