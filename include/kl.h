@@ -488,7 +488,7 @@ kl_status kl_decode_step_paged(kl_handle* h, const int32_t* tokens_d, const int3
  * (freqs_d: fp64 [head_dim / 2], device; theta^(-2 i / head_dim) gives the rotation of kl_decode_step), position = row_positions_d
  * of its row, or where the row lies.
  *   q_d, q_out_d   [n_rows][n_q_heads][head_dim] of row_type, rows q_row_stride and q_out_row_stride elements apart (16-byte
- *                  alignment as above); both NULL: no queries; q_out_d == q_d with equal strides turns them in place
+ *                  alignment as above); both NULL: no queries; q_out_d == q_d with equal strides turns them in place (with others: refused)
  * Angles, and the products of a key, are held in 64 bits, and a key is rounded once, to what the cache holds; queries turn in 32
  * bits.  Values are written as they are.  Query rows that belong to no sequence or to an empty slot are left as they were.
  * Everything else is as in kl_paged_append. */

@@ -55,10 +55,7 @@ kl_status launch_tree(const PagedView& v, const TreeArgs& a, unsigned blocks, Pa
     return launch(kl_paged_tree_merge_kernel<HD, Cfg::NK, Cfg::NG * 128>, dim3(blocks - 1, 16), TA_MERGE_THREADS, 0, order, v, a, (uint32_t)blocks);
 }
 
-// Queries of new rows, or what takes their place in the output.
-kl_status check_row_queries(const kl_paged_cache* c, const void* q, int type, int64_t stride, uint32_t n_q_heads, uint32_t n_rows) {
-    return check_queries(c, q, type, stride, n_q_heads, n_rows);
-}
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 }  // namespace
 
@@ -72,10 +69,11 @@ kl_status kl_paged_append_rotated(const kl_paged_cache* cache, const kl_paged_se
     if ((rc = check_cache(cache, true)) != KL_OK || (rc = check_seqs(cache, seqs)) != KL_OK) return rc;
     if (seqs->n_seqs == 0 || n_rows == 0) return KL_OK;
     if ((rc = check_rows(cache, seqs, row_starts_d, n_rows, k_rows_d, v_rows_d, row_type, k_row_stride, v_row_stride)) != KL_OK) return rc;
-    if (!freqs_d || ((uintptr_t)freqs_d & 7u) || (q_d != nullptr) != (q_out_d != nullptr)) return KL_ERR_INVALID_ARG;
+    if (!freqs_d || ((uintptr_t)freqs_d & 7u) || !aligned4(row_starts_d) || !aligned4(row_positions_d) || (q_d != nullptr) != (q_out_d != nullptr)) return KL_ERR_INVALID_ARG;
+    if (q_d && q_d == q_out_d && n_rows > 1 && q_row_stride != q_out_row_stride) return KL_ERR_INVALID_ARG;   // a row would be written before it is read
     if (q_d) {
-        if ((rc = check_row_queries(cache, q_d, row_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
-        if ((rc = check_row_queries(cache, q_out_d, row_type, q_out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+        if ((rc = check_queries(cache, q_d, row_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+        if ((rc = check_queries(cache, q_out_d, row_type, q_out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
     }
     const int sms = sm_count();
     if (sms <= 0) return KL_ERR_CUDA;
@@ -131,9 +129,10 @@ kl_status kl_paged_tree_attention(const kl_paged_cache* cache, const kl_paged_se
     if (!row_starts_d && n_rows != seqs->n_seqs) return KL_ERR_INVALID_ARG;
     if (q_type != KL_F32 && q_type != KL_BF16) return KL_ERR_INVALID_ARG;
     if (q_type != KL_BF16 || n_rows > 0x7fffffffu) return KL_ERR_UNSUPPORTED_SHAPE;
-    if ((rc = check_row_queries(cache, q_d, q_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
-    if ((rc = check_row_queries(cache, out_d, q_type, out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+    if ((rc = check_queries(cache, q_d, q_type, q_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
+    if ((rc = check_queries(cache, out_d, q_type, out_row_stride, n_q_heads, n_rows)) != KL_OK) return rc;
     if ((uint64_t)n_rows * (n_q_heads / cache->n_kv_heads) > 0x7fffffffull) return KL_ERR_UNSUPPORTED_SHAPE;   // (token, head) pairs are counted in 32 bits
+    if (!aligned4(row_starts_d) || !aligned4(row_positions_d) || !aligned4(mask_d) || !aligned4(lse_d)) return KL_ERR_INVALID_ARG;
     if (!(scale < INFINITY) || (mask_d != nullptr) != (mask_words != 0) || mask_words > (1u << 26)) return KL_ERR_INVALID_ARG;
     const TreeSpace sp = tree_space(cache->head_dim);
     if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;

@@ -876,7 +876,10 @@ extern "C" kl_status kl_sample(const float* logits_d, int64_t row_stride, uint32
                                float* logprobs_d, int32_t* positions_d, void* stream) {
     if (n_rows == 0) return KL_OK;
     if (!logits_d || !uniforms_d || !tokens_d || vocab == 0) return KL_ERR_INVALID_ARG;
-    if (n_rows > 1 && (row_stride < (int64_t)vocab || row_stride > (INT64_MAX >> 34))) return KL_ERR_INVALID_ARG;
+    for (const void* x : {(const void*)logits_d, (const void*)uniforms_d, (const void*)temperature_d, (const void*)top_k_d, (const void*)top_p_d, (const void*)min_p_d,
+                          (const void*)tokens_d, (const void*)logprobs_d, (const void*)positions_d})
+        if ((uintptr_t)x & 3u) return KL_ERR_INVALID_ARG;
+    if (n_rows > 1 && (row_stride < (int64_t)vocab || row_stride > (INT64_MAX >> 27))) return KL_ERR_INVALID_ARG;   // 2^24 rows of it are counted in 64 bits of bytes
     if (vocab > SP_SLICE * SP_MAX_CLUSTER || n_rows > (1u << 24)) return KL_ERR_UNSUPPORTED_SHAPE;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return KL_ERR_CUDA;

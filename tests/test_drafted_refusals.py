@@ -91,3 +91,16 @@ def test_sample_binding():
     x, u, t = torch.zeros(2, 8), torch.zeros(2), torch.zeros(2, dtype=torch.int32)
     with pytest.raises(kl.KlError):   # not on a CUDA device
         kl.kl_sample(x, u, t)
+
+
+def test_numbers_that_are_not_aligned(lib):
+    c, s = C.byref(cache()), C.byref(seqs())
+    for starts, at in ((P + 2, None), (P, P + 1)):
+        assert lib.kl_paged_append_rotated(c, s, starts, 5, P, P, kl.KL_BF16, 256, 256, P, at, None, None, 0, 0, 0, None, None) == BAD
+    for starts, at, mask, lse in ((P + 1, None, None, None), (P, P + 2, None, None), (P, None, P + 2, None), (P, None, None, P + 3)):
+        assert lib.kl_paged_tree_attention(c, s, starts, 5, P, P, kl.KL_BF16, 1024, 1024, 8, 0.0, 0, 0, at, mask, 1 if mask else 0, lse, P, 1 << 30, None, None) == BAD
+    assert sample_call(lib, x=P + 2) == BAD and sample_call(lib, u=P + 1) == BAD and sample_call(lib, tokens=P + 3) == BAD
+
+
+def test_in_place_with_other_strides(lib):
+    assert rotate_call(lib, cache(), seqs(), q=P, qo=P, qs=1024, qos=2048) == BAD
