@@ -535,6 +535,14 @@ __device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b) {
     return r;
 }
 
+// Sixteen bytes, or zeros (no branch around the load).
+__device__ __forceinline__ uint4 ta_load_if(bool yes, const void* p) {
+    uint4 v;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((uint32_t)yes));
+    return v;
+}
+
 // A sequence of the call.
 struct TaSeq {
     uint32_t T, r0, base, len, lo;   // new tokens, their first row, cached positions, positions in all, first position of the window
@@ -789,28 +797,58 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 ++use;
             }
         };
-        // Row RPW * pw + lane of a tile (lanes below RPW): its page is asked for a tile or two ahead of its use.
-        struct Look { int32_t phys; uint32_t off; bool any; };
+        // Page sizes and tiles are multiples of four rows: rows 4 g .. 4 g + 3 of the warp's share of a tile lie in one page, which lane g asks
+        // for a tile or two ahead of its use.
+        constexpr uint32_t STEP_ROWS = 32 / CH;            // rows that the lanes' pieces of one step make up
+        const uint32_t reciprocal = 0xffffffffu / c.page + 1u;
+        const int32_t* table = nullptr;                    // of the piece's sequence
+        int64_t lane_at = 0;                               // of the lane's pieces, behind their rows' group
+        const uint32_t lane_row = lane / CH, lane_dst = lane % CH * (FP8 ? 2u : 1u) / 8u * (NK * 128u) + (pw * RPW + lane_row) * 128u +
+                                                        ((lane % CH * (FP8 ? 2u : 1u) % 8u ^ (lane_row & 7u)) << 4);
+        struct Look { int32_t phys; uint32_t x, off; };    // off == ~0: nothing to read
         auto look_up = [&](uint32_t t) {
-            Look k = {0, 0u, false};
-            const uint32_t x = ta_tile_pos(p.q, t, NK) + pw * RPW + lane;
-            if (t >= p.t1 || lane >= RPW || x >= p.q.len || (x < p.q.lo && x >= a.sinks)) return k;
-            const uint32_t lp = x / c.page;
+            Look k = {0, t < p.t1 ? ta_tile_pos(p.q, t, NK) + pw * RPW : 0u, ~0u};
+            const uint32_t x = k.x + 4u * lane;
+            if (t >= p.t1 || lane >= RPW / 4u || x >= p.q.len || (x + 3u < p.q.lo && x >= a.sinks)) return k;
+            uint32_t lp = __umulhi(x, reciprocal);         // x / page, or one more
+            if (lp * c.page > x) --lp;
             k.off = x - lp * c.page;
-            k.phys = lp < c.table_pages ? c.table[(int64_t)iter.s * c.table_stride + lp] : -1;
-            k.any = true;
+            k.phys = table[lp];
             return k;
         };
-        // where its 16-byte pieces (and its scale bytes) lie; -1: nothing to read
-        auto place = [&](const Look& k, int64_t& at, int64_t& ex) {
-            at = ex = -1;
-            if (!k.any) return;
-            if ((uint32_t)k.phys >= c.n_pages) {
-                pg_error(c);
-                return;
+        // Of a tile: where a lane's group lies in either pool (-1: nothing to read) and its scale bytes, with a mask of those that count.
+        int64_t base = -1, ex = 0;
+        uint32_t ex_mask = 0, first_x = 0;
+        bool inner = false, clean = false;                 // all of the warp's rows are to be read; and can be
+        auto read = [&](uint32_t x) { return x < p.q.len && (x >= p.q.lo || x < a.sinks); };
+        auto place = [&](const Look& k) {
+            base = -1;
+            ex_mask = 0u;
+            first_x = k.x;
+            inner = k.x >= p.q.lo && k.x + RPW <= p.q.len;
+            if (k.off != ~0u) {
+                if ((uint32_t)k.phys >= c.n_pages) {
+                    pg_error(c);
+                } else {
+                    base = (int64_t)k.phys * c.page_b + (int64_t)k.off * c.row_b;
+                    if (FP8) {
+                        ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
+                        ex_mask = ~0u;
+                        if (!inner)
+#pragma unroll
+                            for (uint32_t j = 0; j < 4u; ++j)
+                                if (!read(k.x + 4u * lane + j)) ex_mask &= ~(0xffu << 8 * j);
+                    }
+                }
             }
-            at = (int64_t)k.phys * c.page_b + (int64_t)p.h * c.head_b + (int64_t)k.off * c.row_b;
-            if (FP8) ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
+            clean = inner && __all_sync(0xffffffffu, lane >= RPW / 4u || base >= 0);
+        };
+        auto offset = [&](uint32_t i, bool all) {          // of the lane's piece of step i (-1: nothing to read)
+            const int64_t o = __shfl_sync(0xffffffffu, base, STEP_ROWS <= 4u ? i * STEP_ROWS / 4u : i * (STEP_ROWS / 4u) + lane_row / 4u);
+            const int64_t to = o + lane_at + (i * STEP_ROWS & 3u ? (int64_t)(i * STEP_ROWS & 3u) * c.row_b : 0);
+            if (all) return to;
+            const uint32_t x = first_x + i * STEP_ROWS + lane_row;
+            return (o >= 0) & (x < p.q.len) & ((x >= p.q.lo) | (x < a.sinks)) ? to : (int64_t)-1;
         };
         // the unit's queries: row L of the first (second) 128 is row L % R (128 + L) of it
         auto load_queries = [&]() {
@@ -861,7 +899,6 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                     }
                 }
             }
-            ta_fence_async();
             __syncwarp();
             if (lane == 0u) {
                 mbar_arrive(smem_u32(&s.q_full));
@@ -871,45 +908,47 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         };
         bool ok = true;
         while (ok && iter.next(c, a, p)) {
+            table = c.table + (int64_t)iter.s * c.table_stride;
+            lane_at = (int64_t)p.h * c.head_b + (int64_t)(lane_row & 3u) * c.row_b + lane % CH * 16u;
             Look next = look_up(p.t0);
             const int64_t far = ta_far(a, p.q);
             bool bad = false;
             if constexpr (!FP8) {
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
                     const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
-                    int64_t at, ex;
-                    place(next, at, ex);
+                    place(next);
                     next = look_up(t + 1u);
 #pragma unroll 1
                     for (int kv = 0; ok && kv < 2; ++kv) {
                         ok = take_slot();
                         if (!ok) break;
-                        const uint32_t dst = ring_s + slot * Cfg::SLOT, bar = smem_u32(&s.kv_full[slot]);
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT + lane_dst, bar = smem_u32(&s.kv_full[slot]);
                         const uint8_t* src = kv ? c.v : c.k;
                         if (kv == 0 || !mixed) {
+                            if (clean) {
+#pragma unroll
+                                for (uint32_t i = 0; i < STEPS; ++i) ta_cp16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, src + offset(i, true), 16u);
+                            } else
 #pragma unroll
                             for (uint32_t i = 0; i < STEPS; ++i) {
-                                const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH, row = pw * RPW + r;
-                                const int64_t o = __shfl_sync(0xffffffffu, at, r);
-                                ta_cp16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), src + (o < 0 ? 0 : o + ch * 16u), o < 0 ? 0u : 16u);
+                                const int64_t o = offset(i, false);
+                                ta_cp16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, src + (o < 0 ? 0 : o), o < 0 ? 0u : 16u);
                             }
                             // every thread's arrival comes when its copies have
                             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
                         } else {   // values that some row must not see: what is no number becomes zero here
                             constexpr uint32_t Z = STEPS < 8u ? STEPS : 8u;   // pieces under way
-#pragma unroll 1
+#pragma unroll
                             for (uint32_t i0 = 0; i0 < STEPS; i0 += Z) {
                                 uint4 v[Z];
 #pragma unroll
                                 for (uint32_t z = 0; z < Z; ++z) {
-                                    const uint32_t e = (i0 + z) * 32u + lane;
-                                    const int64_t o = __shfl_sync(0xffffffffu, at, e / CH);
-                                    v[z] = make_uint4(0, 0, 0, 0);
-                                    if (o >= 0) v[z] = *reinterpret_cast<const uint4*>(src + o + e % CH * 16u);
+                                    const int64_t o = offset(i0 + z, false);
+                                    v[z] = ta_load_if(o >= 0, src + o);
                                 }
 #pragma unroll
                                 for (uint32_t z = 0; z < Z; ++z) {
-                                    const uint32_t e = (i0 + z) * 32u + lane, ch = e % CH, row = pw * RPW + e / CH;
+                                    const uint32_t i = i0 + z;
                                     auto odd = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };   // carries where an exponent is all ones
                                     if ((odd(v[z].x) | odd(v[z].y) | odd(v[z].z) | odd(v[z].w)) & 0x80008000u) {
                                         uint32_t w[4] = {v[z].x, v[z].y, v[z].z, v[z].w};
@@ -921,7 +960,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                         v[z] = make_uint4(w[0], w[1], w[2], w[3]);
                                         bad = true;
                                     }
-                                    ta_st16(dst + ch / 8u * (NK * 128u) + row * 128u + ((ch % 8u ^ (row & 7u)) << 4), v[z]);
+                                    ta_st16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, v[z]);
                                 }
                             }
                             mbar_arrive(bar);
@@ -935,23 +974,24 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 // The next tile's loads are under way while one is widened, and the pages of the one after are looked up.
                 uint4 kraw[STEPS], vraw[STEPS];
                 uint32_t ke = 0, ve = 0;
-                int64_t at, ex;
+                int64_t at[STEPS];
+                auto place_all = [&](const Look& k) {
+                    place(k);
+#pragma unroll
+                    for (uint32_t i = 0; i < STEPS; ++i) at[i] = offset(i, clean);
+                };
                 auto request = [&](const uint8_t* src, uint4 (&to)[STEPS]) {
 #pragma unroll
-                    for (uint32_t i = 0; i < STEPS; ++i) {
-                        const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH;
-                        const int64_t o = __shfl_sync(0xffffffffu, at, r);
-                        to[i] = o >= 0 ? *reinterpret_cast<const uint4*>(src + o + ch * 16u) : make_uint4(0, 0, 0, 0);
-                    }
+                    for (uint32_t i = 0; i < STEPS; ++i) to[i] = ta_load_if(at[i] >= 0, src + at[i]);
                 };
-                auto request_scales = [&]() {
+                auto request_scales = [&]() {   // of four rows; a row that nobody sees gets the smallest
                     ke = ve = 0;
-                    if (ex >= 0) {
-                        ke = c.ke[ex];
-                        ve = c.ve[ex];
+                    if (ex_mask) {
+                        ke = *reinterpret_cast<const uint32_t*>(c.ke + ex);
+                        ve = *reinterpret_cast<const uint32_t*>(c.ve + ex);
                     }
                 };
-                place(next, at, ex);
+                place_all(next);
                 next = look_up(p.t0 + 1u);
                 request(c.k, kraw);
                 request_scales();
@@ -959,32 +999,27 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 ok = load_queries();   // (while the first tile's loads are under way)
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
                     const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
-                    // scale bytes; a row that nobody sees gets the smallest
-                    if (lane < RPW) {
-                        s.exps[ntile % TA_RING][0][pw * RPW + lane] = (uint8_t)ke;
-                        s.exps[ntile % TA_RING][1][pw * RPW + lane] = (uint8_t)ve;
+                    if (lane < RPW / 4u) {
+                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][0][pw * RPW + 4u * lane]) = ke & ex_mask;
+                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][1][pw * RPW + 4u * lane]) = ve & ex_mask;
                     }
                     __syncwarp();
                     if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
-                    place(next, at, ex);   // of tile t + 1
+                    place_all(next);   // of tile t + 1
                     next = look_up(t + 2u);
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         ok = ok && take_slot();
                         if (!ok) break;
-                        const uint32_t dst = ring_s + slot * Cfg::SLOT;
+                        const uint32_t dst = ring_s + slot * Cfg::SLOT + lane_dst;
 #pragma unroll
                         for (uint32_t i = 0; i < STEPS; ++i) {
-                            const uint32_t e = i * 32u + lane, r = e / CH, ch = e % CH * 2u, row = pw * RPW + r;
                             uint4 w[2];
                             if (kv == 0) ta_widen(kraw[i], w, false);
                             else bad |= ta_widen(vraw[i], w, mixed);
-                            const uint32_t d = dst + ch / 8u * (NK * 128u) + row * 128u;
-                            ta_st16(d + ((ch % 8u ^ (row & 7u)) << 4), w[0]);
-                            ta_st16(d + (((ch + 1u) % 8u ^ (row & 7u)) << 4), w[1]);
+                            ta_st16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, w[0]);
+                            ta_st16((dst ^ (i * STEP_ROWS & 7u) << 4 ^ 16u) + i * STEP_ROWS * 128u, w[1]);
                         }
-                        // (the fence waits for loads as well: the next ones begin behind it)
-                        ta_fence_async();
                         __syncwarp();
                         if (lane == 0u) mbar_arrive(smem_u32(&s.kv_full[slot]));
                         next_slot();
@@ -1012,12 +1047,13 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
         bool ok = true;
         auto landed = [&](uint32_t n) {   // slot of the ring that is the n-th to be filled
             if (!ta_wait(&s.kv_full[n % NS], n / NS & 1u, s, c.status)) return false;
-            if (!FP8) ta_fence_async();   // the copies behind the barrier were the threads' own, not the copy engine's
+            ta_fence_async();   // what the barrier tells of was written by threads (who do not fence themselves: it would wait for their next loads)
             return true;
         };
         if (warp == (uint32_t)Cfg::QK_WARP) {
             while (ok && iter.next(c, a, p)) {
                 ok = ta_wait(&s.q_full, npiece & 1u, s, c.status);
+                ta_fence_async();
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t, ++tile) {
                     if (!(ok = landed(2u * tile))) break;
                     const uint32_t sl = 2u * tile % NS, b0 = p.two ? 0u : t - p.t0 & 1u, b1 = p.two ? 1u : b0;
