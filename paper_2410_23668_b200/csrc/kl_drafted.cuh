@@ -797,9 +797,11 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 ++use;
             }
         };
-        // Page sizes and tiles are multiples of four rows: rows 4 g .. 4 g + 3 of the warp's share of a tile lie in one page, which lane g asks
-        // for a tile or two ahead of its use.
+        // Page sizes and tiles are multiples of four rows: rows 4 g .. 4 g + 3 of the warp's share of a tile lie in one page.  The warp looks up
+        // a chunk of CT tiles at a time, lane j GPT + g the page of group g of the chunk's tile j, and asks for the next chunk's pages
+        // when it begins with one.
         constexpr uint32_t STEP_ROWS = 32 / CH;            // rows that the lanes' pieces of one step make up
+        constexpr uint32_t GPT = RPW / 4, CT = 32 / GPT;   // groups of a tile, tiles of a chunk
         const uint32_t reciprocal = 0xffffffffu / c.page + 1u;
         const int32_t* table = nullptr;                    // of the piece's sequence
         int64_t lane_at = 0;                               // of the lane's pieces, behind their rows' group
@@ -807,48 +809,46 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                                         ((lane % CH * (FP8 ? 2u : 1u) % 8u ^ (lane_row & 7u)) << 4);
         struct Look { int32_t phys; uint32_t x, off; };    // off == ~0: nothing to read
         auto look_up = [&](uint32_t t) {
-            Look k = {0, t < p.t1 ? ta_tile_pos(p.q, t, NK) + pw * RPW : 0u, ~0u};
-            const uint32_t x = k.x + 4u * lane;
-            if (t >= p.t1 || lane >= RPW / 4u || x >= p.q.len || (x + 3u < p.q.lo && x >= a.sinks)) return k;
-            uint32_t lp = __umulhi(x, reciprocal);         // x / page, or one more
-            if (lp * c.page > x) --lp;
-            k.off = x - lp * c.page;
+            t += lane / GPT;
+            Look k = {0, 0u, ~0u};
+            if (t >= p.t1) return k;
+            k.x = ta_tile_pos(p.q, t, NK) + pw * RPW + 4u * (lane % GPT);
+            if (k.x >= p.q.len || (k.x + 3u < p.q.lo && k.x >= a.sinks)) return k;
+            uint32_t lp = __umulhi(k.x, reciprocal);       // x / page, or one more
+            if (lp * c.page > k.x) --lp;
+            k.off = k.x - lp * c.page;
             k.phys = table[lp];
             return k;
         };
-        // Of a tile: where a lane's group lies in either pool (-1: nothing to read) and its scale bytes, with a mask of those that count.
+        // Of the chunk: where a lane's group lies in either pool (-1: nothing to read) and its scale bytes, with a mask of those that count;
+        // groups all of whose rows are read.
         int64_t base = -1, ex = 0;
-        uint32_t ex_mask = 0, first_x = 0;
-        bool inner = false, clean = false;                 // all of the warp's rows are to be read; and can be
+        uint32_t ex_mask = 0, clean = 0;
         auto read = [&](uint32_t x) { return x < p.q.len && (x >= p.q.lo || x < a.sinks); };
         auto place = [&](const Look& k) {
             base = -1;
             ex_mask = 0u;
-            first_x = k.x;
-            inner = k.x >= p.q.lo && k.x + RPW <= p.q.len;
             if (k.off != ~0u) {
                 if ((uint32_t)k.phys >= c.n_pages) {
                     pg_error(c);
                 } else {
                     base = (int64_t)k.phys * c.page_b + (int64_t)k.off * c.row_b;
-                    if (FP8) {
-                        ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
-                        ex_mask = ~0u;
-                        if (!inner)
+                    if (FP8) ex = ((int64_t)k.phys * c.nkv + p.h) * c.page + k.off;
 #pragma unroll
-                            for (uint32_t j = 0; j < 4u; ++j)
-                                if (!read(k.x + 4u * lane + j)) ex_mask &= ~(0xffu << 8 * j);
-                    }
+                    for (uint32_t j = 0; j < 4u; ++j)
+                        if (read(k.x + j)) ex_mask |= 0xffu << 8 * j;
                 }
             }
-            clean = inner && __all_sync(0xffffffffu, lane >= RPW / 4u || base >= 0);
+            clean = __ballot_sync(0xffffffffu, ex_mask == ~0u);
         };
-        auto offset = [&](uint32_t i, bool all) {          // of the lane's piece of step i (-1: nothing to read)
-            const int64_t o = __shfl_sync(0xffffffffu, base, STEP_ROWS <= 4u ? i * STEP_ROWS / 4u : i * (STEP_ROWS / 4u) + lane_row / 4u);
+        auto all_of = [&](uint32_t j) { return (clean >> j * GPT & (GPT == 32u ? ~0u : (1u << GPT % 32u) - 1u)) == (GPT == 32u ? ~0u : (1u << GPT % 32u) - 1u); };
+        // Of the lane's piece of step i of the chunk's tile j, which begins at position x (-1: nothing to read).
+        auto offset = [&](uint32_t i, uint32_t j, bool all, uint32_t x) {
+            const int64_t o = __shfl_sync(0xffffffffu, base, j * GPT + (STEP_ROWS <= 4u ? i * STEP_ROWS / 4u : i * (STEP_ROWS / 4u) + lane_row / 4u));
             const int64_t to = o + lane_at + (i * STEP_ROWS & 3u ? (int64_t)(i * STEP_ROWS & 3u) * c.row_b : 0);
             if (all) return to;
-            const uint32_t x = first_x + i * STEP_ROWS + lane_row;
-            return (o >= 0) & (x < p.q.len) & ((x >= p.q.lo) | (x < a.sinks)) ? to : (int64_t)-1;
+            const uint32_t at = x + pw * RPW + i * STEP_ROWS + lane_row;
+            return (o >= 0) & (at < p.q.len) & ((at >= p.q.lo) | (at < a.sinks)) ? to : (int64_t)-1;
         };
         // the unit's queries: row L of the first (second) 128 is row L % R (128 + L) of it
         auto load_queries = [&]() {
@@ -912,12 +912,19 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             lane_at = (int64_t)p.h * c.head_b + (int64_t)(lane_row & 3u) * c.row_b + lane % CH * 16u;
             Look next = look_up(p.t0);
             const int64_t far = ta_far(a, p.q);
+            place(next);
+            next = look_up(p.t0 + CT);
+            uint32_t j = 0;   // tile of the chunk
             bool bad = false;
             if constexpr (!FP8) {
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
-                    const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
-                    place(next);
-                    next = look_up(t + 1u);
+                    if (j == CT) {
+                        place(next);
+                        next = look_up(t + CT);
+                        j = 0;
+                    }
+                    const uint32_t x = ta_tile_pos(p.q, t, NK);
+                    const bool mixed = ta_mixed(a, p.q, x, NK, far), all = all_of(j);
 #pragma unroll 1
                     for (int kv = 0; ok && kv < 2; ++kv) {
                         ok = take_slot();
@@ -925,13 +932,13 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         const uint32_t dst = ring_s + slot * Cfg::SLOT + lane_dst, bar = smem_u32(&s.kv_full[slot]);
                         const uint8_t* src = kv ? c.v : c.k;
                         if (kv == 0 || !mixed) {
-                            if (clean) {
+                            if (all) {
 #pragma unroll
-                                for (uint32_t i = 0; i < STEPS; ++i) ta_cp16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, src + offset(i, true), 16u);
+                                for (uint32_t i = 0; i < STEPS; ++i) ta_cp16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, src + offset(i, j, true, x), 16u);
                             } else
 #pragma unroll
                             for (uint32_t i = 0; i < STEPS; ++i) {
-                                const int64_t o = offset(i, false);
+                                const int64_t o = offset(i, j, false, x);
                                 ta_cp16((dst ^ (i * STEP_ROWS & 7u) << 4) + i * STEP_ROWS * 128u, src + (o < 0 ? 0 : o), o < 0 ? 0u : 16u);
                             }
                             // every thread's arrival comes when its copies have
@@ -943,7 +950,7 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                                 uint4 v[Z];
 #pragma unroll
                                 for (uint32_t z = 0; z < Z; ++z) {
-                                    const int64_t o = offset(i0 + z, false);
+                                    const int64_t o = offset(i0 + z, j, false, x);
                                     v[z] = ta_load_if(o >= 0, src + o);
                                 }
 #pragma unroll
@@ -967,18 +974,20 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         }
                         next_slot();
                     }
+                    ++j;
                     // (behind the first tile's copies, which are then under way)
                     if (t == p.t0) ok = ok && load_queries();
                 }
             } else {
-                // The next tile's loads are under way while one is widened, and the pages of the one after are looked up.
+                // The next tile's loads are under way while one is widened.
                 uint4 kraw[STEPS], vraw[STEPS];
                 uint32_t ke = 0, ve = 0;
                 int64_t at[STEPS];
-                auto place_all = [&](const Look& k) {
-                    place(k);
+                auto aim = [&](uint32_t t) {
+                    const bool all = all_of(j);
+                    const uint32_t x = t < p.t1 ? ta_tile_pos(p.q, t, NK) : 0u;
 #pragma unroll
-                    for (uint32_t i = 0; i < STEPS; ++i) at[i] = offset(i, clean);
+                    for (uint32_t i = 0; i < STEPS; ++i) at[i] = offset(i, j, all, x);
                 };
                 auto request = [&](const uint8_t* src, uint4 (&to)[STEPS]) {
 #pragma unroll
@@ -991,22 +1000,26 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         ve = *reinterpret_cast<const uint32_t*>(c.ve + ex);
                     }
                 };
-                place_all(next);
-                next = look_up(p.t0 + 1u);
+                aim(p.t0);
                 request(c.k, kraw);
                 request_scales();
                 request(c.v, vraw);
                 ok = load_queries();   // (while the first tile's loads are under way)
                 for (uint32_t t = p.t0; ok && t < p.t1; ++t) {
                     const bool mixed = ta_mixed(a, p.q, ta_tile_pos(p.q, t, NK), NK, far);
-                    if (lane < RPW / 4u) {
-                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][0][pw * RPW + 4u * lane]) = ke & ex_mask;
-                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][1][pw * RPW + 4u * lane]) = ve & ex_mask;
+                    if (lane / GPT == j) {
+                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][0][pw * RPW + lane % GPT * 4u]) = ke & ex_mask;
+                        *reinterpret_cast<uint32_t*>(&s.exps[ntile % TA_RING][1][pw * RPW + lane % GPT * 4u]) = ve & ex_mask;
                     }
                     __syncwarp();
                     if (lane == 0u) mbar_arrive(smem_u32(&s.exp_full[ntile % TA_RING]));
-                    place_all(next);   // of tile t + 1
-                    next = look_up(t + 2u);
+                    if (++j == CT) {   // tile t + 1 begins a chunk
+                        place(next);
+                        request_scales();
+                        next = look_up(t + 1u + CT);
+                        j = 0;
+                    }
+                    aim(t + 1u);
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         ok = ok && take_slot();
@@ -1025,7 +1038,6 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                         next_slot();
                         if (kv == 0) {
                             request(c.k, kraw);
-                            request_scales();
                         } else {
                             request(c.v, vraw);
                         }
