@@ -1335,18 +1335,24 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
             ta_named_sync(3u, NG * 128u);
             if (bad && me == 0u) s.bad[npiece % TA_RING] = 0u;
             if (!p.two) {
-                mm = -INFINITY;
-                for (uint32_t g = 0; g < NG * 128u; g += 128u)
-                    for (uint32_t j = r; j < 128u; j += R) mm = fmaxf(mm, s.ml[0][g + j]);
+                constexpr uint32_t PARTS = NG * 4;   // fewer where a row has fewer copies
+                float mk[PARTS], lk[PARTS];
+#pragma unroll
+                for (uint32_t k = 0; k < PARTS; ++k) {
+                    const uint32_t at = k / 4u * 128u + k % 4u * R + r;
+                    const bool is = k % 4u < p.split;
+                    mk[k] = is ? s.ml[0][at] : -INFINITY;
+                    lk[k] = is ? s.ml[1][at] : 0.f;
+                }
+                mm = mk[0];
+#pragma unroll
+                for (uint32_t k = 1; k < PARTS; ++k) mm = fmaxf(mm, mk[k]);
                 ll = 0.f;
-                for (uint32_t g = 0; g < NG * 128u; g += 128u)
-                    for (uint32_t j = r; j < 128u; j += R) {
-                        const float mk = s.ml[0][g + j];
-                        if (mk > -INFINITY) ll += s.ml[1][g + j] * ta_exp2(mk - mm);
-                    }
+#pragma unroll
+                for (uint32_t k = 0; k < PARTS; ++k) ll += mk[k] > -INFINITY ? lk[k] * ta_exp2(mk[k] - mm) : 0.f;
             }
             const bool whole = p.slot == ~0u, valid = r < p.rows;
-            const uint32_t gr = p.row0 + r, tok = gr / a.G, head = p.h * a.G + gr - tok * a.G;
+            const uint32_t tok = row.i, head = p.h * a.G + p.row0 + r - tok * a.G;
             if (valid && (p.two || me == r)) {
                 if (whole) {
                     if (a.lse) a.lse[(size_t)(p.q.r0 + tok) * a.nq + head] = ll > 0.f || ll != ll ? (mm + log2f(ll)) * 0.6931471805599453f : -INFINITY;
@@ -1370,10 +1376,11 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                 f[k] = s.ml[0][w] == -INFINITY ? 0.f : ta_exp2(s.ml[0][w] - mm) * s.ml[2][w] * norm;
             }
             const uint32_t first_o = pair ? lane_base + Cfg::O_COL : o_at, c_end = pair ? (grp + 1u) * (HD / 2) : (uint32_t)HD;
-            // (the exchange between copies: 16 columns of a thread side by side, their fours exchanged so that eight threads' lie in all banks)
-            float* const xs = s.x + me * 16u;
-            const float* const xr = s.x + (grp * 128u + r) * 16u;
-            const uint32_t turn = r >> 1 & 3u;   // of all copies of the row: R is a multiple of eight
+            // The exchange between copies: `wide` columns of every valid row's copies at a time, as many as the group's 8 KB hold; their fours are
+            // exchanged so that eight threads' lie in all banks.  (Head size 64: a group has 32 columns.)
+            const uint32_t wide = p.rows <= 8u && HD > 64 ? 64u : p.rows <= 16u ? 32u : 16u, turn = wide == 16u ? r >> 1 & 3u : r & 7u;
+            float* const xs = s.x + grp * 2048u + (share * (wide == 16u ? R : p.rows) + r) * wide;
+            const float* const xr = s.x + grp * 2048u + r * wide;
 #pragma unroll 1
             for (uint32_t c0 = pair ? grp * (HD / 2) : 0u; c0 < c_end; c0 += 16u) {
                 uint32_t x[16];
@@ -1421,24 +1428,28 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
                     }
                     continue;
                 }
-                ta_named_sync(1u + grp, 128u);   // the buffer's last readers are done
+                const uint32_t in = c0 % wide;
+                if (in == 0u) ta_named_sync(1u + grp, 128u);   // the buffer's last readers are done
+                if (valid)
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(xs + ((j / 4 ^ turn) << 2)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                    for (uint32_t j = 0; j < 16u; j += 4u) *reinterpret_cast<float4*>(xs + (((in + j) / 4u ^ turn) << 2)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                if (in + 16u < wide) continue;
                 ta_named_sync(1u + grp, 128u);
                 if (valid) {
-                    const uint32_t cols = 16u / p.split;
+                    const uint32_t cols = wide / p.split, next = (wide == 16u ? R : p.rows) * wide;
                     for (uint32_t j = share * cols; j < (share + 1u) * cols; j += 4u) {
                         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                        for (uint32_t k = 0; k < 128u; k += R) {
-                            const float4 z = *reinterpret_cast<const float4*>(xr + k * 16u + ((j / 4u ^ turn) << 2));
-                            y.x += z.x;
-                            y.y += z.y;
-                            y.z += z.z;
-                            y.w += z.w;
-                        }
-                        if (whole) *reinterpret_cast<uint2*>(out + c0 + j) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-                        else *reinterpret_cast<float4*>(rec + c0 + j) = y;
+#pragma unroll
+                        for (uint32_t k = 0; k < 4u; ++k)
+                            if (k < p.split) {
+                                const float4 z = *reinterpret_cast<const float4*>(xr + k * next + ((j / 4u ^ turn) << 2));
+                                y.x += z.x;
+                                y.y += z.y;
+                                y.z += z.z;
+                                y.w += z.w;
+                            }
+                        if (whole) *reinterpret_cast<uint2*>(out + c0 - in + j) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+                        else *reinterpret_cast<float4*>(rec + c0 - in + j) = y;
                     }
                 }
             }
