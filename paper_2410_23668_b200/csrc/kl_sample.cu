@@ -137,6 +137,20 @@ struct Sampler {
         }
         for (; i < i1; ++i) f(x[i], i);
     }
+    // ... for those of it that `in` names: found first, so that a warp does f as often as its fullest run has some
+    template <class In, class F>
+    __device__ __forceinline__ void over_some(In&& in, F&& f) const {
+        for (uint32_t i = i0; i < i1; i += 32u) {
+            uint32_t todo = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < 32u; ++j)
+                if (i + j < i1 && in(x[i + j])) todo |= 1u << j;
+            for (; todo; todo &= todo - 1u) {
+                const uint32_t a = i + __ffs(todo) - 1u;
+                f(x[a], a);
+            }
+        }
+    }
     __device__ __forceinline__ double block_sum(double v) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -808,9 +822,9 @@ __global__ void __launch_bounds__(SP_THREADS, 2) kl_sample_kernel(const SampleAr
             });
         }
     } else {
-        q.over_run([&](float x, uint32_t i) {
-            if (x >= least) mine += weight(x, i);
-        });
+        auto add = [&](float x, uint32_t i) { mine += weight(x, i); };
+        if (least > -INFINITY) q.over_some([&](float x) { return x >= least; }, add);
+        else q.over_run(add);
     }
     q.block_scan(mine, before, own);
     const uint32_t half = q.turn++ & 1u;
