@@ -546,7 +546,7 @@ __device__ __forceinline__ uint4 ta_load_if(bool yes, const void* p) {
 // A sequence of the call.
 struct TaSeq {
     uint32_t T, r0, base, len, lo;   // new tokens, their first row, cached positions, positions in all, first position of the window
-    uint32_t tiles, head_tiles, first_tile, runs;   // key tiles: head_tiles from position 0 on (sinks), the others from first_tile on; runs of UR rows
+    uint32_t tiles, head_tiles, first_tile, halves; // key tiles: head_tiles from position 0 on (sinks), the others from first_tile on; runs of 128 rows
 };
 template <int NK, int UR>
 __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, uint32_t s) {
@@ -573,12 +573,33 @@ __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, u
     q.first_tile = q.lo / NK;
     q.head_tiles = q.lo ? min((min(a.sinks, q.base) + NK - 1u) / NK, q.first_tile) : 0u;
     q.tiles = q.T ? q.head_tiles + (q.len + NK - 1u) / NK - q.first_tile : 0u;
-    q.runs = (uint32_t)(((uint64_t)q.T * a.G + UR - 1u) / UR);
+    q.halves = (uint32_t)(((uint64_t)q.T * a.G + 127u) / 128u);
     return q;
 }
-__device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.runs; }
+// What the shares are counted in: a tile of a unit of up to 128 rows is one, of more than 128 two -- it takes twice the matrix
+// instructions and exponentials (24 trees of 1 .. 32 tokens, eight query heads to a kv head, 305 us; every tile one: 350).
+__device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.halves; }
+// The unit that `off` lies in, counted from the sequence's first.
+struct TaUnit {
+    uint32_t h, row0, rows, twice;   // kv head, first row, rows, whether a tile counts two
+    uint64_t begin;                  // in the same count as `off`
+    __device__ __forceinline__ uint32_t tile_at(uint64_t at) const { return (uint32_t)(at - begin + twice >> twice); }   // first tile that begins at `at` or behind it
+};
+template <int UR>
+__device__ __forceinline__ TaUnit ta_unit(const TreeArgs& a, const TaSeq& q, uint64_t off) {
+    TaUnit u;
+    const uint64_t k = pg_div(off, q.tiles);
+    u.h = (uint32_t)pg_div(k, q.halves);
+    uint32_t half = (uint32_t)(k - (uint64_t)u.h * q.halves);
+    if (UR == 256) half &= ~1u;
+    u.row0 = half * 128u;
+    u.rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - u.row0);
+    u.twice = u.rows > 128u ? 1u : 0u;
+    u.begin = ((uint64_t)u.h * q.halves + half) * q.tiles;
+    return u;
+}
 
-// Equal shares of the list; border(b) is the first tile of block b's.
+// Equal shares of the list; block b's begins at border(b), with the first tile that begins there or behind it.
 struct TaShares {
     uint64_t per;
     uint32_t rest, blocks;
@@ -611,28 +632,30 @@ struct TaIter {
         q = ta_seq<NK, UR>(c, a, s);
     }
     __device__ __forceinline__ bool next(const PagedView& c, const TreeArgs& a, TaPiece& p) {
-        if (!left) return false;
-        while (off >= ta_work(c, q)) {
-            off -= ta_work(c, q);
-            if (++s >= c.n_seqs) return false;
-            q = ta_seq<NK, UR>(c, a, s);
+        for (;;) {   // (the last half of a tile that counts two is nobody's)
+            if (!left) return false;
+            while (off >= ta_work(c, q)) {
+                off -= ta_work(c, q);
+                if (++s >= c.n_seqs) return false;
+                q = ta_seq<NK, UR>(c, a, s);
+            }
+            const TaUnit u = ta_unit<UR>(a, q, off);
+            const uint64_t end = min(off + left, u.begin + ((uint64_t)q.tiles << u.twice));
+            p.q = q;
+            p.t0 = u.tile_at(off);
+            p.t1 = u.tile_at(end);
+            p.h = u.h;
+            p.row0 = u.row0;
+            p.rows = u.rows;
+            p.two = p.rows > 128u;
+            p.split = p.rows <= 32u && NK == 128 ? 4u : p.rows <= 64u ? 2u : 1u;   // a copy takes 32 keys or more
+            p.R = 128u / p.split;
+            p.slot = p.t0 == 0u && p.t1 == q.tiles ? ~0u : 2u * blockIdx.x + (begun ? 1u : 0u);
+            begun = true;
+            left -= end - off;
+            off = end;
+            if (p.t0 < p.t1) return true;
         }
-        const uint64_t u = pg_div(off, q.tiles);
-        p.q = q;
-        p.t0 = (uint32_t)(off - u * q.tiles);
-        p.h = (uint32_t)pg_div(u, q.runs);
-        const uint32_t run = (uint32_t)(u - (uint64_t)p.h * q.runs);
-        p.row0 = run * UR;
-        p.t1 = (uint32_t)min((uint64_t)q.tiles, p.t0 + left);
-        p.rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - p.row0);
-        p.two = p.rows > 128u;
-        p.split = p.rows <= 32u && NK == 128 ? 4u : p.rows <= 64u ? 2u : 1u;   // a copy takes 32 keys or more
-        p.R = 128u / p.split;
-        p.slot = p.t0 == 0u && p.t1 == q.tiles ? ~0u : 2u * blockIdx.x + (begun ? 1u : 0u);
-        begun = true;
-        off += p.t1 - p.t0;
-        left -= p.t1 - p.t0;
-        return true;
     }
 };
 __device__ __forceinline__ uint32_t ta_tile_pos(const TaSeq& q, uint32_t t, uint32_t nk) {   // first position of tile t
@@ -1488,24 +1511,26 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
         if (++s >= c.n_seqs) return;
         q = ta_seq<NK, UR>(c, a, s);
     }
-    const uint64_t u = pg_div(off, q.tiles), begin = g - (off - u * q.tiles), end = begin + q.tiles;
-    const uint32_t first = b - 1u, h = (uint32_t)pg_div(u, q.runs), run = (uint32_t)(u - (uint64_t)h * q.runs);
-    if (g == begin || shares.border(first) > begin) return;
+    const TaUnit u = ta_unit<UR>(a, q, off);
+    const uint64_t begin = g - (off - u.begin), end = begin + ((uint64_t)q.tiles << u.twice);
+    const uint32_t first = b - 1u;
+    if (g == begin || shares.border(first) > begin || u.tile_at(off) == q.tiles) return;   // (the last: the first block has the whole unit)
     const uint32_t first_slot = 2u * first + (shares.border(first) < begin ? 1u : 0u);
     uint32_t last = min(blocks - 1u, (uint32_t)pg_div(end * blocks - 1u, (uint32_t)min(work, (uint64_t)0xffffffffu)));   // nearly: the last block whose share begins before the unit's end
     last = max(last, b);
     while (last > b && shares.border(last) >= end) --last;
     while (last + 1u < blocks && shares.border(last + 1u) < end) ++last;
-    const uint32_t rows = (uint32_t)min((uint64_t)UR, (uint64_t)q.T * a.G - (uint64_t)run * UR);
-    for (uint32_t r = blockIdx.y * NW + warp; r < rows; r += gridDim.y * NW) {
-        auto slot_of = [&](uint32_t k) { return k == first ? first_slot : 2u * k; };
-        auto holds = [&](uint32_t k) { return shares.border(k) < shares.border(k + 1u); };   // blocks without work left nothing
+    auto slot_of = [&](uint32_t k) { return k == first ? first_slot : 2u * k; };
+    auto tile_at = [&](uint64_t at) { return u.tile_at(min(max(at, begin), end) - begin + u.begin); };
+    auto holds = [&](uint32_t k) { return tile_at(shares.border(k)) < tile_at(shares.border(k + 1u)); };   // blocks without a tile left nothing
+    const bool mine = first + lane <= last && holds(first + lane);   // of the first 32
+    for (uint32_t r = blockIdx.y * NW + warp; r < u.rows; r += gridDim.y * NW) {
         float m = -INFINITY, l = 0.f, sum[COLS];
 #pragma unroll
         for (int j = 0; j < COLS; ++j) sum[j] = 0.f;
         for (uint32_t k0 = first; k0 <= last; k0 += 32u) {   // 32 parts at a time, each lane with the reference and sum of one
             float2 ml = make_float2(-INFINITY, 0.f);
-            if (k0 + lane <= last && holds(k0 + lane)) ml = a.part_ml[(size_t)slot_of(k0 + lane) * TA_RECORD + r];
+            if (k0 == first ? mine : k0 + lane <= last && holds(k0 + lane)) ml = a.part_ml[(size_t)slot_of(k0 + lane) * TA_RECORD + r];
             float mx = fmaxf(m, ml.x);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -1549,7 +1574,7 @@ __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(c
                     for (int j = 0; j < COLS; ++j) sum[j] += wk[z] * x[z][j];
             }
         }
-        const uint32_t gr = run * UR + r, tok = gr / a.G, head = h * a.G + gr - tok * a.G;
+        const uint32_t gr = u.row0 + r, tok = gr / a.G, head = u.h * a.G + gr - tok * a.G;
         const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
         if (a.lse && lane == 0u) a.lse[(size_t)(q.r0 + tok) * a.nq + head] = l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         uint32_t* out = reinterpret_cast<uint32_t*>(a.out + (int64_t)(q.r0 + tok) * a.out_stride + ((size_t)head * HD + lane * COLS) * 2u);

@@ -144,3 +144,18 @@ def test_a_long_run_of_tokens(e4m3, hd, window):
     table = ref.scattered_table([b + t for b, t in seqs], 16, 140, seed=21)
     q = torch.randn(1900, 2, hd, generator=torch.Generator().manual_seed(22)).to(torch.bfloat16).cuda()
     check_tree(c, q, seqs, table, "causal", window=window, sinks=4 if window else 0)
+
+
+@pytest.mark.parametrize("e4m3,hd,nq,seed", [(False, 128, 8, 0), (True, 128, 8, 1), (False, 64, 16, 2), (True, 256, 8, 3), (False, 128, 12, 4)])
+def test_units_of_one_and_of_two_runs_of_rows(e4m3, hd, nq, seed):
+    """Tokens times heads on either side of 128 and 256, next to one another, so that shares begin inside units of either kind."""
+    g = np.random.default_rng(seed)
+    G = nq // 2
+    around = [max(1, x // G + d) for x in (32, 64, 128, 256, 384) for d in (-1, 0, 1)]
+    seqs = [(int(g.integers(0, 1500)), t) for t in around] + [(1900, 1), (0, 1), (-1, 4), (640, 300 // G + 1)]
+    lengths = [max(b, 0) + t for b, t in seqs]
+    n_pages = sum(-(-x // 16) for x in lengths) + 1
+    c = ref.Cache(n_pages, 2, 16, hd, e4m3, seed=30 + seed)
+    table = ref.scattered_table(lengths, 16, n_pages, seed=31)
+    q = torch.randn(sum(t for _, t in seqs), nq, hd, generator=torch.Generator().manual_seed(32)).to(torch.bfloat16).cuda()
+    check_tree(c, q, seqs, table, "tree", seed=33)
