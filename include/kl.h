@@ -515,7 +515,7 @@ kl_status kl_paged_tree_workspace_bytes(const kl_paged_cache* cache, uint32_t n_
  * q_d and out_d: bf16 [n_rows][n_q_heads][head_dim] (KL_F32: KL_ERR_UNSUPPORTED_SHAPE), rows q_row_stride and out_row_stride elements
  * apart; scale <= 0: 1 / sqrt(head_dim); lse_d as in kl_paged_attention, [n_rows][n_q_heads].  A token that sees nothing gets zeros, and
  * -inf; rows that belong to no sequence or to an empty slot are left as they were.  Any number of new tokens and any group size; a
- * cached row is read once for every 128 (token, query head) pairs of its kv head.  What a token does not see has no part in its result,
+ * cached row is read once for every 256 (head size 256: 128) (token, query head) pairs of its kv head.  What a token does not see has no part in its result,
  * whatever it holds; a token that sees an infinity or NaN gets no number in the columns it reaches.
  * Scores, the softmax and all sums are held in 32 bits; in the second product a probability takes part with 15 bits (KL_KV_BF16) or 11
  * (KL_KV_E4M3; fewer for positions whose probability times value scale is below 2^-24 of the largest value scale of the sequence, and

@@ -64,6 +64,11 @@ struct RtPiece {
 // (i, i + hd / 2) that turns together is in one lane's hands.  Cosines and sines of RT_ROWS rows are computed once for all heads.
 // Angles, cosines, sines and the two products of a key are held in 64 bits and the key is rounded once: a scale byte is a whole
 // number, and whether a key passes a border between two scales or codes is a comparison that 32 bits get wrong now and then.
+//
+// What bounds it: for few rows the chain of look-ups (position, page, rows) and the 64-bit sines, about 2 us of them (one row of eight
+// kv and 32 query heads 4.4 us; 32 sequences of eight rows 7.8); for many the instructions of turning, scaling and packing with one block
+// on an SM (8191 rows to e4m3 with 32 query heads 60 us, 173 MB in all and hence 26 at the copy rate).  All heads of a page in one block
+// compute the angles once instead of per head; a row's loads are requested while the one before is worked on (66 us without).
 template <class T, int HD, bool FP8, int RT_THREADS>
 __global__ void __launch_bounds__(RT_THREADS, 1) kl_paged_append_rotated_kernel(const PagedView c, const PagedRows rows, const RotateArgs a) {
     constexpr uint32_t LANES = HD / 16, GROUPS = RT_THREADS / LANES, HALF = HD / 2;
@@ -334,19 +339,20 @@ constexpr size_t rt_smem_bytes() {
 //
 // For a (sequence, kv head) the queries of all new tokens and all G query heads of the group are rows of one matrix product with
 // the cached keys, 128 at a time: S = Q K^T on the tensor cores (accumulators in TMEM), the softmax on S by the threads that own the
-// rows, O += P V on the tensor cores again, with P read from TMEM.  A cached row thus leaves memory once for 128 (token, head) pairs.
+// rows, O += P V on the tensor cores again, with P read from TMEM.  A cached row thus leaves memory once for 128 (token, head) pairs, or 256.
 //
 // One pass over the keys with a running reference m of the exponent and the running sum l: p = 2^(s - m), l += p, O += p v; m is
-// raised, and l and O scaled, only when a score exceeds it by TA_RAISE binades -- until then p is larger than one, which 32-bit sums and
+// raised, and l and O scaled, only when a score exceeds it by TaCfg::RAISE binades -- until then p is larger than one, which 32-bit sums and
 // the 16-bit types of P bear.
 //
-// The work of a call is one list of key tiles: sequences, kv heads, runs of 128 rows, tiles; every block of the grid (one per SM) takes an
-// equal share of it.  A unit (sequence, head, run of rows) cut by the border between two blocks leaves its parts (O, m, l) in the
+// The work of a call is one list of key tiles: sequences, kv heads, runs of up to 256 rows, tiles; every block of the grid (one per SM) takes
+// an equal share of it.  A unit (sequence, head, run of rows) cut by the border between two blocks leaves its parts (O, m, l) in the
 // workspace, and kl_paged_tree_merge_kernel joins them in order.
 //
-// Types.  bf16 caches: Q, K, V as they are, P as two bf16 parts (15 bits of it), both multiplied with V.  e4m3 caches: K's codes as
-// bf16 (exact), its scales applied to the scores in 32 bits; V's codes as f16 (exact), its scales applied to P, which enters as one f16
-// (11 bits) scaled by a power of two common to all columns so far (the largest value scale seen).
+// Types.  bf16 caches: Q, K, V as they are, P as two bf16 parts (15 bits of it), both multiplied with V: one part alone would cost
+// results 8 bits of every probability.  e4m3 caches: Q as f16, a row divided by a power of two (exact but for elements below 2^-28 of its
+// largest), K's codes as f16 (exact), its scales applied to the scores in 32 bits; V's codes as f16 (exact), its scales applied to P, which
+// enters as one f16 (11 bits) scaled by a power of two common to all columns so far (the largest value scale seen).
 //
 // Two streams.  There are two score buffers and two groups of four softmax warps, each with a reference, a sum and an O of its own.  Where a
 // unit has at most 128 rows, the groups take its tiles in turn and are joined at its end; where it has up to 256, each group
@@ -354,6 +360,17 @@ constexpr size_t rt_smem_bytes() {
 // to agree on anything, and a tile's keys and values serve up to 256 rows.  With at most 64 (32) rows each row lies in TMEM's lanes
 // twice (four times), and a copy takes one half (quarter) of the tile's keys -- P is zero elsewhere -- so that all warps share a
 // single row's exponentials.  (Head size 256: O fills half of TMEM, one group of warps takes the buffers in turn, 128 rows.)
+//
+// Roles: 4 or 8 softmax warps (a thread owns a row), a warp that issues Q K^T, one that issues P V (a lone warp needs some five cycles per
+// instruction and one matrix instruction 64: one warp for both fell behind), 4 (bf16: asynchronous copies) or 8 (e4m3: widened in
+// registers) producers.
+//
+// What bounds it (head size 128, 8 kv heads).  Few rows over a bf16 cache: memory (32 x 8 tokens, four heads to a kv head, over 4096
+// positions 123 us for 542 MB, 4.4 TB/s).  Many rows: the softmax -- with both groups at work 128 columns of a warp take some 4100 cycles
+// beside the 3100 that a tile's matrix instructions take (24 trees of up to 32 tokens, eight heads, 308 us; the tensor cores 48 % busy;
+// score buffers of 64 keys, two to a group, so that Q K^T runs ahead of the softmax: 348 where this form took 350, and slower elsewhere).
+// Few rows over an e4m3 cache: the latency of a tile's way through all roles with two tiles under way (32 single tokens, window 2044: 84 us for
+// 121 MB).  Small calls: the chain of look-ups, one tile and the join (five tokens over 700 positions 20.7 us).
 
 struct TreeArgs {
     const int32_t* row_starts;      // [n_seqs + 1] or null: one row per sequence
@@ -577,7 +594,7 @@ __device__ __forceinline__ TaSeq ta_seq(const PagedView& c, const TreeArgs& a, u
     return q;
 }
 // What the shares are counted in: a tile of a unit of up to 128 rows is one, of more than 128 two -- it takes twice the matrix
-// instructions and exponentials (24 trees of 1 .. 32 tokens, eight query heads to a kv head, 305 us; every tile one: 350).
+// instructions and exponentials (24 trees of 1 .. 32 tokens, eight query heads to a kv head, 308 us; every tile one: 350).
 __device__ __forceinline__ uint64_t ta_work(const PagedView& c, const TaSeq& q) { return (uint64_t)q.tiles * c.nkv * q.halves; }
 // The unit that `off` lies in, counted from the sequence's first.
 struct TaUnit {
@@ -1488,7 +1505,8 @@ __global__ void __launch_bounds__(TaCfg<HD, FP8>::NW * 32, 1) kl_paged_tree_kern
 }
 
 // Joins the parts of the units that borders between blocks cut: block (b - 1, y) of the grid has border b, and does nothing unless it is the
-// first border inside its unit.  A warp takes a row: weights 2^(m - largest m), sums in the order of the parts.
+// first border inside its unit.  A warp takes a row: weights 2^(m - largest m), sums in the order of the parts.  Bound by latency: prefix sums
+// over the sequences, look-up of the unit, then a row's parts, four under way; its launch overlaps the main kernel's end.
 constexpr int TA_MERGE_THREADS = 128;
 template <int HD, int NK, int UR>
 __global__ void __launch_bounds__(TA_MERGE_THREADS) kl_paged_tree_merge_kernel(const PagedView c, const TreeArgs a, const uint32_t blocks) {
