@@ -511,7 +511,8 @@ kl_status kl_paged_tree_workspace_bytes(const kl_paged_cache* cache, uint32_t n_
  *   - of the sequence's new tokens, those j whose bit is set in the row's mask (mask_d: [n_rows][mask_words] words of 32 bits, bit j % 32
  *     of word j / 32; bits behind the sequence's last token, and words that are not there, name nothing).  Without mask_d: all j <= i, with a
  *     window those with i - j < window.
- * window = W and one row per sequence is a decode step with a sliding window and n_sinks first positions that stay visible.
+ * window = W and one row per sequence is a decode step with a sliding window and n_sinks first positions that stay visible (row_starts_d ==
+ * NULL says so to the host, which then takes the kernel of kl_paged_attention: half the time for up to eight query heads to a kv head).
  * q_d and out_d: bf16 [n_rows][n_q_heads][head_dim] (KL_F32: KL_ERR_UNSUPPORTED_SHAPE), rows q_row_stride and out_row_stride elements
  * apart; scale <= 0: 1 / sqrt(head_dim); lse_d as in kl_paged_attention, [n_rows][n_q_heads].  A token that sees nothing gets zeros, and
  * -inf; rows that belong to no sequence or to an empty slot are left as they were.  Any number of new tokens and any group size; a

@@ -105,9 +105,9 @@ kl_status launch_attn(const PagedView& v, const PagedAttn& a, int blocks, PagedO
 
 // Both ways into the attention kernels.
 kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int q_type, uint32_t out_mode,
-                        int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale_log2, uint32_t window,
+                        int64_t q_row_stride, int64_t out_row_stride, uint32_t n_q_heads, float scale_log2, uint32_t window, uint32_t n_sinks,
                         const int32_t* selected_d, uint32_t n_select, float* lse_d, void* workspace_d, size_t workspace_bytes,
-                        int32_t* status_d, uint64_t* launches, PagedOrder order) {
+                        int32_t* status_d, uint64_t* launches, PagedOrder order, bool leave_empty = false) {
     if ((selected_d != nullptr) != (n_select != 0) || n_select > 0x7fffffffu) return KL_ERR_INVALID_ARG;
     const AttnSpace sp = attn_space(cache->head_dim);
     if (!workspace_d || ((uintptr_t)workspace_d & 255u) || workspace_bytes < sp.bytes) return KL_ERR_INVALID_ARG;
@@ -126,6 +126,8 @@ kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     a.HT = (a.G + 7) / 8;
     a.scale_log2 = scale_log2;
     a.window = window;
+    a.sinks = n_sinks;
+    a.leave_empty = leave_empty;
     a.selected = selected_d;
     a.n_select = n_select;
     a.lse = lse_d;
@@ -138,6 +140,7 @@ kl_status run_attention(const kl_paged_cache* cache, const kl_paged_seqs* seqs, 
     uint64_t most = (uint64_t)seqs->table_pages * cache->page_size;
     if (selected_d && (uint64_t)n_select * cache->page_size < most) most = (uint64_t)n_select * cache->page_size;
     if (!selected_d && window && (uint64_t)window + 64 < most) most = (uint64_t)window + 64;   // a window may begin inside a tile
+    if (!selected_d && window && n_sinks) most += (uint64_t)n_sinks + 64;
     const bool many = (uint64_t)seqs->n_seqs * cache->n_kv_heads * a.HT >= (uint64_t)blocks;
     a.whole_pairs = most <= (uint64_t)(many ? PA_WHOLE_MANY : PA_WHOLE_FEW) * attn_tile(v, out_mode);
     if (launches) *launches = a.whole_pairs ? 1 : 2;
@@ -208,8 +211,17 @@ kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_se
                                   uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
                                   size_t workspace_bytes, int32_t* status_d, uint64_t* launches, PagedOrder order) {
     const int64_t width = (int64_t)n_q_heads * cache->head_dim;
-    return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, selected_d, n_select, nullptr, workspace_d,
+    return run_attention(cache, seqs, q_d, operand_d, KL_F32, PA_OPERAND, width, width, n_q_heads, 1.f, 0, 0, selected_d, n_select, nullptr, workspace_d,
                          workspace_bytes, status_d, launches, order);
+}
+size_t paged_attention_bytes(uint32_t head_dim) { return attn_space(head_dim).bytes; }
+
+kl_status paged_attention_sinks(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int64_t q_row_stride, int64_t out_row_stride,
+                                uint32_t n_q_heads, float scale_log2, uint32_t window, uint32_t n_sinks, float* lse_d, void* workspace_d,
+                                size_t workspace_bytes, int32_t* status_d, PagedOrder order) {
+    const uint32_t most = seqs->table_pages * cache->page_size;   // (below 2^31)
+    return run_attention(cache, seqs, q_d, out_d, KL_BF16, PA_BF16, q_row_stride, out_row_stride, n_q_heads, scale_log2, window, n_sinks < most ? n_sinks : most,
+                         nullptr, 0, lse_d, workspace_d, workspace_bytes, status_d, nullptr, order, true);
 }
 }  // namespace kl
 
@@ -271,7 +283,7 @@ kl_status kl_paged_attention(const kl_paged_cache* cache, const kl_paged_seqs* s
     if (!(scale < INFINITY)) return KL_ERR_INVALID_ARG;
     const float scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
     return run_attention(cache, seqs, q_d, out_d, q_type, q_type == KL_F32 ? PA_F32 : PA_BF16, q_row_stride, out_row_stride, n_q_heads, scale_log2,
-                         window, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, nullptr, {stream, true});
+                         window, 0, selected_d, n_select, lse_d, workspace_d, workspace_bytes, status_d, nullptr, {stream, true});
 }
 
 }  // extern "C"

@@ -928,9 +928,11 @@ struct PagedAttn {
     uint32_t nq, G, HT;             // G query heads per kv head, in HT tiles of at most eight
     float scale_log2;               // scale * log2(e)
     uint32_t window;                // 0: none
+    uint32_t sinks;                 // positions from 0 on that a window does not hide
     const int32_t* selected;        // [n_seqs][nkv][n_select] or null
     uint32_t n_select;
     float* lse;                     // or null
+    uint32_t leave_empty;           // 1: rows of sequences without a position stay as they were
     uint32_t whole_pairs;           // 1: no pair is shared between blocks (and kl_paged_merge_kernel does not follow)
     // workspace: partial results, one record = [8 heads][hd] sums and [8 heads] (maximum, sum)
     float *part, *part_ml;          // [blocks][2]: the pair that began in an earlier block, the pair that goes on in the next one
@@ -1037,13 +1039,15 @@ constexpr uint32_t PA_WHOLE_FEW = 24, PA_WHOLE_MANY = 64;
 // Positions of sequence s that take part, as tiles.
 struct PaSeq {
     uint32_t len, lo;   // positions [lo, len)
-    uint32_t t0, nt;    // tiles [t0, t0 + nt) of its (virtual) positions
+    uint32_t t0, nt;    // nt tiles of its (virtual) positions: the first `head`, then those from t0 on
+    uint32_t head;      // (first positions in front of a window)
     uint32_t listed;    // entries of the page list that are looked at
 };
 template <uint32_t TP>
 __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, uint32_t len) {
     PaSeq q;
     q.len = len;
+    q.head = 0;
     q.lo = a.window && len > a.window ? len - a.window : 0u;
     if (a.selected) {
         q.listed = min(a.n_select, (len + c.page - 1u) / c.page);
@@ -1053,6 +1057,10 @@ __device__ __forceinline__ PaSeq pa_seq(const PagedView& c, const PagedAttn& a, 
         q.listed = 0;
         q.t0 = q.lo / TP;
         q.nt = len ? (len + TP - 1u) / TP - q.t0 : 0u;
+        if (q.lo && a.sinks) {
+            q.head = min((min(a.sinks, len) + TP - 1u) / TP, q.t0);
+            q.nt += q.head;
+        }
     }
     return q;
 }
@@ -1119,7 +1127,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
     });
     auto length = [&](uint32_t s) { return s < (uint32_t)PA_LENS ? lens[s] : pg_length(c, s); };
 
-    for (uint32_t s = blockIdx.x; s < n; s += gridDim.x)   // sequences without a position: zeros
+    for (uint32_t s = blockIdx.x; s < n && !a.leave_empty; s += gridDim.x)   // sequences without a position: zeros
         if (length(s) == 0u) {
             for (uint32_t i = tid; i < a.nq * (HD / 2); i += NT) pa_store2(c, a, s, i / (HD / 2), i % (HD / 2) * 2u, 0.f, 0.f);
             for (uint32_t i = tid; i < a.nq; i += NT) pa_store_lse(a, s, i, 0.f, 0.f);
@@ -1190,7 +1198,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
             phys = -1;
             lp = PA_NONE;
             row = 0;
-            const uint32_t u = (iq.t0 + b * TPB) * UPT + lane;
+            const uint32_t vt = b * TPB + lane / UPT, u = (vt < iq.head ? vt : iq.t0 - iq.head + vt) * UPT + lane % UPT;
             uint32_t logical;
             if (a.selected) {
                 const uint32_t upp = c.page / UR, e = u / upp;
@@ -1204,7 +1212,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                 logical = u * UR / c.page;
                 row = u * UR - logical * c.page;
             }
-            if (logical * c.page + row + UR <= iq.lo) return;   // before the window: the page may be gone
+            if (logical * c.page + row + UR <= iq.lo && logical * c.page + row >= a.sinks) return;   // before the window: the page may be gone
             phys = pg_physical(c, is, logical);
             if (phys >= 0) lp = logical * c.page + row;
         };
@@ -1243,10 +1251,12 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                     const int32_t phys = __shfl_sync(0xffffffffu, b_phys, at * UPT + v);
                     const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, at * UPT + v), row = __shfl_sync(0xffffffffu, b_row, at * UPT + v);
                     const int32_t r_lo = (int32_t)iq.lo - (int32_t)lp, r_hi = (int32_t)iq.len - (int32_t)lp;   // rows of the unit that count
-                    full = full && r_lo <= 0 && r_hi >= 16;
+                    const int32_t r_sinks = (int32_t)a.sinks - (int32_t)lp;                                     // ... and those below this one
+                    const bool all = (r_lo <= 0 || r_sinks >= 16) && r_hi >= 16;
+                    full = full && all;
                     const int64_t off = (int64_t)max(phys, 0) * c.page_b + (int64_t)(row + r0) * c.row_b;
                     const uint8_t *ks = ik + off, *vs = iv + off;
-                    if (r_lo <= 0 && r_hi >= 16 && c.row_b == ROW) {   // the usual unit: 16 rows in a row, all of which count
+                    if (all && c.row_b == ROW) {   // the usual unit: 16 rows in a row, all of which count
 #pragma unroll
                         for (int i = 0; i < 16 / RPP; ++i) {
                             pa_copy16(kd + k_at[i % NPAT] + (v * 16 + i * RPP) * ROW, ks + i * RPP * ROW);
@@ -1256,7 +1266,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
 #pragma unroll 1
                         for (int i = 0; i < 16 / RPP; ++i) {
                             const int32_t r = i * RPP + (int32_t)r0;
-                            const bool ok = r >= r_lo && r < r_hi;
+                            const bool ok = (r >= r_lo || r < r_sinks) && r < r_hi;
                             pa_copy16(kd + (v * 16 + r) * ROW + ((ch ^ fk_of(r)) << 4), ks, ok);
                             pa_copy16(vd + (v * 16 + r) * ROW + ((ch ^ fv_of(r)) << 4), vs, ok);
                             ks += (int64_t)RPP * c.row_b;
@@ -1276,7 +1286,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         const int32_t phys = __shfl_sync(0xffffffffu, b_phys, src);
                         const uint32_t lp = __shfl_sync(0xffffffffu, b_lp, src), row = __shfl_sync(0xffffffffu, b_row, src);
                         const int32_t p = (int32_t)lp + (r & 3);
-                        const bool ok = lp != PA_NONE && p >= (int32_t)iq.lo && p < (int32_t)iq.len;
+                        const bool ok = lp != PA_NONE && (p >= (int32_t)iq.lo || p < (int32_t)a.sinks) && p < (int32_t)iq.len;
                         const int64_t off = (int64_t)max(phys, 0) * c.page_b + (int64_t)(row + (r & 3)) * c.row_b;
                         pa_copy16(kd + r * ROW + ((ch ^ fk_of(r)) << 4), ik + off, ok);
                         pa_copy16(vd + r * ROW + ((ch ^ fv_of(r)) << 4), iv + off, ok);
@@ -1289,7 +1299,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
                         pa_copy4(exps + st * EXB + lane / UPT * TP + u * 4, (lane < UPT ? c.ke : c.ve) + eoff, phys >= 0);
                     }
                     if (lane < UPT) lps[st * LPN + lane] = lp;
-                    full = __all_sync(0xffffffffu, lp != PA_NONE && lp >= iq.lo && lp + UR <= iq.len);
+                    full = __all_sync(0xffffffffu, lp != PA_NONE && (lp >= iq.lo || lp + UR <= a.sinks) && lp + UR <= iq.len);
                 }
             }
             whole = full ? whole | 1u << st : whole & ~(1u << st);
@@ -1468,7 +1478,7 @@ __global__ void __launch_bounds__(PaCfg<HD, FP8, EX>::NW * 32, 1) kl_paged_attn_
 #pragma unroll
                 for (int x = 0; x < 2 * NS; ++x) {
                     const uint32_t r = x * 8 + g, lp = lps[st * LPN + r / UR], p = lp + r % UR;
-                    if (lp == PA_NONE || p < cq.lo || p >= cq.len) s[2 * x] = s[2 * x + 1] = -INFINITY;
+                    if (lp == PA_NONE || (p < cq.lo && p >= a.sinks) || p >= cq.len) s[2 * x] = s[2 * x + 1] = -INFINITY;
                 }
             }
             float mx[2] = {s[0], s[1]}, mv[2] = {-INFINITY, -INFINITY};

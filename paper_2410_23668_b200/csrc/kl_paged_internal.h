@@ -28,6 +28,13 @@ kl_status paged_attention_operand(const kl_paged_cache* cache, const kl_paged_se
                                   uint32_t n_q_heads, const int32_t* selected_d, uint32_t n_select, void* workspace_d,
                                   size_t workspace_bytes, int32_t* status_d, uint64_t* launches, PagedOrder order);
 
+// kl_paged_attention of bf16 queries with a window behind which the first n_sinks positions stay visible, after its checks -- rows of
+// empty slots stay as they were --, and the workspace it needs.
+size_t paged_attention_bytes(uint32_t head_dim);
+kl_status paged_attention_sinks(const kl_paged_cache* cache, const kl_paged_seqs* seqs, const void* q_d, void* out_d, int64_t q_row_stride, int64_t out_row_stride,
+                                uint32_t n_q_heads, float scale_log2, uint32_t window, uint32_t n_sinks, float* lse_d, void* workspace_d,
+                                size_t workspace_bytes, int32_t* status_d, PagedOrder order);
+
 // What every operator that touches rows checks of its descriptors.
 kl_status paged_check(const kl_paged_cache* cache, const kl_paged_seqs* seqs);
 
