@@ -159,3 +159,16 @@ def test_units_of_one_and_of_two_runs_of_rows(e4m3, hd, nq, seed):
     table = ref.scattered_table(lengths, 16, n_pages, seed=31)
     q = torch.randn(sum(t for _, t in seqs), nq, hd, generator=torch.Generator().manual_seed(32)).to(torch.bfloat16).cuda()
     check_tree(c, q, seqs, table, "tree", seed=33)
+
+
+@pytest.mark.parametrize("e4m3,hd,nq,page", [(False, 128, 8, 8), (True, 128, 16, 24), (False, 64, 2, 4), (True, 64, 6, 16), (False, 256, 4, 20), (True, 256, 16, 1024)])
+@pytest.mark.parametrize("window,sinks", [(7, 3), (40, 17), (333, 64), (500, 1 << 30)])
+def test_single_tokens_with_first_positions(e4m3, hd, nq, page, window, sinks):
+    """Pages of every kind; windows that begin in the page, the group of rows, the tile of the last first position, and far behind it."""
+    seqs = [(b, 1) for b in (0, 2, 6, 9, 15, 22, 41, 60, 100, 399, 700, 1301)] + [(-1, 1)]
+    lengths = [max(b, 0) + t for b, t in seqs]
+    n_pages = sum(-(-x // page) for x in lengths) + 1
+    c = ref.Cache(n_pages, 2, page, hd, e4m3, seed=40)
+    table = ref.scattered_table(lengths, page, n_pages, seed=41)
+    q = torch.randn(len(seqs), nq, hd, generator=torch.Generator().manual_seed(42)).to(torch.bfloat16).cuda()
+    check_tree(c, q, seqs, table, "causal", window=window, sinks=sinks, single=True)
